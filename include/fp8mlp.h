@@ -347,6 +347,100 @@ typedef struct {
 FP8MLP_API int fp8mlp_gemm_plan(int kind, int64_t M, int64_t N, int64_t K, int sm_count, int with_workspace,
                                 fp8mlp_gemm_plan_t* plan);
 
+/* ---------------------------------------------------------------------------------------------------------------
+ * Many such blocks as the experts of one layer, and the step between backward and Adam.  The paper has neither; both
+ * stand next to what it trains: a router chooses top_k of n_experts blocks for every token, the tokens' rows are
+ * brought into expert order (expert e then owns rows offsets[e] .. offsets[e + 1] - 1, a contiguous input of
+ * fp8mlp_forward), and the experts' outputs are summed with the router's weights.
+ *
+ * Routing of T tokens.  x = logits[t, :] (fp32 or bf16, row stride ld_logits elements, any alignment of its type):
+ *   s   = softmax(x)  or  sigma(x)                                          (fp32)
+ *   c_e = s_e + bias_e                      bias[n_experts] nullable; it takes part in the choice alone
+ *   n_groups > 1: the experts form n_groups groups of neighbours; a group's value is the sum of its group_top (1 or 2)
+ *       largest c; only the top_groups groups of the largest values stay in the choice
+ *   experts[t, :] = the top_k experts of the largest c, largest first      (equal values: the lower index first)
+ *   w_j = scale * s_j / D, D = the sum of the chosen s   (renormalise != 0; w_j = 0 where D is 0)
+ *   w_j = scale * s_j                                    (renormalise == 0)
+ * An expert whose logit is -inf, or whose c is -inf or NaN, is never chosen (a mask is -inf in the logits, an expert
+ * out of service -inf in the bias; a row with a NaN or +inf logit has no softmax).  A token with fewer than top_k
+ * experts to choose from gets experts -1 with weights 0 in the slots that are left; a row without any is all -1.
+ * 1 <= n_experts <= FP8MLP_MAX_EXPERTS, 1 <= top_k <= min(FP8MLP_MAX_TOP_K, n_experts),
+ * 1 <= top_groups <= n_groups <= n_experts, n_experts a multiple of n_groups, top_k <= the experts of top_groups groups. */
+enum { FP8MLP_SCORE_SOFTMAX = 0, FP8MLP_SCORE_SIGMOID = 1 };
+#define FP8MLP_MAX_EXPERTS 1024
+#define FP8MLP_MAX_TOP_K 32
+typedef struct {
+    int32_t n_experts, top_k;
+    int32_t score;                          /* FP8MLP_SCORE_*                                       */
+    int32_t n_groups, top_groups, group_top; /* n_groups = 1: no groups (the other two are then 1)  */
+    int32_t renormalise;
+    float scale;
+} fp8mlp_router;
+/* experts int32 [T, top_k], weights fp32 [T, top_k], both contiguous. */
+FP8MLP_API int fp8mlp_route(const fp8mlp_router* router, int64_t T, const void* logits, int logits_dtype, int64_t ld_logits,
+                            const float* bias, int32_t* experts, float* weights, void* stream);
+/* Gradient of the weights' gradient d_weights [T, top_k] with respect to the logits, for the experts that the forward
+ * chose (the choice itself has no gradient, the bias none either); r_j = s_j / D, chosen experts j:
+ *   renormalise, softmax: dx_j = scale r_j (dw_j - sum_i dw_i r_i)            other experts 0
+ *   renormalise, sigmoid: the same times (1 - s_j)                            other experts 0
+ *   plain, sigmoid:       dx_j = scale dw_j s_j (1 - s_j)                     other experts 0
+ *   plain, softmax:       dx_e = s_e (scale dw_e - sum_j scale dw_j s_j)      dw_e = 0 for those not chosen
+ * d_logits has the type of the logits, row stride ld_d_logits, and is overwritten.  Slots with an expert outside
+ * 0 .. n_experts - 1 are skipped (their dw is not used); a row without any gets zeros. */
+FP8MLP_API int fp8mlp_route_backward(const fp8mlp_router* router, int64_t T, const void* logits, int logits_dtype,
+                                     int64_t ld_logits, const int32_t* experts, const float* d_weights, void* d_logits,
+                                     int64_t ld_d_logits, void* stream);
+/* Balance without a loss term: bias_e += rate * sign(mean - counts_e), mean = the sum of the counts / n_experts. */
+FP8MLP_API int fp8mlp_route_update_bias(int n_experts, const int32_t* counts, float rate, float* bias, void* stream);
+
+/* Where every slot's row goes: rows[t, j] = the row of token t's slot j in expert order (by expert, then by token, then
+ * by slot: the order is a function of `experts` alone), -1 for an unused slot (an expert outside 0 .. n_experts - 1).
+ * counts[e] = rows of expert e;  offsets[n_experts + 1] = where they begin, offsets[n_experts] = their sum.
+ * T * top_k < 2^31. */
+FP8MLP_API int fp8mlp_dispatch_plan(int64_t T, int top_k, int n_experts, const int32_t* experts, int32_t* counts,
+                                    int32_t* offsets, int32_t* rows, void* stream);
+/* xe[rows[t, j], :] = x[t, :].  dtype FP8MLP_BF16 or FP8MLP_F32; x has row stride ld_x (elements), xe is contiguous,
+ * [n_rows, d].  A slot whose row is outside 0 .. n_rows - 1 writes nothing; rows that no slot names keep what they held.
+ * Its gradient is fp8mlp_combine of the rows' gradients without weights. */
+FP8MLP_API int fp8mlp_dispatch(int64_t T, int top_k, int64_t d, int dtype, const void* x, int64_t ld_x, const int32_t* rows,
+                               void* xe, int64_t n_rows, void* stream);
+/* y[t, :] = sum_j weights[t, j] ye[rows[t, j], :]  (fp32 sum in the order of the slots, rounded once), weights fp32
+ * [T, top_k], null = 1.  Slots whose row is outside 0 .. n_rows - 1 add nothing; a token without any gets zeros. */
+FP8MLP_API int fp8mlp_combine(int64_t T, int top_k, int64_t d, int dtype, const void* ye, int64_t n_rows, const int32_t* rows,
+                              const float* weights, void* y, int64_t ld_y, void* stream);
+/* dye[rows[t, j], :] = weights[t, j] dy[t, :];  d_weights[t, j] = <dy[t, :], ye[rows[t, j], :]>  (fp32).  Slots whose
+ * row is outside 0 .. n_rows - 1: nothing is written to dye, d_weights = 0.  dye contiguous, not ye itself. */
+FP8MLP_API int fp8mlp_combine_backward(int64_t T, int top_k, int64_t d, int dtype, const void* dy, int64_t ld_dy,
+                                       const void* ye, int64_t n_rows, const int32_t* rows, const float* weights, void* dye,
+                                       float* d_weights, void* stream);
+
+/* Global norm of the gradients of any number of tensors, and clipping to it:
+ *   norm = sqrt(sum over all tensors and elements of g^2)  or  max |g|;   coef = min(1, max_norm / (norm + 1e-6))
+ *   norm_coef[0] = norm, norm_coef[1] = coef (device floats);   fp8mlp_clip_grads also: out = g * coef for every element
+ * g fp32 or bf16 (both may occur in one list), contiguous, n >= 0 elements, aligned to its type only; out of the same
+ * type, g itself or a buffer that overlaps no tensor of the list.  The squares are summed in fp64 (no overflow or
+ * underflow short of the fp32 result's) in an order fixed by the list's sizes.  A NaN anywhere makes norm and coef NaN,
+ * an infinity makes norm infinite and coef 0, as the formulas say.  A coefficient of 1 leaves in-place tensors untouched.
+ * workspace: FP8MLP_NORM_WORKSPACE_BYTES of device memory, 16-byte aligned, no state between calls; calls that may
+ * overlap need one each.  max_norm >= 0. */
+enum { FP8MLP_NORM_L2 = 0, FP8MLP_NORM_INF = 1 };
+#define FP8MLP_NORM_WORKSPACE_BYTES 16384
+typedef struct {
+    const void* g;
+    void* out;                 /* fp8mlp_grad_norm does not use it */
+    int64_t n;
+    int32_t dtype;             /* FP8MLP_BF16 or FP8MLP_F32 */
+} fp8mlp_grad_tensor;
+FP8MLP_API int fp8mlp_grad_norm(const fp8mlp_grad_tensor* grads, int count, int norm_kind, float max_norm, float* norm_coef,
+                                void* workspace, void* stream);
+FP8MLP_API int fp8mlp_clip_grads(const fp8mlp_grad_tensor* grads, int count, int norm_kind, float max_norm, float* norm_coef,
+                                 void* workspace, void* stream);
+/* fp8mlp_adam_step (casts null) or fp8mlp_adam_step_cast on the gradients g * *grad_scale (one fp32 rounding), e.g. the
+ * coefficient that fp8mlp_grad_norm left at norm_coef + 1: clipping without another pass over the gradients. */
+FP8MLP_API int fp8mlp_adam_step_scaled(const fp8mlp_adam_tensor* tensors, const fp8mlp_adam_cast* casts, int count,
+                                       const float* grad_scale, float lr, float beta1, float beta2, float eps,
+                                       float weight_decay, int64_t step, void* stream);
+
 /* The same for bf16 operands (the unquantised last layer of FP8MLP_H_BF16 contexts): A, B bf16, no scales. */
 FP8MLP_API int fp8mlp_gemm_bf16(int64_t M, int64_t N, int64_t K, const void* A, int a_kmajor, const void* B,
                                 int b_kmajor, float* out, void* stream);

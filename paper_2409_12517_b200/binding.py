@@ -21,6 +21,10 @@ E4M3, E5M2 = 0, 1
 BF16, F32 = 0, 1
 SMOOTH, SAVE_FOR_BWD, H_BF16, GU_FP8 = 1, 2, 4, 8
 SCALE_GIVEN, SCALE_FROM_CURRENT_AMAX, SCALE_GIVEN_WEIGHTS_CAST = 0, 1, 2
+SCORE_SOFTMAX, SCORE_SIGMOID = 0, 1
+NORM_L2, NORM_INF = 0, 1
+MAX_EXPERTS, MAX_TOP_K = 1024, 32
+NORM_WORKSPACE_BYTES = 16384
 WS_XQ, WS_W12Q, WS_W3Q, WS_HQ, WS_GU, WS_DYQ, WS_DZQ, WS_HB, WS_W3B = range(9)
 
 EXPORTS = [
@@ -30,6 +34,8 @@ EXPORTS = [
     "fp8mlp_forward_static", "fp8mlp_adam_step", "fp8mlp_scale_from_amax",
     "fp8mlp_merge_weights", "fp8mlp_forward_merged", "fp8mlp_gemm_bf16",
     "fp8mlp_selftest_wait_timeout", "fp8mlp_adam_step_cast", "fp8mlp_gemm_plan", "fp8mlp_code_stats",
+    "fp8mlp_route", "fp8mlp_route_backward", "fp8mlp_route_update_bias", "fp8mlp_dispatch_plan", "fp8mlp_dispatch",
+    "fp8mlp_combine", "fp8mlp_combine_backward", "fp8mlp_grad_norm", "fp8mlp_clip_grads", "fp8mlp_adam_step_scaled",
 ]
 PHASES = ["quant_x", "quant_w12", "quant_w3", "gemm1_swiglu", "gemm2_down", "quant_dy", "dgrad2_swiglu_bwd",
           "wgrad3", "dgrad1", "wgrad12", "misc"]
@@ -65,6 +71,16 @@ class _GemmPlan(C.Structure):
 class _AdamCast(C.Structure):
     _fields_ = [("dst", C.c_void_p), ("cols", C.c_int64), ("ld_dst", C.c_int64), ("scale", C.c_void_p),
                 ("row_div", C.c_void_p), ("amax", C.c_void_p)]
+
+
+class Router(C.Structure):
+    """How tokens choose their experts (fp8mlp_router; made by new_router)."""
+    _fields_ = [(n, C.c_int32) for n in ("n_experts", "top_k", "score", "n_groups", "top_groups", "group_top",
+                                         "renormalise")] + [("scale", C.c_float)]
+
+
+class _GradTensor(C.Structure):
+    _fields_ = [("g", C.c_void_p), ("out", C.c_void_p), ("n", C.c_int64), ("dtype", C.c_int32)]
 
 
 _lib = None
@@ -114,6 +130,18 @@ def lib():
         L.fp8mlp_scale_from_amax.argtypes = [C.c_void_p, C.c_int, C.c_void_p, C.c_void_p]
         L.fp8mlp_profile_enable.argtypes = [C.c_void_p, C.c_int]
         L.fp8mlp_profile_read.argtypes = [C.c_void_p, C.POINTER(C.c_double), C.POINTER(C.c_int64)]
+        p, i32, i64, f32 = C.c_void_p, C.c_int, C.c_int64, C.c_float
+        L.fp8mlp_route.argtypes = [C.POINTER(Router), i64, p, i32, i64, p, p, p, p]
+        L.fp8mlp_route_backward.argtypes = [C.POINTER(Router), i64, p, i32, i64, p, p, p, i64, p]
+        L.fp8mlp_route_update_bias.argtypes = [i32, p, f32, p, p]
+        L.fp8mlp_dispatch_plan.argtypes = [i64, i32, i32, p, p, p, p, p]
+        L.fp8mlp_dispatch.argtypes = [i64, i32, i64, i32, p, i64, p, p, i64, p]
+        L.fp8mlp_combine.argtypes = [i64, i32, i64, i32, p, i64, p, p, p, i64, p]
+        L.fp8mlp_combine_backward.argtypes = [i64, i32, i64, i32, p, i64, p, i64, p, p, p, p, p]
+        L.fp8mlp_grad_norm.argtypes = [C.POINTER(_GradTensor), i32, i32, f32, p, p, p]
+        L.fp8mlp_clip_grads.argtypes = [C.POINTER(_GradTensor), i32, i32, f32, p, p, p]
+        L.fp8mlp_adam_step_scaled.argtypes = [C.POINTER(_AdamTensor), C.POINTER(_AdamCast), i32, p, f32, f32, f32, f32,
+                                              f32, i64, p]
         missing = [name for name in EXPORTS if not hasattr(L, name)]
         if missing:
             raise RuntimeError(f"{LIB_PATH} does not export {missing}")
@@ -246,30 +274,17 @@ def fp8mlp_forward_merged(ctx: int, T: int, x, scale_mode: int, scales: dict, am
                                        C.byref(a) if a is not None else None, _ptr(y), _stream()), "fp8mlp_forward_merged")
 
 
-def fp8mlp_adam_step(tensors: list, lr: float, beta1: float, beta2: float, eps: float, weight_decay: float,
-                     step: int) -> None:
-    """tensors: dicts with torch tensors w, g (fp32), m, v (uint8 codes) and 1-element fp32 tensors
-    scale_m_in, scale_v_in, scale_m_out, scale_v_out, amax_m, amax_v.  Everything is updated in place."""
+def _adam_tensors(tensors: list):
     arr = (_AdamTensor * len(tensors))()
     for a, t in zip(arr, tensors):
         a.w, a.g, a.m, a.v, a.n = t["w"].data_ptr(), t["g"].data_ptr(), t["m"].data_ptr(), t["v"].data_ptr(), t["w"].numel()
         for k in ("scale_m_in", "scale_v_in", "scale_m_out", "scale_v_out", "amax_m", "amax_v"):
             setattr(a, k, t[k].data_ptr())
-    _check(lib().fp8mlp_adam_step(arr, len(tensors), lr, beta1, beta2, eps, weight_decay, step, _stream()),
-           "fp8mlp_adam_step")
+    return arr
 
 
-def fp8mlp_adam_step_cast(tensors: list, casts: list, lr: float, beta1: float, beta2: float, eps: float,
-                          weight_decay: float, step: int) -> None:
-    """fp8mlp_adam_step that also writes the E4M3 codes of the updated weights.  casts: one entry per tensor, None or a
-    dict with dst (device pointer as int, or a uint8 tensor), cols, ld_dst, scale (1-element fp32 tensor), and
-    optionally row_div (fp32 tensor, one per row) and amax (1-element fp32 tensor)."""
-    arr = (_AdamTensor * len(tensors))()
-    for a, t in zip(arr, tensors):
-        a.w, a.g, a.m, a.v, a.n = t["w"].data_ptr(), t["g"].data_ptr(), t["m"].data_ptr(), t["v"].data_ptr(), t["w"].numel()
-        for k in ("scale_m_in", "scale_v_in", "scale_m_out", "scale_v_out", "amax_m", "amax_v"):
-            setattr(a, k, t[k].data_ptr())
-    carr = (_AdamCast * len(tensors))()
+def _adam_casts(casts: list, count: int):
+    carr = (_AdamCast * count)()
     for c, d in zip(carr, casts):
         if d is None:
             continue
@@ -277,8 +292,33 @@ def fp8mlp_adam_step_cast(tensors: list, casts: list, lr: float, beta1: float, b
         c.cols, c.ld_dst, c.scale = d["cols"], d["ld_dst"], d["scale"].data_ptr()
         c.row_div = d["row_div"].data_ptr() if d.get("row_div") is not None else None
         c.amax = d["amax"].data_ptr() if d.get("amax") is not None else None
-    _check(lib().fp8mlp_adam_step_cast(arr, carr, len(tensors), lr, beta1, beta2, eps, weight_decay, step, _stream()),
-           "fp8mlp_adam_step_cast")
+    return carr
+
+
+def fp8mlp_adam_step(tensors: list, lr: float, beta1: float, beta2: float, eps: float, weight_decay: float,
+                     step: int) -> None:
+    """tensors: dicts with torch tensors w, g (fp32), m, v (uint8 codes) and 1-element fp32 tensors
+    scale_m_in, scale_v_in, scale_m_out, scale_v_out, amax_m, amax_v.  Everything is updated in place."""
+    _check(lib().fp8mlp_adam_step(_adam_tensors(tensors), len(tensors), lr, beta1, beta2, eps, weight_decay, step,
+                                  _stream()), "fp8mlp_adam_step")
+
+
+def fp8mlp_adam_step_cast(tensors: list, casts: list, lr: float, beta1: float, beta2: float, eps: float,
+                          weight_decay: float, step: int) -> None:
+    """fp8mlp_adam_step that also writes the E4M3 codes of the updated weights.  casts: one entry per tensor, None or a
+    dict with dst (device pointer as int, or a uint8 tensor), cols, ld_dst, scale (1-element fp32 tensor), and
+    optionally row_div (fp32 tensor, one per row) and amax (1-element fp32 tensor)."""
+    _check(lib().fp8mlp_adam_step_cast(_adam_tensors(tensors), _adam_casts(casts, len(tensors)), len(tensors), lr, beta1,
+                                       beta2, eps, weight_decay, step, _stream()), "fp8mlp_adam_step_cast")
+
+
+def fp8mlp_adam_step_scaled(tensors: list, casts: list | None, grad_scale, lr: float, beta1: float, beta2: float,
+                            eps: float, weight_decay: float, step: int) -> None:
+    """The same two steps (casts None: without the codes) on the gradients times grad_scale, a 1-element fp32 CUDA tensor,
+    e.g. norm_coef[1:] of fp8mlp_grad_norm."""
+    _check(lib().fp8mlp_adam_step_scaled(_adam_tensors(tensors), None if casts is None else _adam_casts(casts, len(tensors)),
+                                         len(tensors), _ptr(grad_scale), lr, beta1, beta2, eps, weight_decay, step, _stream()),
+           "fp8mlp_adam_step_scaled")
 
 
 def fp8mlp_code_stats(codes, fp8_fmt: int, counts, ld: int | None = None) -> None:
@@ -306,6 +346,144 @@ def fp8mlp_scale_from_amax(amax, fp8_fmt: int, scale) -> None:
 def fp8mlp_gemm_bf16(M: int, N: int, K: int, A, a_kmajor: bool, B, b_kmajor: bool, out) -> None:
     _check(lib().fp8mlp_gemm_bf16(M, N, K, _ptr(A), int(a_kmajor), _ptr(B), int(b_kmajor), _ptr(out), _stream()),
            "fp8mlp_gemm_bf16")
+
+
+# ---------------------------------------------------------------- experts of one layer, and clipping
+
+_DTYPES = {torch.bfloat16: BF16, torch.float32: F32}
+
+
+def _as(t, dtype, numel, what):
+    """Device pointer of a contiguous CUDA tensor of the given type and size."""
+    if t.dtype != dtype or t.numel() != numel or not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{what}: a contiguous CUDA tensor of {numel} {dtype} elements is needed, "
+                         f"got {tuple(t.shape)} {t.dtype} on {t.device}")
+    return t.data_ptr()
+
+
+def _matrix(t, cols, what, dtype=None):
+    """(pointer, type, row stride) of a 2-D CUDA tensor whose rows are contiguous; any row stride >= its columns."""
+    if t.dim() != 2 or t.shape[1] != cols or not t.is_cuda or t.dtype not in _DTYPES or (dtype is not None and t.dtype != dtype):
+        raise ValueError(f"{what}: a 2-D CUDA tensor of {cols} columns in {dtype or 'bfloat16 or float32'} is needed, "
+                         f"got {tuple(t.shape)} {t.dtype} on {t.device}")
+    if t.stride(1) != 1 and cols > 1:
+        raise ValueError(f"{what}: the elements of a row must be neighbours")
+    return t.data_ptr(), _DTYPES[t.dtype], t.stride(0) if t.shape[0] > 1 else max(cols, t.stride(0))
+
+
+def new_router(n_experts: int, top_k: int, score: int = SCORE_SOFTMAX, n_groups: int = 1, top_groups: int = 1,
+               group_top: int = 1, renormalise: bool = True, scale: float = 1.0) -> Router:
+    return Router(n_experts, top_k, score, n_groups, top_groups, group_top, int(renormalise), scale)
+
+
+def fp8mlp_route(router: Router, logits, bias, experts, weights) -> None:
+    """logits: [T, n_experts] bf16 or fp32, any row stride; bias: fp32 [n_experts] or None; receives experts (int32
+    [T, top_k]) and weights (fp32 [T, top_k])."""
+    T, n = logits.shape[0], logits.shape[0] * router.top_k
+    ptr, dtype, ld = _matrix(logits, router.n_experts, "logits")
+    _check(lib().fp8mlp_route(router, T, ptr, dtype, ld,
+                              None if bias is None else _as(bias, torch.float32, router.n_experts, "bias"),
+                              _as(experts, torch.int32, n, "experts"), _as(weights, torch.float32, n, "weights"), _stream()),
+           "fp8mlp_route")
+
+
+def fp8mlp_route_backward(router: Router, logits, experts, d_weights, d_logits) -> None:
+    """d_logits (type of the logits, any row stride) from d_weights (fp32 [T, top_k]) for the experts the forward chose."""
+    T, n = logits.shape[0], logits.shape[0] * router.top_k
+    ptr, dtype, ld = _matrix(logits, router.n_experts, "logits")
+    d_ptr, _, ld_d = _matrix(d_logits, router.n_experts, "d_logits", logits.dtype)
+    if d_logits.shape[0] != T:
+        raise ValueError("d_logits: not as many rows as logits")
+    _check(lib().fp8mlp_route_backward(router, T, ptr, dtype, ld, _as(experts, torch.int32, n, "experts"),
+                                       _as(d_weights, torch.float32, n, "d_weights"), d_ptr, ld_d, _stream()),
+           "fp8mlp_route_backward")
+
+
+def fp8mlp_route_update_bias(counts, rate: float, bias) -> None:
+    """bias (fp32 [n_experts], in place) moves by rate towards the experts with fewer rows than the mean (counts, int32)."""
+    n = bias.numel()
+    _check(lib().fp8mlp_route_update_bias(n, _as(counts, torch.int32, n, "counts"), rate, _as(bias, torch.float32, n, "bias"),
+                                          _stream()), "fp8mlp_route_update_bias")
+
+
+def fp8mlp_dispatch_plan(experts, n_experts: int, counts, offsets, rows) -> None:
+    """experts: int32 [T, top_k]; receives counts (int32 [n_experts]), offsets (int32 [n_experts + 1]) and rows (int32
+    [T, top_k])."""
+    T, k = experts.shape
+    _check(lib().fp8mlp_dispatch_plan(T, k, n_experts, _as(experts, torch.int32, T * k, "experts"),
+                                      _as(counts, torch.int32, n_experts, "counts"),
+                                      _as(offsets, torch.int32, n_experts + 1, "offsets"),
+                                      _as(rows, torch.int32, T * k, "rows"), _stream()), "fp8mlp_dispatch_plan")
+
+
+def _rows_pair(token, expert, rows, token_name, expert_name):
+    T, k = rows.shape
+    ptr, dtype, ld = _matrix(token, expert.shape[1], token_name, expert.dtype)
+    if token.shape[0] != T:
+        raise ValueError(f"{token_name}: {token.shape[0]} rows, but rows speaks of {T} tokens")
+    return T, k, ptr, dtype, ld, _as(expert, token.dtype, expert.numel(), expert_name), _as(rows, torch.int32, T * k, "rows")
+
+
+def fp8mlp_dispatch(x, rows, xe) -> None:
+    """xe[rows[t, j]] = x[t]; x: [T, d] bf16 or fp32, any row stride; xe: [n, d] of the same type, contiguous."""
+    T, k, ptr, dtype, ld, xe_ptr, rows_ptr = _rows_pair(x, xe, rows, "x", "xe")
+    _check(lib().fp8mlp_dispatch(T, k, x.shape[1], dtype, ptr, ld, rows_ptr, xe_ptr, xe.shape[0], _stream()), "fp8mlp_dispatch")
+
+
+def fp8mlp_combine(ye, rows, weights, y) -> None:
+    """y[t] = sum_j weights[t, j] ye[rows[t, j]]; weights fp32 [T, top_k] or None (= 1); y: [T, d], any row stride."""
+    T, k, ptr, dtype, ld, ye_ptr, rows_ptr = _rows_pair(y, ye, rows, "y", "ye")
+    _check(lib().fp8mlp_combine(T, k, y.shape[1], dtype, ye_ptr, ye.shape[0], rows_ptr,
+                                None if weights is None else _as(weights, torch.float32, T * k, "weights"), ptr, ld, _stream()),
+           "fp8mlp_combine")
+
+
+def fp8mlp_combine_backward(dy, ye, rows, weights, dye, d_weights) -> None:
+    """dye[rows[t, j]] = weights[t, j] dy[t] and d_weights[t, j] = <dy[t], ye[rows[t, j]]> (fp32 [T, top_k])."""
+    T, k, ptr, dtype, ld, ye_ptr, rows_ptr = _rows_pair(dy, ye, rows, "dy", "ye")
+    _check(lib().fp8mlp_combine_backward(T, k, dy.shape[1], dtype, ptr, ld, ye_ptr, ye.shape[0], rows_ptr,
+                                         _as(weights, torch.float32, T * k, "weights"), _as(dye, ye.dtype, ye.numel(), "dye"),
+                                         _as(d_weights, torch.float32, T * k, "d_weights"), _stream()),
+           "fp8mlp_combine_backward")
+
+
+class GradList:
+    """The tensors of one clipping call, marshalled once; a program whose gradients stay where they are keeps it (it
+    holds the tensors, and addresses only - every call reads the gradients anew)."""
+
+    def __init__(self, grads, outs):
+        self.tensors = (list(grads), list(grads if outs is None else outs))
+        if len(self.tensors[0]) != len(self.tensors[1]):
+            raise ValueError("as many outputs as gradients are needed")
+        self.count = len(self.tensors[0])
+        self.array = (_GradTensor * max(self.count, 1))()
+        for a, g, o in zip(self.array, *self.tensors):
+            if g.dtype not in _DTYPES:
+                raise ValueError(f"gradients are bfloat16 or float32, not {g.dtype}")
+            a.g, a.out, a.n, a.dtype = (_as(g, g.dtype, g.numel(), "gradient"), _as(o, g.dtype, g.numel(), "output"), g.numel(),
+                                        _DTYPES[g.dtype])
+
+
+def new_grad_list(grads, outs=None) -> GradList:
+    """grads: contiguous bf16 / fp32 CUDA tensors; outs: where the clipped ones go (default: in place)."""
+    return GradList(grads, outs)
+
+
+def new_norm_workspace(device="cuda"):
+    return torch.empty(NORM_WORKSPACE_BYTES, dtype=torch.uint8, device=device)
+
+
+def fp8mlp_grad_norm(grads: GradList, norm_kind: int, max_norm: float, norm_coef, workspace) -> None:
+    """norm_coef (fp32 [2]) receives the global norm and min(1, max_norm / (norm + 1e-6))."""
+    _check(lib().fp8mlp_grad_norm(grads.array, grads.count, norm_kind, max_norm, _as(norm_coef, torch.float32, 2, "norm_coef"),
+                                  _as(workspace, torch.uint8, NORM_WORKSPACE_BYTES, "workspace"), _stream()), "fp8mlp_grad_norm")
+
+
+def fp8mlp_clip_grads(grads: GradList, norm_kind: int, max_norm: float, norm_coef, workspace) -> None:
+    """fp8mlp_grad_norm, and out = g * coefficient for every tensor of the list."""
+    _check(lib().fp8mlp_clip_grads(grads.array, grads.count, norm_kind, max_norm, _as(norm_coef, torch.float32, 2, "norm_coef"),
+                                   _as(workspace, torch.uint8, NORM_WORKSPACE_BYTES, "workspace"), _stream()),
+           "fp8mlp_clip_grads")
 
 
 # ---------------------------------------------------------------- conveniences (allocation only)

@@ -28,6 +28,7 @@ struct AdamLaunch {
     AdamSeg seg[kAdamMaxTensors];
     int nseg, wide;
     float lr, beta1, beta2, omb1, omb2, c1, c2, eps, wd;
+    const float* grad_scale;   // SCALED: the gradients are multiplied by this first (clipping)
 };
 struct AdamZero { float* p[3 * kAdamMaxTensors]; };
 
@@ -62,7 +63,9 @@ __device__ __forceinline__ float warp_max_f(float v) {
 
 // CAST: the pass also writes the E4M3 codes of the updated weights (scale, optional per-row divisor: exactly the
 // arithmetic of the quantise pass of the forward, which the next forward can then skip) and their maximum.
-template <bool CAST>
+// SCALED: the gradients are multiplied by *grad_scale first; a variant of its own because the pass is close to
+// instruction-bound under the power cap and the multiplication would cost the plain step as well.
+template <bool CAST, bool SCALED>
 __global__ void __launch_bounds__(kAdamThreads, kAdamBlocksPerSm) adam_kernel(const AdamLaunch q) {
     grid_dependency_wait();
     grid_launch_dependents();
@@ -75,6 +78,7 @@ __global__ void __launch_bounds__(kAdamThreads, kAdamBlocksPerSm) adam_kernel(co
     const uint32_t end = min(begin + sg.units_per_block, sg.n_units);
     const float inv_sm = __fdiv_rn(1.0f, *sg.sm_in), inv_sv = __fdiv_rn(1.0f, *sg.sv_in);
     const float sm_out = *sg.sm_out, sv_out = *sg.sv_out;
+    const float g_scale = SCALED ? *q.grad_scale : 1.0f;
     float max_m = 0.0f, max_v = 0.0f;
     for (uint32_t u0 = begin + threadIdx.x; u0 < end; u0 += kAdamThreads * kAdamUnroll) {
         uint32_t gw[kAdamUnroll][8], ww[kAdamUnroll][8];
@@ -110,7 +114,8 @@ __global__ void __launch_bounds__(kAdamThreads, kAdamBlocksPerSm) adam_kernel(co
             decode8<FP8MLP_E5M2>(vc[k].x, vc[k].y, vp);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float g = __uint_as_float(gw[k][i]);
+                float g = __uint_as_float(gw[k][i]);
+                if constexpr (SCALED) g = __fmul_rn(g, g_scale);
                 const float w = __uint_as_float(ww[k][i]);
                 const float m_prev = __fmul_rn(mp[i], inv_sm);
                 const float v_prev = __fmul_rn(vp[i], inv_sv);
@@ -190,7 +195,7 @@ bool al(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (
 using namespace fp8mlp;
 
 namespace {
-int adam_launch(const fp8mlp_adam_tensor* t, const fp8mlp_adam_cast* casts, int count, float lr, float beta1, float beta2,
+int adam_launch(const fp8mlp_adam_tensor* t, const fp8mlp_adam_cast* casts, const float* grad_scale, int count, float lr, float beta1, float beta2,
                 float eps, float weight_decay, int64_t step, void* stream) {
     if (t == nullptr || count < 1 || count > kAdamMaxTensors) return FP8MLP_ERR_ARG;
     for (int i = 0; casts != nullptr && i < count; ++i) {
@@ -228,6 +233,7 @@ int adam_launch(const fp8mlp_adam_tensor* t, const fp8mlp_adam_cast* casts, int 
     AdamLaunch q{};
     q.nseg = count;
     q.wide = 1;
+    q.grad_scale = grad_scale;
     q.lr = lr; q.beta1 = beta1; q.beta2 = beta2; q.eps = eps; q.wd = weight_decay;
     q.omb1 = 1.0f - beta1;
     q.omb2 = 1.0f - beta2;
@@ -253,8 +259,9 @@ int adam_launch(const fp8mlp_adam_tensor* t, const fp8mlp_adam_cast* casts, int 
         }
     }
     const int grid = static_cast<int>(per_seg) * count;
-    if (casts != nullptr) FP8MLP_CUDA_CHECK(launch_chained(adam_kernel<true>, grid, kAdamThreads, 0, st, q));
-    else FP8MLP_CUDA_CHECK(launch_chained(adam_kernel<false>, grid, kAdamThreads, 0, st, q));
+    auto kernel = casts != nullptr ? (grad_scale != nullptr ? adam_kernel<true, true> : adam_kernel<true, false>)
+                                   : (grad_scale != nullptr ? adam_kernel<false, true> : adam_kernel<false, false>);
+    FP8MLP_CUDA_CHECK(launch_chained(kernel, grid, kAdamThreads, 0, st, q));
     FP8MLP_LAUNCH_CHECK();
     return FP8MLP_OK;
 }
@@ -262,11 +269,19 @@ int adam_launch(const fp8mlp_adam_tensor* t, const fp8mlp_adam_cast* casts, int 
 
 extern "C" int fp8mlp_adam_step(const fp8mlp_adam_tensor* t, int count, float lr, float beta1, float beta2, float eps,
                                 float weight_decay, int64_t step, void* stream) {
-    return adam_launch(t, nullptr, count, lr, beta1, beta2, eps, weight_decay, step, stream);
+    return adam_launch(t, nullptr, nullptr, count, lr, beta1, beta2, eps, weight_decay, step, stream);
 }
 
 extern "C" int fp8mlp_adam_step_cast(const fp8mlp_adam_tensor* t, const fp8mlp_adam_cast* casts, int count, float lr,
                                      float beta1, float beta2, float eps, float weight_decay, int64_t step, void* stream) {
     if (casts == nullptr) return FP8MLP_ERR_ARG;
-    return adam_launch(t, casts, count, lr, beta1, beta2, eps, weight_decay, step, stream);
+    return adam_launch(t, casts, nullptr, count, lr, beta1, beta2, eps, weight_decay, step, stream);
+}
+
+extern "C" int fp8mlp_adam_step_scaled(const fp8mlp_adam_tensor* t, const fp8mlp_adam_cast* casts, int count,
+                                       const float* grad_scale, float lr, float beta1, float beta2, float eps,
+                                       float weight_decay, int64_t step, void* stream) {
+    if (grad_scale == nullptr) return FP8MLP_ERR_ARG;
+    if (!al(grad_scale, 4)) return FP8MLP_ERR_ALIGN;
+    return adam_launch(t, casts, grad_scale, count, lr, beta1, beta2, eps, weight_decay, step, stream);
 }

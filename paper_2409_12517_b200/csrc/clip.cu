@@ -1,0 +1,343 @@
+// Global gradient norm over many tensors, and clipping to it.
+//
+// The list travels in the kernel's parameters, cut into chunks that are numbered through: a block takes every grid-th
+// chunk, whatever tensor it belongs to, so a thousand small tensors cost one launch and no block waits for a large one.
+#include <cmath>
+
+#include "common.cuh"
+
+namespace fp8mlp {
+
+namespace {
+
+constexpr uint32_t kAll = 0xffffffffu;
+constexpr int kClipThreads = 256;
+constexpr int kClipBlocksPerSm = 4;
+constexpr int kClipMaxBlocks = FP8MLP_NORM_WORKSPACE_BYTES / 8;    // one fp64 partial each
+constexpr int kUnroll = 4;                                         // 32-byte accesses in flight per thread
+constexpr int64_t kChunkUnits = kClipThreads * kUnroll;            // 32-byte units of a chunk
+constexpr float kNormEps = 1e-6f;
+
+struct ClipSeg {
+    const uint8_t* g;
+    uint8_t* out;
+    int64_t n;
+    uint32_t first_chunk;
+    int32_t f32;
+};
+// kCap tensors per launch: the parameters of a launch are copied with it, so short lists use the short form
+template <int kCap> struct ClipArgs {
+    double* partial;
+    float* norm_coef;
+    float max_norm;
+    int n_partial, count, inf, accumulate;
+    uint32_t chunks;
+    ClipSeg seg[kCap];
+};
+
+template <typename SRC> struct GradUnit;                           // a unit is 32 bytes
+template <> struct GradUnit<float> { static constexpr int kElems = 8; };
+template <> struct GradUnit<uint16_t> { static constexpr int kElems = 16; };
+__device__ __forceinline__ float as_float(float v) { return v; }
+__device__ __forceinline__ float as_float(uint16_t v) { return __uint_as_float(static_cast<uint32_t>(v) << 16); }
+__device__ __forceinline__ void put(float* p, float v) { *p = v; }
+__device__ __forceinline__ void put(uint16_t* p, float v) { *p = static_cast<uint16_t>(cvt_bf16x2(v, 0.0f) & 0xffffu); }
+
+template <typename SRC> __device__ __forceinline__ void unpack_unit(const uint32_t (&w)[8], float (&v)[GradUnit<SRC>::kElems]);
+template <> __device__ __forceinline__ void unpack_unit<float>(const uint32_t (&w)[8], float (&v)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(w[i]);
+}
+template <> __device__ __forceinline__ void unpack_unit<uint16_t>(const uint32_t (&w)[8], float (&v)[16]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) { v[2 * i] = bf16_lo(w[i]); v[2 * i + 1] = bf16_hi(w[i]); }
+}
+
+// Squares are summed in fp64: a square of an fp32 value is exact there and neither overflows nor underflows.  |g| keeps
+// its bit pattern, which orders like an unsigned integer with NaN above infinity, so a NaN survives the maximum.
+struct NormAcc {
+    double sum = 0.0;
+    uint32_t top = 0;
+    bool inf;
+    __device__ __forceinline__ void add(float v) {
+        if (inf) top = max(top, __float_as_uint(v) & 0x7fffffffu);
+        else sum = fma(static_cast<double>(v), static_cast<double>(v), sum);
+    }
+};
+
+// The tensor's elements lie in units of 32 bytes counted from the 32-byte boundary at or before its first element, so
+// every whole unit is one aligned access whatever the tensor's own alignment; the first and last may be part units.
+template <typename SRC>
+__device__ __forceinline__ void norm_chunk(const ClipSeg& s, int64_t chunk, NormAcc& acc) {
+    constexpr int N = GradUnit<SRC>::kElems;
+    const int64_t lead = static_cast<int64_t>(reinterpret_cast<uintptr_t>(s.g) & 31u) / static_cast<int64_t>(sizeof(SRC));
+    const SRC* base = reinterpret_cast<const SRC*>(s.g) - lead;
+    const int64_t last = lead + s.n;
+    const int64_t u0 = chunk * kChunkUnits + threadIdx.x;
+    uint32_t w[kUnroll][8];
+#pragma unroll
+    for (int k = 0; k < kUnroll; ++k) {
+        const int64_t e = (u0 + k * kClipThreads) * N;
+        if (e >= lead && e + N <= last) ld_global_nc_v8(base + e, w[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < kUnroll; ++k) {
+        const int64_t e = (u0 + k * kClipThreads) * N;
+        if (e >= lead && e + N <= last) {
+            float v[N];
+            unpack_unit<SRC>(w[k], v);
+#pragma unroll
+            for (int i = 0; i < N; ++i) acc.add(v[i]);
+        } else if (e < last && e + N > lead) {
+            for (int i = 0; i < N; ++i)
+                if (e + i >= lead && e + i < last) acc.add(as_float(base[e + i]));
+        }
+    }
+}
+
+template <typename SRC>
+__device__ __forceinline__ void clip_chunk(const ClipSeg& s, int64_t chunk, float coef) {
+    constexpr int N = GradUnit<SRC>::kElems;
+    const int64_t lead = static_cast<int64_t>(reinterpret_cast<uintptr_t>(s.g) & 31u) / static_cast<int64_t>(sizeof(SRC));
+    const SRC* base = reinterpret_cast<const SRC*>(s.g) - lead;
+    SRC* out = reinterpret_cast<SRC*>(s.out) - lead;
+    const bool same = ((reinterpret_cast<uintptr_t>(s.out) ^ reinterpret_cast<uintptr_t>(s.g)) & 31u) == 0;
+    const int64_t last = lead + s.n;
+    const int64_t u0 = chunk * kChunkUnits + threadIdx.x;
+    uint32_t w[kUnroll][8];
+#pragma unroll
+    for (int k = 0; k < kUnroll; ++k) {
+        const int64_t e = (u0 + k * kClipThreads) * N;
+        if (e >= lead && e + N <= last) ld_global_v8(base + e, w[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < kUnroll; ++k) {
+        const int64_t e = (u0 + k * kClipThreads) * N;
+        if (e >= lead && e + N <= last) {
+            float v[N];
+            unpack_unit<SRC>(w[k], v);
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] = __fmul_rn(v[i], coef);
+            if (same) {
+                uint32_t o[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    if constexpr (N == 8) o[i] = __float_as_uint(v[i]);
+                    else o[i] = cvt_bf16x2(v[2 * i], v[2 * i + 1]);
+                }
+                st_global_v8(out + e, o);
+            } else {
+#pragma unroll
+                for (int i = 0; i < N; ++i) put(out + e + i, v[i]);
+            }
+        } else if (e < last && e + N > lead) {
+            for (int i = 0; i < N; ++i)
+                if (e + i >= lead && e + i < last) put(out + e + i, __fmul_rn(as_float(base[e + i]), coef));
+        }
+    }
+}
+
+// the tensor that chunk c belongs to
+template <int kCap>
+__device__ __forceinline__ int find_seg(const ClipArgs<kCap>& a, uint32_t c) {
+    int lo = 0, hi = a.count - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (a.seg[mid].first_chunk <= c) lo = mid;
+        else hi = mid - 1;
+    }
+    return lo;
+}
+
+__device__ __forceinline__ double block_reduce(double v, bool inf, double* part) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        const double w = __shfl_xor_sync(kAll, v, o);
+        v = inf ? __longlong_as_double(max(__double_as_longlong(v), __double_as_longlong(w))) : v + w;
+    }
+    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
+    __syncthreads();
+    v = part[0];
+#pragma unroll
+    for (int i = 1; i < kClipThreads / 32; ++i)
+        v = inf ? __longlong_as_double(max(__double_as_longlong(v), __double_as_longlong(part[i]))) : v + part[i];
+    return v;
+}
+
+// A block's partial: the sum of its squares, or the bit pattern of its maximum (kept as an integer in the fp64 word).
+template <int kCap>
+__global__ void __launch_bounds__(kClipThreads, kClipBlocksPerSm) norm_kernel(const __grid_constant__ ClipArgs<kCap> a) {
+    __shared__ double part[kClipThreads / 32];
+    grid_dependency_wait();
+    grid_launch_dependents();
+    NormAcc acc;
+    acc.inf = a.inf != 0;
+    for (uint32_t c = blockIdx.x; c < a.chunks; c += gridDim.x) {
+        const ClipSeg& s = a.seg[find_seg(a, c)];
+        if (s.f32) norm_chunk<float>(s, c - s.first_chunk, acc);
+        else norm_chunk<uint16_t>(s, c - s.first_chunk, acc);
+    }
+    double v = acc.inf ? __longlong_as_double(static_cast<long long>(acc.top)) : acc.sum;
+    v = block_reduce(v, acc.inf, part);
+    if (threadIdx.x == 0) {
+        if (a.accumulate) {      // a further launch of the same call (a list longer than one launch holds)
+            const double w = a.partial[blockIdx.x];
+            v = acc.inf ? __longlong_as_double(max(__double_as_longlong(v), __double_as_longlong(w))) : v + w;
+        }
+        a.partial[blockIdx.x] = v;
+    }
+}
+
+// Every thread of the block returns (norm, coef), from all partials in their fixed order.
+__device__ __forceinline__ float2 finish_norm(const double* partial, int n_partial, bool inf, float max_norm, double* part) {
+    double v = 0.0;
+    for (int i = threadIdx.x; i < n_partial; i += kClipThreads) {
+        const double w = __ldcg(partial + i);
+        v = inf ? __longlong_as_double(max(__double_as_longlong(v), __double_as_longlong(w))) : v + w;
+    }
+    v = block_reduce(v, inf, part);
+    const float norm = inf ? __uint_as_float(static_cast<uint32_t>(__double_as_longlong(v))) : static_cast<float>(sqrt(v));
+    const float q = __fdiv_rn(max_norm, norm + kNormEps);
+    return make_float2(norm, q >= 1.0f ? 1.0f : q);       // a NaN is not >= 1 and stays
+}
+
+__global__ void __launch_bounds__(kClipThreads) norm_finish_kernel(const double* partial, int n_partial, int inf, float max_norm,
+                                                                  float* norm_coef) {
+    __shared__ double part[kClipThreads / 32];
+    grid_dependency_wait();
+    grid_launch_dependents();
+    const float2 r = finish_norm(partial, n_partial, inf != 0, max_norm, part);
+    if (threadIdx.x == 0) { norm_coef[0] = r.x; norm_coef[1] = r.y; }
+}
+
+// The chunks are walked from the last to the first: what the norm pass read last is still in L2.
+template <int kCap>
+__global__ void __launch_bounds__(kClipThreads, kClipBlocksPerSm) clip_kernel(const __grid_constant__ ClipArgs<kCap> a) {
+    __shared__ double part[kClipThreads / 32];
+    grid_dependency_wait();
+    grid_launch_dependents();
+    const float2 r = finish_norm(a.partial, a.n_partial, a.inf != 0, a.max_norm, part);
+    if (blockIdx.x == 0 && threadIdx.x == 0) { a.norm_coef[0] = r.x; a.norm_coef[1] = r.y; }
+    const float coef = r.y;
+    for (int64_t c = static_cast<int64_t>(a.chunks) - 1 - blockIdx.x; c >= 0; c -= gridDim.x) {
+        const ClipSeg& s = a.seg[find_seg(a, static_cast<uint32_t>(c))];
+        if (coef == 1.0f && s.out == s.g) continue;
+        if (s.f32) clip_chunk<float>(s, c - s.first_chunk, coef);
+        else clip_chunk<uint16_t>(s, c - s.first_chunk, coef);
+    }
+}
+
+bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+
+int64_t seg_chunks(const fp8mlp_grad_tensor& g) {
+    const int64_t esize = g.dtype == FP8MLP_F32 ? 4 : 2;
+    const int64_t bytes = static_cast<int64_t>(reinterpret_cast<uintptr_t>(g.g) & 31u) + g.n * esize;
+    return g.n == 0 ? 0 : (bytes + 32 * kChunkUnits - 1) / (32 * kChunkUnits);
+}
+
+struct ClipCall {
+    const fp8mlp_grad_tensor* grads;
+    int count, inf;
+    float max_norm;
+    float* norm_coef;
+    double* partial;
+    int blocks;
+    cudaStream_t st;
+};
+
+// One launch over grads[from, to); CLIP: the scaling pass, otherwise the norm pass.
+template <bool CLIP, int kCap>
+int clip_launch(const ClipCall& c, int from, int to) {
+    ClipArgs<kCap> a;
+    a.partial = c.partial; a.norm_coef = c.norm_coef; a.max_norm = c.max_norm;
+    a.n_partial = c.blocks; a.inf = c.inf; a.accumulate = from > 0;
+    int64_t chunks = 0;
+    int m = 0;
+    for (int i = from; i < to; ++i) {
+        const fp8mlp_grad_tensor& g = c.grads[i];
+        if (g.n == 0) continue;
+        ClipSeg& s = a.seg[m++];
+        s.g = static_cast<const uint8_t*>(g.g);
+        s.out = static_cast<uint8_t*>(g.out);
+        s.n = g.n;
+        s.first_chunk = static_cast<uint32_t>(chunks);
+        s.f32 = g.dtype == FP8MLP_F32;
+        chunks += seg_chunks(g);
+    }
+    a.count = m;
+    a.chunks = static_cast<uint32_t>(chunks);
+    if constexpr (CLIP) {
+        const int grid = chunks < c.blocks ? (chunks > 0 ? static_cast<int>(chunks) : 1) : c.blocks;
+        FP8MLP_CUDA_CHECK(launch_chained(clip_kernel<kCap>, grid, kClipThreads, 0, c.st, a));
+    } else {
+        FP8MLP_CUDA_CHECK(launch_chained(norm_kernel<kCap>, c.blocks, kClipThreads, 0, c.st, a));
+    }
+    FP8MLP_LAUNCH_CHECK();
+    return FP8MLP_OK;
+}
+
+constexpr int kCapSmall = 16, kCapMid = 120, kCapLarge = 960;      // 0.7, 4 and 31 KB of parameters
+
+template <bool CLIP>
+int clip_pass(const ClipCall& c) {
+    for (int from = 0; from == 0 || from < c.count; from += kCapLarge) {
+        const int to = c.count - from < kCapLarge ? c.count : from + kCapLarge;
+        const int rc = to - from <= kCapSmall ? clip_launch<CLIP, kCapSmall>(c, from, to)
+                       : to - from <= kCapMid ? clip_launch<CLIP, kCapMid>(c, from, to)
+                                              : clip_launch<CLIP, kCapLarge>(c, from, to);
+        if (rc != FP8MLP_OK) return rc;
+    }
+    return FP8MLP_OK;
+}
+
+int clip_run(const fp8mlp_grad_tensor* grads, int count, int kind, float max_norm, float* norm_coef, void* workspace, bool clip,
+             void* stream) {
+    if (kind != FP8MLP_NORM_L2 && kind != FP8MLP_NORM_INF) return FP8MLP_ERR_ARG;
+    if (count < 0 || (count > 0 && grads == nullptr) || norm_coef == nullptr || workspace == nullptr || !(max_norm >= 0.0f))
+        return FP8MLP_ERR_ARG;
+    int64_t chunks = 0;
+    for (int i = 0; i < count; ++i) {
+        const fp8mlp_grad_tensor& g = grads[i];
+        if (g.dtype != FP8MLP_BF16 && g.dtype != FP8MLP_F32) return FP8MLP_ERR_ARG;
+        if (g.n < 0 || g.n > (int64_t(1) << 40)) return FP8MLP_ERR_SHAPE;
+        if (g.n == 0) continue;
+        if (g.g == nullptr || (clip && g.out == nullptr)) return FP8MLP_ERR_ARG;
+        const uintptr_t esize = g.dtype == FP8MLP_F32 ? 4 : 2;
+        if (!aligned(g.g, esize) || (clip && !aligned(g.out, esize))) return FP8MLP_ERR_ALIGN;
+        chunks += seg_chunks(g);
+        if (chunks > 0x7fffffff) return FP8MLP_ERR_SHAPE;
+    }
+    if (!aligned(norm_coef, 4) || !aligned(workspace, 16)) return FP8MLP_ERR_ALIGN;
+    int dev = 0, sms = 0;
+    FP8MLP_CUDA_CHECK(cudaGetDevice(&dev));
+    FP8MLP_CUDA_CHECK(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+    ClipCall c{grads, count, kind == FP8MLP_NORM_INF, max_norm, norm_coef, static_cast<double*>(workspace), 0,
+               static_cast<cudaStream_t>(stream)};
+    int64_t blocks = static_cast<int64_t>(sms) * kClipBlocksPerSm;
+    if (blocks > kClipMaxBlocks) blocks = kClipMaxBlocks;
+    if (blocks > chunks) blocks = chunks > 0 ? chunks : 1;
+    c.blocks = static_cast<int>(blocks);
+    int rc = clip_pass<false>(c);
+    if (rc != FP8MLP_OK) return rc;
+    if (clip) return clip_pass<true>(c);
+    FP8MLP_CUDA_CHECK(launch_chained(norm_finish_kernel, 1, kClipThreads, 0, c.st, static_cast<const double*>(c.partial), c.blocks,
+                                     c.inf, max_norm, norm_coef));
+    FP8MLP_LAUNCH_CHECK();
+    return FP8MLP_OK;
+}
+
+}  // namespace
+
+}  // namespace fp8mlp
+
+using namespace fp8mlp;
+
+extern "C" int fp8mlp_grad_norm(const fp8mlp_grad_tensor* grads, int count, int norm_kind, float max_norm, float* norm_coef,
+                                void* workspace, void* stream) {
+    return clip_run(grads, count, norm_kind, max_norm, norm_coef, workspace, false, stream);
+}
+
+extern "C" int fp8mlp_clip_grads(const fp8mlp_grad_tensor* grads, int count, int norm_kind, float max_norm, float* norm_coef,
+                                 void* workspace, void* stream) {
+    return clip_run(grads, count, norm_kind, max_norm, norm_coef, workspace, true, stream);
+}

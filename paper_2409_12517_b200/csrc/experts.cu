@@ -1,0 +1,379 @@
+// Tokens into expert order and back: the plan (a stable counting sort of the chosen experts), the copy of the rows, the
+// weighted sum of the experts' outputs and its gradient.
+#include "common.cuh"
+
+namespace fp8mlp {
+
+namespace {
+
+constexpr uint32_t kAll = 0xffffffffu;
+
+// ---------------------------------------------------------------- plan
+// Counting sort by one cluster.  Every warp owns a contiguous piece of the slots: it counts its slots per expert, the
+// counts become start positions (over experts, then CTAs, then warps), and a second walk over the same piece hands them
+// out in order - no atomics, so the order is that of the slots.
+constexpr int kPlanWarps = 32;
+constexpr int kPlanMaxCluster = 8;
+
+struct PlanArgs {
+    const int32_t* experts; int32_t *counts, *offsets, *rows;
+    int64_t n;             // slots
+    int64_t per_warp;      // slots of a warp, a multiple of 32
+    int E;
+};
+
+__global__ void __launch_bounds__(kPlanWarps * 32) plan_kernel(const PlanArgs a) {
+    extern __shared__ int32_t hist[];                    // [warps][E]: counts, then start positions
+    __shared__ int32_t scan_part[kPlanWarps];
+    __shared__ int32_t total[FP8MLP_MAX_EXPERTS];        // this CTA's slots per expert; the cluster reads it
+    const int warps = blockDim.x / 32, warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    uint32_t n_cta;
+    asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(n_cta));
+    const uint32_t rank = cluster_ctarank();
+    const int E = a.E;
+    const int64_t begin = (static_cast<int64_t>(rank) * warps + warp) * a.per_warp;
+    const int64_t end = begin + a.per_warp < a.n ? begin + a.per_warp : a.n;
+    int32_t* mine = hist + warp * E;
+    for (int e = lane; e < E; e += 32) mine[e] = 0;
+    grid_dependency_wait();
+    grid_launch_dependents();
+    __syncwarp();
+    for (int64_t i0 = begin; i0 < end; i0 += 32) {
+        const int64_t i = i0 + lane;
+        const int e = i < end ? __ldg(a.experts + i) : -1;
+        const bool used = static_cast<uint32_t>(e) < static_cast<uint32_t>(E);
+        const uint32_t same = __match_any_sync(kAll, used ? e : -1);
+        if (used && lane == __ffs(same) - 1) mine[e] += __popc(same);
+        __syncwarp();
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < E; e += blockDim.x) {
+        int32_t run = 0;
+        for (int w = 0; w < warps; ++w) {
+            const int32_t c = hist[w * E + e];
+            hist[w * E + e] = run;
+            run += c;
+        }
+        total[e] = run;
+    }
+    cluster_sync_all();                                  // every CTA's totals are there
+    // offsets: a scan over the experts, 32 * warps of them at a time
+    int32_t carry = 0;
+    for (int e_base = 0; e_base < E; e_base += blockDim.x) {
+        const int e = e_base + threadIdx.x;
+        int32_t before = 0, all = 0;
+        if (e < E) {
+            for (uint32_t r = 0; r < n_cta; ++r) {
+                int32_t c;
+                asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(c) : "r"(mapa_shared(smem_u32(&total[e]), r)) : "memory");
+                if (r < rank) before += c;
+                all += c;
+            }
+        }
+        int32_t incl = all;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int32_t v = __shfl_up_sync(kAll, incl, o);
+            if (lane >= o) incl += v;
+        }
+        if (lane == 31) scan_part[warp] = incl;
+        __syncthreads();
+        int32_t lower = carry, chunk = 0;
+        for (int w = 0; w < warps; ++w) {
+            if (w < warp) lower += scan_part[w];
+            chunk += scan_part[w];
+        }
+        const int32_t offset = lower + incl - all;
+        if (e < E) {
+            if (rank == 0) {
+                a.counts[e] = all;
+                a.offsets[e] = offset;
+                if (e == E - 1) a.offsets[E] = offset + all;
+            }
+            for (int w = 0; w < warps; ++w) hist[w * E + e] += offset + before;
+        }
+        carry += chunk;
+        __syncthreads();
+    }
+    for (int64_t i0 = begin; i0 < end; i0 += 32) {
+        const int64_t i = i0 + lane;
+        const int e = i < end ? __ldg(a.experts + i) : -1;
+        const bool used = static_cast<uint32_t>(e) < static_cast<uint32_t>(E);
+        const uint32_t same = __match_any_sync(kAll, used ? e : -1);
+        const uint32_t lower = same & ((1u << lane) - 1u);
+        int32_t row = -1;
+        if (used) row = mine[e] + __popc(lower);
+        __syncwarp();
+        if (used && lower == 0u) mine[e] = row + __popc(same);
+        __syncwarp();
+        if (i < end) a.rows[i] = row;
+    }
+    cluster_sync_all();                                  // no CTA leaves while another may still read its totals
+}
+
+// ---------------------------------------------------------------- rows
+// A unit is 16 bytes of a row: 8 bf16 or 4 fp32 elements.
+template <typename T> struct RowUnit;
+template <> struct RowUnit<uint16_t> { static constexpr int kElems = 8; };
+template <> struct RowUnit<float> { static constexpr int kElems = 4; };
+
+__device__ __forceinline__ void unpack(const uint4& w, float (&v)[8]) {
+    v[0] = bf16_lo(w.x); v[1] = bf16_hi(w.x); v[2] = bf16_lo(w.y); v[3] = bf16_hi(w.y);
+    v[4] = bf16_lo(w.z); v[5] = bf16_hi(w.z); v[6] = bf16_lo(w.w); v[7] = bf16_hi(w.w);
+}
+__device__ __forceinline__ void unpack(const uint4& w, float (&v)[4]) {
+    v[0] = __uint_as_float(w.x); v[1] = __uint_as_float(w.y); v[2] = __uint_as_float(w.z); v[3] = __uint_as_float(w.w);
+}
+__device__ __forceinline__ void store_unit(void* p, const float (&v)[8]) {
+    st_global_v4(p, cvt_bf16x2(v[0], v[1]), cvt_bf16x2(v[2], v[3]), cvt_bf16x2(v[4], v[5]), cvt_bf16x2(v[6], v[7]));
+}
+__device__ __forceinline__ void store_unit(void* p, const float (&v)[4]) {
+    st_global_v4(p, __float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+}
+
+constexpr int kRowThreads = 256;
+
+struct RowArgs {
+    const uint8_t* src;        // dispatch: x; combine: ye; combine_backward: ye
+    uint8_t* dst;              // dispatch: xe; combine: y; combine_backward: dye
+    const uint8_t* dy;         // combine_backward
+    const int32_t* rows; const float* weights; float* d_weights;
+    int64_t T, n_rows;
+    int64_t token_bytes;       // row stride of the token side (x, y, dy)
+    int64_t row_bytes;         // of the expert side: its rows are contiguous
+    int64_t units;             // T * units_per_row (dispatch, combine)
+    uint32_t units_per_row;
+    int k;
+};
+
+__global__ void __launch_bounds__(kRowThreads) dispatch_kernel(const RowArgs a) {
+    grid_dependency_wait();
+    grid_launch_dependents();
+    const int64_t u = static_cast<int64_t>(blockIdx.x) * kRowThreads + threadIdx.x;
+    if (u >= a.units) return;
+    const int64_t t = u / a.units_per_row;
+    const int64_t at = (u - t * a.units_per_row) * 16;
+    const uint4 v = ld_global_nc_v4(a.src + t * a.token_bytes + at);
+    for (int j = 0; j < a.k; ++j) {
+        const int64_t row = __ldg(a.rows + t * a.k + j);
+        if (row >= 0 && row < a.n_rows) st_global_v4(a.dst + row * a.row_bytes + at, v.x, v.y, v.z, v.w);
+    }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kRowThreads) combine_kernel(const RowArgs a) {
+    constexpr int N = RowUnit<T>::kElems;
+    grid_dependency_wait();
+    grid_launch_dependents();
+    const int64_t u = static_cast<int64_t>(blockIdx.x) * kRowThreads + threadIdx.x;
+    if (u >= a.units) return;
+    const int64_t t = u / a.units_per_row;
+    const int64_t at = (u - t * a.units_per_row) * 16;
+    float acc[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) acc[i] = 0.0f;
+    for (int j = 0; j < a.k; ++j) {
+        const int64_t row = __ldg(a.rows + t * a.k + j);
+        if (row < 0 || row >= a.n_rows) continue;
+        const float w = a.weights != nullptr ? __ldg(a.weights + t * a.k + j) : 1.0f;
+        float v[N];
+        unpack(ld_global_nc_v4(a.src + row * a.row_bytes + at), v);
+#pragma unroll
+        for (int i = 0; i < N; ++i) acc[i] = fmaf(w, v[i], acc[i]);
+    }
+    store_unit(a.dst + t * a.token_bytes + at, acc);
+}
+
+// One block per token: dy is read once for kSlots slots, every slot's row of ye once.
+constexpr int kSlots = 8;
+
+template <typename T>
+__global__ void __launch_bounds__(kRowThreads) combine_backward_kernel(const RowArgs a) {
+    constexpr int N = RowUnit<T>::kElems;
+    __shared__ float part[kRowThreads / 32][kSlots];
+    grid_dependency_wait();
+    grid_launch_dependents();
+    const int64_t t = blockIdx.x;
+    const uint8_t* dy = a.dy + t * a.token_bytes;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    for (int j0 = 0; j0 < a.k; j0 += kSlots) {
+        const int slots = min(kSlots, a.k - j0);
+        int64_t row[kSlots];
+        float w[kSlots], dot[kSlots];
+#pragma unroll
+        for (int j = 0; j < kSlots; ++j) {
+            row[j] = j < slots ? __ldg(a.rows + t * a.k + j0 + j) : -1;
+            if (row[j] >= a.n_rows) row[j] = -1;
+            w[j] = j < slots ? __ldg(a.weights + t * a.k + j0 + j) : 0.0f;
+            dot[j] = 0.0f;
+        }
+        for (uint32_t u = threadIdx.x; u < a.units_per_row; u += blockDim.x) {
+            const int64_t at = static_cast<int64_t>(u) * 16;
+            float g[N];
+            unpack(ld_global_nc_v4(dy + at), g);
+#pragma unroll
+            for (int j = 0; j < kSlots; ++j) {
+                if (row[j] < 0) continue;
+                float v[N], out[N];
+                unpack(ld_global_nc_v4(a.src + row[j] * a.row_bytes + at), v);
+#pragma unroll
+                for (int i = 0; i < N; ++i) { dot[j] = fmaf(g[i], v[i], dot[j]); out[i] = w[j] * g[i]; }
+                store_unit(a.dst + row[j] * a.row_bytes + at, out);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < kSlots; ++j) {
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) dot[j] += __shfl_xor_sync(kAll, dot[j], o);
+            if (lane == 0) part[warp][j] = dot[j];
+        }
+        __syncthreads();
+        if (threadIdx.x < slots) {
+            float sum = 0.0f;
+            for (int i = 0; i < static_cast<int>(blockDim.x) / 32; ++i) sum += part[i][threadIdx.x];
+            a.d_weights[t * a.k + j0 + threadIdx.x] = sum;
+        }
+        __syncthreads();
+    }
+}
+
+bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+
+// What dispatch, combine and its gradient refuse alike; token / expert are the two row tensors.
+int check_rows(int64_t T, int top_k, int64_t d, int dtype, const void* token, int64_t ld, const void* expert, int64_t n_rows,
+               const int32_t* rows) {
+    if (dtype != FP8MLP_BF16 && dtype != FP8MLP_F32) return FP8MLP_ERR_ARG;
+    if (T < 0 || n_rows < 0 || d <= 0 || d % 16 != 0 || d > (1 << 24) || top_k < 1 || top_k > FP8MLP_MAX_TOP_K)
+        return FP8MLP_ERR_SHAPE;
+    if (T > 0x7fffffff / top_k || n_rows > 0x7fffffff) return FP8MLP_ERR_SHAPE;
+    if (T == 0) return FP8MLP_OK;
+    if (ld < d) return FP8MLP_ERR_SHAPE;
+    if (token == nullptr || rows == nullptr || (expert == nullptr && n_rows > 0)) return FP8MLP_ERR_ARG;
+    const int64_t esize = dtype == FP8MLP_F32 ? 4 : 2;
+    if (!aligned(token, 16) || !aligned(expert, 16) || ld * esize % 16 != 0 || !aligned(rows, 4)) return FP8MLP_ERR_ALIGN;
+    return FP8MLP_OK;
+}
+
+RowArgs row_args(int64_t T, int top_k, int64_t d, int dtype, int64_t ld, int64_t n_rows, const int32_t* rows) {
+    const int64_t esize = dtype == FP8MLP_F32 ? 4 : 2;
+    RowArgs a{};
+    a.rows = rows;
+    a.T = T; a.k = top_k; a.n_rows = n_rows;
+    a.token_bytes = ld * esize;
+    a.row_bytes = d * esize;
+    a.units_per_row = static_cast<uint32_t>(d * esize / 16);
+    a.units = T * a.units_per_row;
+    return a;
+}
+
+int unit_blocks(const RowArgs& a, dim3* grid) {
+    const int64_t blocks = (a.units + kRowThreads - 1) / kRowThreads;
+    if (blocks > 0x7fffffff) return FP8MLP_ERR_SHAPE;
+    *grid = dim3(static_cast<unsigned>(blocks));
+    return FP8MLP_OK;
+}
+
+}  // namespace
+
+}  // namespace fp8mlp
+
+using namespace fp8mlp;
+
+extern "C" int fp8mlp_dispatch_plan(int64_t T, int top_k, int n_experts, const int32_t* experts, int32_t* counts,
+                                    int32_t* offsets, int32_t* rows, void* stream) {
+    if (T < 0 || top_k < 1 || top_k > FP8MLP_MAX_TOP_K || n_experts < 1 || n_experts > FP8MLP_MAX_EXPERTS ||
+        T > 0x7fffffff / top_k)
+        return FP8MLP_ERR_SHAPE;
+    if (counts == nullptr || offsets == nullptr || (T > 0 && (experts == nullptr || rows == nullptr))) return FP8MLP_ERR_ARG;
+    if (!aligned(experts, 4) || !aligned(counts, 4) || !aligned(offsets, 4) || !aligned(rows, 4)) return FP8MLP_ERR_ALIGN;
+    PlanArgs a{};
+    a.experts = experts; a.counts = counts; a.offsets = offsets; a.rows = rows;
+    a.n = T * top_k; a.E = n_experts;
+    int warps = static_cast<int>(a.n / 64 < kPlanWarps ? a.n / 64 : kPlanWarps);
+    if (warps < 4) warps = 4;
+    int cluster = 1;
+    while (cluster < kPlanMaxCluster && a.n > static_cast<int64_t>(cluster) * warps * 64) cluster *= 2;
+    const int64_t workers = static_cast<int64_t>(cluster) * warps;
+    a.per_warp = ((a.n + workers - 1) / workers + 31) / 32 * 32;
+    const size_t smem = static_cast<size_t>(warps) * n_experts * sizeof(int32_t);
+    FP8MLP_CUDA_CHECK(cudaFuncSetAttribute(plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                           kPlanWarps * FP8MLP_MAX_EXPERTS * static_cast<int>(sizeof(int32_t))));
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(cluster));
+    cfg.blockDim = dim3(static_cast<unsigned>(warps * 32));
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = static_cast<cudaStream_t>(stream);
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = static_cast<unsigned>(cluster);
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    FP8MLP_CUDA_CHECK(cudaLaunchKernelEx(&cfg, plan_kernel, static_cast<const PlanArgs>(a)));
+    FP8MLP_LAUNCH_CHECK();
+    return FP8MLP_OK;
+}
+
+extern "C" int fp8mlp_dispatch(int64_t T, int top_k, int64_t d, int dtype, const void* x, int64_t ld_x, const int32_t* rows,
+                               void* xe, int64_t n_rows, void* stream) {
+    const int rc = check_rows(T, top_k, d, dtype, x, ld_x, xe, n_rows, rows);
+    if (rc != FP8MLP_OK) return rc;
+    if (T == 0 || n_rows == 0) return FP8MLP_OK;
+    RowArgs a = row_args(T, top_k, d, dtype, ld_x, n_rows, rows);
+    a.src = static_cast<const uint8_t*>(x);
+    a.dst = static_cast<uint8_t*>(xe);
+    dim3 grid;
+    const int rg = unit_blocks(a, &grid);
+    if (rg != FP8MLP_OK) return rg;
+    FP8MLP_CUDA_CHECK(launch_chained(dispatch_kernel, grid, kRowThreads, 0, static_cast<cudaStream_t>(stream), a));
+    FP8MLP_LAUNCH_CHECK();
+    return FP8MLP_OK;
+}
+
+extern "C" int fp8mlp_combine(int64_t T, int top_k, int64_t d, int dtype, const void* ye, int64_t n_rows, const int32_t* rows,
+                              const float* weights, void* y, int64_t ld_y, void* stream) {
+    const int rc = check_rows(T, top_k, d, dtype, y, ld_y, ye, n_rows, rows);
+    if (rc != FP8MLP_OK) return rc;
+    if (!aligned(weights, 4)) return FP8MLP_ERR_ALIGN;
+    if (T == 0) return FP8MLP_OK;
+    RowArgs a = row_args(T, top_k, d, dtype, ld_y, n_rows, rows);
+    a.src = static_cast<const uint8_t*>(ye);
+    a.dst = static_cast<uint8_t*>(y);
+    a.weights = weights;
+    dim3 grid;
+    const int rg = unit_blocks(a, &grid);
+    if (rg != FP8MLP_OK) return rg;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (dtype == FP8MLP_F32) FP8MLP_CUDA_CHECK(launch_chained(combine_kernel<float>, grid, kRowThreads, 0, st, a));
+    else FP8MLP_CUDA_CHECK(launch_chained(combine_kernel<uint16_t>, grid, kRowThreads, 0, st, a));
+    FP8MLP_LAUNCH_CHECK();
+    return FP8MLP_OK;
+}
+
+extern "C" int fp8mlp_combine_backward(int64_t T, int top_k, int64_t d, int dtype, const void* dy, int64_t ld_dy,
+                                       const void* ye, int64_t n_rows, const int32_t* rows, const float* weights, void* dye,
+                                       float* d_weights, void* stream) {
+    const int rc = check_rows(T, top_k, d, dtype, dy, ld_dy, ye, n_rows, rows);
+    if (rc != FP8MLP_OK) return rc;
+    if (T == 0) return FP8MLP_OK;
+    if (weights == nullptr || d_weights == nullptr || (dye == nullptr && n_rows > 0) || (dye == ye && n_rows > 0))
+        return FP8MLP_ERR_ARG;
+    if (!aligned(dye, 16) || !aligned(weights, 4) || !aligned(d_weights, 4)) return FP8MLP_ERR_ALIGN;
+    RowArgs a = row_args(T, top_k, d, dtype, ld_dy, n_rows, rows);
+    a.src = static_cast<const uint8_t*>(ye);
+    a.dst = static_cast<uint8_t*>(dye);
+    a.dy = static_cast<const uint8_t*>(dy);
+    a.weights = weights;
+    a.d_weights = d_weights;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const dim3 grid(static_cast<unsigned>(T));
+    const int threads = a.units_per_row < static_cast<uint32_t>(kRowThreads) ? static_cast<int>((a.units_per_row + 31) / 32 * 32)
+                                                                             : kRowThreads;
+    if (dtype == FP8MLP_F32) FP8MLP_CUDA_CHECK(launch_chained(combine_backward_kernel<float>, grid, threads, 0, st, a));
+    else FP8MLP_CUDA_CHECK(launch_chained(combine_backward_kernel<uint16_t>, grid, threads, 0, st, a));
+    FP8MLP_LAUNCH_CHECK();
+    return FP8MLP_OK;
+}
