@@ -53,87 +53,96 @@ template <> __device__ __forceinline__ void unpack_unit<uint16_t>(const uint32_t
     for (int i = 0; i < 8; ++i) { v[2 * i] = bf16_lo(w[i]); v[2 * i + 1] = bf16_hi(w[i]); }
 }
 
-// Squares are summed in fp64: a square of an fp32 value is exact there and neither overflows nor underflows.  |g| keeps
-// its bit pattern, which orders like an unsigned integer with NaN above infinity, so a NaN survives the maximum.
-struct NormAcc {
-    double sum = 0.0;
+// Squares are summed in fp64: a square of an fp32 value is exact there and neither overflows nor underflows.  Two sums
+// per thread halve the chain of dependent additions.  |g| keeps its bit pattern, which orders like an unsigned integer
+// with NaN above infinity, so a NaN survives the maximum.
+template <bool INF> struct NormAcc;
+template <> struct NormAcc<false> {
+    double sum[2] = {0.0, 0.0};
+    __device__ __forceinline__ void add(float v, int i) { sum[i & 1] = fma(static_cast<double>(v), static_cast<double>(v), sum[i & 1]); }
+    __device__ __forceinline__ double word() const { return sum[0] + sum[1]; }
+};
+template <> struct NormAcc<true> {
     uint32_t top = 0;
-    bool inf;
-    __device__ __forceinline__ void add(float v) {
-        if (inf) top = max(top, __float_as_uint(v) & 0x7fffffffu);
-        else sum = fma(static_cast<double>(v), static_cast<double>(v), sum);
-    }
+    __device__ __forceinline__ void add(float v, int) { top = max(top, __float_as_uint(v) & 0x7fffffffu); }
+    __device__ __forceinline__ double word() const { return __longlong_as_double(static_cast<long long>(top)); }
 };
 
 // The tensor's elements lie in units of 32 bytes counted from the 32-byte boundary at or before its first element, so
 // every whole unit is one aligned access whatever the tensor's own alignment; the first and last may be part units.
-template <typename SRC>
-__device__ __forceinline__ void norm_chunk(const ClipSeg& s, int64_t chunk, NormAcc& acc) {
-    constexpr int N = GradUnit<SRC>::kElems;
-    const int64_t lead = static_cast<int64_t>(reinterpret_cast<uintptr_t>(s.g) & 31u) / static_cast<int64_t>(sizeof(SRC));
-    const SRC* base = reinterpret_cast<const SRC*>(s.g) - lead;
-    const int64_t last = lead + s.n;
-    const int64_t u0 = chunk * kChunkUnits + threadIdx.x;
-    uint32_t w[kUnroll][8];
-#pragma unroll
-    for (int k = 0; k < kUnroll; ++k) {
-        const int64_t e = (u0 + k * kClipThreads) * N;
-        if (e >= lead && e + N <= last) ld_global_nc_v8(base + e, w[k]);
+// A chunk without part units (all but the ends of a tensor) runs without a comparison per unit.
+template <typename SRC> struct ChunkView {
+    static constexpr int N = GradUnit<SRC>::kElems;
+    const SRC* base;
+    int64_t lead, last, e0;        // first and one past the last element, this thread's first, all counted from base
+    bool whole;
+    __device__ __forceinline__ ChunkView(const ClipSeg& s, uint32_t chunk) {
+        lead = static_cast<int64_t>(reinterpret_cast<uintptr_t>(s.g) & 31u) / static_cast<int64_t>(sizeof(SRC));
+        base = reinterpret_cast<const SRC*>(s.g) - lead;
+        last = lead + s.n;
+        const int64_t first = static_cast<int64_t>(chunk) * kChunkUnits * N;
+        whole = first >= lead && first + kChunkUnits * N <= last;
+        e0 = first + static_cast<int64_t>(threadIdx.x) * N;
     }
+};
+
+template <typename SRC, bool INF>
+__device__ __forceinline__ void norm_chunk(const ClipSeg& s, uint32_t chunk, NormAcc<INF>& acc) {
+    constexpr int N = GradUnit<SRC>::kElems;
+    const ChunkView<SRC> c(s, chunk);
+    if (c.whole) {
+        const SRC* p = c.base + c.e0;
+        uint32_t w[kUnroll][8];
 #pragma unroll
-    for (int k = 0; k < kUnroll; ++k) {
-        const int64_t e = (u0 + k * kClipThreads) * N;
-        if (e >= lead && e + N <= last) {
+        for (int k = 0; k < kUnroll; ++k) ld_global_nc_v8(p + k * kClipThreads * N, w[k]);
+#pragma unroll
+        for (int k = 0; k < kUnroll; ++k) {
             float v[N];
             unpack_unit<SRC>(w[k], v);
 #pragma unroll
-            for (int i = 0; i < N; ++i) acc.add(v[i]);
-        } else if (e < last && e + N > lead) {
+            for (int i = 0; i < N; ++i) acc.add(v[i], i);
+        }
+    } else {
+#pragma unroll 1
+        for (int64_t e = c.e0; e < c.e0 + kChunkUnits * N && e < c.last; e += kClipThreads * N) {
+#pragma unroll 1
             for (int i = 0; i < N; ++i)
-                if (e + i >= lead && e + i < last) acc.add(as_float(base[e + i]));
+                if (e + i >= c.lead && e + i < c.last) acc.add(as_float(c.base[e + i]), 0);
         }
     }
 }
 
 template <typename SRC>
-__device__ __forceinline__ void clip_chunk(const ClipSeg& s, int64_t chunk, float coef) {
+__device__ __forceinline__ void clip_chunk(const ClipSeg& s, uint32_t chunk, float coef) {
     constexpr int N = GradUnit<SRC>::kElems;
-    const int64_t lead = static_cast<int64_t>(reinterpret_cast<uintptr_t>(s.g) & 31u) / static_cast<int64_t>(sizeof(SRC));
-    const SRC* base = reinterpret_cast<const SRC*>(s.g) - lead;
-    SRC* out = reinterpret_cast<SRC*>(s.out) - lead;
-    const bool same = ((reinterpret_cast<uintptr_t>(s.out) ^ reinterpret_cast<uintptr_t>(s.g)) & 31u) == 0;
-    const int64_t last = lead + s.n;
-    const int64_t u0 = chunk * kChunkUnits + threadIdx.x;
-    uint32_t w[kUnroll][8];
+    const ChunkView<SRC> c(s, chunk);
+    SRC* const out = reinterpret_cast<SRC*>(s.out) - c.lead;
+    if (c.whole && ((reinterpret_cast<uintptr_t>(s.out) ^ reinterpret_cast<uintptr_t>(s.g)) & 31u) == 0) {
+        const SRC* p = c.base + c.e0;
+        SRC* q = out + c.e0;
+        uint32_t w[kUnroll][8];
 #pragma unroll
-    for (int k = 0; k < kUnroll; ++k) {
-        const int64_t e = (u0 + k * kClipThreads) * N;
-        if (e >= lead && e + N <= last) ld_global_v8(base + e, w[k]);
-    }
+        for (int k = 0; k < kUnroll; ++k) ld_global_v8(p + k * kClipThreads * N, w[k]);
 #pragma unroll
-    for (int k = 0; k < kUnroll; ++k) {
-        const int64_t e = (u0 + k * kClipThreads) * N;
-        if (e >= lead && e + N <= last) {
+        for (int k = 0; k < kUnroll; ++k) {
             float v[N];
             unpack_unit<SRC>(w[k], v);
 #pragma unroll
             for (int i = 0; i < N; ++i) v[i] = __fmul_rn(v[i], coef);
-            if (same) {
-                uint32_t o[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    if constexpr (N == 8) o[i] = __float_as_uint(v[i]);
-                    else o[i] = cvt_bf16x2(v[2 * i], v[2 * i + 1]);
-                }
-                st_global_v8(out + e, o);
-            } else {
-#pragma unroll
-                for (int i = 0; i < N; ++i) put(out + e + i, v[i]);
+            for (int i = 0; i < 8; ++i) {
+                if constexpr (N == 8) w[k][i] = __float_as_uint(v[i]);
+                else w[k][i] = cvt_bf16x2(v[2 * i], v[2 * i + 1]);
             }
-        } else if (e < last && e + N > lead) {
-            for (int i = 0; i < N; ++i)
-                if (e + i >= lead && e + i < last) put(out + e + i, __fmul_rn(as_float(base[e + i]), coef));
+            st_global_v8(q + k * kClipThreads * N, w[k]);
         }
+    } else {
+        // Ends, and buffers whose alignments differ: one element per thread at a time, neighbours in neighbouring threads.
+        const int64_t first = c.e0 - static_cast<int64_t>(threadIdx.x) * N;
+        const int64_t stop = first + kChunkUnits * N < c.last ? first + kChunkUnits * N : c.last;
+#pragma unroll 4
+        for (int64_t e = (first > c.lead ? first : c.lead) + threadIdx.x; e < stop; e += kClipThreads)
+            put(out + e, __fmul_rn(as_float(c.base[e]), coef));
     }
 }
 
@@ -165,24 +174,22 @@ __device__ __forceinline__ double block_reduce(double v, bool inf, double* part)
 }
 
 // A block's partial: the sum of its squares, or the bit pattern of its maximum (kept as an integer in the fp64 word).
-template <int kCap>
+template <int kCap, bool INF>
 __global__ void __launch_bounds__(kClipThreads, kClipBlocksPerSm) norm_kernel(const __grid_constant__ ClipArgs<kCap> a) {
     __shared__ double part[kClipThreads / 32];
     grid_dependency_wait();
     grid_launch_dependents();
-    NormAcc acc;
-    acc.inf = a.inf != 0;
+    NormAcc<INF> acc;
     for (uint32_t c = blockIdx.x; c < a.chunks; c += gridDim.x) {
         const ClipSeg& s = a.seg[find_seg(a, c)];
-        if (s.f32) norm_chunk<float>(s, c - s.first_chunk, acc);
-        else norm_chunk<uint16_t>(s, c - s.first_chunk, acc);
+        if (s.f32) norm_chunk<float, INF>(s, c - s.first_chunk, acc);
+        else norm_chunk<uint16_t, INF>(s, c - s.first_chunk, acc);
     }
-    double v = acc.inf ? __longlong_as_double(static_cast<long long>(acc.top)) : acc.sum;
-    v = block_reduce(v, acc.inf, part);
+    double v = block_reduce(acc.word(), INF, part);
     if (threadIdx.x == 0) {
         if (a.accumulate) {      // a further launch of the same call (a list longer than one launch holds)
             const double w = a.partial[blockIdx.x];
-            v = acc.inf ? __longlong_as_double(max(__double_as_longlong(v), __double_as_longlong(w))) : v + w;
+            v = INF ? __longlong_as_double(max(__double_as_longlong(v), __double_as_longlong(w))) : v + w;
         }
         a.partial[blockIdx.x] = v;
     }
@@ -222,8 +229,9 @@ __global__ void __launch_bounds__(kClipThreads, kClipBlocksPerSm) clip_kernel(co
     for (int64_t c = static_cast<int64_t>(a.chunks) - 1 - blockIdx.x; c >= 0; c -= gridDim.x) {
         const ClipSeg& s = a.seg[find_seg(a, static_cast<uint32_t>(c))];
         if (coef == 1.0f && s.out == s.g) continue;
-        if (s.f32) clip_chunk<float>(s, c - s.first_chunk, coef);
-        else clip_chunk<uint16_t>(s, c - s.first_chunk, coef);
+        const uint32_t chunk = static_cast<uint32_t>(c) - s.first_chunk;
+        if (s.f32) clip_chunk<float>(s, chunk, coef);
+        else clip_chunk<uint16_t>(s, chunk, coef);
     }
 }
 
@@ -270,7 +278,8 @@ int clip_launch(const ClipCall& c, int from, int to) {
         const int grid = chunks < c.blocks ? (chunks > 0 ? static_cast<int>(chunks) : 1) : c.blocks;
         FP8MLP_CUDA_CHECK(launch_chained(clip_kernel<kCap>, grid, kClipThreads, 0, c.st, a));
     } else {
-        FP8MLP_CUDA_CHECK(launch_chained(norm_kernel<kCap>, c.blocks, kClipThreads, 0, c.st, a));
+        auto kernel = c.inf ? norm_kernel<kCap, true> : norm_kernel<kCap, false>;
+        FP8MLP_CUDA_CHECK(launch_chained(kernel, c.blocks, kClipThreads, 0, c.st, a));
     }
     FP8MLP_LAUNCH_CHECK();
     return FP8MLP_OK;
