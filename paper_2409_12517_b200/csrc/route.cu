@@ -20,7 +20,7 @@ struct RouteArgs {
     int64_t T, ld, ld_d;
     int E, k, score, G, per, top_groups, group_top, renorm;
     float scale;
-    int wide, wide_d;      // rows of logits / d_logits start on a vector boundary
+    int wide, wide_b, wide_d;      // rows of logits, the bias, rows of d_logits start on a vector boundary
     int lane_groups;       // a group is a power-of-two number of whole lanes
 };
 
@@ -93,10 +93,11 @@ template <int LANES> __device__ __forceinline__ float seg_maxf(float v) {
     return v;
 }
 
-// sigma(x) = 1 / (1 + e^-x), written with e^-|x| so that neither end overflows and small values keep their digits
+// sigma(x) = 1 / (1 + e^-x), written with e^-|x| so that neither end overflows and small values keep their digits; the
+// reciprocal is of a number in [1, 2], where the special-function unit's is within one unit of the last place.
 __device__ __forceinline__ float sigmoid_exact(float x) {
     const float e = expf(-fabsf(x));
-    const float r = __fdiv_rn(1.0f, 1.0f + e);
+    const float r = rcp_approx(1.0f + e);
     return x >= 0.0f ? r : e * r;          // NaN takes the second branch and stays NaN
 }
 // 1 - sigma(x) = sigma(-x)
@@ -132,17 +133,36 @@ __device__ __forceinline__ uint32_t group_key(uint32_t k1, uint32_t k2, int grou
     return order_key(v + 0.0f);            // + 0: one zero only
 }
 
+// 8 keys into falling order (19 exchanges)
+__device__ __forceinline__ void exchange(uint32_t& a, uint32_t& b) {
+    const uint32_t hi = max(a, b);
+    b = min(a, b);
+    a = hi;
+}
+__device__ __forceinline__ void sort8(uint32_t (&k)[8]) {
+    exchange(k[0], k[2]); exchange(k[1], k[3]); exchange(k[4], k[6]); exchange(k[5], k[7]);
+    exchange(k[0], k[4]); exchange(k[1], k[5]); exchange(k[2], k[6]); exchange(k[3], k[7]);
+    exchange(k[0], k[1]); exchange(k[2], k[3]); exchange(k[4], k[5]); exchange(k[6], k[7]);
+    exchange(k[2], k[4]); exchange(k[3], k[5]);
+    exchange(k[1], k[4]); exchange(k[3], k[6]);
+    exchange(k[1], k[2]); exchange(k[3], k[4]); exchange(k[5], k[6]);
+}
+
+// The choice: every lane sorts its keys, eight at a time, and the token's lanes take the largest head k times.  What a
+// round costs decides the kernel's time (it is bound by instructions, not by memory), so a round moves keys only; which
+// expert a key belongs to is looked up once at the end, by k lanes side by side, in the unsorted keys in shared memory.
 template <int LANES, int V, typename SRC>
 __global__ void __launch_bounds__(kRouteThreads) route_kernel(const RouteArgs a) {
-    extern __shared__ float smem[];
+    extern __shared__ __align__(16) uint32_t smem[];
     constexpr int kTokens = kRouteThreads / LANES;
-    constexpr int kRow = LANES * V + 1;
+    constexpr int kRow = LANES * V + 4;                   // + 4: rows of neighbouring tokens start in other banks
+    constexpr int kLists = V / 8;
     const int lane = threadIdx.x % LANES, tok = threadIdx.x / LANES;
     const int seg_base = (threadIdx.x & 31) - lane;
-    float* sel_s = smem + tok * a.k;                                               // [kTokens][k] chosen scores ...
-    int32_t* sel_e = reinterpret_cast<int32_t*>(smem + kTokens * a.k) + tok * a.k;  // ... and experts
-    uint32_t* row_keys = reinterpret_cast<uint32_t*>(smem) + 2 * kTokens * a.k + tok * kRow;      // groups across lanes
-    uint32_t* group_keys = reinterpret_cast<uint32_t*>(smem) + 2 * kTokens * a.k + kTokens * kRow + tok * a.G;
+    uint32_t* row_key = smem + tok * kRow;                                          // this token's keys ...
+    float* row_s = reinterpret_cast<float*>(smem + kTokens * kRow) + tok * kRow;    // ... and scores
+    uint32_t* sel_key = smem + 2 * kTokens * kRow + 2 * tok * a.k;                  // a round's key, then its lane and count
+    uint32_t* group_keys = smem + 2 * kTokens * (kRow + a.k) + tok * a.G;
     const int64_t t = static_cast<int64_t>(blockIdx.x) * kTokens + tok;
     const bool live = t < a.T;
     const int e0 = lane * V;
@@ -150,6 +170,7 @@ __global__ void __launch_bounds__(kRouteThreads) route_kernel(const RouteArgs a)
     grid_launch_dependents();
 
     float s[V];
+    uint32_t key[kLists][8];
     if (live) {
         load_row<V, SRC>(static_cast<const SRC*>(a.logits) + t * a.ld, e0, a.E, a.wide != 0, s);
     } else {
@@ -165,207 +186,263 @@ __global__ void __launch_bounds__(kRouteThreads) route_kernel(const RouteArgs a)
 #pragma unroll
         for (int j = 0; j < V; ++j) s[j] = sigmoid_exact(s[j]);
     }
-    uint32_t key[V];
+    if (a.bias != nullptr) {
+        float b[V];
+        load_row<V, float>(a.bias, e0, a.E, a.wide_b != 0, b);      // past the last expert: -inf
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-        const float c = a.bias != nullptr && e0 + j < a.E ? s[j] + __ldg(a.bias + e0 + j) : s[j];
-        key[j] = (masked >> j & 1u) != 0u || !(c > -CUDART_INF_F) ? 0u : order_key(c);
+        for (int j = 0; j < V; ++j) {
+            row_s[e0 + j] = s[j];
+            s[j] += b[j];
+        }
     }
+#pragma unroll
+    for (int j = 0; j < V; ++j) key[j / 8][j % 8] = (masked >> j & 1u) != 0u || !(s[j] > -CUDART_INF_F) ? 0u : order_key(s[j]);
 
-    if (a.G > 1) {
-        if (a.lane_groups) {
-            const int width = a.per / V;                     // lanes of a group
+    if (a.G > 1 && !a.lane_groups) {                      // groups that do not fall on lanes: through shared memory
+#pragma unroll
+        for (int j = 0; j < V; ++j) row_key[e0 + j] = key[j / 8][j % 8];
+        __syncwarp();
+        for (int g = lane; g < a.G; g += LANES) {
             uint32_t k1 = 0, k2 = 0;
-#pragma unroll
-            for (int j = 0; j < V; ++j) { k2 = max(k2, min(k1, key[j])); k1 = max(k1, key[j]); }
-            for (int o = 1; o < width; o <<= 1) {
-                const uint32_t b1 = __shfl_xor_sync(kAll, k1, o), b2 = __shfl_xor_sync(kAll, k2, o);
-                merge_top2(k1, k2, b1, b2);
+            for (int i = 0; i < a.per; ++i) {
+                const uint32_t v = row_key[g * a.per + i];
+                k2 = max(k2, min(k1, v));
+                k1 = max(k1, v);
             }
-            const uint32_t gk = group_key(k1, k2, a.group_top);
-            const int mine = lane / width;
-            int rank = 0;
-            for (int g = 0; g < a.G; ++g) {
-                const uint32_t other = __shfl_sync(kAll, gk, seg_base + g * width);
-                rank += (other > gk || (other == gk && g < mine)) ? 1 : 0;
-            }
-            if (rank >= a.top_groups) {
+            group_keys[g] = group_key(k1, k2, a.group_top);
+        }
+        __syncwarp();
+        int last = -1;
+        bool keep = false;
 #pragma unroll
-                for (int j = 0; j < V; ++j) key[j] = 0u;
-            }
-        } else {
-#pragma unroll
-            for (int j = 0; j < V; ++j) row_keys[e0 + j] = key[j];
-            __syncwarp();
-            for (int g = lane; g < a.G; g += LANES) {
-                uint32_t k1 = 0, k2 = 0;
-                for (int i = 0; i < a.per; ++i) {
-                    const uint32_t v = row_keys[g * a.per + i];
-                    k2 = max(k2, min(k1, v));
-                    k1 = max(k1, v);
+        for (int j = 0; j < V; ++j) {
+            const int g = (e0 + j) / a.per;
+            if (g != last && e0 + j < a.E) {
+                last = g;
+                const uint32_t gk = group_keys[g];
+                int rank = 0;
+                for (int i = 0; i < a.G; ++i) {
+                    const uint32_t other = group_keys[i];
+                    rank += (other > gk || (other == gk && i < g)) ? 1 : 0;
                 }
-                group_keys[g] = group_key(k1, k2, a.group_top);
+                keep = rank < a.top_groups;
             }
-            __syncwarp();
-            int last = -1;
-            bool keep = false;
+            if (!keep) key[j / 8][j % 8] = 0u;
+        }
+    }
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
-                const int g = (e0 + j) / a.per;
-                if (g != last && e0 + j < a.E) {
-                    last = g;
-                    const uint32_t gk = group_keys[g];
-                    int rank = 0;
-                    for (int i = 0; i < a.G; ++i) {
-                        const uint32_t other = group_keys[i];
-                        rank += (other > gk || (other == gk && i < g)) ? 1 : 0;
-                    }
-                    keep = rank < a.top_groups;
-                }
-                if (!keep) key[j] = 0u;
-            }
+    for (int j = 0; j < V; j += 4)
+        *reinterpret_cast<uint4*>(row_key + e0 + j) = make_uint4(key[j / 8][j % 8], key[j / 8][j % 8 + 1], key[j / 8][j % 8 + 2], key[j / 8][j % 8 + 3]);
+#pragma unroll
+    for (int l = 0; l < kLists; ++l) sort8(key[l]);
+
+    if (a.G > 1 && a.lane_groups) {
+        const int width = a.per / V;                     // lanes of a group
+        uint32_t k1 = key[0][0], k2 = key[0][1];
+#pragma unroll
+        for (int l = 1; l < kLists; ++l) merge_top2(k1, k2, key[l][0], key[l][1]);
+        for (int o = 1; o < width; o <<= 1) {
+            const uint32_t b1 = __shfl_xor_sync(kAll, k1, o), b2 = __shfl_xor_sync(kAll, k2, o);
+            merge_top2(k1, k2, b1, b2);
+        }
+        const uint32_t gk = group_key(k1, k2, a.group_top);
+        const int mine = lane / width;
+        int rank = 0;
+        for (int g = 0; g < a.G; ++g) {
+            const uint32_t other = __shfl_sync(kAll, gk, seg_base + g * width);
+            rank += (other > gk || (other == gk && g < mine)) ? 1 : 0;
+        }
+        if (rank >= a.top_groups) {
+#pragma unroll
+            for (int l = 0; l < kLists; ++l)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) key[l][j] = 0u;
         }
     }
 
-    uint32_t best = 0;
+    uint32_t best = key[0][0];
 #pragma unroll
-    for (int j = 0; j < V; ++j) best = max(best, key[j]);
+    for (int l = 1; l < kLists; ++l) best = max(best, key[l][0]);
+    uint32_t prev = 0, count = 0;
     for (int r = 0; r < a.k; ++r) {
         const uint32_t top = seg_max<LANES>(best);
-        // the lowest lane among equals holds the lowest expert, its first equal key the lowest of these
+        // the lowest lane among equals holds the lowest expert; how often it gave this key before tells which of its equals
         const uint32_t holders = (__ballot_sync(kAll, best == top) >> seg_base) & (LANES == 32 ? kAll : (1u << (LANES & 31)) - 1u);
         if (lane == __ffs(holders) - 1) {
-            int at = -1;
-            float score = 0.0f;
-            if (top != 0u) {
+            count = top == prev ? count + 1u : 0u;
+            prev = top;
+            sel_key[2 * r] = top;
+            sel_key[2 * r + 1] = static_cast<uint32_t>(lane) | count << 8;
+            bool taken = false;
+            best = 0;
 #pragma unroll
-                for (int j = V - 1; j >= 0; --j)
-                    if (key[j] == top) { at = j; score = s[j]; }
-                best = 0;
+            for (int l = 0; l < kLists; ++l) {
+                if (!taken && key[l][0] == top) {
+                    taken = true;
 #pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    if (j == at) key[j] = 0u;
-                    best = max(best, key[j]);
+                    for (int j = 0; j < 7; ++j) key[l][j] = key[l][j + 1];
+                    key[l][7] = 0u;
                 }
+                best = max(best, key[l][0]);
             }
-            sel_e[r] = at < 0 ? -1 : e0 + at;
-            sel_s[r] = score;
         }
     }
     __syncwarp();
     float D = 0.0f;
-    for (int r = 0; r < a.k; ++r) D += sel_s[r];
+    constexpr int kMine = LANES >= 4 ? (FP8MLP_MAX_TOP_K + LANES - 1) / LANES : 8;      // k <= LANES * 8 where LANES < 4
+    float score[kMine];
+    int32_t expert[kMine];
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) {
+        const int r = lane + i * LANES;
+        score[i] = 0.0f;
+        expert[i] = -1;
+        if (r < a.k && sel_key[2 * r] != 0u) {
+            const uint32_t want = sel_key[2 * r], who = sel_key[2 * r + 1];
+            const int from = static_cast<int>(who & 255u) * V;
+            uint32_t skip = who >> 8;
+#pragma unroll
+            for (int j = 0; j < V; j += 4) {
+                const uint4 q = *reinterpret_cast<const uint4*>(row_key + from + j);
+                const uint32_t four[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+                for (int m = 0; m < 4; ++m) {
+                    if (four[m] == want) {
+                        if (skip == 0u) expert[i] = from + j + m;
+                        --skip;
+                    }
+                }
+            }
+            score[i] = a.bias != nullptr ? row_s[expert[i]] : key_value(want);
+        }
+        D += score[i];
+    }
+    D = seg_sum<LANES>(D);
     if (live) {
-        for (int r = lane; r < a.k; r += LANES) {
-            const float v = sel_s[r];
-            const float w = a.renorm ? (D == 0.0f ? 0.0f : __fdiv_rn(v, D)) : v;
-            a.experts[t * a.k + r] = sel_e[r];
-            a.weights[t * a.k + r] = w * a.scale;
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) {
+            const int r = lane + i * LANES;
+            if (r < a.k) {
+                const float w = a.renorm ? (D == 0.0f ? 0.0f : __fdiv_rn(score[i], D)) : score[i];
+                a.experts[t * a.k + r] = expert[i];
+                a.weights[t * a.k + r] = w * a.scale;
+            }
         }
     }
 }
 
+// one zero after the other: this token's lanes clear its row of the gradient
+template <int LANES, typename SRC>
+__device__ __forceinline__ void clear_row(SRC* dst, int E, bool wide, int lane) {
+    int done = 0;
+    if (wide) {
+        const float zero[8] = {};
+        for (int e = lane * 8; e + 8 <= E; e += LANES * 8) store8(dst + e, zero);
+        done = E & ~7;
+    }
+    for (int e = done + lane; e < E; e += LANES) store1(dst + e, 0.0f);
+}
+
+// Gradient where only the chosen experts have one: with r_j = s_j / D the softmax's own normaliser cancels, and a
+// sigmoid's score depends on its logit alone.  So k logits are read, not the row; the row is cleared while they are on
+// their way and the k values follow.  One lane per slot, 32 / LANES tokens per warp.
+template <int LANES, typename SRC>
+__global__ void __launch_bounds__(kRouteThreads) route_backward_sparse_kernel(const RouteArgs a) {
+    constexpr int kTokens = kRouteThreads / LANES;
+    const int lane = threadIdx.x % LANES, tok = threadIdx.x / LANES;
+    const int64_t t = static_cast<int64_t>(blockIdx.x) * kTokens + tok;
+    const bool live = t < a.T;
+    grid_dependency_wait();
+    grid_launch_dependents();
+    const bool slot = live && lane < a.k;
+    int e = slot ? __ldg(a.experts + t * a.k + lane) : -1;
+    const float dw_raw = slot ? __ldg(a.d_weights + t * a.k + lane) : 0.0f;
+    if (e < 0 || e >= a.E) e = -1;
+    const float dw = e < 0 ? 0.0f : dw_raw;
+    const float x = e < 0 ? -CUDART_INF_F : load1<SRC>(static_cast<const SRC*>(a.logits) + t * a.ld + e);
+    SRC* dst = static_cast<SRC*>(a.d_logits) + (live ? t : 0) * a.ld_d;
+    if (live) clear_row<LANES, SRC>(dst, a.E, a.wide_d != 0, lane);
+    float s;
+    if (a.score == FP8MLP_SCORE_SOFTMAX) {
+        const float m = seg_maxf<LANES>(x);
+        s = e < 0 ? 0.0f : expf(x - m);
+    } else {
+        s = e < 0 ? 0.0f : sigmoid_exact(x);
+    }
+    float g = s * dw;
+    if (a.renorm) {
+        const float D = seg_sum<LANES>(s);
+        const float r = D == 0.0f ? 0.0f : __fdiv_rn(s, D);
+        g = r * (dw - seg_sum<LANES>(r * dw));
+    }
+    if (a.score == FP8MLP_SCORE_SIGMOID) g *= sigmoid_exact(-x);      // 1 - s
+    __syncwarp();                                                      // the row is clear before its k values are written
+    if (e >= 0) store1(dst + e, a.scale * g);
+}
+
+// Gradient of softmax weights that are not renormalised: every expert of the row has one.
 template <int LANES, int V, typename SRC>
-__global__ void __launch_bounds__(kRouteThreads) route_backward_kernel(const RouteArgs a) {
-    extern __shared__ float smem[];
+__global__ void __launch_bounds__(kRouteThreads) route_backward_dense_kernel(const RouteArgs a) {
+    extern __shared__ __align__(16) uint32_t smem[];
     constexpr int kTokens = kRouteThreads / LANES;
     constexpr int kRow = LANES * V + 4;
     const int lane = threadIdx.x % LANES, tok = threadIdx.x / LANES;
-    float* row = smem + tok * kRow;                                  // gradient of the row (or of its scores)
-    float* sel_x = smem + kTokens * kRow + tok * a.k;                // chosen logits, then s or r
-    float* sel_w = sel_x + kTokens * a.k;                            // their d_weights
-    int32_t* sel_e = reinterpret_cast<int32_t*>(sel_w + kTokens * a.k);
+    float* row = reinterpret_cast<float*>(smem) + tok * kRow;         // gradient of the row's scores, then of its logits
     const int64_t t = static_cast<int64_t>(blockIdx.x) * kTokens + tok;
     const bool live = t < a.T;
     const int e0 = lane * V;
-    const bool dense = a.score == FP8MLP_SCORE_SOFTMAX && !a.renorm;
     grid_dependency_wait();
     grid_launch_dependents();
-    const SRC* src = static_cast<const SRC*>(a.logits) + (live ? t : 0) * a.ld;
-
+    float s[V];
+    if (live) {
+        load_row<V, SRC>(static_cast<const SRC*>(a.logits) + t * a.ld, e0, a.E, a.wide != 0, s);
+    } else {
 #pragma unroll
-    for (int j = 0; j < V; ++j) row[lane + j * LANES] = 0.0f;
-    for (int r = lane; r < a.k; r += LANES) {
-        int e = live ? __ldg(a.experts + t * a.k + r) : -1;
-        if (e < 0 || e >= a.E) e = -1;
-        sel_e[r] = e;
-        sel_w[r] = e < 0 ? 0.0f : __ldg(a.d_weights + t * a.k + r);
-        sel_x[r] = e < 0 ? -CUDART_INF_F : load1<SRC>(src + e);
+        for (int j = 0; j < V; ++j) s[j] = -CUDART_INF_F;
     }
+#pragma unroll
+    for (int j = 0; j < V; j += 4) *reinterpret_cast<float4*>(row + e0 + j) = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     __syncwarp();
     bool any = false;
-    float m = -CUDART_INF_F;
-    for (int r = 0; r < a.k; ++r) { any |= sel_e[r] >= 0; m = fmaxf(m, sel_x[r]); }
-
-    if (dense) {
-        for (int r = lane; r < a.k; r += LANES)
-            if (sel_e[r] >= 0) row[sel_e[r]] = a.scale * sel_w[r];
-        __syncwarp();
-        float s[V];
-        if (live) {
-            load_row<V, SRC>(src, e0, a.E, a.wide != 0, s);
-        } else {
-#pragma unroll
-            for (int j = 0; j < V; ++j) s[j] = -CUDART_INF_F;
-        }
-        softmax_row<LANES, V>(s);
-        float dot = 0.0f;
-#pragma unroll
-        for (int j = 0; j < V; ++j) dot += s[j] * row[e0 + j];
-        dot = seg_sum<LANES>(dot);
-        __syncwarp();
-#pragma unroll
-        for (int j = 0; j < V; ++j) row[e0 + j] = any ? s[j] * (row[e0 + j] - dot) : 0.0f;
-    } else {
-        // s_j (sigmoid) or e^(x_j - max) (softmax: its normaliser cancels in r_j)
-        __syncwarp();
-        float x_mine[(FP8MLP_MAX_TOP_K + LANES - 1) / LANES];
-#pragma unroll
-        for (int i = 0; i < (FP8MLP_MAX_TOP_K + LANES - 1) / LANES; ++i) {
-            const int r = lane + i * LANES;
-            if (r < a.k) {
-                x_mine[i] = sel_x[r];
-                sel_x[r] = sel_e[r] < 0 ? 0.0f : (a.score == FP8MLP_SCORE_SOFTMAX ? expf(x_mine[i] - m) : sigmoid_exact(x_mine[i]));
-            }
-        }
-        __syncwarp();
-        float D = 0.0f, dot = 0.0f;
-        if (a.renorm) {
-            for (int r = 0; r < a.k; ++r) D += sel_x[r];
-            for (int r = 0; r < a.k; ++r) dot += sel_w[r] * (D == 0.0f ? 0.0f : __fdiv_rn(sel_x[r], D));
-        }
-#pragma unroll
-        for (int i = 0; i < (FP8MLP_MAX_TOP_K + LANES - 1) / LANES; ++i) {
-            const int r = lane + i * LANES;
-            if (r < a.k && sel_e[r] >= 0) {
-                float g = a.renorm ? (D == 0.0f ? 0.0f : __fdiv_rn(sel_x[r], D)) * (sel_w[r] - dot) : sel_x[r] * sel_w[r];
-                if (a.score == FP8MLP_SCORE_SIGMOID) g *= sigmoid_exact(-x_mine[i]);      // 1 - s
-                row[sel_e[r]] = a.scale * g;
+    if (live) {
+        for (int r = lane; r < a.k; r += LANES) {
+            const int e = __ldg(a.experts + t * a.k + r);
+            if (e >= 0 && e < a.E) {
+                row[e] = a.scale * __ldg(a.d_weights + t * a.k + r);
+                any = true;
             }
         }
     }
+    any = seg_max<LANES>(any ? 1u : 0u) != 0u;
+    softmax_row<LANES, V>(s);
     __syncwarp();
-    if (!live) return;
+    float ds[V], dot = 0.0f;
+#pragma unroll
+    for (int j = 0; j < V; j += 4) *reinterpret_cast<float4*>(&ds[j]) = *reinterpret_cast<const float4*>(row + e0 + j);
+#pragma unroll
+    for (int j = 0; j < V; ++j) dot += s[j] * ds[j];
+    dot = seg_sum<LANES>(dot);
+#pragma unroll
+    for (int j = 0; j < V; ++j) s[j] = any ? s[j] * (ds[j] - dot) : 0.0f;
     SRC* dst = static_cast<SRC*>(a.d_logits) + t * a.ld_d;
     if (a.wide_d) {
+        if (!live) return;
 #pragma unroll
         for (int b = 0; b < V; b += 8) {
-            const int e = e0 + b;
-            float v[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = row[e + i];
-            if (e + 8 <= a.E) {
-                store8(dst + e, v);
+            if (e0 + b + 8 <= a.E) {
+                store8(dst + e0 + b, &s[b]);
             } else {
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
-                    if (e + i < a.E) store1(dst + e + i, v[i]);
+                    if (e0 + b + i < a.E) store1(dst + e0 + b + i, s[b + i]);
             }
         }
-    } else {
+    } else {                       // through shared memory: neighbouring lanes write neighbouring elements
 #pragma unroll
-        for (int j = 0; j < V; ++j)
-            if (lane + j * LANES < a.E) store1(dst + lane + j * LANES, row[lane + j * LANES]);
+        for (int j = 0; j < V; j += 4) *reinterpret_cast<float4*>(row + e0 + j) = make_float4(s[j], s[j + 1], s[j + 2], s[j + 3]);
+        __syncwarp();
+        if (!live) return;
+        for (int e = lane; e < a.E; e += LANES) store1(dst + e, row[e]);
     }
 }
 
@@ -412,41 +489,65 @@ RouteArgs route_args(const fp8mlp_router* r, int64_t T, const void* logits, int6
     return a;
 }
 
-// BWD: the gradient kernel.  LANES x V covers the row with the fewest lanes that keep V at 8; beyond 256 experts V grows.
-template <bool BWD, int LANES, int V>
-int launch_route(RouteArgs a, int dtype, cudaStream_t st) {
+template <int LANES>
+int launch_tokens(void (*kernel)(const RouteArgs), const RouteArgs& a, size_t smem, cudaStream_t st) {
     constexpr int kTokens = kRouteThreads / LANES;
-    a.lane_groups = a.G > 1 && a.per % V == 0 && ((a.per / V) & (a.per / V - 1)) == 0;
-    size_t floats = static_cast<size_t>(kTokens) * a.k * (BWD ? 3 : 2);
-    if (BWD) floats += static_cast<size_t>(kTokens) * (LANES * V + 4);
-    else if (a.G > 1 && !a.lane_groups) floats += static_cast<size_t>(kTokens) * (LANES * V + 1 + a.G);
-    const size_t smem = floats * sizeof(float);        // at most 22 KiB over all shapes
     const int64_t blocks = (a.T + kTokens - 1) / kTokens;
     if (blocks > 0x7fffffff) return FP8MLP_ERR_SHAPE;
-    const dim3 grid(static_cast<unsigned>(blocks));
-    cudaError_t e;
-    if (dtype == FP8MLP_F32) {
-        auto kernel = BWD ? route_backward_kernel<LANES, V, float> : route_kernel<LANES, V, float>;
-        e = launch_chained(kernel, grid, kRouteThreads, smem, st, a);
-    } else {
-        auto kernel = BWD ? route_backward_kernel<LANES, V, uint16_t> : route_kernel<LANES, V, uint16_t>;
-        e = launch_chained(kernel, grid, kRouteThreads, smem, st, a);
-    }
-    FP8MLP_CUDA_CHECK(e);
+    if (smem > 48 * 1024) FP8MLP_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 64 * 1024));
+    FP8MLP_CUDA_CHECK(launch_chained(kernel, dim3(static_cast<unsigned>(blocks)), kRouteThreads, smem, st, a));
     FP8MLP_LAUNCH_CHECK();
     return FP8MLP_OK;
 }
 
-template <bool BWD>
-int dispatch_route(const RouteArgs& a, int dtype, cudaStream_t st) {
-    if (a.E <= 8) return launch_route<BWD, 1, 8>(a, dtype, st);
-    if (a.E <= 16) return launch_route<BWD, 2, 8>(a, dtype, st);
-    if (a.E <= 32) return launch_route<BWD, 4, 8>(a, dtype, st);
-    if (a.E <= 64) return launch_route<BWD, 8, 8>(a, dtype, st);
-    if (a.E <= 128) return launch_route<BWD, 16, 8>(a, dtype, st);
-    if (a.E <= 256) return launch_route<BWD, 32, 8>(a, dtype, st);
-    if (a.E <= 512) return launch_route<BWD, 32, 16>(a, dtype, st);
-    return launch_route<BWD, 32, 32>(a, dtype, st);
+template <int LANES, int V>
+int launch_route(RouteArgs a, int dtype, cudaStream_t st) {
+    constexpr int kTokens = kRouteThreads / LANES;
+    a.lane_groups = a.G > 1 && a.per % V == 0 && ((a.per / V) & (a.per / V - 1)) == 0;
+    size_t words = static_cast<size_t>(kTokens) * (2 * a.k + 2 * (LANES * V + 4));
+    if (a.G > 1 && !a.lane_groups) words += static_cast<size_t>(kTokens) * a.G;
+    // below 26 KiB up to 512 experts, 50 KiB for 1024 in 1024 groups
+    return launch_tokens<LANES>(dtype == FP8MLP_F32 ? route_kernel<LANES, V, float> : route_kernel<LANES, V, uint16_t>, a,
+                                words * sizeof(float), st);
+}
+template <int LANES, int V>
+int launch_backward_dense(const RouteArgs& a, int dtype, cudaStream_t st) {
+    return launch_tokens<LANES>(dtype == FP8MLP_F32 ? route_backward_dense_kernel<LANES, V, float>
+                                                    : route_backward_dense_kernel<LANES, V, uint16_t>,
+                                a, (kRouteThreads / LANES) * (LANES * V + 4) * sizeof(float), st);
+}
+template <int LANES>
+int launch_backward_sparse(const RouteArgs& a, int dtype, cudaStream_t st) {
+    return launch_tokens<LANES>(dtype == FP8MLP_F32 ? route_backward_sparse_kernel<LANES, float>
+                                                    : route_backward_sparse_kernel<LANES, uint16_t>, a, 0, st);
+}
+
+// LANES x V covers the row with the fewest lanes that keep V at 8; beyond 256 experts V grows.
+int run_route(const RouteArgs& a, int dtype, cudaStream_t st) {
+    if (a.E <= 8) return launch_route<1, 8>(a, dtype, st);
+    if (a.E <= 16) return launch_route<2, 8>(a, dtype, st);
+    if (a.E <= 32) return launch_route<4, 8>(a, dtype, st);
+    if (a.E <= 64) return launch_route<8, 8>(a, dtype, st);
+    if (a.E <= 128) return launch_route<16, 8>(a, dtype, st);
+    if (a.E <= 256) return launch_route<32, 8>(a, dtype, st);
+    if (a.E <= 512) return launch_route<32, 16>(a, dtype, st);
+    return launch_route<32, 32>(a, dtype, st);
+}
+int run_route_backward(const RouteArgs& a, int dtype, cudaStream_t st) {
+    if (a.score == FP8MLP_SCORE_SIGMOID || a.renorm) {
+        if (a.k <= 4) return launch_backward_sparse<4>(a, dtype, st);
+        if (a.k <= 8) return launch_backward_sparse<8>(a, dtype, st);
+        if (a.k <= 16) return launch_backward_sparse<16>(a, dtype, st);
+        return launch_backward_sparse<32>(a, dtype, st);
+    }
+    if (a.E <= 8) return launch_backward_dense<1, 8>(a, dtype, st);
+    if (a.E <= 16) return launch_backward_dense<2, 8>(a, dtype, st);
+    if (a.E <= 32) return launch_backward_dense<4, 8>(a, dtype, st);
+    if (a.E <= 64) return launch_backward_dense<8, 8>(a, dtype, st);
+    if (a.E <= 128) return launch_backward_dense<16, 8>(a, dtype, st);
+    if (a.E <= 256) return launch_backward_dense<32, 8>(a, dtype, st);
+    if (a.E <= 512) return launch_backward_dense<32, 16>(a, dtype, st);
+    return launch_backward_dense<32, 32>(a, dtype, st);
 }
 
 }  // namespace
@@ -468,7 +569,8 @@ extern "C" int fp8mlp_route(const fp8mlp_router* r, int64_t T, const void* logit
         return FP8MLP_ERR_ALIGN;
     RouteArgs a = route_args(r, T, logits, ld, esize);
     a.bias = bias; a.experts = experts; a.weights = weights;
-    return dispatch_route<false>(a, dtype, static_cast<cudaStream_t>(stream));
+    a.wide_b = multiple_of(bias, 32);
+    return run_route(a, dtype, static_cast<cudaStream_t>(stream));
 }
 
 extern "C" int fp8mlp_route_backward(const fp8mlp_router* r, int64_t T, const void* logits, int dtype, int64_t ld,
@@ -486,7 +588,7 @@ extern "C" int fp8mlp_route_backward(const fp8mlp_router* r, int64_t T, const vo
     RouteArgs a = route_args(r, T, logits, ld, esize);
     a.experts = const_cast<int32_t*>(experts); a.d_weights = d_weights; a.d_logits = d_logits; a.ld_d = ld_d;
     a.wide_d = multiple_of(d_logits, 8 * esize) && ld_d % 8 == 0;
-    return dispatch_route<true>(a, dtype, static_cast<cudaStream_t>(stream));
+    return run_route_backward(a, dtype, static_cast<cudaStream_t>(stream));
 }
 
 extern "C" int fp8mlp_route_update_bias(int n_experts, const int32_t* counts, float rate, float* bias, void* stream) {
