@@ -112,24 +112,33 @@ __global__ void __launch_bounds__(kPlanWarps * 32) plan_kernel(const PlanArgs a)
 }
 
 // ---------------------------------------------------------------- rows
-// A unit is 16 bytes of a row: 8 bf16 or 4 fp32 elements.
-template <typename T> struct RowUnit;
-template <> struct RowUnit<uint16_t> { static constexpr int kElems = 8; };
-template <> struct RowUnit<float> { static constexpr int kElems = 4; };
-
-__device__ __forceinline__ void unpack(const uint4& w, float (&v)[8]) {
-    v[0] = bf16_lo(w.x); v[1] = bf16_hi(w.x); v[2] = bf16_lo(w.y); v[3] = bf16_hi(w.y);
-    v[4] = bf16_lo(w.z); v[5] = bf16_hi(w.z); v[6] = bf16_lo(w.w); v[7] = bf16_hi(w.w);
+// Rows are moved in units of W 32-bit words: 8 (32 bytes) where every row starts on a 32-byte boundary, else 4.  A token's
+// threads walk its row together; what a kernel reads for several slots it reads before it uses or writes any of it, so
+// that the loads overlap.
+template <int W> __device__ __forceinline__ void load_unit(const uint8_t* p, uint32_t (&w)[W]) {
+    if constexpr (W == 8) {
+        ld_global_nc_v8(p, w);
+    } else {
+        const uint4 v = ld_global_nc_v4(p);
+        w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+    }
 }
-__device__ __forceinline__ void unpack(const uint4& w, float (&v)[4]) {
-    v[0] = __uint_as_float(w.x); v[1] = __uint_as_float(w.y); v[2] = __uint_as_float(w.z); v[3] = __uint_as_float(w.w);
+template <int W> __device__ __forceinline__ void store_unit(uint8_t* p, const uint32_t (&w)[W]) {
+    if constexpr (W == 8) st_global_v8(p, w);
+    else st_global_v4(p, w[0], w[1], w[2], w[3]);
 }
-__device__ __forceinline__ void store_unit(void* p, const float (&v)[8]) {
-    st_global_v4(p, cvt_bf16x2(v[0], v[1]), cvt_bf16x2(v[2], v[3]), cvt_bf16x2(v[4], v[5]), cvt_bf16x2(v[6], v[7]));
-}
-__device__ __forceinline__ void store_unit(void* p, const float (&v)[4]) {
-    st_global_v4(p, __float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
-}
+// elements of a word: two bf16 or one fp32
+template <typename T> struct Word;
+template <> struct Word<uint16_t> {
+    static constexpr int kElems = 2;
+    static __device__ __forceinline__ void get(uint32_t w, float* v) { v[0] = bf16_lo(w); v[1] = bf16_hi(w); }
+    static __device__ __forceinline__ uint32_t put(const float* v) { return cvt_bf16x2(v[0], v[1]); }
+};
+template <> struct Word<float> {
+    static constexpr int kElems = 1;
+    static __device__ __forceinline__ void get(uint32_t w, float* v) { v[0] = __uint_as_float(w); }
+    static __device__ __forceinline__ uint32_t put(const float* v) { return __float_as_uint(v[0]); }
+};
 
 constexpr int kRowThreads = 256;
 
@@ -138,58 +147,92 @@ struct RowArgs {
     uint8_t* dst;              // dispatch: xe; combine: y; combine_backward: dye
     const uint8_t* dy;         // combine_backward
     const int32_t* rows; const float* weights; float* d_weights;
-    int64_t T, n_rows;
+    int64_t T;
     int64_t token_bytes;       // row stride of the token side (x, y, dy)
-    int64_t row_bytes;         // of the expert side: its rows are contiguous
-    int64_t units;             // T * units_per_row (dispatch, combine)
-    uint32_t units_per_row;
+    uint32_t n_rows;
+    uint32_t row_bytes;        // a row; those of the expert side are contiguous
     int k;
+    int threads_per_token;     // of a block, whose threads hold blockDim.x / threads_per_token tokens
 };
 
+// the byte offset of a slot's row, or -1
+__device__ __forceinline__ int64_t row_offset(const RowArgs& a, int64_t slot) {
+    const uint32_t row = static_cast<uint32_t>(__ldg(a.rows + slot));        // negative: beyond every n_rows
+    return row < a.n_rows ? static_cast<int64_t>(row) * a.row_bytes : -1;
+}
+
+template <int W>
 __global__ void __launch_bounds__(kRowThreads) dispatch_kernel(const RowArgs a) {
     grid_dependency_wait();
     grid_launch_dependents();
-    const int64_t u = static_cast<int64_t>(blockIdx.x) * kRowThreads + threadIdx.x;
-    if (u >= a.units) return;
-    const int64_t t = u / a.units_per_row;
-    const int64_t at = (u - t * a.units_per_row) * 16;
-    const uint4 v = ld_global_nc_v4(a.src + t * a.token_bytes + at);
-    for (int j = 0; j < a.k; ++j) {
-        const int64_t row = __ldg(a.rows + t * a.k + j);
-        if (row >= 0 && row < a.n_rows) st_global_v4(a.dst + row * a.row_bytes + at, v.x, v.y, v.z, v.w);
+    const int in_block = threadIdx.x / a.threads_per_token, lane = threadIdx.x - in_block * a.threads_per_token;
+    const int64_t t = static_cast<int64_t>(blockIdx.x) * (blockDim.x / a.threads_per_token) + in_block;
+    if (t >= a.T) return;
+    const uint32_t step = a.threads_per_token * W * 4;
+    for (uint32_t at = lane * W * 4; at < a.row_bytes; at += step) {
+        uint32_t w[W];
+        load_unit<W>(a.src + t * a.token_bytes + at, w);
+#pragma unroll 4
+        for (int j = 0; j < a.k; ++j) {
+            const int64_t off = row_offset(a, t * a.k + j);
+            if (off >= 0) store_unit<W>(a.dst + off + at, w);
+        }
     }
 }
 
-template <typename T>
+constexpr int kCombineSlots = 4;       // slots whose loads are in flight together
+
+template <typename T, int W, bool WEIGHTED>
 __global__ void __launch_bounds__(kRowThreads) combine_kernel(const RowArgs a) {
-    constexpr int N = RowUnit<T>::kElems;
+    constexpr int E = Word<T>::kElems;
     grid_dependency_wait();
     grid_launch_dependents();
-    const int64_t u = static_cast<int64_t>(blockIdx.x) * kRowThreads + threadIdx.x;
-    if (u >= a.units) return;
-    const int64_t t = u / a.units_per_row;
-    const int64_t at = (u - t * a.units_per_row) * 16;
-    float acc[N];
+    const int in_block = threadIdx.x / a.threads_per_token, lane = threadIdx.x - in_block * a.threads_per_token;
+    const int64_t t = static_cast<int64_t>(blockIdx.x) * (blockDim.x / a.threads_per_token) + in_block;
+    if (t >= a.T) return;
+    const uint32_t step = a.threads_per_token * W * 4;
+    for (uint32_t at = lane * W * 4; at < a.row_bytes; at += step) {
+        float acc[W * E];
 #pragma unroll
-    for (int i = 0; i < N; ++i) acc[i] = 0.0f;
-    for (int j = 0; j < a.k; ++j) {
-        const int64_t row = __ldg(a.rows + t * a.k + j);
-        if (row < 0 || row >= a.n_rows) continue;
-        const float w = a.weights != nullptr ? __ldg(a.weights + t * a.k + j) : 1.0f;
-        float v[N];
-        unpack(ld_global_nc_v4(a.src + row * a.row_bytes + at), v);
+        for (int i = 0; i < W * E; ++i) acc[i] = 0.0f;
+        for (int j0 = 0; j0 < a.k; j0 += kCombineSlots) {
+            uint32_t w[kCombineSlots][W];
+            int64_t off[kCombineSlots];
+            float scale[kCombineSlots];
 #pragma unroll
-        for (int i = 0; i < N; ++i) acc[i] = fmaf(w, v[i], acc[i]);
+            for (int j = 0; j < kCombineSlots; ++j) {
+                off[j] = j0 + j < a.k ? row_offset(a, t * a.k + j0 + j) : -1;
+                scale[j] = WEIGHTED && off[j] >= 0 ? __ldg(a.weights + t * a.k + j0 + j) : 1.0f;
+            }
+#pragma unroll
+            for (int j = 0; j < kCombineSlots; ++j)
+                if (off[j] >= 0) load_unit<W>(a.src + off[j] + at, w[j]);
+#pragma unroll
+            for (int j = 0; j < kCombineSlots; ++j) {
+                if (off[j] < 0) continue;
+#pragma unroll
+                for (int i = 0; i < W; ++i) {
+                    float v[E];
+                    Word<T>::get(w[j][i], v);
+#pragma unroll
+                    for (int e = 0; e < E; ++e)
+                        acc[i * E + e] = WEIGHTED ? fmaf(scale[j], v[e], acc[i * E + e]) : acc[i * E + e] + v[e];
+                }
+            }
+        }
+        uint32_t out[W];
+#pragma unroll
+        for (int i = 0; i < W; ++i) out[i] = Word<T>::put(acc + i * E);
+        store_unit<W>(a.dst + t * a.token_bytes + at, out);
     }
-    store_unit(a.dst + t * a.token_bytes + at, acc);
 }
 
-// One block per token: dy is read once for kSlots slots, every slot's row of ye once.
+// One block per token; dy is read once for kSlots slots, every slot's row of ye once.
 constexpr int kSlots = 8;
 
 template <typename T>
 __global__ void __launch_bounds__(kRowThreads) combine_backward_kernel(const RowArgs a) {
-    constexpr int N = RowUnit<T>::kElems;
+    constexpr int W = 4, E = Word<T>::kElems;
     __shared__ float part[kRowThreads / 32][kSlots];
     grid_dependency_wait();
     grid_launch_dependents();
@@ -198,27 +241,34 @@ __global__ void __launch_bounds__(kRowThreads) combine_backward_kernel(const Row
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     for (int j0 = 0; j0 < a.k; j0 += kSlots) {
         const int slots = min(kSlots, a.k - j0);
-        int64_t row[kSlots];
-        float w[kSlots], dot[kSlots];
+        int64_t off[kSlots];
+        float scale[kSlots], dot[kSlots];
 #pragma unroll
         for (int j = 0; j < kSlots; ++j) {
-            row[j] = j < slots ? __ldg(a.rows + t * a.k + j0 + j) : -1;
-            if (row[j] >= a.n_rows) row[j] = -1;
-            w[j] = j < slots ? __ldg(a.weights + t * a.k + j0 + j) : 0.0f;
+            off[j] = j < slots ? row_offset(a, t * a.k + j0 + j) : -1;
+            scale[j] = off[j] >= 0 ? __ldg(a.weights + t * a.k + j0 + j) : 0.0f;
             dot[j] = 0.0f;
         }
-        for (uint32_t u = threadIdx.x; u < a.units_per_row; u += blockDim.x) {
-            const int64_t at = static_cast<int64_t>(u) * 16;
-            float g[N];
-            unpack(ld_global_nc_v4(dy + at), g);
+        for (uint32_t at = threadIdx.x * W * 4; at < a.row_bytes; at += blockDim.x * W * 4) {
+            uint32_t g[W], w[kSlots][W];
+            load_unit<W>(dy + at, g);
+#pragma unroll
+            for (int j = 0; j < kSlots; ++j)
+                if (off[j] >= 0) load_unit<W>(a.src + off[j] + at, w[j]);
 #pragma unroll
             for (int j = 0; j < kSlots; ++j) {
-                if (row[j] < 0) continue;
-                float v[N], out[N];
-                unpack(ld_global_nc_v4(a.src + row[j] * a.row_bytes + at), v);
+                if (off[j] < 0) continue;
+                uint32_t out[W];
 #pragma unroll
-                for (int i = 0; i < N; ++i) { dot[j] = fmaf(g[i], v[i], dot[j]); out[i] = w[j] * g[i]; }
-                store_unit(a.dst + row[j] * a.row_bytes + at, out);
+                for (int i = 0; i < W; ++i) {
+                    float v[E], d[E], o[E];
+                    Word<T>::get(g[i], d);
+                    Word<T>::get(w[j][i], v);
+#pragma unroll
+                    for (int e = 0; e < E; ++e) { dot[j] = fmaf(d[e], v[e], dot[j]); o[e] = scale[j] * d[e]; }
+                    out[i] = Word<T>::put(o);
+                }
+                store_unit<W>(a.dst + off[j] + at, out);
             }
         }
 #pragma unroll
@@ -258,18 +308,25 @@ RowArgs row_args(int64_t T, int top_k, int64_t d, int dtype, int64_t ld, int64_t
     const int64_t esize = dtype == FP8MLP_F32 ? 4 : 2;
     RowArgs a{};
     a.rows = rows;
-    a.T = T; a.k = top_k; a.n_rows = n_rows;
+    a.T = T; a.k = top_k; a.n_rows = static_cast<uint32_t>(n_rows);
     a.token_bytes = ld * esize;
-    a.row_bytes = d * esize;
-    a.units_per_row = static_cast<uint32_t>(d * esize / 16);
-    a.units = T * a.units_per_row;
+    a.row_bytes = static_cast<uint32_t>(d * esize);
     return a;
 }
 
-int unit_blocks(const RowArgs& a, dim3* grid) {
-    const int64_t blocks = (a.units + kRowThreads - 1) / kRowThreads;
+// Blocks of about kRowThreads threads.  A row's units are dealt evenly to as few rounds of threads as fit a block (whole
+// warps, so that a warp's accesses are neighbours); short rows share a block.
+struct RowGrid { dim3 grid; int threads; };
+int row_grid(RowArgs* a, int unit_bytes, RowGrid* g) {
+    const int units = static_cast<int>(a->row_bytes) / unit_bytes;
+    const int rounds = (units + kRowThreads - 1) / kRowThreads;
+    a->threads_per_token = units <= 32 ? units : ((units + rounds - 1) / rounds + 31) / 32 * 32;
+    int tokens = kRowThreads / a->threads_per_token;
+    if (tokens > a->T) tokens = static_cast<int>(a->T);
+    const int64_t blocks = (a->T + tokens - 1) / tokens;
     if (blocks > 0x7fffffff) return FP8MLP_ERR_SHAPE;
-    *grid = dim3(static_cast<unsigned>(blocks));
+    g->grid = dim3(static_cast<unsigned>(blocks));
+    g->threads = tokens * a->threads_per_token;
     return FP8MLP_OK;
 }
 
@@ -325,10 +382,12 @@ extern "C" int fp8mlp_dispatch(int64_t T, int top_k, int64_t d, int dtype, const
     RowArgs a = row_args(T, top_k, d, dtype, ld_x, n_rows, rows);
     a.src = static_cast<const uint8_t*>(x);
     a.dst = static_cast<uint8_t*>(xe);
-    dim3 grid;
-    const int rg = unit_blocks(a, &grid);
+    const bool wide = aligned(x, 32) && aligned(xe, 32) && a.token_bytes % 32 == 0;
+    RowGrid g;
+    const int rg = row_grid(&a, wide ? 32 : 16, &g);
     if (rg != FP8MLP_OK) return rg;
-    FP8MLP_CUDA_CHECK(launch_chained(dispatch_kernel, grid, kRowThreads, 0, static_cast<cudaStream_t>(stream), a));
+    FP8MLP_CUDA_CHECK(launch_chained(wide ? dispatch_kernel<8> : dispatch_kernel<4>, g.grid, g.threads, 0,
+                                     static_cast<cudaStream_t>(stream), a));
     FP8MLP_LAUNCH_CHECK();
     return FP8MLP_OK;
 }
@@ -343,12 +402,19 @@ extern "C" int fp8mlp_combine(int64_t T, int top_k, int64_t d, int dtype, const 
     a.src = static_cast<const uint8_t*>(ye);
     a.dst = static_cast<uint8_t*>(y);
     a.weights = weights;
-    dim3 grid;
-    const int rg = unit_blocks(a, &grid);
+    const bool wide = aligned(y, 32) && aligned(ye, 32) && a.token_bytes % 32 == 0;
+    RowGrid g;
+    const int rg = row_grid(&a, wide ? 32 : 16, &g);
     if (rg != FP8MLP_OK) return rg;
-    cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (dtype == FP8MLP_F32) FP8MLP_CUDA_CHECK(launch_chained(combine_kernel<float>, grid, kRowThreads, 0, st, a));
-    else FP8MLP_CUDA_CHECK(launch_chained(combine_kernel<uint16_t>, grid, kRowThreads, 0, st, a));
+    void (*kernel)(const RowArgs) = nullptr;
+    if (dtype == FP8MLP_F32) {
+        if (weights != nullptr) kernel = wide ? combine_kernel<float, 8, true> : combine_kernel<float, 4, true>;
+        else kernel = wide ? combine_kernel<float, 8, false> : combine_kernel<float, 4, false>;
+    } else {
+        if (weights != nullptr) kernel = wide ? combine_kernel<uint16_t, 8, true> : combine_kernel<uint16_t, 4, true>;
+        else kernel = wide ? combine_kernel<uint16_t, 8, false> : combine_kernel<uint16_t, 4, false>;
+    }
+    FP8MLP_CUDA_CHECK(launch_chained(kernel, g.grid, g.threads, 0, static_cast<cudaStream_t>(stream), a));
     FP8MLP_LAUNCH_CHECK();
     return FP8MLP_OK;
 }
@@ -370,8 +436,8 @@ extern "C" int fp8mlp_combine_backward(int64_t T, int top_k, int64_t d, int dtyp
     a.d_weights = d_weights;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const dim3 grid(static_cast<unsigned>(T));
-    const int threads = a.units_per_row < static_cast<uint32_t>(kRowThreads) ? static_cast<int>((a.units_per_row + 31) / 32 * 32)
-                                                                             : kRowThreads;
+    const int units = static_cast<int>(a.row_bytes / 16), rounds = (units + kRowThreads - 1) / kRowThreads;
+    const int threads = ((units + rounds - 1) / rounds + 31) / 32 * 32;
     if (dtype == FP8MLP_F32) FP8MLP_CUDA_CHECK(launch_chained(combine_backward_kernel<float>, grid, threads, 0, st, a));
     else FP8MLP_CUDA_CHECK(launch_chained(combine_backward_kernel<uint16_t>, grid, threads, 0, st, a));
     FP8MLP_LAUNCH_CHECK();

@@ -21,7 +21,9 @@ struct RouteArgs {
     int E, k, score, G, per, top_groups, group_top, renorm;
     float scale;
     int wide, wide_b, wide_d;      // rows of logits, the bias, rows of d_logits start on a vector boundary
-    int lane_groups;       // a group is a power-of-two number of whole lanes
+    int lane_shift;        // a group is 2^lane_shift whole lanes; -1: groups do not fall on lanes, and then
+    int sub_shift;         // 2^sub_shift lanes work on a group
+    uint32_t inv_per;      // ceil(2^20 / per)
 };
 
 template <typename SRC> __device__ __forceinline__ float load1(const SRC* p);
@@ -67,223 +69,235 @@ __device__ __forceinline__ void load_row(const SRC* row, int e0, int E, bool wid
     }
 }
 
-// Unsigned key that orders like the float; 0 (no float's key) stands for "cannot be chosen".
-__device__ __forceinline__ uint32_t order_key(float c) {
-    const uint32_t u = __float_as_uint(c);
-    return u ^ ((static_cast<uint32_t>(static_cast<int32_t>(u) >> 31)) | 0x80000000u);
-}
-
-template <int LANES> __device__ __forceinline__ uint32_t seg_max(uint32_t v) {
-    if constexpr (LANES == 32) {
-        return __reduce_max_sync(kAll, v);
-    } else {
-#pragma unroll
-        for (int o = LANES / 2; o > 0; o >>= 1) v = max(v, __shfl_xor_sync(kAll, v, o));
-        return v;
-    }
-}
 template <int LANES> __device__ __forceinline__ float seg_sum(float v) {
 #pragma unroll
     for (int o = LANES / 2; o > 0; o >>= 1) v += __shfl_xor_sync(kAll, v, o);
     return v;
 }
-template <int LANES> __device__ __forceinline__ float seg_maxf(float v) {
+// maximum over the token's lanes; a NaN loses against any number
+template <int LANES> __device__ __forceinline__ float seg_max(float v) {
+    if constexpr (LANES == 32) {
+        float r;
+        asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+        return r;
+    } else {
 #pragma unroll
-    for (int o = LANES / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(kAll, v, o));
-    return v;
+        for (int o = LANES / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(kAll, v, o));
+        return v;
+    }
 }
 
-// sigma(x) = 1 / (1 + e^-x), written with e^-|x| so that neither end overflows and small values keep their digits; the
-// reciprocal is of a number in [1, 2], where the special-function unit's is within one unit of the last place.
-__device__ __forceinline__ float sigmoid_exact(float x) {
-    const float e = expf(-fabsf(x));
-    const float r = rcp_approx(1.0f + e);
-    return x >= 0.0f ? r : e * r;          // NaN takes the second branch and stays NaN
-}
-// 1 - sigma(x) = sigma(-x)
+constexpr float kLog2e = 1.4426950408889634f;
 
-// softmax of the token's row, in place; a row without a finite maximum comes out as NaN
+// Scores on the special-function unit: 2^x and 1/x within 2^-22 relative.  sigma(x) = 1 / (1 + e^-x) keeps its digits at
+// both ends (a small score is the reciprocal of a large number) down to 2^-126, below which it is 0; 1 - sigma(x) =
+// sigma(-x).  The softmax's 2^x keeps subnormal results, so that far smaller experts still have an order.
+__device__ __forceinline__ float ex2_subnormal(float x) {
+    float y;
+    asm("ex2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// Softmax of the token's row, in place; a row without a finite maximum comes out as NaN.  The difference is taken before
+// the factor log2 e: a finite mask (the type's lowest value) would overflow the other way round.
 template <int LANES, int V>
 __device__ __forceinline__ void softmax_row(float (&x)[V]) {
     float m = x[0];
 #pragma unroll
     for (int j = 1; j < V; ++j) m = fmaxf(m, x[j]);
-    m = seg_maxf<LANES>(m);
+    m = seg_max<LANES>(m);
     float sum = 0.0f;
 #pragma unroll
-    for (int j = 0; j < V; ++j) { x[j] = expf(x[j] - m); sum += x[j]; }
+    for (int j = 0; j < V; ++j) { x[j] = ex2_subnormal(__fmul_rn(x[j] - m, kLog2e)); sum += x[j]; }
     sum = seg_sum<LANES>(sum);
-    const float inv = __fdiv_rn(1.0f, sum);
+    const float inv = rcp_approx(sum);
 #pragma unroll
     for (int j = 0; j < V; ++j) x[j] *= inv;
 }
 
 // the larger two of (a1 >= a2) and (b1 >= b2)
-__device__ __forceinline__ void merge_top2(uint32_t& a1, uint32_t& a2, uint32_t b1, uint32_t b2) {
-    a2 = max(min(a1, b1), max(a2, b2));
-    a1 = max(a1, b1);
+__device__ __forceinline__ void merge_top2(float& a1, float& a2, float b1, float b2) {
+    a2 = fmaxf(fminf(a1, b1), fmaxf(a2, b2));
+    a1 = fmaxf(a1, b1);
 }
-__device__ __forceinline__ float key_value(uint32_t k) {      // the float of a key; a missing expert adds nothing
-    return k == 0u ? 0.0f : __uint_as_float(k ^ ((k & 0x80000000u) ? 0x80000000u : 0xffffffffu));
-}
-// a group's value as a key (0: nothing to choose in it)
-__device__ __forceinline__ uint32_t group_key(uint32_t k1, uint32_t k2, int group_top) {
-    if (k1 == 0u) return 0u;
-    const float v = group_top == 2 ? key_value(k1) + key_value(k2) : key_value(k1);
-    return order_key(v + 0.0f);            // + 0: one zero only
+// a group's value; -inf: nothing to choose in it, and a missing second expert adds nothing
+__device__ __forceinline__ float group_value(float c1, float c2, int group_top) {
+    return group_top == 2 && c2 > -CUDART_INF_F ? c1 + c2 : c1;
 }
 
-// 8 keys into falling order (19 exchanges)
-__device__ __forceinline__ void exchange(uint32_t& a, uint32_t& b) {
-    const uint32_t hi = max(a, b);
-    b = min(a, b);
+// 8 values into falling order (19 exchanges)
+__device__ __forceinline__ void exchange(float& a, float& b) {
+    const float hi = fmaxf(a, b);
+    b = fminf(a, b);
     a = hi;
 }
-__device__ __forceinline__ void sort8(uint32_t (&k)[8]) {
-    exchange(k[0], k[2]); exchange(k[1], k[3]); exchange(k[4], k[6]); exchange(k[5], k[7]);
-    exchange(k[0], k[4]); exchange(k[1], k[5]); exchange(k[2], k[6]); exchange(k[3], k[7]);
-    exchange(k[0], k[1]); exchange(k[2], k[3]); exchange(k[4], k[5]); exchange(k[6], k[7]);
-    exchange(k[2], k[4]); exchange(k[3], k[5]);
-    exchange(k[1], k[4]); exchange(k[3], k[6]);
-    exchange(k[1], k[2]); exchange(k[3], k[4]); exchange(k[5], k[6]);
+__device__ __forceinline__ void sort8(float (&c)[8]) {
+    exchange(c[0], c[2]); exchange(c[1], c[3]); exchange(c[4], c[6]); exchange(c[5], c[7]);
+    exchange(c[0], c[4]); exchange(c[1], c[5]); exchange(c[2], c[6]); exchange(c[3], c[7]);
+    exchange(c[0], c[1]); exchange(c[2], c[3]); exchange(c[4], c[5]); exchange(c[6], c[7]);
+    exchange(c[2], c[4]); exchange(c[3], c[5]);
+    exchange(c[1], c[4]); exchange(c[3], c[6]);
+    exchange(c[1], c[2]); exchange(c[3], c[4]); exchange(c[5], c[6]);
+}
+template <int V> __device__ __forceinline__ void put_row(float* row, const float (&v)[V]) {
+#pragma unroll
+    for (int j = 0; j < V; j += 4) *reinterpret_cast<float4*>(row + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
 }
 
-// The choice: every lane sorts its keys, eight at a time, and the token's lanes take the largest head k times.  What a
-// round costs decides the kernel's time (it is bound by instructions, not by memory), so a round moves keys only; which
-// expert a key belongs to is looked up once at the end, by k lanes side by side, in the unsorted keys in shared memory.
+// The choice: every lane sorts its values c, eight at a time, and the token's lanes take the largest head k times.  What a
+// round costs decides the kernel's time (it is bound by instructions, not by memory), so a round moves values only; which
+// expert a value belongs to is looked up once at the end, by k lanes side by side, in the unsorted row in shared memory.
+// -inf stands for "cannot be chosen".
 template <int LANES, int V, typename SRC>
-__global__ void __launch_bounds__(kRouteThreads) route_kernel(const RouteArgs a) {
-    extern __shared__ __align__(16) uint32_t smem[];
+__global__ void __launch_bounds__(kRouteThreads, V > 8 ? 4 : LANES == 32 ? 12 : 16) route_kernel(const RouteArgs a) {
+    extern __shared__ __align__(16) float smem[];
     constexpr int kTokens = kRouteThreads / LANES;
     constexpr int kRow = LANES * V + 4;                   // + 4: rows of neighbouring tokens start in other banks
     constexpr int kLists = V / 8;
     const int lane = threadIdx.x % LANES, tok = threadIdx.x / LANES;
     const int seg_base = (threadIdx.x & 31) - lane;
-    uint32_t* row_key = smem + tok * kRow;                                          // this token's keys ...
-    float* row_s = reinterpret_cast<float*>(smem + kTokens * kRow) + tok * kRow;    // ... and scores
-    uint32_t* sel_key = smem + 2 * kTokens * kRow + 2 * tok * a.k;                  // a round's key, then its lane and count
-    uint32_t* group_keys = smem + 2 * kTokens * (kRow + a.k) + tok * a.G;
-    const int64_t t = static_cast<int64_t>(blockIdx.x) * kTokens + tok;
-    const bool live = t < a.T;
+    float* row_c = smem + tok * kRow;                                               // this token's values ...
+    float* row_s = smem + (kTokens + tok) * kRow;                                   // ... and scores
+    float2* sel = reinterpret_cast<float2*>(smem + 2 * kTokens * kRow) + tok * a.k; // a round's value and its lane
+    float* group_c = smem + 2 * kTokens * (kRow + a.k) + tok * 2 * a.G;     // groups off the lanes: values, then what is kept
     const int e0 = lane * V;
+    const int64_t t = static_cast<int64_t>(blockIdx.x) * kTokens + tok;
+    const bool live = t < a.T, biased = a.bias != nullptr;
     grid_dependency_wait();
     grid_launch_dependents();
 
-    float s[V];
-    uint32_t key[kLists][8];
+    float s[V], bias[V], c[kLists][8];
     if (live) {
         load_row<V, SRC>(static_cast<const SRC*>(a.logits) + t * a.ld, e0, a.E, a.wide != 0, s);
     } else {
 #pragma unroll
         for (int j = 0; j < V; ++j) s[j] = -CUDART_INF_F;
     }
+    if (biased) load_row<V, float>(a.bias, e0, a.E, a.wide_b != 0, bias);
+    // Sums that come out as a number above -inf show that no logit is masked and no value NaN or -inf: additions run beside
+    // the comparisons (another pipe, the one that limits this kernel), and masks are rare.
+    float sum_x = s[0];
     uint32_t masked = 0;
 #pragma unroll
-    for (int j = 0; j < V; ++j) masked |= (s[j] == -CUDART_INF_F ? 1u : 0u) << j;
+    for (int j = 1; j < V; ++j) sum_x += s[j];
+    if (!(sum_x > -CUDART_INF_F)) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) masked |= (s[j] == -CUDART_INF_F ? 1u : 0u) << j;
+    }
     if (a.score == FP8MLP_SCORE_SOFTMAX) {
         softmax_row<LANES, V>(s);
     } else {
 #pragma unroll
-        for (int j = 0; j < V; ++j) s[j] = sigmoid_exact(s[j]);
+        for (int j = 0; j < V; ++j) s[j] = sigmoid_f32(s[j]);
     }
-    if (a.bias != nullptr) {
-        float b[V];
-        load_row<V, float>(a.bias, e0, a.E, a.wide_b != 0, b);      // past the last expert: -inf
+    if (biased) {
+        put_row<V>(row_s + e0, s);
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-            row_s[e0 + j] = s[j];
-            s[j] += b[j];
-        }
+        for (int j = 0; j < V; ++j) s[j] += bias[j];
     }
+    float sum_c = s[0];
 #pragma unroll
-    for (int j = 0; j < V; ++j) key[j / 8][j % 8] = (masked >> j & 1u) != 0u || !(s[j] > -CUDART_INF_F) ? 0u : order_key(s[j]);
+    for (int j = 1; j < V; ++j) sum_c += s[j];
+    if (masked != 0u || !(sum_c > -CUDART_INF_F)) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) s[j] = (masked >> j & 1u) != 0u ? -CUDART_INF_F : fmaxf(s[j], -CUDART_INF_F);   // NaN: -inf
+    }
 
-    if (a.G > 1 && !a.lane_groups) {                      // groups that do not fall on lanes: through shared memory
-#pragma unroll
-        for (int j = 0; j < V; ++j) row_key[e0 + j] = key[j / 8][j % 8];
+    if (a.G > 1 && a.lane_shift < 0) {
+        // Groups that do not fall on lanes: their values through shared memory, 2^sub_shift lanes to a group.
+        put_row<V>(row_c + e0, s);
         __syncwarp();
-        for (int g = lane; g < a.G; g += LANES) {
-            uint32_t k1 = 0, k2 = 0;
-            for (int i = 0; i < a.per; ++i) {
-                const uint32_t v = row_key[g * a.per + i];
-                k2 = max(k2, min(k1, v));
-                k1 = max(k1, v);
-            }
-            group_keys[g] = group_key(k1, k2, a.group_top);
-        }
-        __syncwarp();
-        int last = -1;
-        bool keep = false;
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const int g = (e0 + j) / a.per;
-            if (g != last && e0 + j < a.E) {
-                last = g;
-                const uint32_t gk = group_keys[g];
-                int rank = 0;
-                for (int i = 0; i < a.G; ++i) {
-                    const uint32_t other = group_keys[i];
-                    rank += (other > gk || (other == gk && i < g)) ? 1 : 0;
+        const int sub = lane & ((1 << a.sub_shift) - 1), sub_lanes = 1 << a.sub_shift, at_once = LANES >> a.sub_shift;
+        for (int g0 = 0; g0 < a.G; g0 += at_once) {
+            const int g = g0 + (lane >> a.sub_shift);
+            float c1 = -CUDART_INF_F, c2 = -CUDART_INF_F;
+            if (g < a.G) {
+                for (int i = sub; i < a.per; i += sub_lanes) {
+                    const float v = row_c[g * a.per + i];
+                    c2 = fmaxf(c2, fminf(c1, v));
+                    c1 = fmaxf(c1, v);
                 }
-                keep = rank < a.top_groups;
             }
-            if (!keep) key[j / 8][j % 8] = 0u;
+            for (int o = 1; o < sub_lanes; o <<= 1) {
+                const float b1 = __shfl_xor_sync(kAll, c1, o), b2 = __shfl_xor_sync(kAll, c2, o);
+                merge_top2(c1, c2, b1, b2);
+            }
+            if (g < a.G && sub == 0) group_c[g] = group_value(c1, c2, a.group_top);
         }
+        __syncwarp();
+        float* group_keep = group_c + a.G;
+        for (int g0 = 0; g0 < a.G; g0 += at_once) {
+            const int g = g0 + (lane >> a.sub_shift);
+            int rank = 0;
+            if (g < a.G) {
+                const float mine = group_c[g];
+                for (int i = sub; i < a.G; i += sub_lanes) rank += (i < g ? group_c[i] >= mine : group_c[i] > mine) ? 1 : 0;
+            }
+            for (int o = 1; o < sub_lanes; o <<= 1) rank += __shfl_xor_sync(kAll, rank, o);
+            if (g < a.G && sub == 0) group_keep[g] = rank < a.top_groups ? CUDART_INF_F : -CUDART_INF_F;
+        }
+        __syncwarp();
+#pragma unroll
+        for (int j = 0; j < V; ++j)          // e / per by a product that is exact for e, per <= 1024
+            if (e0 + j < a.E) s[j] = fminf(s[j], group_keep[(static_cast<uint32_t>(e0 + j) * a.inv_per) >> 20]);
     }
+    put_row<V>(row_c + e0, s);
 #pragma unroll
-    for (int j = 0; j < V; j += 4)
-        *reinterpret_cast<uint4*>(row_key + e0 + j) = make_uint4(key[j / 8][j % 8], key[j / 8][j % 8 + 1], key[j / 8][j % 8 + 2], key[j / 8][j % 8 + 3]);
+    for (int l = 0; l < kLists; ++l) {
 #pragma unroll
-    for (int l = 0; l < kLists; ++l) sort8(key[l]);
+        for (int j = 0; j < 8; ++j) c[l][j] = s[l * 8 + j];
+        sort8(c[l]);
+    }
 
-    if (a.G > 1 && a.lane_groups) {
-        const int width = a.per / V;                     // lanes of a group
-        uint32_t k1 = key[0][0], k2 = key[0][1];
+    if (a.G > 1 && a.lane_shift >= 0) {
+        const int width = 1 << a.lane_shift;             // lanes of a group
+        float c1 = c[0][0], c2 = c[0][1];
 #pragma unroll
-        for (int l = 1; l < kLists; ++l) merge_top2(k1, k2, key[l][0], key[l][1]);
+        for (int l = 1; l < kLists; ++l) merge_top2(c1, c2, c[l][0], c[l][1]);
         for (int o = 1; o < width; o <<= 1) {
-            const uint32_t b1 = __shfl_xor_sync(kAll, k1, o), b2 = __shfl_xor_sync(kAll, k2, o);
-            merge_top2(k1, k2, b1, b2);
+            const float b1 = __shfl_xor_sync(kAll, c1, o), b2 = __shfl_xor_sync(kAll, c2, o);
+            merge_top2(c1, c2, b1, b2);
         }
-        const uint32_t gk = group_key(k1, k2, a.group_top);
-        const int mine = lane / width;
+        const float value = group_value(c1, c2, a.group_top);
+        // the group's lanes share the comparisons with the other groups
+        const int mine = lane >> a.lane_shift, sub = lane & (width - 1);
         int rank = 0;
-        for (int g = 0; g < a.G; ++g) {
-            const uint32_t other = __shfl_sync(kAll, gk, seg_base + g * width);
-            rank += (other > gk || (other == gk && g < mine)) ? 1 : 0;
+        const int steps = (a.G + width - 1) >> a.lane_shift;
+#pragma unroll 4
+        for (int i = 0; i < steps; ++i) {
+            const int g = (i << a.lane_shift) + sub;
+            const float other = __shfl_sync(kAll, value, (seg_base + (g << a.lane_shift)) & 31);
+            if (g < a.G && (other > value || (other == value && g < mine))) ++rank;
         }
+        for (int o = 1; o < width; o <<= 1) rank += __shfl_xor_sync(kAll, rank, o);
         if (rank >= a.top_groups) {
 #pragma unroll
             for (int l = 0; l < kLists; ++l)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) key[l][j] = 0u;
+                for (int j = 0; j < 8; ++j) c[l][j] = -CUDART_INF_F;
         }
     }
 
-    uint32_t best = key[0][0];
+    float best = c[0][0];
 #pragma unroll
-    for (int l = 1; l < kLists; ++l) best = max(best, key[l][0]);
-    uint32_t prev = 0, count = 0;
+    for (int l = 1; l < kLists; ++l) best = fmaxf(best, c[l][0]);
+    const uint32_t lower = ((1u << lane) - 1u) << seg_base;      // the token's lanes below this one
     for (int r = 0; r < a.k; ++r) {
-        const uint32_t top = seg_max<LANES>(best);
-        // the lowest lane among equals holds the lowest expert; how often it gave this key before tells which of its equals
-        const uint32_t holders = (__ballot_sync(kAll, best == top) >> seg_base) & (LANES == 32 ? kAll : (1u << (LANES & 31)) - 1u);
-        if (lane == __ffs(holders) - 1) {
-            count = top == prev ? count + 1u : 0u;
-            prev = top;
-            sel_key[2 * r] = top;
-            sel_key[2 * r + 1] = static_cast<uint32_t>(lane) | count << 8;
+        const float top = seg_max<LANES>(best);
+        // the lowest lane among equals holds the lowest expert
+        const bool holds = best == top;
+        if ((__ballot_sync(kAll, holds) & lower) == 0u && holds) {
+            sel[r] = make_float2(top, __int_as_float(lane));
             bool taken = false;
-            best = 0;
+            best = -CUDART_INF_F;
 #pragma unroll
             for (int l = 0; l < kLists; ++l) {
-                if (!taken && key[l][0] == top) {
+                if (kLists == 1 || (!taken && c[l][0] == top)) {
                     taken = true;
 #pragma unroll
-                    for (int j = 0; j < 7; ++j) key[l][j] = key[l][j + 1];
-                    key[l][7] = 0u;
+                    for (int j = 0; j < 7; ++j) c[l][j] = c[l][j + 1];
+                    c[l][7] = -CUDART_INF_F;
                 }
-                best = max(best, key[l][0]);
+                best = fmaxf(best, c[l][0]);
             }
         }
     }
@@ -297,35 +311,36 @@ __global__ void __launch_bounds__(kRouteThreads) route_kernel(const RouteArgs a)
         const int r = lane + i * LANES;
         score[i] = 0.0f;
         expert[i] = -1;
-        if (r < a.k && sel_key[2 * r] != 0u) {
-            const uint32_t want = sel_key[2 * r], who = sel_key[2 * r + 1];
-            const int from = static_cast<int>(who & 255u) * V;
-            uint32_t skip = who >> 8;
+        if (r < a.k && sel[r].x > -CUDART_INF_F) {
+            const float want = sel[r].x;
+            const int owner = __float_as_int(sel[r].y), from = owner * V;
+            int skip = 0;            // equal values of one lane are taken in turn, lowest expert first
+            while (skip < r && sel[r - 1 - skip].x == want && __float_as_int(sel[r - 1 - skip].y) == owner) ++skip;
 #pragma unroll
             for (int j = 0; j < V; j += 4) {
-                const uint4 q = *reinterpret_cast<const uint4*>(row_key + from + j);
-                const uint32_t four[4] = {q.x, q.y, q.z, q.w};
+                const float4 q = *reinterpret_cast<const float4*>(row_c + from + j);
+                const float four[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
                 for (int m = 0; m < 4; ++m) {
                     if (four[m] == want) {
-                        if (skip == 0u) expert[i] = from + j + m;
+                        if (skip == 0) expert[i] = from + j + m;
                         --skip;
                     }
                 }
             }
-            score[i] = a.bias != nullptr ? row_s[expert[i]] : key_value(want);
+            score[i] = biased ? row_s[expert[i]] : want;
         }
         D += score[i];
     }
     D = seg_sum<LANES>(D);
+    const float inv = !a.renorm ? 1.0f : D == 0.0f ? 0.0f : rcp_approx(D);
     if (live) {
 #pragma unroll
         for (int i = 0; i < kMine; ++i) {
             const int r = lane + i * LANES;
             if (r < a.k) {
-                const float w = a.renorm ? (D == 0.0f ? 0.0f : __fdiv_rn(score[i], D)) : score[i];
                 a.experts[t * a.k + r] = expert[i];
-                a.weights[t * a.k + r] = w * a.scale;
+                a.weights[t * a.k + r] = score[i] * inv * a.scale;
             }
         }
     }
@@ -364,18 +379,18 @@ __global__ void __launch_bounds__(kRouteThreads) route_backward_sparse_kernel(co
     if (live) clear_row<LANES, SRC>(dst, a.E, a.wide_d != 0, lane);
     float s;
     if (a.score == FP8MLP_SCORE_SOFTMAX) {
-        const float m = seg_maxf<LANES>(x);
-        s = e < 0 ? 0.0f : expf(x - m);
+        const float m = seg_max<LANES>(x);
+        s = e < 0 ? 0.0f : ex2_approx(__fmul_rn(x - m, kLog2e));
     } else {
-        s = e < 0 ? 0.0f : sigmoid_exact(x);
+        s = e < 0 ? 0.0f : sigmoid_f32(x);
     }
     float g = s * dw;
     if (a.renorm) {
         const float D = seg_sum<LANES>(s);
-        const float r = D == 0.0f ? 0.0f : __fdiv_rn(s, D);
+        const float r = D == 0.0f ? 0.0f : s * rcp_approx(D);
         g = r * (dw - seg_sum<LANES>(r * dw));
     }
-    if (a.score == FP8MLP_SCORE_SIGMOID) g *= sigmoid_exact(-x);      // 1 - s
+    if (a.score == FP8MLP_SCORE_SIGMOID) g *= sigmoid_f32(-x);      // 1 - s
     __syncwarp();                                                      // the row is clear before its k values are written
     if (e >= 0) store1(dst + e, a.scale * g);
 }
@@ -383,11 +398,11 @@ __global__ void __launch_bounds__(kRouteThreads) route_backward_sparse_kernel(co
 // Gradient of softmax weights that are not renormalised: every expert of the row has one.
 template <int LANES, int V, typename SRC>
 __global__ void __launch_bounds__(kRouteThreads) route_backward_dense_kernel(const RouteArgs a) {
-    extern __shared__ __align__(16) uint32_t smem[];
+    extern __shared__ __align__(16) float smem[];
     constexpr int kTokens = kRouteThreads / LANES;
     constexpr int kRow = LANES * V + 4;
     const int lane = threadIdx.x % LANES, tok = threadIdx.x / LANES;
-    float* row = reinterpret_cast<float*>(smem) + tok * kRow;         // gradient of the row's scores, then of its logits
+    float* row = smem + tok * kRow;         // gradient of the row's scores, then of its logits
     const int64_t t = static_cast<int64_t>(blockIdx.x) * kTokens + tok;
     const bool live = t < a.T;
     const int e0 = lane * V;
@@ -413,7 +428,7 @@ __global__ void __launch_bounds__(kRouteThreads) route_backward_dense_kernel(con
             }
         }
     }
-    any = seg_max<LANES>(any ? 1u : 0u) != 0u;
+    any = seg_max<LANES>(any ? 1.0f : 0.0f) != 0.0f;
     softmax_row<LANES, V>(s);
     __syncwarp();
     float ds[V], dot = 0.0f;
@@ -494,7 +509,7 @@ int launch_tokens(void (*kernel)(const RouteArgs), const RouteArgs& a, size_t sm
     constexpr int kTokens = kRouteThreads / LANES;
     const int64_t blocks = (a.T + kTokens - 1) / kTokens;
     if (blocks > 0x7fffffff) return FP8MLP_ERR_SHAPE;
-    if (smem > 48 * 1024) FP8MLP_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 64 * 1024));
+    if (smem > 48 * 1024) FP8MLP_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 72 * 1024));
     FP8MLP_CUDA_CHECK(launch_chained(kernel, dim3(static_cast<unsigned>(blocks)), kRouteThreads, smem, st, a));
     FP8MLP_LAUNCH_CHECK();
     return FP8MLP_OK;
@@ -503,10 +518,15 @@ int launch_tokens(void (*kernel)(const RouteArgs), const RouteArgs& a, size_t sm
 template <int LANES, int V>
 int launch_route(RouteArgs a, int dtype, cudaStream_t st) {
     constexpr int kTokens = kRouteThreads / LANES;
-    a.lane_groups = a.G > 1 && a.per % V == 0 && ((a.per / V) & (a.per / V - 1)) == 0;
+    a.lane_shift = -1;
+    if (a.per % V == 0 && ((a.per / V) & (a.per / V - 1)) == 0)
+        for (a.lane_shift = 0; V << a.lane_shift < a.per;) ++a.lane_shift;
+    a.sub_shift = 0;
+    while ((a.G << (a.sub_shift + 1)) <= LANES && (2 << a.sub_shift) <= a.per) ++a.sub_shift;
+    a.inv_per = ((1u << 20) + a.per - 1) / a.per;
     size_t words = static_cast<size_t>(kTokens) * (2 * a.k + 2 * (LANES * V + 4));
-    if (a.G > 1 && !a.lane_groups) words += static_cast<size_t>(kTokens) * a.G;
-    // below 26 KiB up to 512 experts, 50 KiB for 1024 in 1024 groups
+    if (a.G > 1 && a.lane_shift < 0) words += static_cast<size_t>(kTokens) * 2 * a.G;
+    // below 33 KiB up to 512 experts, 65 KiB for 1024 in 1024 groups
     return launch_tokens<LANES>(dtype == FP8MLP_F32 ? route_kernel<LANES, V, float> : route_kernel<LANES, V, uint16_t>, a,
                                 words * sizeof(float), st);
 }
