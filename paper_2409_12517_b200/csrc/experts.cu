@@ -9,60 +9,85 @@ namespace {
 constexpr uint32_t kAll = 0xffffffffu;
 
 // ---------------------------------------------------------------- plan
-// Counting sort by one cluster.  Every warp owns a contiguous piece of the slots: it counts its slots per expert, the
-// counts become start positions (over experts, then CTAs, then warps), and a second walk over the same piece hands them
-// out in order - no atomics, so the order is that of the slots.
+// Counting sort by one cluster.  Every warp owns a contiguous piece of the slots: it counts them through, 32 at a time,
+// which gives each slot its place among those of its expert in the piece; the counts of all pieces then become start
+// positions (over experts, then CTAs, then warps), and a second walk adds them.  No atomics: the order is that of the
+// slots.  Which lanes of 32 share an expert follows from one ballot per bit of the expert's number (a match instruction
+// took about 70 cycles of its SM each and made the plan of 131072 slots take 39 us).
 constexpr int kPlanWarps = 32;
-constexpr int kPlanMaxCluster = 8;
+constexpr int kPlanMaxCluster = 16;
+constexpr int kPlanUnroll = 4;
+constexpr int kPlanPiece = 32 * kPlanUnroll;
 
 struct PlanArgs {
     const int32_t* experts; int32_t *counts, *offsets, *rows;
     int64_t n;             // slots
     int64_t per_warp;      // slots of a warp, a multiple of 32
-    int E;
+    int E, bits;           // experts, bits of the largest expert's number
+    int key_warps;         // warps of a CTA that own slots (a CTA has more where the experts outnumber them)
 };
 
 __global__ void __launch_bounds__(kPlanWarps * 32) plan_kernel(const PlanArgs a) {
-    extern __shared__ int32_t hist[];                    // [warps][E]: counts, then start positions
+    extern __shared__ int32_t hist[];                    // [key_warps][E]: counts, then start positions
     __shared__ int32_t scan_part[kPlanWarps];
     __shared__ int32_t total[FP8MLP_MAX_EXPERTS];        // this CTA's slots per expert; the cluster reads it
+    __shared__ int32_t start[FP8MLP_MAX_EXPERTS];        // where this CTA's first slot of an expert goes
     const int warps = blockDim.x / 32, warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     uint32_t n_cta;
     asm("mov.u32 %0, %%cluster_nctarank;" : "=r"(n_cta));
     const uint32_t rank = cluster_ctarank();
     const int E = a.E;
-    const int64_t begin = (static_cast<int64_t>(rank) * warps + warp) * a.per_warp;
-    const int64_t end = begin + a.per_warp < a.n ? begin + a.per_warp : a.n;
-    int32_t* mine = hist + warp * E;
-    for (int e = lane; e < E; e += 32) mine[e] = 0;
+    for (int i = threadIdx.x; i < a.key_warps * E; i += blockDim.x) hist[i] = 0;
     grid_dependency_wait();
     grid_launch_dependents();
-    __syncwarp();
-    for (int64_t i0 = begin; i0 < end; i0 += 32) {
-        const int64_t i = i0 + lane;
-        const int e = i < end ? __ldg(a.experts + i) : -1;
-        const bool used = static_cast<uint32_t>(e) < static_cast<uint32_t>(E);
-        const uint32_t same = __match_any_sync(kAll, used ? e : -1);
-        if (used && lane == __ffs(same) - 1) mine[e] += __popc(same);
-        __syncwarp();
+    int64_t begin = (static_cast<int64_t>(rank) * a.key_warps + warp) * a.per_warp;
+    int64_t end = begin + a.per_warp < a.n ? begin + a.per_warp : a.n;
+    if (warp >= a.key_warps) begin = end = 0;
+    int32_t* mine = hist + warp * E;
+    const uint32_t below = (1u << lane) - 1u;
+    __syncthreads();
+    const bool once = a.per_warp <= kPlanPiece;          // the piece stays in registers between the two walks
+    int e[kPlanUnroll], place[kPlanUnroll];
+    for (int64_t i0 = begin + lane; i0 - lane < end; i0 += kPlanPiece) {
+#pragma unroll
+        for (int u = 0; u < kPlanUnroll; ++u) e[u] = i0 + 32 * u < end ? __ldg(a.experts + i0 + 32 * u) : -1;
+#pragma unroll
+        for (int u = 0; u < kPlanUnroll; ++u) {
+            const bool used = static_cast<uint32_t>(e[u]) < static_cast<uint32_t>(E);
+            uint32_t same = __ballot_sync(kAll, used);
+            for (int b = 0; b < a.bits; ++b) {
+                const bool bit = (e[u] >> b & 1) != 0;
+                const uint32_t ones = __ballot_sync(kAll, bit);
+                same &= bit ? ones : ~ones;
+            }
+            const int32_t lower = __popc(same & below);
+            place[u] = used ? mine[e[u]] + lower : -1;
+            __syncwarp();
+            if (used && lower == 0) mine[e[u]] = place[u] + __popc(same);
+            __syncwarp();
+            if (!once && i0 + 32 * u < end) a.rows[i0 + 32 * u] = place[u];
+        }
     }
     __syncthreads();
     for (int e = threadIdx.x; e < E; e += blockDim.x) {
         int32_t run = 0;
-        for (int w = 0; w < warps; ++w) {
+#pragma unroll 8
+        for (int w = 0; w < a.key_warps; ++w) {
             const int32_t c = hist[w * E + e];
             hist[w * E + e] = run;
             run += c;
         }
         total[e] = run;
     }
-    cluster_sync_all();                                  // every CTA's totals are there
-    // offsets: a scan over the experts, 32 * warps of them at a time
+    if (n_cta > 1) cluster_sync_all();                   // every CTA's totals are there
+    else __syncthreads();
+    // offsets: a scan over the experts, one per thread at a time
     int32_t carry = 0;
     for (int e_base = 0; e_base < E; e_base += blockDim.x) {
         const int e = e_base + threadIdx.x;
         int32_t before = 0, all = 0;
         if (e < E) {
+#pragma unroll 8
             for (uint32_t r = 0; r < n_cta; ++r) {
                 int32_t c;
                 asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(c) : "r"(mapa_shared(smem_u32(&total[e]), r)) : "memory");
@@ -90,25 +115,26 @@ __global__ void __launch_bounds__(kPlanWarps * 32) plan_kernel(const PlanArgs a)
                 a.offsets[e] = offset;
                 if (e == E - 1) a.offsets[E] = offset + all;
             }
-            for (int w = 0; w < warps; ++w) hist[w * E + e] += offset + before;
+            start[e] = offset + before;
         }
         carry += chunk;
         __syncthreads();
     }
-    for (int64_t i0 = begin; i0 < end; i0 += 32) {
-        const int64_t i = i0 + lane;
-        const int e = i < end ? __ldg(a.experts + i) : -1;
-        const bool used = static_cast<uint32_t>(e) < static_cast<uint32_t>(E);
-        const uint32_t same = __match_any_sync(kAll, used ? e : -1);
-        const uint32_t lower = same & ((1u << lane) - 1u);
-        int32_t row = -1;
-        if (used) row = mine[e] + __popc(lower);
-        __syncwarp();
-        if (used && lower == 0u) mine[e] = row + __popc(same);
-        __syncwarp();
-        if (i < end) a.rows[i] = row;
+    if (n_cta > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");      // this CTA has read all totals
+    for (int64_t i0 = begin + lane; i0 < end; i0 += kPlanPiece) {
+        if (!once) {
+#pragma unroll
+            for (int u = 0; u < kPlanUnroll; ++u) {
+                const bool in = i0 + 32 * u < end;
+                e[u] = in ? __ldg(a.experts + i0 + 32 * u) : -1;
+                place[u] = in ? a.rows[i0 + 32 * u] : -1;
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kPlanUnroll; ++u)
+            if (i0 + 32 * u < end) a.rows[i0 + 32 * u] = place[u] < 0 ? -1 : place[u] + mine[e[u]] + start[e[u]];
     }
-    cluster_sync_all();                                  // no CTA leaves while another may still read its totals
+    if (n_cta > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");        // and none leaves before the others have
 }
 
 // ---------------------------------------------------------------- rows
@@ -346,15 +372,23 @@ extern "C" int fp8mlp_dispatch_plan(int64_t T, int top_k, int n_experts, const i
     PlanArgs a{};
     a.experts = experts; a.counts = counts; a.offsets = offsets; a.rows = rows;
     a.n = T * top_k; a.E = n_experts;
-    int warps = static_cast<int>(a.n / 64 < kPlanWarps ? a.n / 64 : kPlanWarps);
-    if (warps < 4) warps = 4;
+    while ((1 << a.bits) < n_experts) ++a.bits;
+    // Pieces of kPlanPiece slots fill the warps of one CTA, then of a cluster; beyond that they grow.  Measured with pieces
+    // of 32 / 64 / 128 / 256: 256 x 6 slots 5.7 / 5.1 / 3.9 / 4.9 us, 8192 x 6 7.7 / 7.6 / 6.5 / 8.3 us.
+    int64_t workers = (a.n + kPlanPiece - 1) / kPlanPiece;
     int cluster = 1;
-    while (cluster < kPlanMaxCluster && a.n > static_cast<int64_t>(cluster) * warps * 64) cluster *= 2;
-    const int64_t workers = static_cast<int64_t>(cluster) * warps;
+    while (cluster < kPlanMaxCluster && workers > static_cast<int64_t>(cluster) * kPlanWarps) cluster *= 2;
+    int64_t key_warps = (workers + cluster - 1) / cluster;
+    a.key_warps = static_cast<int>(key_warps < 1 ? 1 : key_warps > kPlanWarps ? kPlanWarps : key_warps);
+    workers = static_cast<int64_t>(cluster) * a.key_warps;
     a.per_warp = ((a.n + workers - 1) / workers + 31) / 32 * 32;
-    const size_t smem = static_cast<size_t>(warps) * n_experts * sizeof(int32_t);
-    FP8MLP_CUDA_CHECK(cudaFuncSetAttribute(plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                           kPlanWarps * FP8MLP_MAX_EXPERTS * static_cast<int>(sizeof(int32_t))));
+    int warps = (n_experts + 31) / 32;                   // the scan takes a thread per expert
+    if (warps < a.key_warps) warps = a.key_warps;
+    const size_t smem = static_cast<size_t>(a.key_warps) * n_experts * sizeof(int32_t);
+    if (smem > 40 * 1024)
+        FP8MLP_CUDA_CHECK(cudaFuncSetAttribute(plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                               kPlanWarps * FP8MLP_MAX_EXPERTS * static_cast<int>(sizeof(int32_t))));
+    if (cluster > 8) FP8MLP_CUDA_CHECK(cudaFuncSetAttribute(plan_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(cluster));
     cfg.blockDim = dim3(static_cast<unsigned>(warps * 32));
