@@ -360,7 +360,7 @@ _DTYPES = {torch.bfloat16: BF16, torch.float32: F32}
 
 def _as(t, dtype, numel, what):
     """Device pointer of a contiguous CUDA tensor of the given type and size."""
-    if t.dtype != dtype or t.numel() != numel or not t.is_cuda or not t.is_contiguous():
+    if t.dtype is not dtype or t.numel() != numel or not (t.is_cuda and t.is_contiguous()):
         raise ValueError(f"{what}: a contiguous CUDA tensor of {numel} {dtype} elements is needed, "
                          f"got {tuple(t.shape)} {t.dtype} on {t.device}")
     return t.data_ptr()
@@ -369,7 +369,7 @@ def _as(t, dtype, numel, what):
 def _matrix(t, cols, what, dtype=None):
     """(pointer, type, row stride) of a 2-D CUDA tensor whose rows are contiguous; any row stride >= its columns."""
     code = _DTYPES.get(t.dtype)
-    if t.dim() != 2 or t.size(1) != cols or code is None or (dtype is not None and t.dtype != dtype) or not t.is_cuda:
+    if t.dim() != 2 or t.size(1) != cols or code is None or (dtype is not None and t.dtype is not dtype) or not t.is_cuda:
         raise ValueError(f"{what}: a 2-D CUDA tensor of {cols} columns in {dtype or 'bfloat16 or float32'} is needed, "
                          f"got {tuple(t.shape)} {t.dtype} on {t.device}")
     ld, step = t.stride()

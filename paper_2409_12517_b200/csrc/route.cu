@@ -333,14 +333,14 @@ __global__ void __launch_bounds__(kRouteThreads, V > 8 ? 4 : LANES == 32 ? 12 : 
         D += score[i];
     }
     D = seg_sum<LANES>(D);
-    const float inv = !a.renorm ? 1.0f : D == 0.0f ? 0.0f : rcp_approx(D);
     if (live) {
 #pragma unroll
         for (int i = 0; i < kMine; ++i) {
             const int r = lane + i * LANES;
             if (r < a.k) {
                 a.experts[t * a.k + r] = expert[i];
-                a.weights[t * a.k + r] = score[i] * inv * a.scale;
+                const float w = a.renorm ? (D == 0.0f ? 0.0f : __fdiv_rn(score[i], D)) : score[i];
+                a.weights[t * a.k + r] = w * a.scale;
             }
         }
     }
@@ -387,7 +387,7 @@ __global__ void __launch_bounds__(kRouteThreads) route_backward_sparse_kernel(co
     float g = s * dw;
     if (a.renorm) {
         const float D = seg_sum<LANES>(s);
-        const float r = D == 0.0f ? 0.0f : s * rcp_approx(D);
+        const float r = D == 0.0f ? 0.0f : __fdiv_rn(s, D);      // exactly 1, and no gradient, for a single expert
         g = r * (dw - seg_sum<LANES>(r * dw));
     }
     if (a.score == FP8MLP_SCORE_SIGMOID) g *= sigmoid_f32(-x);      // 1 - s

@@ -1,0 +1,115 @@
+"""The mixture-of-experts example: one layer's outputs and gradients against the unquantised layer in 64 bits, and a short
+training run.  The experts' products are FP8 (E4M3 forward, E5M2 backward: relative steps of 2^-4 and 2^-3, errors that
+average over a contraction), so outputs are held to 10 % of their norm and gradients to 20 % and a cosine above 0.97; routing
+and clipping themselves are held to tight bounds in their own tests."""
+import pytest
+import torch
+
+from examples.moe_training_step import MoeLayer, train
+from paper_2409_12517_b200 import binding as B
+
+pytestmark = pytest.mark.gpu
+
+
+def _reference(layer, x, dy):
+    """(y, dx, gradients) of the unquantised layer for the experts that were chosen, by automatic differentiation in fp64."""
+    x = x.double().requires_grad_()
+    params = [p.detach().double().clone().requires_grad_() for p in layer.params]
+    chosen = layer.experts.long()
+    s = torch.gather(torch.sigmoid(x @ params[0]), 1, chosen)
+    w = s / s.sum(-1, keepdim=True)
+    y = torch.zeros_like(x)
+    for e in range(layer.E):
+        W1, W2, W3 = params[1 + 3 * e: 4 + 3 * e]
+        gate = x @ W2
+        out = (gate * torch.sigmoid(gate) * (x @ W1)) @ W3
+        y = y + out * (w * (chosen == e)).sum(-1, keepdim=True)
+    y.backward(dy.double())
+    return y.detach(), x.grad, [p.grad for p in params]
+
+
+@pytest.mark.parametrize("E,k,groups", [(8, 2, 1), (16, 3, 4)])
+def test_layer_against_the_unquantised_one(E, k, groups):
+    T, d, f = 300, 128, 208
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    layer = MoeLayer(d, f, E, k, T * k, n_groups=groups, top_groups=max(1, groups // 2), w_std=0.2, seed=1)
+    try:
+        x = torch.randn((T, d), generator=gen, device="cuda").bfloat16()
+        dy = torch.randn((T, d), generator=gen, device="cuda").bfloat16()
+        y = layer.forward(x)
+        dx = layer.backward(dy)
+        assert int(layer.counts.sum()) == T * k and layer.offsets[-1] == T * k
+        ref_y, ref_dx, ref_grads = _reference(layer, x, dy)
+        rel = lambda a, b: float((a.double() - b).norm() / b.norm())
+        cos = lambda a, b: float((a.double() * b).sum() / (a.double().norm() * b.norm()))
+        assert rel(y, ref_y) < 0.1
+        assert rel(dx, ref_dx) < 0.2 and cos(dx, ref_dx) > 0.97
+        for i, (g, r) in enumerate(zip(layer.grads, ref_grads)):
+            if float(r.norm()) > 0:
+                assert rel(g, r) < 0.2 and cos(g, r) > 0.97, f"parameter {i}"
+        before = [p.clone() for p in layer.params]
+        norm, coef = layer.step(max_norm=1.0).tolist()
+        exact = float(torch.sqrt(sum((g.double() ** 2).sum() for g in layer.grads)))
+        assert abs(norm - exact) <= 1e-6 * exact and abs(coef - min(1.0, 1.0 / (exact + 1e-6))) <= 1e-6
+        assert all(not torch.equal(a, b) for a, b, g in zip(before, layer.params, layer.grads) if bool(g.any()))
+        assert B.fp8mlp_status(layer.contexts[0]) == B.OK
+    finally:
+        layer.close()
+
+
+def test_an_expert_that_no_token_chose():
+    T, d, f, E = 40, 64, 96, 4
+    layer = MoeLayer(d, f, E, 2, T * 2, seed=2)
+    try:
+        layer.bias[3] = -float("inf")                    # out of service
+        x = torch.randn((T, d), device="cuda").bfloat16()
+        layer.grads[1 + 9].fill_(5.0)
+        y = layer.forward(x)
+        layer.backward(torch.ones_like(y))
+        assert int(layer.counts[3]) == 0 and not layer.grads[1 + 9].any()
+        assert torch.isfinite(y).all()
+    finally:
+        layer.close()
+
+
+def test_training_follows_the_unquantised_layer():
+    """30 clipped steps beside the same steps of the unquantised layer in fp64 (its own parameters, plain Adam with exact
+    moments, the FP8 layer's choice of experts): losses within 10 % of each other all the way, and both falling."""
+    T, d, f, E, k, lr, max_norm = 256, 64, 96, 4, 2, 3e-3, 0.05
+    gen = torch.Generator(device="cuda").manual_seed(7)
+    layer = MoeLayer(d, f, E, k, T * k, seed=5)
+    teacher = torch.randn((d, d), generator=gen, device="cuda") / d ** 0.5
+    shadow = MoeLayer.__new__(MoeLayer)                  # parameters only
+    shadow.E, shadow.params = E, [p.double() for p in layer.params]
+    m, v = [torch.zeros_like(p) for p in shadow.params], [torch.zeros_like(p) for p in shadow.params]
+    losses = []
+    try:
+        for step in range(1, 31):
+            x = torch.randn((T, d), generator=gen, device="cuda").bfloat16()
+            target = torch.tanh(x.float() @ teacher)
+            y = layer.forward(x)
+            diff = y.float() - target
+            shadow.experts = layer.experts
+            ref_y, _, _ = _reference(shadow, x, torch.zeros_like(y))
+            ref_diff = ref_y - target.double()
+            _, _, grads = _reference(shadow, x, 2.0 / ref_diff.numel() * ref_diff)
+            layer.backward((2.0 / diff.numel() * diff).bfloat16())
+            layer.step(lr, max_norm)
+            norm = torch.sqrt(sum((g ** 2).sum() for g in grads))
+            coef = torch.clamp(max_norm / (norm + 1e-6), max=1.0)
+            for p, g, a, b in zip(shadow.params, grads, m, v):
+                a.mul_(0.9).add_(g * coef, alpha=0.1)
+                b.mul_(0.95).add_((g * coef) ** 2, alpha=0.05)
+                p -= lr * (a / (1 - 0.9 ** step)) / (torch.sqrt(b / (1 - 0.95 ** step)) + 1e-8)
+            losses.append((float(diff.square().mean()), float(ref_diff.square().mean())))
+    finally:
+        layer.close()
+    for got, ref in losses:
+        assert abs(got - ref) <= 0.1 * ref, losses
+    for side in (0, 1):
+        assert sum(l[side] for l in losses[-5:]) < sum(l[side] for l in losses[:5]), losses
+
+
+def test_the_example_runs():
+    losses = train(3, tokens=64, d=64, f=96, n_experts=4)
+    assert len(losses) == 3 and all(0.0 < l < 10.0 for l in losses)
