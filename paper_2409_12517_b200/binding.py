@@ -367,15 +367,15 @@ def _as(t, dtype, numel, what):
 
 
 def _matrix(t, cols, what, dtype=None):
-    """(pointer, type, row stride) of a 2-D CUDA tensor whose rows are contiguous; any row stride >= its columns."""
-    code = _DTYPES.get(t.dtype)
-    if t.dim() != 2 or t.size(1) != cols or code is None or (dtype is not None and t.dtype is not dtype) or not t.is_cuda:
+    """(rows, pointer, type, row stride) of a 2-D CUDA tensor whose rows are contiguous; any row stride >= its columns."""
+    shape, code = t.shape, _DTYPES.get(t.dtype)
+    if len(shape) != 2 or shape[1] != cols or code is None or (dtype is not None and t.dtype is not dtype) or not t.is_cuda:
         raise ValueError(f"{what}: a 2-D CUDA tensor of {cols} columns in {dtype or 'bfloat16 or float32'} is needed, "
-                         f"got {tuple(t.shape)} {t.dtype} on {t.device}")
+                         f"got {tuple(shape)} {t.dtype} on {t.device}")
     ld, step = t.stride()
     if step != 1 and cols > 1:
         raise ValueError(f"{what}: the elements of a row must be neighbours")
-    return t.data_ptr(), code, ld if ld >= cols or t.size(0) > 1 else cols      # a single row's stride may be anything
+    return shape[0], t.data_ptr(), code, ld if ld >= cols or shape[0] > 1 else cols      # a single row's stride may be anything
 
 
 def new_router(n_experts: int, top_k: int, score: int = SCORE_SOFTMAX, n_groups: int = 1, top_groups: int = 1,
@@ -386,20 +386,21 @@ def new_router(n_experts: int, top_k: int, score: int = SCORE_SOFTMAX, n_groups:
 def fp8mlp_route(router: Router, logits, bias, experts, weights) -> None:
     """logits: [T, n_experts] bf16 or fp32, any row stride; bias: fp32 [n_experts] or None; receives experts (int32
     [T, top_k]) and weights (fp32 [T, top_k])."""
-    T, n = logits.shape[0], logits.shape[0] * router.top_k
-    ptr, dtype, ld = _matrix(logits, router.n_experts, "logits")
-    _check(lib().fp8mlp_route(router, T, ptr, dtype, ld,
-                              None if bias is None else _as(bias, torch.float32, router.n_experts, "bias"),
+    E = router.n_experts
+    T, ptr, dtype, ld = _matrix(logits, E, "logits")
+    n = T * router.top_k
+    _check(lib().fp8mlp_route(router, T, ptr, dtype, ld, None if bias is None else _as(bias, torch.float32, E, "bias"),
                               _as(experts, torch.int32, n, "experts"), _as(weights, torch.float32, n, "weights"), _stream()),
            "fp8mlp_route")
 
 
 def fp8mlp_route_backward(router: Router, logits, experts, d_weights, d_logits) -> None:
     """d_logits (type of the logits, any row stride) from d_weights (fp32 [T, top_k]) for the experts the forward chose."""
-    T, n = logits.shape[0], logits.shape[0] * router.top_k
-    ptr, dtype, ld = _matrix(logits, router.n_experts, "logits")
-    d_ptr, _, ld_d = _matrix(d_logits, router.n_experts, "d_logits", logits.dtype)
-    if d_logits.shape[0] != T:
+    E = router.n_experts
+    T, ptr, dtype, ld = _matrix(logits, E, "logits")
+    d_rows, d_ptr, _, ld_d = _matrix(d_logits, E, "d_logits", logits.dtype)
+    n = T * router.top_k
+    if d_rows != T:
         raise ValueError("d_logits: not as many rows as logits")
     _check(lib().fp8mlp_route_backward(router, T, ptr, dtype, ld, _as(experts, torch.int32, n, "experts"),
                                        _as(d_weights, torch.float32, n, "d_weights"), d_ptr, ld_d, _stream()),
@@ -424,32 +425,35 @@ def fp8mlp_dispatch_plan(experts, n_experts: int, counts, offsets, rows) -> None
 
 
 def _rows_pair(token, expert, rows, token_name, expert_name):
+    """What dispatch and combine pass alike: (tokens, slots, d, type, token pointer and row stride, expert pointer and rows,
+    rows pointer)."""
     T, k = rows.shape
-    ptr, dtype, ld = _matrix(token, expert.shape[1], token_name, expert.dtype)
-    if token.shape[0] != T:
-        raise ValueError(f"{token_name}: {token.shape[0]} rows, but rows speaks of {T} tokens")
-    return T, k, ptr, dtype, ld, _as(expert, token.dtype, expert.numel(), expert_name), _as(rows, torch.int32, T * k, "rows")
+    n, d = expert.shape
+    have, ptr, dtype, ld = _matrix(token, d, token_name, expert.dtype)
+    if have != T:
+        raise ValueError(f"{token_name}: {have} rows, but rows speaks of {T} tokens")
+    return T, k, d, dtype, ptr, ld, _as(expert, expert.dtype, n * d, expert_name), n, _as(rows, torch.int32, T * k, "rows")
 
 
 def fp8mlp_dispatch(x, rows, xe) -> None:
     """xe[rows[t, j]] = x[t]; x: [T, d] bf16 or fp32, any row stride; xe: [n, d] of the same type, contiguous."""
-    T, k, ptr, dtype, ld, xe_ptr, rows_ptr = _rows_pair(x, xe, rows, "x", "xe")
-    _check(lib().fp8mlp_dispatch(T, k, x.shape[1], dtype, ptr, ld, rows_ptr, xe_ptr, xe.shape[0], _stream()), "fp8mlp_dispatch")
+    T, k, d, dtype, ptr, ld, xe_ptr, n, rows_ptr = _rows_pair(x, xe, rows, "x", "xe")
+    _check(lib().fp8mlp_dispatch(T, k, d, dtype, ptr, ld, rows_ptr, xe_ptr, n, _stream()), "fp8mlp_dispatch")
 
 
 def fp8mlp_combine(ye, rows, weights, y) -> None:
     """y[t] = sum_j weights[t, j] ye[rows[t, j]]; weights fp32 [T, top_k] or None (= 1); y: [T, d], any row stride."""
-    T, k, ptr, dtype, ld, ye_ptr, rows_ptr = _rows_pair(y, ye, rows, "y", "ye")
-    _check(lib().fp8mlp_combine(T, k, y.shape[1], dtype, ye_ptr, ye.shape[0], rows_ptr,
+    T, k, d, dtype, ptr, ld, ye_ptr, n, rows_ptr = _rows_pair(y, ye, rows, "y", "ye")
+    _check(lib().fp8mlp_combine(T, k, d, dtype, ye_ptr, n, rows_ptr,
                                 None if weights is None else _as(weights, torch.float32, T * k, "weights"), ptr, ld, _stream()),
            "fp8mlp_combine")
 
 
 def fp8mlp_combine_backward(dy, ye, rows, weights, dye, d_weights) -> None:
     """dye[rows[t, j]] = weights[t, j] dy[t] and d_weights[t, j] = <dy[t], ye[rows[t, j]]> (fp32 [T, top_k])."""
-    T, k, ptr, dtype, ld, ye_ptr, rows_ptr = _rows_pair(dy, ye, rows, "dy", "ye")
-    _check(lib().fp8mlp_combine_backward(T, k, dy.shape[1], dtype, ptr, ld, ye_ptr, ye.shape[0], rows_ptr,
-                                         _as(weights, torch.float32, T * k, "weights"), _as(dye, ye.dtype, ye.numel(), "dye"),
+    T, k, d, dtype, ptr, ld, ye_ptr, n, rows_ptr = _rows_pair(dy, ye, rows, "dy", "ye")
+    _check(lib().fp8mlp_combine_backward(T, k, d, dtype, ptr, ld, ye_ptr, n, rows_ptr,
+                                         _as(weights, torch.float32, T * k, "weights"), _as(dye, ye.dtype, n * d, "dye"),
                                          _as(d_weights, torch.float32, T * k, "d_weights"), _stream()),
            "fp8mlp_combine_backward")
 
