@@ -71,11 +71,15 @@ __global__ void __launch_bounds__(kPlanWarps * 32) plan_kernel(const PlanArgs a)
     __syncthreads();
     for (int e = threadIdx.x; e < E; e += blockDim.x) {
         int32_t run = 0;
-#pragma unroll 8
-        for (int w = 0; w < a.key_warps; ++w) {
-            const int32_t c = hist[w * E + e];
-            hist[w * E + e] = run;
-            run += c;
+        for (int w0 = 0; w0 < a.key_warps; w0 += 8) {        // eight counts are read before any is replaced
+            int32_t c[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) c[i] = w0 + i < a.key_warps ? hist[(w0 + i) * E + e] : 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if (w0 + i < a.key_warps) hist[(w0 + i) * E + e] = run;
+                run += c[i];
+            }
         }
         total[e] = run;
     }
@@ -206,10 +210,10 @@ __global__ void __launch_bounds__(kRowThreads) dispatch_kernel(const RowArgs a) 
     }
 }
 
-constexpr int kCombineSlots = 4;       // slots whose loads are in flight together
-
-template <typename T, int W, bool WEIGHTED>
-__global__ void __launch_bounds__(kRowThreads) combine_kernel(const RowArgs a) {
+// S slots of U units are in flight together.  More would cost occupancy (6 or 8 slots of 32 bytes ran 6 to 18 % slower
+// than 3), fewer leave the memory idle, and a last batch that is not full does too.
+template <typename T, int W, bool WEIGHTED, int S, int U>
+__global__ void __launch_bounds__(kRowThreads, S == 4 ? 4 : 0) combine_kernel(const RowArgs a) {
     constexpr int E = Word<T>::kElems;
     grid_dependency_wait();
     grid_launch_dependents();
@@ -217,48 +221,60 @@ __global__ void __launch_bounds__(kRowThreads) combine_kernel(const RowArgs a) {
     const int64_t t = static_cast<int64_t>(blockIdx.x) * (blockDim.x / a.threads_per_token) + in_block;
     if (t >= a.T) return;
     const uint32_t step = a.threads_per_token * W * 4;
-    for (uint32_t at = lane * W * 4; at < a.row_bytes; at += step) {
-        float acc[W * E];
+    for (uint32_t at = lane * W * 4; at < a.row_bytes; at += U * step) {
+        float acc[U][W * E];
 #pragma unroll
-        for (int i = 0; i < W * E; ++i) acc[i] = 0.0f;
-        for (int j0 = 0; j0 < a.k; j0 += kCombineSlots) {
-            uint32_t w[kCombineSlots][W];
-            int64_t off[kCombineSlots];
-            float scale[kCombineSlots];
+        for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int j = 0; j < kCombineSlots; ++j) {
+            for (int i = 0; i < W * E; ++i) acc[u][i] = 0.0f;
+        for (int j0 = 0; j0 < a.k; j0 += S) {
+            uint32_t w[S][U][W];
+            int64_t off[S];
+            float scale[S];
+#pragma unroll
+            for (int j = 0; j < S; ++j) {
                 off[j] = j0 + j < a.k ? row_offset(a, t * a.k + j0 + j) : -1;
                 scale[j] = WEIGHTED && off[j] >= 0 ? __ldg(a.weights + t * a.k + j0 + j) : 1.0f;
             }
 #pragma unroll
-            for (int j = 0; j < kCombineSlots; ++j)
-                if (off[j] >= 0) load_unit<W>(a.src + off[j] + at, w[j]);
+            for (int j = 0; j < S; ++j)
 #pragma unroll
-            for (int j = 0; j < kCombineSlots; ++j) {
+                for (int u = 0; u < U; ++u)
+                    if (off[j] >= 0 && (u == 0 || at + u * step < a.row_bytes)) load_unit<W>(a.src + off[j] + at + u * step, w[j][u]);
+#pragma unroll
+            for (int j = 0; j < S; ++j) {
                 if (off[j] < 0) continue;
 #pragma unroll
-                for (int i = 0; i < W; ++i) {
-                    float v[E];
-                    Word<T>::get(w[j][i], v);
+                for (int u = 0; u < U; ++u)
 #pragma unroll
-                    for (int e = 0; e < E; ++e)
-                        acc[i * E + e] = WEIGHTED ? fmaf(scale[j], v[e], acc[i * E + e]) : acc[i * E + e] + v[e];
-                }
+                    for (int i = 0; i < W; ++i) {
+                        float v[E];
+                        Word<T>::get(w[j][u][i], v);
+#pragma unroll
+                        for (int e = 0; e < E; ++e) {
+                            float& sum = acc[u][i * E + e];
+                            sum = WEIGHTED ? fmaf(scale[j], v[e], sum) : sum + v[e];
+                        }
+                    }
             }
         }
-        uint32_t out[W];
 #pragma unroll
-        for (int i = 0; i < W; ++i) out[i] = Word<T>::put(acc + i * E);
-        store_unit<W>(a.dst + t * a.token_bytes + at, out);
+        for (int u = 0; u < U; ++u) {
+            if (u > 0 && at + u * step >= a.row_bytes) break;
+            uint32_t out[W];
+#pragma unroll
+            for (int i = 0; i < W; ++i) out[i] = Word<T>::put(acc[u] + i * E);
+            store_unit<W>(a.dst + t * a.token_bytes + at + u * step, out);
+        }
     }
 }
 
 // One block per token; dy is read once for kSlots slots, every slot's row of ye once.
 constexpr int kSlots = 8;
 
-template <typename T>
+template <typename T, int W>
 __global__ void __launch_bounds__(kRowThreads) combine_backward_kernel(const RowArgs a) {
-    constexpr int W = 4, E = Word<T>::kElems;
+    constexpr int E = Word<T>::kElems, kBatch = W == 8 ? 2 : 4;       // slots whose loads are in flight together
     __shared__ float part[kRowThreads / 32][kSlots];
     grid_dependency_wait();
     grid_launch_dependents();
@@ -276,25 +292,29 @@ __global__ void __launch_bounds__(kRowThreads) combine_backward_kernel(const Row
             dot[j] = 0.0f;
         }
         for (uint32_t at = threadIdx.x * W * 4; at < a.row_bytes; at += blockDim.x * W * 4) {
-            uint32_t g[W], w[kSlots][W];
+            uint32_t g[W];
             load_unit<W>(dy + at, g);
 #pragma unroll
-            for (int j = 0; j < kSlots; ++j)
-                if (off[j] >= 0) load_unit<W>(a.src + off[j] + at, w[j]);
+            for (int b = 0; b < kSlots; b += kBatch) {
+                uint32_t w[kBatch][W];
 #pragma unroll
-            for (int j = 0; j < kSlots; ++j) {
-                if (off[j] < 0) continue;
-                uint32_t out[W];
+                for (int j = 0; j < kBatch; ++j)
+                    if (off[b + j] >= 0) load_unit<W>(a.src + off[b + j] + at, w[j]);
 #pragma unroll
-                for (int i = 0; i < W; ++i) {
-                    float v[E], d[E], o[E];
-                    Word<T>::get(g[i], d);
-                    Word<T>::get(w[j][i], v);
+                for (int j = 0; j < kBatch; ++j) {
+                    if (off[b + j] < 0) continue;
+                    uint32_t out[W];
 #pragma unroll
-                    for (int e = 0; e < E; ++e) { dot[j] = fmaf(d[e], v[e], dot[j]); o[e] = scale[j] * d[e]; }
-                    out[i] = Word<T>::put(o);
+                    for (int i = 0; i < W; ++i) {
+                        float v[E], d[E], o[E];
+                        Word<T>::get(g[i], d);
+                        Word<T>::get(w[j][i], v);
+#pragma unroll
+                        for (int e = 0; e < E; ++e) { dot[b + j] = fmaf(d[e], v[e], dot[b + j]); o[e] = scale[b + j] * d[e]; }
+                        out[i] = Word<T>::put(o);
+                    }
+                    store_unit<W>(a.dst + off[b + j] + at, out);
                 }
-                store_unit<W>(a.dst + off[j] + at, out);
             }
         }
 #pragma unroll
@@ -343,8 +363,8 @@ RowArgs row_args(int64_t T, int top_k, int64_t d, int dtype, int64_t ld, int64_t
 // Blocks of about kRowThreads threads.  A row's units are dealt evenly to as few rounds of threads as fit a block (whole
 // warps, so that a warp's accesses are neighbours); short rows share a block.
 struct RowGrid { dim3 grid; int threads; };
-int row_grid(RowArgs* a, int unit_bytes, RowGrid* g) {
-    const int units = static_cast<int>(a->row_bytes) / unit_bytes;
+int row_grid(RowArgs* a, int unit_bytes, RowGrid* g) {      // unit_bytes: what a thread takes at a time
+    const int units = (static_cast<int>(a->row_bytes) + unit_bytes - 1) / unit_bytes;
     const int rounds = (units + kRowThreads - 1) / kRowThreads;
     a->threads_per_token = units <= 32 ? units : ((units + rounds - 1) / rounds + 31) / 32 * 32;
     int tokens = kRowThreads / a->threads_per_token;
@@ -354,6 +374,31 @@ int row_grid(RowArgs* a, int unit_bytes, RowGrid* g) {
     g->grid = dim3(static_cast<unsigned>(blocks));
     g->threads = tokens * a->threads_per_token;
     return FP8MLP_OK;
+}
+
+template <typename T, int W, bool WEIGHTED, int S, int U>
+int launch_combine(RowArgs a, cudaStream_t st) {
+    RowGrid g;
+    const int rg = row_grid(&a, W * 4 * U, &g);
+    if (rg != FP8MLP_OK) return rg;
+    FP8MLP_CUDA_CHECK(launch_chained(combine_kernel<T, W, WEIGHTED, S, U>, g.grid, g.threads, 0, st, a));
+    FP8MLP_LAUNCH_CHECK();
+    return FP8MLP_OK;
+}
+
+template <typename T, bool WEIGHTED>
+int run_combine(const RowArgs& a, bool wide, cudaStream_t st) {
+    if (!wide) return launch_combine<T, 4, WEIGHTED, 4, 1>(a, st);
+    if (a.k == 1) return launch_combine<T, 8, WEIGHTED, 1, 2>(a, st);
+    // As many slots at a time as leave the fewest places of the last batch empty, and of these the most.  8192 rows of
+    // 4096 bf16 in us, 2 / 3 / 4 at a time (k = 1: one slot of two units 25.7, else 29.5 / 30.4 / 34.1):
+    //   k = 2: 35.2 / 36.2 / 38.8   3: 47.4 / 42.3 / 44.8   4: 53.6 / 55.1 / 51.6   5: 66.2 / 62.2 / 66.7
+    //   k = 6: 72.6 / 69.9 / 73.2   7: 85.0 / 82.0 / 80.3   8: 92.0 / 89.9 / 88.7
+    int best = 4;
+    for (int s = 3; s >= 2; --s)
+        if ((a.k + s - 1) / s * s < (a.k + best - 1) / best * best) best = s;
+    if (best == 4) return launch_combine<T, 8, WEIGHTED, 4, 1>(a, st);
+    return best == 3 ? launch_combine<T, 8, WEIGHTED, 3, 1>(a, st) : launch_combine<T, 8, WEIGHTED, 2, 1>(a, st);
 }
 
 }  // namespace
@@ -437,20 +482,9 @@ extern "C" int fp8mlp_combine(int64_t T, int top_k, int64_t d, int dtype, const 
     a.dst = static_cast<uint8_t*>(y);
     a.weights = weights;
     const bool wide = aligned(y, 32) && aligned(ye, 32) && a.token_bytes % 32 == 0;
-    RowGrid g;
-    const int rg = row_grid(&a, wide ? 32 : 16, &g);
-    if (rg != FP8MLP_OK) return rg;
-    void (*kernel)(const RowArgs) = nullptr;
-    if (dtype == FP8MLP_F32) {
-        if (weights != nullptr) kernel = wide ? combine_kernel<float, 8, true> : combine_kernel<float, 4, true>;
-        else kernel = wide ? combine_kernel<float, 8, false> : combine_kernel<float, 4, false>;
-    } else {
-        if (weights != nullptr) kernel = wide ? combine_kernel<uint16_t, 8, true> : combine_kernel<uint16_t, 4, true>;
-        else kernel = wide ? combine_kernel<uint16_t, 8, false> : combine_kernel<uint16_t, 4, false>;
-    }
-    FP8MLP_CUDA_CHECK(launch_chained(kernel, g.grid, g.threads, 0, static_cast<cudaStream_t>(stream), a));
-    FP8MLP_LAUNCH_CHECK();
-    return FP8MLP_OK;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (dtype == FP8MLP_F32) return weights != nullptr ? run_combine<float, true>(a, wide, st) : run_combine<float, false>(a, wide, st);
+    return weights != nullptr ? run_combine<uint16_t, true>(a, wide, st) : run_combine<uint16_t, false>(a, wide, st);
 }
 
 extern "C" int fp8mlp_combine_backward(int64_t T, int top_k, int64_t d, int dtype, const void* dy, int64_t ld_dy,
@@ -470,10 +504,12 @@ extern "C" int fp8mlp_combine_backward(int64_t T, int top_k, int64_t d, int dtyp
     a.d_weights = d_weights;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const dim3 grid(static_cast<unsigned>(T));
-    const int units = static_cast<int>(a.row_bytes / 16), rounds = (units + kRowThreads - 1) / kRowThreads;
+    const bool wide = aligned(dy, 32) && aligned(ye, 32) && aligned(dye, 32) && a.token_bytes % 32 == 0;
+    const int units = static_cast<int>(a.row_bytes / (wide ? 32 : 16)), rounds = (units + kRowThreads - 1) / kRowThreads;
     const int threads = ((units + rounds - 1) / rounds + 31) / 32 * 32;
-    if (dtype == FP8MLP_F32) FP8MLP_CUDA_CHECK(launch_chained(combine_backward_kernel<float>, grid, threads, 0, st, a));
-    else FP8MLP_CUDA_CHECK(launch_chained(combine_backward_kernel<uint16_t>, grid, threads, 0, st, a));
+    auto kernel = dtype == FP8MLP_F32 ? (wide ? combine_backward_kernel<float, 8> : combine_backward_kernel<float, 4>)
+                                      : (wide ? combine_backward_kernel<uint16_t, 8> : combine_backward_kernel<uint16_t, 4>);
+    FP8MLP_CUDA_CHECK(launch_chained(kernel, grid, threads, 0, st, a));
     FP8MLP_LAUNCH_CHECK();
     return FP8MLP_OK;
 }
