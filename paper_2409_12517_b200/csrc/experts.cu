@@ -15,6 +15,7 @@ constexpr uint32_t kAll = 0xffffffffu;
 // slots.  Which lanes of 32 share an expert follows from one ballot per bit of the expert's number (a match instruction
 // took about 70 cycles of its SM each and made the plan of 131072 slots take 39 us).
 constexpr int kPlanWarps = 32;
+constexpr int kPlanFill = 8;          // warps of a CTA that own slots before the cluster grows
 constexpr int kPlanMaxCluster = 16;
 constexpr int kPlanUnroll = 4;
 constexpr int kPlanPiece = 32 * kPlanUnroll;
@@ -51,19 +52,24 @@ __global__ void __launch_bounds__(kPlanWarps * 32) plan_kernel(const PlanArgs a)
     for (int64_t i0 = begin + lane; i0 - lane < end; i0 += kPlanPiece) {
 #pragma unroll
         for (int u = 0; u < kPlanUnroll; ++u) e[u] = i0 + 32 * u < end ? __ldg(a.experts + i0 + 32 * u) : -1;
+        uint32_t same[kPlanUnroll];
+#pragma unroll
+        for (int u = 0; u < kPlanUnroll; ++u) same[u] = __ballot_sync(kAll, static_cast<uint32_t>(e[u]) < static_cast<uint32_t>(E));
+        for (int b = 0; b < a.bits; ++b) {
+#pragma unroll
+            for (int u = 0; u < kPlanUnroll; ++u) {
+                const bool bit = (e[u] >> b & 1) != 0;
+                const uint32_t ones = __ballot_sync(kAll, bit);
+                same[u] &= bit ? ones : ~ones;
+            }
+        }
 #pragma unroll
         for (int u = 0; u < kPlanUnroll; ++u) {
             const bool used = static_cast<uint32_t>(e[u]) < static_cast<uint32_t>(E);
-            uint32_t same = __ballot_sync(kAll, used);
-            for (int b = 0; b < a.bits; ++b) {
-                const bool bit = (e[u] >> b & 1) != 0;
-                const uint32_t ones = __ballot_sync(kAll, bit);
-                same &= bit ? ones : ~ones;
-            }
-            const int32_t lower = __popc(same & below);
+            const int32_t lower = __popc(same[u] & below);
             place[u] = used ? mine[e[u]] + lower : -1;
             __syncwarp();
-            if (used && lower == 0) mine[e[u]] = place[u] + __popc(same);
+            if (used && lower == 0) mine[e[u]] = place[u] + __popc(same[u]);
             __syncwarp();
             if (!once && i0 + 32 * u < end) a.rows[i0 + 32 * u] = place[u];
         }
@@ -418,11 +424,12 @@ extern "C" int fp8mlp_dispatch_plan(int64_t T, int top_k, int n_experts, const i
     a.experts = experts; a.counts = counts; a.offsets = offsets; a.rows = rows;
     a.n = T * top_k; a.E = n_experts;
     while ((1 << a.bits) < n_experts) ++a.bits;
-    // Pieces of kPlanPiece slots fill the warps of one CTA, then of a cluster; beyond that they grow.  Measured with pieces
-    // of 32 / 64 / 128 / 256: 256 x 6 slots 5.7 / 5.1 / 3.9 / 4.9 us, 8192 x 6 7.7 / 7.6 / 6.5 / 8.3 us.
+    // Pieces of kPlanPiece slots fill kPlanFill warps of one CTA, then of a cluster, then more warps of it, and then grow.
+    // A CTA's warps share the ballots' issue slots, so CTAs first: 32768 slots 6.1 / 4.3 / 4.3 us with 32 / 16 / 8 warps, 8192
+    // slots of 256 experts 7.5 / 5.1 / 3.9 us.  Pieces of 64 slots take 5.0 and 3.6 us there, but 7.3 instead of 5.8 for 49152.
     int64_t workers = (a.n + kPlanPiece - 1) / kPlanPiece;
     int cluster = 1;
-    while (cluster < kPlanMaxCluster && workers > static_cast<int64_t>(cluster) * kPlanWarps) cluster *= 2;
+    while (cluster < kPlanMaxCluster && workers > static_cast<int64_t>(cluster) * kPlanFill) cluster *= 2;
     int64_t key_warps = (workers + cluster - 1) / cluster;
     a.key_warps = static_cast<int>(key_warps < 1 ? 1 : key_warps > kPlanWarps ? kPlanWarps : key_warps);
     workers = static_cast<int64_t>(cluster) * a.key_warps;
