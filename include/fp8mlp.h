@@ -354,7 +354,7 @@ FP8MLP_API int fp8mlp_gemm_plan(int kind, int64_t M, int64_t N, int64_t K, int s
  * fp8mlp_forward), and the experts' outputs are summed with the router's weights.
  *
  * Routing of T tokens.  x = logits[t, :] (fp32 or bf16, row stride ld_logits elements, any alignment of its type):
- *   s   = softmax(x)  or  sigma(x)                                          (fp32)
+ *   s   = softmax(x)  or  sigma(x)                       (fp32; a sigma below 2^-126 counts as 0)
  *   c_e = s_e + bias_e                      bias[n_experts] nullable; it takes part in the choice alone
  *   n_groups > 1: the experts form n_groups groups of neighbours; a group's value is the sum of its group_top (1 or 2)
  *       largest c; only the top_groups groups of the largest values stay in the choice
@@ -364,6 +364,8 @@ FP8MLP_API int fp8mlp_gemm_plan(int kind, int64_t M, int64_t N, int64_t K, int s
  * An expert whose logit is -inf, or whose c is -inf or NaN, is never chosen (a mask is -inf in the logits, an expert
  * out of service -inf in the bias; a row with a NaN or +inf logit has no softmax).  A token with fewer than top_k
  * experts to choose from gets experts -1 with weights 0 in the slots that are left; a row without any is all -1.
+ * The arrays of this section other than rows of d elements are aligned to their type only; rows (x, xe, ye, y, dy, dye)
+ * start on 16-byte boundaries and d is a multiple of 16.  No output overlaps an input unless a function says so.
  * 1 <= n_experts <= FP8MLP_MAX_EXPERTS, 1 <= top_k <= min(FP8MLP_MAX_TOP_K, n_experts),
  * 1 <= top_groups <= n_groups <= n_experts, n_experts a multiple of n_groups, top_k <= the experts of top_groups groups. */
 enum { FP8MLP_SCORE_SOFTMAX = 0, FP8MLP_SCORE_SIGMOID = 1 };
@@ -385,8 +387,8 @@ FP8MLP_API int fp8mlp_route(const fp8mlp_router* router, int64_t T, const void* 
  *   renormalise, sigmoid: the same times (1 - s_j)                            other experts 0
  *   plain, sigmoid:       dx_j = scale dw_j s_j (1 - s_j)                     other experts 0
  *   plain, softmax:       dx_e = s_e (scale dw_e - sum_j scale dw_j s_j)      dw_e = 0 for those not chosen
- * d_logits has the type of the logits, row stride ld_d_logits, and is overwritten.  Slots with an expert outside
- * 0 .. n_experts - 1 are skipped (their dw is not used); a row without any gets zeros. */
+ * d_logits has the type of the logits, row stride ld_d_logits, is not the logits' own buffer, and is overwritten.
+ * Slots with an expert outside 0 .. n_experts - 1 are skipped (their dw is not used); a row without any gets zeros. */
 FP8MLP_API int fp8mlp_route_backward(const fp8mlp_router* router, int64_t T, const void* logits, int logits_dtype,
                                      int64_t ld_logits, const int32_t* experts, const float* d_weights, void* d_logits,
                                      int64_t ld_d_logits, void* stream);
@@ -396,11 +398,12 @@ FP8MLP_API int fp8mlp_route_update_bias(int n_experts, const int32_t* counts, fl
 /* Where every slot's row goes: rows[t, j] = the row of token t's slot j in expert order (by expert, then by token, then
  * by slot: the order is a function of `experts` alone), -1 for an unused slot (an expert outside 0 .. n_experts - 1).
  * counts[e] = rows of expert e;  offsets[n_experts + 1] = where they begin, offsets[n_experts] = their sum.
- * T * top_k < 2^31. */
+ * T * top_k < 2^31; rows is another buffer than experts. */
 FP8MLP_API int fp8mlp_dispatch_plan(int64_t T, int top_k, int n_experts, const int32_t* experts, int32_t* counts,
                                     int32_t* offsets, int32_t* rows, void* stream);
 /* xe[rows[t, j], :] = x[t, :].  dtype FP8MLP_BF16 or FP8MLP_F32; x has row stride ld_x (elements), xe is contiguous,
- * [n_rows, d].  A slot whose row is outside 0 .. n_rows - 1 writes nothing; rows that no slot names keep what they held.
+ * [n_rows, d].  A slot whose row is outside 0 .. n_rows - 1 writes nothing; rows that no slot names keep what they held,
+ * and no row is named twice (a plan names each once).
  * Its gradient is fp8mlp_combine of the rows' gradients without weights. */
 FP8MLP_API int fp8mlp_dispatch(int64_t T, int top_k, int64_t d, int dtype, const void* x, int64_t ld_x, const int32_t* rows,
                                void* xe, int64_t n_rows, void* stream);

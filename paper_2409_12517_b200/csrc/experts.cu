@@ -350,7 +350,7 @@ int check_rows(int64_t T, int top_k, int64_t d, int dtype, const void* token, in
     if (T > 0x7fffffff / top_k || n_rows > 0x7fffffff) return FP8MLP_ERR_SHAPE;
     if (T == 0) return FP8MLP_OK;
     if (ld < d) return FP8MLP_ERR_SHAPE;
-    if (token == nullptr || rows == nullptr || (expert == nullptr && n_rows > 0)) return FP8MLP_ERR_ARG;
+    if (token == nullptr || rows == nullptr || (expert == nullptr && n_rows > 0) || token == expert) return FP8MLP_ERR_ARG;
     const int64_t esize = dtype == FP8MLP_F32 ? 4 : 2;
     if (!aligned(token, 16) || !aligned(expert, 16) || ld * esize % 16 != 0 || !aligned(rows, 4)) return FP8MLP_ERR_ALIGN;
     return FP8MLP_OK;
@@ -418,7 +418,8 @@ extern "C" int fp8mlp_dispatch_plan(int64_t T, int top_k, int n_experts, const i
     if (T < 0 || top_k < 1 || top_k > FP8MLP_MAX_TOP_K || n_experts < 1 || n_experts > FP8MLP_MAX_EXPERTS ||
         T > 0x7fffffff / top_k)
         return FP8MLP_ERR_SHAPE;
-    if (counts == nullptr || offsets == nullptr || (T > 0 && (experts == nullptr || rows == nullptr))) return FP8MLP_ERR_ARG;
+    if (counts == nullptr || offsets == nullptr || (T > 0 && (experts == nullptr || rows == nullptr || rows == experts)))
+        return FP8MLP_ERR_ARG;
     if (!aligned(experts, 4) || !aligned(counts, 4) || !aligned(offsets, 4) || !aligned(rows, 4)) return FP8MLP_ERR_ALIGN;
     PlanArgs a{};
     a.experts = experts; a.counts = counts; a.offsets = offsets; a.rows = rows;

@@ -314,20 +314,22 @@ __global__ void __launch_bounds__(kRouteThreads, V > 8 ? 4 : LANES == 32 ? 12 : 
         if (r < a.k && sel[r].x > -CUDART_INF_F) {
             const float want = sel[r].x;
             const int owner = __float_as_int(sel[r].y), from = owner * V;
-            int skip = 0;            // equal values of one lane are taken in turn, lowest expert first
+            // equal values of one lane are taken in turn, lowest expert first: the first place of the value, and for the
+            // next of its equals one place further each
+            int skip = 0;
             while (skip < r && sel[r - 1 - skip].x == want && __float_as_int(sel[r - 1 - skip].y) == owner) ++skip;
+            int place = from;
 #pragma unroll
-            for (int j = 0; j < V; j += 4) {
+            for (int j = V - 4; j >= 0; j -= 4) {
                 const float4 q = *reinterpret_cast<const float4*>(row_c + from + j);
-                const float four[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-                for (int m = 0; m < 4; ++m) {
-                    if (four[m] == want) {
-                        if (skip == 0) expert[i] = from + j + m;
-                        --skip;
-                    }
-                }
+                if (q.w == want) place = from + j + 3;
+                if (q.z == want) place = from + j + 2;
+                if (q.y == want) place = from + j + 1;
+                if (q.x == want) place = from + j;
             }
+            for (; skip > 0; --skip)
+                do { ++place; } while (place < from + V - 1 && row_c[place] != want);
+            expert[i] = place;
             score[i] = biased ? row_s[expert[i]] : want;
         }
         D += score[i];
@@ -601,7 +603,8 @@ extern "C" int fp8mlp_route_backward(const fp8mlp_router* r, int64_t T, const vo
     if (dtype != FP8MLP_BF16 && dtype != FP8MLP_F32) return FP8MLP_ERR_ARG;
     if (T < 0 || (T > 0 && (ld < r->n_experts || ld_d < r->n_experts))) return FP8MLP_ERR_SHAPE;
     if (T == 0) return FP8MLP_OK;
-    if (logits == nullptr || experts == nullptr || d_weights == nullptr || d_logits == nullptr) return FP8MLP_ERR_ARG;
+    if (logits == nullptr || experts == nullptr || d_weights == nullptr || d_logits == nullptr || d_logits == logits)
+        return FP8MLP_ERR_ARG;
     const int esize = dtype == FP8MLP_F32 ? 4 : 2;
     if (!multiple_of(logits, esize) || !multiple_of(d_logits, esize) || !multiple_of(experts, 4) || !multiple_of(d_weights, 4))
         return FP8MLP_ERR_ALIGN;

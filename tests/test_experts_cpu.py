@@ -43,10 +43,11 @@ def test_route_refusals(lib):
     assert route(r, x=P + 2) == B.ERR_ALIGN and route(r, x=P + 1, dt=B.BF16) == B.ERR_ALIGN
     assert route(r, bias=P + 2) == B.ERR_ALIGN and route(r, e=P + 1) == B.ERR_ALIGN and route(r, w=P + 2) == B.ERR_ALIGN
     assert route(r, T=0, x=None, e=None, w=None, ld=0) == B.OK
-    back = lambda r, T=4, x=P, dt=B.F32, ld=8, e=P, w=P, dx=P, ldd=8: lib.fp8mlp_route_backward(r, T, x, dt, ld, e, w, dx, ldd, None)
+    back = lambda r, T=4, x=P, dt=B.F32, ld=8, e=P, w=P, dx=2 * P, ldd=8: lib.fp8mlp_route_backward(r, T, x, dt, ld, e, w, dx, ldd, None)
     assert back(None) == B.ERR_ARG and back(r, dt=5) == B.ERR_ARG
     assert back(r, ld=7) == B.ERR_SHAPE and back(r, ldd=7) == B.ERR_SHAPE and back(r, T=-2) == B.ERR_SHAPE
     assert back(r, x=None) == B.ERR_ARG and back(r, dx=None) == B.ERR_ARG and back(r, e=None) == B.ERR_ARG and back(r, w=None) == B.ERR_ARG
+    assert back(r, dx=P, x=P) == B.ERR_ARG             # not in place
     assert back(r, dx=P + 2) == B.ERR_ALIGN and back(r, w=P + 2) == B.ERR_ALIGN
     assert back(r, T=0) == B.OK
     bias = lib.fp8mlp_route_update_bias
@@ -56,10 +57,11 @@ def test_route_refusals(lib):
 
 
 def test_plan_refusals(lib):
-    plan = lambda T=4, k=2, E=8, e=P, c=P, o=P, r=P: lib.fp8mlp_dispatch_plan(T, k, E, e, c, o, r, None)
+    plan = lambda T=4, k=2, E=8, e=P, c=P, o=P, r=2 * P: lib.fp8mlp_dispatch_plan(T, k, E, e, c, o, r, None)
     assert plan(T=-1) == B.ERR_SHAPE and plan(k=0) == B.ERR_SHAPE and plan(k=33) == B.ERR_SHAPE
     assert plan(E=0) == B.ERR_SHAPE and plan(E=1025) == B.ERR_SHAPE and plan(T=2 ** 30, k=4) == B.ERR_SHAPE
     assert plan(e=None) == B.ERR_ARG and plan(c=None) == B.ERR_ARG and plan(o=None) == B.ERR_ARG and plan(r=None) == B.ERR_ARG
+    assert plan(r=P) == B.ERR_ARG                      # rows is not experts
     assert plan(e=P + 2) == B.ERR_ALIGN and plan(c=P + 1) == B.ERR_ALIGN and plan(o=P + 2) == B.ERR_ALIGN and plan(r=P + 2) == B.ERR_ALIGN
 
 
@@ -76,6 +78,7 @@ def test_row_refusals(lib):
         assert call(**{token: None}) == B.ERR_ARG and call(r=None) == B.ERR_ARG and call(**{expert: None}) == B.ERR_ARG
         assert call(**{token: P + 8}) == B.ERR_ALIGN and call(**{expert: P + 8}) == B.ERR_ALIGN and call(ld=36) == B.ERR_ALIGN
         assert call(r=P + 2) == B.ERR_ALIGN
+        assert call(**{token: 2 * P}) == B.ERR_ARG     # token and expert rows are different buffers
         assert call(T=0) == B.OK
     assert comb(w=P + 2) == B.ERR_ALIGN
     assert back(w=None) == B.ERR_ARG and back(dw=None) == B.ERR_ARG and back(dye=None) == B.ERR_ARG
