@@ -83,7 +83,7 @@ class _GradTensor(C.Structure):
     _fields_ = [("g", C.c_void_p), ("out", C.c_void_p), ("n", C.c_int64), ("dtype", C.c_int32)]
 
 
-_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_raw_stream, _device = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
 _lib = None
 
 
@@ -160,9 +160,7 @@ def _ptr(t):
 def _stream():
     """The current stream's handle.  torch.cuda.current_stream() builds a stream object around it, which takes longer
     (3.4 us) than a launch; the accessor that torch's own generated code uses takes 0.1 us."""
-    if _raw_stream is not None:
-        return _raw_stream(torch._C._cuda_getDevice())
-    return torch.cuda.current_stream().cuda_stream
+    return _raw_stream(_device()) if _raw_stream is not None else torch.cuda.current_stream().cuda_stream
 
 
 def _check(code: int, where: str):
@@ -356,6 +354,7 @@ def fp8mlp_gemm_bf16(M: int, N: int, K: int, A, a_kmajor: bool, B, b_kmajor: boo
 # ---------------------------------------------------------------- experts of one layer, and clipping
 
 _DTYPES = {torch.bfloat16: BF16, torch.float32: F32}
+_F32, _I32, _U8 = torch.float32, torch.int32, torch.uint8
 
 
 def _as(t, dtype, numel, what):
@@ -389,8 +388,8 @@ def fp8mlp_route(router: Router, logits, bias, experts, weights) -> None:
     E = router.n_experts
     T, ptr, dtype, ld = _matrix(logits, E, "logits")
     n = T * router.top_k
-    _check(lib().fp8mlp_route(router, T, ptr, dtype, ld, None if bias is None else _as(bias, torch.float32, E, "bias"),
-                              _as(experts, torch.int32, n, "experts"), _as(weights, torch.float32, n, "weights"), _stream()),
+    _check(lib().fp8mlp_route(router, T, ptr, dtype, ld, None if bias is None else _as(bias, _F32, E, "bias"),
+                              _as(experts, _I32, n, "experts"), _as(weights, _F32, n, "weights"), _stream()),
            "fp8mlp_route")
 
 
@@ -402,15 +401,15 @@ def fp8mlp_route_backward(router: Router, logits, experts, d_weights, d_logits) 
     n = T * router.top_k
     if d_rows != T:
         raise ValueError("d_logits: not as many rows as logits")
-    _check(lib().fp8mlp_route_backward(router, T, ptr, dtype, ld, _as(experts, torch.int32, n, "experts"),
-                                       _as(d_weights, torch.float32, n, "d_weights"), d_ptr, ld_d, _stream()),
+    _check(lib().fp8mlp_route_backward(router, T, ptr, dtype, ld, _as(experts, _I32, n, "experts"),
+                                       _as(d_weights, _F32, n, "d_weights"), d_ptr, ld_d, _stream()),
            "fp8mlp_route_backward")
 
 
 def fp8mlp_route_update_bias(counts, rate: float, bias) -> None:
     """bias (fp32 [n_experts], in place) moves by rate towards the experts with fewer rows than the mean (counts, int32)."""
     n = bias.numel()
-    _check(lib().fp8mlp_route_update_bias(n, _as(counts, torch.int32, n, "counts"), rate, _as(bias, torch.float32, n, "bias"),
+    _check(lib().fp8mlp_route_update_bias(n, _as(counts, _I32, n, "counts"), rate, _as(bias, _F32, n, "bias"),
                                           _stream()), "fp8mlp_route_update_bias")
 
 
@@ -418,10 +417,10 @@ def fp8mlp_dispatch_plan(experts, n_experts: int, counts, offsets, rows) -> None
     """experts: int32 [T, top_k]; receives counts (int32 [n_experts]), offsets (int32 [n_experts + 1]) and rows (int32
     [T, top_k])."""
     T, k = experts.shape
-    _check(lib().fp8mlp_dispatch_plan(T, k, n_experts, _as(experts, torch.int32, T * k, "experts"),
-                                      _as(counts, torch.int32, n_experts, "counts"),
-                                      _as(offsets, torch.int32, n_experts + 1, "offsets"),
-                                      _as(rows, torch.int32, T * k, "rows"), _stream()), "fp8mlp_dispatch_plan")
+    _check(lib().fp8mlp_dispatch_plan(T, k, n_experts, _as(experts, _I32, T * k, "experts"),
+                                      _as(counts, _I32, n_experts, "counts"),
+                                      _as(offsets, _I32, n_experts + 1, "offsets"),
+                                      _as(rows, _I32, T * k, "rows"), _stream()), "fp8mlp_dispatch_plan")
 
 
 def _rows_pair(token, expert, rows, token_name, expert_name):
@@ -432,7 +431,7 @@ def _rows_pair(token, expert, rows, token_name, expert_name):
     have, ptr, dtype, ld = _matrix(token, d, token_name, expert.dtype)
     if have != T:
         raise ValueError(f"{token_name}: {have} rows, but rows speaks of {T} tokens")
-    return T, k, d, dtype, ptr, ld, _as(expert, expert.dtype, n * d, expert_name), n, _as(rows, torch.int32, T * k, "rows")
+    return T, k, d, dtype, ptr, ld, _as(expert, expert.dtype, n * d, expert_name), n, _as(rows, _I32, T * k, "rows")
 
 
 def fp8mlp_dispatch(x, rows, xe) -> None:
@@ -445,7 +444,7 @@ def fp8mlp_combine(ye, rows, weights, y) -> None:
     """y[t] = sum_j weights[t, j] ye[rows[t, j]]; weights fp32 [T, top_k] or None (= 1); y: [T, d], any row stride."""
     T, k, d, dtype, ptr, ld, ye_ptr, n, rows_ptr = _rows_pair(y, ye, rows, "y", "ye")
     _check(lib().fp8mlp_combine(T, k, d, dtype, ye_ptr, n, rows_ptr,
-                                None if weights is None else _as(weights, torch.float32, T * k, "weights"), ptr, ld, _stream()),
+                                None if weights is None else _as(weights, _F32, T * k, "weights"), ptr, ld, _stream()),
            "fp8mlp_combine")
 
 
@@ -453,8 +452,8 @@ def fp8mlp_combine_backward(dy, ye, rows, weights, dye, d_weights) -> None:
     """dye[rows[t, j]] = weights[t, j] dy[t] and d_weights[t, j] = <dy[t], ye[rows[t, j]]> (fp32 [T, top_k])."""
     T, k, d, dtype, ptr, ld, ye_ptr, n, rows_ptr = _rows_pair(dy, ye, rows, "dy", "ye")
     _check(lib().fp8mlp_combine_backward(T, k, d, dtype, ptr, ld, ye_ptr, n, rows_ptr,
-                                         _as(weights, torch.float32, T * k, "weights"), _as(dye, ye.dtype, n * d, "dye"),
-                                         _as(d_weights, torch.float32, T * k, "d_weights"), _stream()),
+                                         _as(weights, _F32, T * k, "weights"), _as(dye, ye.dtype, n * d, "dye"),
+                                         _as(d_weights, _F32, T * k, "d_weights"), _stream()),
            "fp8mlp_combine_backward")
 
 
@@ -486,14 +485,14 @@ def new_norm_workspace(device="cuda"):
 
 def fp8mlp_grad_norm(grads: GradList, norm_kind: int, max_norm: float, norm_coef, workspace) -> None:
     """norm_coef (fp32 [2]) receives the global norm and min(1, max_norm / (norm + 1e-6))."""
-    _check(lib().fp8mlp_grad_norm(grads.array, grads.count, norm_kind, max_norm, _as(norm_coef, torch.float32, 2, "norm_coef"),
-                                  _as(workspace, torch.uint8, NORM_WORKSPACE_BYTES, "workspace"), _stream()), "fp8mlp_grad_norm")
+    _check(lib().fp8mlp_grad_norm(grads.array, grads.count, norm_kind, max_norm, _as(norm_coef, _F32, 2, "norm_coef"),
+                                  _as(workspace, _U8, NORM_WORKSPACE_BYTES, "workspace"), _stream()), "fp8mlp_grad_norm")
 
 
 def fp8mlp_clip_grads(grads: GradList, norm_kind: int, max_norm: float, norm_coef, workspace) -> None:
     """fp8mlp_grad_norm, and out = g * coefficient for every tensor of the list."""
-    _check(lib().fp8mlp_clip_grads(grads.array, grads.count, norm_kind, max_norm, _as(norm_coef, torch.float32, 2, "norm_coef"),
-                                   _as(workspace, torch.uint8, NORM_WORKSPACE_BYTES, "workspace"), _stream()),
+    _check(lib().fp8mlp_clip_grads(grads.array, grads.count, norm_kind, max_norm, _as(norm_coef, _F32, 2, "norm_coef"),
+                                   _as(workspace, _U8, NORM_WORKSPACE_BYTES, "workspace"), _stream()),
            "fp8mlp_clip_grads")
 
 

@@ -1,7 +1,11 @@
 // Global gradient norm over many tensors, and clipping to it.
 //
-// The list travels in the kernel's parameters, cut into chunks that are numbered through: a block takes every grid-th
-// chunk, whatever tensor it belongs to, so a thousand small tensors cost one launch and no block waits for a large one.
+// The list travels in the kernel's parameters, cut into chunks that are numbered through and dealt to the blocks whatever
+// tensor they belong to, so a thousand small tensors cost one launch and no block waits for a large one.
+//
+// The norm reads every byte once (541 MB fp32: 79 us, 6.9 TB/s; 271 MB bf16: 41 us).  Clipping has to know the norm before it
+// writes, so it reads them again: three passes over the bytes, less what L2 keeps (541 MB: 243 us, at the measured copy rate
+// the three passes less 64 MB would take 238).  The Adam pass can apply the coefficient instead and saves two of the three.
 #include <cmath>
 
 #include "common.cuh"
@@ -14,7 +18,7 @@ constexpr uint32_t kAll = 0xffffffffu;
 constexpr int kClipThreads = 256;
 constexpr int kClipBlocksPerSm = 4;
 constexpr int kClipMaxBlocks = FP8MLP_NORM_WORKSPACE_BYTES / 8;    // one fp64 partial each
-constexpr int kUnroll = 4;                                         // 32-byte accesses in flight per thread
+constexpr int kUnroll = 4;                                         // 32-byte accesses in flight per thread (2: 1 % slower)
 constexpr int64_t kChunkUnits = kClipThreads * kUnroll;            // 32-byte units of a chunk
 constexpr float kNormEps = 1e-6f;
 // The clipping pass walks the chunks from the last to the first: it finds what the norm pass read last still in L2.  So that

@@ -197,6 +197,8 @@ __device__ __forceinline__ int64_t row_offset(const RowArgs& a, int64_t slot) {
     return row < a.n_rows ? static_cast<int64_t>(row) * a.row_bytes : -1;
 }
 
+// A row of x is read once and written once per slot: bound by DRAM writes.  16384 x 4096 bf16 to two rows each: 61 us for
+// 403 MB, 6.6 TB/s.
 template <int W>
 __global__ void __launch_bounds__(kRowThreads) dispatch_kernel(const RowArgs a) {
     grid_dependency_wait();
@@ -216,8 +218,9 @@ __global__ void __launch_bounds__(kRowThreads) dispatch_kernel(const RowArgs a) 
     }
 }
 
-// S slots of U units are in flight together.  More would cost occupancy (6 or 8 slots of 32 bytes ran 6 to 18 % slower
-// than 3), fewer leave the memory idle, and a last batch that is not full does too.
+// Bound by DRAM reads: 8192 x 4096 bf16 from six rows each take 69.9 us for 470 MB, 6.7 TB/s.  S slots of U units are in
+// flight together.  More would cost occupancy (6 or 8 slots of 32 bytes ran 6 to 18 % slower than 3), fewer leave the
+// memory idle, and a last batch that is not full does too.
 template <typename T, int W, bool WEIGHTED, int S, int U>
 __global__ void __launch_bounds__(kRowThreads, S == 4 ? 4 : 0) combine_kernel(const RowArgs a) {
     constexpr int E = Word<T>::kElems;
@@ -275,7 +278,9 @@ __global__ void __launch_bounds__(kRowThreads, S == 4 ? 4 : 0) combine_kernel(co
     }
 }
 
-// One block per token; dy is read once for kSlots slots, every slot's row of ye once.
+// One block per token; dy is read once for kSlots slots, every slot's row of ye once, and the dot products stay in
+// registers until the row's end.  8192 x 4096 bf16 with six rows each: 131.5 us for 873 MB, 6.6 TB/s (the measured copy
+// rate is 6.5); with four 32-byte units in flight 157 us, with eight 16-byte units 143.
 constexpr int kSlots = 8;
 
 template <typename T, int W>
