@@ -113,3 +113,57 @@ def test_training_follows_the_unquantised_layer():
 def test_the_example_runs():
     losses = train(3, tokens=64, d=64, f=96, n_experts=4)
     assert len(losses) == 3 and all(0.0 < l < 10.0 for l in losses)
+
+
+def test_the_chain_in_a_cuda_graph():
+    """Routing, plan, dispatch, combine, their gradients and clipping captured once and replayed on new inputs: the same bits as
+    the calls themselves."""
+    T, E, k, d = 700, 64, 6, 256
+    gen = torch.Generator(device="cuda").manual_seed(11)
+    router = B.new_router(E, k, B.SCORE_SIGMOID, 8, 4, 2, True, 2.5)
+    new = lambda *shape, dtype=torch.float32: torch.zeros(shape, dtype=dtype, device="cuda")
+    logits, bias, x, dy = new(T, E), new(E), new(T, d, dtype=torch.bfloat16), new(T, d, dtype=torch.bfloat16)
+    out = dict(experts=new(T, k, dtype=torch.int32), weights=new(T, k), counts=new(E, dtype=torch.int32),
+               offsets=new(E + 1, dtype=torch.int32), rows=new(T, k, dtype=torch.int32), xe=new(T * k, d, dtype=torch.bfloat16),
+               y=new(T, d, dtype=torch.bfloat16), dye=new(T * k, d, dtype=torch.bfloat16), dw=new(T, k), dx=new(T, d, dtype=torch.bfloat16),
+               dlogits=new(T, E), norm_coef=new(2), clipped=new(T, E))
+    lst, ws = B.new_grad_list([out["dlogits"]], [out["clipped"]]), B.new_norm_workspace()
+
+    def chain():
+        B.fp8mlp_route(router, logits, bias, out["experts"], out["weights"])
+        B.fp8mlp_dispatch_plan(out["experts"], E, out["counts"], out["offsets"], out["rows"])
+        B.fp8mlp_dispatch(x, out["rows"], out["xe"])
+        B.fp8mlp_combine(out["xe"], out["rows"], out["weights"], out["y"])
+        B.fp8mlp_combine_backward(dy, out["xe"], out["rows"], out["weights"], out["dye"], out["dw"])
+        B.fp8mlp_combine(out["dye"], out["rows"], None, out["dx"])
+        B.fp8mlp_route_backward(router, logits, out["experts"], out["dw"], out["dlogits"])
+        B.fp8mlp_clip_grads(lst, B.NORM_L2, 0.5, out["norm_coef"], ws)
+
+    def inputs():
+        for t in (logits, x, dy):
+            t.copy_(torch.randn(t.shape, generator=gen, device="cuda"))
+        bias.copy_(0.05 * torch.randn(E, generator=gen, device="cuda"))
+
+    inputs()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        chain()
+        side.synchronize()
+        with torch.cuda.graph(graph, stream=side):
+            chain()
+    torch.cuda.current_stream().wait_stream(side)
+    for _ in range(3):
+        inputs()
+        chain()
+        want = {n: t.clone() for n, t in out.items()}
+        for t in out.values():
+            t.fill_(-3)
+        graph.replay()
+        torch.cuda.synchronize()
+        for n, t in out.items():
+            assert torch.equal(t, want[n]), n
+        # y = sum of the weights times x, up to the rounding of y
+        total = want["weights"].sum(-1, keepdim=True) * x.float()
+        assert torch.allclose(want["y"].float(), total, rtol=2.0 ** -7, atol=1e-6)
