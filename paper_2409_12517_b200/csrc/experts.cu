@@ -1,5 +1,7 @@
 // Tokens into expert order and back: the plan (a stable counting sort of the chosen experts), the copy of the rows, the
 // weighted sum of the experts' outputs and its gradient.
+#include <atomic>
+
 #include "common.cuh"
 
 namespace fp8mlp {
@@ -346,6 +348,35 @@ __global__ void __launch_bounds__(kRowThreads) combine_backward_kernel(const Row
 
 bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
+// Clusters of 16 CTAs are beyond the portable size: whether the device has room for one (a part of a GPU may not) is asked
+// once per device, for the largest CTA that a plan launches.
+int plan_max_cluster(int* limit) {
+    static std::atomic<int> known[64];
+    int dev = 0;
+    FP8MLP_CUDA_CHECK(cudaGetDevice(&dev));
+    *limit = dev < 64 ? known[dev].load(std::memory_order_relaxed) : 0;
+    if (*limit != 0) return FP8MLP_OK;
+    const int smem = kPlanWarps * FP8MLP_MAX_EXPERTS * static_cast<int>(sizeof(int32_t));
+    FP8MLP_CUDA_CHECK(cudaFuncSetAttribute(plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    FP8MLP_CUDA_CHECK(cudaFuncSetAttribute(plan_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(kPlanMaxCluster);
+    cfg.blockDim = dim3(kPlanWarps * 32);
+    cfg.dynamicSmemBytes = smem;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = kPlanMaxCluster;
+    attr[0].val.clusterDim.y = 1;
+    attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    int fit = 0;
+    FP8MLP_CUDA_CHECK(cudaOccupancyMaxActiveClusters(&fit, plan_kernel, &cfg));
+    *limit = fit > 0 ? kPlanMaxCluster : 8;
+    if (dev < 64) known[dev].store(*limit, std::memory_order_relaxed);
+    return FP8MLP_OK;
+}
+
 // What dispatch, combine and its gradient refuse alike; token / expert are the two row tensors.
 int check_rows(int64_t T, int top_k, int64_t d, int dtype, const void* token, int64_t ld, const void* expert, int64_t n_rows,
                const int32_t* rows) {
@@ -435,7 +466,12 @@ extern "C" int fp8mlp_dispatch_plan(int64_t T, int top_k, int n_experts, const i
     // slots of 256 experts 7.5 / 5.1 / 3.9 us.  Pieces of 64 slots take 5.0 and 3.6 us there, but 7.3 instead of 5.8 for 49152.
     int64_t workers = (a.n + kPlanPiece - 1) / kPlanPiece;
     int cluster = 1;
-    while (cluster < kPlanMaxCluster && workers > static_cast<int64_t>(cluster) * kPlanFill) cluster *= 2;
+    int max_cluster = 8;
+    if (workers > 8 * kPlanFill) {
+        const int rc = plan_max_cluster(&max_cluster);
+        if (rc != FP8MLP_OK) return rc;
+    }
+    while (cluster < max_cluster && workers > static_cast<int64_t>(cluster) * kPlanFill) cluster *= 2;
     int64_t key_warps = (workers + cluster - 1) / cluster;
     a.key_warps = static_cast<int>(key_warps < 1 ? 1 : key_warps > kPlanWarps ? kPlanWarps : key_warps);
     workers = static_cast<int64_t>(cluster) * a.key_warps;
@@ -446,7 +482,6 @@ extern "C" int fp8mlp_dispatch_plan(int64_t T, int top_k, int n_experts, const i
     if (smem > 40 * 1024)
         FP8MLP_CUDA_CHECK(cudaFuncSetAttribute(plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                                kPlanWarps * FP8MLP_MAX_EXPERTS * static_cast<int>(sizeof(int32_t))));
-    if (cluster > 8) FP8MLP_CUDA_CHECK(cudaFuncSetAttribute(plan_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(cluster));
     cfg.blockDim = dim3(static_cast<unsigned>(warps * 32));
