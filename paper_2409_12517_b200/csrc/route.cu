@@ -143,39 +143,50 @@ template <int V> __device__ __forceinline__ void put_row(float* row, const float
     for (int j = 0; j < V; j += 4) *reinterpret_cast<float4*>(row + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
 }
 
-// The choice: every lane sorts its values c, eight at a time, and the token's lanes take the largest head k times.  The
-// kernel is bound by instructions, not by memory (16384 tokens, 8 of 256 experts in 4 of 8 groups: 605 warp instructions
-// a token, 13.6 us where the bytes need 2.7; without groups and bias 9.3 us), so a round moves values only; which expert a
-// value belongs to is looked up once at the end, by k lanes side by side, in the unsorted row in shared memory.
-// -inf stands for "cannot be chosen".  A token alone takes 2.4 us, most of it the launch.
-// Blocks per SM: 12 of 40 registers with a whole warp per token (16 of 32: 14.0 us), 16 where tokens share a warp (64
-// experts: 5.9 us, 7.3 with 12).  More experts per lane and fewer lanes per token were slower or equal.
-template <int LANES, int V, typename SRC>
-__global__ void __launch_bounds__(kRouteThreads, V > 8 ? 4 : LANES == 32 ? 12 : 16) route_kernel(const RouteArgs a) {
-    extern __shared__ __align__(16) float smem[];
-    constexpr int kTokens = kRouteThreads / LANES;
-    constexpr int kRow = LANES * V + 4;                   // + 4: rows of neighbouring tokens start in other banks
-    constexpr int kLists = V / 8;
-    const int lane = threadIdx.x % LANES, tok = threadIdx.x / LANES;
-    const int seg_base = (threadIdx.x & 31) - lane;
-    float* row_c = smem + tok * kRow;                                               // this token's values ...
-    float* row_s = smem + (kTokens + tok) * kRow;                                   // ... and scores
-    float2* sel = reinterpret_cast<float2*>(smem + 2 * kTokens * kRow) + tok * a.k; // a round's value and its lane
-    float* group_c = smem + 2 * kTokens * (kRow + a.k) + tok * 2 * a.G;     // groups off the lanes: values, then what is kept
-    const int e0 = lane * V;
-    const int64_t t = static_cast<int64_t>(blockIdx.x) * kTokens + tok;
-    const bool live = t < a.T, biased = a.bias != nullptr;
-    grid_dependency_wait();
-    grid_launch_dependents();
-
-    float s[V], bias[V], c[kLists][8];
-    if (live) {
-        load_row<V, SRC>(static_cast<const SRC*>(a.logits) + t * a.ld, e0, a.E, a.wide != 0, s);
-    } else {
-#pragma unroll
-        for (int j = 0; j < V; ++j) s[j] = -CUDART_INF_F;
+// Groups that do not fall on lanes: their values through shared memory (the row, then values and verdicts of the groups),
+// 2^sub_shift lanes to a group.  Takes the experts of the groups that are not kept out of the lane's values.
+template <int LANES, int V>
+__device__ __forceinline__ void drop_groups_in_shared(const RouteArgs& a, int lane, int e0, float* row_c, float* group_c, float (&s)[V]) {
+    put_row<V>(row_c + e0, s);
+    __syncwarp();
+    const int sub = lane & ((1 << a.sub_shift) - 1), sub_lanes = 1 << a.sub_shift, at_once = LANES >> a.sub_shift;
+    for (int g0 = 0; g0 < a.G; g0 += at_once) {
+        const int g = g0 + (lane >> a.sub_shift);
+        float c1 = -CUDART_INF_F, c2 = -CUDART_INF_F;
+        if (g < a.G) {
+            for (int i = sub; i < a.per; i += sub_lanes) {
+                const float v = row_c[g * a.per + i];
+                c2 = fmaxf(c2, fminf(c1, v));
+                c1 = fmaxf(c1, v);
+            }
+        }
+        for (int o = 1; o < sub_lanes; o <<= 1) {
+            const float b1 = __shfl_xor_sync(kAll, c1, o), b2 = __shfl_xor_sync(kAll, c2, o);
+            merge_top2(c1, c2, b1, b2);
+        }
+        if (g < a.G && sub == 0) group_c[g] = group_value(c1, c2, a.group_top);
     }
-    if (biased) load_row<V, float>(a.bias, e0, a.E, a.wide_b != 0, bias);
+    __syncwarp();
+    float* group_keep = group_c + a.G;
+    for (int g0 = 0; g0 < a.G; g0 += at_once) {
+        const int g = g0 + (lane >> a.sub_shift);
+        int rank = 0;
+        if (g < a.G) {
+            const float mine = group_c[g];
+            for (int i = sub; i < a.G; i += sub_lanes) rank += (i < g ? group_c[i] >= mine : group_c[i] > mine) ? 1 : 0;
+        }
+        for (int o = 1; o < sub_lanes; o <<= 1) rank += __shfl_xor_sync(kAll, rank, o);
+        if (g < a.G && sub == 0) group_keep[g] = rank < a.top_groups ? CUDART_INF_F : -CUDART_INF_F;
+    }
+    __syncwarp();
+#pragma unroll
+    for (int j = 0; j < V; ++j)          // e / per by a product that is exact for e, per <= 1024
+        if (e0 + j < a.E) s[j] = fminf(s[j], group_keep[(static_cast<uint32_t>(e0 + j) * a.inv_per) >> 20]);
+}
+
+// Scores and values of the choice of one token, s: in logits, out values c; the scores go to row_s where a bias parts them.
+template <int LANES, int V>
+__device__ __forceinline__ void score_row(const RouteArgs& a, int e0, bool biased, const float (&bias)[V], float* row_s, float (&s)[V]) {
     // Sums that come out as a number above -inf show that no logit is masked and no value NaN or -inf: additions run beside
     // the comparisons (another pipe, the one that limits this kernel), and masks are rare.
     float sum_x = s[0];
@@ -204,148 +215,195 @@ __global__ void __launch_bounds__(kRouteThreads, V > 8 ? 4 : LANES == 32 ? 12 : 
 #pragma unroll
         for (int j = 0; j < V; ++j) s[j] = (masked >> j & 1u) != 0u ? -CUDART_INF_F : fmaxf(s[j], -CUDART_INF_F);   // NaN: -inf
     }
+}
 
-    if (a.G > 1 && a.lane_shift < 0) {
-        // Groups that do not fall on lanes: their values through shared memory, 2^sub_shift lanes to a group.
-        put_row<V>(row_c + e0, s);
-        __syncwarp();
-        const int sub = lane & ((1 << a.sub_shift) - 1), sub_lanes = 1 << a.sub_shift, at_once = LANES >> a.sub_shift;
-        for (int g0 = 0; g0 < a.G; g0 += at_once) {
-            const int g = g0 + (lane >> a.sub_shift);
-            float c1 = -CUDART_INF_F, c2 = -CUDART_INF_F;
-            if (g < a.G) {
-                for (int i = sub; i < a.per; i += sub_lanes) {
-                    const float v = row_c[g * a.per + i];
-                    c2 = fmaxf(c2, fminf(c1, v));
-                    c1 = fmaxf(c1, v);
-                }
-            }
-            for (int o = 1; o < sub_lanes; o <<= 1) {
-                const float b1 = __shfl_xor_sync(kAll, c1, o), b2 = __shfl_xor_sync(kAll, c2, o);
-                merge_top2(c1, c2, b1, b2);
-            }
-            if (g < a.G && sub == 0) group_c[g] = group_value(c1, c2, a.group_top);
-        }
-        __syncwarp();
-        float* group_keep = group_c + a.G;
-        for (int g0 = 0; g0 < a.G; g0 += at_once) {
-            const int g = g0 + (lane >> a.sub_shift);
-            int rank = 0;
-            if (g < a.G) {
-                const float mine = group_c[g];
-                for (int i = sub; i < a.G; i += sub_lanes) rank += (i < g ? group_c[i] >= mine : group_c[i] > mine) ? 1 : 0;
-            }
-            for (int o = 1; o < sub_lanes; o <<= 1) rank += __shfl_xor_sync(kAll, rank, o);
-            if (g < a.G && sub == 0) group_keep[g] = rank < a.top_groups ? CUDART_INF_F : -CUDART_INF_F;
-        }
-        __syncwarp();
+// The choice: every lane sorts its values c, eight at a time, and the token's lanes take the largest head k times.  The
+// kernel is bound by instructions, not by memory (16384 tokens, 8 of 256 experts in 4 of 8 groups: 605 warp instructions
+// a token with Q = 1), so a round moves values only; which expert a value belongs to is looked up once at the end, by k
+// lanes side by side, in the unsorted row in shared memory.  -inf stands for "cannot be chosen".
+// The lanes hold Q tokens, whose steps are interleaved: the group loops and rounds run once for both, and one's reductions
+// wait behind the other's.  With Q = 2 those 16384 tokens take 11.9 us instead of 13.7 (65536: 35.8 and 43.8, 8192: 9.1
+// and 8.5, 4096: 5.2 and 6.6; the bytes need 2.7 at 16384); without groups 9.7 and 9.4, one token 2.6 and 2.2.
+// Blocks per SM with Q = 1: 12 of 40 registers with a whole warp per token (16 of 32: 14.0 us), 16 where tokens share a
+// warp (64 experts: 5.9 us, 7.3 with 12).  More experts per lane and fewer lanes per token were slower or equal.
+template <int LANES, int V, int Q, typename SRC>
+__global__ void __launch_bounds__(kRouteThreads, Q > 1 ? 8 : V > 8 ? 4 : LANES == 32 ? 12 : 16) route_kernel(const RouteArgs a) {
+    extern __shared__ __align__(16) float smem[];
+    constexpr int kTokens = kRouteThreads / LANES * Q;
+    constexpr int kRow = LANES * V + 4;                   // + 4: rows of neighbouring tokens start in other banks
+    constexpr int kLists = V / 8;
+    const int lane = threadIdx.x % LANES, seg_base = (threadIdx.x & 31) - lane;
+    const int e0 = lane * V;
+    const bool biased = a.bias != nullptr;
+    float *row_c[Q], *row_s[Q], *group_c[Q];              // a token's values and scores; its groups, where they are off the lanes
+    float2* sel[Q];                                       // a round's value and its lane
+    int64_t t[Q];
 #pragma unroll
-        for (int j = 0; j < V; ++j)          // e / per by a product that is exact for e, per <= 1024
-            if (e0 + j < a.E) s[j] = fminf(s[j], group_keep[(static_cast<uint32_t>(e0 + j) * a.inv_per) >> 20]);
+    for (int q = 0; q < Q; ++q) {
+        const int tok = threadIdx.x / LANES * Q + q;
+        row_c[q] = smem + tok * kRow;
+        row_s[q] = smem + (kTokens + tok) * kRow;
+        sel[q] = reinterpret_cast<float2*>(smem + 2 * kTokens * kRow) + tok * a.k;
+        group_c[q] = smem + 2 * kTokens * (kRow + a.k) + tok * 2 * a.G;
+        t[q] = static_cast<int64_t>(blockIdx.x) * kTokens + tok;
     }
-    put_row<V>(row_c + e0, s);
+    grid_dependency_wait();
+    grid_launch_dependents();
+
+    float s[Q][V], bias[V], c[Q][kLists][8];
 #pragma unroll
-    for (int l = 0; l < kLists; ++l) {
+    for (int q = 0; q < Q; ++q) {
+        if (t[q] < a.T) {
+            load_row<V, SRC>(static_cast<const SRC*>(a.logits) + t[q] * a.ld, e0, a.E, a.wide != 0, s[q]);
+        } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) c[l][j] = s[l * 8 + j];
-        sort8(c[l]);
+            for (int j = 0; j < V; ++j) s[q][j] = -CUDART_INF_F;
+        }
+    }
+    if (biased) load_row<V, float>(a.bias, e0, a.E, a.wide_b != 0, bias);
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+        score_row<LANES, V>(a, e0, biased, bias, row_s[q], s[q]);
+        if constexpr (Q == 1) {
+            if (a.G > 1 && a.lane_shift < 0) drop_groups_in_shared<LANES, V>(a, lane, e0, row_c[q], group_c[q], s[q]);
+        }
+        put_row<V>(row_c[q] + e0, s[q]);
+#pragma unroll
+        for (int l = 0; l < kLists; ++l) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) c[q][l][j] = s[q][l * 8 + j];
+            sort8(c[q][l]);
+        }
     }
 
     if (a.G > 1 && a.lane_shift >= 0) {
         const int width = 1 << a.lane_shift;             // lanes of a group
-        float c1 = c[0][0], c2 = c[0][1];
+        float c1[Q], c2[Q], value[Q];
+        int rank[Q];
 #pragma unroll
-        for (int l = 1; l < kLists; ++l) merge_top2(c1, c2, c[l][0], c[l][1]);
-        for (int o = 1; o < width; o <<= 1) {
-            const float b1 = __shfl_xor_sync(kAll, c1, o), b2 = __shfl_xor_sync(kAll, c2, o);
-            merge_top2(c1, c2, b1, b2);
+        for (int q = 0; q < Q; ++q) {
+            c1[q] = c[q][0][0];
+            c2[q] = c[q][0][1];
+#pragma unroll
+            for (int l = 1; l < kLists; ++l) merge_top2(c1[q], c2[q], c[q][l][0], c[q][l][1]);
         }
-        const float value = group_value(c1, c2, a.group_top);
+        for (int o = 1; o < width; o <<= 1) {
+#pragma unroll
+            for (int q = 0; q < Q; ++q) {
+                const float b1 = __shfl_xor_sync(kAll, c1[q], o), b2 = __shfl_xor_sync(kAll, c2[q], o);
+                merge_top2(c1[q], c2[q], b1, b2);
+            }
+        }
+#pragma unroll
+        for (int q = 0; q < Q; ++q) {
+            value[q] = group_value(c1[q], c2[q], a.group_top);
+            rank[q] = 0;
+        }
         // the group's lanes share the comparisons with the other groups
-        const int mine = lane >> a.lane_shift, sub = lane & (width - 1);
-        int rank = 0;
-        const int steps = (a.G + width - 1) >> a.lane_shift;
-#pragma unroll 4
+        const int mine = lane >> a.lane_shift, sub = lane & (width - 1), steps = (a.G + width - 1) >> a.lane_shift;
+        constexpr int kSteps = Q == 1 ? 4 : 1;
+#pragma unroll kSteps
         for (int i = 0; i < steps; ++i) {
             const int g = (i << a.lane_shift) + sub;
-            const float other = __shfl_sync(kAll, value, (seg_base + (g << a.lane_shift)) & 31);
-            if (g < a.G && (other > value || (other == value && g < mine))) ++rank;
+#pragma unroll
+            for (int q = 0; q < Q; ++q) {
+                const float other = __shfl_sync(kAll, value[q], (seg_base + (g << a.lane_shift)) & 31);
+                if (g < a.G && (other > value[q] || (other == value[q] && g < mine))) ++rank[q];
+            }
         }
-        for (int o = 1; o < width; o <<= 1) rank += __shfl_xor_sync(kAll, rank, o);
-        if (rank >= a.top_groups) {
+        for (int o = 1; o < width; o <<= 1) {
+#pragma unroll
+            for (int q = 0; q < Q; ++q) rank[q] += __shfl_xor_sync(kAll, rank[q], o);
+        }
+#pragma unroll
+        for (int q = 0; q < Q; ++q) {
+            if (rank[q] < a.top_groups) continue;
 #pragma unroll
             for (int l = 0; l < kLists; ++l)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) c[l][j] = -CUDART_INF_F;
+                for (int j = 0; j < 8; ++j) c[q][l][j] = -CUDART_INF_F;
         }
     }
 
-    float best = c[0][0];
+    float best[Q];
 #pragma unroll
-    for (int l = 1; l < kLists; ++l) best = fmaxf(best, c[l][0]);
+    for (int q = 0; q < Q; ++q) {
+        best[q] = c[q][0][0];
+#pragma unroll
+        for (int l = 1; l < kLists; ++l) best[q] = fmaxf(best[q], c[q][l][0]);
+    }
     const uint32_t lower = ((1u << lane) - 1u) << seg_base;      // the token's lanes below this one
     for (int r = 0; r < a.k; ++r) {
-        const float top = seg_max<LANES>(best);
-        // the lowest lane among equals holds the lowest expert
-        const bool holds = best == top;
-        if ((__ballot_sync(kAll, holds) & lower) == 0u && holds) {
-            sel[r] = make_float2(top, __int_as_float(lane));
+        float top[Q];
+        bool gives[Q];
+#pragma unroll
+        for (int q = 0; q < Q; ++q) top[q] = seg_max<LANES>(best[q]);
+#pragma unroll
+        for (int q = 0; q < Q; ++q) {       // the lowest lane among equals holds the lowest expert
+            const bool holds = best[q] == top[q];
+            gives[q] = (__ballot_sync(kAll, holds) & lower) == 0u && holds;
+        }
+#pragma unroll
+        for (int q = 0; q < Q; ++q) {
+            if (!gives[q]) continue;
+            sel[q][r] = make_float2(top[q], __int_as_float(lane));
             bool taken = false;
-            best = -CUDART_INF_F;
+            best[q] = -CUDART_INF_F;
 #pragma unroll
             for (int l = 0; l < kLists; ++l) {
-                if (kLists == 1 || (!taken && c[l][0] == top)) {
+                if (kLists == 1 || (!taken && c[q][l][0] == top[q])) {
                     taken = true;
 #pragma unroll
-                    for (int j = 0; j < 7; ++j) c[l][j] = c[l][j + 1];
-                    c[l][7] = -CUDART_INF_F;
+                    for (int j = 0; j < 7; ++j) c[q][l][j] = c[q][l][j + 1];
+                    c[q][l][7] = -CUDART_INF_F;
                 }
-                best = fmaxf(best, c[l][0]);
+                best[q] = fmaxf(best[q], c[q][l][0]);
             }
         }
     }
     __syncwarp();
-    float D = 0.0f;
     constexpr int kMine = LANES >= 4 ? (FP8MLP_MAX_TOP_K + LANES - 1) / LANES : 8;      // k <= LANES * 8 where LANES < 4
-    float score[kMine];
-    int32_t expert[kMine];
 #pragma unroll
-    for (int i = 0; i < kMine; ++i) {
-        const int r = lane + i * LANES;
-        score[i] = 0.0f;
-        expert[i] = -1;
-        if (r < a.k && sel[r].x > -CUDART_INF_F) {
-            const float want = sel[r].x;
-            const int owner = __float_as_int(sel[r].y), from = owner * V;
-            // equal values of one lane are taken in turn, lowest expert first: the first place of the value, and for the
-            // next of its equals one place further each
-            int skip = 0;
-            while (skip < r && sel[r - 1 - skip].x == want && __float_as_int(sel[r - 1 - skip].y) == owner) ++skip;
-            int place = from;
+    for (int q = 0; q < Q; ++q) {
+        float D = 0.0f, score[kMine];
+        int32_t expert[kMine];
 #pragma unroll
-            for (int j = V - 4; j >= 0; j -= 4) {
-                const float4 q = *reinterpret_cast<const float4*>(row_c + from + j);
-                if (q.w == want) place = from + j + 3;
-                if (q.z == want) place = from + j + 2;
-                if (q.y == want) place = from + j + 1;
-                if (q.x == want) place = from + j;
+        for (int i = 0; i < kMine; ++i) {
+            const int r = lane + i * LANES;
+            score[i] = 0.0f;
+            expert[i] = -1;
+            if (r < a.k && sel[q][r].x > -CUDART_INF_F) {
+                const float want = sel[q][r].x;
+                const int owner = __float_as_int(sel[q][r].y), from = owner * V;
+                // equal values of one lane are taken in turn, lowest expert first: the first place of the value, and for
+                // the next of its equals one place further each
+                int skip = 0;
+                while (skip < r && sel[q][r - 1 - skip].x == want && __float_as_int(sel[q][r - 1 - skip].y) == owner) ++skip;
+                int place = from;
+#pragma unroll
+                for (int j = V - 4; j >= 0; j -= 4) {
+                    const float4 w = *reinterpret_cast<const float4*>(row_c[q] + from + j);
+                    if (w.w == want) place = from + j + 3;
+                    if (w.z == want) place = from + j + 2;
+                    if (w.y == want) place = from + j + 1;
+                    if (w.x == want) place = from + j;
+                }
+                for (; skip > 0; --skip)
+                    do { ++place; } while (place < from + V - 1 && row_c[q][place] != want);
+                expert[i] = place;
+                score[i] = biased ? row_s[q][place] : want;
             }
-            for (; skip > 0; --skip)
-                do { ++place; } while (place < from + V - 1 && row_c[place] != want);
-            expert[i] = place;
-            score[i] = biased ? row_s[expert[i]] : want;
+            D += score[i];
         }
-        D += score[i];
-    }
-    D = seg_sum<LANES>(D);
-    if (live) {
+        D = seg_sum<LANES>(D);
+        if (t[q] >= a.T) continue;
 #pragma unroll
         for (int i = 0; i < kMine; ++i) {
             const int r = lane + i * LANES;
             if (r < a.k) {
-                a.experts[t * a.k + r] = expert[i];
                 const float w = a.renorm ? (D == 0.0f ? 0.0f : __fdiv_rn(score[i], D)) : score[i];
-                a.weights[t * a.k + r] = w * a.scale;
+                a.experts[t[q] * a.k + r] = expert[i];
+                a.weights[t[q] * a.k + r] = w * a.scale;
             }
         }
     }
@@ -512,9 +570,9 @@ RouteArgs route_args(const fp8mlp_router* r, int64_t T, const void* logits, int6
     return a;
 }
 
-template <int LANES>
+template <int LANES, int Q = 1>
 int launch_tokens(void (*kernel)(const RouteArgs), const RouteArgs& a, size_t smem, cudaStream_t st) {
-    constexpr int kTokens = kRouteThreads / LANES;
+    constexpr int kTokens = kRouteThreads / LANES * Q;
     const int64_t blocks = (a.T + kTokens - 1) / kTokens;
     if (blocks > 0x7fffffff) return FP8MLP_ERR_SHAPE;
     if (smem > 48 * 1024) FP8MLP_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 72 * 1024));
@@ -523,20 +581,23 @@ int launch_tokens(void (*kernel)(const RouteArgs), const RouteArgs& a, size_t sm
     return FP8MLP_OK;
 }
 
-template <int LANES, int V>
+// whether a group is a power-of-two number of whole lanes
+bool groups_on_lanes(const RouteArgs& a, int V) { return a.per % V == 0 && ((a.per / V) & (a.per / V - 1)) == 0; }
+
+template <int LANES, int V, int Q = 1>
 int launch_route(RouteArgs a, int dtype, cudaStream_t st) {
-    constexpr int kTokens = kRouteThreads / LANES;
+    constexpr int kTokens = kRouteThreads / LANES * Q;
     a.lane_shift = -1;
-    if (a.per % V == 0 && ((a.per / V) & (a.per / V - 1)) == 0)
+    if (groups_on_lanes(a, V))
         for (a.lane_shift = 0; V << a.lane_shift < a.per;) ++a.lane_shift;
     a.sub_shift = 0;
     while ((a.G << (a.sub_shift + 1)) <= LANES && (2 << a.sub_shift) <= a.per) ++a.sub_shift;
     a.inv_per = ((1u << 20) + a.per - 1) / a.per;
     size_t words = static_cast<size_t>(kTokens) * (2 * a.k + 2 * (LANES * V + 4));
     if (a.G > 1 && a.lane_shift < 0) words += static_cast<size_t>(kTokens) * 2 * a.G;
-    // below 33 KiB up to 512 experts, 65 KiB for 1024 in 1024 groups
-    return launch_tokens<LANES>(dtype == FP8MLP_F32 ? route_kernel<LANES, V, float> : route_kernel<LANES, V, uint16_t>, a,
-                                words * sizeof(float), st);
+    // below 36 KiB up to 512 experts, 65 KiB for 1024 in 1024 groups
+    return launch_tokens<LANES, Q>(dtype == FP8MLP_F32 ? route_kernel<LANES, V, Q, float> : route_kernel<LANES, V, Q, uint16_t>, a,
+                                   words * sizeof(float), st);
 }
 template <int LANES, int V>
 int launch_backward_dense(const RouteArgs& a, int dtype, cudaStream_t st) {
@@ -557,7 +618,10 @@ int run_route(const RouteArgs& a, int dtype, cudaStream_t st) {
     if (a.E <= 32) return launch_route<4, 8>(a, dtype, st);
     if (a.E <= 64) return launch_route<8, 8>(a, dtype, st);
     if (a.E <= 128) return launch_route<16, 8>(a, dtype, st);
-    if (a.E <= 256) return launch_route<32, 8>(a, dtype, st);
+    // A whole warp per token: two at a time where groups of whole lanes are chosen and the tokens fill the SMs (1024 tokens
+    // 3.1 us one at a time and 3.3 in twos; groups off the lanes, 16384 x 160: 16.0 and 16.9).
+    if (a.E <= 256)
+        return a.G > 1 && a.T > 1024 && groups_on_lanes(a, 8) ? launch_route<32, 8, 2>(a, dtype, st) : launch_route<32, 8>(a, dtype, st);
     if (a.E <= 512) return launch_route<32, 16>(a, dtype, st);
     return launch_route<32, 32>(a, dtype, st);
 }

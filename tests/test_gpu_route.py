@@ -109,6 +109,30 @@ def test_route_groups(E, groups, top_groups, k, group_top):
         _check_backward(rng, router, logits, experts, kind, True, 2.5)
 
 
+@pytest.mark.parametrize("E,groups,top_groups,k,group_top", [(256, 8, 4, 8, 2), (192, 6, 2, 5, 1), (144, 9, 4, 8, 2), (136, 17, 3, 20, 2),
+                                                             (256, 2, 1, 32, 2)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
+def test_many_tokens_as_few(E, groups, top_groups, k, group_top, dtype):
+    """Large calls take two tokens per warp at a time: the same bits as small calls on parts of the rows, masks among them,
+    and the plain form on the last rows (an odd number of them)."""
+    rng = np.random.default_rng(E + k)
+    T = 1501
+    logits = _logits(rng, T, E, dtype)
+    logits[5] = -float("inf")
+    logits[6, ::3] = -float("inf")
+    logits[1499, 4:] = -float("inf")
+    logits[1500, 7] = float("nan")
+    bias = torch.from_numpy(rng.normal(0, 0.1, E).astype(np.float32)).cuda()
+    for kind, b in (("sigmoid", bias), ("softmax", None)):
+        kw = dict(groups=groups, top_groups=top_groups, group_top=group_top, renorm=True, scale=2.5)
+        _, experts, weights = _route(logits, b, k, kind, **kw)
+        for begin, end in ((0, 700), (700, 1500), (1500, 1501)):
+            _, e, w = _route(logits[begin:end], b, k, kind, **kw)
+            assert torch.equal(e, experts[begin:end]) and torch.equal(w, weights[begin:end])
+        tail = slice(1470, 1501)
+        _compare(logits[tail], b, experts[tail], weights[tail], k, kind, **kw)
+
+
 @pytest.mark.parametrize("E", [7, 64, 256, 600])
 @pytest.mark.parametrize("kind", ["softmax", "sigmoid"])
 def test_equal_values_go_to_the_lowest_index(kind, E):
