@@ -151,6 +151,54 @@ def test_combine_backward(T, k, E, d, pad, dtype):
     assert (np.abs(d_weights.cpu().numpy() - dw) <= (d / 32 + 32) * 2.0 ** -24 * size).all()
 
 
+@DTYPES
+@pytest.mark.parametrize("T,k,d", [(37, 1, 4112), (50, 1, 80), (21, 2, 2064), (9, 3, 528), (11, 4, 272), (5, 8, 1040), (3, 11, 48)])
+def test_rows_on_16_byte_boundaries(T, k, d, dtype):
+    """Buffers that start 16 bytes past a 32-byte boundary, between guard zones: the same bits as on aligned buffers (sums run
+    over the slots in order either way; dot products are held to their bar), guards intact."""
+    rng = np.random.default_rng(T + d)
+    E, n = 16, T * k
+    experts = _experts(rng, T, k, E, 0.2)
+    _, _, rows = _plan(experts, E)
+    weights = torch.from_numpy(rng.random((T, k)).astype(np.float32)).cuda()
+    shift = 16 // torch.empty(0, dtype=dtype).element_size()
+    guards = []
+
+    def place(r, content=None):
+        flat = torch.full((2 * shift + r * d + 64,), 7.0, dtype=dtype, device="cuda")
+        view = flat[shift:shift + r * d].view(r, d)
+        assert view.data_ptr() % 32 == 16
+        if content is not None:
+            view.copy_(content)
+        guards.append((flat, shift, r * d))
+        return view
+
+    draw = lambda r: torch.from_numpy(rng.normal(0, 1, (r, d)).astype(np.float32)).cuda().to(dtype)
+    x, ye, dy = draw(T), draw(n), draw(T)
+    xe, y, y1, dye, dw = torch.zeros_like(ye), torch.empty_like(x), torch.empty_like(x), torch.zeros_like(ye), torch.empty((T, k), device="cuda")
+    B.fp8mlp_dispatch(x, rows, xe)
+    B.fp8mlp_combine(ye, rows, weights, y)
+    B.fp8mlp_combine(ye, rows, None, y1)
+    B.fp8mlp_combine_backward(dy, ye, rows, weights, dye, dw)
+    x_, ye_, dy_, xe_, dye_ = place(T, x), place(n, ye), place(T, dy), place(n, torch.zeros_like(ye)), place(n, torch.zeros_like(ye))
+    yw_, y1_, dw_ = place(T), place(T), torch.empty_like(dw)
+    B.fp8mlp_dispatch(x_, rows, xe_)
+    B.fp8mlp_combine(ye_, rows, weights, yw_)
+    B.fp8mlp_combine(ye_, rows, None, y1_)
+    B.fp8mlp_combine_backward(dy_, ye_, rows, weights, dye_, dw_)
+    for a, b in ((xe, xe_), (y, yw_), (y1, y1_), (dye, dye_)):
+        assert torch.equal(a, b)
+    r = rows.cpu().numpy()
+    size = np.array([[np.abs(dy[t].double().cpu().numpy() * ye[r[t, j]].double().cpu().numpy()).sum() if r[t, j] >= 0 else 0.0
+                      for j in range(k)] for t in range(T)])
+    assert (np.abs((dw - dw_).cpu().numpy()) <= 2 * (d / 32 + 32) * 2.0 ** -24 * size).all()
+    want, _ = R.combine(ye.float().cpu().numpy(), r, weights.cpu().numpy())
+    step = 2.0 ** -7 if dtype == torch.bfloat16 else 2.0 ** -23
+    assert (np.abs(y.float().cpu().numpy() - want) <= (k * 2.0 ** -24 * 8 + 0.51 * step * np.abs(want))).all()
+    for flat, s, count in guards:
+        assert bool((flat[:s] == 7.0).all()) and bool((flat[s + count:] == 7.0).all())
+
+
 def test_combine_gradient_against_differences():
     """<dy, combine(...)> is linear in each argument: differences of the 64-bit form are exact up to its rounding, so the
     kernel's gradients are held to their own fp32 bar."""

@@ -265,6 +265,31 @@ def test_route_repeats_bit_for_bit():
         assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
 
 
+@pytest.mark.parametrize("E,T", [(6, 40), (64, 33), (100, 9), (256, 1300), (512, 7)])
+def test_arrays_on_4_byte_boundaries(E, T):
+    """Bias, experts, weights and their gradients 4 bytes past a 32-byte boundary: the same bits as aligned ones."""
+    rng = np.random.default_rng(E)
+    k = min(E, 5)
+    logits = _logits(rng, T, E, torch.float32)
+    bias = torch.from_numpy(rng.normal(0, 0.1, E).astype(np.float32)).cuda()
+    off = lambda n, dtype: torch.full((n + 9,), 7, dtype=dtype, device="cuda")
+    bias_, experts_, weights_, dw_ = off(E, torch.float32), off(T * k, torch.int32), off(T * k, torch.float32), off(T * k, torch.float32)
+    bias_[1:E + 1] = bias
+    router, experts, weights = _route(logits, bias, k, "sigmoid")
+    B.fp8mlp_route(router, logits, bias_[1:E + 1], experts_[1:T * k + 1].view(T, k), weights_[1:T * k + 1].view(T, k))
+    assert torch.equal(experts_[1:T * k + 1].view(T, k), experts) and torch.equal(weights_[1:T * k + 1].view(T, k), weights)
+    for a in (experts_, weights_):
+        assert bool((a[0] == 7) & (a[T * k + 1:] == 7).all())
+    dw = torch.from_numpy(rng.normal(0, 1, (T, k)).astype(np.float32)).cuda()
+    dw_[1:T * k + 1] = dw.flatten()
+    for kind in ("sigmoid", "softmax"):
+        router = B.new_router(E, k, KIND[kind], renormalise=False)
+        a, b = torch.empty_like(logits), torch.empty_like(logits)
+        B.fp8mlp_route_backward(router, logits, experts, dw, a)
+        B.fp8mlp_route_backward(router, logits, experts_[1:T * k + 1].view(T, k), dw_[1:T * k + 1].view(T, k), b)
+        assert torch.equal(a, b)
+
+
 @pytest.mark.parametrize("E", [1, 8, 60, 1024])
 def test_update_bias(E):
     rng = np.random.default_rng(E)
