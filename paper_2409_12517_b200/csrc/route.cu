@@ -21,8 +21,9 @@ struct RouteArgs {
     int E, k, score, G, per, top_groups, group_top, renorm;
     float scale;
     int wide, wide_b, wide_d;      // rows of logits, the bias, rows of d_logits start on a vector boundary
-    int lane_shift;        // a group is 2^lane_shift whole lanes; -1: groups do not fall on lanes, and then
-    int sub_shift;         // 2^sub_shift lanes work on a group
+    // How a row lies on its lanes: blocks of lay_per experts on 2^lane_shift lanes each, per_lane to a lane.  A block is a group
+    // where the groups fall on lanes (on_lanes), else the row; then 2^sub_shift lanes work on a group in shared memory.
+    int lay_per, lane_shift, per_lane, on_lanes, sub_shift;
     uint32_t inv_per;      // ceil(2^20 / per)
 };
 
@@ -55,7 +56,7 @@ __device__ __forceinline__ void store8(uint16_t* p, const float* v) {
     st_global_v4(p, cvt_bf16x2(v[0], v[1]), cvt_bf16x2(v[2], v[3]), cvt_bf16x2(v[4], v[5]), cvt_bf16x2(v[6], v[7]));
 }
 
-// this lane's V logits of one row; experts beyond E read as -inf
+// a lane's logits of one row, experts e0 .. E - 1 (at most V); the places beyond them read as -inf
 template <int V, typename SRC>
 __device__ __forceinline__ void load_row(const SRC* row, int e0, int E, bool wide, float (&x)[V]) {
 #pragma unroll
@@ -233,7 +234,9 @@ __global__ void __launch_bounds__(kRouteThreads, Q > 1 ? 8 : V > 8 ? 4 : LANES =
     constexpr int kRow = LANES * V + 4;                   // + 4: rows of neighbouring tokens start in other banks
     constexpr int kLists = V / 8;
     const int lane = threadIdx.x % LANES, seg_base = (threadIdx.x & 31) - lane;
-    const int e0 = lane * V;
+    const int e0 = lane * V;                              // this lane's places in the rows in shared memory, and its experts
+    const int first = (lane >> a.lane_shift) * a.lay_per + (lane & ((1 << a.lane_shift) - 1)) * a.per_lane;
+    const int end = min(min(first + a.per_lane, ((lane >> a.lane_shift) + 1) * a.lay_per), a.E);
     const bool biased = a.bias != nullptr;
     float *row_c[Q], *row_s[Q], *group_c[Q];              // a token's values and scores; its groups, where they are off the lanes
     float2* sel[Q];                                       // a round's value and its lane
@@ -254,18 +257,18 @@ __global__ void __launch_bounds__(kRouteThreads, Q > 1 ? 8 : V > 8 ? 4 : LANES =
 #pragma unroll
     for (int q = 0; q < Q; ++q) {
         if (t[q] < a.T) {
-            load_row<V, SRC>(static_cast<const SRC*>(a.logits) + t[q] * a.ld, e0, a.E, a.wide != 0, s[q]);
+            load_row<V, SRC>(static_cast<const SRC*>(a.logits) + t[q] * a.ld, first, end, a.wide != 0, s[q]);
         } else {
 #pragma unroll
             for (int j = 0; j < V; ++j) s[q][j] = -CUDART_INF_F;
         }
     }
-    if (biased) load_row<V, float>(a.bias, e0, a.E, a.wide_b != 0, bias);
+    if (biased) load_row<V, float>(a.bias, first, end, a.wide_b != 0, bias);
 #pragma unroll
     for (int q = 0; q < Q; ++q) {
         score_row<LANES, V>(a, e0, biased, bias, row_s[q], s[q]);
         if constexpr (Q == 1) {
-            if (a.G > 1 && a.lane_shift < 0) drop_groups_in_shared<LANES, V>(a, lane, e0, row_c[q], group_c[q], s[q]);
+            if (a.G > 1 && !a.on_lanes) drop_groups_in_shared<LANES, V>(a, lane, e0, row_c[q], group_c[q], s[q]);
         }
         put_row<V>(row_c[q] + e0, s[q]);
 #pragma unroll
@@ -276,7 +279,7 @@ __global__ void __launch_bounds__(kRouteThreads, Q > 1 ? 8 : V > 8 ? 4 : LANES =
         }
     }
 
-    if (a.G > 1 && a.lane_shift >= 0) {
+    if (a.on_lanes) {
         const int width = 1 << a.lane_shift;             // lanes of a group
         float c1[Q], c2[Q], value[Q];
         int rank[Q];
@@ -390,7 +393,7 @@ __global__ void __launch_bounds__(kRouteThreads, Q > 1 ? 8 : V > 8 ? 4 : LANES =
                 }
                 for (; skip > 0; --skip)
                     do { ++place; } while (place < from + V - 1 && row_c[q][place] != want);
-                expert[i] = place;
+                expert[i] = (owner >> a.lane_shift) * a.lay_per + (owner & ((1 << a.lane_shift) - 1)) * a.per_lane + place - from;
                 score[i] = biased ? row_s[q][place] : want;
             }
             D += score[i];
@@ -581,20 +584,40 @@ int launch_tokens(void (*kernel)(const RouteArgs), const RouteArgs& a, size_t sm
     return FP8MLP_OK;
 }
 
-// whether a group is a power-of-two number of whole lanes
-bool groups_on_lanes(const RouteArgs& a, int V) { return a.per % V == 0 && ((a.per / V) & (a.per / V - 1)) == 0; }
+// Lanes of a token whose groups lie on lanes of their own, V experts to a lane: a power of two for each group, and one of
+// such groups.  More than 32: they do not fit.
+int group_lanes(int G, int per, int V) {
+    int groups = 1, width = 1;
+    while (groups < G) groups *= 2;
+    while (width * V < per) width *= 2;
+    return groups * width;
+}
 
 template <int LANES, int V, int Q = 1>
 int launch_route(RouteArgs a, int dtype, cudaStream_t st) {
     constexpr int kTokens = kRouteThreads / LANES * Q;
-    a.lane_shift = -1;
-    if (groups_on_lanes(a, V))
-        for (a.lane_shift = 0; V << a.lane_shift < a.per;) ++a.lane_shift;
+    a.on_lanes = a.G > 1 && group_lanes(a.G, a.per, V) <= LANES;
+    a.lay_per = a.on_lanes ? a.per : a.E;
+    a.lane_shift = 0;
+    if (a.on_lanes) {
+        int groups = 1;
+        while (groups < a.G) groups *= 2;
+        while ((groups << (a.lane_shift + 1)) <= LANES) ++a.lane_shift;
+    } else {
+        while ((1 << (a.lane_shift + 1)) <= LANES) ++a.lane_shift;
+    }
+    // Whole vectors where the groups divide into them; else the same share for every lane, and single loads (a group's first
+    // expert is then off the vector boundaries).
+    a.per_lane = V;
+    if (a.on_lanes && a.per % 8 != 0) {
+        a.per_lane = (a.per + (1 << a.lane_shift) - 1) >> a.lane_shift;
+        a.wide = a.wide_b = 0;
+    }
     a.sub_shift = 0;
     while ((a.G << (a.sub_shift + 1)) <= LANES && (2 << a.sub_shift) <= a.per) ++a.sub_shift;
     a.inv_per = ((1u << 20) + a.per - 1) / a.per;
     size_t words = static_cast<size_t>(kTokens) * (2 * a.k + 2 * (LANES * V + 4));
-    if (a.G > 1 && a.lane_shift < 0) words += static_cast<size_t>(kTokens) * 2 * a.G;
+    if (a.G > 1 && !a.on_lanes) words += static_cast<size_t>(kTokens) * 2 * a.G;
     // below 36 KiB up to 512 experts, 65 KiB for 1024 in 1024 groups
     return launch_tokens<LANES, Q>(dtype == FP8MLP_F32 ? route_kernel<LANES, V, Q, float> : route_kernel<LANES, V, Q, uint16_t>, a,
                                    words * sizeof(float), st);
@@ -611,17 +634,25 @@ int launch_backward_sparse(const RouteArgs& a, int dtype, cudaStream_t st) {
                                                     : route_backward_sparse_kernel<LANES, uint16_t>, a, 0, st);
 }
 
-// LANES x V covers the row with the fewest lanes that keep V at 8; beyond 256 experts V grows.
+// LANES x V covers the row with the fewest lanes that keep V at 8; beyond 256 experts V grows.  Groups get lanes of their own
+// where 32 are enough for that.
 int run_route(const RouteArgs& a, int dtype, cudaStream_t st) {
-    if (a.E <= 8) return launch_route<1, 8>(a, dtype, st);
-    if (a.E <= 16) return launch_route<2, 8>(a, dtype, st);
-    if (a.E <= 32) return launch_route<4, 8>(a, dtype, st);
-    if (a.E <= 64) return launch_route<8, 8>(a, dtype, st);
-    if (a.E <= 128) return launch_route<16, 8>(a, dtype, st);
-    // A whole warp per token: two at a time where groups of whole lanes are chosen and the tokens fill the SMs (1024 tokens
-    // 3.1 us one at a time and 3.3 in twos; groups off the lanes, 16384 x 160: 16.0 and 16.9).
-    if (a.E <= 256)
-        return a.G > 1 && a.T > 1024 && groups_on_lanes(a, 8) ? launch_route<32, 8, 2>(a, dtype, st) : launch_route<32, 8>(a, dtype, st);
+    int lanes = 1;
+    while (lanes * 8 < a.E) lanes *= 2;
+    if (a.G > 1 && a.E <= 256) {
+        const int grouped = group_lanes(a.G, a.per, 8);
+        if (grouped <= 32) lanes = grouped;
+    }
+    if (lanes == 1) return launch_route<1, 8>(a, dtype, st);
+    if (lanes == 2) return launch_route<2, 8>(a, dtype, st);
+    if (lanes == 4) return launch_route<4, 8>(a, dtype, st);
+    if (lanes == 8) return launch_route<8, 8>(a, dtype, st);
+    if (lanes == 16) return launch_route<16, 8>(a, dtype, st);
+    // A whole warp per token: two at a time where groups on lanes are chosen and the tokens fill the SMs (1024 tokens 3.1 us
+    // one at a time and 3.3 in twos).
+    if (lanes == 32)
+        return a.G > 1 && a.T > 1024 && group_lanes(a.G, a.per, 8) <= 32 ? launch_route<32, 8, 2>(a, dtype, st)
+                                                                          : launch_route<32, 8>(a, dtype, st);
     if (a.E <= 512) return launch_route<32, 16>(a, dtype, st);
     return launch_route<32, 32>(a, dtype, st);
 }

@@ -96,7 +96,9 @@ def _check_backward(rng, router, logits, experts, kind, renorm, scale, pad=0, sh
 
 @pytest.mark.parametrize("E,groups,top_groups,k", [(64, 8, 3, 6), (256, 8, 4, 8), (32, 4, 1, 8), (128, 2, 1, 8), (512, 8, 4, 8),
                                                    (60, 4, 2, 6), (96, 4, 3, 8), (12, 6, 2, 3), (21, 7, 7, 5), (8, 8, 3, 3),
-                                                   (1024, 32, 5, 16), (1000, 8, 4, 8), (24, 3, 1, 8)])
+                                                   (1024, 32, 5, 16), (1000, 8, 4, 8), (24, 3, 1, 8), (160, 8, 3, 6), (128, 64, 10, 8),
+                                                   (255, 3, 2, 8), (300, 5, 2, 8), (16, 8, 4, 4), (1024, 512, 40, 32), (204, 17, 4, 9),
+                                                   (800, 100, 7, 12)])
 @pytest.mark.parametrize("group_top", [1, 2])
 def test_route_groups(E, groups, top_groups, k, group_top):
     rng = np.random.default_rng(E + groups)
@@ -110,7 +112,7 @@ def test_route_groups(E, groups, top_groups, k, group_top):
 
 
 @pytest.mark.parametrize("E,groups,top_groups,k,group_top", [(256, 8, 4, 8, 2), (192, 6, 2, 5, 1), (144, 9, 4, 8, 2), (136, 17, 3, 20, 2),
-                                                             (256, 2, 1, 32, 2)])
+                                                             (256, 2, 1, 32, 2), (160, 8, 3, 6, 1), (216, 8, 4, 8, 2)])
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=["f32", "bf16"])
 def test_many_tokens_as_few(E, groups, top_groups, k, group_top, dtype):
     """Large calls take two tokens per warp at a time: the same bits as small calls on parts of the rows, masks among them,
