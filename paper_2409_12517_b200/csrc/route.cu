@@ -20,6 +20,7 @@ struct RouteArgs {
     int64_t T, ld, ld_d;
     int E, k, score, G, per, top_groups, group_top, renorm;
     float scale;
+    int can_lose;                  // renormalised softmax whose choice may pass over the row's largest logits
     int wide, wide_b, wide_d;      // rows of logits, the bias, rows of d_logits start on a vector boundary
     // How a row lies on its lanes: blocks of lay_per experts on 2^lane_shift lanes each, per_lane to a lane.  A block is a group
     // where the groups fall on lanes (on_lanes), else the row; then 2^sub_shift lanes work on a group in shared memory.
@@ -399,6 +400,27 @@ __global__ void __launch_bounds__(kRouteThreads, Q > 1 ? 8 : V > 8 ? 4 : LANES =
             D += score[i];
         }
         D = seg_sum<LANES>(D);
+        if (a.can_lose) {
+            // Where a bias or the groups hold back the experts of the large logits, the chosen scores can be so small that fp32
+            // keeps few of their digits or none (D = 0).  Their ratios are the softmax over the chosen logits all the same, which
+            // are read again for such tokens (D >= 2^-64 leaves every weight above 2^-62 all its digits).
+            const bool lost = t[q] < a.T && D < 0x1p-64f;
+            if (__any_sync(kAll, lost)) {
+                const SRC* row = static_cast<const SRC*>(a.logits) + t[q] * a.ld;
+                float top = -CUDART_INF_F, sum = 0.0f;
+#pragma unroll
+                for (int i = 0; i < kMine; ++i)
+                    if (lost && expert[i] >= 0) top = fmaxf(top, load1<SRC>(row + expert[i]));
+                top = seg_max<LANES>(top);
+#pragma unroll
+                for (int i = 0; i < kMine; ++i) {
+                    if (lost && expert[i] >= 0) score[i] = ex2_subnormal(__fmul_rn(load1<SRC>(row + expert[i]) - top, kLog2e));
+                    sum += score[i];
+                }
+                sum = seg_sum<LANES>(sum);
+                if (lost) D = sum;
+            }
+        }
         if (t[q] >= a.T) continue;
 #pragma unroll
         for (int i = 0; i < kMine; ++i) {
@@ -693,6 +715,7 @@ extern "C" int fp8mlp_route(const fp8mlp_router* r, int64_t T, const void* logit
     RouteArgs a = route_args(r, T, logits, ld, esize);
     a.bias = bias; a.experts = experts; a.weights = weights;
     a.wide_b = multiple_of(bias, 32);
+    a.can_lose = a.renorm && a.score == FP8MLP_SCORE_SOFTMAX && (bias != nullptr || a.G > 1);
     return run_route(a, dtype, static_cast<cudaStream_t>(stream));
 }
 

@@ -303,3 +303,77 @@ def test_update_bias(E):
     B.fp8mlp_route_update_bias(torch.from_numpy(counts).cuda(), 1e-3, dev)
     sign = np.sign(int(counts.sum()) - counts.astype(np.int64) * E).astype(np.float32)
     assert np.array_equal(dev.cpu().numpy(), bias + np.float32(1e-3) * sign)
+
+
+def _softmax_of_chosen(x, experts):
+    """e^x_j / sum_i e^x_i over the chosen experts, in 64 bits: what renormalised softmax weights are, whatever the rest of the row."""
+    v = np.exp(x[experts].astype(np.float64) - x[experts].max())
+    return v / v.sum()
+
+
+@pytest.mark.parametrize("E,groups,top_groups", [(3, 1, 1), (12, 1, 1), (16, 4, 2), (40, 1, 1), (256, 1, 1), (256, 8, 4), (66, 33, 20),
+                                                 (600, 1, 1)])
+def test_renormalised_softmax_far_below_the_rows_maximum(E, groups, top_groups):
+    """An expert out of service (bias -inf), or held back by a finite bias, may stand so far above the others that their scores
+    leave fp32.  Their renormalised weights are still the softmax over the chosen logits, and the gradient is that formula's.
+    Rows of every distance share warps; rows that lose nothing keep the bits that they have alone.  A weight has in addition the
+    subnormal spacing 2^-149 of its score over D >= 2^-64."""
+    rng = np.random.default_rng(E + groups)
+    k, per = min(2 if E < 12 else 5, E - 1), E // groups
+    gaps = np.array([0.0, 120.0, 3.0, 40.0, 45.0, 60.0, 80.0, 86.0, 88.0, 95.0, 100.0, 103.0, 104.0, 106.0, 110.0, 150.0, 1e4, 3e38, 0.5],
+                    np.float32)
+    x = rng.normal(0, 1, (gaps.size, E)).astype(np.float32)
+    x[:, 0] = gaps
+    if E == 3:
+        x[1] = [0.0, -120.0, -121.0]
+    for out_of_service in (-np.inf, -4.0):
+        bias = rng.normal(0, 1e-3, E).astype(np.float32)
+        bias[0] = out_of_service
+        if groups > 1:
+            bias[:per] = out_of_service
+        logits, dev_bias = torch.from_numpy(x).cuda(), torch.from_numpy(bias).cuda()
+        kw = dict(groups=groups, top_groups=top_groups, group_top=min(2, per), renorm=True, scale=2.5)
+        router, experts, weights = _route(logits, dev_bias, k, "softmax", **kw)
+        dw = rng.normal(0, 1, (gaps.size, k)).astype(np.float32)
+        if E == 3:
+            dw[1] = [1.0, -1.0]
+        d_logits = torch.full_like(logits, 7.0)
+        B.fp8mlp_route_backward(router, logits, experts, torch.from_numpy(dw).cuda(), d_logits)
+        got_e, got_w, got_dx = experts.cpu().numpy(), weights.cpu().numpy(), d_logits.cpu().numpy().astype(np.float64)
+        for t in range(gaps.size):
+            assert (got_e[t] > 0).all() and len(set(got_e[t])) == k
+            r = _softmax_of_chosen(x[t], got_e[t])
+            np.testing.assert_allclose(got_w[t], 2.5 * r, rtol=_tol(x[t], E), atol=2.5 * 2.0 ** -85, err_msg=f"gap {gaps[t]}")
+            want = np.zeros(E)
+            want[got_e[t]] = 2.5 * r * (dw[t] - (dw[t] * r).sum())
+            allowed = 4 * _tol(x[t], E) * 2.5 * np.abs(dw[t]).max() + 2.0 ** -24 * np.abs(want)
+            assert (np.abs(got_dx[t] - want) <= allowed).all(), f"gap {gaps[t]}"
+        for t in (0, 2, 18):
+            _, e, w = _route(logits[t:t + 1], dev_bias, k, "softmax", **kw)
+            assert torch.equal(e[0], experts[t]) and torch.equal(w[0], weights[t])
+
+
+@pytest.mark.parametrize("kind", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("renorm", [True, False])
+def test_backward_of_finite_masks_and_lost_scores(kind, renorm):
+    """Rows under a finite mask (all but one expert, and all of them), rows of equal logits whose sigmoid is 0 in fp32, and a row
+    that spreads over hundreds: the gradient follows from the forward's weights."""
+    rng = np.random.default_rng(17)
+    E, k = 24, 4
+    x = rng.normal(0, 1, (4, E)).astype(np.float32)
+    lowest = np.finfo(np.float32).min
+    x[0, 1:] = lowest
+    x[1] = lowest
+    x[2] = -200.0
+    x[3] *= 100.0
+    logits = torch.from_numpy(x).cuda()
+    router, experts, weights = _route(logits, None, k, kind, renorm=renorm, scale=1.5)
+    dw = rng.normal(0, 1, (4, k)).astype(np.float32)
+    d_logits = torch.full_like(logits, 7.0)
+    B.fp8mlp_route_backward(router, logits, experts, torch.from_numpy(dw).cuda(), d_logits)
+    got_e, got = experts.cpu().numpy(), d_logits.cpu().numpy()
+    if kind == "sigmoid":
+        assert not got[1:3].any() and not weights[1:3].any()         # weights that are 0 whatever the logits do
+    for t in range(4):
+        ref = R.route_backward_row(x[t], got_e[t], dw[t], kind, renorm, 1.5)
+        assert (np.abs(got[t] - ref) <= 4 * _tol(x[t], E) * 1.5 * np.abs(dw[t]).max() + 2.0 ** -24 * np.abs(ref)).all(), f"row {t}"
