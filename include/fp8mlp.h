@@ -357,7 +357,8 @@ FP8MLP_API int fp8mlp_gemm_plan(int kind, int64_t M, int64_t N, int64_t K, int s
  *   s   = softmax(x)  or  sigma(x)                       (fp32; a sigma below 2^-126 counts as 0)
  *   c_e = s_e + bias_e                      bias[n_experts] nullable; it takes part in the choice alone
  *   n_groups > 1: the experts form n_groups groups of neighbours; a group's value is the sum of its group_top (1 or 2)
- *       largest c; only the top_groups groups of the largest values stay in the choice
+ *       largest c (fp32; a sum below the type's lowest value counts as that value); only the top_groups groups of the
+ *       largest values stay in the choice
  *   experts[t, :] = the top_k experts of the largest c, largest first      (equal values: the lower index first)
  *   w_j = scale * s_j / D, D = the sum of the chosen s   (renormalise != 0).  Softmax: that is e^x_j over the sum of the
  *       chosen e^x_i, also where the chosen s are too small for fp32; sigmoid: w_j = 0 where D is 0

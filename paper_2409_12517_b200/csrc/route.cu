@@ -121,9 +121,10 @@ __device__ __forceinline__ void merge_top2(float& a1, float& a2, float b1, float
     a2 = fmaxf(fminf(a1, b1), fmaxf(a2, b2));
     a1 = fmaxf(a1, b1);
 }
-// a group's value; -inf: nothing to choose in it, and a missing second expert adds nothing
+// a group's value; -inf: nothing to choose in it, and a missing second expert adds nothing.  Two finite values whose sum
+// falls below fp32 (a bias of the lowest value) are held at its lowest: their group has something to choose.
 __device__ __forceinline__ float group_value(float c1, float c2, int group_top) {
-    return group_top == 2 && c2 > -CUDART_INF_F ? c1 + c2 : c1;
+    return group_top == 2 && c2 > -CUDART_INF_F ? fmaxf(c1 + c2, -CUDART_MAX_NORMAL_F) : c1;
 }
 
 // 8 values into falling order (19 exchanges)

@@ -377,3 +377,27 @@ def test_backward_of_finite_masks_and_lost_scores(kind, renorm):
     for t in range(4):
         ref = R.route_backward_row(x[t], got_e[t], dw[t], kind, renorm, 1.5)
         assert (np.abs(got[t] - ref) <= 4 * _tol(x[t], E) * 1.5 * np.abs(dw[t]).max() + 2.0 ** -24 * np.abs(ref)).all(), f"row {t}"
+
+
+@pytest.mark.parametrize("E,groups", [(16, 4), (24, 6), (66, 33), (256, 16), (300, 20), (700, 50), (960, 32)])
+@pytest.mark.parametrize("kind", ["softmax", "sigmoid"])
+def test_groups_under_the_lowest_bias(kind, E, groups):
+    """A bias of the type's lowest value puts experts last, not out of service: two of them add up beyond fp32, and their group
+    still stands before one that has nothing to choose."""
+    rng = np.random.default_rng(E)
+    per = E // groups
+    k = per + 1                                        # the last group's experts and one more
+    x = rng.normal(0, 1, (9, E)).astype(np.float32)
+    x[:, :per] = -np.inf                               # the first group is masked
+    bias = np.full(E, np.finfo(np.float32).min, np.float32)
+    bias[-per:] = rng.normal(0, 0.1, per)              # and only the last one is in use without a bias of that size
+    kw = dict(groups=groups, top_groups=2, group_top=2, renorm=False, scale=1.0)
+    _, experts, weights = _route(torch.from_numpy(x).cuda(), torch.from_numpy(bias).cuda(), k, kind, **kw)
+    got = experts.cpu().numpy()
+    for t in range(9):
+        ref_e, ref_w, _ = R.route_row(x[t], bias, k, kind, **kw)
+        assert ref_e[-1] == per                        # the first of the second group
+        # near scores of the last group may be ordered either way
+        assert set(got[t]) == set(ref_e) and got[t][-1] == per
+        order = np.argsort(got[t])
+        np.testing.assert_allclose(weights[t].cpu().numpy()[order], ref_w[np.argsort(ref_e)], rtol=_tol(x[t], E), atol=1e-38)
