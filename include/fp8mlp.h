@@ -414,7 +414,7 @@ FP8MLP_API int fp8mlp_dispatch(int64_t T, int top_k, int64_t d, int dtype, const
 FP8MLP_API int fp8mlp_combine(int64_t T, int top_k, int64_t d, int dtype, const void* ye, int64_t n_rows, const int32_t* rows,
                               const float* weights, void* y, int64_t ld_y, void* stream);
 /* dye[rows[t, j], :] = weights[t, j] dy[t, :];  d_weights[t, j] = <dy[t, :], ye[rows[t, j], :]>  (fp32).  Slots whose
- * row is outside 0 .. n_rows - 1: nothing is written to dye, d_weights = 0.  dye contiguous, not ye itself. */
+ * row is outside 0 .. n_rows - 1: nothing is written to dye, d_weights = 0.  dye contiguous, neither ye nor dy itself. */
 FP8MLP_API int fp8mlp_combine_backward(int64_t T, int top_k, int64_t d, int dtype, const void* dy, int64_t ld_dy,
                                        const void* ye, int64_t n_rows, const int32_t* rows, const float* weights, void* dye,
                                        float* d_weights, void* stream);

@@ -541,7 +541,7 @@ extern "C" int fp8mlp_combine_backward(int64_t T, int top_k, int64_t d, int dtyp
     const int rc = check_rows(T, top_k, d, dtype, dy, ld_dy, ye, n_rows, rows);
     if (rc != FP8MLP_OK) return rc;
     if (T == 0) return FP8MLP_OK;
-    if (weights == nullptr || d_weights == nullptr || (dye == nullptr && n_rows > 0) || (dye == ye && n_rows > 0))
+    if (weights == nullptr || d_weights == nullptr || (n_rows > 0 && (dye == nullptr || dye == ye || dye == dy)))
         return FP8MLP_ERR_ARG;
     if (!aligned(dye, 16) || !aligned(weights, 4) || !aligned(d_weights, 4)) return FP8MLP_ERR_ALIGN;
     RowArgs a = row_args(T, top_k, d, dtype, ld_dy, n_rows, rows);

@@ -173,3 +173,10 @@ def test_reference_plan_by_hand():
     counts, offsets, rows = R.plan(np.array([[2, 0], [-1, 2], [0, 1]]), 3)
     assert list(counts) == [2, 1, 2] and list(offsets) == [0, 2, 3, 5]
     assert rows.tolist() == [[3, 0], [-1, 4], [1, 2]]
+
+
+def test_combine_gradient_is_not_written_over_its_input(lib):
+    """With one expert per token dye and dy have the same shape; a block would overwrite rows of dy that others still read."""
+    back = lambda dy, dye, n=4: lib.fp8mlp_combine_backward(4, 1, 32, B.BF16, dy, 32, 2 * P, n, P, P, dye, P, None)
+    assert back(P, P) == B.ERR_ARG
+    assert back(3 * P, 3 * P) == B.ERR_ARG
