@@ -83,7 +83,8 @@ class _GradTensor(C.Structure):
     _fields_ = [("g", C.c_void_p), ("out", C.c_void_p), ("n", C.c_int64), ("dtype", C.c_int32)]
 
 
-_raw_stream, _device = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 _lib = None
 
 
@@ -157,10 +158,21 @@ def _ptr(t):
     return C.c_void_p(t.data_ptr())
 
 
-def _stream():
-    """The current stream's handle.  torch.cuda.current_stream() builds a stream object around it, which takes longer
-    (3.4 us) than a launch; the accessor that torch's own generated code uses takes 0.1 us."""
-    return _raw_stream(_device()) if _raw_stream is not None else torch.cuda.current_stream().cuda_stream
+def _stream(here=None):
+    """The current stream's handle (here: the current GPU, if the caller has asked for it).  torch.cuda.current_stream()
+    builds a stream object around it, which takes longer (3.4 us) than a launch; the accessor that torch's own generated
+    code uses takes 0.1 us."""
+    if _raw_stream is None:
+        return torch.cuda.current_stream().cuda_stream
+    return _raw_stream(_device() if here is None else here)
+
+
+def _here():
+    """The current GPU, to whose stream a call goes; None where there is none, which no tensor lies on."""
+    try:
+        return _device()
+    except (RuntimeError, AssertionError):
+        return None
 
 
 def _check(code: int, where: str):
@@ -357,20 +369,21 @@ _DTYPES = {torch.bfloat16: BF16, torch.float32: F32}
 _F32, _I32, _U8 = torch.float32, torch.int32, torch.uint8
 
 
-def _as(t, dtype, numel, what):
-    """Device pointer of a contiguous CUDA tensor of the given type and size."""
-    if t.dtype is not dtype or t.numel() != numel or not (t.is_cuda and t.is_contiguous()):
-        raise ValueError(f"{what}: a contiguous CUDA tensor of {numel} {dtype} elements is needed, "
+def _as(t, dtype, numel, what, here):
+    """Device pointer of a contiguous tensor of the given type and size on the current GPU."""
+    if t.dtype is not dtype or t.numel() != numel or t.get_device() != here or not t.is_contiguous():
+        raise ValueError(f"{what}: a contiguous CUDA tensor of {numel} {dtype} elements on the current GPU is needed, "
                          f"got {tuple(t.shape)} {t.dtype} on {t.device}")
     return t.data_ptr()
 
 
-def _matrix(t, cols, what, dtype=None):
-    """(rows, pointer, type, row stride) of a 2-D CUDA tensor whose rows are contiguous; any row stride >= its columns."""
+def _matrix(t, cols, what, here, dtype=None):
+    """(rows, pointer, type, row stride) of a 2-D tensor on the current GPU whose rows are contiguous; any row stride >= its
+    columns."""
     shape, code = t.shape, _DTYPES.get(t.dtype)
-    if len(shape) != 2 or shape[1] != cols or code is None or (dtype is not None and t.dtype is not dtype) or not t.is_cuda:
-        raise ValueError(f"{what}: a 2-D CUDA tensor of {cols} columns in {dtype or 'bfloat16 or float32'} is needed, "
-                         f"got {tuple(shape)} {t.dtype} on {t.device}")
+    if len(shape) != 2 or shape[1] != cols or code is None or (dtype is not None and t.dtype is not dtype) or t.get_device() != here:
+        raise ValueError(f"{what}: a 2-D CUDA tensor of {cols} columns in {dtype or 'bfloat16 or float32'} on the current GPU is "
+                         f"needed, got {tuple(shape)} {t.dtype} on {t.device}")
     ld, step = t.stride()
     if step != 1 and cols > 1:
         raise ValueError(f"{what}: the elements of a row must be neighbours")
@@ -385,75 +398,76 @@ def new_router(n_experts: int, top_k: int, score: int = SCORE_SOFTMAX, n_groups:
 def fp8mlp_route(router: Router, logits, bias, experts, weights) -> None:
     """logits: [T, n_experts] bf16 or fp32, any row stride; bias: fp32 [n_experts] or None; receives experts (int32
     [T, top_k]) and weights (fp32 [T, top_k])."""
-    E = router.n_experts
-    T, ptr, dtype, ld = _matrix(logits, E, "logits")
+    E, here = router.n_experts, _here()
+    T, ptr, dtype, ld = _matrix(logits, E, "logits", here)
     n = T * router.top_k
-    _check(lib().fp8mlp_route(router, T, ptr, dtype, ld, None if bias is None else _as(bias, _F32, E, "bias"),
-                              _as(experts, _I32, n, "experts"), _as(weights, _F32, n, "weights"), _stream()),
+    _check(lib().fp8mlp_route(router, T, ptr, dtype, ld, None if bias is None else _as(bias, _F32, E, "bias", here),
+                              _as(experts, _I32, n, "experts", here), _as(weights, _F32, n, "weights", here), _stream(here)),
            "fp8mlp_route")
 
 
 def fp8mlp_route_backward(router: Router, logits, experts, d_weights, d_logits) -> None:
     """d_logits (type of the logits, any row stride) from d_weights (fp32 [T, top_k]) for the experts the forward chose."""
-    E = router.n_experts
-    T, ptr, dtype, ld = _matrix(logits, E, "logits")
-    d_rows, d_ptr, _, ld_d = _matrix(d_logits, E, "d_logits", logits.dtype)
+    E, here = router.n_experts, _here()
+    T, ptr, dtype, ld = _matrix(logits, E, "logits", here)
+    d_rows, d_ptr, _, ld_d = _matrix(d_logits, E, "d_logits", here, logits.dtype)
     n = T * router.top_k
     if d_rows != T:
         raise ValueError("d_logits: not as many rows as logits")
-    _check(lib().fp8mlp_route_backward(router, T, ptr, dtype, ld, _as(experts, _I32, n, "experts"),
-                                       _as(d_weights, _F32, n, "d_weights"), d_ptr, ld_d, _stream()),
+    _check(lib().fp8mlp_route_backward(router, T, ptr, dtype, ld, _as(experts, _I32, n, "experts", here),
+                                       _as(d_weights, _F32, n, "d_weights", here), d_ptr, ld_d, _stream(here)),
            "fp8mlp_route_backward")
 
 
 def fp8mlp_route_update_bias(counts, rate: float, bias) -> None:
     """bias (fp32 [n_experts], in place) moves by rate towards the experts with fewer rows than the mean (counts, int32)."""
-    n = bias.numel()
-    _check(lib().fp8mlp_route_update_bias(n, _as(counts, _I32, n, "counts"), rate, _as(bias, _F32, n, "bias"),
-                                          _stream()), "fp8mlp_route_update_bias")
+    n, here = bias.numel(), _here()
+    _check(lib().fp8mlp_route_update_bias(n, _as(counts, _I32, n, "counts", here), rate, _as(bias, _F32, n, "bias", here),
+                                          _stream(here)), "fp8mlp_route_update_bias")
 
 
 def fp8mlp_dispatch_plan(experts, n_experts: int, counts, offsets, rows) -> None:
     """experts: int32 [T, top_k]; receives counts (int32 [n_experts]), offsets (int32 [n_experts + 1]) and rows (int32
     [T, top_k])."""
-    T, k = experts.shape
-    _check(lib().fp8mlp_dispatch_plan(T, k, n_experts, _as(experts, _I32, T * k, "experts"),
-                                      _as(counts, _I32, n_experts, "counts"),
-                                      _as(offsets, _I32, n_experts + 1, "offsets"),
-                                      _as(rows, _I32, T * k, "rows"), _stream()), "fp8mlp_dispatch_plan")
+    (T, k), here = experts.shape, _here()
+    _check(lib().fp8mlp_dispatch_plan(T, k, n_experts, _as(experts, _I32, T * k, "experts", here),
+                                      _as(counts, _I32, n_experts, "counts", here),
+                                      _as(offsets, _I32, n_experts + 1, "offsets", here),
+                                      _as(rows, _I32, T * k, "rows", here), _stream(here)), "fp8mlp_dispatch_plan")
 
 
 def _rows_pair(token, expert, rows, token_name, expert_name):
-    """What dispatch and combine pass alike: (tokens, slots, d, type, token pointer and row stride, expert pointer and rows,
-    rows pointer)."""
+    """What dispatch and combine pass alike: (current GPU, tokens, slots, d, type, token pointer and row stride, expert pointer and
+    rows, rows pointer)."""
     T, k = rows.shape
     n, d = expert.shape
-    have, ptr, dtype, ld = _matrix(token, d, token_name, expert.dtype)
+    here = _here()
+    have, ptr, dtype, ld = _matrix(token, d, token_name, here, expert.dtype)
     if have != T:
         raise ValueError(f"{token_name}: {have} rows, but rows speaks of {T} tokens")
-    return T, k, d, dtype, ptr, ld, _as(expert, expert.dtype, n * d, expert_name), n, _as(rows, _I32, T * k, "rows")
+    return here, T, k, d, dtype, ptr, ld, _as(expert, expert.dtype, n * d, expert_name, here), n, _as(rows, _I32, T * k, "rows", here)
 
 
 def fp8mlp_dispatch(x, rows, xe) -> None:
     """xe[rows[t, j]] = x[t]; x: [T, d] bf16 or fp32, any row stride; xe: [n, d] of the same type, contiguous."""
-    T, k, d, dtype, ptr, ld, xe_ptr, n, rows_ptr = _rows_pair(x, xe, rows, "x", "xe")
-    _check(lib().fp8mlp_dispatch(T, k, d, dtype, ptr, ld, rows_ptr, xe_ptr, n, _stream()), "fp8mlp_dispatch")
+    here, T, k, d, dtype, ptr, ld, xe_ptr, n, rows_ptr = _rows_pair(x, xe, rows, "x", "xe")
+    _check(lib().fp8mlp_dispatch(T, k, d, dtype, ptr, ld, rows_ptr, xe_ptr, n, _stream(here)), "fp8mlp_dispatch")
 
 
 def fp8mlp_combine(ye, rows, weights, y) -> None:
     """y[t] = sum_j weights[t, j] ye[rows[t, j]]; weights fp32 [T, top_k] or None (= 1); y: [T, d], any row stride."""
-    T, k, d, dtype, ptr, ld, ye_ptr, n, rows_ptr = _rows_pair(y, ye, rows, "y", "ye")
+    here, T, k, d, dtype, ptr, ld, ye_ptr, n, rows_ptr = _rows_pair(y, ye, rows, "y", "ye")
     _check(lib().fp8mlp_combine(T, k, d, dtype, ye_ptr, n, rows_ptr,
-                                None if weights is None else _as(weights, _F32, T * k, "weights"), ptr, ld, _stream()),
+                                None if weights is None else _as(weights, _F32, T * k, "weights", here), ptr, ld, _stream(here)),
            "fp8mlp_combine")
 
 
 def fp8mlp_combine_backward(dy, ye, rows, weights, dye, d_weights) -> None:
     """dye[rows[t, j]] = weights[t, j] dy[t] and d_weights[t, j] = <dy[t], ye[rows[t, j]]> (fp32 [T, top_k])."""
-    T, k, d, dtype, ptr, ld, ye_ptr, n, rows_ptr = _rows_pair(dy, ye, rows, "dy", "ye")
+    here, T, k, d, dtype, ptr, ld, ye_ptr, n, rows_ptr = _rows_pair(dy, ye, rows, "dy", "ye")
     _check(lib().fp8mlp_combine_backward(T, k, d, dtype, ptr, ld, ye_ptr, n, rows_ptr,
-                                         _as(weights, _F32, T * k, "weights"), _as(dye, ye.dtype, n * d, "dye"),
-                                         _as(d_weights, _F32, T * k, "d_weights"), _stream()),
+                                         _as(weights, _F32, T * k, "weights", here), _as(dye, ye.dtype, n * d, "dye", here),
+                                         _as(d_weights, _F32, T * k, "d_weights", here), _stream(here)),
            "fp8mlp_combine_backward")
 
 
@@ -467,11 +481,12 @@ class GradList:
             raise ValueError("as many outputs as gradients are needed")
         self.count = len(self.tensors[0])
         self.array = (_GradTensor * max(self.count, 1))()
+        self.device = _here()
         for a, g, o in zip(self.array, *self.tensors):
             if g.dtype not in _DTYPES:
                 raise ValueError(f"gradients are bfloat16 or float32, not {g.dtype}")
-            a.g, a.out, a.n, a.dtype = (_as(g, g.dtype, g.numel(), "gradient"), _as(o, g.dtype, g.numel(), "output"), g.numel(),
-                                        _DTYPES[g.dtype])
+            a.g, a.out, a.n, a.dtype = (_as(g, g.dtype, g.numel(), "gradient", self.device),
+                                        _as(o, g.dtype, g.numel(), "output", self.device), g.numel(), _DTYPES[g.dtype])
 
 
 def new_grad_list(grads, outs=None) -> GradList:
@@ -483,17 +498,22 @@ def new_norm_workspace(device="cuda"):
     return torch.empty(NORM_WORKSPACE_BYTES, dtype=torch.uint8, device=device)
 
 
+def _clip_args(grads, norm_kind, max_norm, norm_coef, workspace):
+    here = _here()
+    if grads.device != here:
+        raise ValueError(f"gradients: the list was made for GPU {grads.device}, the current one is {here}")
+    return (grads.array, grads.count, norm_kind, max_norm, _as(norm_coef, _F32, 2, "norm_coef", here),
+            _as(workspace, _U8, NORM_WORKSPACE_BYTES, "workspace", here), _stream(here))
+
+
 def fp8mlp_grad_norm(grads: GradList, norm_kind: int, max_norm: float, norm_coef, workspace) -> None:
     """norm_coef (fp32 [2]) receives the global norm and min(1, max_norm / (norm + 1e-6))."""
-    _check(lib().fp8mlp_grad_norm(grads.array, grads.count, norm_kind, max_norm, _as(norm_coef, _F32, 2, "norm_coef"),
-                                  _as(workspace, _U8, NORM_WORKSPACE_BYTES, "workspace"), _stream()), "fp8mlp_grad_norm")
+    _check(lib().fp8mlp_grad_norm(*_clip_args(grads, norm_kind, max_norm, norm_coef, workspace)), "fp8mlp_grad_norm")
 
 
 def fp8mlp_clip_grads(grads: GradList, norm_kind: int, max_norm: float, norm_coef, workspace) -> None:
     """fp8mlp_grad_norm, and out = g * coefficient for every tensor of the list."""
-    _check(lib().fp8mlp_clip_grads(grads.array, grads.count, norm_kind, max_norm, _as(norm_coef, _F32, 2, "norm_coef"),
-                                   _as(workspace, _U8, NORM_WORKSPACE_BYTES, "workspace"), _stream()),
-           "fp8mlp_clip_grads")
+    _check(lib().fp8mlp_clip_grads(*_clip_args(grads, norm_kind, max_norm, norm_coef, workspace)), "fp8mlp_clip_grads")
 
 
 # ---------------------------------------------------------------- conveniences (allocation only)

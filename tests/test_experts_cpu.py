@@ -180,3 +180,60 @@ def test_combine_gradient_is_not_written_over_its_input(lib):
     back = lambda dy, dye, n=4: lib.fp8mlp_combine_backward(4, 1, 32, B.BF16, dy, 32, 2 * P, n, P, P, dye, P, None)
     assert back(P, P) == B.ERR_ARG
     assert back(3 * P, 3 * P) == B.ERR_ARG
+
+
+class _Elsewhere:
+    """Looks like a contiguous tensor on a GPU; its pointer is not valid and no refused call follows it."""
+
+    def __init__(self, shape, dtype, device):
+        self.shape, self.dtype, self._device = torch.Size(shape), dtype, device
+        self.device, self.is_cuda = f"cuda:{device}", True
+
+    def numel(self):
+        return self.shape.numel()
+
+    def stride(self):
+        return tuple(int(np.prod(self.shape[i + 1:])) for i in range(len(self.shape)))
+
+    def is_contiguous(self):
+        return True
+
+    def get_device(self):
+        return self._device
+
+    def data_ptr(self):
+        return P
+
+
+def test_binding_refuses_tensors_of_another_gpu(monkeypatch):
+    """One argument after the other on GPU 1 while GPU 0 is current."""
+    monkeypatch.setattr(B, "_device", lambda: 0)
+    f32, i32, bf16, u8 = torch.float32, torch.int32, torch.bfloat16, torch.uint8
+    r = B.new_router(8, 2)
+    slots, weights, logits, rows = ((4, 2), i32), ((4, 2), f32), ((4, 8), f32), ((4, 32), bf16)
+    wide = ((8, 32), bf16)
+    calls = [
+        (lambda x, b, e, w: B.fp8mlp_route(r, x, b, e, w), [logits, ((8,), f32), slots, weights]),
+        (lambda x, e, w, d: B.fp8mlp_route_backward(r, x, e, w, d), [logits, slots, weights, logits]),
+        (lambda c, b: B.fp8mlp_route_update_bias(c, 1e-3, b), [((8,), i32), ((8,), f32)]),
+        (lambda e, c, o, p: B.fp8mlp_dispatch_plan(e, 8, c, o, p), [slots, ((8,), i32), ((9,), i32), slots]),
+        (B.fp8mlp_dispatch, [rows, slots, wide]),
+        (B.fp8mlp_combine, [wide, slots, weights, rows]),
+        (B.fp8mlp_combine_backward, [rows, wide, slots, weights, wide, weights]),
+        (lambda g, o: B.new_grad_list([g], [o]), [logits, logits]),
+    ]
+    for call, args in calls:
+        for away in range(len(args)):
+            with pytest.raises(ValueError, match="cuda:1"):
+                call(*[_Elsewhere(shape, dtype, int(i == away)) for i, (shape, dtype) in enumerate(args)])
+    # a list made while its GPU was current, and the small buffers of a call
+    grads = B.new_grad_list([_Elsewhere((4, 8), f32, 0)])
+    small = [((2,), f32), ((B.NORM_WORKSPACE_BYTES,), u8)]
+    for call in (B.fp8mlp_grad_norm, B.fp8mlp_clip_grads):
+        for away in range(2):
+            with pytest.raises(ValueError, match="cuda:1"):
+                call(grads, B.NORM_L2, 1.0, *[_Elsewhere(shape, dtype, int(i == away)) for i, (shape, dtype) in enumerate(small)])
+        with monkeypatch.context() as m:
+            m.setattr(B, "_device", lambda: 1)
+            with pytest.raises(ValueError, match="gradients"):
+                call(grads, B.NORM_L2, 1.0, *[_Elsewhere(shape, dtype, 1) for shape, dtype in small])
