@@ -331,9 +331,10 @@ def fp8mlp_adam_step_scaled(tensors: list, casts: list | None, grad_scale, lr: f
                             eps: float, weight_decay: float, step: int) -> None:
     """The same two steps (casts None: without the codes) on the gradients times grad_scale, a 1-element fp32 CUDA tensor,
     e.g. norm_coef[1:] of fp8mlp_grad_norm."""
+    here = _here()
     _check(lib().fp8mlp_adam_step_scaled(_adam_tensors(tensors), None if casts is None else _adam_casts(casts, len(tensors)),
-                                         len(tensors), _ptr(grad_scale), lr, beta1, beta2, eps, weight_decay, step, _stream()),
-           "fp8mlp_adam_step_scaled")
+                                         len(tensors), _as(grad_scale, _F32, 1, "grad_scale", here), lr, beta1, beta2, eps,
+                                         weight_decay, step, _stream(here)), "fp8mlp_adam_step_scaled")
 
 
 def fp8mlp_code_stats(codes, fp8_fmt: int, counts, ld: int | None = None) -> None:

@@ -237,3 +237,12 @@ def test_binding_refuses_tensors_of_another_gpu(monkeypatch):
             m.setattr(B, "_device", lambda: 1)
             with pytest.raises(ValueError, match="gradients"):
                 call(grads, B.NORM_L2, 1.0, *[_Elsewhere(shape, dtype, 1) for shape, dtype in small])
+
+
+@pytest.mark.parametrize("bad", [((1,), torch.float64, 0), ((1,), torch.bfloat16, 0), ((2,), torch.float32, 0), ((1,), torch.float32, 1)],
+                         ids=["f64", "bf16", "norm and coefficient", "another GPU"])
+def test_adam_coefficient_is_one_fp32_element(monkeypatch, bad):
+    """The kernel reads one float; of the pair that the norm call fills that would be the norm."""
+    monkeypatch.setattr(B, "_device", lambda: 0)
+    with pytest.raises(ValueError, match="grad_scale"):
+        B.fp8mlp_adam_step_scaled([], None, _Elsewhere(*bad), 1e-3, 0.9, 0.95, 1e-8, 0.0, 1)
