@@ -423,8 +423,10 @@ FP8MLP_API int fp8mlp_combine_backward(int64_t T, int top_k, int64_t d, int dtyp
  *   norm = sqrt(sum over all tensors and elements of g^2)  or  max |g|;   coef = min(1, max_norm / (norm + 1e-6))
  *   norm_coef[0] = norm, norm_coef[1] = coef (device floats);   fp8mlp_clip_grads also: out = g * coef for every element
  * g fp32 or bf16 (both may occur in one list), contiguous, n >= 0 elements, aligned to its type only; out of the same
- * type, g itself or a buffer that overlaps no tensor of the list.  The squares are summed in fp64 (no overflow or
- * underflow short of the fp32 result's) in an order fixed by the list's sizes.  A NaN anywhere makes norm and coef NaN,
+ * type, g itself or a buffer that overlaps no tensor of the list.  The squares of each aligned 32 bytes are summed in
+ * fp32 where that sum lies well inside its range, else one by one in fp64, and all else in fp64: the norm is within
+ * 3 2^-24 of itself, with no overflow or underflow short of the fp32 result's.  The order is fixed by the list's sizes, the
+ * addresses modulo 32 and the device's number of SMs: no atomics.  A NaN anywhere makes norm and coef NaN,
  * an infinity makes norm infinite and coef 0, as the formulas say.  A coefficient of 1 leaves in-place tensors untouched.
  * workspace: FP8MLP_NORM_WORKSPACE_BYTES of device memory, 16-byte aligned, no state between calls; calls that may
  * overlap need one each.  max_norm >= 0. */

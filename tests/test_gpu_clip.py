@@ -185,3 +185,25 @@ def test_adam_with_the_clip_coefficient(cast):
         assert torch.equal(states[0][key], states[1][key]), key
     assert torch.equal(codes[0], codes[1]) and bool(codes[0].any()) == cast
     assert torch.equal(states[0]["g"], g)              # the fused form leaves the gradient as it was
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("n", [1, 7, 16, 33, 1000, 8191, 70001, 3_000_003])
+def test_norm_of_the_same_values_at_other_addresses(n, dtype):
+    """The grouping of the sum follows the addresses modulo 32: at equal ones the norm has the same bits, at others it stays within
+    its bound.  The 8 or 16 squares of a 32-byte unit are summed in fp32, at most four roundings of 2^-24 one after the other (the
+    squares of bf16 are exact there), the units in fp64; the root halves a relative error and is rounded once: 2 + 1 times 2^-24."""
+    rng = np.random.default_rng(n)
+    values = torch.from_numpy((rng.normal(0, 1, n) * np.exp(rng.normal(0, 2, n))).astype(np.float32)).to(dtype)
+    exact, _ = R.clip([values.float().numpy()], 1.0, "l2")
+    size = values.element_size()
+    by_shift = {}
+    for shift in range(32 // size):
+        for _ in range(2):
+            flat = torch.zeros(n + 2 * shift + 64, dtype=dtype, device="cuda")
+            g = flat[shift:shift + n]
+            g.copy_(values)
+            assert g.data_ptr() % 32 == shift * size
+            got = _run([g], None, 1.0, "l2", norm_only=True)
+            assert abs(float(got[0]) - exact) <= 3.001 * 2.0 ** -24 * exact
+            assert np.array_equal(by_shift.setdefault(shift, got), got)
