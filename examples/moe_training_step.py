@@ -48,11 +48,10 @@ class MoeLayer:
         self.grads = [torch.zeros_like(p) for p in self.params]
         self.grad_list = B.new_grad_list(self.grads)
         self.norm_coef, self.workspace = torch.zeros(2, device="cuda"), B.new_norm_workspace()
-        one = lambda: torch.ones(1, device="cuda")
-        self.adam = [dict(w=p, g=g, m=torch.zeros(p.numel(), dtype=torch.uint8, device="cuda"),
-                          v=torch.zeros(p.numel(), dtype=torch.uint8, device="cuda"), scale_m_in=one(), scale_v_in=one(),
-                          scale_m_out=one(), scale_v_out=one(), amax_m=torch.zeros(1, device="cuda"),
-                          amax_v=torch.zeros(1, device="cuda")) for p, g in zip(self.params, self.grads)]
+        one, zero = (lambda: torch.ones(1, device="cuda")), (lambda: torch.zeros(1, device="cuda"))
+        codes = lambda p: torch.zeros(p.numel(), dtype=torch.uint8, device="cuda")
+        self.adam = [dict(w=p, g=g, m=codes(p), v=codes(p), scale_m_in=one(), scale_v_in=one(), scale_m_out=one(), scale_v_out=one(),
+                          amax_m=zero(), amax_v=zero()) for p, g in zip(self.params, self.grads)]
         self.steps = 0
 
     def close(self):
@@ -108,17 +107,31 @@ class MoeLayer:
         torch.matmul(self.x.float().T, d_logits, out=self.grads[0])
         return (dx.float() + d_logits @ self.params[0].T).bfloat16()
 
-    def step(self, lr: float = 1e-3, max_norm: float = 1.0, bias_rate: float = 1e-3):
+    def choose_moment_scales(self, beta1: float, beta2: float):
+        """The scales that this step writes its moments with: delayed, from the maxima of the last step, with room for moments
+        that grow; a tensor without a gradient so far starts from a bound of this step's, for no element of the clipped
+        gradients is larger than their norm.
+
+        m gets more room than v.  E4M3 keeps values down to 2^-18.8 of its largest, E5M2 down to 2^-32.8, in terms of the
+        gradient 2^-16.4; with these factors an element's v outlasts its m, where an m without its v would make a step of many
+        times the learning rate."""
+        bound = self.norm_coef[:1] * self.norm_coef[1:]
+        for t in self.adam:
+            top_m = torch.where(t["amax_m"] > 0, 16 * t["amax_m"], 8 * (1 - beta1) * bound)
+            top_v = torch.where(t["amax_v"] > 0, 4 * t["amax_v"], (1 - beta2) * bound ** 2)
+            B.fp8mlp_scale_from_amax(top_m, B.E4M3, t["scale_m_out"])
+            B.fp8mlp_scale_from_amax(top_v, B.E5M2, t["scale_v_out"])
+
+    def step(self, lr: float = 1e-3, max_norm: float = 1.0, bias_rate: float = 1e-3, beta1: float = 0.9, beta2: float = 0.95):
         """Clipped Adam step on all parameters, and the router's balance bias.  Returns (norm, coefficient), on the device."""
         self.steps += 1
         B.fp8mlp_grad_norm(self.grad_list, B.NORM_L2, max_norm, self.norm_coef, self.workspace)
+        self.choose_moment_scales(beta1, beta2)
         for i in range(0, len(self.adam), 8):
-            B.fp8mlp_adam_step_scaled(self.adam[i:i + 8], None, self.norm_coef[1:], lr, 0.9, 0.95, 1e-8, 0.0, self.steps)
-        for t in self.adam:                              # the moments' scales follow their maxima, one step late
+            B.fp8mlp_adam_step_scaled(self.adam[i:i + 8], None, self.norm_coef[1:], lr, beta1, beta2, 1e-8, 0.0, self.steps)
+        for t in self.adam:                              # what the codes were written with
             t["scale_m_in"].copy_(t["scale_m_out"])
             t["scale_v_in"].copy_(t["scale_v_out"])
-            B.fp8mlp_scale_from_amax(t["amax_m"], B.E4M3, t["scale_m_out"])
-            B.fp8mlp_scale_from_amax(t["amax_v"], B.E5M2, t["scale_v_out"])
         B.fp8mlp_route_update_bias(self.counts, bias_rate, self.bias)
         return self.norm_coef
 

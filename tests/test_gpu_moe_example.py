@@ -167,3 +167,56 @@ def test_the_chain_in_a_cuda_graph():
         # y = sum of the weights times x, up to the rounding of y
         total = want["weights"].sum(-1, keepdim=True) * x.float()
         assert torch.allclose(want["y"].float(), total, rtol=2.0 ** -7, atol=1e-6)
+
+
+def _decode(codes, dtype, scale):
+    return codes.view(dtype).double() / scale.double()
+
+
+@pytest.mark.parametrize("max_norm", [0.05, 1e3], ids=["clipped", "not clipped"])
+def test_moments_of_the_first_steps(max_norm):
+    """The FP8 moments against exact ones of the same gradients from the first step on, an expert that joins in the third step
+    included.  Per element, a code adds half a step: 2^-4 of an E4M3 value, 2^-3 of an E5M2 value, or half the smallest step
+    (2^-10, 2^-17) over the scale; what the last step was off by is carried on with beta.  Parameters: a step moves them by at most
+    about lr, from either moments, as long as no v is lost beside its m; three steps are held to 3 lr."""
+    T, d, f, E, k, lr, beta1, beta2 = 256, 64, 96, 4, 2, 1e-3, 0.9, 0.95
+    gen = torch.Generator(device="cuda").manual_seed(13)
+    layer = MoeLayer(d, f, E, k, T * k, seed=6)
+    try:
+        layer.bias[3] = -float("inf")
+        w = [p.double() for p in layer.params]
+        exact = [[torch.zeros_like(p) for p in w] for _ in range(2)]
+        off = [[torch.zeros_like(p) for p in w] for _ in range(2)]
+        for step in range(1, 4):
+            if step == 3:
+                layer.bias[3] = 1.0
+            x = torch.randn((T, d), generator=gen, device="cuda").bfloat16()
+            layer.forward(x)
+            layer.backward((torch.randn((T, d), generator=gen, device="cuda") / T).bfloat16())
+            grads = [g.double() for g in layer.grads]
+            _, coef = layer.step(lr, max_norm, bias_rate=0.0).tolist()
+            assert (coef < 1.0) == (max_norm < 1.0)
+            for i, (t, g) in enumerate(zip(layer.adam, grads)):
+                shape = g.shape
+                if step < 3 and i >= 1 + 9:
+                    assert not g.any() and not t["m"].any() and not t["v"].any()
+                for j, (beta, value, code, half, least, dtype) in enumerate((
+                        (beta1, coef * g, "m", 2.0 ** -4, 2.0 ** -10, torch.float8_e4m3fn),
+                        (beta2, (coef * g) ** 2, "v", 2.0 ** -3, 2.0 ** -17, torch.float8_e5m2))):
+                    exact[j][i] = beta * exact[j][i] + (1 - beta) * value
+                    scale = t[f"scale_{code}_in"]
+                    got = _decode(t[code], dtype, scale).view(shape)
+                    carried = beta * off[j][i]
+                    allowed = carried + half * (exact[j][i].abs() + carried) + least / scale.double() + 1e-5 * exact[j][i].abs()
+                    assert bool(((got - exact[j][i]).abs() <= allowed).all()), f"{code} of parameter {i}, step {step}"
+                    off[j][i] = allowed
+                assert not bool(((t["m"] & 0x7f) != 0)[t["v"] == 0].any()), "an m without its v"
+                if g.any():
+                    # the codes carry the moments, not a few of their largest elements
+                    assert float((_decode(t["m"], torch.float8_e4m3fn, t["scale_m_in"]).view(shape) - exact[0][i]).norm()) < \
+                        0.1 * float(exact[0][i].norm()), f"m of parameter {i}, step {step}"
+                upd = (exact[0][i] / (1 - beta1 ** step)) / (torch.sqrt(exact[1][i] / (1 - beta2 ** step)) + 1e-8)
+                w[i] = w[i] - lr * upd
+                assert float((layer.params[i].double() - w[i]).abs().max()) <= 3 * lr, f"parameter {i}, step {step}"
+    finally:
+        layer.close()
