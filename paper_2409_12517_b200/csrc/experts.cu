@@ -91,6 +91,7 @@ __global__ void __launch_bounds__(kPlanWarps * 32) plan_kernel(const PlanArgs a)
         }
         total[e] = run;
     }
+    __syncwarp();                                        // the loop ends earlier for some lanes, the cluster's barriers take whole warps
     if (n_cta > 1) cluster_sync_all();                   // every CTA's totals are there
     else __syncthreads();
     // offsets: a scan over the experts, one per thread at a time
@@ -146,6 +147,7 @@ __global__ void __launch_bounds__(kPlanWarps * 32) plan_kernel(const PlanArgs a)
         for (int u = 0; u < kPlanUnroll; ++u)
             if (i0 + 32 * u < end) a.rows[i0 + 32 * u] = place[u] < 0 ? -1 : place[u] + mine[e[u]] + start[e[u]];
     }
+    __syncwarp();                                        // a ragged piece ends earlier for some lanes
     if (n_cta > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");        // and none leaves before the others have
 }
 

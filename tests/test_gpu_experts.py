@@ -272,3 +272,16 @@ def test_other_stream_and_repeats():
         B.fp8mlp_combine_backward(y1, late, rows, w, dye1, dw1)
     torch.cuda.current_stream().wait_stream(side)
     assert torch.equal(y0, y1) and torch.equal(dye0, dye1) and torch.equal(dw0, dw1)
+
+
+@pytest.mark.parametrize("T,k,E", [(1025, 1, 5), (2049, 3, 60), (4099, 5, 33), (8193, 2, 1000), (20011, 7, 257)])
+def test_plan_with_ragged_warps(T, k, E):
+    """Numbers of slots and experts that leave some lanes of a warp without work before each barrier of the cluster; repeated, the
+    same bits."""
+    rng = np.random.default_rng(T)
+    experts = _experts(rng, T, k, E, 0.1)
+    first = _plan(experts, E)
+    for got, want in zip(first, R.plan(experts, E)):
+        assert np.array_equal(got.cpu().numpy(), want)
+    for _ in range(20):
+        assert all(torch.equal(a, b) for a, b in zip(first, _plan(experts, E)))
