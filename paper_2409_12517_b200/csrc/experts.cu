@@ -351,7 +351,8 @@ __global__ void __launch_bounds__(kRowThreads) combine_backward_kernel(const Row
 bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
 // Clusters of 16 CTAs are beyond the portable size: whether the device has room for one (a part of a GPU may not) is asked
-// once per device, for the largest CTA that a plan launches.
+// once per device, for the largest CTA that a plan launches, whose shared memory is allowed here as well.  Plans that do not
+// ask have at most kPlanFill warps with slots to a CTA: 32 KiB and the 8 KiB of static arrays, within the default 48.
 int plan_max_cluster(int* limit) {
     static std::atomic<int> known[64];
     int dev = 0;
@@ -481,9 +482,6 @@ extern "C" int fp8mlp_dispatch_plan(int64_t T, int top_k, int n_experts, const i
     int warps = (n_experts + 31) / 32;                   // the scan takes a thread per expert
     if (warps < a.key_warps) warps = a.key_warps;
     const size_t smem = static_cast<size_t>(a.key_warps) * n_experts * sizeof(int32_t);
-    if (smem > 40 * 1024)
-        FP8MLP_CUDA_CHECK(cudaFuncSetAttribute(plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                               kPlanWarps * FP8MLP_MAX_EXPERTS * static_cast<int>(sizeof(int32_t))));
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(cluster));
     cfg.blockDim = dim3(static_cast<unsigned>(warps * 32));
