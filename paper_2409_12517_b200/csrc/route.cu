@@ -225,8 +225,8 @@ __device__ __forceinline__ void score_row(const RouteArgs& a, int e0, bool biase
 // a token with Q = 1), so a round moves values only; which expert a value belongs to is looked up once at the end, by k
 // lanes side by side, in the unsorted row in shared memory.  -inf stands for "cannot be chosen".
 // The lanes hold Q tokens, whose steps are interleaved: the group loops and rounds run once for both, and one's reductions
-// wait behind the other's.  With Q = 2 those 16384 tokens take 11.9 us instead of 13.7 (65536: 35.8 and 43.8, 8192: 9.1
-// and 8.5, 4096: 5.2 and 6.6; the bytes need 2.7 at 16384); without groups 9.7 and 9.4, one token 2.6 and 2.2.
+// wait behind the other's.  With Q = 2 those 16384 tokens take 11.2 us instead of 13.3 (65536: 35.6 and 43.1; the bytes need
+// 2.7 at 16384; other sizes: two_at_a_time); without groups 9.7 and 9.4, one token 2.6 and 2.2.
 // Blocks per SM with Q = 1: 12 of 40 registers with a whole warp per token (16 of 32: 14.0 us), 16 where tokens share a
 // warp (64 experts: 5.9 us, 7.3 with 12).  More experts per lane and fewer lanes per token were slower or equal.
 template <int LANES, int V, int Q, typename SRC>
@@ -657,6 +657,20 @@ int launch_backward_sparse(const RouteArgs& a, int dtype, cudaStream_t st) {
                                                     : route_backward_sparse_kernel<LANES, uint16_t>, a, 0, st);
 }
 
+// A whole warp per token, groups on lanes: whether each warp takes two tokens.  Two share the steps' waits and instructions, one
+// ends sooner and lets more blocks in: 24 tokens an SM at a time beside a second launch (half of 12 blocks of 4), 40 in twos
+// (half of 10 blocks of 8), so the better of the two changes with the number of tokens, and sooner where the row fills the warp.
+// us one at a time / in twos, 8 of 256 in 8 groups and 6 of 160 in 8:
+//   tokens      1024        3000        3500        5000        6144        8192        9600        10500       16384
+//   256      3.1 / 3.3   4.7 / 4.5   4.9 / 4.6   6.7 / 5.9   7.0 / 8.4   8.0 / 8.7   8.9 / 8.8   9.4 / 8.9   13.3 / 11.2
+//   160      2.7 / 3.1   3.6 / 3.9   3.8 / 3.9   5.9 / 5.1   5.9 / 8.3   6.8 / 8.4   7.8 / 8.4   8.3 / 8.4   11.8 / 11.3
+bool two_at_a_time(const RouteArgs& a) {
+    const bool full = a.E > 192;
+    if (a.T <= 24 * 148) return full && a.T > 2048;
+    if (a.T <= 40 * 148) return true;
+    return a.T > (full ? 60 : 72) * 148;
+}
+
 // LANES x V covers the row with the fewest lanes that keep V at 8; beyond 256 experts V grows.  Groups get lanes of their own
 // where 32 are enough for that.
 int run_route(const RouteArgs& a, int dtype, cudaStream_t st) {
@@ -671,11 +685,9 @@ int run_route(const RouteArgs& a, int dtype, cudaStream_t st) {
     if (lanes == 4) return launch_route<4, 8>(a, dtype, st);
     if (lanes == 8) return launch_route<8, 8>(a, dtype, st);
     if (lanes == 16) return launch_route<16, 8>(a, dtype, st);
-    // A whole warp per token: two at a time where groups on lanes are chosen and the tokens fill the SMs (1024 tokens 3.1 us
-    // one at a time and 3.3 in twos).
     if (lanes == 32)
-        return a.G > 1 && a.T > 1024 && group_lanes(a.G, a.per, 8) <= 32 ? launch_route<32, 8, 2>(a, dtype, st)
-                                                                          : launch_route<32, 8>(a, dtype, st);
+        return a.G > 1 && group_lanes(a.G, a.per, 8) <= 32 && two_at_a_time(a) ? launch_route<32, 8, 2>(a, dtype, st)
+                                                                                : launch_route<32, 8>(a, dtype, st);
     if (a.E <= 512) return launch_route<32, 16>(a, dtype, st);
     return launch_route<32, 32>(a, dtype, st);
 }

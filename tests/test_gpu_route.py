@@ -401,3 +401,21 @@ def test_groups_under_the_lowest_bias(kind, E, groups):
         assert set(got[t]) == set(ref_e) and got[t][-1] == per
         order = np.argsort(got[t])
         np.testing.assert_allclose(weights[t].cpu().numpy()[order], ref_w[np.argsort(ref_e)], rtol=_tol(x[t], E), atol=1e-38)
+
+
+@pytest.mark.parametrize("E,groups,top_groups,k", [(256, 8, 4, 8), (160, 8, 3, 6), (144, 9, 4, 4)])
+@pytest.mark.parametrize("T", [2301, 5003, 7001, 9001, 10901])
+def test_any_number_of_tokens_as_few(E, groups, top_groups, k, T):
+    """One or two tokens per warp, by the number of tokens: the same bits as small calls on parts of the rows."""
+    rng = np.random.default_rng(T + E)
+    logits = _logits(rng, T, E, torch.float32)
+    logits[11] = -float("inf")
+    logits[T - 2, 5:] = -float("inf")
+    bias = torch.from_numpy(rng.normal(0, 0.1, E).astype(np.float32)).cuda()
+    for kind, b in (("sigmoid", bias), ("softmax", bias), ("softmax", None)):
+        kw = dict(groups=groups, top_groups=top_groups, group_top=2, renorm=True, scale=2.5)
+        _, experts, weights = _route(logits, b, k, kind, **kw)
+        for begin in range(0, T, 1000):
+            _, e, w = _route(logits[begin:begin + 1000], b, k, kind, **kw)
+            assert torch.equal(e, experts[begin:begin + 1000]) and torch.equal(w, weights[begin:begin + 1000])
+        _compare(logits[T - 20:], b, experts[T - 20:], weights[T - 20:], k, kind, **kw)
