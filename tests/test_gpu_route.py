@@ -419,3 +419,27 @@ def test_any_number_of_tokens_as_few(E, groups, top_groups, k, T):
             _, e, w = _route(logits[begin:begin + 1000], b, k, kind, **kw)
             assert torch.equal(e, experts[begin:begin + 1000]) and torch.equal(w, weights[begin:begin + 1000])
         _compare(logits[T - 20:], b, experts[T - 20:], weights[T - 20:], k, kind, **kw)
+
+
+@pytest.mark.parametrize("E,groups,top_groups,k", [(2, 2, 1, 1), (2, 2, 2, 2), (6, 2, 1, 3), (10, 2, 1, 4), (14, 2, 2, 9), (16, 2, 1, 8), (16, 2, 2, 16),
+                                                   (9, 3, 2, 4), (15, 3, 1, 5), (20, 4, 3, 15), (28, 7, 2, 8), (8, 4, 3, 5)])
+@pytest.mark.parametrize("kind", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("group_top", [1, 2])
+def test_few_experts_in_groups(kind, E, groups, top_groups, k, group_top):
+    """Tokens on two, four and eight lanes whose groups are lanes of their own; nearly every row is decided by more than a rounding
+    and has to be equal."""
+    rng = np.random.default_rng(100 * E + groups)
+    for T, dtype, with_bias in ((1, torch.float32, False), (131, torch.float32, True), (257, torch.bfloat16, False)):
+        logits = _logits(rng, T, E, dtype)
+        if T > 100:
+            logits[3] = -float("inf")
+            logits[4, 1:] = -float("inf")
+            logits[5, : E // groups] = -float("inf")
+        bias = torch.from_numpy(rng.normal(0, 0.1, E).astype(np.float32)).cuda() if with_bias else None
+        kw = dict(groups=groups, top_groups=top_groups, group_top=group_top, renorm=True, scale=2.5)
+        router, experts, weights = _route(logits, bias, k, kind, **kw)
+        _compare(logits, bias, experts, weights, k, kind, **kw)
+        x, b = logits.float().cpu().numpy(), None if bias is None else bias.cpu().numpy()
+        decided = [t for t in range(T) if R.route_row(x[t], b, k, kind, **kw)[2] >= 1e-5]
+        assert len(decided) >= 0.9 * T
+        _check_backward(rng, router, logits, experts, kind, True, 2.5)
