@@ -223,7 +223,7 @@ __global__ void __launch_bounds__(kRowThreads) dispatch_kernel(const RowArgs a) 
 }
 
 // Bound by DRAM reads: 8192 x 4096 bf16 from six rows each take 69.9 us for 470 MB, 6.7 TB/s.  S slots of U units are in
-// flight together.  More would cost occupancy (6 or 8 slots of 32 bytes ran 6 to 18 % slower than 3), fewer leave the
+// flight together.  More would cost occupancy (6 or 8 slots of 32 bytes ran 14 and 22 % slower than 3), fewer leave the
 // memory idle, and a last batch that is not full does too.
 template <typename T, int W, bool WEIGHTED, int S, int U>
 __global__ void __launch_bounds__(kRowThreads, S == 4 ? 4 : 0) combine_kernel(const RowArgs a) {

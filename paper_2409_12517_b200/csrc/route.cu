@@ -220,9 +220,10 @@ __device__ __forceinline__ void score_row(const RouteArgs& a, int e0, bool biase
     }
 }
 
-// The choice: every lane sorts its values c, eight at a time, and the token's lanes take the largest head k times.  The
-// kernel is bound by instructions, not by memory (16384 tokens, 8 of 256 experts in 4 of 8 groups: 605 warp instructions
-// a token with Q = 1), so a round moves values only; which expert a value belongs to is looked up once at the end, by k
+// The choice: every lane sorts its values c, eight at a time, and the token's lanes take the largest head k times.  Instructions
+// cost more than the bytes (8 of 256 experts in 4 of 8 groups: 523 warp instructions a token with Q = 2; their issue takes 30
+// of 35.6 us for 65536 tokens, and 7.5 of 11.2 us for 16384, where the rest goes to every block's first loads and a second
+// wave that is not full), so a round moves values only; which expert a value belongs to is looked up once at the end, by k
 // lanes side by side, in the unsorted row in shared memory.  -inf stands for "cannot be chosen".
 // The lanes hold Q tokens, whose steps are interleaved: the group loops and rounds run once for both, and one's reductions
 // wait behind the other's.  With Q = 2 those 16384 tokens take 11.2 us instead of 13.3 (65536: 35.6 and 43.1; the bytes need
