@@ -222,7 +222,7 @@ __global__ void __launch_bounds__(kRowThreads) dispatch_kernel(const RowArgs a) 
     }
 }
 
-// Bound by DRAM reads: 8192 x 4096 bf16 from six rows each take 69.9 us for 470 MB, 6.7 TB/s.  S slots of U units are in
+// Bound by DRAM reads: 8192 x 4096 bf16 from six rows each take 70.4 us for 470 MB, 6.7 TB/s.  S slots of U units are in
 // flight together.  More would cost occupancy (6 or 8 slots of 32 bytes ran 14 and 22 % slower than 3), fewer leave the
 // memory idle, and a last batch that is not full does too.
 template <typename T, int W, bool WEIGHTED, int S, int U>
@@ -437,8 +437,8 @@ int run_combine(const RowArgs& a, bool wide, cudaStream_t st) {
     if (a.k == 1) return launch_combine<T, 8, WEIGHTED, 1, 2>(a, st);
     // As many slots at a time as leave the fewest places of the last batch empty, and of these the most.  8192 rows of
     // 4096 bf16 in us, 2 / 3 / 4 at a time (k = 1: one slot of two units 25.7, else 29.5 / 30.4 / 34.1):
-    //   k = 2: 35.2 / 36.2 / 38.8   3: 47.4 / 42.3 / 44.8   4: 53.6 / 55.1 / 51.6   5: 66.2 / 62.2 / 66.7
-    //   k = 6: 72.6 / 69.9 / 73.2   7: 85.0 / 82.0 / 80.3   8: 92.0 / 89.9 / 88.7
+    //   k = 2: 35.8 / 36.6 / 39.4   3: 48.1 / 42.8 / 45.3   4: 54.0 / 55.8 / 52.2   5: 66.6 / 62.7 / 67.8
+    //   k = 6: 73.2 / 70.4 / 73.7   7: 85.8 / 82.7 / 80.9   8: 92.7 / 90.6 / 89.1
     int best = 4;
     for (int s = 3; s >= 2; --s)
         if ((a.k + s - 1) / s * s < (a.k + best - 1) / best * best) best = s;
