@@ -70,9 +70,13 @@ enum {
 enum {
     FP8MLP_SCALE_GIVEN = 0,              /* delayed scaling: use the scale buffers as they are  */
     FP8MLP_SCALE_FROM_CURRENT_AMAX = 1,  /* just-in-time: derive every scale from this call's data */
-    FP8MLP_SCALE_GIVEN_WEIGHTS_CAST = 2  /* fp8mlp_forward only: as SCALE_GIVEN, and the context's FP8 weight buffers
+    FP8MLP_SCALE_GIVEN_WEIGHTS_CAST = 2, /* fp8mlp_forward only: as SCALE_GIVEN, and the context's FP8 weight buffers
                                             already hold this step's codes (fp8mlp_adam_step_cast wrote them): the
                                             weight pass is skipped, W1/W2/W3 are not read (may be null), amax.w* stay */
+    FP8MLP_SCALE_GIVEN_X_CAST = 3,       /* fp8mlp_forward, fp8mlp_forward_merged: as SCALE_GIVEN, and FP8MLP_WS_XQ already holds
+                                            this call's T rows of codes Q(x scales.x) (fp8mlp_rmsnorm wrote them): x is not read
+                                            (may be null), amax.x stays                                                   */
+    FP8MLP_SCALE_GIVEN_BOTH_CAST = 4     /* fp8mlp_forward only: the two together */
 };
 enum { /* fp8mlp_workspace: internal buffers, for inspection by tests */
     FP8MLP_WS_XQ = 0,   /* E4M3 [T,d]   quantised x                                   */
@@ -451,6 +455,82 @@ FP8MLP_API int fp8mlp_adam_step_scaled(const fp8mlp_adam_tensor* tensors, const 
 /* The same for bf16 operands (the unquantised last layer of FP8MLP_H_BF16 contexts): A, B bf16, no scales. */
 FP8MLP_API int fp8mlp_gemm_bf16(int64_t M, int64_t N, int64_t K, const void* A, int a_kmajor, const void* B,
                                 int b_kmajor, float* out, void* stream);
+
+/* ---------------------------------------------------------------------------------------------------------------
+ * The norm in front of the block, with the residual's addition.  The paper trains a Llama-style model, whose MLP blocks read
+ *   h = x + residual                                     (residual null: h = x)
+ *   y[t, i] = h[t, i] * rstd[t] * gain[i],               rstd[t] = 1 / sqrt(mean_i h[t, i]^2 + eps)
+ * x, residual, h: T rows of d elements of one type (FP8MLP_BF16 or FP8MLP_F32) with a row stride each; gain fp32 [d], null = 1.
+ * h is rounded to that type once, and the norm is that of the rounded values: the gradient of what was computed follows from
+ * the stored h.  Squares are summed in fp32.  h_out receives h (null: not wanted; needs a residual); it may be x or the
+ * residual itself, no other outputs overlap inputs.  out_kind:
+ *   FP8MLP_RMS_SAME       y in the type of x
+ *   FP8MLP_RMS_E4M3       y: E4M3 codes Q(y * *scale), `scale` one device float that is read (delayed scaling)
+ *   FP8MLP_RMS_E4M3_ROWS  y: E4M3 codes Q(y * scale[t]), scale fp32 [T] written: 448 / max_i |y[t, i]| (1 where that maximum is
+ *                         zero or not finite)
+ * scale is not used by FP8MLP_RMS_SAME.  amax (nullable, not with FP8MLP_RMS_E4M3_ROWS): receives max |y| of this call (before
+ * any cast).  rstd (nullable): fp32 [T], for the backward pass.  With y = a context's FP8MLP_WS_XQ buffer (ld_y = d), scales.x
+ * and amax.x the codes are the block's own operand: fp8mlp_forward with FP8MLP_SCALE_GIVEN_X_CAST does not read x again.
+ * d a multiple of 16, at most FP8MLP_MAX_NORM_WIDTH; row strides in elements, at least d, of 16 bytes' multiples; all rows and
+ * gain start on 16-byte boundaries.  A row that holds a NaN or an infinity has no norm (NaN where the
+ * formulas say so); a row of zeros is zeros if eps > 0. */
+enum { FP8MLP_RMS_SAME = 0, FP8MLP_RMS_E4M3 = 1, FP8MLP_RMS_E4M3_ROWS = 2 };
+#define FP8MLP_MAX_NORM_WIDTH 16384
+FP8MLP_API int fp8mlp_rmsnorm(int64_t T, int64_t d, int dtype, const void* x, int64_t ld_x, const void* residual,
+                              int64_t ld_residual, void* h_out, int64_t ld_h, const float* gain, float eps, int out_kind, void* y,
+                              int64_t ld_y, float* scale, float* amax, float* rstd, void* stream);
+/* Its gradient (any cast straight-through), from the stored h and rstd:
+ *   g = dy * gain;   dx[t, i] = rstd[t] * (g[t, i] - h[t, i] rstd[t] * mean_j(g[t, j] h[t, j] rstd[t])) + dh[t, i]
+ *   d_gain[i] = sum_t dy[t, i] h[t, i] rstd[t]           (fp32, overwritten)
+ * dh (nullable): what reached h along the residual stream.  dx is the gradient of x and of the residual alike.  dy, h, dh, dx
+ * of one type, a row stride each, as above; dx may be dy or dh itself.  d_gain is null if the gain has no gradient; it needs
+ * `workspace`: FP8MLP_RMS_PARTIALS * d floats, 16-byte aligned, no state between calls; calls that may overlap need one each. */
+#define FP8MLP_RMS_PARTIALS 592
+FP8MLP_API int fp8mlp_rmsnorm_backward(int64_t T, int64_t d, int dtype, const void* dy, int64_t ld_dy, const void* h, int64_t ld_h,
+                                       const float* gain, const float* rstd, const void* dh, int64_t ld_dh, void* dx,
+                                       int64_t ld_dx, float* d_gain, void* workspace, void* stream);
+
+/* ---------------------------------------------------------------------------------------------------------------
+ * 4-bit operands with a scale per block: quantisation, its inverse, and the product.  An operand is a matrix [rows, cols] whose
+ * columns are the contraction.  Elements are E2M1 (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives), cut along each row into blocks:
+ *   FP8MLP_MXFP4  blocks of 32, scale E8M0 (a power of two)
+ *   FP8MLP_NVFP4  blocks of 16, scale E4M3 (not negative), and one fp32 scale g for the whole tensor
+ *   value[r, c] = element[r, c] * block_scale[r, c / block]     (NVFP4: times 1 / g)
+ * codes: element c of a row is the low (c even) or high (c odd) half of byte c / 2; row stride ld_codes bytes, a multiple of 16.
+ * block_scales: bytes in tiles of 128 rows x 4 blocks, 512 bytes each, tiles of one row group side by side: block b of row r is
+ *   at ((r / 128) * ceil(n_blocks / 4) + b / 4) * 512 + (r % 32) * 16 + (r % 128) / 32 * 4 + b % 4,  n_blocks = ceil(cols / block)
+ * (the order in which the tensor cores take them).  An operand's block_scales are fp8mlp_fp4_scale_bytes long; bytes of blocks that
+ * do not exist are 0 and so is the high half of a row's last byte if cols is odd (fp8mlp_quantize_fp4 writes both).
+ *
+ * fp8mlp_quantize_fp4: src [rows, cols], bf16 or fp32, row stride ld_src, any alignment of its type.
+ *   transpose = 0: the operand is src;   transpose != 0: it is src^T ([cols, rows], blocks along the rows of src)
+ *   v = src (MXFP4), src * g (NVFP4, one fp32 rounding);   a = max |v| over a block
+ *   MXFP4: block scale 2^(floor(log2 a) - 2), at least 2^-127 (values from 6 to 8 times it become 6)
+ *   NVFP4: block scale Q_e4m3(a / 6), saturating; elements of a block whose scale rounds to 0 are 0
+ *   element = v / block scale, rounded once to the nearest (ties to the even code), beyond 6 to 6
+ * A block that holds a NaN or an infinity gets the scale NaN, so that all of it is NaN.
+ * scale: g (NVFP4; null for MXFP4, whose scale_mode is FP8MLP_SCALE_GIVEN).  FP8MLP_SCALE_FROM_CURRENT_AMAX: g is written first:
+ * the largest power of two with g * max |src| <= 448 * 6 (1 if that maximum is zero or not finite; within 2^-100 .. 2^100).
+ * amax: receives max |src| (NaN left out); nullable with FP8MLP_SCALE_GIVEN.  Row r of the operand: codes + r * ld_codes, where
+ * (columns + 1) / 2 bytes are used and those up to the next multiple of 16 cleared; codes and block_scales 16-byte aligned. */
+enum { FP8MLP_MXFP4 = 0, FP8MLP_NVFP4 = 1 };
+/* Bytes of the block scales of a [rows, cols] operand (0 for a bad format or a negative size). */
+FP8MLP_API int64_t fp8mlp_fp4_scale_bytes(int fp4_fmt, int64_t rows, int64_t cols);
+FP8MLP_API int fp8mlp_quantize_fp4(const void* src, int src_dtype, int64_t rows, int64_t cols, int64_t ld_src, int transpose,
+                                   int fp4_fmt, int scale_mode, float* scale, float* amax, uint8_t* codes, int64_t ld_codes,
+                                   uint8_t* block_scales, void* stream);
+/* out[r, c] = element * block scale * (1 / *scale)  (scale as above), bf16 or fp32, row stride ld_out, aligned to its type. */
+FP8MLP_API int fp8mlp_dequantize_fp4(const uint8_t* codes, int64_t ld_codes, const uint8_t* block_scales, const float* scale,
+                                     int64_t rows, int64_t cols, int fp4_fmt, void* out, int out_dtype, int64_t ld_out,
+                                     void* stream);
+/* Product of two operands of one format, as the 4-bit counterpart of fp8mlp_gemm_fp8:
+ *   out[m, n] = (sum_k A(m, k) B(n, k)) * ((1 / *scale_a) * (1 / *scale_b)),   fp32 accumulation, out bf16 or fp32
+ * A [M, K], B [N, K]: codes and block scales as above; scale_a, scale_b null = 1 (always null for MXFP4).  out: row stride
+ * ld_out >= N elements, aligned to its type, overlaps no operand.  M = 0 or N = 0: nothing to do.  K >= 1, any; M, N, K <= 2^24.
+ * A layer y = x W^T is trained with it as y = Q(x) Q(W)^T, dx = Q(dy) Q(W^T)^T, dW = Q(dy^T) Q(x^T)^T. */
+FP8MLP_API int fp8mlp_gemm_fp4(int64_t M, int64_t N, int64_t K, int fp4_fmt, const uint8_t* A, int64_t ld_a, const uint8_t* a_scales,
+                               const float* scale_a, const uint8_t* B, int64_t ld_b, const uint8_t* b_scales, const float* scale_b,
+                               void* out, int out_dtype, int64_t ld_out, void* stream);
 
 #ifdef __cplusplus
 }

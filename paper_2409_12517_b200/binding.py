@@ -20,11 +20,14 @@ STATIC_SCRATCH_BYTES = 4 * 1024 * 1024
 E4M3, E5M2 = 0, 1
 BF16, F32 = 0, 1
 SMOOTH, SAVE_FOR_BWD, H_BF16, GU_FP8 = 1, 2, 4, 8
-SCALE_GIVEN, SCALE_FROM_CURRENT_AMAX, SCALE_GIVEN_WEIGHTS_CAST = 0, 1, 2
+SCALE_GIVEN, SCALE_FROM_CURRENT_AMAX, SCALE_GIVEN_WEIGHTS_CAST, SCALE_GIVEN_X_CAST, SCALE_GIVEN_BOTH_CAST = 0, 1, 2, 3, 4
 SCORE_SOFTMAX, SCORE_SIGMOID = 0, 1
 NORM_L2, NORM_INF = 0, 1
 MAX_EXPERTS, MAX_TOP_K = 1024, 32
 NORM_WORKSPACE_BYTES = 16384
+RMS_SAME, RMS_E4M3, RMS_E4M3_ROWS = 0, 1, 2
+MAX_NORM_WIDTH, RMS_PARTIALS = 16384, 592
+MXFP4, NVFP4 = 0, 1
 WS_XQ, WS_W12Q, WS_W3Q, WS_HQ, WS_GU, WS_DYQ, WS_DZQ, WS_HB, WS_W3B = range(9)
 
 EXPORTS = [
@@ -36,6 +39,8 @@ EXPORTS = [
     "fp8mlp_selftest_wait_timeout", "fp8mlp_adam_step_cast", "fp8mlp_gemm_plan", "fp8mlp_code_stats",
     "fp8mlp_route", "fp8mlp_route_backward", "fp8mlp_route_update_bias", "fp8mlp_dispatch_plan", "fp8mlp_dispatch",
     "fp8mlp_combine", "fp8mlp_combine_backward", "fp8mlp_grad_norm", "fp8mlp_clip_grads", "fp8mlp_adam_step_scaled",
+    "fp8mlp_rmsnorm", "fp8mlp_rmsnorm_backward", "fp8mlp_fp4_scale_bytes", "fp8mlp_quantize_fp4", "fp8mlp_dequantize_fp4",
+    "fp8mlp_gemm_fp4",
 ]
 PHASES = ["quant_x", "quant_w12", "quant_w3", "gemm1_swiglu", "gemm2_down", "quant_dy", "dgrad2_swiglu_bwd",
           "wgrad3", "dgrad1", "wgrad12", "misc"]
@@ -144,6 +149,13 @@ def lib():
         L.fp8mlp_clip_grads.argtypes = [C.POINTER(_GradTensor), i32, i32, f32, p, p, p]
         L.fp8mlp_adam_step_scaled.argtypes = [C.POINTER(_AdamTensor), C.POINTER(_AdamCast), i32, p, f32, f32, f32, f32,
                                               f32, i64, p]
+        L.fp8mlp_rmsnorm.argtypes = [i64, i64, i32, p, i64, p, i64, p, i64, p, f32, i32, p, i64, p, p, p, p]
+        L.fp8mlp_rmsnorm_backward.argtypes = [i64, i64, i32, p, i64, p, i64, p, p, p, i64, p, i64, p, p, p]
+        L.fp8mlp_fp4_scale_bytes.restype = i64
+        L.fp8mlp_fp4_scale_bytes.argtypes = [i32, i64, i64]
+        L.fp8mlp_quantize_fp4.argtypes = [p, i32, i64, i64, i64, i32, i32, i32, p, p, p, i64, p, p]
+        L.fp8mlp_dequantize_fp4.argtypes = [p, i64, p, p, i64, i64, i32, p, i32, i64, p]
+        L.fp8mlp_gemm_fp4.argtypes = [i64, i64, i64, i32, p, i64, p, p, p, i64, p, p, p, i32, i64, p]
         missing = [name for name in EXPORTS if not hasattr(L, name)]
         if missing:
             raise RuntimeError(f"{LIB_PATH} does not export {missing}")
@@ -515,6 +527,148 @@ def fp8mlp_grad_norm(grads: GradList, norm_kind: int, max_norm: float, norm_coef
 def fp8mlp_clip_grads(grads: GradList, norm_kind: int, max_norm: float, norm_coef, workspace) -> None:
     """fp8mlp_grad_norm, and out = g * coefficient for every tensor of the list."""
     _check(lib().fp8mlp_clip_grads(*_clip_args(grads, norm_kind, max_norm, norm_coef, workspace)), "fp8mlp_clip_grads")
+
+
+# ---------------------------------------------------------------- the norm in front of the block
+
+def _rows_like(t, rows, cols, dtype, what, here):
+    """(pointer, row stride) of a [rows, cols] tensor of one type, or (None, 0)."""
+    if t is None:
+        return None, 0
+    have, ptr, _, ld = _matrix(t, cols, what, here, dtype)
+    if have != rows:
+        raise ValueError(f"{what}: {have} rows, {rows} are needed")
+    return ptr, ld
+
+
+def fp8mlp_rmsnorm(x, residual, gain, eps: float, y, h=None, out: int = RMS_SAME, scale=None, amax=None, rstd=None) -> None:
+    """h = x + residual, y = h / rms(h) * gain.  x, residual, h: [T, d] bf16 or fp32, any row stride; residual, gain (fp32
+    [d]), h, amax (1-element fp32) and rstd (fp32 [T]) may be None; h may be x or residual.  y by `out`: RMS_SAME: [T, d] of
+    x's type; RMS_E4M3: codes (uint8 [T, d], or a device pointer as int, e.g. a context's WS_XQ, with rows of d bytes) of
+    y * scale (1-element fp32, read); RMS_E4M3_ROWS: codes, scale (fp32 [T]) is written."""
+    here = _here()
+    T, d = x.shape
+    x_ptr, ld_x = _rows_like(x, T, d, x.dtype, "x", here)
+    r_ptr, ld_r = _rows_like(residual, T, d, x.dtype, "residual", here)
+    h_ptr, ld_h = _rows_like(h, T, d, x.dtype, "h", here)
+    if out == RMS_SAME:
+        y_ptr, ld_y = _rows_like(y, T, d, x.dtype, "y", here)
+    elif isinstance(y, int):
+        y_ptr, ld_y = y, d
+    else:
+        y_ptr, ld_y = _bytes(y, T, d, "y", here)
+    n_scales = T if out == RMS_E4M3_ROWS else 1
+    _check(lib().fp8mlp_rmsnorm(T, d, _DTYPES[x.dtype], x_ptr, ld_x, r_ptr, ld_r, h_ptr, ld_h,
+                                None if gain is None else _as(gain, _F32, d, "gain", here), eps, out, y_ptr, ld_y,
+                                None if scale is None else _as(scale, _F32, n_scales, "scale", here),
+                                None if amax is None else _as(amax, _F32, 1, "amax", here),
+                                None if rstd is None else _as(rstd, _F32, T, "rstd", here), _stream(here)), "fp8mlp_rmsnorm")
+
+
+def fp8mlp_rmsnorm_backward(dy, h, gain, rstd, dh, dx, d_gain, workspace) -> None:
+    """dx [T, d] (may be dy or dh) and d_gain (fp32 [d], or None) from dy, the stored h and rstd; dh: what reached h along the
+    residual stream, or None; workspace: new_rmsnorm_workspace(d), or None without d_gain."""
+    here = _here()
+    T, d = h.shape
+    h_ptr, ld_h = _rows_like(h, T, d, h.dtype, "h", here)
+    dy_ptr, ld_dy = _rows_like(dy, T, d, h.dtype, "dy", here)
+    dh_ptr, ld_dh = _rows_like(dh, T, d, h.dtype, "dh", here)
+    dx_ptr, ld_dx = _rows_like(dx, T, d, h.dtype, "dx", here)
+    _check(lib().fp8mlp_rmsnorm_backward(T, d, _DTYPES[h.dtype], dy_ptr, ld_dy, h_ptr, ld_h,
+                                         None if gain is None else _as(gain, _F32, d, "gain", here),
+                                         _as(rstd, _F32, T, "rstd", here), dh_ptr, ld_dh, dx_ptr, ld_dx,
+                                         None if d_gain is None else _as(d_gain, _F32, d, "d_gain", here),
+                                         None if workspace is None else _as(workspace, _F32, RMS_PARTIALS * d, "workspace", here),
+                                         _stream(here)), "fp8mlp_rmsnorm_backward")
+
+
+def new_rmsnorm_workspace(d: int, device="cuda"):
+    return torch.empty(RMS_PARTIALS * d, dtype=torch.float32, device=device)
+
+
+# ---------------------------------------------------------------- 4-bit operands
+
+def _bytes(t, rows, cols, what, here):
+    """(pointer, row stride) of a uint8 matrix whose rows are contiguous, at least `cols` long."""
+    shape = t.shape
+    if t.dtype is not _U8 or len(shape) != 2 or shape[0] != rows or shape[1] < cols or t.get_device() != here or t.stride(1) != 1:
+        raise ValueError(f"{what}: a 2-D uint8 CUDA tensor of {rows} rows of {cols} bytes on the current GPU is needed, got "
+                         f"{tuple(shape)} {t.dtype} on {t.device}")
+    ld = t.stride(0)
+    return t.data_ptr(), ld if rows > 1 else max(ld, shape[1])
+
+
+class Fp4Operand:
+    """A [rows, cols] matrix in 4 bits, its columns the contraction of a product: codes (uint8 [rows, at least cols / 2 rounded
+    up to 16]), block scales (uint8, fp8mlp_fp4_scale_bytes) and, for NVFP4, the tensor's scale (1-element fp32, None = 1 in
+    a product)."""
+
+    def __init__(self, fmt: int, rows: int, cols: int, codes, scales, scale=None):
+        self.fmt, self.rows, self.cols, self.codes, self.scales, self.scale = fmt, rows, cols, codes, scales, scale
+        self.code_bytes = (cols + 31) // 32 * 16
+        self.scale_bytes = fp8mlp_fp4_scale_bytes(fmt, rows, cols)
+        self.amax = None
+
+    def pointers(self, what, here):
+        """(codes, their row stride, block scales, scale)"""
+        codes, ld = _bytes(self.codes, self.rows, self.code_bytes, what + " codes", here)
+        return (codes, ld, _as(self.scales, _U8, self.scale_bytes, what + " scales", here),
+                None if self.scale is None else _as(self.scale, _F32, 1, what + " scale", here))
+
+
+def fp8mlp_fp4_scale_bytes(fmt: int, rows: int, cols: int) -> int:
+    return int(lib().fp8mlp_fp4_scale_bytes(fmt, rows, cols))
+
+
+def new_fp4(fmt: int, rows: int, cols: int, scale=None, device="cuda") -> Fp4Operand:
+    """Buffers for a [rows, cols] operand; NVFP4: with the given tensor scale, or one of its own, initialised to 1."""
+    if fmt == NVFP4 and scale is None:
+        scale = torch.ones(1, dtype=torch.float32, device=device)
+    op = Fp4Operand(fmt, rows, cols, torch.empty((rows, (cols + 31) // 32 * 16), dtype=torch.uint8, device=device),
+                    torch.empty(fp8mlp_fp4_scale_bytes(fmt, rows, cols), dtype=torch.uint8, device=device), scale)
+    op.amax = torch.zeros(1, dtype=torch.float32, device=device)
+    return op
+
+
+def fp8mlp_quantize_fp4(src, operand: Fp4Operand, transpose: bool = False, scale_mode: int = SCALE_GIVEN, amax=None) -> None:
+    """src: 2-D bf16 or fp32, any row stride; fills operand (of src, or of its transpose).  SCALE_FROM_CURRENT_AMAX (NVFP4)
+    writes operand.scale first; amax (1-element fp32): receives max |src| (in that mode the operand's own if None)."""
+    here = _here()
+    rows, cols = src.shape
+    _, ptr, dtype, ld = _matrix(src, cols, "src", here)
+    if (operand.rows, operand.cols) != ((cols, rows) if transpose else (rows, cols)):
+        raise ValueError(f"operand: {operand.rows} x {operand.cols}, but src is {rows} x {cols}{' (transposed)' if transpose else ''}")
+    codes, ld_codes, scales, scale = operand.pointers("operand", here)
+    if amax is None and scale_mode == SCALE_FROM_CURRENT_AMAX:
+        amax = operand.amax
+    _check(lib().fp8mlp_quantize_fp4(ptr, dtype, rows, cols, ld, int(transpose), operand.fmt, scale_mode, scale,
+                                     None if amax is None else _as(amax, _F32, 1, "amax", here), codes, ld_codes, scales,
+                                     _stream(here)), "fp8mlp_quantize_fp4")
+
+
+def fp8mlp_dequantize_fp4(operand: Fp4Operand, out) -> None:
+    """out: [rows, cols] bf16 or fp32, any row stride, receives the values that the operand stands for."""
+    here = _here()
+    rows, ptr, dtype, ld = _matrix(out, operand.cols, "out", here)
+    if rows != operand.rows:
+        raise ValueError(f"out: {rows} rows, the operand has {operand.rows}")
+    codes, ld_codes, scales, scale = operand.pointers("operand", here)
+    _check(lib().fp8mlp_dequantize_fp4(codes, ld_codes, scales, scale, rows, operand.cols, operand.fmt, ptr, dtype, ld, _stream(here)),
+           "fp8mlp_dequantize_fp4")
+
+
+def fp8mlp_gemm_fp4(a: Fp4Operand, b: Fp4Operand, out) -> None:
+    """out[m, n] = sum_k a[m, k] b[n, k]; out: [a.rows, b.rows] bf16 or fp32, any row stride."""
+    here = _here()
+    if a.fmt != b.fmt or a.cols != b.cols:
+        raise ValueError(f"operands: formats {a.fmt} and {b.fmt}, contractions {a.cols} and {b.cols}")
+    rows, ptr, dtype, ld = _matrix(out, b.rows, "out", here)
+    if rows != a.rows:
+        raise ValueError(f"out: {rows} rows, the first operand has {a.rows}")
+    a_codes, ld_a, a_scales, a_scale = a.pointers("a", here)
+    b_codes, ld_b, b_scales, b_scale = b.pointers("b", here)
+    _check(lib().fp8mlp_gemm_fp4(a.rows, b.rows, a.cols, a.fmt, a_codes, ld_a, a_scales, a_scale, b_codes, ld_b, b_scales, b_scale,
+                                 ptr, dtype, ld, _stream(here)), "fp8mlp_gemm_fp4")
 
 
 # ---------------------------------------------------------------- conveniences (allocation only)

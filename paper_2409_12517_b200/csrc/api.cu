@@ -37,6 +37,14 @@ __global__ void zero_floats_kernel(ZeroList z) {
         z.vec[i] = 0.0f;
 }
 
+int clear_float(float* p, cudaStream_t st) {
+    ZeroList z{};
+    z.p[0] = p;
+    FP8MLP_CUDA_CHECK(launch_chained(zero_floats_kernel, 1, 32, 0, st, z));
+    FP8MLP_LAUNCH_CHECK();
+    return FP8MLP_OK;
+}
+
 // Self-test of the bounded waits: one thread waits on a barrier that nothing ever completes, with
 // a short limit.  The wait must give up, raise the status word and let the kernel end normally.
 __global__ void wait_selftest_kernel(int* status, uint64_t timeout_ns, int* gave_up) {
@@ -213,17 +221,21 @@ int gemm1_swiglu(fp8mlp_ctx* c, int64_t T, const fp8mlp_scales* s, float* amax_h
     return launch_gemm(EPI_SWIGLU_FWD, false, true, FP8MLP_E4M3, FP8MLP_E4M3, tmA, tmB0, tmB1, a, c->sm_count, st);
 }
 
+// The scale modes of fp8mlp_forward in which the context's FP8 buffers already hold the weights' or x's codes.
+bool weights_are_cast(int mode) { return mode == FP8MLP_SCALE_GIVEN_WEIGHTS_CAST || mode == FP8MLP_SCALE_GIVEN_BOTH_CAST; }
+bool x_is_cast(int mode) { return mode == FP8MLP_SCALE_GIVEN_X_CAST || mode == FP8MLP_SCALE_GIVEN_BOTH_CAST; }
+
 // Everything fp8mlp_forward can refuse before it enqueues anything.
 int check_forward_args(const fp8mlp_ctx* c, int64_t T, const void* x, const float* W1, const float* W2, const float* W3,
                        int mode, const fp8mlp_scales* sc, const fp8mlp_amax* am, const void* y) {
     if (c == nullptr || sc == nullptr) return FP8MLP_ERR_ARG;
-    const bool cast_done = mode == FP8MLP_SCALE_GIVEN_WEIGHTS_CAST;      // the FP8 weight buffers are already filled
+    const bool cast_done = weights_are_cast(mode);
     if (!cast_done && (W1 == nullptr || W2 == nullptr || W3 == nullptr)) return FP8MLP_ERR_ARG;
-    if (mode != FP8MLP_SCALE_GIVEN && mode != FP8MLP_SCALE_FROM_CURRENT_AMAX && !cast_done) return FP8MLP_ERR_ARG;
+    if (mode != FP8MLP_SCALE_GIVEN && mode != FP8MLP_SCALE_FROM_CURRENT_AMAX && !cast_done && !x_is_cast(mode)) return FP8MLP_ERR_ARG;
     if (cast_done && (c->flags & FP8MLP_H_BF16)) return FP8MLP_ERR_ARG;  // that variant keeps W3 in bf16, not as codes
     if (!on_device_of(c)) return FP8MLP_ERR_STATE;
     if (T < 0 || T > c->T_max) return FP8MLP_ERR_SHAPE;
-    if (T > 0 && (x == nullptr || y == nullptr)) return FP8MLP_ERR_ARG;
+    if (T > 0 && ((x == nullptr && !x_is_cast(mode)) || y == nullptr)) return FP8MLP_ERR_ARG;
     if (sc->x == nullptr || sc->w12 == nullptr || sc->w3 == nullptr || sc->h == nullptr) return FP8MLP_ERR_ARG;
     if (mode == FP8MLP_SCALE_FROM_CURRENT_AMAX &&
         (am == nullptr || am->x == nullptr || am->w1 == nullptr || am->w2 == nullptr || am->w3 == nullptr || am->h == nullptr))
@@ -438,14 +450,14 @@ int fp8mlp_update_scales(fp8mlp_ctx* c, const fp8mlp_amax* am, fp8mlp_scales* sc
 int fp8mlp_forward(fp8mlp_ctx* c, int64_t T, const void* x, const float* W1, const float* W2, const float* W3,
                    int mode, fp8mlp_scales* sc, fp8mlp_amax* am, void* y, void* stream) {
     FP8MLP_TRY(check_forward_args(c, T, x, W1, W2, W3, mode, sc, am, y));
-    const bool weights_cast = mode == FP8MLP_SCALE_GIVEN_WEIGHTS_CAST;
-    if (weights_cast) mode = FP8MLP_SCALE_GIVEN;
+    const bool weights_cast = weights_are_cast(mode), x_cast = x_is_cast(mode);
+    if (weights_cast || x_cast) mode = FP8MLP_SCALE_GIVEN;
     const bool gu_fp8 = (c->flags & FP8MLP_GU_FP8) != 0;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const bool smooth = (c->flags & FP8MLP_SMOOTH) != 0;
     const int64_t d = c->d, f = c->f;
     // amax sinks the caller did not provide
-    float* a_x = (am && am->x) ? am->x : c->dummy + 0;
+    float* a_x = (am && am->x && !x_cast) ? am->x : c->dummy + 0;      // x's maximum came with its codes
     float* a_w1 = (am && am->w1) ? am->w1 : c->dummy + 1;
     float* a_w2 = (am && am->w2) ? am->w2 : c->dummy + 2;
     float* a_w3 = (am && am->w3) ? am->w3 : c->dummy + 3;
@@ -459,7 +471,7 @@ int fp8mlp_forward(fp8mlp_ctx* c, int64_t T, const void* x, const float* W1, con
         if (weights_cast) FP8MLP_TRY(zero_floats(c, {a_x, a_gu}, st, a_h, f));     // the weights' maxima came with their codes
         else FP8MLP_TRY(zero_floats(c, {a_x, a_w1, a_w2, a_w3, a_gu}, st, a_h, f));
     }
-    {   // x -> E4M3
+    if (!x_cast) {   // x -> E4M3
         PhaseTimer pt(c, FP8MLP_PH_QUANT_X, st);
         FP8MLP_TRY(quantize_tensor(x, FP8MLP_BF16, T, d, FP8MLP_E4M3, mode, sc->x, a_x, nullptr, nullptr, nullptr, c->xq, d, c->sm_count, st));
     }
@@ -580,23 +592,25 @@ int fp8mlp_merge_weights(fp8mlp_ctx* c, const float* W1, const float* W2, const 
 int fp8mlp_forward_merged(fp8mlp_ctx* c, int64_t T, const void* x, int mode, fp8mlp_scales* sc, fp8mlp_amax* am,
                           void* y, void* stream) {
     if (c == nullptr || sc == nullptr) return FP8MLP_ERR_ARG;
+    const bool x_cast = mode == FP8MLP_SCALE_GIVEN_X_CAST;
+    if (x_cast) mode = FP8MLP_SCALE_GIVEN;
     if (mode != FP8MLP_SCALE_GIVEN && mode != FP8MLP_SCALE_FROM_CURRENT_AMAX) return FP8MLP_ERR_ARG;
     if (T < 0 || T > c->T_max) return FP8MLP_ERR_SHAPE;
     if (!on_device_of(c) || !c->merged) return FP8MLP_ERR_STATE;
-    if (T > 0 && (x == nullptr || y == nullptr)) return FP8MLP_ERR_ARG;
+    if (T > 0 && ((x == nullptr && !x_cast) || y == nullptr)) return FP8MLP_ERR_ARG;
     if (sc->x == nullptr || sc->w12 == nullptr || sc->w3 == nullptr || sc->h == nullptr) return FP8MLP_ERR_ARG;
     if (mode == FP8MLP_SCALE_FROM_CURRENT_AMAX && (am == nullptr || am->x == nullptr || am->h == nullptr)) return FP8MLP_ERR_ARG;
     if (!aligned16(x) || !aligned16(y)) return FP8MLP_ERR_ALIGN;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const int64_t d = c->d, f = c->f;
-    float* a_x = (am && am->x) ? am->x : c->dummy + 0;
+    float* a_x = (am && am->x && !x_cast) ? am->x : c->dummy + 0;
     float* a_h = (am && am->h) ? am->h : nullptr;                // maxima of H only if asked for
     if (T == 0) return FP8MLP_OK;
     {
         PhaseTimer pt(c, FP8MLP_PH_MISC, st);
         FP8MLP_TRY(zero_floats(c, {a_x}, st, a_h, f));
     }
-    {
+    if (!x_cast) {
         PhaseTimer pt(c, FP8MLP_PH_QUANT_X, st);
         FP8MLP_TRY(quantize_tensor(x, FP8MLP_BF16, T, d, FP8MLP_E4M3, mode, sc->x, a_x, nullptr, nullptr, nullptr, c->xq, d, c->sm_count, st));
     }
@@ -759,7 +773,7 @@ int fp8mlp_forward_static(int64_t T, int64_t d, int64_t f, uint32_t flags, const
                           const float* W2, const float* W3, int mode, fp8mlp_scales* sc, fp8mlp_amax* am, void* y,
                           void* stream) {
     if (flags & ~uint32_t(FP8MLP_SMOOTH)) return FP8MLP_ERR_ARG;
-    if (mode == FP8MLP_SCALE_GIVEN_WEIGHTS_CAST) return FP8MLP_ERR_ARG;      // nothing persists in the built-in scratch
+    if (weights_are_cast(mode) || x_is_cast(mode)) return FP8MLP_ERR_ARG;    // nothing persists in the built-in scratch
     if (T < 0 || d <= 0 || f <= 0 || d % 16 != 0 || f % 16 != 0) return FP8MLP_ERR_SHAPE;
     if (T > (1 << 22) || d > (1 << 22) || f > (1 << 22)) return FP8MLP_ERR_TOO_LARGE;
     if (T * d + 3 * d * f + T * f + 8 * f + 4096 > int64_t(FP8MLP_STATIC_SCRATCH_BYTES)) return FP8MLP_ERR_TOO_LARGE;

@@ -14,6 +14,7 @@ namespace fp8mlp {
 void set_cuda_error(const char* what, cudaError_t e);
 void set_cuda_error_str(const char* what, const char* msg);
 void count_launch();
+int clear_float(float* p, cudaStream_t st);      // *p = 0, in the stream's order
 
 #define FP8MLP_CUDA_CHECK(expr)                                   \
     do {                                                          \

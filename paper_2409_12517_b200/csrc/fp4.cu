@@ -1,0 +1,520 @@
+// 4-bit operands: quantisation of a matrix or its transpose into E2M1 codes with block scales, and back.
+//
+// Both directions stream their matrix once.  A block of threads owns 128 rows of the operand, so that it owns whole tiles of
+// block scales (512 bytes each, gathered in shared memory and written in one piece), and a stretch of columns.  The quotient
+// v / scale is taken exactly: a product with the reciprocal, corrected with its remainder (fused multiply-adds), so that the
+// one rounding to E2M1 is right in ties and next to them; MXFP4 scales are powers of two and need none of that.
+#include "common.cuh"
+
+namespace fp8mlp {
+
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kTileRows = 128;            // operand rows of a block of threads, and of a tile of scales
+constexpr int kScaleTile = 512;           // bytes: 128 rows x 4 blocks
+constexpr int kCols = 256;                // operand columns of a block of threads, matrix as it is
+constexpr int kColsT = 128;               // the same for the transposed matrix
+
+template <int FMT> struct Fmt;
+template <> struct Fmt<FP8MLP_MXFP4> { static constexpr int kBlock = 32; };
+template <> struct Fmt<FP8MLP_NVFP4> { static constexpr int kBlock = 16; };
+
+struct QuantArgs {
+    const uint8_t* src;
+    int64_t ld;                           // bytes
+    int64_t rows, cols;                   // of the operand
+    uint8_t *codes, *scales;
+    int64_t ld_codes;
+    const unsigned int* amax_in;          // null: the scale is given
+    unsigned int* amax_out;               // raised to max |src|; null: not wanted
+    float* scale;                         // NVFP4; written where amax_in is given
+    int col_tiles, scale_tiles;           // blocks of threads / tiles of scales along the columns
+};
+
+// place of a block's scale in its tile
+__device__ __forceinline__ int scale_at(int row, int block) { return (row & 31) * 16 + (row >> 5) * 4 + block; }
+
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
+    f32x2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+// eight floats -> eight E2M1 codes, first in the low half of the low byte; nearest, ties to even, saturating
+__device__ __forceinline__ uint32_t cvt_e2m1x8(const float (&v)[8]) {
+    uint32_t r;
+    asm("{\n\t"
+        ".reg .b8 a, b, c, d;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\t"
+        "mov.b32 %0, {a, b, c, d};\n\t"
+        "}\n"
+        : "=r"(r) : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]));
+    return r;
+}
+// two codes (a byte) -> two floats
+__device__ __forceinline__ void e2m1x2_to_f32(uint32_t byte, float& lo, float& hi) {
+    uint32_t h2;
+    asm("{\n\t"
+        ".reg .b8 a, b, c, d;\n\t"
+        "mov.b32 {a, b, c, d}, %1;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %0, a;\n\t"
+        "}\n"
+        : "=r"(h2) : "r"(byte));
+    asm("cvt.f32.f16 %0, %1;" : "=f"(lo) : "h"(static_cast<unsigned short>(h2 & 0xFFFFu)));
+    asm("cvt.f32.f16 %0, %1;" : "=f"(hi) : "h"(static_cast<unsigned short>(h2 >> 16)));
+}
+
+// Largest power of two g with g * amax <= 448 * 6 = 0.65625 * 2^12; 1 for a zero or non-finite amax; within 2^-100 .. 2^100.
+__device__ __forceinline__ float tensor_scale(float amax) {
+    if (!(amax > 0.0f) || isinf(amax)) return 1.0f;
+    int e;
+    const float m = frexpf(amax, &e);
+    const int k = m <= 0.65625f ? 12 - e : 11 - e;
+    return ldexpf(1.0f, max(-100, min(100, k)));
+}
+
+// One block of values (of which those past the matrix are 0) -> its codes, eight to a word, and its scale's byte.
+// `top`: max |src| of the block's bit patterns (a NaN is above infinity there).  g: the tensor's scale (NVFP4).
+template <int FMT>
+__device__ __forceinline__ uint32_t quantise_block(const float (&v)[Fmt<FMT>::kBlock], uint32_t top, float g,
+                                                   uint32_t (&code)[Fmt<FMT>::kBlock / 8]) {
+    constexpr int N = Fmt<FMT>::kBlock;
+    if constexpr (FMT == FP8MLP_MXFP4) {
+        // exponent field of 2^(floor(log2 a) - 2), biased as E8M0; subnormal and zero maxima get the smallest scale
+        uint32_t byte = top >> 23;
+        byte = byte > 2u ? byte - 2u : 0u;
+        const bool finite = top < 0x7f800000u;
+        const float inv = __uint_as_float((254u - byte) << 23);          // 2^(127 - byte): exact products
+#pragma unroll
+        for (int i = 0; i < N / 8; ++i) {
+            float q[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) q[k] = __fmul_rn(v[8 * i + k], inv);
+            code[i] = cvt_e2m1x8(q);
+        }
+        return finite ? byte : 0xffu;
+    } else {
+        const float a = __fmul_rn(__uint_as_float(top), g);
+        const bool finite = __float_as_uint(a) < 0x7f800000u;
+        const uint32_t byte = cvt_fp8x2<FP8MLP_E4M3>(finite ? __fdiv_rn(a, 6.0f) : 0.0f, 0.0f) & 0xffu;
+        float s, unused;
+        e4m3x2_to_f32(byte, s, unused);
+        const float r = s > 0.0f ? __fdiv_rn(1.0f, s) : 0.0f;
+        const f32x2 g2 = pack2(g, g), s2 = pack2(-s, -s), r2 = pack2(r, r);
+#pragma unroll
+        for (int i = 0; i < N / 8; ++i) {
+            float q[8];
+#pragma unroll
+            for (int k = 0; k < 8; k += 2) {
+                const f32x2 x = mul2(pack2(v[8 * i + k], v[8 * i + k + 1]), g2);
+                // x / s rounded once to fp32 (s has four bits, so the remainder is exact).  That is a border between two
+                // codes only if x / s is one: s * border has at most seven bits, so an x next to it is at least one of
+                // its last places off, and x / s more than half a place of the quotient's (1 / 1.875)
+                const f32x2 t = mul2(x, r2);
+                unpack2(fma2(fma2(s2, t, x), r2, t), q[k], q[k + 1]);
+            }
+            code[i] = cvt_e2m1x8(q);
+        }
+        return finite ? byte : 0x7fu;
+    }
+}
+
+template <typename SRC> __device__ __forceinline__ float to_f32(SRC v);
+template <> __device__ __forceinline__ float to_f32<float>(float v) { return v; }
+template <> __device__ __forceinline__ float to_f32<uint16_t>(uint16_t v) { return __uint_as_float(static_cast<uint32_t>(v) << 16); }
+
+__device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7fffffffu; }
+
+// max |src| of a block of threads, NaN left out, raised to *out
+__device__ __forceinline__ void raise_amax(float v, unsigned int* out) {
+    __shared__ float part[kThreads / 32];
+    v = warp_max_nonneg(v);
+    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
+    __syncthreads();
+    if (threadIdx.x < 32) {
+        v = warp_max_nonneg(threadIdx.x < kThreads / 32 ? part[threadIdx.x] : 0.0f);
+        if (threadIdx.x == 0 && v > 0.0f) atomicMax(out, __float_as_uint(v));
+    }
+}
+
+__device__ __forceinline__ float scale_of(const QuantArgs& p) {
+    if (p.amax_in == nullptr) return *p.scale;
+    const float g = tensor_scale(__uint_as_float(__ldcg(p.amax_in)));
+    if (blockIdx.x == 0 && threadIdx.x == 0) *p.scale = g;
+    return g;
+}
+
+// ---------------------------------------------------------------- the matrix as it is
+// A thread takes a block of 16 or 32 columns of a row at a time; neighbours take neighbouring blocks of the row.
+// VEC: rows start on 16-byte boundaries.
+template <typename SRC, int FMT, bool VEC>
+__global__ void __launch_bounds__(kThreads) quantise_kernel(const QuantArgs p) {
+    constexpr int N = Fmt<FMT>::kBlock, kBlocks = kCols / N, kTiles = kBlocks / 4, kItems = kTileRows * kBlocks / kThreads;
+    __shared__ __align__(16) uint8_t scales[kTiles * kScaleTile];
+    const int64_t row_tile = blockIdx.x / p.col_tiles;
+    const int64_t row0 = row_tile * kTileRows, col0 = (blockIdx.x - row_tile * p.col_tiles) * kCols;
+    grid_dependency_wait();
+    grid_launch_dependents();
+    const float g = FMT == FP8MLP_NVFP4 ? scale_of(p) : 1.0f;
+    float seen = 0.0f;
+    const int64_t padded = (p.cols + 31) & ~int64_t(31);          // columns whose codes are written
+#pragma unroll 2
+    for (int it = 0; it < kItems; ++it) {
+        const int item = it * kThreads + threadIdx.x, r = item / kBlocks, b = item % kBlocks;
+        const int64_t row = row0 + r, col = col0 + b * N;
+        float v[N];
+        uint32_t top = 0, byte = 0;
+        if (row < p.rows && col < padded) {
+            const SRC* at = reinterpret_cast<const SRC*>(p.src + row * p.ld) + col;
+            if (VEC && col + N <= p.cols) {
+                constexpr int kWords = N * sizeof(SRC) / 16;
+#pragma unroll
+                for (int i = 0; i < kWords; ++i) {
+                    const uint4 w = ld_global_nc_v4(reinterpret_cast<const uint8_t*>(at) + 16 * i);
+                    const uint32_t words[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        if constexpr (sizeof(SRC) == 4) v[4 * i + k] = __uint_as_float(words[k]);
+                        else { v[8 * i + 2 * k] = bf16_lo(words[k]); v[8 * i + 2 * k + 1] = bf16_hi(words[k]); }
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < N; ++i) v[i] = col + i < p.cols ? to_f32(at[i]) : 0.0f;
+            }
+#pragma unroll
+            for (int i = 0; i < N; ++i) top = max(top, abs_bits(v[i]));
+            if (p.amax_out != nullptr) {
+                if (top <= 0x7f800000u) seen = fmaxf(seen, __uint_as_float(top));
+                else
+#pragma unroll
+                    for (int i = 0; i < N; ++i) seen = fmaxf(seen, fabsf(v[i]));
+            }
+            uint32_t code[N / 8];
+            byte = quantise_block<FMT>(v, top, g, code);
+            if (col >= p.cols) byte = 0;
+            uint8_t* out = p.codes + row * p.ld_codes + col / 2;
+            if constexpr (N == 32) st_global_v4(out, code[0], code[1], code[2], code[3]); else st_global_v2(out, code[0], code[1]);
+        }
+        scales[(b >> 2) * kScaleTile + scale_at(r, b & 3)] = static_cast<uint8_t>(byte);
+    }
+    __syncthreads();
+    const int64_t tile0 = col0 / (4 * N);
+    uint8_t* out = p.scales + (row_tile * p.scale_tiles + tile0) * kScaleTile;
+    const int bytes = static_cast<int>(min(static_cast<int64_t>(kTiles), p.scale_tiles - tile0)) * kScaleTile;
+    for (int i = 16 * threadIdx.x; i < bytes; i += 16 * kThreads) *reinterpret_cast<uint4*>(out + i) = *reinterpret_cast<const uint4*>(scales + i);
+    if (p.amax_out != nullptr) raise_amax(seen, p.amax_out);
+}
+
+// ---------------------------------------------------------------- the transposed matrix
+// Operand rows are the source's columns.  A thread takes two neighbouring columns over 32 source rows (a warp reads 64
+// neighbouring columns of a row at once), which are one or two whole blocks of each; the codes go through shared memory so
+// that they leave in pieces of 64 bytes.  VEC: the two columns can be read at once.
+template <typename SRC, int FMT, bool VEC>
+__global__ void __launch_bounds__(kThreads) quantise_transposed_kernel(const QuantArgs p) {
+    constexpr int N = Fmt<FMT>::kBlock, kTiles = kColsT / (4 * N), kPitch = kColsT / 2 + 16;
+    __shared__ __align__(16) uint8_t scales[kTiles * kScaleTile];
+    __shared__ __align__(16) uint8_t codes[kTileRows * kPitch];
+    const int64_t row_tile = blockIdx.x / p.col_tiles;
+    const int64_t row0 = row_tile * kTileRows, col0 = (blockIdx.x - row_tile * p.col_tiles) * kColsT;
+    grid_dependency_wait();
+    grid_launch_dependents();
+    const float g = FMT == FP8MLP_NVFP4 ? scale_of(p) : 1.0f;
+    float seen = 0.0f;
+    const int pair = 2 * (threadIdx.x & 63), k0 = 32 * (threadIdx.x >> 6);        // operand rows of the tile, source rows
+    float v[2][32];
+    const bool both = row0 + pair + 1 < p.rows;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+        const int64_t k = col0 + k0 + i;
+        v[0][i] = v[1][i] = 0.0f;
+        if (k < p.cols && row0 + pair < p.rows) {
+            const SRC* at = reinterpret_cast<const SRC*>(p.src + k * p.ld) + row0 + pair;
+            if (VEC && both) {
+                if constexpr (sizeof(SRC) == 4) {
+                    const float2 w = __ldg(reinterpret_cast<const float2*>(at));
+                    v[0][i] = w.x; v[1][i] = w.y;
+                } else {
+                    const uint32_t w = __ldg(reinterpret_cast<const uint32_t*>(at));
+                    v[0][i] = bf16_lo(w); v[1][i] = bf16_hi(w);
+                }
+            } else {
+                v[0][i] = to_f32(at[0]);
+                if (both) v[1][i] = to_f32(at[1]);
+            }
+        }
+    }
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+        const int r = pair + c;
+        uint32_t words[4];
+#pragma unroll
+        for (int j = 0; j < 32 / N; ++j) {
+            float block[N];
+            uint32_t top = 0;
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                block[i] = v[c][N * j + i];
+                top = max(top, abs_bits(block[i]));
+            }
+            if (p.amax_out != nullptr)
+#pragma unroll
+                for (int i = 0; i < N; ++i) seen = fmaxf(seen, fabsf(block[i]));
+            uint32_t code[N / 8];
+            uint32_t byte = quantise_block<FMT>(block, top, g, code);
+            if (row0 + r >= p.rows || col0 + k0 + N * j >= p.cols) byte = 0;
+            const int b = k0 / N + j;
+            scales[(b >> 2) * kScaleTile + scale_at(r, b & 3)] = static_cast<uint8_t>(byte);
+#pragma unroll
+            for (int i = 0; i < N / 8; ++i) words[j * (N / 8) + i] = code[i];
+        }
+        *reinterpret_cast<uint4*>(codes + r * kPitch + k0 / 2) = make_uint4(words[0], words[1], words[2], words[3]);
+    }
+    __syncthreads();
+    const int64_t tile0 = col0 / (4 * N);
+    uint8_t* out = p.scales + (row_tile * p.scale_tiles + tile0) * kScaleTile;
+    const int bytes = static_cast<int>(min(static_cast<int64_t>(kTiles), p.scale_tiles - tile0)) * kScaleTile;
+    for (int i = 16 * threadIdx.x; i < bytes; i += 16 * kThreads) *reinterpret_cast<uint4*>(out + i) = *reinterpret_cast<const uint4*>(scales + i);
+    const int64_t padded = (p.cols + 31) & ~int64_t(31);
+    for (int i = threadIdx.x; i < kTileRows * (kColsT / 32); i += kThreads) {
+        const int r = i / (kColsT / 32), c = i % (kColsT / 32);
+        if (row0 + r < p.rows && col0 + 32 * c < padded)
+            *reinterpret_cast<uint4*>(p.codes + (row0 + r) * p.ld_codes + (col0 + 32 * c) / 2) = *reinterpret_cast<const uint4*>(codes + r * kPitch + 16 * c);
+    }
+    if (p.amax_out != nullptr) raise_amax(seen, p.amax_out);
+}
+
+// max |src| over a matrix with a row stride, NaN left out: a block takes 64 rows' worth of 1024 columns
+template <typename SRC, bool VEC>
+__global__ void __launch_bounds__(kThreads) amax_kernel(const uint8_t* src, int64_t ld, int64_t rows, int64_t cols, unsigned int* amax) {
+    constexpr int kPer = 16 / sizeof(SRC);
+    const int64_t units = (cols + kPer - 1) / kPer, all = rows * units;
+    const int64_t step = static_cast<int64_t>(gridDim.x) * kThreads;
+    float seen = 0.0f;
+    grid_dependency_wait();
+    grid_launch_dependents();
+    const bool one_row = VEC && ld == cols * static_cast<int64_t>(sizeof(SRC)) && cols % kPer == 0;       // no division then
+    for (int64_t i0 = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; i0 < all; i0 += 4 * step) {
+        uint4 w[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int64_t i = i0 + k * step;
+            w[k] = make_uint4(0u, 0u, 0u, 0u);
+            if (i >= all) continue;
+            const int64_t row = one_row ? 0 : i / units, unit = one_row ? i : i - row * units;
+            const SRC* at = reinterpret_cast<const SRC*>(src + row * ld) + unit * kPer;
+            if (VEC && (one_row || unit * kPer + kPer <= cols)) {
+                w[k] = ld_global_nc_v4(at);
+            } else {
+                for (int e = 0; e < kPer && unit * kPer + e < cols; ++e) seen = fmaxf(seen, fabsf(to_f32(at[e])));
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const uint32_t words[4] = {w[k].x, w[k].y, w[k].z, w[k].w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if constexpr (sizeof(SRC) == 4) seen = fmaxf(seen, fabsf(__uint_as_float(words[j])));
+                else seen = fmaxf(seen, fmaxf(fabsf(bf16_lo(words[j])), fabsf(bf16_hi(words[j]))));
+            }
+        }
+    }
+    raise_amax(seen, amax);
+}
+
+__global__ void scale_only_kernel(const unsigned int* amax, float* scale) {        // a matrix without elements
+    grid_dependency_wait();
+    grid_launch_dependents();
+    *scale = tensor_scale(__uint_as_float(__ldcg(amax)));
+}
+
+// ---------------------------------------------------------------- back to values
+struct DequantArgs {
+    const uint8_t *codes, *scales;
+    const float* scale;
+    uint8_t* out;
+    int64_t ld_codes, ld_out;             // bytes
+    int64_t rows, cols;
+    int col_tiles, scale_tiles;
+};
+
+// A thread takes 16 columns of a row.  VEC: output rows start on 16-byte boundaries.
+template <typename DST, int FMT, bool VEC>
+__global__ void __launch_bounds__(kThreads) dequantise_kernel(const DequantArgs p) {
+    constexpr int N = Fmt<FMT>::kBlock, kPerRow = kCols / 16, kItems = kTileRows * kPerRow / kThreads;
+    const int64_t row_tile = blockIdx.x / p.col_tiles;
+    const int64_t row0 = row_tile * kTileRows, col0 = (blockIdx.x - row_tile * p.col_tiles) * kCols;
+    grid_dependency_wait();
+    grid_launch_dependents();
+    const float inv_g = p.scale != nullptr ? __fdiv_rn(1.0f, *p.scale) : 1.0f;
+#pragma unroll 4
+    for (int it = 0; it < kItems; ++it) {
+        const int item = it * kThreads + threadIdx.x, r = item / kPerRow;
+        const int64_t row = row0 + r, col = col0 + 16 * (item % kPerRow);
+        if (row >= p.rows || col >= p.cols) continue;
+        const uint2 code = __ldg(reinterpret_cast<const uint2*>(p.codes + row * p.ld_codes + col / 2));
+        const int64_t block = col / N;
+        const uint32_t byte = __ldg(p.scales + (row_tile * p.scale_tiles + block / 4) * kScaleTile +
+                                    scale_at(r, static_cast<int>(block & 3)));
+        float s, unused;
+        if constexpr (FMT == FP8MLP_MXFP4) s = byte == 0xffu ? __uint_as_float(0x7fffffffu) : byte == 0u ? __uint_as_float(0x00400000u) : __uint_as_float(byte << 23);
+        else e4m3x2_to_f32(byte, s, unused);
+        float v[16];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) e2m1x2_to_f32(((i < 4 ? code.x : code.y) >> (8 * (i & 3))) & 0xffu, v[2 * i], v[2 * i + 1]);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            v[i] = __fmul_rn(v[i], s);                       // exact, but for MXFP4 scales at the ends of fp32's range
+            if constexpr (FMT == FP8MLP_NVFP4) v[i] = __fmul_rn(v[i], inv_g);
+        }
+        DST* out = reinterpret_cast<DST*>(p.out + row * p.ld_out) + col;
+        if (VEC && col + 16 <= p.cols) {
+            if constexpr (sizeof(DST) == 4) {
+#pragma unroll
+                for (int i = 0; i < 16; i += 4)
+                    st_global_v4(out + i, __float_as_uint(v[i]), __float_as_uint(v[i + 1]), __float_as_uint(v[i + 2]), __float_as_uint(v[i + 3]));
+            } else {
+#pragma unroll
+                for (int i = 0; i < 16; i += 8)
+                    st_global_v4(out + i, cvt_bf16x2(v[i], v[i + 1]), cvt_bf16x2(v[i + 2], v[i + 3]), cvt_bf16x2(v[i + 4], v[i + 5]), cvt_bf16x2(v[i + 6], v[i + 7]));
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (col + i < p.cols) {
+                    if constexpr (sizeof(DST) == 4) out[i] = v[i];
+                    else out[i] = static_cast<uint16_t>(cvt_bf16x2(v[i], 0.0f) & 0xffffu);
+                }
+        }
+    }
+}
+
+// ---------------------------------------------------------------- host side
+bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+constexpr int64_t kMost = int64_t(1) << 24;      // rows and columns
+
+template <typename SRC, int FMT>
+cudaError_t launch_quantise(const QuantArgs& a, bool transpose, dim3 grid, cudaStream_t st) {
+    if (transpose) {
+        const bool vec = aligned(a.src, 2 * sizeof(SRC)) && a.ld % (2 * sizeof(SRC)) == 0;
+        return vec ? launch_chained(quantise_transposed_kernel<SRC, FMT, true>, grid, dim3(kThreads), 0, st, a)
+                   : launch_chained(quantise_transposed_kernel<SRC, FMT, false>, grid, dim3(kThreads), 0, st, a);
+    }
+    const bool vec = aligned(a.src, 16) && a.ld % 16 == 0;
+    return vec ? launch_chained(quantise_kernel<SRC, FMT, true>, grid, dim3(kThreads), 0, st, a)
+               : launch_chained(quantise_kernel<SRC, FMT, false>, grid, dim3(kThreads), 0, st, a);
+}
+
+template <typename SRC>
+cudaError_t launch_amax(const void* src, int64_t ld, int64_t rows, int64_t cols, unsigned int* amax, int sms, cudaStream_t st) {
+    const int64_t units = rows * ((cols * sizeof(SRC) + 15) / 16), blocks = (units + 4 * kThreads - 1) / (4 * kThreads);
+    const dim3 grid(static_cast<unsigned>(blocks < 8 * sms ? blocks : 8 * sms));
+    const uint8_t* p = static_cast<const uint8_t*>(src);
+    const bool vec = aligned(src, 16) && ld % 16 == 0;
+    return vec ? launch_chained(amax_kernel<SRC, true>, grid, dim3(kThreads), 0, st, p, ld, rows, cols, amax)
+               : launch_chained(amax_kernel<SRC, false>, grid, dim3(kThreads), 0, st, p, ld, rows, cols, amax);
+}
+
+}  // namespace
+}  // namespace fp8mlp
+
+using namespace fp8mlp;
+
+extern "C" int64_t fp8mlp_fp4_scale_bytes(int fmt, int64_t rows, int64_t cols) {
+    if ((fmt != FP8MLP_MXFP4 && fmt != FP8MLP_NVFP4) || rows < 0 || cols < 0 || rows > kMost || cols > kMost) return 0;
+    const int64_t per_tile = 4 * (fmt == FP8MLP_MXFP4 ? 32 : 16);
+    return (rows + kTileRows - 1) / kTileRows * ((cols + per_tile - 1) / per_tile) * kScaleTile;
+}
+
+extern "C" int fp8mlp_quantize_fp4(const void* src, int src_dtype, int64_t rows, int64_t cols, int64_t ld_src, int transpose,
+                                   int fmt, int scale_mode, float* scale, float* amax, uint8_t* codes, int64_t ld_codes,
+                                   uint8_t* block_scales, void* stream) {
+    if (src_dtype != FP8MLP_BF16 && src_dtype != FP8MLP_F32) return FP8MLP_ERR_ARG;
+    if (fmt != FP8MLP_MXFP4 && fmt != FP8MLP_NVFP4) return FP8MLP_ERR_ARG;
+    const bool current = scale_mode == FP8MLP_SCALE_FROM_CURRENT_AMAX;
+    if (scale_mode != FP8MLP_SCALE_GIVEN && !current) return FP8MLP_ERR_ARG;
+    if (fmt == FP8MLP_MXFP4 && (scale != nullptr || current)) return FP8MLP_ERR_ARG;
+    if (fmt == FP8MLP_NVFP4 && scale == nullptr) return FP8MLP_ERR_ARG;
+    if (current && amax == nullptr) return FP8MLP_ERR_ARG;
+    if (rows < 0 || cols < 0 || rows > kMost || cols > kMost || (rows > 1 && ld_src < cols)) return FP8MLP_ERR_SHAPE;
+    const bool t = transpose != 0;
+    const int64_t R = t ? cols : rows, C = t ? rows : cols;                 // of the operand
+    if (ld_codes % 16 != 0 || (R > 0 && ld_codes < (C + 31) / 32 * 16)) return FP8MLP_ERR_SHAPE;
+    const int width = t ? kColsT : kCols;
+    const int64_t tiles = (R + kTileRows - 1) / kTileRows * ((C + width - 1) / width);          // blocks of threads
+    if (tiles > INT32_MAX) return FP8MLP_ERR_SHAPE;
+    if (rows > 0 && cols > 0 && (src == nullptr || codes == nullptr || block_scales == nullptr)) return FP8MLP_ERR_ARG;
+    const int bytes = src_dtype == FP8MLP_F32 ? 4 : 2;
+    if (!aligned(src, bytes) || !aligned(codes, 16) || !aligned(block_scales, 16) || !aligned(scale, 4) || !aligned(amax, 4)) return FP8MLP_ERR_ALIGN;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    int dev = 0, sms = 0;
+    FP8MLP_CUDA_CHECK(cudaGetDevice(&dev));
+    FP8MLP_CUDA_CHECK(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+    if (amax != nullptr)
+        if (int rc = clear_float(amax, st)) return rc;
+    unsigned int* amax_bits = reinterpret_cast<unsigned int*>(amax);
+    if (rows == 0 || cols == 0) {
+        if (current) {
+            FP8MLP_CUDA_CHECK(launch_chained(scale_only_kernel, dim3(1), dim3(1), 0, st, static_cast<const unsigned int*>(amax_bits), scale));
+            count_launch();
+        }
+        return FP8MLP_OK;
+    }
+    const int64_t ld = ld_src * bytes;
+    if (current) {
+        FP8MLP_CUDA_CHECK(src_dtype == FP8MLP_F32 ? launch_amax<float>(src, ld, rows, cols, amax_bits, sms, st)
+                                                  : launch_amax<uint16_t>(src, ld, rows, cols, amax_bits, sms, st));
+        count_launch();
+    }
+    QuantArgs a{};
+    a.src = static_cast<const uint8_t*>(src); a.ld = ld; a.rows = R; a.cols = C;
+    a.codes = codes; a.scales = block_scales; a.ld_codes = ld_codes; a.scale = scale;
+    a.amax_in = current ? amax_bits : nullptr;
+    a.amax_out = current ? nullptr : amax_bits;
+    const int per_tile = 4 * (fmt == FP8MLP_MXFP4 ? 32 : 16);
+    a.scale_tiles = static_cast<int>((C + per_tile - 1) / per_tile);
+    a.col_tiles = static_cast<int>((C + width - 1) / width);
+    const dim3 grid(static_cast<unsigned>(tiles));
+    const bool f32 = src_dtype == FP8MLP_F32;
+    const cudaError_t e = fmt == FP8MLP_MXFP4 ? (f32 ? launch_quantise<float, FP8MLP_MXFP4>(a, t, grid, st) : launch_quantise<uint16_t, FP8MLP_MXFP4>(a, t, grid, st))
+                                              : (f32 ? launch_quantise<float, FP8MLP_NVFP4>(a, t, grid, st) : launch_quantise<uint16_t, FP8MLP_NVFP4>(a, t, grid, st));
+    FP8MLP_CUDA_CHECK(e);
+    count_launch();
+    return FP8MLP_OK;
+}
+
+extern "C" int fp8mlp_dequantize_fp4(const uint8_t* codes, int64_t ld_codes, const uint8_t* block_scales, const float* scale,
+                                     int64_t rows, int64_t cols, int fmt, void* out, int out_dtype, int64_t ld_out, void* stream) {
+    if (out_dtype != FP8MLP_BF16 && out_dtype != FP8MLP_F32) return FP8MLP_ERR_ARG;
+    if (fmt != FP8MLP_MXFP4 && fmt != FP8MLP_NVFP4) return FP8MLP_ERR_ARG;
+    if (fmt == FP8MLP_MXFP4 && scale != nullptr) return FP8MLP_ERR_ARG;
+    if (rows < 0 || cols < 0 || rows > kMost || cols > kMost || (rows > 1 && ld_out < cols)) return FP8MLP_ERR_SHAPE;
+    if (ld_codes % 16 != 0 || (rows > 0 && ld_codes < (cols + 31) / 32 * 16)) return FP8MLP_ERR_SHAPE;
+    const int64_t tiles = (rows + kTileRows - 1) / kTileRows * ((cols + kCols - 1) / kCols);
+    if (tiles > INT32_MAX) return FP8MLP_ERR_SHAPE;
+    if (rows > 0 && cols > 0 && (codes == nullptr || block_scales == nullptr || out == nullptr)) return FP8MLP_ERR_ARG;
+    const int bytes = out_dtype == FP8MLP_F32 ? 4 : 2;
+    if (!aligned(codes, 16) || !aligned(block_scales, 16) || !aligned(scale, 4) || !aligned(out, bytes)) return FP8MLP_ERR_ALIGN;
+    if (rows == 0 || cols == 0) return FP8MLP_OK;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    DequantArgs a{};
+    a.codes = codes; a.scales = block_scales; a.scale = scale; a.out = static_cast<uint8_t*>(out);
+    a.ld_codes = ld_codes; a.ld_out = ld_out * bytes; a.rows = rows; a.cols = cols;
+    const int per_tile = 4 * (fmt == FP8MLP_MXFP4 ? 32 : 16);
+    a.scale_tiles = static_cast<int>((cols + per_tile - 1) / per_tile);
+    a.col_tiles = static_cast<int>((cols + kCols - 1) / kCols);
+    const dim3 grid(static_cast<unsigned>(tiles));
+    const bool vec = aligned(out, 16) && a.ld_out % 16 == 0;
+#define FP8MLP_DEQUANT(D, F) (vec ? launch_chained(dequantise_kernel<D, F, true>, grid, dim3(kThreads), 0, st, a) \
+                                  : launch_chained(dequantise_kernel<D, F, false>, grid, dim3(kThreads), 0, st, a))
+    const bool f32 = out_dtype == FP8MLP_F32;
+    const cudaError_t e = fmt == FP8MLP_MXFP4 ? (f32 ? FP8MLP_DEQUANT(float, FP8MLP_MXFP4) : FP8MLP_DEQUANT(uint16_t, FP8MLP_MXFP4))
+                                              : (f32 ? FP8MLP_DEQUANT(float, FP8MLP_NVFP4) : FP8MLP_DEQUANT(uint16_t, FP8MLP_NVFP4));
+#undef FP8MLP_DEQUANT
+    FP8MLP_CUDA_CHECK(e);
+    count_launch();
+    return FP8MLP_OK;
+}

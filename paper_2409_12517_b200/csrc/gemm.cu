@@ -1088,6 +1088,24 @@ int make_tmap_out_f32(CUtensorMap* map, const void* base, uint64_t cols, uint64_
     return FP8MLP_OK;
 }
 
+int make_tmap_bytes(CUtensorMap* map, const void* base, uint64_t inner, uint64_t outer, uint64_t row_stride, uint32_t box_rows,
+                    bool swizzle) {
+    EncodeTiledFn fn = encode_fn();
+    if (fn == nullptr) return FP8MLP_ERR_CUDA;
+    const cuuint64_t dims[2] = {inner, outer};
+    const cuuint64_t strides[1] = {row_stride};
+    const cuuint32_t box[2] = {128, box_rows};
+    const cuuint32_t elem[2] = {1, 1};
+    CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, elem,
+                    CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE,
+                    CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) {
+        set_cuda_error_str("cuTensorMapEncodeTiled", "driver rejected the tensor map of a 4-bit operand");
+        return FP8MLP_ERR_CUDA;
+    }
+    return FP8MLP_OK;
+}
+
 int make_tmap_u8(CUtensorMap* map, const void* base, uint64_t inner, uint64_t outer, uint64_t row_stride) {
     return make_tmap(map, base, 1, false, inner, outer, row_stride);
 }

@@ -103,6 +103,9 @@ int make_tmap_u8(CUtensorMap* map, const void* base, uint64_t inner, uint64_t ou
 // the GEMM will read the matrix (an MN-major 16-bit operand is fetched in boxes of 64 K-rows).
 int make_tmap(CUtensorMap* map, const void* base, int elem_bytes, bool mn_major, uint64_t inner, uint64_t outer,
               uint64_t row_stride_bytes);
+// A matrix of bytes in boxes of 128 bytes x box_rows rows, with the 128-byte swizzle or without one; zero fill out of bounds.
+int make_tmap_bytes(CUtensorMap* map, const void* base, uint64_t inner, uint64_t outer, uint64_t row_stride, uint32_t box_rows,
+                    bool swizzle);
 
 // Tensor map of the saved activations for the backward epilogue's ring: boxes of 64 bytes x 128 rows, 64-byte swizzle.
 int make_tmap_ring(CUtensorMap* map, const void* base, int elem_bytes, uint64_t inner, uint64_t outer, uint64_t row_stride_bytes);

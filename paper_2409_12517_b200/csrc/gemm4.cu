@@ -1,0 +1,540 @@
+// Product of two 4-bit operands with block scales: tcgen05.mma kind::mxf4 / kind::mxf4nvf4 on operands streamed by TMA, block
+// scales brought from shared into tensor memory next to the accumulators, fp32 accumulation.
+//
+//   D[p, q] = sum_k P(p, k) Q(q, k)          P: the operand whose rows are the accumulator's rows (128 per CTA)
+//
+// P is A and Q is B, or the other way round where A has few rows: a product of one token with a large weight matrix is bound by
+// reading the weights, so their rows fill the 128 accumulator rows and the tokens are its 16 to 128 columns.
+//
+// A CTA is one TMA warp, one warp that issues the MMAs and 4 or 8 epilogue warps; two accumulators alternate, so that the
+// epilogue of a tile overlaps the main loop of the next.  A stage holds 256 columns of the contraction: 128 bytes of codes a
+// row, and the scales' tiles of 512 bytes as they lie in memory (32 rows of 16 bytes), which tcgen05.cp copies to the four lane
+// quadrants of 4 tensor-memory columns.  The scales of two stages alternate in tensor memory: those of stage i are copied once
+// the MMAs of stage i - 2 are done.
+//
+// Large products: CTA pairs on 256 x 192 tiles (cta_group::2; each CTA loads its 128 rows of P, half of the rows of Q, and the
+// scales of all of Q).  Products with fewer tiles than SMs: single CTAs on 128 x 16 .. 128 tiles, the contraction cut among
+// the 2, 4 or 8 CTAs of a cluster, which add their partial tiles over distributed shared memory in the order of their ranks.
+// Every wait is bounded.
+#include "gemm.cuh"
+
+#include <mutex>
+
+namespace fp8mlp {
+
+namespace {
+
+constexpr int kRows = 128;                   // accumulator rows of a CTA
+constexpr int kStageK = 256;                 // columns of the contraction per stage
+constexpr int kStepK = 64;                   // and per MMA
+constexpr int kScaleTile = 512;              // 128 rows x 4 blocks
+
+struct Gemm4Args {
+    int P, Q, K;
+    int p_tiles, q_tiles, stages_k;          // stages_k: stages of the whole contraction
+    int p_scale_tiles, q_scale_tiles;        // scale tiles of a row group
+    int split;                               // CTAs of a cluster that share a tile's contraction (at most stages_k)
+    int group;                               // rasterisation: bands of this many p tiles
+    int swap;                                // out is [Q, P]
+    int f32, vec;                            // fp32 output; bytes that its rows are aligned to (32, 16 or less)
+    const float *s0, *s1;
+    uint8_t* out;
+    int64_t ld_out;                          // elements
+};
+
+template <int FMT, int TN, bool PAIR> struct Shape {
+    static constexpr int kBlock = FMT == FP8MLP_MXFP4 ? 32 : 16;
+    static constexpr int kTiles = kStageK / (4 * kBlock);                 // scale tiles of a stage, per 128 rows
+    static constexpr int kQGroups = (TN + 127) / 128;                     // 128-row groups of scales that a tile of Q touches
+    static constexpr int kPBytes = kRows * 128, kQBytes = (PAIR ? TN / 2 : TN) * 128;
+    static constexpr int kSfBytes = kTiles * kScaleTile;                  // per 128 rows
+    static constexpr int kStageBytes = kPBytes + kQBytes + (1 + kQGroups) * kSfBytes;
+    static constexpr int kStages = PAIR ? 6 : TN == 128 ? 5 : TN == 64 ? 3 : 4;
+    static constexpr int kEpiWarps = TN >= 64 ? 8 : 4;
+    static constexpr int kThreads = 64 + 32 * kEpiWarps;
+    static constexpr int kWarpCols = TN / (kEpiWarps / 4);                // columns of a tile that an epilogue warp drains
+    static constexpr int kSfCols = 4 * kTiles * (1 + kQGroups);           // tensor-memory columns of a stage's scales
+    static constexpr int kCols = 2 * TN + 2 * kSfCols;
+    static constexpr int kTmem = kCols <= 128 ? 128 : kCols <= 256 ? 256 : 512;
+    static constexpr int kCtasPerSm = TN <= 64 ? 2 : 1;
+    static_assert(kCols <= 512 && kTmem * kCtasPerSm <= 512, "tensor memory");
+};
+
+struct __align__(8) Tail4 {
+    uint64_t full[6], empty[6], tmem_full[2], tmem_empty[2];
+    uint32_t tmem_base;
+    int abort;
+};
+
+template <int FMT, int TN, bool PAIR>
+constexpr size_t smem4_bytes() {
+    return 1024 + size_t(Shape<FMT, TN, PAIR>::kStages) * Shape<FMT, TN, PAIR>::kStageBytes + sizeof(Tail4);
+}
+static_assert(smem4_bytes<FP8MLP_NVFP4, 192, true>() <= 232448 && smem4_bytes<FP8MLP_NVFP4, 128, false>() <= 232448, "shared memory");
+static_assert(2 * (smem4_bytes<FP8MLP_NVFP4, 64, false>() + 1024) <= 233472 && 2 * (smem4_bytes<FP8MLP_NVFP4, 32, false>() + 1024) <= 233472,
+              "two CTAs of the narrow tiles share an SM");
+
+// Operand rows of 128 bytes with the 128-byte swizzle: 8-row groups 1024 bytes apart.
+__device__ __forceinline__ uint64_t operand_desc(uint32_t addr) {
+    return static_cast<uint64_t>((addr & 0x3FFFFu) >> 4) | (1ull << 16) | (uint64_t(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
+}
+// A tile of scales, 32 rows of 16 bytes one after the other, no swizzle: 8-row groups 128 bytes apart.
+__device__ __forceinline__ uint64_t scales_desc(uint32_t addr) {
+    return static_cast<uint64_t>((addr & 0x3FFFFu) >> 4) | (1ull << 16) | (uint64_t(128 >> 4) << 32) | (1ull << 46);
+}
+// 512 bytes of scales -> 4 columns of tensor memory, the same in each quadrant of 32 lanes
+template <bool PAIR>
+__device__ __forceinline__ void copy_scales(uint32_t tmem, uint64_t desc) {
+    if constexpr (PAIR) asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
+    else asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
+}
+template <int FMT, bool PAIR>
+__device__ __forceinline__ void umma_f4(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sf_a, uint32_t sf_b, uint32_t accumulate) {
+#define FP8MLP_UMMA4(GROUP, KIND, VEC)                                                                             \
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"                                                  \
+                 "tcgen05.mma.cta_group::" GROUP ".kind::" KIND ".block_scale.scale_vec::" VEC " [%0], %1, %2, %3, [%4], [%5], p;\n\t}\n" \
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sf_a), "r"(sf_b), "r"(accumulate) : "memory")
+    if constexpr (FMT == FP8MLP_MXFP4) {
+        if constexpr (PAIR) FP8MLP_UMMA4("2", "mxf4", "2X"); else FP8MLP_UMMA4("1", "mxf4", "2X");
+    } else {
+        if constexpr (PAIR) FP8MLP_UMMA4("2", "mxf4nvf4", "4X"); else FP8MLP_UMMA4("1", "mxf4nvf4", "4X");
+    }
+#undef FP8MLP_UMMA4
+}
+// Instruction descriptor: [7,10) and [10,12) element types (E2M1 = 1); [17,23) N >> 3; bit 23 scale type (E4M3 = 0, E8M0 = 1);
+// [24,29) M >> 4; [29,31) and [4,6): byte of the 32-bit tensor-memory cell where A's and B's scales begin.
+template <int FMT, int TN, bool PAIR>
+__device__ __forceinline__ uint32_t idesc4(uint32_t sf_byte) {
+    return (sf_byte << 4) | (1u << 7) | (1u << 10) | (uint32_t(TN >> 3) << 17) | (uint32_t(FMT == FP8MLP_MXFP4 ? 1 : 0) << 23) |
+           (uint32_t((PAIR ? 256 : 128) >> 4) << 24) | (sf_byte << 29);
+}
+
+__device__ __forceinline__ void tile4_coords(const Gemm4Args& p, int tile, int& p_tile, int& q_tile) {
+    const int per_band = p.group * p.q_tiles, band = tile / per_band, first = band * p.group;
+    const int rows = min(p.p_tiles - first, p.group), in_band = tile - band * per_band;
+    p_tile = first + in_band % rows;
+    q_tile = in_band / rows;
+}
+
+template <int N>
+__device__ __forceinline__ void tmem_ld_cols(uint32_t taddr, uint32_t (&r)[N]) {
+    if constexpr (N == 32) {
+        tmem_ld32(taddr, r);
+    } else {
+        static_assert(N == 16, "16 or 32 columns");
+        asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+                     : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+                       "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+                     : "r"(taddr) : "memory");
+    }
+}
+
+__device__ __forceinline__ void store_one(const Gemm4Args& p, int64_t at, float v) {
+    if (p.f32) reinterpret_cast<float*>(p.out)[at] = v;
+    else reinterpret_cast<uint16_t*>(p.out)[at] = static_cast<uint16_t>(cvt_bf16x2(v, 0.0f) & 0xffffu);
+}
+
+// N neighbouring outputs of a row, `have` of them inside the matrix
+template <int N>
+__device__ __forceinline__ void store_cols(const Gemm4Args& p, int64_t at, const float (&v)[N], int have) {
+    if (have < N || p.vec < 16) {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (i < have) store_one(p, at + i, v[i]);
+        return;
+    }
+    if (p.f32) {
+        float* dst = reinterpret_cast<float*>(p.out) + at;
+#pragma unroll
+        for (int i = 0; i < N; i += 8) {
+            uint32_t w[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) w[k] = __float_as_uint(v[i + k]);
+            if (p.vec >= 32) {
+                st_global_v8(dst + i, w);
+            } else {
+                st_global_v4(dst + i, w[0], w[1], w[2], w[3]);
+                st_global_v4(dst + i + 4, w[4], w[5], w[6], w[7]);
+            }
+        }
+    } else {
+        uint16_t* dst = reinterpret_cast<uint16_t*>(p.out) + at;
+#pragma unroll
+        for (int i = 0; i < N; i += 16) {
+            uint32_t w[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) w[k] = cvt_bf16x2(v[i + 2 * k], v[i + 2 * k + 1]);
+            if (p.vec >= 32) {
+                st_global_v8(dst + i, w);
+            } else {
+                st_global_v4(dst + i, w[0], w[1], w[2], w[3]);
+                st_global_v4(dst + i + 8, w[4], w[5], w[6], w[7]);
+            }
+        }
+    }
+}
+
+template <int FMT, int TN, bool PAIR>
+__global__ void __launch_bounds__(Shape<FMT, TN, PAIR>::kThreads, Shape<FMT, TN, PAIR>::kCtasPerSm)
+gemm4_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_constant__ CUtensorMap tmQ,
+             const __grid_constant__ CUtensorMap tmSfP, const __grid_constant__ CUtensorMap tmSfQ, const Gemm4Args p) {
+    using S = Shape<FMT, TN, PAIR>;
+    constexpr int kStages = S::kStages, kStageBytes = S::kStageBytes;
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t raw_addr = smem_u32(smem_raw);
+    const uint32_t tiles_addr = (raw_addr + 1023u) & ~1023u;
+    Tail4* tail = reinterpret_cast<Tail4*>(smem_raw + (tiles_addr - raw_addr) + size_t(kStages) * kStageBytes);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = (PAIR || p.split > 1) ? cluster_ctarank() : 0u;
+    const int ctas = PAIR ? 2 : p.split;                             // per tile
+    const int first_tile = static_cast<int>(blockIdx.x) / ctas, tile_step = static_cast<int>(gridDim.x) / ctas;
+    const int num_tiles = p.p_tiles * p.q_tiles;
+    // a cluster that splits the contraction has one tile, and this CTA these stages of it
+    const int kb_begin = p.split > 1 ? static_cast<int>(rank) * p.stages_k / p.split : 0;
+    const int kb_end = p.split > 1 ? (static_cast<int>(rank) + 1) * p.stages_k / p.split : p.stages_k;
+    volatile int* abort_flag = &tail->abort;
+
+    if (threadIdx.x == 0) {
+        tma_prefetch_desc(&tmP);
+        tma_prefetch_desc(&tmQ);
+        tma_prefetch_desc(&tmSfP);
+        tma_prefetch_desc(&tmSfQ);
+        for (int s = 0; s < kStages; ++s) {
+            mbar_init(smem_u32(&tail->full[s]), 1);
+            mbar_init(smem_u32(&tail->empty[s]), 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(smem_u32(&tail->tmem_full[b]), 1);
+            mbar_init(smem_u32(&tail->tmem_empty[b]), (PAIR ? 2 : 1) * S::kEpiWarps);
+        }
+        tail->abort = 0;
+        mbar_init_fence();
+    }
+    if (warp == 1) {
+        if constexpr (PAIR) { tmem_alloc_pair(smem_u32(&tail->tmem_base), S::kTmem); tmem_relinquish_pair(); }
+        else { tmem_alloc(smem_u32(&tail->tmem_base), S::kTmem); tmem_relinquish(); }
+    }
+    tc_fence_before();
+    if constexpr (PAIR) cluster_sync_all(); else __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem_base = tail->tmem_base;
+    grid_dependency_wait();
+    grid_launch_dependents();
+
+    if (warp == 0) {
+        // ------------------------------------------------------------ TMA producer
+        if (lane == 0) {
+            uint32_t stage = 0, phase = 0;
+            bool ok = true;
+            for (int tile = first_tile; ok && tile < num_tiles; tile += tile_step) {
+                int p_tile, q_tile;
+                tile4_coords(p, tile, p_tile, q_tile);
+                const int p_group = PAIR ? 2 * p_tile + static_cast<int>(rank) : p_tile, p0 = p_group * kRows;
+                const int q0 = q_tile * TN, q_first = q0 + (PAIR ? static_cast<int>(rank) * (TN / 2) : 0), q_group = q0 / kRows;
+                for (int kb = kb_begin; kb < kb_end; ++kb) {
+                    if (!mbar_wait(smem_u32(&tail->empty[stage]), phase ^ 1u, abort_flag, nullptr)) { ok = false; break; }
+                    const uint32_t dst = tiles_addr + stage * kStageBytes, sf = dst + S::kPBytes + S::kQBytes;
+                    const uint32_t own = smem_u32(&tail->full[stage]);
+                    const uint32_t bar = PAIR ? mapa_shared(own, 0) : own;         // a pair's bytes are counted by rank 0
+                    if (!PAIR || rank == 0) mbar_expect_tx(own, (PAIR ? 2 : 1) * kStageBytes);
+                    auto load = [&](uint32_t to, const CUtensorMap* map, int x, int y) {
+                        if constexpr (PAIR) tma_load_2d_pair(to, map, bar, x, y); else tma_load_2d(to, map, bar, x, y);
+                    };
+                    load(dst, &tmP, kb * (kStageK / 2), p0);
+                    load(dst + S::kPBytes, &tmQ, kb * (kStageK / 2), q_first);
+                    // a tile of scales is 4 rows of 128 bytes of its map; a last stage may read tiles of the next row group,
+                    // which no MMA uses
+                    load(sf, &tmSfP, 0, (p_group * p.p_scale_tiles + kb * S::kTiles) * 4);
+#pragma unroll
+                    for (int j = 0; j < S::kQGroups; ++j)
+                        load(sf + (1 + j) * S::kSfBytes, &tmSfQ, 0, ((q_group + j) * p.q_scale_tiles + kb * S::kTiles) * 4);
+                    if (++stage == kStages) { stage = 0; phase ^= 1u; }
+                }
+            }
+        }
+    } else if (warp == 1) {
+        // ------------------------------------------------------------ MMA issuer (CTA pair: rank 0 only)
+        if (lane == 0 && rank * (PAIR ? 1u : 0u) == 0u) {
+            uint32_t stage = 0, phase = 0, count = 0;
+            bool ok = true;
+            int it = 0;
+            for (int tile = first_tile; ok && tile < num_tiles; tile += tile_step, ++it) {
+                int p_tile, q_tile;
+                tile4_coords(p, tile, p_tile, q_tile);
+                const uint32_t acc = it & 1, acc_phase = (it >> 1) & 1;
+                if (!mbar_wait(smem_u32(&tail->tmem_empty[acc]), acc_phase ^ 1u, abort_flag, nullptr)) break;
+                tc_fence_after();
+                const uint32_t d_tmem = tmem_base + acc * TN;
+                const uint32_t q_offset = static_cast<uint32_t>((q_tile * TN) % kRows) / 32u;     // first column of the tile's scales
+                for (int kb = kb_begin; kb < kb_end; ++kb, ++count) {
+                    if (!mbar_wait(smem_u32(&tail->full[stage]), phase, abort_flag, nullptr)) { ok = false; break; }
+                    if (count >= 2) {        // the scales' columns: free once the MMAs of two stages ago are done
+                        const uint32_t before = stage >= 2 ? stage - 2 : stage + kStages - 2;
+                        const uint32_t parity = ((count - 2) / kStages) & 1u;
+                        if (!mbar_wait(smem_u32(&tail->empty[before]), parity, abort_flag, nullptr)) { ok = false; break; }
+                    }
+                    tc_fence_after();
+                    const uint32_t p_addr = tiles_addr + stage * kStageBytes, q_addr = p_addr + S::kPBytes, sf_addr = q_addr + S::kQBytes;
+                    const uint32_t sf_p = tmem_base + 2 * TN + (count & 1u) * S::kSfCols, sf_q = sf_p + 4 * S::kTiles;
+                    const int left = p.K - kb * kStageK;
+#pragma unroll
+                    for (int t = 0; t < S::kTiles; ++t) {
+                        if (t * 4 * S::kBlock >= left) break;
+                        copy_scales<PAIR>(sf_p + 4 * t, scales_desc(sf_addr + t * kScaleTile));
+#pragma unroll
+                        for (int j = 0; j < S::kQGroups; ++j)
+                            copy_scales<PAIR>(sf_q + 4 * (t * S::kQGroups + j), scales_desc(sf_addr + (1 + j) * S::kSfBytes + t * kScaleTile));
+                    }
+#pragma unroll
+                    for (int k = 0; k < kStageK / kStepK; ++k) {
+                        if (k * kStepK >= left) break;
+                        // a cell of four scales is 64 columns of NVFP4, and 128 of MXFP4, which take it in two halves
+                        const int t = FMT == FP8MLP_MXFP4 ? k / 2 : k;
+                        const uint32_t byte = FMT == FP8MLP_MXFP4 ? 2u * (k & 1) : 0u;
+                        umma_f4<FMT, PAIR>(d_tmem, operand_desc(p_addr + 32 * k), operand_desc(q_addr + 32 * k), idesc4<FMT, TN, PAIR>(byte),
+                                           sf_p + 4 * t, sf_q + 4 * t * S::kQGroups + q_offset, (kb != kb_begin || k != 0) ? 1u : 0u);
+                    }
+                    if constexpr (PAIR) umma_commit_pair(smem_u32(&tail->empty[stage])); else umma_commit(smem_u32(&tail->empty[stage]));
+                    if (++stage == kStages) { stage = 0; phase ^= 1u; }
+                }
+                if (ok) {
+                    if constexpr (PAIR) umma_commit_pair(smem_u32(&tail->tmem_full[acc])); else umma_commit(smem_u32(&tail->tmem_full[acc]));
+                }
+            }
+        }
+    } else {
+        // ------------------------------------------------------------ epilogue
+        const int quad = warp & 3, part = (warp - 2) >> 2;
+        const float dq = __fmul_rn(p.s0 != nullptr ? __fdiv_rn(1.0f, *p.s0) : 1.0f, p.s1 != nullptr ? __fdiv_rn(1.0f, *p.s1) : 1.0f);
+        constexpr int kChunk = S::kWarpCols < 32 ? 16 : 32;
+        int it = 0;
+        for (int tile = first_tile; tile < num_tiles; tile += tile_step, ++it) {
+            int p_tile, q_tile;
+            tile4_coords(p, tile, p_tile, q_tile);
+            const uint32_t acc = it & 1, acc_phase = (it >> 1) & 1;
+            const bool got = mbar_wait(smem_u32(&tail->tmem_full[acc]), acc_phase, abort_flag, nullptr);
+            if (!__all_sync(0xffffffffu, got)) break;
+            tc_fence_after();
+            const uint32_t taddr = tmem_base + acc * TN + part * S::kWarpCols + (static_cast<uint32_t>(quad * 32) << 16);
+            const int row = (PAIR ? 2 * p_tile + static_cast<int>(rank) : p_tile) * kRows + quad * 32 + lane;
+            const int col0 = q_tile * TN + part * S::kWarpCols;
+#pragma unroll 1
+            for (int c = 0; c < S::kWarpCols; c += kChunk) {
+                if (col0 + c >= p.Q) break;
+                uint32_t r[kChunk];
+                tmem_ld_cols<kChunk>(taddr + c, r);
+                tmem_ld_wait();
+                if (p.split > 1) {
+                    // this share of the tile into shared memory, [column][row]; every operand stage has been read
+                    float* mine = reinterpret_cast<float*>(smem_raw + (tiles_addr - raw_addr)) + (part * S::kWarpCols + c) * kRows + quad * 32 + lane;
+#pragma unroll
+                    for (int i = 0; i < kChunk; ++i) mine[i * kRows] = __uint_as_float(r[i]);
+                    continue;
+                }
+                if (row >= p.P) continue;
+                float v[kChunk];
+#pragma unroll
+                for (int i = 0; i < kChunk; ++i) v[i] = __fmul_rn(__uint_as_float(r[i]), dq);
+                if (p.swap) {
+#pragma unroll
+                    for (int i = 0; i < kChunk; ++i)
+                        if (col0 + c + i < p.Q) store_one(p, static_cast<int64_t>(col0 + c + i) * p.ld_out + row, v[i]);
+                } else {
+                    store_cols<kChunk>(p, static_cast<int64_t>(row) * p.ld_out + col0 + c, v, p.Q - (col0 + c));
+                }
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) {
+                if constexpr (PAIR) mbar_arrive_cluster(mapa_shared(smem_u32(&tail->tmem_empty[acc]), 0));
+                else mbar_arrive(smem_u32(&tail->tmem_empty[acc]));
+            }
+        }
+    }
+
+    // ---------------------------------------------------------------- teardown
+    tc_fence_before();
+    __syncthreads();
+    if (*abort_flag) {
+        for (int i = 0; i < 200; ++i) __nanosleep(1000);      // copies in flight land before shared memory is released
+        __syncthreads();
+    }
+    if (!PAIR && p.split > 1) {
+        cluster_sync_all();                                   // all shares of the tile lie in their CTAs' shared memory
+        const float dq = __fmul_rn(p.s0 != nullptr ? __fdiv_rn(1.0f, *p.s0) : 1.0f, p.s1 != nullptr ? __fdiv_rn(1.0f, *p.s1) : 1.0f);
+        int p_tile, q_tile;
+        tile4_coords(p, first_tile, p_tile, q_tile);
+        const int cols = min(TN, p.Q - q_tile * TN), rows = min(kRows, p.P - p_tile * kRows);
+        // this CTA's part of the tile's cols x 128 words, each the sum of the shares in rank order
+        for (int i = static_cast<int>(rank) * S::kThreads + threadIdx.x; i < cols * kRows; i += p.split * S::kThreads) {
+            // the order of the words follows the output's rows
+            const int c = p.swap ? i / kRows : i % cols, r = p.swap ? i % kRows : i / cols;
+            if (r >= rows) continue;
+            const uint32_t at = tiles_addr + 4u * static_cast<uint32_t>(c * kRows + r);
+            float v = 0.0f;
+            for (int s = 0; s < p.split; ++s) {
+                float w;
+                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(w) : "r"(mapa_shared(at, s)) : "memory");
+                v = s == 0 ? w : __fadd_rn(v, w);
+            }
+            const int64_t row = p_tile * kRows + r, col = q_tile * TN + c;
+            store_one(p, p.swap ? col * p.ld_out + row : row * p.ld_out + col, __fmul_rn(v, dq));
+        }
+    }
+    if (PAIR || p.split > 1) cluster_sync_all();              // nobody leaves while its memory can be reached
+    if (warp == 1) {
+        __syncwarp();
+        tc_fence_after();
+        if constexpr (PAIR) tmem_dealloc_pair(tmem_base, S::kTmem); else tmem_dealloc(tmem_base, S::kTmem);
+    }
+}
+
+// ---------------------------------------------------------------- host side
+bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+
+template <int FMT, int TN, bool PAIR>
+int launch4(const CUtensorMap (&tm)[4], const Gemm4Args& a, int sm_count, cudaStream_t st) {
+    using S = Shape<FMT, TN, PAIR>;
+    constexpr size_t kSmem = smem4_bytes<FMT, TN, PAIR>();
+    constexpr int kMaxDevices = 64;
+    static std::once_flag once_dev[kMaxDevices];
+    static cudaError_t err_dev[kMaxDevices] = {};
+    static int clusters_dev[kMaxDevices] = {};
+    int dev = 0;
+    FP8MLP_CUDA_CHECK(cudaGetDevice(&dev));
+    if (dev < 0 || dev >= kMaxDevices) { set_cuda_error_str("4-bit product", "device ordinal out of range"); return FP8MLP_ERR_CUDA; }
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[2];
+    cfg.blockDim = dim3(S::kThreads);
+    cfg.dynamicSmemBytes = kSmem;
+    cfg.stream = st;
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    const int cluster = PAIR ? 2 : a.split;
+    if (cluster > 1) {
+        attr[1].id = cudaLaunchAttributeClusterDimension;
+        attr[1].val.clusterDim.x = cluster;
+        attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+        cfg.numAttrs = 2;
+    }
+    std::call_once(once_dev[dev], [&] {
+        err_dev[dev] = cudaFuncSetAttribute(gemm4_kernel<FMT, TN, PAIR>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kSmem));
+        if (PAIR && err_dev[dev] == cudaSuccess) {
+            cfg.gridDim = dim3(static_cast<unsigned>(sm_count) & ~1u);
+            err_dev[dev] = cudaOccupancyMaxActiveClusters(&clusters_dev[dev], gemm4_kernel<FMT, TN, PAIR>, &cfg);
+        }
+    });
+    FP8MLP_CUDA_CHECK(err_dev[dev]);
+    const int64_t tiles = static_cast<int64_t>(a.p_tiles) * a.q_tiles;
+    int64_t grid;
+    if (PAIR) {
+        if (clusters_dev[dev] < 1) { set_cuda_error_str("4-bit product", "no CTA pair fits on the device"); return FP8MLP_ERR_CUDA; }
+        grid = 2 * (tiles < clusters_dev[dev] ? tiles : clusters_dev[dev]);
+    } else if (a.split > 1) {
+        grid = tiles * a.split;                               // a tile per cluster
+    } else {
+        const int64_t most = static_cast<int64_t>(sm_count) * S::kCtasPerSm;
+        grid = tiles < most ? tiles : most;
+    }
+    cfg.gridDim = dim3(static_cast<unsigned>(grid));
+    FP8MLP_CUDA_CHECK(cudaLaunchKernelEx(&cfg, gemm4_kernel<FMT, TN, PAIR>, tm[0], tm[1], tm[2], tm[3], a));
+    count_launch();
+    return FP8MLP_OK;
+}
+
+struct Plan4 { bool pair, swap; int tn, split; };
+
+// How a product runs.  Many tiles: CTA pairs on 256 x 192 tiles.  Otherwise tiles of 128 rows of the longer side (if the other
+// has at most 128 rows) by as many columns as the other side needs, and the contraction split until the CTAs fill the SMs.
+Plan4 plan4(int64_t M, int64_t N, int64_t K, int sms) {
+    Plan4 pl{};
+    const int64_t shorter = M < N ? M : N;
+    const int64_t pairs = (M + 255) / 256 * ((N + 191) / 192);
+    pl.pair = shorter > 128 && 2 * pairs >= sms / 2;
+    if (pl.pair) { pl.tn = 192; pl.split = 1; return pl; }
+    pl.swap = shorter <= 128 && M < N;
+    pl.tn = shorter <= 16 ? 16 : shorter <= 32 ? 32 : shorter <= 64 ? 64 : 128;
+    const int64_t P = pl.swap ? N : M, Q = pl.swap ? M : N;
+    const int64_t tiles = (P + 127) / 128 * ((Q + pl.tn - 1) / pl.tn), room = static_cast<int64_t>(sms) * (pl.tn <= 64 ? 2 : 1);
+    const int64_t stages = (K + kStageK - 1) / kStageK;
+    pl.split = 8;
+    while (pl.split > 1 && (tiles * pl.split > room || stages < 2 * pl.split)) pl.split /= 2;
+    return pl;
+}
+
+template <int FMT>
+int dispatch4(const Plan4& pl, const CUtensorMap (&tm)[4], const Gemm4Args& a, int sms, cudaStream_t st) {
+    if (pl.pair) return launch4<FMT, 192, true>(tm, a, sms, st);
+    switch (pl.tn) {
+        case 16: return launch4<FMT, 16, false>(tm, a, sms, st);
+        case 32: return launch4<FMT, 32, false>(tm, a, sms, st);
+        case 64: return launch4<FMT, 64, false>(tm, a, sms, st);
+        default: return launch4<FMT, 128, false>(tm, a, sms, st);
+    }
+}
+
+}  // namespace
+}  // namespace fp8mlp
+
+using namespace fp8mlp;
+
+extern "C" int fp8mlp_gemm_fp4(int64_t M, int64_t N, int64_t K, int fmt, const uint8_t* A, int64_t ld_a, const uint8_t* a_scales,
+                               const float* scale_a, const uint8_t* B, int64_t ld_b, const uint8_t* b_scales, const float* scale_b,
+                               void* out, int out_dtype, int64_t ld_out, void* stream) {
+    if (fmt != FP8MLP_MXFP4 && fmt != FP8MLP_NVFP4) return FP8MLP_ERR_ARG;
+    if (out_dtype != FP8MLP_BF16 && out_dtype != FP8MLP_F32) return FP8MLP_ERR_ARG;
+    if (fmt == FP8MLP_MXFP4 && (scale_a != nullptr || scale_b != nullptr)) return FP8MLP_ERR_ARG;
+    constexpr int64_t kMost = int64_t(1) << 24;
+    if (M < 0 || N < 0 || K < 1 || M > kMost || N > kMost || K > kMost) return FP8MLP_ERR_SHAPE;
+    const int64_t row = (K + 31) / 32 * 16;
+    if (ld_a % 16 != 0 || ld_b % 16 != 0 || ld_a < row || ld_b < row || (M > 1 && ld_out < N)) return FP8MLP_ERR_SHAPE;
+    const int block = fmt == FP8MLP_MXFP4 ? 32 : 16;
+    const int64_t scale_tiles = (K + 4 * block - 1) / (4 * block);
+    // coordinates of the scales' tensor maps are 32-bit row numbers of 128 bytes
+    if (((M > N ? M : N) + 127) / 128 * scale_tiles * 4 > INT32_MAX) return FP8MLP_ERR_SHAPE;
+    if ((M + 127) / 128 * ((N + 15) / 16) > INT32_MAX / 8) return FP8MLP_ERR_SHAPE;
+    if (M == 0 || N == 0) return FP8MLP_OK;
+    if (A == nullptr || a_scales == nullptr || B == nullptr || b_scales == nullptr || out == nullptr) return FP8MLP_ERR_ARG;
+    const int bytes = out_dtype == FP8MLP_F32 ? 4 : 2;
+    if (!aligned(A, 16) || !aligned(B, 16) || !aligned(a_scales, 16) || !aligned(b_scales, 16) || !aligned(out, bytes)) return FP8MLP_ERR_ALIGN;
+    if (!aligned(scale_a, 4) || !aligned(scale_b, 4)) return FP8MLP_ERR_ALIGN;
+    int dev = 0, sms = 0;
+    FP8MLP_CUDA_CHECK(cudaGetDevice(&dev));
+    FP8MLP_CUDA_CHECK(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+    const Plan4 pl = plan4(M, N, K, sms);
+    struct Side { const uint8_t *codes, *scales; int64_t ld, rows; };
+    const Side a_side{A, a_scales, ld_a, M}, b_side{B, b_scales, ld_b, N};
+    const Side &P = pl.swap ? b_side : a_side, &Q = pl.swap ? a_side : b_side;
+    CUtensorMap tm[4];
+    const uint64_t row_bytes = static_cast<uint64_t>((K + 1) / 2);
+    const uint32_t sf_rows = 4u * kStageK / (4u * block);                     // 128-byte rows of a stage's scales
+    auto codes_map = [&](CUtensorMap* m, const Side& s, uint32_t box) { return make_tmap_bytes(m, s.codes, row_bytes, s.rows, s.ld, box, true); };
+    auto scales_map = [&](CUtensorMap* m, const Side& s) {
+        return make_tmap_bytes(m, s.scales, 128, static_cast<uint64_t>((s.rows + 127) / 128 * scale_tiles * 4), 128, sf_rows, false);
+    };
+    int rc = codes_map(&tm[0], P, kRows);
+    if (rc == FP8MLP_OK) rc = codes_map(&tm[1], Q, pl.pair ? pl.tn / 2 : pl.tn);
+    if (rc == FP8MLP_OK) rc = scales_map(&tm[2], P);
+    if (rc == FP8MLP_OK) rc = scales_map(&tm[3], Q);
+    if (rc != FP8MLP_OK) return rc;
+    Gemm4Args a{};
+    a.P = static_cast<int>(P.rows); a.Q = static_cast<int>(Q.rows); a.K = static_cast<int>(K);
+    a.p_tiles = (a.P + (pl.pair ? 255 : 127)) / (pl.pair ? 256 : 128);
+    a.q_tiles = (a.Q + pl.tn - 1) / pl.tn;
+    a.stages_k = static_cast<int>((K + kStageK - 1) / kStageK);
+    a.p_scale_tiles = a.q_scale_tiles = static_cast<int>(scale_tiles);
+    a.split = pl.split;
+    a.group = 16;
+    a.swap = pl.swap ? 1 : 0;
+    a.f32 = out_dtype == FP8MLP_F32 ? 1 : 0;
+    a.vec = 1;
+    for (int v = 32; v >= 16 && a.vec == 1; v /= 2)
+        if (aligned(out, v) && (M <= 1 || ld_out * bytes % v == 0)) a.vec = v;
+    a.s0 = scale_a; a.s1 = scale_b;
+    a.out = static_cast<uint8_t*>(out);
+    a.ld_out = ld_out;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    return fmt == FP8MLP_MXFP4 ? dispatch4<FP8MLP_MXFP4>(pl, tm, a, sms, st) : dispatch4<FP8MLP_NVFP4>(pl, tm, a, sms, st);
+}

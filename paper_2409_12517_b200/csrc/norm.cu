@@ -1,0 +1,493 @@
+// Root-mean-square norm with the residual's addition, its output optionally as E4M3 codes, and its gradient.
+//
+// Both directions are one pass over their rows: a row's units of 32 bytes lie in the registers of the threads that share it
+// (as many as the row has units, a power of two; several rows per block where they are short), the row's sums go through
+// shuffles and one barrier, and the blocks stay for many rows, so that the gain is read once per block and the next row's
+// loads are on their way while the present row is summed and written.
+#include "common.cuh"
+
+namespace fp8mlp {
+
+namespace {
+
+constexpr uint32_t kAll = 0xffffffffu;
+constexpr int kMaxWarps = 16;
+
+struct NormArgs {
+    const uint8_t *x, *residual;
+    uint8_t *h, *y;
+    const float* gain;
+    float *scale, *rstd;
+    unsigned int* amax;
+    int64_t T, ld_x, ld_res, ld_h, ld_y;      // row strides in bytes
+    float eps, inv_d;
+    int units, tpr;                           // 32-byte units of a row; threads that share it
+};
+
+struct NormBackArgs {
+    const uint8_t *dy, *h, *dh;
+    uint8_t* dx;
+    const float *gain, *rstd;
+    float* partial;                           // [grid][d], null: no gradient of the gain
+    int64_t T, ld_dy, ld_h, ld_dh, ld_dx;
+    float inv_d;
+    int units, tpr, d;
+};
+
+template <typename SRC> struct Unit;          // 32 bytes of a row
+template <> struct Unit<float> { static constexpr int kElems = 8; };
+template <> struct Unit<uint16_t> { static constexpr int kElems = 16; };
+
+// rows start on 16-byte boundaries; WIDE: all of them on 32-byte ones.  Plain loads, not the read-only path: h may be x.
+template <bool WIDE>
+__device__ __forceinline__ void load_unit(const uint8_t* p, uint32_t (&w)[8]) {
+    if constexpr (WIDE) {
+        asm volatile("ld.global.L1::no_allocate.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                     : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
+                     : "l"(p) : "memory");
+    } else {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            asm volatile("ld.global.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];"
+                         : "=r"(w[4 * i]), "=r"(w[4 * i + 1]), "=r"(w[4 * i + 2]), "=r"(w[4 * i + 3])
+                         : "l"(p + 16 * i) : "memory");
+    }
+}
+template <bool WIDE>
+__device__ __forceinline__ void store_unit(uint8_t* p, const uint32_t (&w)[8]) {
+    if constexpr (WIDE) {
+        st_global_v8(p, w);
+    } else {
+        st_global_v4(p, w[0], w[1], w[2], w[3]);
+        st_global_v4(p + 16, w[4], w[5], w[6], w[7]);
+    }
+}
+
+template <typename SRC>
+__device__ __forceinline__ float elem(const uint32_t (&w)[8], int i) {
+    if constexpr (sizeof(SRC) == 4) return __uint_as_float(w[i]);
+    else return (i & 1) ? bf16_hi(w[i >> 1]) : bf16_lo(w[i >> 1]);
+}
+template <typename SRC>
+__device__ __forceinline__ void pack_unit(const float (&v)[Unit<SRC>::kElems], uint32_t (&w)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        if constexpr (sizeof(SRC) == 4) w[i] = __float_as_uint(v[i]);
+        else w[i] = cvt_bf16x2(v[2 * i], v[2 * i + 1]);
+    }
+}
+// x + r, rounded to the type
+template <typename SRC>
+__device__ __forceinline__ void add_unit(uint32_t (&w)[8], const uint32_t (&r)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        if constexpr (sizeof(SRC) == 4) w[i] = __float_as_uint(__fadd_rn(__uint_as_float(w[i]), __uint_as_float(r[i])));
+        else w[i] = cvt_bf16x2(__fadd_rn(bf16_lo(w[i]), bf16_lo(r[i])), __fadd_rn(bf16_hi(w[i]), bf16_hi(r[i])));
+    }
+}
+template <int N>
+__device__ __forceinline__ void load_gain(const float* gain, int first, float (&v)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; i += 4) {
+        const float4 q = gain != nullptr ? __ldg(reinterpret_cast<const float4*>(gain + first + i)) : make_float4(1.0f, 1.0f, 1.0f, 1.0f);
+        v[i] = q.x; v[i + 1] = q.y; v[i + 2] = q.z; v[i + 3] = q.w;
+    }
+}
+
+// Sum (or maximum of values >= 0) over the tpr threads of a row; every one of them gets it.  `part`: a word per warp; the
+// caller alternates between two of them, so that one barrier per call is enough.
+template <bool MAX>
+__device__ __forceinline__ float over_row(float v, int tpr, float* part) {
+    auto join = [](float a, float b) { return MAX ? fmaxf(a, b) : __fadd_rn(a, b); };
+    const int lanes = min(tpr, 32);
+    for (int o = lanes >> 1; o > 0; o >>= 1) v = join(v, __shfl_xor_sync(kAll, v, o));
+    if (tpr <= 32) return v;
+    const int warp = threadIdx.x >> 5, per_row = tpr >> 5, first = warp & ~(per_row - 1);
+    if ((threadIdx.x & 31) == 0) part[warp] = v;
+    __syncthreads();
+    v = part[first];
+    for (int i = 1; i < per_row; ++i) v = join(v, part[first + i]);
+    return v;
+}
+
+// ---------------------------------------------------------------- forward
+// NU: units per thread.  With one (d <= 8192 bf16, 4096 fp32) the next row is fetched ahead and the gain stays in registers.
+template <typename SRC, int BLOCK, int NU, bool WIDE, int OUT>
+__global__ void __launch_bounds__(BLOCK) norm_kernel(const NormArgs p) {
+    constexpr int E = Unit<SRC>::kElems;
+    __shared__ float part_sum[2][kMaxWarps], part_max[2][kMaxWarps];
+    const int sub = threadIdx.x / p.tpr, u0 = threadIdx.x % p.tpr, rows = BLOCK / p.tpr;
+    const int64_t step = static_cast<int64_t>(gridDim.x) * rows;
+    int64_t row = static_cast<int64_t>(blockIdx.x) * rows + sub;
+    grid_dependency_wait();
+    grid_launch_dependents();
+    float gain[E];
+    if (NU == 1 && u0 < p.units) load_gain<E>(p.gain, u0 * E, gain);
+    float scale = 1.0f, run_max = 0.0f;
+    if (OUT == FP8MLP_RMS_E4M3) scale = *p.scale;
+    uint32_t next[NU][8], next_res[NU][8];
+    auto fetch = [&](int64_t r) {
+#pragma unroll
+        for (int k = 0; k < NU; ++k) {
+            const int u = u0 + k * p.tpr;
+            if (r < p.T && u < p.units) {
+                load_unit<WIDE>(p.x + r * p.ld_x + 32 * u, next[k]);
+                if (p.residual != nullptr) load_unit<WIDE>(p.residual + r * p.ld_res + 32 * u, next_res[k]);
+            }
+        }
+    };
+    fetch(row);
+    int parity = 0;
+    // every thread of the block makes the same number of rounds: rows past the end take part in the barriers only
+    for (int64_t first = static_cast<int64_t>(blockIdx.x) * rows; first < p.T; first += step, row += step, parity ^= 1) {
+        const bool here = row < p.T;
+        uint32_t h[NU][8];
+        float sum = 0.0f;
+#pragma unroll
+        for (int k = 0; k < NU; ++k) {
+            const int u = u0 + k * p.tpr;
+            if (!here || u >= p.units) continue;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) h[k][i] = next[k][i];
+            if (p.residual != nullptr) {
+                add_unit<SRC>(h[k], next_res[k]);
+                if (p.h != nullptr) store_unit<WIDE>(p.h + row * p.ld_h + 32 * u, h[k]);
+            }
+            float s[2] = {0.0f, 0.0f};
+#pragma unroll
+            for (int i = 0; i < E; ++i) { const float v = elem<SRC>(h[k], i); s[i & 1] = __fmaf_rn(v, v, s[i & 1]); }
+            sum = __fadd_rn(sum, __fadd_rn(s[0], s[1]));
+        }
+        if (NU == 1) fetch(row + step);
+        sum = over_row<false>(sum, p.tpr, part_sum[parity]);
+        const float rstd = __fdiv_rn(1.0f, __fsqrt_rn(__fmaf_rn(sum, p.inv_d, p.eps)));
+        if (here && u0 == 0 && p.rstd != nullptr) p.rstd[row] = rstd;
+        float top = 0.0f;
+        if (OUT == FP8MLP_RMS_E4M3_ROWS) {
+#pragma unroll
+            for (int k = 0; k < NU; ++k) {
+                const int u = u0 + k * p.tpr;
+                if (!here || u >= p.units) continue;
+                if (NU > 1) load_gain<E>(p.gain, u * E, gain);
+#pragma unroll
+                for (int i = 0; i < E; ++i) top = fmaxf(top, fabsf(__fmul_rn(__fmul_rn(elem<SRC>(h[k], i), rstd), gain[i])));
+            }
+            top = over_row<true>(top, p.tpr, part_max[parity]);
+            scale = __fdiv_rn(448.0f, top);
+            if (!(top > 0.0f) || isinf(top) || isinf(scale)) scale = 1.0f;
+            if (here && u0 == 0) p.scale[row] = scale;
+        }
+#pragma unroll
+        for (int k = 0; k < NU; ++k) {
+            const int u = u0 + k * p.tpr;
+            if (!here || u >= p.units) continue;
+            if (NU > 1) load_gain<E>(p.gain, u * E, gain);
+            float v[E];
+#pragma unroll
+            for (int i = 0; i < E; ++i) v[i] = __fmul_rn(__fmul_rn(elem<SRC>(h[k], i), rstd), gain[i]);
+            if (OUT != FP8MLP_RMS_E4M3_ROWS) {
+#pragma unroll
+                for (int i = 0; i < E; ++i) run_max = fmaxf(run_max, fabsf(v[i]));
+            }
+            if constexpr (OUT == FP8MLP_RMS_SAME) {
+                uint32_t w[8];
+                pack_unit<SRC>(v, w);
+                store_unit<WIDE>(p.y + row * p.ld_y + 32 * u, w);
+            } else {
+                uint8_t* dst = p.y + row * p.ld_y + E * u;
+                uint32_t c[E / 4];
+#pragma unroll
+                for (int i = 0; i < E / 4; ++i)
+                    c[i] = cvt_fp8x4<FP8MLP_E4M3>(__fmul_rn(v[4 * i], scale), __fmul_rn(v[4 * i + 1], scale),
+                                                  __fmul_rn(v[4 * i + 2], scale), __fmul_rn(v[4 * i + 3], scale));
+                if constexpr (E == 16) st_global_v4(dst, c[0], c[1], c[2], c[3]); else st_global_v2(dst, c[0], c[1]);
+            }
+        }
+        if (NU > 1) fetch(row + step);
+    }
+    if (OUT != FP8MLP_RMS_E4M3_ROWS && p.amax != nullptr) {
+        __syncthreads();
+        run_max = warp_max_nonneg(run_max);
+        if ((threadIdx.x & 31) == 0) part_max[0][threadIdx.x >> 5] = run_max;
+        __syncthreads();
+        if (threadIdx.x < 32) {
+            run_max = warp_max_nonneg(threadIdx.x < BLOCK / 32 ? part_max[0][threadIdx.x] : 0.0f);
+            // a single block has the whole maximum (nobody cleared the word for it then)
+            if (threadIdx.x == 0 && gridDim.x == 1) *p.amax = __float_as_uint(run_max);
+            else if (threadIdx.x == 0 && run_max > 0.0f) atomicMax(p.amax, __float_as_uint(run_max));
+        }
+    }
+}
+
+// ---------------------------------------------------------------- backward
+// A thread keeps the columns of its units through all rows of its block and sums their part of d_gain in registers (NU = 1)
+// or in its own words of shared memory; blocks leave one row of partial sums each, which a second kernel adds in their order.
+template <typename SRC, int BLOCK, int NU, bool WIDE>
+__global__ void __launch_bounds__(BLOCK) norm_backward_kernel(const NormBackArgs p) {
+    constexpr int E = Unit<SRC>::kElems;
+    __shared__ float part_sum[2][kMaxWarps];
+    extern __shared__ float d_gain_row[];                        // [d]: NU > 1, or where several rows share a block
+    const int sub = threadIdx.x / p.tpr, u0 = threadIdx.x % p.tpr, rows = BLOCK / p.tpr;
+    const int64_t step = static_cast<int64_t>(gridDim.x) * rows;
+    int64_t row = static_cast<int64_t>(blockIdx.x) * rows + sub;
+    const bool want = p.partial != nullptr;
+    float gain[E], acc[E];
+#pragma unroll
+    for (int i = 0; i < E; ++i) acc[i] = 0.0f;
+    if (NU > 1 && want)
+        for (int i = threadIdx.x; i < p.d; i += BLOCK) d_gain_row[i] = 0.0f;
+    grid_dependency_wait();
+    grid_launch_dependents();
+    if (NU == 1 && u0 < p.units) load_gain<E>(p.gain, u0 * E, gain);
+    if (NU > 1) __syncthreads();
+    uint32_t next_dy[NU][8], next_h[NU][8];
+    float next_rstd = 0.0f;
+    auto fetch = [&](int64_t r) {
+#pragma unroll
+        for (int k = 0; k < NU; ++k) {
+            const int u = u0 + k * p.tpr;
+            if (r < p.T && u < p.units) {
+                load_unit<WIDE>(p.dy + r * p.ld_dy + 32 * u, next_dy[k]);
+                load_unit<WIDE>(p.h + r * p.ld_h + 32 * u, next_h[k]);
+            }
+        }
+        if (r < p.T) next_rstd = __ldg(p.rstd + r);
+    };
+    fetch(row);
+    int parity = 0;
+    for (int64_t first = static_cast<int64_t>(blockIdx.x) * rows; first < p.T; first += step, row += step, parity ^= 1) {
+        const bool here = row < p.T;
+        const float rstd = next_rstd;
+        uint32_t dy[NU][8], h[NU][8], dh[NU][8];
+        float sum = 0.0f;
+#pragma unroll
+        for (int k = 0; k < NU; ++k) {
+            const int u = u0 + k * p.tpr;
+            if (!here || u >= p.units) continue;
+            if (p.dh != nullptr) load_unit<WIDE>(p.dh + row * p.ld_dh + 32 * u, dh[k]);
+            if (NU > 1) load_gain<E>(p.gain, u * E, gain);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) { dy[k][i] = next_dy[k][i]; h[k][i] = next_h[k][i]; }
+            float s[2] = {0.0f, 0.0f};
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+                const float unit = __fmul_rn(elem<SRC>(h[k], i), rstd), d = elem<SRC>(dy[k], i);
+                s[i & 1] = __fmaf_rn(__fmul_rn(d, gain[i]), unit, s[i & 1]);
+                if (NU == 1) acc[i] = __fmaf_rn(d, unit, acc[i]);
+                else if (want) d_gain_row[u * E + i] = __fmaf_rn(d, unit, d_gain_row[u * E + i]);
+            }
+            sum = __fadd_rn(sum, __fadd_rn(s[0], s[1]));
+        }
+        if (NU == 1) fetch(row + step);
+        sum = over_row<false>(sum, p.tpr, part_sum[parity]);
+        const float mean = __fmul_rn(sum, p.inv_d);
+#pragma unroll
+        for (int k = 0; k < NU; ++k) {
+            const int u = u0 + k * p.tpr;
+            if (!here || u >= p.units) continue;
+            if (NU > 1) load_gain<E>(p.gain, u * E, gain);
+            float v[E];
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+                const float unit = __fmul_rn(elem<SRC>(h[k], i), rstd), g = __fmul_rn(elem<SRC>(dy[k], i), gain[i]);
+                v[i] = __fmul_rn(rstd, __fmaf_rn(-unit, mean, g));
+                if (p.dh != nullptr) v[i] = __fadd_rn(v[i], elem<SRC>(dh[k], i));
+            }
+            uint32_t w[8];
+            pack_unit<SRC>(v, w);
+            store_unit<WIDE>(p.dx + row * p.ld_dx + 32 * u, w);
+        }
+        if (NU > 1) fetch(row + step);
+    }
+    if (!want) return;
+    float* out = p.partial + static_cast<int64_t>(blockIdx.x) * p.d;
+    if (NU == 1) {
+        if (rows == 1) {
+            if (u0 < p.units)
+#pragma unroll
+                for (int i = 0; i < E; i += 4) *reinterpret_cast<float4*>(out + u0 * E + i) = make_float4(acc[i], acc[i + 1], acc[i + 2], acc[i + 3]);
+            return;
+        }
+        // the rows of a warp first, then warp after warp
+        for (int o = p.tpr; o < 32; o <<= 1)
+#pragma unroll
+            for (int i = 0; i < E; ++i) acc[i] = __fadd_rn(acc[i], __shfl_xor_sync(kAll, acc[i], o));
+        const bool speaks = p.tpr >= 32 || (threadIdx.x & 31) < p.tpr;
+        const int turns = p.tpr >= 32 ? rows : BLOCK / 32, mine = p.tpr >= 32 ? sub : threadIdx.x >> 5;
+        for (int turn = 0; turn < turns; ++turn) {
+            if (turn == mine && speaks && u0 < p.units)
+#pragma unroll
+                for (int i = 0; i < E; ++i) d_gain_row[u0 * E + i] = turn == 0 ? acc[i] : __fadd_rn(d_gain_row[u0 * E + i], acc[i]);
+            __syncthreads();
+        }
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < p.d; i += BLOCK) out[i] = d_gain_row[i];
+}
+
+// d_gain[i] = sum of the blocks' partial sums: 32 columns a block, 8 warps with every eighth partial row each
+__global__ void __launch_bounds__(256) norm_gain_kernel(const float* partial, int n_partial, int d, float* d_gain) {
+    __shared__ float part[8][32];
+    const int col = blockIdx.x * 32 + (threadIdx.x & 31), warp = threadIdx.x >> 5;
+    grid_dependency_wait();
+    grid_launch_dependents();
+    float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (col < d) {
+        for (int i = warp; i < n_partial; i += 32)
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (i + 8 * k < n_partial) s[k] = __fadd_rn(s[k], __ldcg(partial + static_cast<int64_t>(i + 8 * k) * d + col));
+    }
+    part[warp][threadIdx.x & 31] = __fadd_rn(__fadd_rn(s[0], s[1]), __fadd_rn(s[2], s[3]));
+    __syncthreads();
+    if (warp == 0 && col < d) {
+        float v = part[0][threadIdx.x];
+#pragma unroll
+        for (int k = 1; k < 8; ++k) v = __fadd_rn(v, part[k][threadIdx.x]);
+        d_gain[col] = v;
+    }
+}
+
+// ---------------------------------------------------------------- host side
+bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+
+int sm_count_of_current(int* sms) {
+    int dev = 0;
+    FP8MLP_CUDA_CHECK(cudaGetDevice(&dev));
+    FP8MLP_CUDA_CHECK(cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev));
+    return FP8MLP_OK;
+}
+
+struct RowShape { int units, tpr, block, nu; };
+// threads and units per row
+RowShape row_shape(int64_t d, int elems) {
+    RowShape s;
+    s.units = static_cast<int>(d / elems);
+    s.block = s.units <= 256 ? 256 : 512;
+    s.tpr = 1;
+    while (s.tpr < s.units && s.tpr < s.block) s.tpr <<= 1;
+    const int need = (s.units + s.tpr - 1) / s.tpr;
+    s.nu = need <= 2 ? need : 4;
+    return s;
+}
+
+// a row stride in elements -> bytes; false where it is no multiple of 16 bytes or shorter than the row
+bool stride_ok(int64_t T, int64_t ld, int64_t d, int bytes) { return T <= 1 || (ld >= d && ld * bytes % 16 == 0); }
+
+template <typename SRC, int BLOCK, int NU, bool WIDE>
+cudaError_t launch_norm(const NormArgs& a, int out, dim3 grid, cudaStream_t st) {
+    switch (out) {
+        case FP8MLP_RMS_SAME: return launch_chained(norm_kernel<SRC, BLOCK, NU, WIDE, FP8MLP_RMS_SAME>, grid, dim3(BLOCK), 0, st, a);
+        case FP8MLP_RMS_E4M3: return launch_chained(norm_kernel<SRC, BLOCK, NU, WIDE, FP8MLP_RMS_E4M3>, grid, dim3(BLOCK), 0, st, a);
+        default: return launch_chained(norm_kernel<SRC, BLOCK, NU, WIDE, FP8MLP_RMS_E4M3_ROWS>, grid, dim3(BLOCK), 0, st, a);
+    }
+}
+
+template <typename SRC, int BLOCK, int NU, bool WIDE>
+cudaError_t launch_norm_backward(const NormBackArgs& a, size_t smem, dim3 grid, cudaStream_t st) {
+    if (smem > 48 * 1024) {
+        cudaError_t e = cudaFuncSetAttribute(norm_backward_kernel<SRC, BLOCK, NU, WIDE>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                             FP8MLP_MAX_NORM_WIDTH * 4);
+        if (e != cudaSuccess) return e;
+    }
+    return launch_chained(norm_backward_kernel<SRC, BLOCK, NU, WIDE>, grid, dim3(BLOCK), smem, st, a);
+}
+
+// the instantiation for a shape: F<SRC, BLOCK, NU, WIDE>
+#define FP8MLP_NORM_PICK(F, SRC, WIDE, ...)                                                    \
+    (s.block == 256 ? F<SRC, 256, 1, WIDE>(__VA_ARGS__) : s.nu == 1 ? F<SRC, 512, 1, WIDE>(__VA_ARGS__) \
+     : s.nu == 2 ? F<SRC, 512, 2, WIDE>(__VA_ARGS__) : F<SRC, 512, 4, WIDE>(__VA_ARGS__))
+#define FP8MLP_NORM_LAUNCH(F, ...)                                                                                        \
+    (dtype == FP8MLP_F32 ? (wide ? FP8MLP_NORM_PICK(F, float, true, __VA_ARGS__) : FP8MLP_NORM_PICK(F, float, false, __VA_ARGS__)) \
+                         : (wide ? FP8MLP_NORM_PICK(F, uint16_t, true, __VA_ARGS__) : FP8MLP_NORM_PICK(F, uint16_t, false, __VA_ARGS__)))
+
+}  // namespace
+}  // namespace fp8mlp
+
+using namespace fp8mlp;
+
+extern "C" int fp8mlp_rmsnorm(int64_t T, int64_t d, int dtype, const void* x, int64_t ld_x, const void* residual,
+                              int64_t ld_residual, void* h_out, int64_t ld_h, const float* gain, float eps, int out_kind, void* y,
+                              int64_t ld_y, float* scale, float* amax, float* rstd, void* stream) {
+    if (dtype != FP8MLP_BF16 && dtype != FP8MLP_F32) return FP8MLP_ERR_ARG;
+    if (out_kind < FP8MLP_RMS_SAME || out_kind > FP8MLP_RMS_E4M3_ROWS) return FP8MLP_ERR_ARG;
+    if (h_out != nullptr && residual == nullptr) return FP8MLP_ERR_ARG;
+    if (out_kind == FP8MLP_RMS_E4M3_ROWS && amax != nullptr) return FP8MLP_ERR_ARG;
+    if (!(eps >= 0.0f)) return FP8MLP_ERR_ARG;
+    const int bytes = dtype == FP8MLP_F32 ? 4 : 2, out_bytes = out_kind == FP8MLP_RMS_SAME ? bytes : 1;
+    if (T < 0 || T > (int64_t(1) << 40) || d < 16 || d % 16 != 0 || d > FP8MLP_MAX_NORM_WIDTH) return FP8MLP_ERR_SHAPE;
+    if (!stride_ok(T, ld_x, d, bytes) || !stride_ok(T, ld_y, d, out_bytes)) return FP8MLP_ERR_SHAPE;
+    if (residual != nullptr && !stride_ok(T, ld_residual, d, bytes)) return FP8MLP_ERR_SHAPE;
+    if (h_out != nullptr && !stride_ok(T, ld_h, d, bytes)) return FP8MLP_ERR_SHAPE;
+    if (T > 0 && (x == nullptr || y == nullptr)) return FP8MLP_ERR_ARG;
+    if (out_kind == FP8MLP_RMS_E4M3 && scale == nullptr) return FP8MLP_ERR_ARG;
+    if (out_kind == FP8MLP_RMS_E4M3_ROWS && T > 0 && scale == nullptr) return FP8MLP_ERR_ARG;
+    if (!aligned(x, 16) || !aligned(residual, 16) || !aligned(h_out, 16) || !aligned(y, 16) || !aligned(gain, 16)) return FP8MLP_ERR_ALIGN;
+    if (!aligned(scale, 4) || !aligned(amax, 4) || !aligned(rstd, 4)) return FP8MLP_ERR_ALIGN;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (T == 0) return amax != nullptr ? clear_float(amax, st) : FP8MLP_OK;
+    int sms = 0;
+    if (int rc = sm_count_of_current(&sms)) return rc;
+    const RowShape s = row_shape(d, 32 / bytes);
+    NormArgs a{};
+    a.x = static_cast<const uint8_t*>(x); a.residual = static_cast<const uint8_t*>(residual);
+    a.h = static_cast<uint8_t*>(h_out); a.y = static_cast<uint8_t*>(y);
+    a.gain = gain; a.scale = scale; a.rstd = rstd; a.amax = reinterpret_cast<unsigned int*>(amax);
+    a.T = T; a.ld_x = ld_x * bytes; a.ld_res = ld_residual * bytes; a.ld_h = ld_h * bytes; a.ld_y = ld_y * out_bytes;
+    a.eps = eps; a.inv_d = 1.0f / static_cast<float>(d); a.units = s.units; a.tpr = s.tpr;
+    auto on32 = [&](const void* q, int64_t ld) { return aligned(q, 32) && (T <= 1 || ld % 32 == 0); };
+    const bool wide = on32(x, a.ld_x) && (residual == nullptr || on32(residual, a.ld_res)) && (h_out == nullptr || on32(h_out, a.ld_h)) &&
+                      (out_kind != FP8MLP_RMS_SAME || on32(y, a.ld_y));
+    const int64_t rows = s.block / s.tpr, blocks = (T + rows - 1) / rows, most = static_cast<int64_t>(sms) * (1024 / s.block);
+    const dim3 grid(static_cast<unsigned>(blocks < most ? blocks : most));
+    if (amax != nullptr && grid.x > 1)
+        if (int rc = clear_float(amax, st)) return rc;
+    FP8MLP_CUDA_CHECK(FP8MLP_NORM_LAUNCH(launch_norm, a, out_kind, grid, st));
+    count_launch();
+    return FP8MLP_OK;
+}
+
+extern "C" int fp8mlp_rmsnorm_backward(int64_t T, int64_t d, int dtype, const void* dy, int64_t ld_dy, const void* h, int64_t ld_h,
+                                       const float* gain, const float* rstd, const void* dh, int64_t ld_dh, void* dx,
+                                       int64_t ld_dx, float* d_gain, void* workspace, void* stream) {
+    if (dtype != FP8MLP_BF16 && dtype != FP8MLP_F32) return FP8MLP_ERR_ARG;
+    if (d_gain != nullptr && workspace == nullptr) return FP8MLP_ERR_ARG;
+    const int bytes = dtype == FP8MLP_F32 ? 4 : 2;
+    if (T < 0 || T > (int64_t(1) << 40) || d < 16 || d % 16 != 0 || d > FP8MLP_MAX_NORM_WIDTH) return FP8MLP_ERR_SHAPE;
+    if (!stride_ok(T, ld_dy, d, bytes) || !stride_ok(T, ld_h, d, bytes) || !stride_ok(T, ld_dx, d, bytes)) return FP8MLP_ERR_SHAPE;
+    if (dh != nullptr && !stride_ok(T, ld_dh, d, bytes)) return FP8MLP_ERR_SHAPE;
+    if (T > 0 && (dy == nullptr || h == nullptr || rstd == nullptr || dx == nullptr)) return FP8MLP_ERR_ARG;
+    if (dx != nullptr && dx == h) return FP8MLP_ERR_ARG;
+    if (!aligned(dy, 16) || !aligned(h, 16) || !aligned(dh, 16) || !aligned(dx, 16) || !aligned(gain, 16) || !aligned(workspace, 16))
+        return FP8MLP_ERR_ALIGN;
+    if (!aligned(rstd, 4) || !aligned(d_gain, 4)) return FP8MLP_ERR_ALIGN;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (T == 0) {
+        if (d_gain != nullptr) FP8MLP_CUDA_CHECK(cudaMemsetAsync(d_gain, 0, sizeof(float) * d, st));
+        return FP8MLP_OK;
+    }
+    int sms = 0;
+    if (int rc = sm_count_of_current(&sms)) return rc;
+    const RowShape s = row_shape(d, 32 / bytes);
+    NormBackArgs a{};
+    a.dy = static_cast<const uint8_t*>(dy); a.h = static_cast<const uint8_t*>(h); a.dh = static_cast<const uint8_t*>(dh);
+    a.dx = static_cast<uint8_t*>(dx);
+    a.gain = gain; a.rstd = rstd; a.partial = d_gain != nullptr ? static_cast<float*>(workspace) : nullptr;
+    a.T = T; a.ld_dy = ld_dy * bytes; a.ld_h = ld_h * bytes; a.ld_dh = ld_dh * bytes; a.ld_dx = ld_dx * bytes;
+    a.inv_d = 1.0f / static_cast<float>(d); a.units = s.units; a.tpr = s.tpr; a.d = static_cast<int>(d);
+    auto on32 = [&](const void* q, int64_t ld) { return aligned(q, 32) && (T <= 1 || ld % 32 == 0); };
+    const bool wide = on32(dy, a.ld_dy) && on32(h, a.ld_h) && on32(dx, a.ld_dx) && (dh == nullptr || on32(dh, a.ld_dh));
+    const int64_t rows = s.block / s.tpr, blocks = (T + rows - 1) / rows;
+    int64_t most = static_cast<int64_t>(sms) * (512 / s.block);
+    if (most > FP8MLP_RMS_PARTIALS) most = FP8MLP_RMS_PARTIALS;      // a row of the workspace per block
+    const dim3 grid(static_cast<unsigned>(blocks < most ? blocks : most));
+    const size_t smem = d_gain != nullptr && (s.nu > 1 || rows > 1) ? sizeof(float) * d : 0;
+    FP8MLP_CUDA_CHECK(FP8MLP_NORM_LAUNCH(launch_norm_backward, a, smem, grid, st));
+    count_launch();
+    if (d_gain != nullptr) {
+        FP8MLP_CUDA_CHECK(launch_chained(norm_gain_kernel, dim3(static_cast<unsigned>((d + 31) / 32)), dim3(256), 0, st,
+                                         static_cast<const float*>(workspace), static_cast<int>(grid.x), static_cast<int>(d), d_gain));
+        count_launch();
+    }
+    return FP8MLP_OK;
+}
