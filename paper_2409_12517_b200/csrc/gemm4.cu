@@ -74,13 +74,20 @@ static_assert(smem4_bytes<FP8MLP_NVFP4, 192, true>() <= 232448 && smem4_bytes<FP
 static_assert(2 * (smem4_bytes<FP8MLP_NVFP4, 64, false>() + 1024) <= 233472 && 2 * (smem4_bytes<FP8MLP_NVFP4, 32, false>() + 1024) <= 233472,
               "two CTAs of the narrow tiles share an SM");
 
+// Matrix descriptors: address / 16 in the low 14 bits, then (bit 16) a leading offset that neither layout uses, and in the
+// upper half the distance of 8-row groups / 16, the version and the swizzle.
 // Operand rows of 128 bytes with the 128-byte swizzle: 8-row groups 1024 bytes apart.
-__device__ __forceinline__ uint64_t operand_desc(uint32_t addr) {
-    return static_cast<uint64_t>((addr & 0x3FFFFu) >> 4) | (1ull << 16) | (uint64_t(1024 >> 4) << 32) | (1ull << 46) | (2ull << 61);
+__device__ __forceinline__ uint64_t operand_desc(uint32_t addr16) {
+    return (uint64_t((1024u >> 4) | (1u << 14) | (2u << 29)) << 32) | (addr16 | (1u << 16));
 }
 // A tile of scales, 32 rows of 16 bytes one after the other, no swizzle: 8-row groups 128 bytes apart.
-__device__ __forceinline__ uint64_t scales_desc(uint32_t addr) {
-    return static_cast<uint64_t>((addr & 0x3FFFFu) >> 4) | (1ull << 16) | (uint64_t(128 >> 4) << 32) | (1ull << 46);
+__device__ __forceinline__ uint64_t scales_desc(uint32_t addr16) {
+    return (uint64_t((128u >> 4) | (1u << 14)) << 32) | (addr16 | (1u << 16));
+}
+__device__ __forceinline__ uint32_t elect_one() {
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}\n" : "=r"(r));
+    return r;
 }
 // 512 bytes of scales -> 4 columns of tensor memory, the same in each quadrant of 32 lanes
 template <bool PAIR>
@@ -107,6 +114,30 @@ template <int FMT, int TN, bool PAIR>
 __device__ __forceinline__ uint32_t idesc4(uint32_t sf_byte) {
     return (sf_byte << 4) | (1u << 7) | (1u << 10) | (uint32_t(TN >> 3) << 17) | (uint32_t(FMT == FP8MLP_MXFP4 ? 1 : 0) << 23) |
            (uint32_t((PAIR ? 256 : 128) >> 4) << 24) | (sf_byte << 29);
+}
+
+// The scale copies and MMAs of one stage (FULL: all 256 columns of it; else the `left` that there are).
+template <int FMT, int TN, bool PAIR, bool FULL>
+__device__ __forceinline__ void issue_stage(uint32_t d_tmem, uint32_t base, uint32_t sf_base, uint32_t sf_p, uint32_t sf_q,
+                                            uint32_t q_offset, bool accumulate, int left) {
+    using S = Shape<FMT, TN, PAIR>;
+#pragma unroll
+    for (int t = 0; t < S::kTiles; ++t) {
+        if (!FULL && t * 4 * S::kBlock >= left) break;
+        copy_scales<PAIR>(sf_p + 4 * t, scales_desc(sf_base + t * (kScaleTile >> 4)));
+#pragma unroll
+        for (int j = 0; j < S::kQGroups; ++j)
+            copy_scales<PAIR>(sf_q + 4 * (t * S::kQGroups + j), scales_desc(sf_base + ((1 + j) * S::kSfBytes + t * kScaleTile) / 16));
+    }
+#pragma unroll
+    for (int k = 0; k < kStageK / kStepK; ++k) {
+        if (!FULL && k * kStepK >= left) break;
+        // a cell of four scales is 64 columns of NVFP4, and 128 of MXFP4, which take it in two halves
+        const int t = FMT == FP8MLP_MXFP4 ? k / 2 : k;
+        const uint32_t byte = FMT == FP8MLP_MXFP4 ? 2u * (k & 1) : 0u;
+        umma_f4<FMT, PAIR>(d_tmem, operand_desc(base + 2 * k), operand_desc(base + (S::kPBytes >> 4) + 2 * k), idesc4<FMT, TN, PAIR>(byte),
+                           sf_p + 4 * t, sf_q + 4 * t * S::kQGroups + q_offset, (accumulate || k != 0) ? 1u : 0u);
+    }
 }
 
 __device__ __forceinline__ void tile4_coords(const Gemm4Args& p, int tile, int& p_tile, int& q_tile) {
@@ -254,7 +285,11 @@ gemm4_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_constant__ CU
         }
     } else if (warp == 1) {
         // ------------------------------------------------------------ MMA issuer (CTA pair: rank 0 only)
-        if (lane == 0 && rank * (PAIR ? 1u : 0u) == 0u) {
+        // The whole warp walks the loop and one elected lane issues: addresses and descriptors then are the warp's, not a
+        // lane's, which the tensor instructions need (moving them over from a lane's registers took longer than the MMAs: 10 to
+        // 16 instructions a stage).
+        if (!PAIR || rank == 0u) {
+            const uint32_t leader = elect_one();
             uint32_t stage = 0, phase = 0, count = 0;
             bool ok = true;
             int it = 0;
@@ -262,44 +297,36 @@ gemm4_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_constant__ CU
                 int p_tile, q_tile;
                 tile4_coords(p, tile, p_tile, q_tile);
                 const uint32_t acc = it & 1, acc_phase = (it >> 1) & 1;
-                if (!mbar_wait(smem_u32(&tail->tmem_empty[acc]), acc_phase ^ 1u, abort_flag, nullptr)) break;
+                if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&tail->tmem_empty[acc]), acc_phase ^ 1u, abort_flag, nullptr))) break;
                 tc_fence_after();
                 const uint32_t d_tmem = tmem_base + acc * TN;
                 const uint32_t q_offset = static_cast<uint32_t>((q_tile * TN) % kRows) / 32u;     // first column of the tile's scales
                 for (int kb = kb_begin; kb < kb_end; ++kb, ++count) {
-                    if (!mbar_wait(smem_u32(&tail->full[stage]), phase, abort_flag, nullptr)) { ok = false; break; }
+                    bool go = mbar_wait(smem_u32(&tail->full[stage]), phase, abort_flag, nullptr);
                     if (count >= 2) {        // the scales' columns: free once the MMAs of two stages ago are done
                         const uint32_t before = stage >= 2 ? stage - 2 : stage + kStages - 2;
                         const uint32_t parity = ((count - 2) / kStages) & 1u;
-                        if (!mbar_wait(smem_u32(&tail->empty[before]), parity, abort_flag, nullptr)) { ok = false; break; }
+                        go = go && mbar_wait(smem_u32(&tail->empty[before]), parity, abort_flag, nullptr);
                     }
+                    ok = __all_sync(0xffffffffu, go);
+                    if (!ok) break;
                     tc_fence_after();
-                    const uint32_t p_addr = tiles_addr + stage * kStageBytes, q_addr = p_addr + S::kPBytes, sf_addr = q_addr + S::kQBytes;
                     const uint32_t sf_p = tmem_base + 2 * TN + (count & 1u) * S::kSfCols, sf_q = sf_p + 4 * S::kTiles;
-                    const int left = p.K - kb * kStageK;
-#pragma unroll
-                    for (int t = 0; t < S::kTiles; ++t) {
-                        if (t * 4 * S::kBlock >= left) break;
-                        copy_scales<PAIR>(sf_p + 4 * t, scales_desc(sf_addr + t * kScaleTile));
-#pragma unroll
-                        for (int j = 0; j < S::kQGroups; ++j)
-                            copy_scales<PAIR>(sf_q + 4 * (t * S::kQGroups + j), scales_desc(sf_addr + (1 + j) * S::kSfBytes + t * kScaleTile));
+                    const uint32_t base = (tiles_addr + stage * kStageBytes) >> 4;        // descriptors count in 16 bytes
+                    const uint32_t sf_base = base + ((S::kPBytes + S::kQBytes) >> 4);
+                    if (leader) {
+                        const int left = p.K - kb * kStageK;
+                        if (left >= kStageK) issue_stage<FMT, TN, PAIR, true>(d_tmem, base, sf_base, sf_p, sf_q, q_offset, kb != kb_begin, left);
+                        else issue_stage<FMT, TN, PAIR, false>(d_tmem, base, sf_base, sf_p, sf_q, q_offset, kb != kb_begin, left);
+                        if constexpr (PAIR) umma_commit_pair(smem_u32(&tail->empty[stage])); else umma_commit(smem_u32(&tail->empty[stage]));
                     }
-#pragma unroll
-                    for (int k = 0; k < kStageK / kStepK; ++k) {
-                        if (k * kStepK >= left) break;
-                        // a cell of four scales is 64 columns of NVFP4, and 128 of MXFP4, which take it in two halves
-                        const int t = FMT == FP8MLP_MXFP4 ? k / 2 : k;
-                        const uint32_t byte = FMT == FP8MLP_MXFP4 ? 2u * (k & 1) : 0u;
-                        umma_f4<FMT, PAIR>(d_tmem, operand_desc(p_addr + 32 * k), operand_desc(q_addr + 32 * k), idesc4<FMT, TN, PAIR>(byte),
-                                           sf_p + 4 * t, sf_q + 4 * t * S::kQGroups + q_offset, (kb != kb_begin || k != 0) ? 1u : 0u);
-                    }
-                    if constexpr (PAIR) umma_commit_pair(smem_u32(&tail->empty[stage])); else umma_commit(smem_u32(&tail->empty[stage]));
+                    __syncwarp();
                     if (++stage == kStages) { stage = 0; phase ^= 1u; }
                 }
-                if (ok) {
+                if (ok && leader) {
                     if constexpr (PAIR) umma_commit_pair(smem_u32(&tail->tmem_full[acc])); else umma_commit(smem_u32(&tail->tmem_full[acc]));
                 }
+                __syncwarp();
             }
         }
     } else {
