@@ -9,8 +9,8 @@
 // A CTA is one TMA warp, one warp that issues the MMAs and 4 or 8 epilogue warps; two accumulators alternate, so that the
 // epilogue of a tile overlaps the main loop of the next.  A stage holds 256 columns of the contraction: 128 bytes of codes a
 // row, and the scales' tiles of 512 bytes as they lie in memory (32 rows of 16 bytes), which tcgen05.cp copies to the four lane
-// quadrants of 4 tensor-memory columns.  The scales of two stages alternate in tensor memory: those of stage i are copied once
-// the MMAs of stage i - 2 are done.
+// quadrants of 4 tensor-memory columns.  Tensor memory holds the scales of two to five stages: those
+// of a stage are copied once the MMAs that read their place last are done.
 //
 // Large products: CTA pairs on 256 x 192 tiles (cta_group::2; each CTA loads its 128 rows of P, half of the rows of Q, and the
 // scales of all of Q).  Products with fewer tiles than SMs: single CTAs on 128 x 16 .. 128 tiles, the contraction cut among
@@ -51,13 +51,16 @@ template <int FMT, int TN, bool PAIR> struct Shape {
     static constexpr int kStageBytes = kPBytes + kQBytes + (1 + kQGroups) * kSfBytes;
     static constexpr int kStages = PAIR ? 6 : TN == 128 ? 5 : TN == 64 ? 3 : 4;
     static constexpr int kEpiWarps = TN >= 64 ? 8 : 4;
+    static constexpr int kCtasPerSm = TN <= 64 ? 2 : 1;
     static constexpr int kThreads = 64 + 32 * kEpiWarps;
     static constexpr int kWarpCols = TN / (kEpiWarps / 4);                // columns of a tile that an epilogue warp drains
     static constexpr int kSfCols = 4 * kTiles * (1 + kQGroups);           // tensor-memory columns of a stage's scales
-    static constexpr int kCols = 2 * TN + 2 * kSfCols;
+    // stages whose scales tensor memory holds at a time: as many as fit, at least two
+    static constexpr int kRoom = (512 / kCtasPerSm - 2 * TN) / kSfCols;
+    static constexpr int kSfSlots = kRoom < kStages - 1 ? kRoom : kStages - 1;
+    static constexpr int kCols = 2 * TN + kSfSlots * kSfCols;
     static constexpr int kTmem = kCols <= 128 ? 128 : kCols <= 256 ? 256 : 512;
-    static constexpr int kCtasPerSm = TN <= 64 ? 2 : 1;
-    static_assert(kCols <= 512 && kTmem * kCtasPerSm <= 512, "tensor memory");
+    static_assert(kSfSlots >= 2 && kCols <= 512 && kTmem * kCtasPerSm <= 512, "tensor memory");
 };
 
 struct __align__(8) Tail4 {
@@ -303,15 +306,15 @@ gemm4_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_constant__ CU
                 const uint32_t q_offset = static_cast<uint32_t>((q_tile * TN) % kRows) / 32u;     // first column of the tile's scales
                 for (int kb = kb_begin; kb < kb_end; ++kb, ++count) {
                     bool go = mbar_wait(smem_u32(&tail->full[stage]), phase, abort_flag, nullptr);
-                    if (count >= 2) {        // the scales' columns: free once the MMAs of two stages ago are done
-                        const uint32_t before = stage >= 2 ? stage - 2 : stage + kStages - 2;
-                        const uint32_t parity = ((count - 2) / kStages) & 1u;
+                    if (count >= S::kSfSlots) {        // the scales' columns: free once the MMAs that read them last are done
+                        const uint32_t before = stage >= S::kSfSlots ? stage - S::kSfSlots : stage + kStages - S::kSfSlots;
+                        const uint32_t parity = ((count - S::kSfSlots) / kStages) & 1u;
                         go = go && mbar_wait(smem_u32(&tail->empty[before]), parity, abort_flag, nullptr);
                     }
                     ok = __all_sync(0xffffffffu, go);
                     if (!ok) break;
                     tc_fence_after();
-                    const uint32_t sf_p = tmem_base + 2 * TN + (count & 1u) * S::kSfCols, sf_q = sf_p + 4 * S::kTiles;
+                    const uint32_t sf_p = tmem_base + 2 * TN + (count % S::kSfSlots) * S::kSfCols, sf_q = sf_p + 4 * S::kTiles;
                     const uint32_t base = (tiles_addr + stage * kStageBytes) >> 4;        // descriptors count in 16 bytes
                     const uint32_t sf_base = base + ((S::kPBytes + S::kQBytes) >> 4);
                     if (leader) {
