@@ -531,13 +531,15 @@ def fp8mlp_clip_grads(grads: GradList, norm_kind: int, max_norm: float, norm_coe
 
 # ---------------------------------------------------------------- the norm in front of the block
 
-def _rows_like(t, rows, cols, dtype, what, here):
-    """(pointer, row stride) of a [rows, cols] tensor of one type, or (None, 0)."""
+def _rows_like(t, shape, dtype, what, here):
+    """(pointer, row stride) of a tensor of one shape [rows, cols] and type whose rows are contiguous, or (None, 0)."""
     if t is None:
         return None, 0
-    have, ptr, _, ld = _matrix(t, cols, what, here, dtype)
-    if have != rows:
-        raise ValueError(f"{what}: {have} rows, {rows} are needed")
+    if t.dtype is dtype and t.shape == shape and t.get_device() == here and t.is_contiguous():      # the usual case, quickly
+        return t.data_ptr(), shape[1]
+    have, ptr, _, ld = _matrix(t, shape[1], what, here, dtype)
+    if have != shape[0]:
+        raise ValueError(f"{what}: {have} rows, {shape[0]} are needed")
     return ptr, ld
 
 
@@ -547,20 +549,20 @@ def fp8mlp_rmsnorm(x, residual, gain, eps: float, y, h=None, out: int = RMS_SAME
     x's type; RMS_E4M3: codes (uint8 [T, d], or a device pointer as int, e.g. a context's WS_XQ, with rows of d bytes) of
     y * scale (1-element fp32, read); RMS_E4M3_ROWS: codes, scale (fp32 [T]) is written."""
     here = _here()
-    T, d = x.shape
-    x_ptr, ld_x = _rows_like(x, T, d, x.dtype, "x", here)
-    r_ptr, ld_r = _rows_like(residual, T, d, x.dtype, "residual", here)
-    h_ptr, ld_h = _rows_like(h, T, d, x.dtype, "h", here)
+    shape, dtype = x.shape, x.dtype
+    T, d = shape
+    x_ptr, ld_x = _rows_like(x, shape, dtype, "x", here)
+    r_ptr, ld_r = _rows_like(residual, shape, dtype, "residual", here)
+    h_ptr, ld_h = _rows_like(h, shape, dtype, "h", here)
     if out == RMS_SAME:
-        y_ptr, ld_y = _rows_like(y, T, d, x.dtype, "y", here)
+        y_ptr, ld_y = _rows_like(y, shape, dtype, "y", here)
     elif isinstance(y, int):
         y_ptr, ld_y = y, d
     else:
         y_ptr, ld_y = _bytes(y, T, d, "y", here)
-    n_scales = T if out == RMS_E4M3_ROWS else 1
-    _check(lib().fp8mlp_rmsnorm(T, d, _DTYPES[x.dtype], x_ptr, ld_x, r_ptr, ld_r, h_ptr, ld_h,
+    _check(lib().fp8mlp_rmsnorm(T, d, _DTYPES[dtype], x_ptr, ld_x, r_ptr, ld_r, h_ptr, ld_h,
                                 None if gain is None else _as(gain, _F32, d, "gain", here), eps, out, y_ptr, ld_y,
-                                None if scale is None else _as(scale, _F32, n_scales, "scale", here),
+                                None if scale is None else _as(scale, _F32, T if out == RMS_E4M3_ROWS else 1, "scale", here),
                                 None if amax is None else _as(amax, _F32, 1, "amax", here),
                                 None if rstd is None else _as(rstd, _F32, T, "rstd", here), _stream(here)), "fp8mlp_rmsnorm")
 
@@ -569,12 +571,13 @@ def fp8mlp_rmsnorm_backward(dy, h, gain, rstd, dh, dx, d_gain, workspace) -> Non
     """dx [T, d] (may be dy or dh) and d_gain (fp32 [d], or None) from dy, the stored h and rstd; dh: what reached h along the
     residual stream, or None; workspace: new_rmsnorm_workspace(d), or None without d_gain."""
     here = _here()
-    T, d = h.shape
-    h_ptr, ld_h = _rows_like(h, T, d, h.dtype, "h", here)
-    dy_ptr, ld_dy = _rows_like(dy, T, d, h.dtype, "dy", here)
-    dh_ptr, ld_dh = _rows_like(dh, T, d, h.dtype, "dh", here)
-    dx_ptr, ld_dx = _rows_like(dx, T, d, h.dtype, "dx", here)
-    _check(lib().fp8mlp_rmsnorm_backward(T, d, _DTYPES[h.dtype], dy_ptr, ld_dy, h_ptr, ld_h,
+    shape, dtype = h.shape, h.dtype
+    T, d = shape
+    h_ptr, ld_h = _rows_like(h, shape, dtype, "h", here)
+    dy_ptr, ld_dy = _rows_like(dy, shape, dtype, "dy", here)
+    dh_ptr, ld_dh = _rows_like(dh, shape, dtype, "dh", here)
+    dx_ptr, ld_dx = _rows_like(dx, shape, dtype, "dx", here)
+    _check(lib().fp8mlp_rmsnorm_backward(T, d, _DTYPES[dtype], dy_ptr, ld_dy, h_ptr, ld_h,
                                          None if gain is None else _as(gain, _F32, d, "gain", here),
                                          _as(rstd, _F32, T, "rstd", here), dh_ptr, ld_dh, dx_ptr, ld_dx,
                                          None if d_gain is None else _as(d_gain, _F32, d, "d_gain", here),
@@ -590,30 +593,36 @@ def new_rmsnorm_workspace(d: int, device="cuda"):
 
 def _bytes(t, rows, cols, what, here):
     """(pointer, row stride) of a uint8 matrix whose rows are contiguous, at least `cols` long."""
-    shape = t.shape
-    if t.dtype is not _U8 or len(shape) != 2 or shape[0] != rows or shape[1] < cols or t.get_device() != here or t.stride(1) != 1:
+    shape, strides = t.shape, t.stride()
+    if len(shape) != 2 or t.dtype is not _U8 or shape[0] != rows or shape[1] < cols or t.get_device() != here or strides[1] != 1:
         raise ValueError(f"{what}: a 2-D uint8 CUDA tensor of {rows} rows of {cols} bytes on the current GPU is needed, got "
                          f"{tuple(shape)} {t.dtype} on {t.device}")
-    ld = t.stride(0)
-    return t.data_ptr(), ld if rows > 1 else max(ld, shape[1])
+    return t.data_ptr(), strides[0] if rows > 1 else max(strides[0], shape[1])
 
 
 class Fp4Operand:
     """A [rows, cols] matrix in 4 bits, its columns the contraction of a product: codes (uint8 [rows, at least cols / 2 rounded
-    up to 16]), block scales (uint8, fp8mlp_fp4_scale_bytes) and, for NVFP4, the tensor's scale (1-element fp32, None = 1 in
-    a product)."""
+    up to 16], any row stride), block scales (uint8, fp8mlp_fp4_scale_bytes) and, for NVFP4, the tensor's scale (1-element fp32,
+    None = 1).  Marshalled once: it holds the tensors and their addresses; what is in them is read anew by every call."""
 
-    def __init__(self, fmt: int, rows: int, cols: int, codes, scales, scale=None):
-        self.fmt, self.rows, self.cols, self.codes, self.scales, self.scale = fmt, rows, cols, codes, scales, scale
-        self.code_bytes = (cols + 31) // 32 * 16
-        self.scale_bytes = fp8mlp_fp4_scale_bytes(fmt, rows, cols)
-        self.amax = None
+    def __init__(self, fmt: int, rows: int, cols: int, codes, scales, scale=None, amax=None):
+        self.fmt, self.rows, self.cols, self.device = fmt, rows, cols, codes.get_device()
+        self._tensors = (codes, scales, scale, amax)
+        self.codes_ptr, self.ld_codes = _bytes(codes, rows, (cols + 31) // 32 * 16, "codes", self.device)
+        self.scales_ptr = _as(scales, _U8, fp8mlp_fp4_scale_bytes(fmt, rows, cols), "block scales", self.device)
+        self.scale_ptr = None if scale is None else _as(scale, _F32, 1, "scale", self.device)
+        self.amax_ptr = None if amax is None else _as(amax, _F32, 1, "amax", self.device)
 
-    def pointers(self, what, here):
-        """(codes, their row stride, block scales, scale)"""
-        codes, ld = _bytes(self.codes, self.rows, self.code_bytes, what + " codes", here)
-        return (codes, ld, _as(self.scales, _U8, self.scale_bytes, what + " scales", here),
-                None if self.scale is None else _as(self.scale, _F32, 1, what + " scale", here))
+    codes = property(lambda self: self._tensors[0])
+    scales = property(lambda self: self._tensors[1])
+    scale = property(lambda self: self._tensors[2])
+    amax = property(lambda self: self._tensors[3])
+
+
+def _operand(op, what, here):
+    if op.device != here or here is None:
+        raise ValueError(f"{what}: an operand on the current GPU is needed, this one is on {op.codes.device}")
+    return op
 
 
 def fp8mlp_fp4_scale_bytes(fmt: int, rows: int, cols: int) -> int:
@@ -624,37 +633,37 @@ def new_fp4(fmt: int, rows: int, cols: int, scale=None, device="cuda") -> Fp4Ope
     """Buffers for a [rows, cols] operand; NVFP4: with the given tensor scale, or one of its own, initialised to 1."""
     if fmt == NVFP4 and scale is None:
         scale = torch.ones(1, dtype=torch.float32, device=device)
-    op = Fp4Operand(fmt, rows, cols, torch.empty((rows, (cols + 31) // 32 * 16), dtype=torch.uint8, device=device),
-                    torch.empty(fp8mlp_fp4_scale_bytes(fmt, rows, cols), dtype=torch.uint8, device=device), scale)
-    op.amax = torch.zeros(1, dtype=torch.float32, device=device)
-    return op
+    return Fp4Operand(fmt, rows, cols, torch.empty((rows, (cols + 31) // 32 * 16), dtype=torch.uint8, device=device),
+                      torch.empty(fp8mlp_fp4_scale_bytes(fmt, rows, cols), dtype=torch.uint8, device=device), scale,
+                      torch.zeros(1, dtype=torch.float32, device=device))
 
 
 def fp8mlp_quantize_fp4(src, operand: Fp4Operand, transpose: bool = False, scale_mode: int = SCALE_GIVEN, amax=None) -> None:
     """src: 2-D bf16 or fp32, any row stride; fills operand (of src, or of its transpose).  SCALE_FROM_CURRENT_AMAX (NVFP4)
     writes operand.scale first; amax (1-element fp32): receives max |src| (in that mode the operand's own if None)."""
     here = _here()
-    rows, cols = src.shape
-    _, ptr, dtype, ld = _matrix(src, cols, "src", here)
-    if (operand.rows, operand.cols) != ((cols, rows) if transpose else (rows, cols)):
-        raise ValueError(f"operand: {operand.rows} x {operand.cols}, but src is {rows} x {cols}{' (transposed)' if transpose else ''}")
-    codes, ld_codes, scales, scale = operand.pointers("operand", here)
-    if amax is None and scale_mode == SCALE_FROM_CURRENT_AMAX:
-        amax = operand.amax
-    _check(lib().fp8mlp_quantize_fp4(ptr, dtype, rows, cols, ld, int(transpose), operand.fmt, scale_mode, scale,
-                                     None if amax is None else _as(amax, _F32, 1, "amax", here), codes, ld_codes, scales,
-                                     _stream(here)), "fp8mlp_quantize_fp4")
+    shape, dtype = src.shape, src.dtype
+    if shape != ((operand.cols, operand.rows) if transpose else (operand.rows, operand.cols)):
+        raise ValueError(f"operand: {operand.rows} x {operand.cols}, but src is {tuple(shape)}{' (to be transposed)' if transpose else ''}")
+    if dtype not in _DTYPES:
+        raise ValueError(f"src: bfloat16 or float32 is needed, not {dtype}")
+    ptr, ld = _rows_like(src, shape, dtype, "src", here)
+    o = _operand(operand, "operand", here)
+    amax_ptr = _as(amax, _F32, 1, "amax", here) if amax is not None else o.amax_ptr if scale_mode == SCALE_FROM_CURRENT_AMAX else None
+    _check(lib().fp8mlp_quantize_fp4(ptr, _DTYPES[dtype], shape[0], shape[1], ld, 1 if transpose else 0, o.fmt, scale_mode, o.scale_ptr,
+                                     amax_ptr, o.codes_ptr, o.ld_codes, o.scales_ptr, _stream(here)), "fp8mlp_quantize_fp4")
 
 
 def fp8mlp_dequantize_fp4(operand: Fp4Operand, out) -> None:
     """out: [rows, cols] bf16 or fp32, any row stride, receives the values that the operand stands for."""
     here = _here()
-    rows, ptr, dtype, ld = _matrix(out, operand.cols, "out", here)
-    if rows != operand.rows:
-        raise ValueError(f"out: {rows} rows, the operand has {operand.rows}")
-    codes, ld_codes, scales, scale = operand.pointers("operand", here)
-    _check(lib().fp8mlp_dequantize_fp4(codes, ld_codes, scales, scale, rows, operand.cols, operand.fmt, ptr, dtype, ld, _stream(here)),
-           "fp8mlp_dequantize_fp4")
+    dtype = out.dtype
+    if dtype not in _DTYPES:
+        raise ValueError(f"out: bfloat16 or float32 is needed, not {dtype}")
+    ptr, ld = _rows_like(out, (operand.rows, operand.cols), dtype, "out", here)
+    o = _operand(operand, "operand", here)
+    _check(lib().fp8mlp_dequantize_fp4(o.codes_ptr, o.ld_codes, o.scales_ptr, o.scale_ptr, o.rows, o.cols, o.fmt, ptr, _DTYPES[dtype], ld,
+                                       _stream(here)), "fp8mlp_dequantize_fp4")
 
 
 def fp8mlp_gemm_fp4(a: Fp4Operand, b: Fp4Operand, out) -> None:
@@ -662,13 +671,13 @@ def fp8mlp_gemm_fp4(a: Fp4Operand, b: Fp4Operand, out) -> None:
     here = _here()
     if a.fmt != b.fmt or a.cols != b.cols:
         raise ValueError(f"operands: formats {a.fmt} and {b.fmt}, contractions {a.cols} and {b.cols}")
-    rows, ptr, dtype, ld = _matrix(out, b.rows, "out", here)
-    if rows != a.rows:
-        raise ValueError(f"out: {rows} rows, the first operand has {a.rows}")
-    a_codes, ld_a, a_scales, a_scale = a.pointers("a", here)
-    b_codes, ld_b, b_scales, b_scale = b.pointers("b", here)
-    _check(lib().fp8mlp_gemm_fp4(a.rows, b.rows, a.cols, a.fmt, a_codes, ld_a, a_scales, a_scale, b_codes, ld_b, b_scales, b_scale,
-                                 ptr, dtype, ld, _stream(here)), "fp8mlp_gemm_fp4")
+    dtype = out.dtype
+    if dtype not in _DTYPES:
+        raise ValueError(f"out: bfloat16 or float32 is needed, not {dtype}")
+    _operand(a, "a", here), _operand(b, "b", here)
+    ptr, ld = _rows_like(out, (a.rows, b.rows), dtype, "out", here)
+    _check(lib().fp8mlp_gemm_fp4(a.rows, b.rows, a.cols, a.fmt, a.codes_ptr, a.ld_codes, a.scales_ptr, a.scale_ptr, b.codes_ptr,
+                                 b.ld_codes, b.scales_ptr, b.scale_ptr, ptr, _DTYPES[dtype], ld, _stream(here)), "fp8mlp_gemm_fp4")
 
 
 # ---------------------------------------------------------------- conveniences (allocation only)

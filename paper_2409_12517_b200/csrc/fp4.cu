@@ -147,104 +147,153 @@ __device__ __forceinline__ float scale_of(const QuantArgs& p) {
     return g;
 }
 
+// Tiles are walked from the last to the first where the maximum has just been looked for: the end of the matrix is what L2
+// still holds of that pass.
+__device__ __forceinline__ void tile_of(const QuantArgs& p, int64_t& row_tile, int64_t& col_tile) {
+    const int64_t tile = p.amax_in != nullptr ? gridDim.x - 1 - blockIdx.x : blockIdx.x;
+    row_tile = tile / p.col_tiles;
+    col_tile = tile - row_tile * p.col_tiles;
+}
+
+// The block's tiles of scales, gathered in shared memory, to their place.
+__device__ __forceinline__ void write_scales(const QuantArgs& p, const uint8_t* scales, int64_t row_tile, int64_t first, int tiles) {
+    uint8_t* out = p.scales + (row_tile * p.scale_tiles + first) * kScaleTile;
+    const int bytes = static_cast<int>(min(static_cast<int64_t>(tiles), p.scale_tiles - first)) * kScaleTile;
+    for (int i = 16 * threadIdx.x; i < bytes; i += 16 * kThreads) *reinterpret_cast<uint4*>(out + i) = *reinterpret_cast<const uint4*>(scales + i);
+}
+
 // ---------------------------------------------------------------- the matrix as it is
-// A thread takes a block of 16 or 32 columns of a row at a time; neighbours take neighbouring blocks of the row.
-// VEC: rows start on 16-byte boundaries.
+// A thread takes a block of 16 or 32 columns of a row at a time, neighbours take neighbouring blocks of the row; the loads of
+// kBatch blocks (256 bytes) are on their way together, which takes addresses without branches: a block that is not wholly
+// inside the matrix reads the first one instead, and its own elements one by one.
+// VEC: rows start on 16-byte boundaries and are at least one block long.
 template <typename SRC, int FMT, bool VEC>
-__global__ void __launch_bounds__(kThreads) quantise_kernel(const QuantArgs p) {
+__global__ void __launch_bounds__(kThreads, 2) quantise_kernel(const QuantArgs p) {
     constexpr int N = Fmt<FMT>::kBlock, kBlocks = kCols / N, kTiles = kBlocks / 4, kItems = kTileRows * kBlocks / kThreads;
+    constexpr int kWords = VEC ? N * sizeof(SRC) / 16 : 1, kBatch = VEC ? 16 / kWords : 1;
     __shared__ __align__(16) uint8_t scales[kTiles * kScaleTile];
-    const int64_t row_tile = blockIdx.x / p.col_tiles;
-    const int64_t row0 = row_tile * kTileRows, col0 = (blockIdx.x - row_tile * p.col_tiles) * kCols;
+    int64_t row_tile, col_tile;
+    tile_of(p, row_tile, col_tile);
+    const int64_t row0 = row_tile * kTileRows, col0 = col_tile * kCols;
+    const int b = threadIdx.x % kBlocks, r0 = threadIdx.x / kBlocks;
+    const int64_t col = col0 + b * N;
     grid_dependency_wait();
     grid_launch_dependents();
     const float g = FMT == FP8MLP_NVFP4 ? scale_of(p) : 1.0f;
     float seen = 0.0f;
     const int64_t padded = (p.cols + 31) & ~int64_t(31);          // columns whose codes are written
-#pragma unroll 2
-    for (int it = 0; it < kItems; ++it) {
-        const int item = it * kThreads + threadIdx.x, r = item / kBlocks, b = item % kBlocks;
-        const int64_t row = row0 + r, col = col0 + b * N;
-        float v[N];
-        uint32_t top = 0, byte = 0;
-        if (row < p.rows && col < padded) {
-            const SRC* at = reinterpret_cast<const SRC*>(p.src + row * p.ld) + col;
-            if (VEC && col + N <= p.cols) {
-                constexpr int kWords = N * sizeof(SRC) / 16;
+    const bool whole = col + N <= p.cols;
+#pragma unroll 1
+    for (int first = 0; first < kItems; first += kBatch) {
+        if (row0 + first * (kThreads / kBlocks) >= p.rows) {      // no row of the batch exists: its scales are 0
+            for (int k = 0; k < kBatch; ++k)
+                scales[(b >> 2) * kScaleTile + scale_at(r0 + (first + k) * (kThreads / kBlocks), b & 3)] = 0;
+            continue;
+        }
+        uint4 w[kBatch][kWords];
+        if constexpr (VEC) {
 #pragma unroll
-                for (int i = 0; i < kWords; ++i) {
-                    const uint4 w = ld_global_nc_v4(reinterpret_cast<const uint8_t*>(at) + 16 * i);
-                    const uint32_t words[4] = {w.x, w.y, w.z, w.w};
+            for (int k = 0; k < kBatch; ++k) {
+                const int64_t row = row0 + r0 + (first + k) * (kThreads / kBlocks);
+                const uint8_t* at = (whole && row < p.rows) ? p.src + row * p.ld + col * static_cast<int64_t>(sizeof(SRC)) : p.src;
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        if constexpr (sizeof(SRC) == 4) v[4 * i + k] = __uint_as_float(words[k]);
-                        else { v[8 * i + 2 * k] = bf16_lo(words[k]); v[8 * i + 2 * k + 1] = bf16_hi(words[k]); }
+                for (int i = 0; i < kWords; ++i) w[k][i] = ld_global_nc_v4(at + 16 * i);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) {
+            const int r = r0 + (first + k) * (kThreads / kBlocks);
+            const int64_t row = row0 + r;
+            uint32_t byte = 0;
+            if (row < p.rows && col < padded) {
+                float v[N];
+                if (VEC && whole) {
+#pragma unroll
+                    for (int i = 0; i < kWords; ++i) {
+                        const uint32_t words[4] = {w[k][i].x, w[k][i].y, w[k][i].z, w[k][i].w};
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            if constexpr (sizeof(SRC) == 4) v[(4 * i + j) % N] = __uint_as_float(words[j]);
+                            else { v[(8 * i + 2 * j) % N] = bf16_lo(words[j]); v[(8 * i + 2 * j + 1) % N] = bf16_hi(words[j]); }
+                        }
+                    }
+                } else {
+                    const SRC* at = reinterpret_cast<const SRC*>(p.src + row * p.ld) + col;
+#pragma unroll
+                    for (int i = 0; i < N; ++i) v[i] = col + i < p.cols ? to_f32(at[i]) : 0.0f;
+                }
+                uint32_t top = 0;
+#pragma unroll
+                for (int i = 0; i < N; ++i) top = max(top, abs_bits(v[i]));
+                if (p.amax_out != nullptr) {
+                    if (top <= 0x7f800000u) {
+                        seen = fmaxf(seen, __uint_as_float(top));
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < N; ++i) seen = fmaxf(seen, fabsf(v[i]));
                     }
                 }
-            } else {
-#pragma unroll
-                for (int i = 0; i < N; ++i) v[i] = col + i < p.cols ? to_f32(at[i]) : 0.0f;
+                uint32_t code[N / 8];
+                byte = quantise_block<FMT>(v, top, g, code);
+                if (col >= p.cols) byte = 0;
+                uint8_t* out = p.codes + row * p.ld_codes + col / 2;
+                if constexpr (N == 32) st_global_v4(out, code[0], code[1], code[2], code[3]); else st_global_v2(out, code[0], code[1]);
             }
-#pragma unroll
-            for (int i = 0; i < N; ++i) top = max(top, abs_bits(v[i]));
-            if (p.amax_out != nullptr) {
-                if (top <= 0x7f800000u) seen = fmaxf(seen, __uint_as_float(top));
-                else
-#pragma unroll
-                    for (int i = 0; i < N; ++i) seen = fmaxf(seen, fabsf(v[i]));
-            }
-            uint32_t code[N / 8];
-            byte = quantise_block<FMT>(v, top, g, code);
-            if (col >= p.cols) byte = 0;
-            uint8_t* out = p.codes + row * p.ld_codes + col / 2;
-            if constexpr (N == 32) st_global_v4(out, code[0], code[1], code[2], code[3]); else st_global_v2(out, code[0], code[1]);
+            scales[(b >> 2) * kScaleTile + scale_at(r, b & 3)] = static_cast<uint8_t>(byte);
         }
-        scales[(b >> 2) * kScaleTile + scale_at(r, b & 3)] = static_cast<uint8_t>(byte);
     }
     __syncthreads();
-    const int64_t tile0 = col0 / (4 * N);
-    uint8_t* out = p.scales + (row_tile * p.scale_tiles + tile0) * kScaleTile;
-    const int bytes = static_cast<int>(min(static_cast<int64_t>(kTiles), p.scale_tiles - tile0)) * kScaleTile;
-    for (int i = 16 * threadIdx.x; i < bytes; i += 16 * kThreads) *reinterpret_cast<uint4*>(out + i) = *reinterpret_cast<const uint4*>(scales + i);
+    write_scales(p, scales, row_tile, col0 / (4 * N), kTiles);
     if (p.amax_out != nullptr) raise_amax(seen, p.amax_out);
 }
 
 // ---------------------------------------------------------------- the transposed matrix
 // Operand rows are the source's columns.  A thread takes two neighbouring columns over 32 source rows (a warp reads 64
-// neighbouring columns of a row at once), which are one or two whole blocks of each; the codes go through shared memory so
-// that they leave in pieces of 64 bytes.  VEC: the two columns can be read at once.
+// neighbouring columns of a row at once), which are one or two whole blocks of each; all its loads are on their way together
+// (addresses past the matrix are moved to its last row and column, their values cleared), and the codes go through shared
+// memory so that they leave in pieces of 64 bytes.  VEC: the source's columns come in pairs that can
+// be read at once.
 template <typename SRC, int FMT, bool VEC>
-__global__ void __launch_bounds__(kThreads) quantise_transposed_kernel(const QuantArgs p) {
+__global__ void __launch_bounds__(kThreads, 2) quantise_transposed_kernel(const QuantArgs p) {
     constexpr int N = Fmt<FMT>::kBlock, kTiles = kColsT / (4 * N), kPitch = kColsT / 2 + 16;
     __shared__ __align__(16) uint8_t scales[kTiles * kScaleTile];
     __shared__ __align__(16) uint8_t codes[kTileRows * kPitch];
-    const int64_t row_tile = blockIdx.x / p.col_tiles;
-    const int64_t row0 = row_tile * kTileRows, col0 = (blockIdx.x - row_tile * p.col_tiles) * kColsT;
+    int64_t row_tile, col_tile;
+    tile_of(p, row_tile, col_tile);
+    const int64_t row0 = row_tile * kTileRows, col0 = col_tile * kColsT;
+    const int pair = 2 * (threadIdx.x & 63), k0 = 32 * (threadIdx.x >> 6);        // operand rows of the tile, source rows
+    const int rows = static_cast<int>(min(p.rows - row0, static_cast<int64_t>(kTileRows)));
+    const int cols = static_cast<int>(min(p.cols - col0, static_cast<int64_t>(kColsT)));
+    const bool one = pair < rows, two = pair + 1 < rows;
     grid_dependency_wait();
     grid_launch_dependents();
     const float g = FMT == FP8MLP_NVFP4 ? scale_of(p) : 1.0f;
     float seen = 0.0f;
-    const int pair = 2 * (threadIdx.x & 63), k0 = 32 * (threadIdx.x >> 6);        // operand rows of the tile, source rows
     float v[2][32];
-    const bool both = row0 + pair + 1 < p.rows;
+    {
+        const int c0 = VEC ? min(pair, rows - 2) : min(pair, rows - 1), c1 = min(pair + 1, rows - 1);      // (VEC: rows is even)
+        const uint8_t* base = p.src + col0 * p.ld + row0 * static_cast<int64_t>(sizeof(SRC));
 #pragma unroll
-    for (int i = 0; i < 32; ++i) {
-        const int64_t k = col0 + k0 + i;
-        v[0][i] = v[1][i] = 0.0f;
-        if (k < p.cols && row0 + pair < p.rows) {
-            const SRC* at = reinterpret_cast<const SRC*>(p.src + k * p.ld) + row0 + pair;
-            if (VEC && both) {
-                if constexpr (sizeof(SRC) == 4) {
-                    const float2 w = __ldg(reinterpret_cast<const float2*>(at));
-                    v[0][i] = w.x; v[1][i] = w.y;
-                } else {
-                    const uint32_t w = __ldg(reinterpret_cast<const uint32_t*>(at));
-                    v[0][i] = bf16_lo(w); v[1][i] = bf16_hi(w);
-                }
+        for (int i = 0; i < 32; ++i) {
+            const SRC* at = reinterpret_cast<const SRC*>(base + min(k0 + i, cols - 1) * p.ld);
+            if constexpr (VEC && sizeof(SRC) == 4) {
+                const float2 w = __ldg(reinterpret_cast<const float2*>(at + c0));
+                v[0][i] = w.x; v[1][i] = w.y;
+            } else if constexpr (VEC) {
+                v[0][i] = __uint_as_float(__ldg(reinterpret_cast<const uint32_t*>(at + c0)));
             } else {
-                v[0][i] = to_f32(at[0]);
-                if (both) v[1][i] = to_f32(at[1]);
+                v[0][i] = to_f32(__ldg(at + c0)); v[1][i] = to_f32(__ldg(at + c1));
             }
+        }
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+            if constexpr (VEC && sizeof(SRC) == 2) {
+                const uint32_t w = __float_as_uint(v[0][i]);
+                v[0][i] = bf16_lo(w); v[1][i] = bf16_hi(w);
+            }
+            const bool in = k0 + i < cols;
+            v[0][i] = in && one ? v[0][i] : 0.0f;
+            v[1][i] = in && two ? v[1][i] : 0.0f;
         }
     }
 #pragma unroll
@@ -260,12 +309,13 @@ __global__ void __launch_bounds__(kThreads) quantise_transposed_kernel(const Qua
                 block[i] = v[c][N * j + i];
                 top = max(top, abs_bits(block[i]));
             }
-            if (p.amax_out != nullptr)
+            if (p.amax_out != nullptr) {
 #pragma unroll
                 for (int i = 0; i < N; ++i) seen = fmaxf(seen, fabsf(block[i]));
+            }
             uint32_t code[N / 8];
             uint32_t byte = quantise_block<FMT>(block, top, g, code);
-            if (row0 + r >= p.rows || col0 + k0 + N * j >= p.cols) byte = 0;
+            if (r >= rows || k0 + N * j >= cols) byte = 0;
             const int b = k0 / N + j;
             scales[(b >> 2) * kScaleTile + scale_at(r, b & 3)] = static_cast<uint8_t>(byte);
 #pragma unroll
@@ -274,20 +324,17 @@ __global__ void __launch_bounds__(kThreads) quantise_transposed_kernel(const Qua
         *reinterpret_cast<uint4*>(codes + r * kPitch + k0 / 2) = make_uint4(words[0], words[1], words[2], words[3]);
     }
     __syncthreads();
-    const int64_t tile0 = col0 / (4 * N);
-    uint8_t* out = p.scales + (row_tile * p.scale_tiles + tile0) * kScaleTile;
-    const int bytes = static_cast<int>(min(static_cast<int64_t>(kTiles), p.scale_tiles - tile0)) * kScaleTile;
-    for (int i = 16 * threadIdx.x; i < bytes; i += 16 * kThreads) *reinterpret_cast<uint4*>(out + i) = *reinterpret_cast<const uint4*>(scales + i);
-    const int64_t padded = (p.cols + 31) & ~int64_t(31);
+    write_scales(p, scales, row_tile, col0 / (4 * N), kTiles);
+    const int padded = (cols + 31) & ~31;
     for (int i = threadIdx.x; i < kTileRows * (kColsT / 32); i += kThreads) {
         const int r = i / (kColsT / 32), c = i % (kColsT / 32);
-        if (row0 + r < p.rows && col0 + 32 * c < padded)
+        if (r < rows && 32 * c < padded)
             *reinterpret_cast<uint4*>(p.codes + (row0 + r) * p.ld_codes + (col0 + 32 * c) / 2) = *reinterpret_cast<const uint4*>(codes + r * kPitch + 16 * c);
     }
     if (p.amax_out != nullptr) raise_amax(seen, p.amax_out);
 }
 
-// max |src| over a matrix with a row stride, NaN left out: a block takes 64 rows' worth of 1024 columns
+// max |src| over a matrix with a row stride, NaN left out
 template <typename SRC, bool VEC>
 __global__ void __launch_bounds__(kThreads) amax_kernel(const uint8_t* src, int64_t ld, int64_t rows, int64_t cols, unsigned int* amax) {
     constexpr int kPer = 16 / sizeof(SRC);
@@ -341,53 +388,76 @@ struct DequantArgs {
     int col_tiles, scale_tiles;
 };
 
-// A thread takes 16 columns of a row.  VEC: output rows start on 16-byte boundaries.
-template <typename DST, int FMT, bool VEC>
+// A thread takes 32 columns of a row at a time (16 bytes of codes), four rows' loads on their way together.
+// ALIGN: bytes that output rows are aligned to (32, 16, or less as 1).
+template <typename DST, int FMT, int ALIGN>
 __global__ void __launch_bounds__(kThreads) dequantise_kernel(const DequantArgs p) {
-    constexpr int N = Fmt<FMT>::kBlock, kPerRow = kCols / 16, kItems = kTileRows * kPerRow / kThreads;
+    constexpr int N = Fmt<FMT>::kBlock, kPerRow = kCols / 32, kItems = kTileRows * kPerRow / kThreads, kStep = kThreads / kPerRow;
     const int64_t row_tile = blockIdx.x / p.col_tiles;
-    const int64_t row0 = row_tile * kTileRows, col0 = (blockIdx.x - row_tile * p.col_tiles) * kCols;
+    const int64_t row0 = row_tile * kTileRows, col = (blockIdx.x - row_tile * p.col_tiles) * kCols + 32 * (threadIdx.x % kPerRow);
     grid_dependency_wait();
     grid_launch_dependents();
+    if (col >= p.cols) return;
     const float inv_g = p.scale != nullptr ? __fdiv_rn(1.0f, *p.scale) : 1.0f;
-#pragma unroll 4
+    const int r0 = threadIdx.x / kPerRow;
+    const int64_t block = col / N;                    // the first of the columns' one or two blocks
+    const uint8_t* scales = p.scales + (row_tile * p.scale_tiles + block / 4) * kScaleTile + (block & 3);
+    uint4 code[kItems];
+    uint32_t bytes[kItems];
+#pragma unroll
     for (int it = 0; it < kItems; ++it) {
-        const int item = it * kThreads + threadIdx.x, r = item / kPerRow;
-        const int64_t row = row0 + r, col = col0 + 16 * (item % kPerRow);
-        if (row >= p.rows || col >= p.cols) continue;
-        const uint2 code = __ldg(reinterpret_cast<const uint2*>(p.codes + row * p.ld_codes + col / 2));
-        const int64_t block = col / N;
-        const uint32_t byte = __ldg(p.scales + (row_tile * p.scale_tiles + block / 4) * kScaleTile +
-                                    scale_at(r, static_cast<int>(block & 3)));
-        float s, unused;
-        if constexpr (FMT == FP8MLP_MXFP4) s = byte == 0xffu ? __uint_as_float(0x7fffffffu) : byte == 0u ? __uint_as_float(0x00400000u) : __uint_as_float(byte << 23);
-        else e4m3x2_to_f32(byte, s, unused);
-        float v[16];
+        const int r = static_cast<int>(min(static_cast<int64_t>(r0 + it * kStep), p.rows - 1 - row0));
+        code[it] = ld_global_nc_v4(p.codes + (row0 + r) * p.ld_codes + col / 2);
+        if constexpr (N == 32) bytes[it] = __ldg(scales + scale_at(r, 0));
+        else bytes[it] = __ldg(reinterpret_cast<const unsigned short*>(scales + scale_at(r, 0)));
+    }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) e2m1x2_to_f32(((i < 4 ? code.x : code.y) >> (8 * (i & 3))) & 0xffu, v[2 * i], v[2 * i + 1]);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            v[i] = __fmul_rn(v[i], s);                       // exact, but for MXFP4 scales at the ends of fp32's range
-            if constexpr (FMT == FP8MLP_NVFP4) v[i] = __fmul_rn(v[i], inv_g);
+    for (int it = 0; it < kItems; ++it) {
+        const int64_t row = row0 + r0 + it * kStep;
+        if (row >= p.rows) break;
+        float s[2];
+        if constexpr (FMT == FP8MLP_MXFP4) {
+            const uint32_t e = bytes[it];             // 2^(e - 127); NaN; the smallest is subnormal in fp32
+            s[0] = s[1] = __uint_as_float(e == 0xffu ? 0x7fffffffu : e == 0u ? 0x00400000u : e << 23);
+        } else {
+            e4m3x2_to_f32(bytes[it], s[0], s[1]);
         }
         DST* out = reinterpret_cast<DST*>(p.out + row * p.ld_out) + col;
-        if (VEC && col + 16 <= p.cols) {
-            if constexpr (sizeof(DST) == 4) {
+        const uint32_t words[4] = {code[it].x, code[it].y, code[it].z, code[it].w};
 #pragma unroll
-                for (int i = 0; i < 16; i += 4)
-                    st_global_v4(out + i, __float_as_uint(v[i]), __float_as_uint(v[i + 1]), __float_as_uint(v[i + 2]), __float_as_uint(v[i + 3]));
+        for (int h = 0; h < 2; ++h) {                 // 16 columns at a time
+            float v[16];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) e2m1x2_to_f32((words[2 * h + i / 4] >> (8 * (i & 3))) & 0xffu, v[2 * i], v[2 * i + 1]);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                v[i] = __fmul_rn(v[i], s[h]);         // exact, but for MXFP4 scales at the ends of fp32's range
+                if constexpr (FMT == FP8MLP_NVFP4) v[i] = __fmul_rn(v[i], inv_g);
+            }
+            if (ALIGN >= 16 && col + 16 * h + 16 <= p.cols) {
+#pragma unroll
+                for (int i = 0; i < 16; i += 32 / sizeof(DST)) {
+                    uint32_t w[8];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        if constexpr (sizeof(DST) == 4) w[k] = __float_as_uint(v[(i + k) % 16]);
+                        else w[k] = cvt_bf16x2(v[(i + 2 * k) % 16], v[(i + 2 * k + 1) % 16]);
+                    }
+                    if constexpr (ALIGN >= 32) {
+                        st_global_v8(out + 16 * h + i, w);
+                    } else {
+                        st_global_v4(out + 16 * h + i, w[0], w[1], w[2], w[3]);
+                        st_global_v4(out + 16 * h + i + 16 / sizeof(DST), w[4], w[5], w[6], w[7]);
+                    }
+                }
             } else {
 #pragma unroll
-                for (int i = 0; i < 16; i += 8)
-                    st_global_v4(out + i, cvt_bf16x2(v[i], v[i + 1]), cvt_bf16x2(v[i + 2], v[i + 3]), cvt_bf16x2(v[i + 4], v[i + 5]), cvt_bf16x2(v[i + 6], v[i + 7]));
+                for (int i = 0; i < 16; ++i)
+                    if (col + 16 * h + i < p.cols) {
+                        if constexpr (sizeof(DST) == 4) out[16 * h + i] = v[i];
+                        else out[16 * h + i] = static_cast<uint16_t>(cvt_bf16x2(v[i], 0.0f) & 0xffffu);
+                    }
             }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-                if (col + i < p.cols) {
-                    if constexpr (sizeof(DST) == 4) out[i] = v[i];
-                    else out[i] = static_cast<uint16_t>(cvt_bf16x2(v[i], 0.0f) & 0xffffu);
-                }
         }
     }
 }
@@ -399,11 +469,11 @@ constexpr int64_t kMost = int64_t(1) << 24;      // rows and columns
 template <typename SRC, int FMT>
 cudaError_t launch_quantise(const QuantArgs& a, bool transpose, dim3 grid, cudaStream_t st) {
     if (transpose) {
-        const bool vec = aligned(a.src, 2 * sizeof(SRC)) && a.ld % (2 * sizeof(SRC)) == 0;
+        const bool vec = aligned(a.src, 2 * sizeof(SRC)) && a.ld % (2 * sizeof(SRC)) == 0 && a.rows % 2 == 0;
         return vec ? launch_chained(quantise_transposed_kernel<SRC, FMT, true>, grid, dim3(kThreads), 0, st, a)
                    : launch_chained(quantise_transposed_kernel<SRC, FMT, false>, grid, dim3(kThreads), 0, st, a);
     }
-    const bool vec = aligned(a.src, 16) && a.ld % 16 == 0;
+    const bool vec = aligned(a.src, 16) && a.ld % 16 == 0 && a.cols >= Fmt<FMT>::kBlock;
     return vec ? launch_chained(quantise_kernel<SRC, FMT, true>, grid, dim3(kThreads), 0, st, a)
                : launch_chained(quantise_kernel<SRC, FMT, false>, grid, dim3(kThreads), 0, st, a);
 }
@@ -507,9 +577,11 @@ extern "C" int fp8mlp_dequantize_fp4(const uint8_t* codes, int64_t ld_codes, con
     a.scale_tiles = static_cast<int>((cols + per_tile - 1) / per_tile);
     a.col_tiles = static_cast<int>((cols + kCols - 1) / kCols);
     const dim3 grid(static_cast<unsigned>(tiles));
-    const bool vec = aligned(out, 16) && a.ld_out % 16 == 0;
-#define FP8MLP_DEQUANT(D, F) (vec ? launch_chained(dequantise_kernel<D, F, true>, grid, dim3(kThreads), 0, st, a) \
-                                  : launch_chained(dequantise_kernel<D, F, false>, grid, dim3(kThreads), 0, st, a))
+    const int align = aligned(out, 32) && a.ld_out % 32 == 0 ? 32 : aligned(out, 16) && a.ld_out % 16 == 0 ? 16 : 1;
+#define FP8MLP_DEQUANT(D, F)                                                                                  \
+    (align == 32 ? launch_chained(dequantise_kernel<D, F, 32>, grid, dim3(kThreads), 0, st, a)                \
+     : align == 16 ? launch_chained(dequantise_kernel<D, F, 16>, grid, dim3(kThreads), 0, st, a)              \
+                   : launch_chained(dequantise_kernel<D, F, 1>, grid, dim3(kThreads), 0, st, a))
     const bool f32 = out_dtype == FP8MLP_F32;
     const cudaError_t e = fmt == FP8MLP_MXFP4 ? (f32 ? FP8MLP_DEQUANT(float, FP8MLP_MXFP4) : FP8MLP_DEQUANT(uint16_t, FP8MLP_MXFP4))
                                               : (f32 ? FP8MLP_DEQUANT(float, FP8MLP_NVFP4) : FP8MLP_DEQUANT(uint16_t, FP8MLP_NVFP4));

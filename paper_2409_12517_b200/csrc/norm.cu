@@ -94,20 +94,27 @@ __device__ __forceinline__ void load_gain(const float* gain, int first, float (&
     }
 }
 
-// Sum (or maximum of values >= 0) over the tpr threads of a row; every one of them gets it.  `part`: a word per warp; the
-// caller alternates between two of them, so that one barrier per call is enough.
+// Sum of one value, and with MAX the maximum of another (>= 0), over the tpr threads of a row; every one of them gets both.
+// `part`: two words per warp; the caller alternates between two such arrays, so that one barrier per call is enough.
 template <bool MAX>
-__device__ __forceinline__ float over_row(float v, int tpr, float* part) {
-    auto join = [](float a, float b) { return MAX ? fmaxf(a, b) : __fadd_rn(a, b); };
-    const int lanes = min(tpr, 32);
-    for (int o = lanes >> 1; o > 0; o >>= 1) v = join(v, __shfl_xor_sync(kAll, v, o));
-    if (tpr <= 32) return v;
+__device__ __forceinline__ void over_row(float& sum, float& top, int tpr, float* part) {
+    for (int o = min(tpr, 32) >> 1; o > 0; o >>= 1) {
+        sum = __fadd_rn(sum, __shfl_xor_sync(kAll, sum, o));
+        if (MAX) top = fmaxf(top, __shfl_xor_sync(kAll, top, o));
+    }
+    if (tpr <= 32) return;
     const int warp = threadIdx.x >> 5, per_row = tpr >> 5, first = warp & ~(per_row - 1);
-    if ((threadIdx.x & 31) == 0) part[warp] = v;
+    if ((threadIdx.x & 31) == 0) {
+        part[warp] = sum;
+        if (MAX) part[kMaxWarps + warp] = top;
+    }
     __syncthreads();
-    v = part[first];
-    for (int i = 1; i < per_row; ++i) v = join(v, part[first + i]);
-    return v;
+    sum = part[first];
+    for (int i = 1; i < per_row; ++i) sum = __fadd_rn(sum, part[first + i]);
+    if (MAX) {
+        top = part[kMaxWarps + first];
+        for (int i = 1; i < per_row; ++i) top = fmaxf(top, part[kMaxWarps + first + i]);
+    }
 }
 
 // ---------------------------------------------------------------- forward
@@ -115,7 +122,7 @@ __device__ __forceinline__ float over_row(float v, int tpr, float* part) {
 template <typename SRC, int BLOCK, int NU, bool WIDE, int OUT>
 __global__ void __launch_bounds__(BLOCK) norm_kernel(const NormArgs p) {
     constexpr int E = Unit<SRC>::kElems;
-    __shared__ float part_sum[2][kMaxWarps], part_max[2][kMaxWarps];
+    __shared__ float part[2][2 * kMaxWarps];
     const int sub = threadIdx.x / p.tpr, u0 = threadIdx.x % p.tpr, rows = BLOCK / p.tpr;
     const int64_t step = static_cast<int64_t>(gridDim.x) * rows;
     int64_t row = static_cast<int64_t>(blockIdx.x) * rows + sub;
@@ -142,7 +149,7 @@ __global__ void __launch_bounds__(BLOCK) norm_kernel(const NormArgs p) {
     for (int64_t first = static_cast<int64_t>(blockIdx.x) * rows; first < p.T; first += step, row += step, parity ^= 1) {
         const bool here = row < p.T;
         uint32_t h[NU][8];
-        float sum = 0.0f;
+        float sum = 0.0f, top = 0.0f;                       // of h^2, and max |h gain|
 #pragma unroll
         for (int k = 0; k < NU; ++k) {
             const int u = u0 + k * p.tpr;
@@ -153,29 +160,30 @@ __global__ void __launch_bounds__(BLOCK) norm_kernel(const NormArgs p) {
                 add_unit<SRC>(h[k], next_res[k]);
                 if (p.h != nullptr) store_unit<WIDE>(p.h + row * p.ld_h + 32 * u, h[k]);
             }
+            if (NU > 1) load_gain<E>(p.gain, u * E, gain);
             float s[2] = {0.0f, 0.0f};
 #pragma unroll
-            for (int i = 0; i < E; ++i) { const float v = elem<SRC>(h[k], i); s[i & 1] = __fmaf_rn(v, v, s[i & 1]); }
+            for (int i = 0; i < E; ++i) {
+                const float v = elem<SRC>(h[k], i);
+                s[i & 1] = __fmaf_rn(v, v, s[i & 1]);
+                top = fmaxf(top, fabsf(__fmul_rn(v, gain[i])));
+            }
             sum = __fadd_rn(sum, __fadd_rn(s[0], s[1]));
         }
         if (NU == 1) fetch(row + step);
-        sum = over_row<false>(sum, p.tpr, part_sum[parity]);
+        over_row<OUT == FP8MLP_RMS_E4M3_ROWS>(sum, top, p.tpr, part[parity]);
         const float rstd = __fdiv_rn(1.0f, __fsqrt_rn(__fmaf_rn(sum, p.inv_d, p.eps)));
         if (here && u0 == 0 && p.rstd != nullptr) p.rstd[row] = rstd;
-        float top = 0.0f;
+        // y = (h gain) factor; codes with a scale of the row's own do not depend on rstd, as it cancels
+        float factor = rstd;
+        if (OUT == FP8MLP_RMS_E4M3) factor = __fmul_rn(rstd, scale);
         if (OUT == FP8MLP_RMS_E4M3_ROWS) {
-#pragma unroll
-            for (int k = 0; k < NU; ++k) {
-                const int u = u0 + k * p.tpr;
-                if (!here || u >= p.units) continue;
-                if (NU > 1) load_gain<E>(p.gain, u * E, gain);
-#pragma unroll
-                for (int i = 0; i < E; ++i) top = fmaxf(top, fabsf(__fmul_rn(__fmul_rn(elem<SRC>(h[k], i), rstd), gain[i])));
-            }
-            top = over_row<true>(top, p.tpr, part_max[parity]);
-            scale = __fdiv_rn(448.0f, top);
-            if (!(top > 0.0f) || isinf(top) || isinf(scale)) scale = 1.0f;
-            if (here && u0 == 0) p.scale[row] = scale;
+            const float most = __fmul_rn(top, rstd), row_scale = __fdiv_rn(448.0f, most);
+            const bool sound = most > 0.0f && !isinf(most) && !isinf(row_scale);
+            if (sound) factor = __fdiv_rn(448.0f, top);
+            if (here && u0 == 0) p.scale[row] = sound ? row_scale : 1.0f;
+        } else {
+            run_max = fmaxf(run_max, __fmul_rn(top, rstd));
         }
 #pragma unroll
         for (int k = 0; k < NU; ++k) {
@@ -184,11 +192,7 @@ __global__ void __launch_bounds__(BLOCK) norm_kernel(const NormArgs p) {
             if (NU > 1) load_gain<E>(p.gain, u * E, gain);
             float v[E];
 #pragma unroll
-            for (int i = 0; i < E; ++i) v[i] = __fmul_rn(__fmul_rn(elem<SRC>(h[k], i), rstd), gain[i]);
-            if (OUT != FP8MLP_RMS_E4M3_ROWS) {
-#pragma unroll
-                for (int i = 0; i < E; ++i) run_max = fmaxf(run_max, fabsf(v[i]));
-            }
+            for (int i = 0; i < E; ++i) v[i] = __fmul_rn(__fmul_rn(elem<SRC>(h[k], i), gain[i]), factor);
             if constexpr (OUT == FP8MLP_RMS_SAME) {
                 uint32_t w[8];
                 pack_unit<SRC>(v, w);
@@ -197,9 +201,7 @@ __global__ void __launch_bounds__(BLOCK) norm_kernel(const NormArgs p) {
                 uint8_t* dst = p.y + row * p.ld_y + E * u;
                 uint32_t c[E / 4];
 #pragma unroll
-                for (int i = 0; i < E / 4; ++i)
-                    c[i] = cvt_fp8x4<FP8MLP_E4M3>(__fmul_rn(v[4 * i], scale), __fmul_rn(v[4 * i + 1], scale),
-                                                  __fmul_rn(v[4 * i + 2], scale), __fmul_rn(v[4 * i + 3], scale));
+                for (int i = 0; i < E / 4; ++i) c[i] = cvt_fp8x4<FP8MLP_E4M3>(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
                 if constexpr (E == 16) st_global_v4(dst, c[0], c[1], c[2], c[3]); else st_global_v2(dst, c[0], c[1]);
             }
         }
@@ -208,10 +210,10 @@ __global__ void __launch_bounds__(BLOCK) norm_kernel(const NormArgs p) {
     if (OUT != FP8MLP_RMS_E4M3_ROWS && p.amax != nullptr) {
         __syncthreads();
         run_max = warp_max_nonneg(run_max);
-        if ((threadIdx.x & 31) == 0) part_max[0][threadIdx.x >> 5] = run_max;
+        if ((threadIdx.x & 31) == 0) part[0][threadIdx.x >> 5] = run_max;
         __syncthreads();
         if (threadIdx.x < 32) {
-            run_max = warp_max_nonneg(threadIdx.x < BLOCK / 32 ? part_max[0][threadIdx.x] : 0.0f);
+            run_max = warp_max_nonneg(threadIdx.x < BLOCK / 32 ? part[0][threadIdx.x] : 0.0f);
             // a single block has the whole maximum (nobody cleared the word for it then)
             if (threadIdx.x == 0 && gridDim.x == 1) *p.amax = __float_as_uint(run_max);
             else if (threadIdx.x == 0 && run_max > 0.0f) atomicMax(p.amax, __float_as_uint(run_max));
@@ -279,7 +281,8 @@ __global__ void __launch_bounds__(BLOCK) norm_backward_kernel(const NormBackArgs
             sum = __fadd_rn(sum, __fadd_rn(s[0], s[1]));
         }
         if (NU == 1) fetch(row + step);
-        sum = over_row<false>(sum, p.tpr, part_sum[parity]);
+        float unused = 0.0f;
+        over_row<false>(sum, unused, p.tpr, part_sum[parity]);
         const float mean = __fmul_rn(sum, p.inv_d);
 #pragma unroll
         for (int k = 0; k < NU; ++k) {
@@ -325,26 +328,40 @@ __global__ void __launch_bounds__(BLOCK) norm_backward_kernel(const NormBackArgs
     for (int i = threadIdx.x; i < p.d; i += BLOCK) out[i] = d_gain_row[i];
 }
 
-// d_gain[i] = sum of the blocks' partial sums: 32 columns a block, 8 warps with every eighth partial row each
-__global__ void __launch_bounds__(256) norm_gain_kernel(const float* partial, int n_partial, int d, float* d_gain) {
-    __shared__ float part[8][32];
-    const int col = blockIdx.x * 32 + (threadIdx.x & 31), warp = threadIdx.x >> 5;
+// d_gain[i] = sum of the blocks' partial sums: 128 columns a block, every one of 32 warps takes every 32nd partial row and has
+// all their loads on their way together
+constexpr int kGainWarps = 32;
+__global__ void __launch_bounds__(32 * kGainWarps) norm_gain_kernel(const float* partial, int n_partial, int d, float* d_gain) {
+    __shared__ float4 part[kGainWarps][32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, col = blockIdx.x * 128 + 4 * lane;
     grid_dependency_wait();
     grid_launch_dependents();
-    float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    auto add = [](float4& a, const float4& b) {
+        a.x = __fadd_rn(a.x, b.x); a.y = __fadd_rn(a.y, b.y); a.z = __fadd_rn(a.z, b.z); a.w = __fadd_rn(a.w, b.w);
+    };
     if (col < d) {
-        for (int i = warp; i < n_partial; i += 32)
+        const float* at = partial + col;
+        for (int i = warp; i < n_partial; i += 8 * kGainWarps) {
+            float4 v[8];
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (i + 8 * k < n_partial) s[k] = __fadd_rn(s[k], __ldcg(partial + static_cast<int64_t>(i + 8 * k) * d + col));
+            for (int k = 0; k < 8; ++k) {
+                const int row = min(i + k * kGainWarps, n_partial - 1);
+                v[k] = __ldcg(reinterpret_cast<const float4*>(at + static_cast<int64_t>(row) * d));
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (i + k * kGainWarps < n_partial) add(sum, v[k]);
+        }
     }
-    part[warp][threadIdx.x & 31] = __fadd_rn(__fadd_rn(s[0], s[1]), __fadd_rn(s[2], s[3]));
+    part[warp][lane] = sum;
     __syncthreads();
-    if (warp == 0 && col < d) {
-        float v = part[0][threadIdx.x];
+    if (threadIdx.x < 128 && blockIdx.x * 128 + threadIdx.x < d) {
+        const float* mine = reinterpret_cast<const float*>(part) + threadIdx.x;
+        float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int k = 1; k < 8; ++k) v = __fadd_rn(v, part[k][threadIdx.x]);
-        d_gain[col] = v;
+        for (int k = 0; k < kGainWarps; ++k) v[k & 3] = __fadd_rn(v[k & 3], mine[128 * k]);
+        d_gain[blockIdx.x * 128 + threadIdx.x] = __fadd_rn(__fadd_rn(v[0], v[1]), __fadd_rn(v[2], v[3]));
     }
 }
 
@@ -485,7 +502,7 @@ extern "C" int fp8mlp_rmsnorm_backward(int64_t T, int64_t d, int dtype, const vo
     FP8MLP_CUDA_CHECK(FP8MLP_NORM_LAUNCH(launch_norm_backward, a, smem, grid, st));
     count_launch();
     if (d_gain != nullptr) {
-        FP8MLP_CUDA_CHECK(launch_chained(norm_gain_kernel, dim3(static_cast<unsigned>((d + 31) / 32)), dim3(256), 0, st,
+        FP8MLP_CUDA_CHECK(launch_chained(norm_gain_kernel, dim3(static_cast<unsigned>((d + 127) / 128)), dim3(32 * kGainWarps), 0, st,
                                          static_cast<const float*>(workspace), static_cast<int>(grid.x), static_cast<int>(d), d_gain));
         count_launch();
     }
