@@ -1088,22 +1088,32 @@ int make_tmap_out_f32(CUtensorMap* map, const void* base, uint64_t cols, uint64_
     return FP8MLP_OK;
 }
 
-int make_tmap_bytes(CUtensorMap* map, const void* base, uint64_t inner, uint64_t outer, uint64_t row_stride, uint32_t box_rows,
-                    bool swizzle) {
+namespace {
+int make_tmap_bytes(CUtensorMap* map, const void* base, uint32_t rank, const cuuint64_t* dims, const cuuint64_t* strides,
+                    const cuuint32_t* box, CUtensorMapSwizzle swizzle) {
     EncodeTiledFn fn = encode_fn();
     if (fn == nullptr) return FP8MLP_ERR_CUDA;
-    const cuuint64_t dims[2] = {inner, outer};
-    const cuuint64_t strides[1] = {row_stride};
-    const cuuint32_t box[2] = {128, box_rows};
-    const cuuint32_t elem[2] = {1, 1};
-    CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, elem,
-                    CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE,
-                    CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    const cuuint32_t elem[3] = {1, 1, 1};
+    CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, rank, const_cast<void*>(base), dims, strides, box, elem,
+                    CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r != CUDA_SUCCESS) {
         set_cuda_error_str("cuTensorMapEncodeTiled", "driver rejected the tensor map of a 4-bit operand");
         return FP8MLP_ERR_CUDA;
     }
     return FP8MLP_OK;
+}
+}  // namespace
+
+int make_tmap_fp4(CUtensorMap* map, const void* base, uint64_t row_bytes, uint64_t rows, uint64_t row_stride, uint32_t box_rows) {
+    const cuuint64_t dims[2] = {row_bytes, rows}, strides[1] = {row_stride};
+    const cuuint32_t box[2] = {128, box_rows};
+    return make_tmap_bytes(map, base, 2, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B);
+}
+
+int make_tmap_fp4_scales(CUtensorMap* map, const void* base, uint64_t tiles, uint64_t groups, uint32_t box_rows, uint32_t box_groups) {
+    const cuuint64_t dims[3] = {128, 4 * tiles, groups}, strides[2] = {128, 512 * tiles};
+    const cuuint32_t box[3] = {128, box_rows, box_groups};
+    return make_tmap_bytes(map, base, 3, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_NONE);
 }
 
 int make_tmap_u8(CUtensorMap* map, const void* base, uint64_t inner, uint64_t outer, uint64_t row_stride) {

@@ -6,15 +6,19 @@
 // P is A and Q is B, or the other way round where A has few rows: a product of one token with a large weight matrix is bound by
 // reading the weights, so their rows fill the 128 accumulator rows and the tokens are its 16 to 128 columns.
 //
-// A CTA is one TMA warp, one warp that issues the MMAs and 4 or 8 epilogue warps; two accumulators alternate, so that the
-// epilogue of a tile overlaps the main loop of the next.  A stage holds 256 columns of the contraction: 128 bytes of codes a
+// A CTA is one TMA warp, one warp that issues the MMAs and 4 or 8 epilogue warps.  At 384 cycles of MMAs a stage the loops of
+// the first two are what bounds the kernel: a wait that need not wait takes 100 cycles, so each asks for the next stage's
+// barrier before it issues the present stage and looks at the answer afterwards; the whole warp walks the loop and one elected lane
+// issues, for addresses and descriptors then are the warp's, as the tensor instructions need them (moving them over from a
+// lane's registers: 115 cycles for each of 10 to 16 instructions a stage).  A stage holds 256 columns of the contraction: 128 bytes of codes a
 // row, and the scales' tiles of 512 bytes as they lie in memory (32 rows of 16 bytes), which tcgen05.cp copies to the four lane
-// quadrants of 4 tensor-memory columns.  Tensor memory holds the scales of two to five stages: those
+// quadrants of 4 tensor-memory columns.  Tensor memory holds the scales of two stages or more: those
 // of a stage are copied once the MMAs that read their place last are done.
 //
 // Large products: CTA pairs on 256 x 192 tiles (cta_group::2; each CTA loads its 128 rows of P, half of the rows of Q, and the
-// scales of all of Q).  Products with fewer tiles than SMs: single CTAs on 128 x 16 .. 128 tiles, the contraction cut among
-// the 2, 4 or 8 CTAs of a cluster, which add their partial tiles over distributed shared memory in the order of their ranks.
+// scales of all of Q); two accumulators alternate, so that the epilogue of a tile overlaps the main loop of the next.  Others:
+// single CTAs, two to an SM, on one 128 x 16 .. 128 tile each; with few tiles the contraction is cut among the 2, 4 or 8 CTAs of a
+// cluster, which add their shares over distributed shared memory in the order of their ranks.
 // Every wait is bounded.
 #include "gemm.cuh"
 
@@ -28,11 +32,11 @@ constexpr int kRows = 128;                   // accumulator rows of a CTA
 constexpr int kStageK = 256;                 // columns of the contraction per stage
 constexpr int kStepK = 64;                   // and per MMA
 constexpr int kScaleTile = 512;              // 128 rows x 4 blocks
+constexpr uint32_t kAll = 0xffffffffu;
 
 struct Gemm4Args {
     int P, Q, K;
     int p_tiles, q_tiles, stages_k;          // stages_k: stages of the whole contraction
-    int p_scale_tiles, q_scale_tiles;        // scale tiles of a row group
     int split;                               // CTAs of a cluster that share a tile's contraction (at most stages_k)
     int group;                               // rasterisation: bands of this many p tiles
     int swap;                                // out is [Q, P]
@@ -49,16 +53,18 @@ template <int FMT, int TN, bool PAIR> struct Shape {
     static constexpr int kPBytes = kRows * 128, kQBytes = (PAIR ? TN / 2 : TN) * 128;
     static constexpr int kSfBytes = kTiles * kScaleTile;                  // per 128 rows
     static constexpr int kStageBytes = kPBytes + kQBytes + (1 + kQGroups) * kSfBytes;
-    static constexpr int kStages = PAIR ? 6 : TN == 128 ? 5 : TN == 64 ? 3 : 4;
+    // A pair runs for many tiles, with two accumulators; a single CTA has one tile and one accumulator, and shares its SM with
+    // another that works while it starts or ends.
+    static constexpr int kCtasPerSm = PAIR ? 1 : 2, kAccs = PAIR ? 2 : 1;
+    static constexpr int kStages = PAIR ? 6 : TN >= 64 ? 3 : 4;
     static constexpr int kEpiWarps = TN >= 64 ? 8 : 4;
-    static constexpr int kCtasPerSm = TN <= 64 ? 2 : 1;
     static constexpr int kThreads = 64 + 32 * kEpiWarps;
     static constexpr int kWarpCols = TN / (kEpiWarps / 4);                // columns of a tile that an epilogue warp drains
     static constexpr int kSfCols = 4 * kTiles * (1 + kQGroups);           // tensor-memory columns of a stage's scales
     // stages whose scales tensor memory holds at a time: as many as fit, at least two
-    static constexpr int kRoom = (512 / kCtasPerSm - 2 * TN) / kSfCols;
-    static constexpr int kSfSlots = kRoom < kStages - 1 ? kRoom : kStages - 1;
-    static constexpr int kCols = 2 * TN + kSfSlots * kSfCols;
+    static constexpr int kRoom = (512 / kCtasPerSm - kAccs * TN) / kSfCols;
+    static constexpr int kSfSlots = kRoom < kStages ? kRoom : kStages;
+    static constexpr int kCols = kAccs * TN + kSfSlots * kSfCols;
     static constexpr int kTmem = kCols <= 128 ? 128 : kCols <= 256 ? 256 : 512;
     static_assert(kSfSlots >= 2 && kCols <= 512 && kTmem * kCtasPerSm <= 512, "tensor memory");
 };
@@ -73,9 +79,9 @@ template <int FMT, int TN, bool PAIR>
 constexpr size_t smem4_bytes() {
     return 1024 + size_t(Shape<FMT, TN, PAIR>::kStages) * Shape<FMT, TN, PAIR>::kStageBytes + sizeof(Tail4);
 }
-static_assert(smem4_bytes<FP8MLP_NVFP4, 192, true>() <= 232448 && smem4_bytes<FP8MLP_NVFP4, 128, false>() <= 232448, "shared memory");
-static_assert(2 * (smem4_bytes<FP8MLP_NVFP4, 64, false>() + 1024) <= 233472 && 2 * (smem4_bytes<FP8MLP_NVFP4, 32, false>() + 1024) <= 233472,
-              "two CTAs of the narrow tiles share an SM");
+static_assert(smem4_bytes<FP8MLP_NVFP4, 192, true>() <= 232448, "shared memory");
+static_assert(2 * (smem4_bytes<FP8MLP_NVFP4, 128, false>() + 1024) <= 233472 && 2 * (smem4_bytes<FP8MLP_NVFP4, 32, false>() + 1024) <= 233472,
+              "two single CTAs share an SM");
 
 // Matrix descriptors: address / 16 in the low 14 bits, then (bit 16) a leading offset that neither layout uses, and in the
 // upper half the distance of 8-row groups / 16, the version and the swizzle.
@@ -86,6 +92,20 @@ __device__ __forceinline__ uint64_t operand_desc(uint32_t addr16) {
 // A tile of scales, 32 rows of 16 bytes one after the other, no swizzle: 8-row groups 128 bytes apart.
 __device__ __forceinline__ uint64_t scales_desc(uint32_t addr16) {
     return (uint64_t((128u >> 4) | (1u << 14)) << 32) | (addr16 | (1u << 16));
+}
+// The place in the ring of stages and the parity of its round.
+template <int N> struct Ring {
+    uint32_t stage = 0, phase = 0;
+    __device__ __forceinline__ void next() {
+        if (++stage == N) { stage = 0; phase ^= 1u; }
+    }
+};
+// Whether a barrier's phase is complete, without waiting for it.
+__device__ __forceinline__ bool mbar_peek(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}\n"
+                 : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok != 0;
 }
 __device__ __forceinline__ uint32_t elect_one() {
     uint32_t r;
@@ -117,6 +137,18 @@ template <int FMT, int TN, bool PAIR>
 __device__ __forceinline__ uint32_t idesc4(uint32_t sf_byte) {
     return (sf_byte << 4) | (1u << 7) | (1u << 10) | (uint32_t(TN >> 3) << 17) | (uint32_t(FMT == FP8MLP_MXFP4 ? 1 : 0) << 23) |
            (uint32_t((PAIR ? 256 : 128) >> 4) << 24) | (sf_byte << 29);
+}
+
+// Scales are a tensor of 128-byte rows, four to a tile, by the tiles of a row group, by the row groups.
+__device__ __forceinline__ void tma_load_3d(uint32_t smem_dst, const CUtensorMap* m, uint32_t bar, int32_t x, int32_t y, int32_t z) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+        ::"r"(smem_dst), "l"(reinterpret_cast<uint64_t>(m)), "r"(bar), "r"(x), "r"(y), "r"(z) : "memory");
+}
+__device__ __forceinline__ void tma_load_3d_pair(uint32_t smem_dst, const CUtensorMap* m, uint32_t bar_cluster, int32_t x, int32_t y, int32_t z) {
+    asm volatile(
+        "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+        ::"r"(smem_dst), "l"(reinterpret_cast<uint64_t>(m)), "r"(bar_cluster), "r"(x), "r"(y), "r"(z) : "memory");
 }
 
 // The scale copies and MMAs of one stage (FULL: all 256 columns of it; else the `left` that there are).
@@ -257,74 +289,85 @@ gemm4_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_constant__ CU
 
     if (warp == 0) {
         // ------------------------------------------------------------ TMA producer
-        if (lane == 0) {
-            uint32_t stage = 0, phase = 0;
-            bool ok = true;
-            for (int tile = first_tile; ok && tile < num_tiles; tile += tile_step) {
-                int p_tile, q_tile;
-                tile4_coords(p, tile, p_tile, q_tile);
-                const int p_group = PAIR ? 2 * p_tile + static_cast<int>(rank) : p_tile, p0 = p_group * kRows;
-                const int q0 = q_tile * TN, q_first = q0 + (PAIR ? static_cast<int>(rank) * (TN / 2) : 0), q_group = q0 / kRows;
-                for (int kb = kb_begin; kb < kb_end; ++kb) {
-                    if (!mbar_wait(smem_u32(&tail->empty[stage]), phase ^ 1u, abort_flag, nullptr)) { ok = false; break; }
-                    const uint32_t dst = tiles_addr + stage * kStageBytes, sf = dst + S::kPBytes + S::kQBytes;
-                    const uint32_t own = smem_u32(&tail->full[stage]);
-                    const uint32_t bar = PAIR ? mapa_shared(own, 0) : own;         // a pair's bytes are counted by rank 0
-                    if (!PAIR || rank == 0) mbar_expect_tx(own, (PAIR ? 2 : 1) * kStageBytes);
-                    auto load = [&](uint32_t to, const CUtensorMap* map, int x, int y) {
-                        if constexpr (PAIR) tma_load_2d_pair(to, map, bar, x, y); else tma_load_2d(to, map, bar, x, y);
-                    };
-                    load(dst, &tmP, kb * (kStageK / 2), p0);
-                    load(dst + S::kPBytes, &tmQ, kb * (kStageK / 2), q_first);
-                    // a tile of scales is 4 rows of 128 bytes of its map; a last stage may read tiles of the next row group,
-                    // which no MMA uses
-                    load(sf, &tmSfP, 0, (p_group * p.p_scale_tiles + kb * S::kTiles) * 4);
-#pragma unroll
-                    for (int j = 0; j < S::kQGroups; ++j)
-                        load(sf + (1 + j) * S::kSfBytes, &tmSfQ, 0, ((q_group + j) * p.q_scale_tiles + kb * S::kTiles) * 4);
-                    if (++stage == kStages) { stage = 0; phase ^= 1u; }
+        const uint32_t leader = elect_one();
+        Ring<kStages> ring;
+        bool ok = true, ready = false;
+        for (int tile = first_tile; ok && tile < num_tiles; tile += tile_step) {
+            int p_tile, q_tile;
+            tile4_coords(p, tile, p_tile, q_tile);
+            const int p_group = PAIR ? 2 * p_tile + static_cast<int>(rank) : p_tile, p0 = p_group * kRows;
+            const int q0 = q_tile * TN, q_first = q0 + (PAIR ? static_cast<int>(rank) * (TN / 2) : 0), q_group = q0 / kRows;
+            for (int kb = kb_begin; kb < kb_end; ++kb) {
+                if (!ready) {
+                    ok = __all_sync(kAll, mbar_wait(smem_u32(&tail->empty[ring.stage]), ring.phase ^ 1u, abort_flag, nullptr));
+                    if (!ok) break;
                 }
+                const uint32_t dst = tiles_addr + ring.stage * kStageBytes, sf = dst + S::kPBytes + S::kQBytes;
+                const uint32_t own = smem_u32(&tail->full[ring.stage]);
+                ring.next();
+                const bool free = mbar_peek(smem_u32(&tail->empty[ring.stage]), ring.phase ^ 1u);
+                if (leader) {
+                    if constexpr (PAIR) {
+                        const uint32_t bar = mapa_shared(own, 0);                  // a pair's bytes are counted by rank 0
+                        if (rank == 0) mbar_expect_tx(own, 2 * kStageBytes);
+                        tma_load_2d_pair(dst, &tmP, bar, kb * (kStageK / 2), p0);
+                        tma_load_2d_pair(dst + S::kPBytes, &tmQ, bar, kb * (kStageK / 2), q_first);
+                        tma_load_3d_pair(sf, &tmSfP, bar, 0, kb * S::kTiles * 4, p_group);
+                        tma_load_3d_pair(sf + S::kSfBytes, &tmSfQ, bar, 0, kb * S::kTiles * 4, q_group);
+                    } else {
+                        mbar_expect_tx(own, kStageBytes);
+                        tma_load_2d(dst, &tmP, own, kb * (kStageK / 2), p0);
+                        tma_load_2d(dst + S::kPBytes, &tmQ, own, kb * (kStageK / 2), q_first);
+                        tma_load_3d(sf, &tmSfP, own, 0, kb * S::kTiles * 4, p_group);
+                        tma_load_3d(sf + S::kSfBytes, &tmSfQ, own, 0, kb * S::kTiles * 4, q_group);
+                    }
+                }
+                ready = __all_sync(kAll, free);
             }
         }
     } else if (warp == 1) {
         // ------------------------------------------------------------ MMA issuer (CTA pair: rank 0 only)
-        // The whole warp walks the loop and one elected lane issues: addresses and descriptors then are the warp's, not a
-        // lane's, which the tensor instructions need (moving them over from a lane's registers took longer than the MMAs: 10 to
-        // 16 instructions a stage).
         if (!PAIR || rank == 0u) {
             const uint32_t leader = elect_one();
-            uint32_t stage = 0, phase = 0, count = 0;
-            bool ok = true;
+            Ring<kStages> ring;
+            uint32_t count = 0;
+            bool ok = true, ready = false;
             int it = 0;
             for (int tile = first_tile; ok && tile < num_tiles; tile += tile_step, ++it) {
                 int p_tile, q_tile;
                 tile4_coords(p, tile, p_tile, q_tile);
-                const uint32_t acc = it & 1, acc_phase = (it >> 1) & 1;
-                if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(&tail->tmem_empty[acc]), acc_phase ^ 1u, abort_flag, nullptr))) break;
+                const uint32_t acc = it % S::kAccs, acc_phase = (it / S::kAccs) & 1;
+                if (!__all_sync(kAll, mbar_wait(smem_u32(&tail->tmem_empty[acc]), acc_phase ^ 1u, abort_flag, nullptr))) break;
                 tc_fence_after();
                 const uint32_t d_tmem = tmem_base + acc * TN;
                 const uint32_t q_offset = static_cast<uint32_t>((q_tile * TN) % kRows) / 32u;     // first column of the tile's scales
-                for (int kb = kb_begin; kb < kb_end; ++kb, ++count) {
-                    bool go = mbar_wait(smem_u32(&tail->full[stage]), phase, abort_flag, nullptr);
-                    if (count >= S::kSfSlots) {        // the scales' columns: free once the MMAs that read them last are done
-                        const uint32_t before = stage >= S::kSfSlots ? stage - S::kSfSlots : stage + kStages - S::kSfSlots;
-                        const uint32_t parity = ((count - S::kSfSlots) / kStages) & 1u;
-                        go = go && mbar_wait(smem_u32(&tail->empty[before]), parity, abort_flag, nullptr);
+                for (int kb = kb_begin; kb < kb_end; ++kb) {
+                    // The scales' columns of this stage are free once the MMAs that read them last are done.  With as many
+                    // places as stages the stage's own barriers say so: it was not filled again before.
+                    auto scales_free = [&](bool wait) {
+                        if (S::kSfSlots == kStages || count < S::kSfSlots) return true;
+                        const uint32_t before = ring.stage >= S::kSfSlots ? ring.stage - S::kSfSlots : ring.stage + kStages - S::kSfSlots;
+                        const uint32_t bar = smem_u32(&tail->empty[before]), parity = ((count - S::kSfSlots) / kStages) & 1u;
+                        return wait ? mbar_wait(bar, parity, abort_flag, nullptr) : mbar_peek(bar, parity);
+                    };
+                    if (!ready) {
+                        ok = __all_sync(kAll, mbar_wait(smem_u32(&tail->full[ring.stage]), ring.phase, abort_flag, nullptr) && scales_free(true));
+                        if (!ok) break;
                     }
-                    ok = __all_sync(0xffffffffu, go);
-                    if (!ok) break;
                     tc_fence_after();
-                    const uint32_t sf_p = tmem_base + 2 * TN + (count % S::kSfSlots) * S::kSfCols, sf_q = sf_p + 4 * S::kTiles;
-                    const uint32_t base = (tiles_addr + stage * kStageBytes) >> 4;        // descriptors count in 16 bytes
-                    const uint32_t sf_base = base + ((S::kPBytes + S::kQBytes) >> 4);
+                    const uint32_t sf_p = tmem_base + S::kAccs * TN + (count % S::kSfSlots) * S::kSfCols, sf_q = sf_p + 4 * S::kTiles;
+                    const uint32_t base = (tiles_addr + ring.stage * kStageBytes) >> 4;        // descriptors count in 16 bytes
+                    const uint32_t sf_base = base + ((S::kPBytes + S::kQBytes) >> 4), done = smem_u32(&tail->empty[ring.stage]);
+                    ring.next();
+                    ++count;
+                    const bool filled = mbar_peek(smem_u32(&tail->full[ring.stage]), ring.phase), room = scales_free(false);
                     if (leader) {
                         const int left = p.K - kb * kStageK;
                         if (left >= kStageK) issue_stage<FMT, TN, PAIR, true>(d_tmem, base, sf_base, sf_p, sf_q, q_offset, kb != kb_begin, left);
                         else issue_stage<FMT, TN, PAIR, false>(d_tmem, base, sf_base, sf_p, sf_q, q_offset, kb != kb_begin, left);
-                        if constexpr (PAIR) umma_commit_pair(smem_u32(&tail->empty[stage])); else umma_commit(smem_u32(&tail->empty[stage]));
+                        if constexpr (PAIR) umma_commit_pair(done); else umma_commit(done);
                     }
-                    __syncwarp();
-                    if (++stage == kStages) { stage = 0; phase ^= 1u; }
+                    ready = __all_sync(kAll, filled && room);
                 }
                 if (ok && leader) {
                     if constexpr (PAIR) umma_commit_pair(smem_u32(&tail->tmem_full[acc])); else umma_commit(smem_u32(&tail->tmem_full[acc]));
@@ -336,14 +379,14 @@ gemm4_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_constant__ CU
         // ------------------------------------------------------------ epilogue
         const int quad = warp & 3, part = (warp - 2) >> 2;
         const float dq = __fmul_rn(p.s0 != nullptr ? __fdiv_rn(1.0f, *p.s0) : 1.0f, p.s1 != nullptr ? __fdiv_rn(1.0f, *p.s1) : 1.0f);
-        constexpr int kChunk = S::kWarpCols < 32 ? 16 : 32;
+        constexpr int kChunk = S::kWarpCols < 32 ? 16 : 32, kShareRows = kRows + 4, kShareCols = TN + 4;
         int it = 0;
         for (int tile = first_tile; tile < num_tiles; tile += tile_step, ++it) {
             int p_tile, q_tile;
             tile4_coords(p, tile, p_tile, q_tile);
-            const uint32_t acc = it & 1, acc_phase = (it >> 1) & 1;
+            const uint32_t acc = it % S::kAccs, acc_phase = (it / S::kAccs) & 1;
             const bool got = mbar_wait(smem_u32(&tail->tmem_full[acc]), acc_phase, abort_flag, nullptr);
-            if (!__all_sync(0xffffffffu, got)) break;
+            if (!__all_sync(kAll, got)) break;
             tc_fence_after();
             const uint32_t taddr = tmem_base + acc * TN + part * S::kWarpCols + (static_cast<uint32_t>(quad * 32) << 16);
             const int row = (PAIR ? 2 * p_tile + static_cast<int>(rank) : p_tile) * kRows + quad * 32 + lane;
@@ -355,10 +398,19 @@ gemm4_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_constant__ CU
                 tmem_ld_cols<kChunk>(taddr + c, r);
                 tmem_ld_wait();
                 if (p.split > 1) {
-                    // this share of the tile into shared memory, [column][row]; every operand stage has been read
-                    float* mine = reinterpret_cast<float*>(smem_raw + (tiles_addr - raw_addr)) + (part * S::kWarpCols + c) * kRows + quad * 32 + lane;
+                    // this share of the tile into shared memory (every operand stage has been read), in the order of the output's
+                    // rows: [column][accumulator row] if the output is [Q, P], else [accumulator row][column]
+                    float* share = reinterpret_cast<float*>(smem_raw + (tiles_addr - raw_addr));
+                    const int first = part * S::kWarpCols + c, mine = quad * 32 + lane;
+                    if (p.swap) {
 #pragma unroll
-                    for (int i = 0; i < kChunk; ++i) mine[i * kRows] = __uint_as_float(r[i]);
+                        for (int i = 0; i < kChunk; ++i) share[(first + i) * kShareRows + mine] = __uint_as_float(r[i]);
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < kChunk; i += 4)
+                            *reinterpret_cast<float4*>(share + mine * kShareCols + first + i) =
+                                make_float4(__uint_as_float(r[i]), __uint_as_float(r[i + 1]), __uint_as_float(r[i + 2]), __uint_as_float(r[i + 3]));
+                    }
                     continue;
                 }
                 if (row >= p.P) continue;
@@ -395,20 +447,36 @@ gemm4_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_constant__ CU
         int p_tile, q_tile;
         tile4_coords(p, first_tile, p_tile, q_tile);
         const int cols = min(TN, p.Q - q_tile * TN), rows = min(kRows, p.P - p_tile * kRows);
-        // this CTA's part of the tile's cols x 128 words, each the sum of the shares in rank order
-        for (int i = static_cast<int>(rank) * S::kThreads + threadIdx.x; i < cols * kRows; i += p.split * S::kThreads) {
-            // the order of the words follows the output's rows
-            const int c = p.swap ? i / kRows : i % cols, r = p.swap ? i % kRows : i / cols;
-            if (r >= rows) continue;
-            const uint32_t at = tiles_addr + 4u * static_cast<uint32_t>(c * kRows + r);
-            float v = 0.0f;
-            for (int s = 0; s < p.split; ++s) {
-                float w;
-                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(w) : "r"(mapa_shared(at, s)) : "memory");
-                v = s == 0 ? w : __fadd_rn(v, w);
+        // rows of the output, four words of one at a time; this CTA's part of them, each the sum of the shares in rank order
+        const int lines = p.swap ? cols : rows, len = p.swap ? rows : cols, pitch = p.swap ? kRows + 4 : TN + 4;
+        const int quads = (len + 3) / 4;
+        const int64_t line0 = p.swap ? int64_t(q_tile) * TN : int64_t(p_tile) * kRows, word0 = p.swap ? int64_t(p_tile) * kRows : int64_t(q_tile) * TN;
+        for (int i = static_cast<int>(rank) * S::kThreads + threadIdx.x; i < lines * quads; i += p.split * S::kThreads) {
+            const int line = i / quads, word = 4 * (i - line * quads);
+            const uint32_t at = tiles_addr + 4u * static_cast<uint32_t>(line * pitch + word);
+            float4 v[8];
+#pragma unroll
+            for (int s = 0; s < 8; ++s)
+                if (s < p.split)
+                    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                                 : "=f"(v[s].x), "=f"(v[s].y), "=f"(v[s].z), "=f"(v[s].w) : "r"(mapa_shared(at, s)) : "memory");
+            float4 sum = v[0];
+#pragma unroll
+            for (int s = 1; s < 8; ++s)
+                if (s < p.split) {
+                    sum.x = __fadd_rn(sum.x, v[s].x); sum.y = __fadd_rn(sum.y, v[s].y);
+                    sum.z = __fadd_rn(sum.z, v[s].z); sum.w = __fadd_rn(sum.w, v[s].w);
+                }
+            const float out[4] = {__fmul_rn(sum.x, dq), __fmul_rn(sum.y, dq), __fmul_rn(sum.z, dq), __fmul_rn(sum.w, dq)};
+            const int64_t to = (line0 + line) * p.ld_out + word0 + word;
+            if (p.vec >= 16 && word + 4 <= len) {
+                if (p.f32) st_global_v4(reinterpret_cast<float*>(p.out) + to, __float_as_uint(out[0]), __float_as_uint(out[1]), __float_as_uint(out[2]), __float_as_uint(out[3]));
+                else st_global_v2(reinterpret_cast<uint16_t*>(p.out) + to, cvt_bf16x2(out[0], out[1]), cvt_bf16x2(out[2], out[3]));
+            } else {
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (word + k < len) store_one(p, to + k, out[k]);
             }
-            const int64_t row = p_tile * kRows + r, col = q_tile * TN + c;
-            store_one(p, p.swap ? col * p.ld_out + row : row * p.ld_out + col, __fmul_rn(v, dq));
         }
     }
     if (PAIR || p.split > 1) cluster_sync_all();              // nobody leaves while its memory can be reached
@@ -462,11 +530,8 @@ int launch4(const CUtensorMap (&tm)[4], const Gemm4Args& a, int sm_count, cudaSt
     if (PAIR) {
         if (clusters_dev[dev] < 1) { set_cuda_error_str("4-bit product", "no CTA pair fits on the device"); return FP8MLP_ERR_CUDA; }
         grid = 2 * (tiles < clusters_dev[dev] ? tiles : clusters_dev[dev]);
-    } else if (a.split > 1) {
-        grid = tiles * a.split;                               // a tile per cluster
     } else {
-        const int64_t most = static_cast<int64_t>(sm_count) * S::kCtasPerSm;
-        grid = tiles < most ? tiles : most;
+        grid = tiles * a.split;                               // a tile per CTA or cluster
     }
     cfg.gridDim = dim3(static_cast<unsigned>(grid));
     FP8MLP_CUDA_CHECK(cudaLaunchKernelEx(&cfg, gemm4_kernel<FMT, TN, PAIR>, tm[0], tm[1], tm[2], tm[3], a));
@@ -487,7 +552,7 @@ Plan4 plan4(int64_t M, int64_t N, int64_t K, int sms) {
     pl.swap = shorter <= 128 && M < N;
     pl.tn = shorter <= 16 ? 16 : shorter <= 32 ? 32 : shorter <= 64 ? 64 : 128;
     const int64_t P = pl.swap ? N : M, Q = pl.swap ? M : N;
-    const int64_t tiles = (P + 127) / 128 * ((Q + pl.tn - 1) / pl.tn), room = static_cast<int64_t>(sms) * (pl.tn <= 64 ? 2 : 1);
+    const int64_t tiles = (P + 127) / 128 * ((Q + pl.tn - 1) / pl.tn), room = static_cast<int64_t>(sms) * 2;
     const int64_t stages = (K + kStageK - 1) / kStageK;
     pl.split = 8;
     while (pl.split > 1 && (tiles * pl.split > room || stages < 2 * pl.split)) pl.split /= 2;
@@ -522,8 +587,6 @@ extern "C" int fp8mlp_gemm_fp4(int64_t M, int64_t N, int64_t K, int fmt, const u
     if (ld_a % 16 != 0 || ld_b % 16 != 0 || ld_a < row || ld_b < row || (M > 1 && ld_out < N)) return FP8MLP_ERR_SHAPE;
     const int block = fmt == FP8MLP_MXFP4 ? 32 : 16;
     const int64_t scale_tiles = (K + 4 * block - 1) / (4 * block);
-    // coordinates of the scales' tensor maps are 32-bit row numbers of 128 bytes
-    if (((M > N ? M : N) + 127) / 128 * scale_tiles * 4 > INT32_MAX) return FP8MLP_ERR_SHAPE;
     if ((M + 127) / 128 * ((N + 15) / 16) > INT32_MAX / 8) return FP8MLP_ERR_SHAPE;
     if (M == 0 || N == 0) return FP8MLP_OK;
     if (A == nullptr || a_scales == nullptr || B == nullptr || b_scales == nullptr || out == nullptr) return FP8MLP_ERR_ARG;
@@ -540,21 +603,20 @@ extern "C" int fp8mlp_gemm_fp4(int64_t M, int64_t N, int64_t K, int fmt, const u
     CUtensorMap tm[4];
     const uint64_t row_bytes = static_cast<uint64_t>((K + 1) / 2);
     const uint32_t sf_rows = 4u * kStageK / (4u * block);                     // 128-byte rows of a stage's scales
-    auto codes_map = [&](CUtensorMap* m, const Side& s, uint32_t box) { return make_tmap_bytes(m, s.codes, row_bytes, s.rows, s.ld, box, true); };
-    auto scales_map = [&](CUtensorMap* m, const Side& s) {
-        return make_tmap_bytes(m, s.scales, 128, static_cast<uint64_t>((s.rows + 127) / 128 * scale_tiles * 4), 128, sf_rows, false);
+    auto codes_map = [&](CUtensorMap* m, const Side& s, uint32_t box) { return make_tmap_fp4(m, s.codes, row_bytes, s.rows, s.ld, box); };
+    auto scales_map = [&](CUtensorMap* m, const Side& s, uint32_t groups) {
+        return make_tmap_fp4_scales(m, s.scales, static_cast<uint64_t>(scale_tiles), static_cast<uint64_t>((s.rows + 127) / 128), sf_rows, groups);
     };
     int rc = codes_map(&tm[0], P, kRows);
     if (rc == FP8MLP_OK) rc = codes_map(&tm[1], Q, pl.pair ? pl.tn / 2 : pl.tn);
-    if (rc == FP8MLP_OK) rc = scales_map(&tm[2], P);
-    if (rc == FP8MLP_OK) rc = scales_map(&tm[3], Q);
+    if (rc == FP8MLP_OK) rc = scales_map(&tm[2], P, 1);
+    if (rc == FP8MLP_OK) rc = scales_map(&tm[3], Q, (pl.tn + 127) / 128);
     if (rc != FP8MLP_OK) return rc;
     Gemm4Args a{};
     a.P = static_cast<int>(P.rows); a.Q = static_cast<int>(Q.rows); a.K = static_cast<int>(K);
     a.p_tiles = (a.P + (pl.pair ? 255 : 127)) / (pl.pair ? 256 : 128);
     a.q_tiles = (a.Q + pl.tn - 1) / pl.tn;
     a.stages_k = static_cast<int>((K + kStageK - 1) / kStageK);
-    a.p_scale_tiles = a.q_scale_tiles = static_cast<int>(scale_tiles);
     a.split = pl.split;
     a.group = 16;
     a.swap = pl.swap ? 1 : 0;
