@@ -6,11 +6,12 @@
 // P is A and Q is B, or the other way round where A has few rows: a product of one token with a large weight matrix is bound by
 // reading the weights, so their rows fill the 128 accumulator rows and the tokens are its 16 to 128 columns.
 //
-// A CTA is one TMA warp, one warp that issues the MMAs and 4 or 8 epilogue warps.  At 384 cycles of MMAs a stage the loops of
-// the first two are what bounds the kernel: a wait that need not wait takes 100 cycles, so each asks for the next stage's
-// barrier before it issues the present stage and looks at the answer afterwards; the whole warp walks the loop and one elected lane
-// issues, for addresses and descriptors then are the warp's, as the tensor instructions need them (moving them over from a
-// lane's registers: 115 cycles for each of 10 to 16 instructions a stage).  A stage holds 256 columns of the contraction: 128 bytes of codes a
+// A CTA is two TMA warps, which take turns, one warp that issues the MMAs and 4 or 8 epilogue warps.  At 384 cycles of MMAs a
+// stage, the loops of the first three are what bounds the kernel: a wait takes 100 cycles though nothing is to be waited for, a
+// stage's loads 290.  So the MMA warp has one barrier to look at, asks for the next stage's before it issues the present stage, and
+// all of it walks the loop while one elected lane issues, for addresses and descriptors then are the warp's, as the tensor
+// instructions need them (moving them over from a lane's registers: 115 cycles for each of 10 to 16 instructions a stage).
+// A stage holds 256 columns of the contraction: 128 bytes of codes a
 // row, and the scales' tiles of 512 bytes as they lie in memory (32 rows of 16 bytes), which tcgen05.cp copies to the four lane
 // quadrants of 4 tensor-memory columns.  Tensor memory holds the scales of two stages or more: those
 // of a stage are copied once the MMAs that read their place last are done.
@@ -33,6 +34,7 @@ constexpr int kStageK = 256;                 // columns of the contraction per s
 constexpr int kStepK = 64;                   // and per MMA
 constexpr int kScaleTile = 512;              // 128 rows x 4 blocks
 constexpr uint32_t kAll = 0xffffffffu;
+constexpr int kOtherWarps = 3;               // two TMA producers, the MMA issuer
 
 struct Gemm4Args {
     int P, Q, K;
@@ -58,12 +60,12 @@ template <int FMT, int TN, bool PAIR> struct Shape {
     static constexpr int kCtasPerSm = PAIR ? 1 : 2, kAccs = PAIR ? 2 : 1;
     static constexpr int kStages = PAIR ? 6 : TN >= 64 ? 3 : 4;
     static constexpr int kEpiWarps = TN >= 64 ? 8 : 4;
-    static constexpr int kThreads = 64 + 32 * kEpiWarps;
+    static constexpr int kThreads = 32 * (kOtherWarps + kEpiWarps);
     static constexpr int kWarpCols = TN / (kEpiWarps / 4);                // columns of a tile that an epilogue warp drains
     static constexpr int kSfCols = 4 * kTiles * (1 + kQGroups);           // tensor-memory columns of a stage's scales
     // stages whose scales tensor memory holds at a time: as many as fit, at least two
     static constexpr int kRoom = (512 / kCtasPerSm - kAccs * TN) / kSfCols;
-    static constexpr int kSfSlots = kRoom < kStages ? kRoom : kStages;
+    static constexpr int kSfSlots = kRoom < kStages ? kRoom : kStages, kLag = kStages - kSfSlots;
     static constexpr int kCols = kAccs * TN + kSfSlots * kSfCols;
     static constexpr int kTmem = kCols <= 128 ? 128 : kCols <= 256 ? 256 : 512;
     static_assert(kSfSlots >= 2 && kCols <= 512 && kTmem * kCtasPerSm <= 512, "tensor memory");
@@ -276,7 +278,7 @@ gemm4_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_constant__ CU
         tail->abort = 0;
         mbar_init_fence();
     }
-    if (warp == 1) {
+    if (warp == 2) {
         if constexpr (PAIR) { tmem_alloc_pair(smem_u32(&tail->tmem_base), S::kTmem); tmem_relinquish_pair(); }
         else { tmem_alloc(smem_u32(&tail->tmem_base), S::kTmem); tmem_relinquish(); }
     }
@@ -287,50 +289,45 @@ gemm4_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_constant__ CU
     grid_dependency_wait();
     grid_launch_dependents();
 
-    if (warp == 0) {
-        // ------------------------------------------------------------ TMA producer
-        const uint32_t leader = elect_one();
-        Ring<kStages> ring;
-        bool ok = true, ready = false;
-        for (int tile = first_tile; ok && tile < num_tiles; tile += tile_step) {
-            int p_tile, q_tile;
+    if (warp < 2) {
+        // ------------------------------------------------------------ TMA producers: every other stage each
+        // A stage's barrier is armed, so that it can complete, kLag stages after its loads were issued: then the stage whose
+        // scales it overwrites in tensor memory is known to be done, and the MMA warp has one barrier to wait for, not two.
+        if (lane == 0) {
+            const int per_tile = kb_end - kb_begin, my_tiles = first_tile < num_tiles ? (num_tiles - 1 - first_tile) / tile_step + 1 : 0;
+            const uint32_t total = static_cast<uint32_t>(per_tile) * my_tiles;
+            int tile = first_tile, kb = kb_begin + warp, p_tile, q_tile;
             tile4_coords(p, tile, p_tile, q_tile);
-            const int p_group = PAIR ? 2 * p_tile + static_cast<int>(rank) : p_tile, p0 = p_group * kRows;
-            const int q0 = q_tile * TN, q_first = q0 + (PAIR ? static_cast<int>(rank) * (TN / 2) : 0), q_group = q0 / kRows;
-            for (int kb = kb_begin; kb < kb_end; ++kb) {
-                if (!ready) {
-                    ok = __all_sync(kAll, mbar_wait(smem_u32(&tail->empty[ring.stage]), ring.phase ^ 1u, abort_flag, nullptr));
-                    if (!ok) break;
+            for (uint32_t n = warp; n < total + S::kLag; n += 2, kb += 2) {
+                const uint32_t stage = n % kStages, parity = (n / kStages) & 1u;
+                if (!mbar_wait(smem_u32(&tail->empty[stage]), parity ^ 1u, abort_flag, nullptr)) break;
+                if ((!PAIR || rank == 0) && n + 1 > S::kLag)         // a pair's bytes are counted by rank 0
+                    mbar_expect_tx(smem_u32(&tail->full[(n - S::kLag) % kStages]), (PAIR ? 2 : 1) * kStageBytes);
+                if (n >= total) continue;
+                while (kb >= kb_end) { kb -= per_tile; tile += tile_step; tile4_coords(p, tile, p_tile, q_tile); }
+                const int p_group = PAIR ? 2 * p_tile + static_cast<int>(rank) : p_tile, p0 = p_group * kRows;
+                const int q0 = q_tile * TN, q_first = q0 + (PAIR ? static_cast<int>(rank) * (TN / 2) : 0), q_group = q0 / kRows;
+                const uint32_t dst = tiles_addr + stage * kStageBytes, sf = dst + S::kPBytes + S::kQBytes;
+                const uint32_t bar = PAIR ? mapa_shared(smem_u32(&tail->full[stage]), 0) : smem_u32(&tail->full[stage]);
+                if constexpr (PAIR) {
+                    tma_load_2d_pair(dst, &tmP, bar, kb * (kStageK / 2), p0);
+                    tma_load_2d_pair(dst + S::kPBytes, &tmQ, bar, kb * (kStageK / 2), q_first);
+                    tma_load_3d_pair(sf, &tmSfP, bar, 0, kb * S::kTiles * 4, p_group);
+                    tma_load_3d_pair(sf + S::kSfBytes, &tmSfQ, bar, 0, kb * S::kTiles * 4, q_group);
+                } else {
+                    tma_load_2d(dst, &tmP, bar, kb * (kStageK / 2), p0);
+                    tma_load_2d(dst + S::kPBytes, &tmQ, bar, kb * (kStageK / 2), q_first);
+                    tma_load_3d(sf, &tmSfP, bar, 0, kb * S::kTiles * 4, p_group);
+                    tma_load_3d(sf + S::kSfBytes, &tmSfQ, bar, 0, kb * S::kTiles * 4, q_group);
                 }
-                const uint32_t dst = tiles_addr + ring.stage * kStageBytes, sf = dst + S::kPBytes + S::kQBytes;
-                const uint32_t own = smem_u32(&tail->full[ring.stage]);
-                ring.next();
-                const bool free = mbar_peek(smem_u32(&tail->empty[ring.stage]), ring.phase ^ 1u);
-                if (leader) {
-                    if constexpr (PAIR) {
-                        const uint32_t bar = mapa_shared(own, 0);                  // a pair's bytes are counted by rank 0
-                        if (rank == 0) mbar_expect_tx(own, 2 * kStageBytes);
-                        tma_load_2d_pair(dst, &tmP, bar, kb * (kStageK / 2), p0);
-                        tma_load_2d_pair(dst + S::kPBytes, &tmQ, bar, kb * (kStageK / 2), q_first);
-                        tma_load_3d_pair(sf, &tmSfP, bar, 0, kb * S::kTiles * 4, p_group);
-                        tma_load_3d_pair(sf + S::kSfBytes, &tmSfQ, bar, 0, kb * S::kTiles * 4, q_group);
-                    } else {
-                        mbar_expect_tx(own, kStageBytes);
-                        tma_load_2d(dst, &tmP, own, kb * (kStageK / 2), p0);
-                        tma_load_2d(dst + S::kPBytes, &tmQ, own, kb * (kStageK / 2), q_first);
-                        tma_load_3d(sf, &tmSfP, own, 0, kb * S::kTiles * 4, p_group);
-                        tma_load_3d(sf + S::kSfBytes, &tmSfQ, own, 0, kb * S::kTiles * 4, q_group);
-                    }
-                }
-                ready = __all_sync(kAll, free);
             }
         }
-    } else if (warp == 1) {
+    } else if (warp == 2) {
         // ------------------------------------------------------------ MMA issuer (CTA pair: rank 0 only)
         if (!PAIR || rank == 0u) {
             const uint32_t leader = elect_one();
             Ring<kStages> ring;
-            uint32_t count = 0;
+            uint32_t slot = 0;
             bool ok = true, ready = false;
             int it = 0;
             for (int tile = first_tile; ok && tile < num_tiles; tile += tile_step, ++it) {
@@ -342,32 +339,24 @@ gemm4_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_constant__ CU
                 const uint32_t d_tmem = tmem_base + acc * TN;
                 const uint32_t q_offset = static_cast<uint32_t>((q_tile * TN) % kRows) / 32u;     // first column of the tile's scales
                 for (int kb = kb_begin; kb < kb_end; ++kb) {
-                    // The scales' columns of this stage are free once the MMAs that read them last are done.  With as many
-                    // places as stages the stage's own barriers say so: it was not filled again before.
-                    auto scales_free = [&](bool wait) {
-                        if (S::kSfSlots == kStages || count < S::kSfSlots) return true;
-                        const uint32_t before = ring.stage >= S::kSfSlots ? ring.stage - S::kSfSlots : ring.stage + kStages - S::kSfSlots;
-                        const uint32_t bar = smem_u32(&tail->empty[before]), parity = ((count - S::kSfSlots) / kStages) & 1u;
-                        return wait ? mbar_wait(bar, parity, abort_flag, nullptr) : mbar_peek(bar, parity);
-                    };
                     if (!ready) {
-                        ok = __all_sync(kAll, mbar_wait(smem_u32(&tail->full[ring.stage]), ring.phase, abort_flag, nullptr) && scales_free(true));
+                        ok = __all_sync(kAll, mbar_wait(smem_u32(&tail->full[ring.stage]), ring.phase, abort_flag, nullptr));
                         if (!ok) break;
                     }
                     tc_fence_after();
-                    const uint32_t sf_p = tmem_base + S::kAccs * TN + (count % S::kSfSlots) * S::kSfCols, sf_q = sf_p + 4 * S::kTiles;
+                    const uint32_t sf_p = tmem_base + S::kAccs * TN + slot * S::kSfCols, sf_q = sf_p + 4 * S::kTiles;
                     const uint32_t base = (tiles_addr + ring.stage * kStageBytes) >> 4;        // descriptors count in 16 bytes
                     const uint32_t sf_base = base + ((S::kPBytes + S::kQBytes) >> 4), done = smem_u32(&tail->empty[ring.stage]);
                     ring.next();
-                    ++count;
-                    const bool filled = mbar_peek(smem_u32(&tail->full[ring.stage]), ring.phase), room = scales_free(false);
+                    if (++slot == S::kSfSlots) slot = 0;
+                    const bool filled = mbar_peek(smem_u32(&tail->full[ring.stage]), ring.phase);
                     if (leader) {
                         const int left = p.K - kb * kStageK;
                         if (left >= kStageK) issue_stage<FMT, TN, PAIR, true>(d_tmem, base, sf_base, sf_p, sf_q, q_offset, kb != kb_begin, left);
                         else issue_stage<FMT, TN, PAIR, false>(d_tmem, base, sf_base, sf_p, sf_q, q_offset, kb != kb_begin, left);
                         if constexpr (PAIR) umma_commit_pair(done); else umma_commit(done);
                     }
-                    ready = __all_sync(kAll, filled && room);
+                    ready = __all_sync(kAll, filled);
                 }
                 if (ok && leader) {
                     if constexpr (PAIR) umma_commit_pair(smem_u32(&tail->tmem_full[acc])); else umma_commit(smem_u32(&tail->tmem_full[acc]));
@@ -377,7 +366,7 @@ gemm4_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_constant__ CU
         }
     } else {
         // ------------------------------------------------------------ epilogue
-        const int quad = warp & 3, part = (warp - 2) >> 2;
+        const int quad = warp & 3, part = (warp - kOtherWarps) >> 2;
         const float dq = __fmul_rn(p.s0 != nullptr ? __fdiv_rn(1.0f, *p.s0) : 1.0f, p.s1 != nullptr ? __fdiv_rn(1.0f, *p.s1) : 1.0f);
         constexpr int kChunk = S::kWarpCols < 32 ? 16 : 32, kShareRows = kRows + 4, kShareCols = TN + 4;
         int it = 0;
@@ -480,7 +469,7 @@ gemm4_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_constant__ CU
         }
     }
     if (PAIR || p.split > 1) cluster_sync_all();              // nobody leaves while its memory can be reached
-    if (warp == 1) {
+    if (warp == 2) {
         __syncwarp();
         tc_fence_after();
         if constexpr (PAIR) tmem_dealloc_pair(tmem_base, S::kTmem); else tmem_dealloc(tmem_base, S::kTmem);
