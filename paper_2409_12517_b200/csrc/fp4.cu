@@ -14,11 +14,10 @@ constexpr int kThreads = 256;
 constexpr int kTileRows = 128;            // operand rows of a block of threads, and of a tile of scales
 constexpr int kScaleTile = 512;           // bytes: 128 rows x 4 blocks
 constexpr int kCols = 256;                // operand columns of a block of threads, matrix as it is
-constexpr int kColsT = 128;               // the same for the transposed matrix
-
 template <int FMT> struct Fmt;
 template <> struct Fmt<FP8MLP_MXFP4> { static constexpr int kBlock = 32; };
 template <> struct Fmt<FP8MLP_NVFP4> { static constexpr int kBlock = 16; };
+
 
 struct QuantArgs {
     const uint8_t* src;
@@ -57,12 +56,13 @@ __device__ __forceinline__ uint32_t cvt_e2m1x8(const float (&v)[8]) {
 // two codes (a byte) -> two floats
 __device__ __forceinline__ void e2m1x2_to_f32(uint32_t byte, float& lo, float& hi) {
     uint32_t h2;
+    // (taken apart as 16 bits: with four bytes of a 32-bit register a byte loaded from memory came out as 0)
     asm("{\n\t"
-        ".reg .b8 a, b, c, d;\n\t"
-        "mov.b32 {a, b, c, d}, %1;\n\t"
+        ".reg .b8 a, b;\n\t"
+        "mov.b16 {a, b}, %1;\n\t"
         "cvt.rn.f16x2.e2m1x2 %0, a;\n\t"
         "}\n"
-        : "=r"(h2) : "r"(byte));
+        : "=r"(h2) : "h"(static_cast<unsigned short>(byte)));
     asm("cvt.f32.f16 %0, %1;" : "=f"(lo) : "h"(static_cast<unsigned short>(h2 & 0xFFFFu)));
     asm("cvt.f32.f16 %0, %1;" : "=f"(hi) : "h"(static_cast<unsigned short>(h2 >> 16)));
 }
@@ -126,7 +126,14 @@ template <typename SRC> __device__ __forceinline__ float to_f32(SRC v);
 template <> __device__ __forceinline__ float to_f32<float>(float v) { return v; }
 template <> __device__ __forceinline__ float to_f32<uint16_t>(uint16_t v) { return __uint_as_float(static_cast<uint32_t>(v) << 16); }
 
-__device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7fffffffu; }
+// The bit pattern of max |v|, a NaN (above infinity) if there is one; two values an instruction.
+template <int N>
+__device__ __forceinline__ uint32_t top_bits(const float (&v)[N]) {
+    float top = 0.0f;
+#pragma unroll
+    for (int i = 0; i < N; i += 2) asm("max.NaN.abs.f32 %0, %0, %1, %2;" : "+f"(top) : "f"(v[i]), "f"(v[i + 1]));
+    return __float_as_uint(top) & 0x7fffffffu;
+}
 
 // max |src| of a block of threads, NaN left out, raised to *out
 __device__ __forceinline__ void raise_amax(float v, unsigned int* out) {
@@ -164,13 +171,13 @@ __device__ __forceinline__ void write_scales(const QuantArgs& p, const uint8_t* 
 
 // ---------------------------------------------------------------- the matrix as it is
 // A thread takes a block of 16 or 32 columns of a row at a time, neighbours take neighbouring blocks of the row; the loads of
-// kBatch blocks (256 bytes) are on their way together, which takes addresses without branches: a block that is not wholly
+// kBatch blocks (128 bytes) are on their way together, which takes addresses without branches: a block that is not wholly
 // inside the matrix reads the first one instead, and its own elements one by one.
 // VEC: rows start on 16-byte boundaries and are at least one block long.
 template <typename SRC, int FMT, bool VEC>
-__global__ void __launch_bounds__(kThreads, 2) quantise_kernel(const QuantArgs p) {
+__global__ void __launch_bounds__(kThreads, 4) quantise_kernel(const QuantArgs p) {
     constexpr int N = Fmt<FMT>::kBlock, kBlocks = kCols / N, kTiles = kBlocks / 4, kItems = kTileRows * kBlocks / kThreads;
-    constexpr int kWords = VEC ? N * sizeof(SRC) / 16 : 1, kBatch = VEC ? 16 / kWords : 1;
+    constexpr int kWords = VEC ? N * sizeof(SRC) / 16 : 1, kBatch = VEC ? (kWords < 8 ? 8 / kWords : 1) : 1;
     __shared__ __align__(16) uint8_t scales[kTiles * kScaleTile];
     int64_t row_tile, col_tile;
     tile_of(p, row_tile, col_tile);
@@ -222,9 +229,7 @@ __global__ void __launch_bounds__(kThreads, 2) quantise_kernel(const QuantArgs p
 #pragma unroll
                     for (int i = 0; i < N; ++i) v[i] = col + i < p.cols ? to_f32(at[i]) : 0.0f;
                 }
-                uint32_t top = 0;
-#pragma unroll
-                for (int i = 0; i < N; ++i) top = max(top, abs_bits(v[i]));
+                const uint32_t top = top_bits(v);
                 if (p.amax_out != nullptr) {
                     if (top <= 0x7f800000u) {
                         seen = fmaxf(seen, __uint_as_float(top));
@@ -248,33 +253,31 @@ __global__ void __launch_bounds__(kThreads, 2) quantise_kernel(const QuantArgs p
 }
 
 // ---------------------------------------------------------------- the transposed matrix
-// Operand rows are the source's columns.  A thread takes two neighbouring columns over 32 source rows (a warp reads 64
-// neighbouring columns of a row at once), which are one or two whole blocks of each; all its loads are on their way together
-// (addresses past the matrix are moved to its last row and column, their values cleared), and the codes go through shared
-// memory so that they leave in pieces of 64 bytes.  VEC: the source's columns come in pairs that can
-// be read at once.
+// Operand rows are the source's columns.  A thread takes two neighbouring columns over one block of source rows (a warp reads 64
+// neighbouring columns of a row at once), a block of threads 128 columns over four blocks: one tile of scales.  All loads of a
+// thread are on their way together (addresses past the matrix are moved to its last row and column, their values cleared); the
+// codes go through shared memory, so that they leave in pieces of 32 or 64 bytes.  VEC: the source's columns come in pairs
+// that can be read at once.
 template <typename SRC, int FMT, bool VEC>
-__global__ void __launch_bounds__(kThreads, 2) quantise_transposed_kernel(const QuantArgs p) {
-    constexpr int N = Fmt<FMT>::kBlock, kTiles = kColsT / (4 * N), kPitch = kColsT / 2 + 16;
-    __shared__ __align__(16) uint8_t scales[kTiles * kScaleTile];
+__global__ void __launch_bounds__(kThreads, FMT == FP8MLP_MXFP4 ? 3 : 4) quantise_transposed_kernel(const QuantArgs p) {
+    constexpr int N = Fmt<FMT>::kBlock, kColsT = 4 * N, kPitch = kColsT / 2 + 16;
+    __shared__ __align__(16) uint8_t scales[kScaleTile];
     __shared__ __align__(16) uint8_t codes[kTileRows * kPitch];
     int64_t row_tile, col_tile;
     tile_of(p, row_tile, col_tile);
     const int64_t row0 = row_tile * kTileRows, col0 = col_tile * kColsT;
-    const int pair = 2 * (threadIdx.x & 63), k0 = 32 * (threadIdx.x >> 6);        // operand rows of the tile, source rows
+    const int pair = 2 * (threadIdx.x & 63), b = threadIdx.x >> 6, k0 = N * b;        // operand rows of the tile, block
     const int rows = static_cast<int>(min(p.rows - row0, static_cast<int64_t>(kTileRows)));
     const int cols = static_cast<int>(min(p.cols - col0, static_cast<int64_t>(kColsT)));
-    const bool one = pair < rows, two = pair + 1 < rows;
     grid_dependency_wait();
     grid_launch_dependents();
     const float g = FMT == FP8MLP_NVFP4 ? scale_of(p) : 1.0f;
-    float seen = 0.0f;
-    float v[2][32];
+    float v[2][N];
     {
         const int c0 = VEC ? min(pair, rows - 2) : min(pair, rows - 1), c1 = min(pair + 1, rows - 1);      // (VEC: rows is even)
         const uint8_t* base = p.src + col0 * p.ld + row0 * static_cast<int64_t>(sizeof(SRC));
 #pragma unroll
-        for (int i = 0; i < 32; ++i) {
+        for (int i = 0; i < N; ++i) {
             const SRC* at = reinterpret_cast<const SRC*>(base + min(k0 + i, cols - 1) * p.ld);
             if constexpr (VEC && sizeof(SRC) == 4) {
                 const float2 w = __ldg(reinterpret_cast<const float2*>(at + c0));
@@ -285,46 +288,44 @@ __global__ void __launch_bounds__(kThreads, 2) quantise_transposed_kernel(const 
                 v[0][i] = to_f32(__ldg(at + c0)); v[1][i] = to_f32(__ldg(at + c1));
             }
         }
+        if constexpr (VEC && sizeof(SRC) == 2) {
 #pragma unroll
-        for (int i = 0; i < 32; ++i) {
-            if constexpr (VEC && sizeof(SRC) == 2) {
+            for (int i = 0; i < N; ++i) {
                 const uint32_t w = __float_as_uint(v[0][i]);
                 v[0][i] = bf16_lo(w); v[1][i] = bf16_hi(w);
             }
-            const bool in = k0 + i < cols;
-            v[0][i] = in && one ? v[0][i] : 0.0f;
-            v[1][i] = in && two ? v[1][i] : 0.0f;
+        }
+        if (rows < kTileRows || cols < kColsT) {
+            const bool one = pair < rows, two = pair + 1 < rows;
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const bool in = k0 + i < cols;
+                v[0][i] = in && one ? v[0][i] : 0.0f;
+                v[1][i] = in && two ? v[1][i] : 0.0f;
+            }
         }
     }
+    float seen = 0.0f;
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
         const int r = pair + c;
-        uint32_t words[4];
+        const uint32_t top = top_bits(v[c]);
+        if (p.amax_out != nullptr) {
+            if (top <= 0x7f800000u) {
+                seen = fmaxf(seen, __uint_as_float(top));
+            } else {
 #pragma unroll
-        for (int j = 0; j < 32 / N; ++j) {
-            float block[N];
-            uint32_t top = 0;
-#pragma unroll
-            for (int i = 0; i < N; ++i) {
-                block[i] = v[c][N * j + i];
-                top = max(top, abs_bits(block[i]));
+                for (int i = 0; i < N; ++i) seen = fmaxf(seen, fabsf(v[c][i]));
             }
-            if (p.amax_out != nullptr) {
-#pragma unroll
-                for (int i = 0; i < N; ++i) seen = fmaxf(seen, fabsf(block[i]));
-            }
-            uint32_t code[N / 8];
-            uint32_t byte = quantise_block<FMT>(block, top, g, code);
-            if (r >= rows || k0 + N * j >= cols) byte = 0;
-            const int b = k0 / N + j;
-            scales[(b >> 2) * kScaleTile + scale_at(r, b & 3)] = static_cast<uint8_t>(byte);
-#pragma unroll
-            for (int i = 0; i < N / 8; ++i) words[j * (N / 8) + i] = code[i];
         }
-        *reinterpret_cast<uint4*>(codes + r * kPitch + k0 / 2) = make_uint4(words[0], words[1], words[2], words[3]);
+        uint32_t code[N / 8];
+        const uint32_t byte = quantise_block<FMT>(v[c], top, g, code);
+        scales[scale_at(r, b)] = static_cast<uint8_t>(r < rows && k0 < cols ? byte : 0u);
+        if constexpr (N == 32) *reinterpret_cast<uint4*>(codes + r * kPitch + k0 / 2) = make_uint4(code[0], code[1], code[2], code[3]);
+        else *reinterpret_cast<uint2*>(codes + r * kPitch + k0 / 2) = make_uint2(code[0], code[1]);
     }
     __syncthreads();
-    write_scales(p, scales, row_tile, col0 / (4 * N), kTiles);
+    write_scales(p, scales, row_tile, col_tile, 1);
     const int padded = (cols + 31) & ~31;
     for (int i = threadIdx.x; i < kTileRows * (kColsT / 32); i += kThreads) {
         const int r = i / (kColsT / 32), c = i % (kColsT / 32);
@@ -388,8 +389,20 @@ struct DequantArgs {
     int col_tiles, scale_tiles;
 };
 
+// What a scale's byte stands for.
+template <int FMT>
+__device__ __forceinline__ float block_scale(uint32_t byte) {
+    if constexpr (FMT == FP8MLP_MXFP4) {          // 2^(byte - 127); the smallest is subnormal in fp32, the last NaN
+        return __uint_as_float(byte == 0xffu ? 0x7fffffffu : byte == 0u ? 0x00400000u : byte << 23);
+    } else {
+        float s, unused;
+        e4m3x2_to_f32(byte, s, unused);
+        return s;
+    }
+}
+
 // A thread takes 32 columns of a row at a time (16 bytes of codes), four rows' loads on their way together.
-// ALIGN: bytes that output rows are aligned to (32, 16, or less as 1).
+// ALIGN: bytes that output rows are aligned to (32 or 16).
 template <typename DST, int FMT, int ALIGN>
 __global__ void __launch_bounds__(kThreads) dequantise_kernel(const DequantArgs p) {
     constexpr int N = Fmt<FMT>::kBlock, kPerRow = kCols / 32, kItems = kTileRows * kPerRow / kThreads, kStep = kThreads / kPerRow;
@@ -415,13 +428,7 @@ __global__ void __launch_bounds__(kThreads) dequantise_kernel(const DequantArgs 
     for (int it = 0; it < kItems; ++it) {
         const int64_t row = row0 + r0 + it * kStep;
         if (row >= p.rows) break;
-        float s[2];
-        if constexpr (FMT == FP8MLP_MXFP4) {
-            const uint32_t e = bytes[it];             // 2^(e - 127); NaN; the smallest is subnormal in fp32
-            s[0] = s[1] = __uint_as_float(e == 0xffu ? 0x7fffffffu : e == 0u ? 0x00400000u : e << 23);
-        } else {
-            e4m3x2_to_f32(bytes[it], s[0], s[1]);
-        }
+        const float s[2] = {block_scale<FMT>(bytes[it] & 0xffu), block_scale<FMT>(N == 32 ? bytes[it] : bytes[it] >> 8)};
         DST* out = reinterpret_cast<DST*>(p.out + row * p.ld_out) + col;
         const uint32_t words[4] = {code[it].x, code[it].y, code[it].z, code[it].w};
 #pragma unroll
@@ -434,7 +441,7 @@ __global__ void __launch_bounds__(kThreads) dequantise_kernel(const DequantArgs 
                 v[i] = __fmul_rn(v[i], s[h]);         // exact, but for MXFP4 scales at the ends of fp32's range
                 if constexpr (FMT == FP8MLP_NVFP4) v[i] = __fmul_rn(v[i], inv_g);
             }
-            if (ALIGN >= 16 && col + 16 * h + 16 <= p.cols) {
+            if (col + 16 * h + 16 <= p.cols) {
 #pragma unroll
                 for (int i = 0; i < 16; i += 32 / sizeof(DST)) {
                     uint32_t w[8];
@@ -457,6 +464,47 @@ __global__ void __launch_bounds__(kThreads) dequantise_kernel(const DequantArgs 
                         if constexpr (sizeof(DST) == 4) out[16 * h + i] = v[i];
                         else out[16 * h + i] = static_cast<uint16_t>(cvt_bf16x2(v[i], 0.0f) & 0xffffu);
                     }
+            }
+        }
+    }
+}
+
+// The same for output rows on any boundary: a warp takes 64 neighbouring columns of a row at a time, two a lane, so that what it
+// writes is in one piece.
+constexpr int kNarrowRows = 32;
+template <typename DST, int FMT>
+__global__ void __launch_bounds__(kThreads) dequantise_narrow_kernel(const DequantArgs p) {
+    constexpr int N = Fmt<FMT>::kBlock, kRowsPerWarp = kNarrowRows / 2;
+    const int64_t row_tile = blockIdx.x / p.col_tiles;
+    const int warp = threadIdx.x >> 5;
+    const int64_t row0 = row_tile * kNarrowRows + (warp >> 2) * kRowsPerWarp;
+    const int64_t col = (blockIdx.x - row_tile * p.col_tiles) * kCols + 64 * (warp & 3) + 2 * (threadIdx.x & 31);
+    grid_dependency_wait();
+    grid_launch_dependents();
+    if (col >= p.cols || row0 >= p.rows) return;
+    const float inv_g = p.scale != nullptr ? __fdiv_rn(1.0f, *p.scale) : 1.0f;
+    const int64_t block = col / N;
+    uint32_t code[kRowsPerWarp], bytes[kRowsPerWarp];
+#pragma unroll
+    for (int i = 0; i < kRowsPerWarp; ++i) {
+        const int64_t row = min(row0 + i, p.rows - 1);
+        code[i] = __ldg(p.codes + row * p.ld_codes + col / 2);
+        bytes[i] = __ldg(p.scales + (row / kTileRows * p.scale_tiles + block / 4) * kScaleTile + scale_at(static_cast<int>(row % kTileRows), static_cast<int>(block & 3)));
+    }
+#pragma unroll
+    for (int i = 0; i < kRowsPerWarp; ++i) {
+        if (row0 + i >= p.rows) break;
+        const float s = block_scale<FMT>(bytes[i]);
+        float v[2];
+        e2m1x2_to_f32(code[i], v[0], v[1]);
+        DST* out = reinterpret_cast<DST*>(p.out + (row0 + i) * p.ld_out) + col;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            v[k] = __fmul_rn(v[k], s);
+            if constexpr (FMT == FP8MLP_NVFP4) v[k] = __fmul_rn(v[k], inv_g);
+            if (col + k < p.cols) {
+                if constexpr (sizeof(DST) == 4) out[k] = v[k];
+                else out[k] = static_cast<uint16_t>(cvt_bf16x2(v[k], 0.0f) & 0xffffu);
             }
         }
     }
@@ -513,7 +561,7 @@ extern "C" int fp8mlp_quantize_fp4(const void* src, int src_dtype, int64_t rows,
     const bool t = transpose != 0;
     const int64_t R = t ? cols : rows, C = t ? rows : cols;                 // of the operand
     if (ld_codes % 16 != 0 || (R > 0 && ld_codes < (C + 31) / 32 * 16)) return FP8MLP_ERR_SHAPE;
-    const int width = t ? kColsT : kCols;
+    const int width = t ? 4 * (fmt == FP8MLP_MXFP4 ? 32 : 16) : kCols;
     const int64_t tiles = (R + kTileRows - 1) / kTileRows * ((C + width - 1) / width);          // blocks of threads
     if (tiles > INT32_MAX) return FP8MLP_ERR_SHAPE;
     if (rows > 0 && cols > 0 && (src == nullptr || codes == nullptr || block_scales == nullptr)) return FP8MLP_ERR_ARG;
@@ -563,7 +611,11 @@ extern "C" int fp8mlp_dequantize_fp4(const uint8_t* codes, int64_t ld_codes, con
     if (fmt == FP8MLP_MXFP4 && scale != nullptr) return FP8MLP_ERR_ARG;
     if (rows < 0 || cols < 0 || rows > kMost || cols > kMost || (rows > 1 && ld_out < cols)) return FP8MLP_ERR_SHAPE;
     if (ld_codes % 16 != 0 || (rows > 0 && ld_codes < (cols + 31) / 32 * 16)) return FP8MLP_ERR_SHAPE;
-    const int64_t tiles = (rows + kTileRows - 1) / kTileRows * ((cols + kCols - 1) / kCols);
+    const int align = aligned(out, 32) && ld_out * (out_dtype == FP8MLP_F32 ? 4 : 2) % 32 == 0   ? 32
+                      : aligned(out, 16) && ld_out * (out_dtype == FP8MLP_F32 ? 4 : 2) % 16 == 0 ? 16
+                                                                                                 : 1;
+    const int tile_rows = align >= 16 ? kTileRows : kNarrowRows;
+    const int64_t tiles = (rows + tile_rows - 1) / tile_rows * ((cols + kCols - 1) / kCols);
     if (tiles > INT32_MAX) return FP8MLP_ERR_SHAPE;
     if (rows > 0 && cols > 0 && (codes == nullptr || block_scales == nullptr || out == nullptr)) return FP8MLP_ERR_ARG;
     const int bytes = out_dtype == FP8MLP_F32 ? 4 : 2;
@@ -577,11 +629,10 @@ extern "C" int fp8mlp_dequantize_fp4(const uint8_t* codes, int64_t ld_codes, con
     a.scale_tiles = static_cast<int>((cols + per_tile - 1) / per_tile);
     a.col_tiles = static_cast<int>((cols + kCols - 1) / kCols);
     const dim3 grid(static_cast<unsigned>(tiles));
-    const int align = aligned(out, 32) && a.ld_out % 32 == 0 ? 32 : aligned(out, 16) && a.ld_out % 16 == 0 ? 16 : 1;
 #define FP8MLP_DEQUANT(D, F)                                                                                  \
     (align == 32 ? launch_chained(dequantise_kernel<D, F, 32>, grid, dim3(kThreads), 0, st, a)                \
      : align == 16 ? launch_chained(dequantise_kernel<D, F, 16>, grid, dim3(kThreads), 0, st, a)              \
-                   : launch_chained(dequantise_kernel<D, F, 1>, grid, dim3(kThreads), 0, st, a))
+                   : launch_chained(dequantise_narrow_kernel<D, F>, grid, dim3(kThreads), 0, st, a))
     const bool f32 = out_dtype == FP8MLP_F32;
     const cudaError_t e = fmt == FP8MLP_MXFP4 ? (f32 ? FP8MLP_DEQUANT(float, FP8MLP_MXFP4) : FP8MLP_DEQUANT(uint16_t, FP8MLP_MXFP4))
                                               : (f32 ? FP8MLP_DEQUANT(float, FP8MLP_NVFP4) : FP8MLP_DEQUANT(uint16_t, FP8MLP_NVFP4));
