@@ -463,17 +463,17 @@ FP8MLP_API int fp8mlp_gemm_bf16(int64_t M, int64_t N, int64_t K, const void* A, 
  * x, residual, h: T rows of d elements of one type (FP8MLP_BF16 or FP8MLP_F32) with a row stride each; gain fp32 [d], null = 1.
  * h is rounded to that type once, and the norm is that of the rounded values: the gradient of what was computed follows from
  * the stored h.  Squares are summed in fp32.  h_out receives h (null: not wanted; needs a residual); it may be x or the
- * residual itself, no other outputs overlap inputs.  out_kind:
+ * residual itself, no other outputs overlap inputs or one another.  out_kind:
  *   FP8MLP_RMS_SAME       y in the type of x
  *   FP8MLP_RMS_E4M3       y: E4M3 codes Q(y * *scale), `scale` one device float that is read (delayed scaling)
  *   FP8MLP_RMS_E4M3_ROWS  y: E4M3 codes Q(y * scale[t]), scale fp32 [T] written: 448 / max_i |y[t, i]| (1 where that maximum is
- *                         zero or not finite)
+ *                         zero or not finite, or where 448 / max_i |h[t, i] gain[i]| leaves fp32)
  * scale is not used by FP8MLP_RMS_SAME.  amax (nullable, not with FP8MLP_RMS_E4M3_ROWS): receives max |y| of this call (before
  * any cast).  rstd (nullable): fp32 [T], for the backward pass.  With y = a context's FP8MLP_WS_XQ buffer (ld_y = d), scales.x
  * and amax.x the codes are the block's own operand: fp8mlp_forward with FP8MLP_SCALE_GIVEN_X_CAST does not read x again.
  * d a multiple of 16, at most FP8MLP_MAX_NORM_WIDTH; row strides in elements, at least d, of 16 bytes' multiples; all rows and
- * gain start on 16-byte boundaries.  A row that holds a NaN or an infinity has no norm (NaN where the
- * formulas say so); a row of zeros is zeros if eps > 0. */
+ * gain start on 16-byte boundaries.  A row that holds a NaN or an infinity, or whose sum of squares leaves fp32 (elements around
+ * 2^64), has no norm: rstd is NaN or 0, and y what the formulas make of that; a row of zeros is zeros if eps > 0. */
 enum { FP8MLP_RMS_SAME = 0, FP8MLP_RMS_E4M3 = 1, FP8MLP_RMS_E4M3_ROWS = 2 };
 #define FP8MLP_MAX_NORM_WIDTH 16384
 FP8MLP_API int fp8mlp_rmsnorm(int64_t T, int64_t d, int dtype, const void* x, int64_t ld_x, const void* residual,

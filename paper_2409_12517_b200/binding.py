@@ -550,6 +550,8 @@ def fp8mlp_rmsnorm(x, residual, gain, eps: float, y, h=None, out: int = RMS_SAME
     y * scale (1-element fp32, read); RMS_E4M3_ROWS: codes, scale (fp32 [T]) is written."""
     here = _here()
     shape, dtype = x.shape, x.dtype
+    if len(shape) != 2 or dtype not in _DTYPES:
+        raise ValueError(f"x: a 2-D bfloat16 or float32 tensor is needed, got {tuple(shape)} {dtype}")
     T, d = shape
     x_ptr, ld_x = _rows_like(x, shape, dtype, "x", here)
     r_ptr, ld_r = _rows_like(residual, shape, dtype, "residual", here)
@@ -572,6 +574,8 @@ def fp8mlp_rmsnorm_backward(dy, h, gain, rstd, dh, dx, d_gain, workspace) -> Non
     residual stream, or None; workspace: new_rmsnorm_workspace(d), or None without d_gain."""
     here = _here()
     shape, dtype = h.shape, h.dtype
+    if len(shape) != 2 or dtype not in _DTYPES:
+        raise ValueError(f"h: a 2-D bfloat16 or float32 tensor is needed, got {tuple(shape)} {dtype}")
     T, d = shape
     h_ptr, ld_h = _rows_like(h, shape, dtype, "h", here)
     dy_ptr, ld_dy = _rows_like(dy, shape, dtype, "dy", here)

@@ -179,8 +179,9 @@ __global__ void __launch_bounds__(BLOCK) norm_kernel(const NormArgs p) {
         if (OUT == FP8MLP_RMS_E4M3) factor = __fmul_rn(rstd, scale);
         if (OUT == FP8MLP_RMS_E4M3_ROWS) {
             const float most = __fmul_rn(top, rstd), row_scale = __fdiv_rn(448.0f, most);
-            const bool sound = most > 0.0f && !isinf(most) && !isinf(row_scale);
-            if (sound) factor = __fdiv_rn(448.0f, top);
+            const float to_codes = __fdiv_rn(448.0f, top);
+            const bool sound = most > 0.0f && !isinf(most) && !isinf(row_scale) && !isinf(to_codes);
+            if (sound) factor = to_codes;
             if (here && u0 == 0) p.scale[row] = sound ? row_scale : 1.0f;
         } else {
             run_max = fmaxf(run_max, __fmul_rn(top, rstd));
@@ -437,6 +438,7 @@ extern "C" int fp8mlp_rmsnorm(int64_t T, int64_t d, int dtype, const void* x, in
     if (residual != nullptr && !stride_ok(T, ld_residual, d, bytes)) return FP8MLP_ERR_SHAPE;
     if (h_out != nullptr && !stride_ok(T, ld_h, d, bytes)) return FP8MLP_ERR_SHAPE;
     if (T > 0 && (x == nullptr || y == nullptr)) return FP8MLP_ERR_ARG;
+    if (y != nullptr && (y == x || y == residual || y == h_out)) return FP8MLP_ERR_ARG;
     if (out_kind == FP8MLP_RMS_E4M3 && scale == nullptr) return FP8MLP_ERR_ARG;
     if (out_kind == FP8MLP_RMS_E4M3_ROWS && T > 0 && scale == nullptr) return FP8MLP_ERR_ARG;
     if (!aligned(x, 16) || !aligned(residual, 16) || !aligned(h_out, 16) || !aligned(y, 16) || !aligned(gain, 16)) return FP8MLP_ERR_ALIGN;

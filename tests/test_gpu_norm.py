@@ -117,6 +117,20 @@ def test_forward_rows_without_a_norm():
     assert torch.isnan(y[0]).all()                                       # 0 / 0
 
 
+def test_rows_too_small_for_a_scale_of_their_own():
+    """448 / maximum beyond fp32, with the maximum of y, or of h gain alone: scale 1, codes of y as it is, no NaN."""
+    x = torch.randn(5, 64, device="cuda")
+    for row, top in ((1, 1e-37), (2, 1.2e-36), (3, 1e-44)):
+        x[row] = 0
+        x[row, 3], x[row, 4] = top, -top / 2
+    for gain in (None, torch.full((64,), 1.0, device="cuda")):
+        y, scale = torch.full((5, 64), 0x55, dtype=torch.uint8, device="cuda"), torch.zeros(5, device="cuda")
+        B.fp8mlp_rmsnorm(x, None, gain, EPS, y, out=B.RMS_E4M3_ROWS, scale=scale)
+        v = y.view(torch.float8_e4m3fn).float()
+        assert (scale[1:4] == 1).all() and (v[1:4] == 0).all()
+        assert (v[[0, 4]].abs().amax(-1) == 448).all() and (scale[[0, 4]] > 1).all()
+
+
 @pytest.mark.parametrize("T", [0, 1, 2000])
 def test_amax_is_of_this_call(T):
     amax = torch.full((1,), 1e30, device="cuda")

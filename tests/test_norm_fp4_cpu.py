@@ -26,7 +26,7 @@ def nothing_launched(lib):
 
 
 def test_norm_refusals(lib):
-    def norm(T=4, d=64, dt=B.BF16, x=P, ldx=64, res=None, ldr=64, h=None, ldh=64, gain=P, eps=1e-5, out=B.RMS_SAME, y=P, ldy=64,
+    def norm(T=4, d=64, dt=B.BF16, x=P, ldx=64, res=None, ldr=64, h=None, ldh=64, gain=P, eps=1e-5, out=B.RMS_SAME, y=8 * P, ldy=64,
              scale=None, amax=None, rstd=None):
         return lib.fp8mlp_rmsnorm(T, d, dt, x, ldx, res, ldr, h, ldh, gain, eps, out, y, ldy, scale, amax, rstd, None)
     for bad in (dict(dt=2), dict(dt=-1), dict(out=3), dict(out=-1), dict(h=P), dict(x=None), dict(y=None), dict(eps=-1.0),
@@ -35,10 +35,13 @@ def test_norm_refusals(lib):
     for bad in (dict(T=-1), dict(d=0), dict(d=24), dict(d=B.MAX_NORM_WIDTH + 16), dict(ldx=48), dict(ldx=68), dict(ldy=0),
                 dict(res=P, ldr=60), dict(res=P, h=P, ldh=-64), dict(out=B.RMS_E4M3, scale=P, ldy=72)):
         assert norm(**bad) == B.ERR_SHAPE, bad
-    for bad in (dict(x=P + 8), dict(y=P + 2), dict(gain=P + 4), dict(res=P + 8), dict(res=P, h=P + 8), dict(rstd=P + 2),
+    for bad in (dict(x=P + 8), dict(y=8 * P + 2), dict(gain=P + 4), dict(res=P + 8), dict(res=P, h=P + 8), dict(rstd=P + 2),
                 dict(amax=P + 1), dict(out=B.RMS_E4M3, scale=P + 2)):
         assert norm(**bad) == B.ERR_ALIGN, bad
     assert norm(T=0, x=None, y=None) == B.OK
+    # outputs that overlap an input or each other
+    for bad in (dict(y=P, x=P), dict(y=P, x=2 * P, res=P), dict(y=P, x=2 * P, res=3 * P, h=P)):
+        assert norm(**bad) == B.ERR_ARG, bad
 
 
 def test_norm_backward_refusals(lib):
@@ -103,6 +106,11 @@ def test_binding_refuses(lib):
         B.fp8mlp_rmsnorm(x, None, None, 1e-5, x)
     with pytest.raises(ValueError, match="current GPU"):
         B.fp8mlp_rmsnorm_backward(x, x, None, None, None, x, None, None)
+    for other in (x.half(), x[0], x.int()):
+        with pytest.raises(ValueError, match="2-D bfloat16 or float32"):
+            B.fp8mlp_rmsnorm(other, None, None, 1e-5, other)
+        with pytest.raises(ValueError, match="2-D bfloat16 or float32"):
+            B.fp8mlp_rmsnorm_backward(other, other, None, None, None, other, None, None)
     op = B.new_fp4(B.MXFP4, 4, 64, device="cpu")
     assert op.scales.numel() == 512 and op.codes.shape == (4, 32) and op.scale is None
     with pytest.raises(ValueError, match="current GPU"):
