@@ -16,10 +16,13 @@
 // quadrants of 4 tensor-memory columns.  Tensor memory holds the scales of two stages or more: those
 // of a stage are copied once the MMAs that read their place last are done.
 //
-// Large products: CTA pairs on 256 x 192 tiles (cta_group::2; each CTA loads its 128 rows of P, half of the rows of Q, and the
-// scales of all of Q); two accumulators alternate, so that the epilogue of a tile overlaps the main loop of the next.  Others:
-// single CTAs, two to an SM, on one 128 x 16 .. 128 tile each; with few tiles the contraction is cut among the 2, 4 or 8 CTAs of a
-// cluster, which add their shares over distributed shared memory in the order of their ranks.
+// Large products: CTA pairs on 256 x 256 tiles (cta_group::2; each CTA loads its 128 rows of P, half of the rows of Q, and the
+// scales of all of Q).  What bounds them is the way from L2 to the SMs, some 60 bytes a clock: 35 KB (MXFP4) a stage of 512 cycles
+// of MMAs.  (256 x 192 tiles with two accumulators want 31 KB for 384: 8192 x 8192 x 16384 NVFP4 445 us, this way 360.)  The one
+// accumulator goes to registers as a whole, so that the next tile's MMAs have it back at once; the loads, which set the pace, run on
+// meanwhile.  The output leaves through shared memory in bulk stores (8192 x 8192 x 256: 49 us with stores of 32 bytes a lane, 26).
+// Others: single CTAs, two to an SM, on one 128 x 16 .. 128 tile each; with few tiles the contraction is cut among the 2, 4 or 8
+// CTAs of a cluster, which add their shares over distributed shared memory in the order of their ranks.
 // Every wait is bounded.
 #include "gemm.cuh"
 
@@ -42,7 +45,7 @@ struct Gemm4Args {
     int split;                               // CTAs of a cluster that share a tile's contraction (at most stages_k)
     int group;                               // rasterisation: bands of this many p tiles
     int swap;                                // out is [Q, P]
-    int f32, vec;                            // fp32 output; bytes that its rows are aligned to (32, 16 or less)
+    int f32, vec;                            // fp32 output; 16: its rows start on 16-byte boundaries
     const float *s0, *s1;
     uint8_t* out;
     int64_t ld_out;                          // elements
@@ -55,10 +58,11 @@ template <int FMT, int TN, bool PAIR> struct Shape {
     static constexpr int kPBytes = kRows * 128, kQBytes = (PAIR ? TN / 2 : TN) * 128;
     static constexpr int kSfBytes = kTiles * kScaleTile;                  // per 128 rows
     static constexpr int kStageBytes = kPBytes + kQBytes + (1 + kQGroups) * kSfBytes;
-    // A pair runs for many tiles, with two accumulators; a single CTA has one tile and one accumulator, and shares its SM with
-    // another that works while it starts or ends.
-    static constexpr int kCtasPerSm = PAIR ? 1 : 2, kAccs = PAIR ? 2 : 1;
-    static constexpr int kStages = PAIR ? 6 : TN >= 64 ? 3 : 4;
+    // A single CTA shares its SM with another that works while it starts or ends.
+    static constexpr int kCtasPerSm = PAIR ? 1 : 2, kAccs = PAIR && TN <= 192 ? 2 : 1;
+    static constexpr int kStoreBytes = PAIR ? 8 * 4096 : 0;               // staging of the output, 4 KB for each epilogue warp
+    static constexpr int kFit = (232448 - 1024 - 256 - kStoreBytes) / kStageBytes;
+    static constexpr int kStages = PAIR ? (kFit < 6 ? kFit : 6) : TN >= 64 ? 3 : 4;
     static constexpr int kEpiWarps = TN >= 64 ? 8 : 4;
     static constexpr int kThreads = 32 * (kOtherWarps + kEpiWarps);
     static constexpr int kWarpCols = TN / (kEpiWarps / 4);                // columns of a tile that an epilogue warp drains
@@ -79,9 +83,9 @@ struct __align__(8) Tail4 {
 
 template <int FMT, int TN, bool PAIR>
 constexpr size_t smem4_bytes() {
-    return 1024 + size_t(Shape<FMT, TN, PAIR>::kStages) * Shape<FMT, TN, PAIR>::kStageBytes + sizeof(Tail4);
+    return 1024 + size_t(Shape<FMT, TN, PAIR>::kStages) * Shape<FMT, TN, PAIR>::kStageBytes + Shape<FMT, TN, PAIR>::kStoreBytes + sizeof(Tail4);
 }
-static_assert(smem4_bytes<FP8MLP_NVFP4, 192, true>() <= 232448, "shared memory");
+static_assert(smem4_bytes<FP8MLP_NVFP4, 256, true>() <= 232448 && smem4_bytes<FP8MLP_MXFP4, 256, true>() <= 232448, "shared memory");
 static_assert(2 * (smem4_bytes<FP8MLP_NVFP4, 128, false>() + 1024) <= 233472 && 2 * (smem4_bytes<FP8MLP_NVFP4, 32, false>() + 1024) <= 233472,
               "two single CTAs share an SM");
 
@@ -205,53 +209,170 @@ __device__ __forceinline__ void store_one(const Gemm4Args& p, int64_t at, float 
 // N neighbouring outputs of a row, `have` of them inside the matrix
 template <int N>
 __device__ __forceinline__ void store_cols(const Gemm4Args& p, int64_t at, const float (&v)[N], int have) {
-    if (have < N || p.vec < 16) {
+    if (have < N || p.vec != 16) {
 #pragma unroll
         for (int i = 0; i < N; ++i)
             if (i < have) store_one(p, at + i, v[i]);
-        return;
-    }
-    if (p.f32) {
+    } else if (p.f32) {
         float* dst = reinterpret_cast<float*>(p.out) + at;
 #pragma unroll
-        for (int i = 0; i < N; i += 8) {
-            uint32_t w[8];
-#pragma unroll
-            for (int k = 0; k < 8; ++k) w[k] = __float_as_uint(v[i + k]);
-            if (p.vec >= 32) {
-                st_global_v8(dst + i, w);
-            } else {
-                st_global_v4(dst + i, w[0], w[1], w[2], w[3]);
-                st_global_v4(dst + i + 4, w[4], w[5], w[6], w[7]);
-            }
-        }
+        for (int i = 0; i < N; i += 4)
+            st_global_v4(dst + i, __float_as_uint(v[i]), __float_as_uint(v[i + 1]), __float_as_uint(v[i + 2]), __float_as_uint(v[i + 3]));
     } else {
         uint16_t* dst = reinterpret_cast<uint16_t*>(p.out) + at;
 #pragma unroll
-        for (int i = 0; i < N; i += 16) {
-            uint32_t w[8];
+        for (int i = 0; i < N; i += 8)
+            st_global_v4(dst + i, cvt_bf16x2(v[i], v[i + 1]), cvt_bf16x2(v[i + 2], v[i + 3]), cvt_bf16x2(v[i + 4], v[i + 5]), cvt_bf16x2(v[i + 6], v[i + 7]));
+    }
+}
+
+// 32 columns of a warp's 32 rows (a lane has a row) into its 4 KB of staging: rows of 128 bytes (fp32) or 64 (bf16), their 16-byte
+// pieces swizzled as a tensor map with rows of that length does it.
+__device__ __forceinline__ void stage_rows(bool f32, uint32_t block, int lane, const float (&v)[32]) {
+    if (f32) {
 #pragma unroll
-            for (int k = 0; k < 8; ++k) w[k] = cvt_bf16x2(v[i + 2 * k], v[i + 2 * k + 1]);
-            if (p.vec >= 32) {
-                st_global_v8(dst + i, w);
-            } else {
-                st_global_v4(dst + i, w[0], w[1], w[2], w[3]);
-                st_global_v4(dst + i + 8, w[4], w[5], w[6], w[7]);
+        for (int c = 0; c < 8; ++c)
+            st_shared_v4(block + lane * 128u + ((c ^ (lane & 7)) << 4), __float_as_uint(v[4 * c]), __float_as_uint(v[4 * c + 1]),
+                         __float_as_uint(v[4 * c + 2]), __float_as_uint(v[4 * c + 3]));
+    } else {
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+            st_shared_v4(block + lane * 64u + ((c ^ ((lane >> 1) & 3)) << 4), cvt_bf16x2(v[8 * c], v[8 * c + 1]), cvt_bf16x2(v[8 * c + 2], v[8 * c + 3]),
+                         cvt_bf16x2(v[8 * c + 4], v[8 * c + 5]), cvt_bf16x2(v[8 * c + 6], v[8 * c + 7]));
+    }
+}
+
+// Rows on 16-byte boundaries: one lane sends the block off as a bulk tensor store, which cuts off what lies outside the matrix, but
+// along a row in pieces of 16 bytes: a row's end inside such a piece is for write_rows.
+__device__ __forceinline__ void send_rows(const CUtensorMap* out, bool f32, uint32_t stage, uint32_t& sent, int lane, int row, int col,
+                                          const float (&v)[32]) {
+    if (!f32) stage += (sent++ & 1u) * 2048u;                 // the staging holds two blocks of bf16, one of fp32
+    if (lane == 0) {                                          // the store that used this block last has read it
+        if (f32) tma_store_wait_read<0>(); else tma_store_wait_read<1>();
+    }
+    __syncwarp();
+    stage_rows(f32, stage, lane, v);
+    fence_smem_to_async_proxy();
+    __syncwarp();
+    if (lane == 0) {
+        tma_store_2d(out, stage, col, row);
+        tma_store_commit();
+    }
+}
+
+__device__ __forceinline__ uint32_t shared_word(uint32_t at) {
+    uint32_t w;
+    asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w) : "r"(at) : "memory");
+    return w;
+}
+
+// Rows on any boundary, `rows` x `cols` of the block inside the matrix: each row is written by neighbouring lanes, in words of four
+// bytes (16384 x 1411 bf16 with a row per lane, element by element: 234 us; this way 74, with write_wide 39).
+__device__ __forceinline__ void write_rows(const Gemm4Args& p, uint32_t stage, int lane, int row, int col, int rows, int cols,
+                                           const float (&v)[32]) {
+    if (lane == 0) tma_store_wait_read<0>();
+    __syncwarp();                                             // the last block has been read
+    stage_rows(p.f32 != 0, stage, lane, v);
+    __syncwarp();
+    constexpr int kBatch = 8;                                 // loads under way together
+    if (p.f32) {
+        float* dst = reinterpret_cast<float*>(p.out) + static_cast<int64_t>(row) * p.ld_out + col + lane;
+#pragma unroll 1
+        for (int r0 = 0; r0 < rows; r0 += kBatch) {
+            uint32_t w[kBatch];
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) w[k] = shared_word(stage + (r0 + k) * 128u + (((lane >> 2) ^ k) << 4) + (lane & 3) * 4u);
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k)
+                if (lane < cols && r0 + k < rows) dst[(r0 + k) * p.ld_out] = __uint_as_float(w[k]);
+        }
+    } else {
+        // two rows at a time, 16 lanes each; a row on an odd element begins with one element, and every lane's word is the upper
+        // half of its own and the lower half of the next one's
+        const int l = lane & 15;
+        uint16_t* base = reinterpret_cast<uint16_t*>(p.out) + static_cast<int64_t>(row + (lane >> 4)) * p.ld_out + col;
+#pragma unroll 1
+        for (int r0 = 0; r0 < rows; r0 += 2 * kBatch) {
+            uint32_t w[kBatch];
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) {
+                const int r = r0 + 2 * k + (lane >> 4);
+                w[k] = shared_word(stage + r * 64u + (((l >> 2) ^ (k & 3)) << 4) + (l & 3) * 4u);
+            }
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) {
+                uint16_t* dst = base + (r0 + 2 * k) * p.ld_out;
+                const bool odd = (reinterpret_cast<uintptr_t>(dst) & 2) != 0, here = r0 + 2 * k + (lane >> 4) < rows;
+                const uint32_t next = __shfl_down_sync(kAll, w[k], 1, 16), pair = odd ? __funnelshift_r(w[k], next, 16) : w[k];
+                const int c = 2 * l + (odd ? 1 : 0);            // the columns of `pair`: c, c + 1
+                if (here && c + 1 < cols && c + 1 < 32) *reinterpret_cast<uint32_t*>(dst + c) = pair;
+                else if (here && c < cols) dst[c] = static_cast<uint16_t>(pair & 0xffffu);
+                if (here && odd && l == 0) dst[0] = static_cast<uint16_t>(w[k] & 0xffffu);
             }
         }
     }
 }
 
-template <int FMT, int TN, bool PAIR>
+// The same for 128 bf16 columns, all inside the matrix, with stores of 16 bytes: 16 lanes take a row, each a piece of 8 elements that
+// begins on a 16-byte boundary of the output, i.e. the row's elements from head + 8 l on, put together from the staged pieces l and
+// l + 1; what is left at the ends of the row, 8 elements in all, goes one by one.  16 rows at a time in the 4 KB of staging.
+__device__ __forceinline__ void write_wide(const Gemm4Args& p, uint32_t stage, int lane, int row, int col, int rows, const uint32_t (&w)[64]) {
+    constexpr int kBatch = 2;
+    const int l = lane & 15;
+#pragma unroll
+    for (int pass = 0; pass < 2; ++pass) {
+        __syncwarp();                                         // the last block has been read
+        if ((lane >> 4) == pass)
+#pragma unroll
+            for (int c = 0; c < 16; ++c) st_shared_v4(stage + l * 256u + ((c ^ l) << 4), w[4 * c], w[4 * c + 1], w[4 * c + 2], w[4 * c + 3]);
+        __syncwarp();
+#pragma unroll
+        for (int r0 = 0; r0 < 16; r0 += 2 * kBatch) {         // the loads of a batch of rows are under way together
+            uint4 own[kBatch];
+            uint32_t edge[kBatch];
+            int head[kBatch];
+            uint16_t* dst[kBatch];
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) {
+                const int r = r0 + 2 * k + (lane >> 4);
+                dst[k] = reinterpret_cast<uint16_t*>(p.out) + static_cast<int64_t>(row + 16 * pass + r) * p.ld_out + col;
+                head[k] = static_cast<int>((0u - static_cast<uint32_t>(reinterpret_cast<uintptr_t>(dst[k]) >> 1)) & 7u);
+                own[k] = ld_shared_v4(stage + r * 256u + ((l ^ r) << 4));
+                const int e = l < head[k] ? l : 120 + (l & 7);
+                edge[k] = shared_word(stage + r * 256u + (((e >> 3) ^ r) << 4) + ((e & 7) >> 1) * 4u) >> (16 * (e & 1));
+            }
+#pragma unroll
+            for (int k = 0; k < kBatch; ++k) {
+                const bool here = 16 * pass + r0 + 2 * k + (lane >> 4) < rows;
+                const uint32_t x[8] = {own[k].x, own[k].y, own[k].z, own[k].w, __shfl_down_sync(kAll, own[k].x, 1, 16), __shfl_down_sync(kAll, own[k].y, 1, 16),
+                                       __shfl_down_sync(kAll, own[k].z, 1, 16), __shfl_down_sync(kAll, own[k].w, 1, 16)};
+                uint32_t y[6], z[5], o[4];
+#pragma unroll
+                for (int i = 0; i < 6; ++i) y[i] = (head[k] & 4) ? x[i + 2] : x[i];
+#pragma unroll
+                for (int i = 0; i < 5; ++i) z[i] = (head[k] & 2) ? y[i + 1] : y[i];
+                const uint32_t pick = (head[k] & 1) ? 0x5432u : 0x3210u;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[i] = __byte_perm(z[i], z[i + 1], pick);
+                if (here && (head[k] == 0 || l < 15)) st_global_v4(dst[k] + head[k] + 8 * l, o[0], o[1], o[2], o[3]);
+                if (here && head[k] != 0 && l < 8) dst[k][l < head[k] ? l : 120 + l] = static_cast<uint16_t>(edge[k] & 0xffffu);
+            }
+        }
+    }
+}
+
+// BULK (pairs): the output's rows are on 16-byte boundaries and leave in bulk stores.
+template <int FMT, int TN, bool PAIR, bool BULK>
 __global__ void __launch_bounds__(Shape<FMT, TN, PAIR>::kThreads, Shape<FMT, TN, PAIR>::kCtasPerSm)
 gemm4_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_constant__ CUtensorMap tmQ,
-             const __grid_constant__ CUtensorMap tmSfP, const __grid_constant__ CUtensorMap tmSfQ, const Gemm4Args p) {
+             const __grid_constant__ CUtensorMap tmSfP, const __grid_constant__ CUtensorMap tmSfQ,
+             const __grid_constant__ CUtensorMap tmOut, const Gemm4Args p) {
     using S = Shape<FMT, TN, PAIR>;
     constexpr int kStages = S::kStages, kStageBytes = S::kStageBytes;
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw_addr = smem_u32(smem_raw);
     const uint32_t tiles_addr = (raw_addr + 1023u) & ~1023u;
-    Tail4* tail = reinterpret_cast<Tail4*>(smem_raw + (tiles_addr - raw_addr) + size_t(kStages) * kStageBytes);
+    Tail4* tail = reinterpret_cast<Tail4*>(smem_raw + (tiles_addr - raw_addr) + size_t(kStages) * kStageBytes + S::kStoreBytes);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = (PAIR || p.split > 1) ? cluster_ctarank() : 0u;
     const int ctas = PAIR ? 2 : p.split;                             // per tile
@@ -267,6 +388,7 @@ gemm4_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_constant__ CU
         tma_prefetch_desc(&tmQ);
         tma_prefetch_desc(&tmSfP);
         tma_prefetch_desc(&tmSfQ);
+        if (BULK) tma_prefetch_desc(&tmOut);
         for (int s = 0; s < kStages; ++s) {
             mbar_init(smem_u32(&tail->full[s]), 1);
             mbar_init(smem_u32(&tail->empty[s]), 1);
@@ -337,7 +459,9 @@ gemm4_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_constant__ CU
                 if (!__all_sync(kAll, mbar_wait(smem_u32(&tail->tmem_empty[acc]), acc_phase ^ 1u, abort_flag, nullptr))) break;
                 tc_fence_after();
                 const uint32_t d_tmem = tmem_base + acc * TN;
-                const uint32_t q_offset = static_cast<uint32_t>((q_tile * TN) % kRows) / 32u;     // first column of the tile's scales
+                // first column of the tile's scales; the MMA takes them from even columns only, so that tiles narrower than 64 are
+                // for products with one such tile
+                const uint32_t q_offset = TN >= 64 ? static_cast<uint32_t>((q_tile * TN) % kRows) / 32u : 0u;
                 for (int kb = kb_begin; kb < kb_end; ++kb) {
                     if (!ready) {
                         ok = __all_sync(kAll, mbar_wait(smem_u32(&tail->full[ring.stage]), ring.phase, abort_flag, nullptr));
@@ -369,6 +493,9 @@ gemm4_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_constant__ CU
         const int quad = warp & 3, part = (warp - kOtherWarps) >> 2;
         const float dq = __fmul_rn(p.s0 != nullptr ? __fdiv_rn(1.0f, *p.s0) : 1.0f, p.s1 != nullptr ? __fdiv_rn(1.0f, *p.s1) : 1.0f);
         constexpr int kChunk = S::kWarpCols < 32 ? 16 : 32, kShareRows = kRows + 4, kShareCols = TN + 4;
+        // staging of the output: a pair's own, or (a single CTA has one tile) operand stages, which have all been read by then
+        const uint32_t stage = tiles_addr + (PAIR ? kStages * kStageBytes : 0) + (warp - kOtherWarps) * 4096;
+        uint32_t sent = 0;
         int it = 0;
         for (int tile = first_tile; tile < num_tiles; tile += tile_step, ++it) {
             int p_tile, q_tile;
@@ -380,47 +507,82 @@ gemm4_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_constant__ CU
             const uint32_t taddr = tmem_base + acc * TN + part * S::kWarpCols + (static_cast<uint32_t>(quad * 32) << 16);
             const int row = (PAIR ? 2 * p_tile + static_cast<int>(rank) : p_tile) * kRows + quad * 32 + lane;
             const int col0 = q_tile * TN + part * S::kWarpCols;
-#pragma unroll 1
-            for (int c = 0; c < S::kWarpCols; c += kChunk) {
-                if (col0 + c >= p.Q) break;
-                uint32_t r[kChunk];
-                tmem_ld_cols<kChunk>(taddr + c, r);
+            if constexpr (PAIR) {
+                // the whole accumulator into registers first, so that the next tile's MMAs may have it while this one is stored
+                uint32_t r[S::kWarpCols / 32][32];
+#pragma unroll
+                for (int c = 0; c < S::kWarpCols / 32; ++c) tmem_ld32(taddr + 32 * c, r[c]);
                 tmem_ld_wait();
-                if (p.split > 1) {
-                    // this share of the tile into shared memory (every operand stage has been read), in the order of the output's
-                    // rows: [column][accumulator row] if the output is [Q, P], else [accumulator row][column]
-                    float* share = reinterpret_cast<float*>(smem_raw + (tiles_addr - raw_addr));
-                    const int first = part * S::kWarpCols + c, mine = quad * 32 + lane;
-                    if (p.swap) {
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_cluster(mapa_shared(smem_u32(&tail->tmem_empty[acc]), 0));
+                static_assert(S::kWarpCols == 128, "write_wide");
+                if (!BULK && !p.f32 && col0 + 128 <= p.Q) {
+                    uint32_t w[64];
 #pragma unroll
-                        for (int i = 0; i < kChunk; ++i) share[(first + i) * kShareRows + mine] = __uint_as_float(r[i]);
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < kChunk; i += 4)
-                            *reinterpret_cast<float4*>(share + mine * kShareCols + first + i) =
-                                make_float4(__uint_as_float(r[i]), __uint_as_float(r[i + 1]), __uint_as_float(r[i + 2]), __uint_as_float(r[i + 3]));
-                    }
+                    for (int i = 0; i < 64; ++i) w[i] = cvt_bf16x2(__fmul_rn(__uint_as_float(r[i >> 4][2 * i & 31]), dq), __fmul_rn(__uint_as_float(r[i >> 4][(2 * i + 1) & 31]), dq));
+                    if (row - lane < p.P) write_wide(p, stage, lane, row - lane, col0, min(32, p.P - (row - lane)), w);
                     continue;
                 }
-                if (row >= p.P) continue;
-                float v[kChunk];
 #pragma unroll
-                for (int i = 0; i < kChunk; ++i) v[i] = __fmul_rn(__uint_as_float(r[i]), dq);
-                if (p.swap) {
+                for (int c = 0; c < S::kWarpCols / 32; ++c) {
+                    const int col = col0 + 32 * c;
+                    if (col >= p.Q || row - lane >= p.P) break;
+                    float v[32];
 #pragma unroll
-                    for (int i = 0; i < kChunk; ++i)
-                        if (col0 + c + i < p.Q) store_one(p, static_cast<int64_t>(col0 + c + i) * p.ld_out + row, v[i]);
-                } else {
-                    store_cols<kChunk>(p, static_cast<int64_t>(row) * p.ld_out + col0 + c, v, p.Q - (col0 + c));
+                    for (int i = 0; i < 32; ++i) v[i] = __fmul_rn(__uint_as_float(r[c][i]), dq);
+                    const bool cut = col + 32 > p.Q && (p.Q & (p.f32 ? 3 : 7)) != 0;
+                    if (BULK && !cut) send_rows(&tmOut, p.f32 != 0, stage, sent, lane, row - lane, col, v);
+                    else write_rows(p, stage, lane, row - lane, col, min(32, p.P - (row - lane)), min(32, p.Q - col), v);
                 }
-            }
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) {
-                if constexpr (PAIR) mbar_arrive_cluster(mapa_shared(smem_u32(&tail->tmem_empty[acc]), 0));
-                else mbar_arrive(smem_u32(&tail->tmem_empty[acc]));
+            } else {
+#pragma unroll 1
+                for (int c = 0; c < S::kWarpCols; c += kChunk) {
+                    if (col0 + c >= p.Q) break;
+                    uint32_t r[kChunk];
+                    tmem_ld_cols<kChunk>(taddr + c, r);
+                    tmem_ld_wait();
+                    if (p.split > 1) {
+                        // this share of the tile into shared memory (every operand stage has been read), in the order of the output's
+                        // rows: [column][accumulator row] if the output is [Q, P], else [accumulator row][column]
+                        float* share = reinterpret_cast<float*>(smem_raw + (tiles_addr - raw_addr));
+                        const int first = part * S::kWarpCols + c, mine = quad * 32 + lane;
+                        if (p.swap) {
+#pragma unroll
+                            for (int i = 0; i < kChunk; ++i) share[(first + i) * kShareRows + mine] = __uint_as_float(r[i]);
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < kChunk; i += 4)
+                                *reinterpret_cast<float4*>(share + mine * kShareCols + first + i) =
+                                    make_float4(__uint_as_float(r[i]), __uint_as_float(r[i + 1]), __uint_as_float(r[i + 2]), __uint_as_float(r[i + 3]));
+                        }
+                        continue;
+                    }
+                    if (row - lane >= p.P) break;
+                    float v[kChunk];
+#pragma unroll
+                    for (int i = 0; i < kChunk; ++i) v[i] = __fmul_rn(__uint_as_float(r[i]), dq);
+                    if constexpr (kChunk == 32) {
+                        if (!p.swap && p.vec != 16) {
+                            write_rows(p, stage, lane, row - lane, col0 + c, min(32, p.P - (row - lane)), min(32, p.Q - (col0 + c)), v);
+                            continue;
+                        }
+                    }
+                    if (row >= p.P) continue;
+                    if (p.swap) {
+#pragma unroll
+                        for (int i = 0; i < kChunk; ++i)
+                            if (col0 + c + i < p.Q) store_one(p, static_cast<int64_t>(col0 + c + i) * p.ld_out + row, v[i]);
+                    } else {
+                        store_cols<kChunk>(p, static_cast<int64_t>(row) * p.ld_out + col0 + c, v, p.Q - (col0 + c));
+                    }
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&tail->tmem_empty[acc]));
             }
         }
+        if (BULK && lane == 0) tma_store_wait_all();          // the staged output has reached global memory
     }
 
     // ---------------------------------------------------------------- teardown
@@ -458,7 +620,7 @@ gemm4_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_constant__ CU
                 }
             const float out[4] = {__fmul_rn(sum.x, dq), __fmul_rn(sum.y, dq), __fmul_rn(sum.z, dq), __fmul_rn(sum.w, dq)};
             const int64_t to = (line0 + line) * p.ld_out + word0 + word;
-            if (p.vec >= 16 && word + 4 <= len) {
+            if (p.vec == 16 && word + 4 <= len) {
                 if (p.f32) st_global_v4(reinterpret_cast<float*>(p.out) + to, __float_as_uint(out[0]), __float_as_uint(out[1]), __float_as_uint(out[2]), __float_as_uint(out[3]));
                 else st_global_v2(reinterpret_cast<uint16_t*>(p.out) + to, cvt_bf16x2(out[0], out[1]), cvt_bf16x2(out[2], out[3]));
             } else {
@@ -479,8 +641,8 @@ gemm4_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_constant__ CU
 // ---------------------------------------------------------------- host side
 bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
-template <int FMT, int TN, bool PAIR>
-int launch4(const CUtensorMap (&tm)[4], const Gemm4Args& a, int sm_count, cudaStream_t st) {
+template <int FMT, int TN, bool PAIR, bool BULK>
+int launch4(const CUtensorMap (&tm)[5], const Gemm4Args& a, int sm_count, cudaStream_t st) {
     using S = Shape<FMT, TN, PAIR>;
     constexpr size_t kSmem = smem4_bytes<FMT, TN, PAIR>();
     constexpr int kMaxDevices = 64;
@@ -507,10 +669,10 @@ int launch4(const CUtensorMap (&tm)[4], const Gemm4Args& a, int sm_count, cudaSt
         cfg.numAttrs = 2;
     }
     std::call_once(once_dev[dev], [&] {
-        err_dev[dev] = cudaFuncSetAttribute(gemm4_kernel<FMT, TN, PAIR>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kSmem));
+        err_dev[dev] = cudaFuncSetAttribute(gemm4_kernel<FMT, TN, PAIR, BULK>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kSmem));
         if (PAIR && err_dev[dev] == cudaSuccess) {
             cfg.gridDim = dim3(static_cast<unsigned>(sm_count) & ~1u);
-            err_dev[dev] = cudaOccupancyMaxActiveClusters(&clusters_dev[dev], gemm4_kernel<FMT, TN, PAIR>, &cfg);
+            err_dev[dev] = cudaOccupancyMaxActiveClusters(&clusters_dev[dev], gemm4_kernel<FMT, TN, PAIR, BULK>, &cfg);
         }
     });
     FP8MLP_CUDA_CHECK(err_dev[dev]);
@@ -523,39 +685,49 @@ int launch4(const CUtensorMap (&tm)[4], const Gemm4Args& a, int sm_count, cudaSt
         grid = tiles * a.split;                               // a tile per CTA or cluster
     }
     cfg.gridDim = dim3(static_cast<unsigned>(grid));
-    FP8MLP_CUDA_CHECK(cudaLaunchKernelEx(&cfg, gemm4_kernel<FMT, TN, PAIR>, tm[0], tm[1], tm[2], tm[3], a));
+    FP8MLP_CUDA_CHECK(cudaLaunchKernelEx(&cfg, gemm4_kernel<FMT, TN, PAIR, BULK>, tm[0], tm[1], tm[2], tm[3], tm[4], a));
     count_launch();
     return FP8MLP_OK;
 }
 
 struct Plan4 { bool pair, swap; int tn, split; };
 
-// How a product runs.  Many tiles: CTA pairs on 256 x 192 tiles.  Otherwise tiles of 128 rows of the longer side (if the other
-// has at most 128 rows) by as many columns as the other side needs, and the contraction split until the CTAs fill the SMs.
+// How a product runs, by what was measured on 148 SMs (NVFP4, bf16 out; us in a chain of launches).
+// CTA pairs on 256 x 256 tiles, where at least half of the SMs get one (1536 x 2048 x 4096, 48 pairs: 11.4, single CTAs 14.0;
+// 1500 x 1500 x 4096, 36 pairs: 15.1 and 12.0).  Otherwise single CTAs: their 128 rows are of the longer side where the other one has
+// at most 128, by as many columns as that one needs; with more than 64 of them, tiles 64 wide as long as all are on the SMs at once
+// (1024 x 1024 x 1024: 4.7, 128 wide 6.1; 512 x 8192 x 1024, 512 tiles: 11.0 and 8.5).  The contraction is split where it has 8 stages
+// or more (1 x 4096 x 4096, 16 stages: 6.5 -> 5.8 with 4 shares; 1 x 4096 x 1024, 4 stages: 4.0 -> 4.8 with 2), into shares of at least
+// 2 stages, for as many CTAs as there are SMs (256 x 4096 x 4096, 128 tiles: 9.3 whole, 10.6 with 2 shares), or twice as many
+// where a share still has 16 stages (1 x 11008 x 11008, 86 tiles: 18.1 -> 15.9).
 Plan4 plan4(int64_t M, int64_t N, int64_t K, int sms) {
     Plan4 pl{};
     const int64_t shorter = M < N ? M : N;
-    const int64_t pairs = (M + 255) / 256 * ((N + 191) / 192);
+    const int64_t pairs = (M + 255) / 256 * ((N + 255) / 256);
     pl.pair = shorter > 128 && 2 * pairs >= sms / 2;
-    if (pl.pair) { pl.tn = 192; pl.split = 1; return pl; }
+    if (pl.pair) { pl.tn = 256; pl.split = 1; return pl; }
     pl.swap = shorter <= 128 && M < N;
-    pl.tn = shorter <= 16 ? 16 : shorter <= 32 ? 32 : shorter <= 64 ? 64 : 128;
     const int64_t P = pl.swap ? N : M, Q = pl.swap ? M : N;
-    const int64_t tiles = (P + 127) / 128 * ((Q + pl.tn - 1) / pl.tn), room = static_cast<int64_t>(sms) * 2;
+    auto tiles = [&](int tn) { return (P + 127) / 128 * ((Q + tn - 1) / tn); };
+    pl.tn = shorter <= 16 ? 16 : shorter <= 32 ? 32 : shorter <= 64 || tiles(64) <= 2 * sms ? 64 : 128;
     const int64_t stages = (K + kStageK - 1) / kStageK;
+    auto fits = [&](int split) {
+        const int64_t ctas = tiles(pl.tn) * split;
+        return stages >= 8 && stages >= 2 * split && (ctas <= sms || (ctas <= 2 * sms && stages >= 16 * split));
+    };
     pl.split = 8;
-    while (pl.split > 1 && (tiles * pl.split > room || stages < 2 * pl.split)) pl.split /= 2;
+    while (pl.split > 1 && !fits(pl.split)) pl.split /= 2;
     return pl;
 }
 
 template <int FMT>
-int dispatch4(const Plan4& pl, const CUtensorMap (&tm)[4], const Gemm4Args& a, int sms, cudaStream_t st) {
-    if (pl.pair) return launch4<FMT, 192, true>(tm, a, sms, st);
+int dispatch4(const Plan4& pl, const CUtensorMap (&tm)[5], const Gemm4Args& a, int sms, cudaStream_t st) {
+    if (pl.pair) return a.vec == 16 ? launch4<FMT, 256, true, true>(tm, a, sms, st) : launch4<FMT, 256, true, false>(tm, a, sms, st);
     switch (pl.tn) {
-        case 16: return launch4<FMT, 16, false>(tm, a, sms, st);
-        case 32: return launch4<FMT, 32, false>(tm, a, sms, st);
-        case 64: return launch4<FMT, 64, false>(tm, a, sms, st);
-        default: return launch4<FMT, 128, false>(tm, a, sms, st);
+        case 16: return launch4<FMT, 16, false, false>(tm, a, sms, st);
+        case 32: return launch4<FMT, 32, false, false>(tm, a, sms, st);
+        case 64: return launch4<FMT, 64, false, false>(tm, a, sms, st);
+        default: return launch4<FMT, 128, false, false>(tm, a, sms, st);
     }
 }
 
@@ -589,7 +761,7 @@ extern "C" int fp8mlp_gemm_fp4(int64_t M, int64_t N, int64_t K, int fmt, const u
     struct Side { const uint8_t *codes, *scales; int64_t ld, rows; };
     const Side a_side{A, a_scales, ld_a, M}, b_side{B, b_scales, ld_b, N};
     const Side &P = pl.swap ? b_side : a_side, &Q = pl.swap ? a_side : b_side;
-    CUtensorMap tm[4];
+    CUtensorMap tm[5] = {};
     const uint64_t row_bytes = static_cast<uint64_t>((K + 1) / 2);
     const uint32_t sf_rows = 4u * kStageK / (4u * block);                     // 128-byte rows of a stage's scales
     auto codes_map = [&](CUtensorMap* m, const Side& s, uint32_t box) { return make_tmap_fp4(m, s.codes, row_bytes, s.rows, s.ld, box); };
@@ -600,19 +772,21 @@ extern "C" int fp8mlp_gemm_fp4(int64_t M, int64_t N, int64_t K, int fmt, const u
     if (rc == FP8MLP_OK) rc = codes_map(&tm[1], Q, pl.pair ? pl.tn / 2 : pl.tn);
     if (rc == FP8MLP_OK) rc = scales_map(&tm[2], P, 1);
     if (rc == FP8MLP_OK) rc = scales_map(&tm[3], Q, (pl.tn + 127) / 128);
+    const int vec = aligned(out, 16) && (M <= 1 || ld_out * bytes % 16 == 0) ? 16 : 1;
+    if (rc == FP8MLP_OK && pl.pair && vec == 16)
+        rc = out_dtype == FP8MLP_F32 ? make_tmap_out_f32(&tm[4], out, N, M, ld_out * bytes) : make_tmap_out_bf16(&tm[4], out, N, M, ld_out * bytes);
     if (rc != FP8MLP_OK) return rc;
     Gemm4Args a{};
     a.P = static_cast<int>(P.rows); a.Q = static_cast<int>(Q.rows); a.K = static_cast<int>(K);
     a.p_tiles = (a.P + (pl.pair ? 255 : 127)) / (pl.pair ? 256 : 128);
     a.q_tiles = (a.Q + pl.tn - 1) / pl.tn;
+    if (pl.tn < 64 && a.q_tiles != 1) return FP8MLP_ERR_SHAPE;               // (the plan makes none: see q_offset)
     a.stages_k = static_cast<int>((K + kStageK - 1) / kStageK);
     a.split = pl.split;
     a.group = 16;
     a.swap = pl.swap ? 1 : 0;
     a.f32 = out_dtype == FP8MLP_F32 ? 1 : 0;
-    a.vec = 1;
-    for (int v = 32; v >= 16 && a.vec == 1; v /= 2)
-        if (aligned(out, v) && (M <= 1 || ld_out * bytes % v == 0)) a.vec = v;
+    a.vec = vec;
     a.s0 = scale_a; a.s1 = scale_b;
     a.out = static_cast<uint8_t*>(out);
     a.ld_out = ld_out;

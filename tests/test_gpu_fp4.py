@@ -182,6 +182,21 @@ def test_product_on_cta_pairs(fmt, M, N, K):
         product_close(out, av, bv)
 
 
+@pytest.mark.parametrize("M,N,K", [(2100, 2070, 320), (300, 1000, 64), (140, 129, 2048), (2049, 1985, 33)])
+def test_product_rows_on_any_boundary(M, N, K):
+    """Rows that begin on even and odd elements, ends inside a block of 32 x 32, and what lies around them."""
+    a, av = operand(M, K, B.MXFP4, 1)
+    b, bv = operand(N, K, B.MXFP4, 2)
+    for dtype in (torch.float32, torch.bfloat16):
+        for pad, offset in ((0, 0), (1, 0), (2, 1), (2 + N % 2, 1), (8 - N % 8, 8), (8 - N % 8, 4)):
+            base = torch.full((offset + M * (N + pad) + 64,), 33.0, dtype=dtype, device="cuda")
+            out = base[offset:offset + M * (N + pad)].view(M, N + pad)[:, :N]
+            B.fp8mlp_gemm_fp4(a, b, out)
+            product_close(out, av, bv)
+            out.fill_(33.0)
+            assert (base == 33.0).all()
+
+
 @pytest.mark.parametrize("fmt", FORMATS)
 @pytest.mark.parametrize("M", [1, 40, 2048])
 def test_product_nan_stays_in_its_row(fmt, M):
