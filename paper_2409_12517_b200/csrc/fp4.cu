@@ -13,7 +13,8 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kTileRows = 128;            // operand rows of a block of threads, and of a tile of scales
 constexpr int kScaleTile = 512;           // bytes: 128 rows x 4 blocks
-constexpr int kCols = 256;                // operand columns of a block of threads, matrix as it is
+constexpr int kCols = 128;                // operand columns of a block of threads, matrix as it is
+constexpr int kColsBack = 256;            // and back
 template <int FMT> struct Fmt;
 template <> struct Fmt<FP8MLP_MXFP4> { static constexpr int kBlock = 32; };
 template <> struct Fmt<FP8MLP_NVFP4> { static constexpr int kBlock = 16; };
@@ -76,12 +77,10 @@ __device__ __forceinline__ float tensor_scale(float amax) {
     return ldexpf(1.0f, max(-100, min(100, k)));
 }
 
-// One block of values (of which those past the matrix are 0) -> its codes, eight to a word, and its scale's byte.
+// A block of values, or N of them (those past the matrix are 0) -> their codes, eight to a word, and the block's scale's byte.
 // `top`: max |src| of the block's bit patterns (a NaN is above infinity there).  g: the tensor's scale (NVFP4).
-template <int FMT>
-__device__ __forceinline__ uint32_t quantise_block(const float (&v)[Fmt<FMT>::kBlock], uint32_t top, float g,
-                                                   uint32_t (&code)[Fmt<FMT>::kBlock / 8]) {
-    constexpr int N = Fmt<FMT>::kBlock;
+template <int FMT, int N>
+__device__ __forceinline__ uint32_t quantise_block(const float (&v)[N], uint32_t top, float g, uint32_t (&code)[N / 8]) {
     if constexpr (FMT == FP8MLP_MXFP4) {
         // exponent field of 2^(floor(log2 a) - 2), biased as E8M0; subnormal and zero maxima get the smallest scale
         uint32_t byte = top >> 23;
@@ -99,10 +98,14 @@ __device__ __forceinline__ uint32_t quantise_block(const float (&v)[Fmt<FMT>::kB
     } else {
         const float a = __fmul_rn(__uint_as_float(top), g);
         const bool finite = __float_as_uint(a) < 0x7f800000u;
-        const uint32_t byte = cvt_fp8x2<FP8MLP_E4M3>(finite ? __fdiv_rn(a, 6.0f) : 0.0f, 0.0f) & 0xffu;
+        // a / 6: a product with the reciprocal, corrected with its remainder.  E4M3's borders times 6 are fp32 numbers, and for any
+        // other a the quotient is more than half a last place from them, so that what is left of its error turns no scale.
+        constexpr float kSixth = 1.0f / 6.0f;
+        const float near = __fmul_rn(a, kSixth), sixth = __fmaf_rn(__fmaf_rn(-6.0f, near, a), kSixth, near);
+        const uint32_t byte = cvt_fp8x2<FP8MLP_E4M3>(finite ? sixth : 0.0f, 0.0f) & 0xffu;
         float s, unused;
         e4m3x2_to_f32(byte, s, unused);
-        const float r = s > 0.0f ? __fdiv_rn(1.0f, s) : 0.0f;
+        const float r = s > 0.0f ? rcp_approx(s) : 0.0f;       // within a last place, which the correction below squares
         const f32x2 g2 = pack2(g, g), s2 = pack2(-s, -s), r2 = pack2(r, r);
 #pragma unroll
         for (int i = 0; i < N / 8; ++i) {
@@ -170,85 +173,157 @@ __device__ __forceinline__ void write_scales(const QuantArgs& p, const uint8_t* 
 }
 
 // ---------------------------------------------------------------- the matrix as it is
-// A thread takes a block of 16 or 32 columns of a row at a time, neighbours take neighbouring blocks of the row; the loads of
-// kBatch blocks (128 bytes) are on their way together, which takes addresses without branches: a block that is not wholly
-// inside the matrix reads the first one instead, and its own elements one by one.
-// VEC: rows start on 16-byte boundaries and are at least one block long.
+// A block of threads has 128 columns of 128 rows, a thread 16 columns of every 32nd row (NVFP4 a block; MXFP4 half of one, whose
+// maximum it shares with its neighbour).  VEC: rows start on 16-byte boundaries; the loads of 128 bytes a thread are on their way
+// together, which takes addresses without branches: 16 columns that are not wholly inside the matrix read the first ones instead,
+// and their own elements one by one.  Other rows are fetched element by element, neighbouring lanes neighbouring elements, 32 rows
+// at a time while those before are worked on, and go through shared memory.
+// INSIDE: the block's rows and columns are all in the matrix.
+constexpr int kPart = 16, kParts = kCols / kPart, kRowStep = kThreads / kParts, kChunks = kTileRows / kRowStep;
+template <typename SRC> constexpr int kPitch = kCols + 16 / sizeof(SRC);
+
+template <typename SRC>
+__device__ __forceinline__ void unpack_part(const uint4 (&w)[kPart * sizeof(SRC) / 16], float (&v)[kPart]) {
+#pragma unroll
+    for (int i = 0; i < int(kPart * sizeof(SRC) / 16); ++i) {
+        const uint32_t words[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if constexpr (sizeof(SRC) == 4) v[4 * i + j] = __uint_as_float(words[j]);
+            else { v[(8 * i + 2 * j) % kPart] = bf16_lo(words[j]); v[(8 * i + 2 * j + 1) % kPart] = bf16_hi(words[j]); }
+        }
+    }
+}
+
+// The scales of rows of a tile that do not exist.
+__device__ __forceinline__ void no_rows(uint8_t* scales, int tiles, int first_row) {
+    for (int t = 0; t < tiles; ++t)
+        for (int r = first_row + threadIdx.x; r < kTileRows; r += kThreads) *reinterpret_cast<uint32_t*>(scales + t * kScaleTile + scale_at(r, 0)) = 0u;
+}
+
+// The 16 columns from `col` on of row r of the tile: codes (to `out`), scale, and what they add to the maximum.
+template <int FMT, bool INSIDE>
+__device__ __forceinline__ void finish_part(const QuantArgs& p, uint8_t* scales, int64_t row0, int64_t col, int part, int r, float g,
+                                            uint8_t* out, const float (&v)[kPart], float& seen) {
+    uint32_t top = top_bits(v);
+    if (p.amax_out != nullptr) {
+        if (top <= 0x7f800000u) {
+            seen = fmaxf(seen, __uint_as_float(top));
+        } else {
+#pragma unroll
+            for (int i = 0; i < kPart; ++i) seen = fmaxf(seen, fabsf(v[i]));
+        }
+    }
+    if (FMT == FP8MLP_MXFP4) top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+    uint32_t code[kPart / 8];
+    uint32_t byte = quantise_block<FMT, kPart>(v, top, g, code);
+    const bool here = INSIDE || row0 + r < p.rows;
+    const int64_t block_col = FMT == FP8MLP_MXFP4 ? col & ~int64_t(31) : col;
+    if (!INSIDE && (!here || block_col >= p.cols)) byte = 0;             // blocks that do not exist
+    if (INSIDE || (here && col < ((p.cols + 31) & ~int64_t(31)))) st_global_v2(out, code[0], code[1]);
+    const int b = FMT == FP8MLP_MXFP4 ? part >> 1 : part;
+    if (FMT == FP8MLP_NVFP4 || (part & 1) == 0) scales[(b >> 2) * kScaleTile + scale_at(r, b & 3)] = static_cast<uint8_t>(byte);
+}
+
+template <typename SRC, int FMT, bool INSIDE>
+__device__ __forceinline__ float quantise_aligned(const QuantArgs& p, uint8_t* scales, int64_t row0, int64_t col, int part, int r0, float g) {
+    constexpr int kWords = kPart * sizeof(SRC) / 16, kBatch = 8 / kWords;
+    float seen = 0.0f;
+    const bool whole = INSIDE || col + kPart <= p.cols;
+    const uint8_t* src = p.src + (row0 + r0) * p.ld + col * static_cast<int64_t>(sizeof(SRC));
+    uint8_t* out = p.codes + (row0 + r0) * p.ld_codes + col / 2;
+#pragma unroll 1
+    for (int first = 0; first < kChunks; first += kBatch) {
+        if (!INSIDE && row0 + first * kRowStep >= p.rows) {
+            no_rows(scales, kCols / (4 * Fmt<FMT>::kBlock), first * kRowStep);
+            break;
+        }
+        uint4 w[kBatch][kWords];
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) {
+            const uint8_t* at = src + (first + k) * kRowStep * p.ld;
+            if (!INSIDE && !(whole && row0 + r0 + (first + k) * kRowStep < p.rows)) at = p.src;
+#pragma unroll
+            for (int i = 0; i < kWords; ++i) w[k][i] = ld_global_nc_v4(at + 16 * i);
+        }
+#pragma unroll
+        for (int k = 0; k < kBatch; ++k) {
+            const int r = r0 + (first + k) * kRowStep;
+            float v[kPart];
+            unpack_part<SRC>(w[k], v);
+            if (!INSIDE && row0 + r >= p.rows) {
+#pragma unroll
+                for (int i = 0; i < kPart; ++i) v[i] = 0.0f;
+            } else if (!INSIDE && !whole) {
+                const SRC* at = reinterpret_cast<const SRC*>(src + (first + k) * kRowStep * p.ld);
+#pragma unroll
+                for (int i = 0; i < kPart; ++i) v[i] = col + i < p.cols ? to_f32(at[i]) : 0.0f;
+            }
+            finish_part<FMT, INSIDE>(p, scales, row0, col, part, r, g, out + (first + k) * kRowStep * p.ld_codes, v, seen);
+        }
+    }
+    return seen;
+}
+
+template <typename SRC, int FMT>
+__device__ __forceinline__ float quantise_unaligned(const QuantArgs& p, uint8_t* scales, int64_t row0, int64_t col0, int part, int r0, float g) {
+    constexpr int kRowsPerWarp = kRowStep / (kThreads / 32), kPerLane = kCols / 32;
+    constexpr int kBuffers = sizeof(SRC) == 4 ? 1 : 2;            // 17 KB either way
+    __shared__ __align__(16) SRC stage[kBuffers][kRowStep][kPitch<SRC>];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    float seen = 0.0f;
+    SRC next[kRowsPerWarp][kPerLane];
+    auto fetch = [&](int chunk) {
+#pragma unroll
+        for (int k = 0; k < kRowsPerWarp; ++k) {
+            const int64_t row = row0 + chunk * kRowStep + warp * kRowsPerWarp + k;
+            const SRC* at = reinterpret_cast<const SRC*>(p.src + row * p.ld) + col0;
+#pragma unroll
+            for (int i = 0; i < kPerLane; ++i) next[k][i] = row < p.rows && col0 + lane + 32 * i < p.cols ? at[lane + 32 * i] : SRC(0);
+        }
+    };
+    fetch(0);
+#pragma unroll 1
+    for (int chunk = 0; chunk < kChunks; ++chunk) {
+        if (row0 + chunk * kRowStep >= p.rows) {
+            no_rows(scales, kCols / (4 * Fmt<FMT>::kBlock), chunk * kRowStep);
+            break;
+        }
+#pragma unroll
+        for (int k = 0; k < kRowsPerWarp; ++k)
+#pragma unroll
+            for (int i = 0; i < kPerLane; ++i) stage[chunk % kBuffers][warp * kRowsPerWarp + k][lane + 32 * i] = next[k][i];
+        __syncthreads();
+        if (chunk + 1 < kChunks) fetch(chunk + 1);
+        uint4 w[kPart * sizeof(SRC) / 16];
+#pragma unroll
+        for (int i = 0; i < int(kPart * sizeof(SRC) / 16); ++i) w[i] = reinterpret_cast<const uint4*>(&stage[chunk % kBuffers][r0][part * kPart])[i];
+        if (kBuffers == 1) __syncthreads();
+        float v[kPart];
+        unpack_part<SRC>(w, v);
+        finish_part<FMT, false>(p, scales, row0, col0 + part * kPart, part, r0 + chunk * kRowStep, g,
+                                p.codes + (row0 + r0 + chunk * kRowStep) * p.ld_codes + (col0 + part * kPart) / 2, v, seen);
+    }
+    return seen;
+}
+
 template <typename SRC, int FMT, bool VEC>
 __global__ void __launch_bounds__(kThreads, 4) quantise_kernel(const QuantArgs p) {
-    constexpr int N = Fmt<FMT>::kBlock, kBlocks = kCols / N, kTiles = kBlocks / 4, kItems = kTileRows * kBlocks / kThreads;
-    constexpr int kWords = VEC ? N * sizeof(SRC) / 16 : 1, kBatch = VEC ? (kWords < 8 ? 8 / kWords : 1) : 1;
+    constexpr int kTiles = kCols / (4 * Fmt<FMT>::kBlock);
     __shared__ __align__(16) uint8_t scales[kTiles * kScaleTile];
     int64_t row_tile, col_tile;
     tile_of(p, row_tile, col_tile);
     const int64_t row0 = row_tile * kTileRows, col0 = col_tile * kCols;
-    const int b = threadIdx.x % kBlocks, r0 = threadIdx.x / kBlocks;
-    const int64_t col = col0 + b * N;
+    const int part = threadIdx.x % kParts, r0 = threadIdx.x / kParts;
     grid_dependency_wait();
     grid_launch_dependents();
     const float g = FMT == FP8MLP_NVFP4 ? scale_of(p) : 1.0f;
-    float seen = 0.0f;
-    const int64_t padded = (p.cols + 31) & ~int64_t(31);          // columns whose codes are written
-    const bool whole = col + N <= p.cols;
-#pragma unroll 1
-    for (int first = 0; first < kItems; first += kBatch) {
-        if (row0 + first * (kThreads / kBlocks) >= p.rows) {      // no row of the batch exists: its scales are 0
-            for (int k = 0; k < kBatch; ++k)
-                scales[(b >> 2) * kScaleTile + scale_at(r0 + (first + k) * (kThreads / kBlocks), b & 3)] = 0;
-            continue;
-        }
-        uint4 w[kBatch][kWords];
-        if constexpr (VEC) {
-#pragma unroll
-            for (int k = 0; k < kBatch; ++k) {
-                const int64_t row = row0 + r0 + (first + k) * (kThreads / kBlocks);
-                const uint8_t* at = (whole && row < p.rows) ? p.src + row * p.ld + col * static_cast<int64_t>(sizeof(SRC)) : p.src;
-#pragma unroll
-                for (int i = 0; i < kWords; ++i) w[k][i] = ld_global_nc_v4(at + 16 * i);
-            }
-        }
-#pragma unroll
-        for (int k = 0; k < kBatch; ++k) {
-            const int r = r0 + (first + k) * (kThreads / kBlocks);
-            const int64_t row = row0 + r;
-            uint32_t byte = 0;
-            if (row < p.rows && col < padded) {
-                float v[N];
-                if (VEC && whole) {
-#pragma unroll
-                    for (int i = 0; i < kWords; ++i) {
-                        const uint32_t words[4] = {w[k][i].x, w[k][i].y, w[k][i].z, w[k][i].w};
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            if constexpr (sizeof(SRC) == 4) v[(4 * i + j) % N] = __uint_as_float(words[j]);
-                            else { v[(8 * i + 2 * j) % N] = bf16_lo(words[j]); v[(8 * i + 2 * j + 1) % N] = bf16_hi(words[j]); }
-                        }
-                    }
-                } else {
-                    const SRC* at = reinterpret_cast<const SRC*>(p.src + row * p.ld) + col;
-#pragma unroll
-                    for (int i = 0; i < N; ++i) v[i] = col + i < p.cols ? to_f32(at[i]) : 0.0f;
-                }
-                const uint32_t top = top_bits(v);
-                if (p.amax_out != nullptr) {
-                    if (top <= 0x7f800000u) {
-                        seen = fmaxf(seen, __uint_as_float(top));
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < N; ++i) seen = fmaxf(seen, fabsf(v[i]));
-                    }
-                }
-                uint32_t code[N / 8];
-                byte = quantise_block<FMT>(v, top, g, code);
-                if (col >= p.cols) byte = 0;
-                uint8_t* out = p.codes + row * p.ld_codes + col / 2;
-                if constexpr (N == 32) st_global_v4(out, code[0], code[1], code[2], code[3]); else st_global_v2(out, code[0], code[1]);
-            }
-            scales[(b >> 2) * kScaleTile + scale_at(r, b & 3)] = static_cast<uint8_t>(byte);
-        }
-    }
+    float seen;
+    if constexpr (!VEC) seen = quantise_unaligned<SRC, FMT>(p, scales, row0, col0, part, r0, g);
+    else if (row0 + kTileRows <= p.rows && col0 + kCols <= p.cols) seen = quantise_aligned<SRC, FMT, true>(p, scales, row0, col0 + part * kPart, part, r0, g);
+    else seen = quantise_aligned<SRC, FMT, false>(p, scales, row0, col0 + part * kPart, part, r0, g);
     __syncthreads();
-    write_scales(p, scales, row_tile, col0 / (4 * N), kTiles);
+    write_scales(p, scales, row_tile, col0 / (4 * Fmt<FMT>::kBlock), kTiles);
     if (p.amax_out != nullptr) raise_amax(seen, p.amax_out);
 }
 
@@ -260,9 +335,9 @@ __global__ void __launch_bounds__(kThreads, 4) quantise_kernel(const QuantArgs p
 // that can be read at once.
 template <typename SRC, int FMT, bool VEC>
 __global__ void __launch_bounds__(kThreads, FMT == FP8MLP_MXFP4 ? 3 : 4) quantise_transposed_kernel(const QuantArgs p) {
-    constexpr int N = Fmt<FMT>::kBlock, kColsT = 4 * N, kPitch = kColsT / 2 + 16;
+    constexpr int N = Fmt<FMT>::kBlock, kColsT = 4 * N, kCodePitch = kColsT / 2 + 16;
     __shared__ __align__(16) uint8_t scales[kScaleTile];
-    __shared__ __align__(16) uint8_t codes[kTileRows * kPitch];
+    __shared__ __align__(16) uint8_t codes[kTileRows * kCodePitch];
     int64_t row_tile, col_tile;
     tile_of(p, row_tile, col_tile);
     const int64_t row0 = row_tile * kTileRows, col0 = col_tile * kColsT;
@@ -275,10 +350,12 @@ __global__ void __launch_bounds__(kThreads, FMT == FP8MLP_MXFP4 ? 3 : 4) quantis
     float v[2][N];
     {
         const int c0 = VEC ? min(pair, rows - 2) : min(pair, rows - 1), c1 = min(pair + 1, rows - 1);      // (VEC: rows is even)
-        const uint8_t* base = p.src + col0 * p.ld + row0 * static_cast<int64_t>(sizeof(SRC));
+        const uint8_t* base = p.src + (col0 + min(k0, cols - 1)) * p.ld + row0 * static_cast<int64_t>(sizeof(SRC));
+        const int last = max(cols - 1 - k0, 0);                 // rows of the source that lie behind the first of the thread's
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const SRC* at = reinterpret_cast<const SRC*>(base + min(k0 + i, cols - 1) * p.ld);
+            const SRC* at = reinterpret_cast<const SRC*>(base);
+            if (i < last) base += p.ld;
             if constexpr (VEC && sizeof(SRC) == 4) {
                 const float2 w = __ldg(reinterpret_cast<const float2*>(at + c0));
                 v[0][i] = w.x; v[1][i] = w.y;
@@ -319,10 +396,10 @@ __global__ void __launch_bounds__(kThreads, FMT == FP8MLP_MXFP4 ? 3 : 4) quantis
             }
         }
         uint32_t code[N / 8];
-        const uint32_t byte = quantise_block<FMT>(v[c], top, g, code);
+        const uint32_t byte = quantise_block<FMT, N>(v[c], top, g, code);
         scales[scale_at(r, b)] = static_cast<uint8_t>(r < rows && k0 < cols ? byte : 0u);
-        if constexpr (N == 32) *reinterpret_cast<uint4*>(codes + r * kPitch + k0 / 2) = make_uint4(code[0], code[1], code[2], code[3]);
-        else *reinterpret_cast<uint2*>(codes + r * kPitch + k0 / 2) = make_uint2(code[0], code[1]);
+        if constexpr (N == 32) *reinterpret_cast<uint4*>(codes + r * kCodePitch + k0 / 2) = make_uint4(code[0], code[1], code[2], code[3]);
+        else *reinterpret_cast<uint2*>(codes + r * kCodePitch + k0 / 2) = make_uint2(code[0], code[1]);
     }
     __syncthreads();
     write_scales(p, scales, row_tile, col_tile, 1);
@@ -330,35 +407,41 @@ __global__ void __launch_bounds__(kThreads, FMT == FP8MLP_MXFP4 ? 3 : 4) quantis
     for (int i = threadIdx.x; i < kTileRows * (kColsT / 32); i += kThreads) {
         const int r = i / (kColsT / 32), c = i % (kColsT / 32);
         if (r < rows && 32 * c < padded)
-            *reinterpret_cast<uint4*>(p.codes + (row0 + r) * p.ld_codes + (col0 + 32 * c) / 2) = *reinterpret_cast<const uint4*>(codes + r * kPitch + 16 * c);
+            *reinterpret_cast<uint4*>(p.codes + (row0 + r) * p.ld_codes + (col0 + 32 * c) / 2) = *reinterpret_cast<const uint4*>(codes + r * kCodePitch + 16 * c);
     }
     if (p.amax_out != nullptr) raise_amax(seen, p.amax_out);
 }
 
-// max |src| over a matrix with a row stride, NaN left out
-template <typename SRC, bool VEC>
-__global__ void __launch_bounds__(kThreads) amax_kernel(const uint8_t* src, int64_t ld, int64_t rows, int64_t cols, unsigned int* amax) {
+// max |src| over a matrix with a row stride, NaN left out.  A row is cut into units of 16 bytes on 16-byte boundaries, the first and
+// the last of which it may fill in part.  FLAT: one row, as a matrix without gaps between its rows is.
+template <typename SRC, bool FLAT>
+__global__ void __launch_bounds__(kThreads) amax_kernel(const uint8_t* src, int64_t ld, int64_t rows, int64_t cols, int64_t units, unsigned int* amax) {
     constexpr int kPer = 16 / sizeof(SRC);
-    const int64_t units = (cols + kPer - 1) / kPer, all = rows * units;
-    const int64_t step = static_cast<int64_t>(gridDim.x) * kThreads;
+    const int64_t step = static_cast<int64_t>(gridDim.x) * kThreads, step_rows = FLAT ? 0 : step / units, step_units = step - step_rows * units;
+    int64_t unit = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x, row = FLAT ? 0 : unit / units;
+    unit -= row * units;
     float seen = 0.0f;
     grid_dependency_wait();
     grid_launch_dependents();
-    const bool one_row = VEC && ld == cols * static_cast<int64_t>(sizeof(SRC)) && cols % kPer == 0;       // no division then
-    for (int64_t i0 = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x; i0 < all; i0 += 4 * step) {
+    while (FLAT ? unit < units : row < rows) {
         uint4 w[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            const int64_t i = i0 + k * step;
             w[k] = make_uint4(0u, 0u, 0u, 0u);
-            if (i >= all) continue;
-            const int64_t row = one_row ? 0 : i / units, unit = one_row ? i : i - row * units;
-            const SRC* at = reinterpret_cast<const SRC*>(src + row * ld) + unit * kPer;
-            if (VEC && (one_row || unit * kPer + kPer <= cols)) {
-                w[k] = ld_global_nc_v4(at);
-            } else {
-                for (int e = 0; e < kPer && unit * kPer + e < cols; ++e) seen = fmaxf(seen, fabsf(to_f32(at[e])));
+            if (FLAT ? unit < units : row < rows) {
+                const SRC* at = reinterpret_cast<const SRC*>(src + row * ld);
+                const int64_t first = unit * kPer - static_cast<int64_t>((reinterpret_cast<uintptr_t>(at) & 15) / sizeof(SRC));
+                if (first >= 0 && first + kPer <= cols) {
+                    w[k] = ld_global_nc_v4(at + first);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < kPer; ++e)
+                        if (first + e >= 0 && first + e < cols) seen = fmaxf(seen, fabsf(to_f32(at[first + e])));
+                }
             }
+            row += step_rows;
+            unit += step_units;
+            if (!FLAT && unit >= units) { unit -= units; ++row; }
         }
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
@@ -405,9 +488,9 @@ __device__ __forceinline__ float block_scale(uint32_t byte) {
 // ALIGN: bytes that output rows are aligned to (32 or 16).
 template <typename DST, int FMT, int ALIGN>
 __global__ void __launch_bounds__(kThreads) dequantise_kernel(const DequantArgs p) {
-    constexpr int N = Fmt<FMT>::kBlock, kPerRow = kCols / 32, kItems = kTileRows * kPerRow / kThreads, kStep = kThreads / kPerRow;
+    constexpr int N = Fmt<FMT>::kBlock, kPerRow = kColsBack / 32, kItems = kTileRows * kPerRow / kThreads, kStep = kThreads / kPerRow;
     const int64_t row_tile = blockIdx.x / p.col_tiles;
-    const int64_t row0 = row_tile * kTileRows, col = (blockIdx.x - row_tile * p.col_tiles) * kCols + 32 * (threadIdx.x % kPerRow);
+    const int64_t row0 = row_tile * kTileRows, col = (blockIdx.x - row_tile * p.col_tiles) * kColsBack + 32 * (threadIdx.x % kPerRow);
     grid_dependency_wait();
     grid_launch_dependents();
     if (col >= p.cols) return;
@@ -478,7 +561,7 @@ __global__ void __launch_bounds__(kThreads) dequantise_narrow_kernel(const Dequa
     const int64_t row_tile = blockIdx.x / p.col_tiles;
     const int warp = threadIdx.x >> 5;
     const int64_t row0 = row_tile * kNarrowRows + (warp >> 2) * kRowsPerWarp;
-    const int64_t col = (blockIdx.x - row_tile * p.col_tiles) * kCols + 64 * (warp & 3) + 2 * (threadIdx.x & 31);
+    const int64_t col = (blockIdx.x - row_tile * p.col_tiles) * kColsBack + 64 * (warp & 3) + 2 * (threadIdx.x & 31);
     grid_dependency_wait();
     grid_launch_dependents();
     if (col >= p.cols || row0 >= p.rows) return;
@@ -514,6 +597,10 @@ __global__ void __launch_bounds__(kThreads) dequantise_narrow_kernel(const Dequa
 bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 constexpr int64_t kMost = int64_t(1) << 24;      // rows and columns
 
+constexpr unsigned int kLittleShared = 8;        // percent
+template <typename SRC>
+bool vec_rows(const void* src, int64_t ld, int64_t cols) { return aligned(src, 16) && ld % 16 == 0 && cols >= kPart; }
+
 template <typename SRC, int FMT>
 cudaError_t launch_quantise(const QuantArgs& a, bool transpose, dim3 grid, cudaStream_t st) {
     if (transpose) {
@@ -521,19 +608,25 @@ cudaError_t launch_quantise(const QuantArgs& a, bool transpose, dim3 grid, cudaS
         return vec ? launch_chained(quantise_transposed_kernel<SRC, FMT, true>, grid, dim3(kThreads), 0, st, a)
                    : launch_chained(quantise_transposed_kernel<SRC, FMT, false>, grid, dim3(kThreads), 0, st, a);
     }
-    const bool vec = aligned(a.src, 16) && a.ld % 16 == 0 && a.cols >= Fmt<FMT>::kBlock;
-    return vec ? launch_chained(quantise_kernel<SRC, FMT, true>, grid, dim3(kThreads), 0, st, a)
-               : launch_chained(quantise_kernel<SRC, FMT, false>, grid, dim3(kThreads), 0, st, a);
+    if (!vec_rows<SRC>(a.src, a.ld, a.cols)) return launch_chained(quantise_kernel<SRC, FMT, false>, grid, dim3(kThreads), 0, st, a);
+    // behind the search for the maximum the SMs are divided nearly as needed, and asking again costs 4 us of blocks not set up early:
+    // worth it for large matrices only (1531 x 512 fp32 6.0 us, asking again 10; 11008 x 4096 fp32 64 and 57; 4096 x 4096 26.2 and 24.7)
+    const bool divided = a.amax_in != nullptr && a.rows * a.cols * static_cast<int64_t>(sizeof(SRC)) < (int64_t(64) << 20);
+    return divided ? launch_chained(quantise_kernel<SRC, FMT, true>, grid, dim3(kThreads), 0, st, a)
+                                : launch_chained_shared(kLittleShared, quantise_kernel<SRC, FMT, true>, grid, dim3(kThreads), 0, st, a);
 }
 
 template <typename SRC>
 cudaError_t launch_amax(const void* src, int64_t ld, int64_t rows, int64_t cols, unsigned int* amax, int sms, cudaStream_t st) {
-    const int64_t units = rows * ((cols * sizeof(SRC) + 15) / 16), blocks = (units + 4 * kThreads - 1) / (4 * kThreads);
+    constexpr int64_t kPer = 16 / sizeof(SRC);
+    if (ld == cols * static_cast<int64_t>(sizeof(SRC)) || rows == 1) { cols *= rows; rows = 1; }
+    // a row that begins inside a unit reaches into one more than its length says
+    const int64_t units = (cols + kPer - 1) / kPer + (aligned(src, 16) && (rows == 1 || ld % 16 == 0) ? 0 : 1);
+    const int64_t blocks = (rows * units + 4 * kThreads - 1) / (4 * kThreads);
     const dim3 grid(static_cast<unsigned>(blocks < 8 * sms ? blocks : 8 * sms));
     const uint8_t* p = static_cast<const uint8_t*>(src);
-    const bool vec = aligned(src, 16) && ld % 16 == 0;
-    return vec ? launch_chained(amax_kernel<SRC, true>, grid, dim3(kThreads), 0, st, p, ld, rows, cols, amax)
-               : launch_chained(amax_kernel<SRC, false>, grid, dim3(kThreads), 0, st, p, ld, rows, cols, amax);
+    return rows == 1 ? launch_chained_shared(kLittleShared, amax_kernel<SRC, true>, grid, dim3(kThreads), 0, st, p, ld, rows, cols, units, amax)
+                     : launch_chained_shared(kLittleShared, amax_kernel<SRC, false>, grid, dim3(kThreads), 0, st, p, ld, rows, cols, units, amax);
 }
 
 }  // namespace
@@ -615,7 +708,7 @@ extern "C" int fp8mlp_dequantize_fp4(const uint8_t* codes, int64_t ld_codes, con
                       : aligned(out, 16) && ld_out * (out_dtype == FP8MLP_F32 ? 4 : 2) % 16 == 0 ? 16
                                                                                                  : 1;
     const int tile_rows = align >= 16 ? kTileRows : kNarrowRows;
-    const int64_t tiles = (rows + tile_rows - 1) / tile_rows * ((cols + kCols - 1) / kCols);
+    const int64_t tiles = (rows + tile_rows - 1) / tile_rows * ((cols + kColsBack - 1) / kColsBack);
     if (tiles > INT32_MAX) return FP8MLP_ERR_SHAPE;
     if (rows > 0 && cols > 0 && (codes == nullptr || block_scales == nullptr || out == nullptr)) return FP8MLP_ERR_ARG;
     const int bytes = out_dtype == FP8MLP_F32 ? 4 : 2;
@@ -627,7 +720,7 @@ extern "C" int fp8mlp_dequantize_fp4(const uint8_t* codes, int64_t ld_codes, con
     a.ld_codes = ld_codes; a.ld_out = ld_out * bytes; a.rows = rows; a.cols = cols;
     const int per_tile = 4 * (fmt == FP8MLP_MXFP4 ? 32 : 16);
     a.scale_tiles = static_cast<int>((cols + per_tile - 1) / per_tile);
-    a.col_tiles = static_cast<int>((cols + kCols - 1) / kCols);
+    a.col_tiles = static_cast<int>((cols + kColsBack - 1) / kColsBack);
     const dim3 grid(static_cast<unsigned>(tiles));
 #define FP8MLP_DEQUANT(D, F)                                                                                  \
     (align == 32 ? launch_chained(dequantise_kernel<D, F, 32>, grid, dim3(kThreads), 0, st, a)                \

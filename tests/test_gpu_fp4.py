@@ -59,6 +59,23 @@ def test_quantise(fmt, dtype, transpose):
             check_operand(op, src, float(op.scale), transpose)
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows,cols,pad,offset", [(1, 1, 0, 0), (1, 7, 0, 3), (300, 517, 0, 0), (300, 517, 0, 1), (97, 515, 5, 3), (4, 100000, 0, 0),
+                                                  (2000, 9, 1, 0), (700, 1024, 8, 8)])
+def test_maximum_wherever_it_lies(rows, cols, pad, offset, dtype):
+    """The data's maximum in the corners and at the edges of rows on any boundary, with larger values and NaN between the rows."""
+    base = torch.full((offset + rows * (cols + pad) + 16,), 1e6, dtype=dtype, device="cuda")
+    base[::2] = math.nan
+    src = base[offset:offset + rows * (cols + pad)].view(rows, cols + pad)[:, :cols]
+    op = B.new_fp4(B.NVFP4, rows, cols)
+    for at in {(0, 0), (0, cols - 1), (rows - 1, 0), (rows - 1, cols - 1), (rows // 2, cols // 2), (rows // 3, cols - 1)}:
+        src.fill_(0.5)
+        src[at] = -3.0
+        B.fp8mlp_quantize_fp4(src, op, scale_mode=B.SCALE_FROM_CURRENT_AMAX)
+        assert float(op.amax) == 3.0 and float(op.scale) == R.tensor_scale(3.0)
+        check_operand(op, src, float(op.scale), False)
+
+
 @pytest.mark.parametrize("transpose", [False, True])
 @pytest.mark.parametrize("fmt", FORMATS)
 def test_quantise_special_blocks(fmt, transpose):
