@@ -31,6 +31,12 @@ struct QuantArgs {
     float* scale;                         // NVFP4; written where amax_in is given
     int col_tiles, scale_tiles;           // blocks of threads / tiles of scales along the columns
 };
+// the same matrix as the search for its maximum takes it: units of 16 bytes, a matrix without gaps as one row
+struct AmaxArgs {
+    const uint8_t* src;
+    int64_t ld, rows, cols, units;
+    unsigned int* amax;
+};
 
 // place of a block's scale in its tile
 __device__ __forceinline__ int scale_at(int row, int block) { return (row & 31) * 16 + (row >> 5) * 4 + block; }
@@ -308,23 +314,18 @@ __device__ __forceinline__ float quantise_unaligned(const QuantArgs& p, uint8_t*
 }
 
 template <typename SRC, int FMT, bool VEC>
-__global__ void __launch_bounds__(kThreads, 4) quantise_kernel(const QuantArgs p) {
+__device__ __forceinline__ float quantise_tile(const QuantArgs& p, int64_t row_tile, int64_t col_tile, float g) {
     constexpr int kTiles = kCols / (4 * Fmt<FMT>::kBlock);
     __shared__ __align__(16) uint8_t scales[kTiles * kScaleTile];
-    int64_t row_tile, col_tile;
-    tile_of(p, row_tile, col_tile);
     const int64_t row0 = row_tile * kTileRows, col0 = col_tile * kCols;
     const int part = threadIdx.x % kParts, r0 = threadIdx.x / kParts;
-    grid_dependency_wait();
-    grid_launch_dependents();
-    const float g = FMT == FP8MLP_NVFP4 ? scale_of(p) : 1.0f;
     float seen;
     if constexpr (!VEC) seen = quantise_unaligned<SRC, FMT>(p, scales, row0, col0, part, r0, g);
     else if (row0 + kTileRows <= p.rows && col0 + kCols <= p.cols) seen = quantise_aligned<SRC, FMT, true>(p, scales, row0, col0 + part * kPart, part, r0, g);
     else seen = quantise_aligned<SRC, FMT, false>(p, scales, row0, col0 + part * kPart, part, r0, g);
     __syncthreads();
     write_scales(p, scales, row_tile, col0 / (4 * Fmt<FMT>::kBlock), kTiles);
-    if (p.amax_out != nullptr) raise_amax(seen, p.amax_out);
+    return seen;
 }
 
 // ---------------------------------------------------------------- the transposed matrix
@@ -334,19 +335,14 @@ __global__ void __launch_bounds__(kThreads, 4) quantise_kernel(const QuantArgs p
 // codes go through shared memory, so that they leave in pieces of 32 or 64 bytes.  VEC: the source's columns come in pairs
 // that can be read at once.
 template <typename SRC, int FMT, bool VEC>
-__global__ void __launch_bounds__(kThreads, FMT == FP8MLP_MXFP4 ? 3 : 4) quantise_transposed_kernel(const QuantArgs p) {
+__device__ __forceinline__ float quantise_transposed_tile(const QuantArgs& p, int64_t row_tile, int64_t col_tile, float g) {
     constexpr int N = Fmt<FMT>::kBlock, kColsT = 4 * N, kCodePitch = kColsT / 2 + 16;
     __shared__ __align__(16) uint8_t scales[kScaleTile];
     __shared__ __align__(16) uint8_t codes[kTileRows * kCodePitch];
-    int64_t row_tile, col_tile;
-    tile_of(p, row_tile, col_tile);
     const int64_t row0 = row_tile * kTileRows, col0 = col_tile * kColsT;
     const int pair = 2 * (threadIdx.x & 63), b = threadIdx.x >> 6, k0 = N * b;        // operand rows of the tile, block
     const int rows = static_cast<int>(min(p.rows - row0, static_cast<int64_t>(kTileRows)));
     const int cols = static_cast<int>(min(p.cols - col0, static_cast<int64_t>(kColsT)));
-    grid_dependency_wait();
-    grid_launch_dependents();
-    const float g = FMT == FP8MLP_NVFP4 ? scale_of(p) : 1.0f;
     float v[2][N];
     {
         const int c0 = VEC ? min(pair, rows - 2) : min(pair, rows - 1), c1 = min(pair + 1, rows - 1);      // (VEC: rows is even)
@@ -409,34 +405,47 @@ __global__ void __launch_bounds__(kThreads, FMT == FP8MLP_MXFP4 ? 3 : 4) quantis
         if (r < rows && 32 * c < padded)
             *reinterpret_cast<uint4*>(p.codes + (row0 + r) * p.ld_codes + (col0 + 32 * c) / 2) = *reinterpret_cast<const uint4*>(codes + r * kCodePitch + 16 * c);
     }
+    return seen;
+}
+
+// ---------------------------------------------------------------- kernels
+// TRANSPOSED: of the source's transpose.  A block of threads to a tile.
+template <typename SRC, int FMT, bool TRANSPOSED, bool VEC>
+__global__ void __launch_bounds__(kThreads, TRANSPOSED && FMT == FP8MLP_MXFP4 ? 3 : 4) quantise_kernel(const QuantArgs p) {
+    int64_t row_tile, col_tile;
+    tile_of(p, row_tile, col_tile);
+    grid_dependency_wait();
+    grid_launch_dependents();
+    const float g = FMT == FP8MLP_NVFP4 ? scale_of(p) : 1.0f;
+    float seen;
+    if constexpr (TRANSPOSED) seen = quantise_transposed_tile<SRC, FMT, VEC>(p, row_tile, col_tile, g);
+    else seen = quantise_tile<SRC, FMT, VEC>(p, row_tile, col_tile, g);
     if (p.amax_out != nullptr) raise_amax(seen, p.amax_out);
 }
 
-// max |src| over a matrix with a row stride, NaN left out.  A row is cut into units of 16 bytes on 16-byte boundaries, the first and
-// the last of which it may fill in part.  FLAT: one row, as a matrix without gaps between its rows is.
+// max |src| over the units first, first + step, .. of a matrix with a row stride, NaN left out.  A row is cut into units of 16 bytes
+// on 16-byte boundaries, the first and the last of which it may fill in part.  FLAT: one row.
 template <typename SRC, bool FLAT>
-__global__ void __launch_bounds__(kThreads) amax_kernel(const uint8_t* src, int64_t ld, int64_t rows, int64_t cols, int64_t units, unsigned int* amax) {
+__device__ __forceinline__ float amax_of(const AmaxArgs& p, int64_t first_unit, int64_t step) {
     constexpr int kPer = 16 / sizeof(SRC);
-    const int64_t step = static_cast<int64_t>(gridDim.x) * kThreads, step_rows = FLAT ? 0 : step / units, step_units = step - step_rows * units;
-    int64_t unit = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x, row = FLAT ? 0 : unit / units;
+    const int64_t units = p.units, step_rows = FLAT ? 0 : step / units, step_units = step - step_rows * units;
+    int64_t unit = first_unit, row = FLAT ? 0 : unit / units;
     unit -= row * units;
     float seen = 0.0f;
-    grid_dependency_wait();
-    grid_launch_dependents();
-    while (FLAT ? unit < units : row < rows) {
+    while (FLAT ? unit < units : row < p.rows) {
         uint4 w[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             w[k] = make_uint4(0u, 0u, 0u, 0u);
-            if (FLAT ? unit < units : row < rows) {
-                const SRC* at = reinterpret_cast<const SRC*>(src + row * ld);
+            if (FLAT ? unit < units : row < p.rows) {
+                const SRC* at = reinterpret_cast<const SRC*>(p.src + row * p.ld);
                 const int64_t first = unit * kPer - static_cast<int64_t>((reinterpret_cast<uintptr_t>(at) & 15) / sizeof(SRC));
-                if (first >= 0 && first + kPer <= cols) {
+                if (first >= 0 && first + kPer <= p.cols) {
                     w[k] = ld_global_nc_v4(at + first);
                 } else {
 #pragma unroll
                     for (int e = 0; e < kPer; ++e)
-                        if (first + e >= 0 && first + e < cols) seen = fmaxf(seen, fabsf(to_f32(at[first + e])));
+                        if (first + e >= 0 && first + e < p.cols) seen = fmaxf(seen, fabsf(to_f32(at[first + e])));
                 }
             }
             row += step_rows;
@@ -453,7 +462,50 @@ __global__ void __launch_bounds__(kThreads) amax_kernel(const uint8_t* src, int6
             }
         }
     }
-    raise_amax(seen, amax);
+    return seen;
+}
+template <typename SRC, bool FLAT>
+__global__ void __launch_bounds__(kThreads) amax_kernel(const AmaxArgs p) {
+    grid_dependency_wait();
+    grid_launch_dependents();
+    raise_amax(amax_of<SRC, FLAT>(p, static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x, static_cast<int64_t>(gridDim.x) * kThreads), p.amax);
+}
+
+// A small matrix with a scale of its own data (NVFP4) in one launch: the blocks of one cluster look for the maximum together,
+// exchange it over distributed shared memory and share the tiles.
+constexpr int kCluster = 16;
+template <typename SRC, bool TRANSPOSED, bool VEC>
+__global__ void __launch_bounds__(kThreads) quantise_small_kernel(const QuantArgs p, const AmaxArgs m, int tiles) {
+    __shared__ float warp_max[kThreads / 32], block_max[kCluster];
+    const int rank = static_cast<int>(cluster_ctarank());
+    cluster_begin();
+    grid_dependency_wait();
+    grid_launch_dependents();
+    float top = warp_max_nonneg(amax_of<SRC, false>(m, rank * kThreads + threadIdx.x, kCluster * kThreads));
+    if ((threadIdx.x & 31) == 0) warp_max[threadIdx.x >> 5] = top;
+    cluster_begun();
+    __syncthreads();
+    if (threadIdx.x < kCluster) {                     // to every block's list
+        top = warp_max[0];
+#pragma unroll
+        for (int i = 1; i < kThreads / 32; ++i) top = fmaxf(top, warp_max[i]);
+        st_cluster_f32(mapa_shared(smem_u32(&block_max[rank]), threadIdx.x), top);
+    }
+    cluster_sync_all();
+    top = block_max[0];
+#pragma unroll
+    for (int i = 1; i < kCluster; ++i) top = fmaxf(top, block_max[i]);
+    const float g = tensor_scale(top);
+    if (rank == 0 && threadIdx.x == 0) {
+        *m.amax = __float_as_uint(top);
+        *p.scale = g;
+    }
+    for (int tile = rank; tile < tiles; tile += kCluster) {
+        const int row_tile = tile / p.col_tiles;
+        if constexpr (TRANSPOSED) quantise_transposed_tile<SRC, FP8MLP_NVFP4, VEC>(p, row_tile, tile - row_tile * p.col_tiles, g);
+        else quantise_tile<SRC, FP8MLP_NVFP4, VEC>(p, row_tile, tile - row_tile * p.col_tiles, g);
+        __syncthreads();                              // the tile's shared memory is free
+    }
 }
 
 __global__ void scale_only_kernel(const unsigned int* amax, float* scale) {        // a matrix without elements
@@ -596,37 +648,70 @@ __global__ void __launch_bounds__(kThreads) dequantise_narrow_kernel(const Dequa
 // ---------------------------------------------------------------- host side
 bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 constexpr int64_t kMost = int64_t(1) << 24;      // rows and columns
+// One launch instead of three (its call 5.8 us, theirs 9.6) up to where 16 SMs take longer for the data: 256 x 1024 bf16 4.9 and 5.0 us
+// on the device, 512 x 1024 7.4 and 4.9.
+constexpr int64_t kSmallBytes = int64_t(512) << 10, kSmallTiles = 2 * kCluster;
 
 constexpr unsigned int kLittleShared = 8;        // percent
+
 template <typename SRC>
 bool vec_rows(const void* src, int64_t ld, int64_t cols) { return aligned(src, 16) && ld % 16 == 0 && cols >= kPart; }
+// pairs of columns can be read at once
+template <typename SRC>
+bool vec_pairs(const QuantArgs& a) { return aligned(a.src, 2 * sizeof(SRC)) && a.ld % (2 * sizeof(SRC)) == 0 && a.rows % 2 == 0; }
 
 template <typename SRC, int FMT>
 cudaError_t launch_quantise(const QuantArgs& a, bool transpose, dim3 grid, cudaStream_t st) {
-    if (transpose) {
-        const bool vec = aligned(a.src, 2 * sizeof(SRC)) && a.ld % (2 * sizeof(SRC)) == 0 && a.rows % 2 == 0;
-        return vec ? launch_chained(quantise_transposed_kernel<SRC, FMT, true>, grid, dim3(kThreads), 0, st, a)
-                   : launch_chained(quantise_transposed_kernel<SRC, FMT, false>, grid, dim3(kThreads), 0, st, a);
-    }
-    if (!vec_rows<SRC>(a.src, a.ld, a.cols)) return launch_chained(quantise_kernel<SRC, FMT, false>, grid, dim3(kThreads), 0, st, a);
+    if (transpose)
+        return vec_pairs<SRC>(a) ? launch_chained(quantise_kernel<SRC, FMT, true, true>, grid, dim3(kThreads), 0, st, a)
+                                 : launch_chained(quantise_kernel<SRC, FMT, true, false>, grid, dim3(kThreads), 0, st, a);
+    if (!vec_rows<SRC>(a.src, a.ld, a.cols)) return launch_chained(quantise_kernel<SRC, FMT, false, false>, grid, dim3(kThreads), 0, st, a);
     // behind the search for the maximum the SMs are divided nearly as needed, and asking again costs 4 us of blocks not set up early:
     // worth it for large matrices only (1531 x 512 fp32 6.0 us, asking again 10; 11008 x 4096 fp32 64 and 57; 4096 x 4096 26.2 and 24.7)
     const bool divided = a.amax_in != nullptr && a.rows * a.cols * static_cast<int64_t>(sizeof(SRC)) < (int64_t(64) << 20);
-    return divided ? launch_chained(quantise_kernel<SRC, FMT, true>, grid, dim3(kThreads), 0, st, a)
-                                : launch_chained_shared(kLittleShared, quantise_kernel<SRC, FMT, true>, grid, dim3(kThreads), 0, st, a);
+    return divided ? launch_chained(quantise_kernel<SRC, FMT, false, true>, grid, dim3(kThreads), 0, st, a)
+                   : launch_chained_shared(kLittleShared, quantise_kernel<SRC, FMT, false, true>, grid, dim3(kThreads), 0, st, a);
 }
 
 template <typename SRC>
-cudaError_t launch_amax(const void* src, int64_t ld, int64_t rows, int64_t cols, unsigned int* amax, int sms, cudaStream_t st) {
+AmaxArgs amax_args(const void* src, int64_t ld, int64_t rows, int64_t cols, unsigned int* amax) {
     constexpr int64_t kPer = 16 / sizeof(SRC);
     if (ld == cols * static_cast<int64_t>(sizeof(SRC)) || rows == 1) { cols *= rows; rows = 1; }
     // a row that begins inside a unit reaches into one more than its length says
     const int64_t units = (cols + kPer - 1) / kPer + (aligned(src, 16) && (rows == 1 || ld % 16 == 0) ? 0 : 1);
-    const int64_t blocks = (rows * units + 4 * kThreads - 1) / (4 * kThreads);
+    return AmaxArgs{static_cast<const uint8_t*>(src), ld, rows, cols, units, amax};
+}
+
+template <typename SRC>
+cudaError_t launch_amax(const AmaxArgs& a, int sms, cudaStream_t st) {
+    const int64_t blocks = (a.rows * a.units + 4 * kThreads - 1) / (4 * kThreads);
     const dim3 grid(static_cast<unsigned>(blocks < 8 * sms ? blocks : 8 * sms));
-    const uint8_t* p = static_cast<const uint8_t*>(src);
-    return rows == 1 ? launch_chained_shared(kLittleShared, amax_kernel<SRC, true>, grid, dim3(kThreads), 0, st, p, ld, rows, cols, units, amax)
-                     : launch_chained_shared(kLittleShared, amax_kernel<SRC, false>, grid, dim3(kThreads), 0, st, p, ld, rows, cols, units, amax);
+    return a.rows == 1 ? launch_chained_shared(kLittleShared, amax_kernel<SRC, true>, grid, dim3(kThreads), 0, st, a)
+                       : launch_chained_shared(kLittleShared, amax_kernel<SRC, false>, grid, dim3(kThreads), 0, st, a);
+}
+
+template <typename SRC, bool TRANSPOSED, bool VEC>
+cudaError_t launch_small(const QuantArgs& a, const AmaxArgs& m, int tiles, cudaStream_t st) {
+    cudaError_t e = cudaFuncSetAttribute(quantise_small_kernel<SRC, TRANSPOSED, VEC>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(kCluster);
+    cfg.blockDim = dim3(kThreads);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = kCluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, quantise_small_kernel<SRC, TRANSPOSED, VEC>, a, m, tiles);
+}
+template <typename SRC>
+cudaError_t dispatch_small(const QuantArgs& a, const AmaxArgs& m, bool transpose, int tiles, cudaStream_t st) {
+    if (transpose) return vec_pairs<SRC>(a) ? launch_small<SRC, true, true>(a, m, tiles, st) : launch_small<SRC, true, false>(a, m, tiles, st);
+    return vec_rows<SRC>(a.src, a.ld, a.cols) ? launch_small<SRC, false, true>(a, m, tiles, st) : launch_small<SRC, false, false>(a, m, tiles, st);
 }
 
 }  // namespace
@@ -664,7 +749,8 @@ extern "C" int fp8mlp_quantize_fp4(const void* src, int src_dtype, int64_t rows,
     int dev = 0, sms = 0;
     FP8MLP_CUDA_CHECK(cudaGetDevice(&dev));
     FP8MLP_CUDA_CHECK(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
-    if (amax != nullptr)
+    const bool one_launch = current && rows > 0 && cols > 0 && rows * cols * bytes <= kSmallBytes && tiles <= kSmallTiles;
+    if (amax != nullptr && !one_launch)
         if (int rc = clear_float(amax, st)) return rc;
     unsigned int* amax_bits = reinterpret_cast<unsigned int*>(amax);
     if (rows == 0 || cols == 0) {
@@ -675,9 +761,10 @@ extern "C" int fp8mlp_quantize_fp4(const void* src, int src_dtype, int64_t rows,
         return FP8MLP_OK;
     }
     const int64_t ld = ld_src * bytes;
-    if (current) {
-        FP8MLP_CUDA_CHECK(src_dtype == FP8MLP_F32 ? launch_amax<float>(src, ld, rows, cols, amax_bits, sms, st)
-                                                  : launch_amax<uint16_t>(src, ld, rows, cols, amax_bits, sms, st));
+    const bool f32 = src_dtype == FP8MLP_F32;
+    const AmaxArgs m = f32 ? amax_args<float>(src, ld, rows, cols, amax_bits) : amax_args<uint16_t>(src, ld, rows, cols, amax_bits);
+    if (current && !one_launch) {
+        FP8MLP_CUDA_CHECK(f32 ? launch_amax<float>(m, sms, st) : launch_amax<uint16_t>(m, sms, st));
         count_launch();
     }
     QuantArgs a{};
@@ -689,7 +776,11 @@ extern "C" int fp8mlp_quantize_fp4(const void* src, int src_dtype, int64_t rows,
     a.scale_tiles = static_cast<int>((C + per_tile - 1) / per_tile);
     a.col_tiles = static_cast<int>((C + width - 1) / width);
     const dim3 grid(static_cast<unsigned>(tiles));
-    const bool f32 = src_dtype == FP8MLP_F32;
+    if (one_launch) {
+        FP8MLP_CUDA_CHECK(f32 ? dispatch_small<float>(a, m, t, static_cast<int>(tiles), st) : dispatch_small<uint16_t>(a, m, t, static_cast<int>(tiles), st));
+        count_launch();
+        return FP8MLP_OK;
+    }
     const cudaError_t e = fmt == FP8MLP_MXFP4 ? (f32 ? launch_quantise<float, FP8MLP_MXFP4>(a, t, grid, st) : launch_quantise<uint16_t, FP8MLP_MXFP4>(a, t, grid, st))
                                               : (f32 ? launch_quantise<float, FP8MLP_NVFP4>(a, t, grid, st) : launch_quantise<uint16_t, FP8MLP_NVFP4>(a, t, grid, st));
     FP8MLP_CUDA_CHECK(e);

@@ -12,6 +12,7 @@ namespace {
 
 constexpr uint32_t kAll = 0xffffffffu;
 constexpr int kMaxWarps = 16;
+constexpr int kCluster = 16;                // blocks of the one cluster that takes a short batch as a whole
 
 struct NormArgs {
     const uint8_t *x, *residual;
@@ -22,6 +23,7 @@ struct NormArgs {
     int64_t T, ld_x, ld_res, ld_h, ld_y;      // row strides in bytes
     float eps, inv_d;
     int units, tpr;                           // 32-byte units of a row; threads that share it
+    int cluster;                              // the grid is one cluster: it finds the maximum by itself
 };
 
 struct NormBackArgs {
@@ -32,6 +34,7 @@ struct NormBackArgs {
     int64_t T, ld_dy, ld_h, ld_dh, ld_dx;
     float inv_d;
     int units, tpr, d;
+    float* d_gain;                            // not null: the grid is one cluster, which adds the blocks' sums itself
 };
 
 template <typename SRC> struct Unit;          // 32 bytes of a row
@@ -129,6 +132,8 @@ template <typename SRC, int BLOCK, int NU, bool WIDE, int OUT>
 __global__ void __launch_bounds__(BLOCK) norm_kernel(const NormArgs p) {
     constexpr int E = Unit<SRC>::kElems;
     __shared__ float part[2][2 * kMaxWarps];
+    __shared__ float block_max[kCluster];
+    if (p.cluster) cluster_begin();
     const int sub = threadIdx.x / p.tpr, u0 = threadIdx.x % p.tpr, rows = BLOCK / p.tpr;
     const int64_t step = static_cast<int64_t>(gridDim.x) * rows;
     int64_t row = static_cast<int64_t>(blockIdx.x) * rows + sub;
@@ -221,16 +226,26 @@ __global__ void __launch_bounds__(BLOCK) norm_kernel(const NormArgs p) {
         __syncthreads();
         if (threadIdx.x < 32) {
             run_max = warp_max_nonneg(threadIdx.x < BLOCK / 32 ? part[0][threadIdx.x] : 0.0f);
-            // a single block has the whole maximum (nobody cleared the word for it then)
+            // a single block or cluster has the whole maximum (nobody cleared the word for it then)
             if (threadIdx.x == 0 && gridDim.x == 1) *p.amax = __float_as_uint(run_max);
-            else if (threadIdx.x == 0 && run_max > 0.0f) atomicMax(p.amax, __float_as_uint(run_max));
+            else if (threadIdx.x == 0 && !p.cluster && run_max > 0.0f) atomicMax(p.amax, __float_as_uint(run_max));
+        }
+        if (p.cluster) {
+            cluster_begun();
+            if (threadIdx.x == 0) st_cluster_f32(mapa_shared(smem_u32(&block_max[cluster_ctarank()]), 0), run_max);
+            cluster_sync_all();
+            if (blockIdx.x == 0 && threadIdx.x < 32) {
+                run_max = warp_max_nonneg(threadIdx.x < kCluster ? block_max[threadIdx.x] : 0.0f);
+                if (threadIdx.x == 0) *p.amax = __float_as_uint(run_max);
+            }
         }
     }
 }
 
 // ---------------------------------------------------------------- backward
 // A thread keeps the columns of its units through all rows of its block and sums their part of d_gain in registers (NU = 1)
-// or in its own words of shared memory; blocks leave one row of partial sums each, which a second kernel adds in their order.
+// or in its own words of shared memory; blocks leave one row of partial sums each, which a second kernel
+// adds in their order; a cluster that has the whole batch adds them over distributed shared memory.
 template <typename SRC, int BLOCK, int NU, bool WIDE>
 __global__ void __launch_bounds__(BLOCK) norm_backward_kernel(const NormBackArgs p) {
     constexpr int E = Unit<SRC>::kElems;
@@ -239,7 +254,7 @@ __global__ void __launch_bounds__(BLOCK) norm_backward_kernel(const NormBackArgs
     const int sub = threadIdx.x / p.tpr, u0 = threadIdx.x % p.tpr, rows = BLOCK / p.tpr;
     const int64_t step = static_cast<int64_t>(gridDim.x) * rows;
     int64_t row = static_cast<int64_t>(blockIdx.x) * rows + sub;
-    const bool want = p.partial != nullptr;
+    const bool together = p.d_gain != nullptr, want = p.partial != nullptr || together;
     float gain[E], acc[E];
 #pragma unroll
     for (int i = 0; i < E; ++i) acc[i] = 0.0f;
@@ -312,7 +327,7 @@ __global__ void __launch_bounds__(BLOCK) norm_backward_kernel(const NormBackArgs
     if (!want) return;
     float* out = p.partial + static_cast<int64_t>(blockIdx.x) * p.d;
     if (NU == 1) {
-        if (rows == 1) {
+        if (rows == 1 && !together) {
             if (u0 < p.units)
 #pragma unroll
                 for (int i = 0; i < E; i += 4) *reinterpret_cast<float4*>(out + u0 * E + i) = make_float4(acc[i], acc[i + 1], acc[i + 2], acc[i + 3]);
@@ -330,6 +345,21 @@ __global__ void __launch_bounds__(BLOCK) norm_backward_kernel(const NormBackArgs
                 for (int i = 0; i < E; ++i) d_gain_row[u0 * E + i] = turn == 0 ? acc[i] : __fadd_rn(d_gain_row[u0 * E + i], acc[i]);
             __syncthreads();
         }
+    }
+    if (together) {
+        // every block adds its share of the columns over all blocks' rows of sums, in the order of their ranks
+        cluster_sync_all();
+        for (int i = blockIdx.x * BLOCK + threadIdx.x; i < p.d; i += kCluster * BLOCK) {
+            const uint32_t at = smem_u32(d_gain_row + i);
+            float v[kCluster];
+#pragma unroll
+            for (int b = 0; b < kCluster; ++b) v[b] = ld_cluster_f32(mapa_shared(at, b));
+#pragma unroll
+            for (int b = 1; b < kCluster; ++b) v[0] = __fadd_rn(v[0], v[b]);
+            p.d_gain[i] = v[0];
+        }
+        cluster_sync_all();                                      // nobody leaves while its sums are read
+        return;
     }
     __syncthreads();
     for (int i = threadIdx.x; i < p.d; i += BLOCK) out[i] = d_gain_row[i];
@@ -395,15 +425,44 @@ RowShape row_shape(int64_t d, int elems) {
     return s;
 }
 
+// Whether one cluster takes the batch, without a launch before (which clears the maximum) or after it (which adds up the gradient of
+// the gain): two rounds of its blocks take as long on the device as the launch, and a call 2 us less (32 x 4096 bf16, two rounds:
+// forward 4.1 and 3.3 us on the device, 8.2 and 10.1 called, backward 6.0 and 5.6, 7.8 and 9.8; 64 x 4096, four rounds: 5.6 and 3.3 forward,
+// 7.6 and 5.6 backward).  Wide rows take longer than a launch already in their second round.
+bool one_cluster_does(const RowShape& s, int64_t blocks) { return blocks <= (s.nu == 1 ? 2 : 1) * kCluster; }
+
 // a row stride in elements -> bytes; false where it is no multiple of 16 bytes or shorter than the row
 bool stride_ok(int64_t T, int64_t ld, int64_t d, int bytes) { return T <= 1 || (ld >= d && ld * bytes % 16 == 0); }
 
+// A chained launch, or (one_cluster) of a grid that is one cluster.
+template <typename ARGS>
+cudaError_t launch_rows(void (*kernel)(ARGS), bool one_cluster, dim3 grid, int block, size_t smem, cudaStream_t st, const ARGS& a) {
+    if (!one_cluster) return launch_chained(kernel, grid, dim3(block), smem, st, a);
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3(block);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = kCluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, kernel, a);
+}
+
 template <typename SRC, int BLOCK, int NU, bool WIDE>
 cudaError_t launch_norm(const NormArgs& a, int out, dim3 grid, cudaStream_t st) {
+    const bool one = a.cluster != 0;
     switch (out) {
-        case FP8MLP_RMS_SAME: return launch_chained(norm_kernel<SRC, BLOCK, NU, WIDE, FP8MLP_RMS_SAME>, grid, dim3(BLOCK), 0, st, a);
-        case FP8MLP_RMS_E4M3: return launch_chained(norm_kernel<SRC, BLOCK, NU, WIDE, FP8MLP_RMS_E4M3>, grid, dim3(BLOCK), 0, st, a);
-        default: return launch_chained(norm_kernel<SRC, BLOCK, NU, WIDE, FP8MLP_RMS_E4M3_ROWS>, grid, dim3(BLOCK), 0, st, a);
+        case FP8MLP_RMS_SAME: return launch_rows(norm_kernel<SRC, BLOCK, NU, WIDE, FP8MLP_RMS_SAME>, one, grid, BLOCK, 0, st, a);
+        case FP8MLP_RMS_E4M3: return launch_rows(norm_kernel<SRC, BLOCK, NU, WIDE, FP8MLP_RMS_E4M3>, one, grid, BLOCK, 0, st, a);
+        default: return launch_rows(norm_kernel<SRC, BLOCK, NU, WIDE, FP8MLP_RMS_E4M3_ROWS>, one, grid, BLOCK, 0, st, a);
     }
 }
 
@@ -414,7 +473,7 @@ cudaError_t launch_norm_backward(const NormBackArgs& a, size_t smem, dim3 grid, 
                                              FP8MLP_MAX_NORM_WIDTH * 4);
         if (e != cudaSuccess) return e;
     }
-    return launch_chained(norm_backward_kernel<SRC, BLOCK, NU, WIDE>, grid, dim3(BLOCK), smem, st, a);
+    return launch_rows(norm_backward_kernel<SRC, BLOCK, NU, WIDE>, a.d_gain != nullptr, grid, BLOCK, smem, st, a);
 }
 
 // the instantiation for a shape: F<SRC, BLOCK, NU, WIDE>
@@ -464,8 +523,9 @@ extern "C" int fp8mlp_rmsnorm(int64_t T, int64_t d, int dtype, const void* x, in
     const bool wide = on32(x, a.ld_x) && (residual == nullptr || on32(residual, a.ld_res)) && (h_out == nullptr || on32(h_out, a.ld_h)) &&
                       (out_kind != FP8MLP_RMS_SAME || on32(y, a.ld_y));
     const int64_t rows = s.block / s.tpr, blocks = (T + rows - 1) / rows, most = static_cast<int64_t>(sms) * (1024 / s.block);
-    const dim3 grid(static_cast<unsigned>(blocks < most ? blocks : most));
-    if (amax != nullptr && grid.x > 1)
+    a.cluster = amax != nullptr && blocks > 1 && one_cluster_does(s, blocks) ? 1 : 0;
+    const dim3 grid(static_cast<unsigned>(a.cluster ? kCluster : blocks < most ? blocks : most));
+    if (amax != nullptr && grid.x > 1 && !a.cluster)
         if (int rc = clear_float(amax, st)) return rc;
     FP8MLP_CUDA_CHECK(FP8MLP_NORM_LAUNCH(launch_norm, a, out_kind, grid, st));
     count_launch();
@@ -505,11 +565,13 @@ extern "C" int fp8mlp_rmsnorm_backward(int64_t T, int64_t d, int dtype, const vo
     const int64_t rows = s.block / s.tpr, blocks = (T + rows - 1) / rows;
     int64_t most = static_cast<int64_t>(sms) * (512 / s.block);
     if (most > FP8MLP_RMS_PARTIALS) most = FP8MLP_RMS_PARTIALS;      // a row of the workspace per block
-    const dim3 grid(static_cast<unsigned>(blocks < most ? blocks : most));
-    const size_t smem = d_gain != nullptr && (s.nu > 1 || rows > 1) ? sizeof(float) * d : 0;
+    const bool one_cluster = d_gain != nullptr && one_cluster_does(s, blocks);
+    if (one_cluster) { a.d_gain = d_gain; a.partial = nullptr; }
+    const dim3 grid(static_cast<unsigned>(one_cluster ? kCluster : blocks < most ? blocks : most));
+    const size_t smem = d_gain != nullptr && (s.nu > 1 || rows > 1 || one_cluster) ? sizeof(float) * d : 0;
     FP8MLP_CUDA_CHECK(FP8MLP_NORM_LAUNCH(launch_norm_backward, a, smem, grid, st));
     count_launch();
-    if (d_gain != nullptr) {
+    if (d_gain != nullptr && !one_cluster) {
         FP8MLP_CUDA_CHECK(launch_chained(norm_gain_kernel, dim3(static_cast<unsigned>((d + 127) / 128)), dim3(32 * kGainWarps), 0, st,
                                          static_cast<const float*>(workspace), static_cast<int>(grid.x), static_cast<int>(d), d_gain));
         count_launch();
