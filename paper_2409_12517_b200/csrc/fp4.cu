@@ -544,112 +544,153 @@ __device__ __forceinline__ float block_scale(uint32_t byte) {
     }
 }
 
-// A thread takes 32 columns of a row at a time (16 bytes of codes), four rows' loads on their way together.
-// ALIGN: bytes that output rows are aligned to (32 or 16).
+// The 16 columns of 8 bytes of codes.
+template <int FMT>
+__device__ __forceinline__ void values_of(uint2 code, float scale, float inv_g, float (&v)[16]) {
+    const uint32_t words[2] = {code.x, code.y};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) e2m1x2_to_f32((words[i / 4] >> (8 * (i & 3))) & 0xffu, v[2 * i], v[2 * i + 1]);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        v[i] = __fmul_rn(v[i], scale);            // exact, but for MXFP4 scales at the ends of fp32's range
+        if constexpr (FMT == FP8MLP_NVFP4) v[i] = __fmul_rn(v[i], inv_g);
+    }
+}
+
+// A thread takes 64 bytes of output of a row at a time, 32 columns of bf16 or 16 of fp32; the loads of its rows are on their way
+// together.  ALIGN: bytes that output rows are aligned to (32 or 16).
 template <typename DST, int FMT, int ALIGN>
 __global__ void __launch_bounds__(kThreads) dequantise_kernel(const DequantArgs p) {
-    constexpr int N = Fmt<FMT>::kBlock, kPerRow = kColsBack / 32, kItems = kTileRows * kPerRow / kThreads, kStep = kThreads / kPerRow;
+    constexpr int N = Fmt<FMT>::kBlock, kPer = 64 / sizeof(DST), kHalves = kPer / 16;
+    constexpr int kPerRow = kColsBack / kPer, kStep = kThreads / kPerRow, kBatch = 4, kItems = kTileRows / kStep;
     const int64_t row_tile = blockIdx.x / p.col_tiles;
-    const int64_t row0 = row_tile * kTileRows, col = (blockIdx.x - row_tile * p.col_tiles) * kColsBack + 32 * (threadIdx.x % kPerRow);
+    const int64_t row0 = row_tile * kTileRows, col = (blockIdx.x - row_tile * p.col_tiles) * kColsBack + kPer * (threadIdx.x % kPerRow);
     grid_dependency_wait();
     grid_launch_dependents();
     if (col >= p.cols) return;
     const float inv_g = p.scale != nullptr ? __fdiv_rn(1.0f, *p.scale) : 1.0f;
     const int r0 = threadIdx.x / kPerRow;
-    const int64_t block = col / N;                    // the first of the columns' one or two blocks
+    const int64_t block = col / N;                    // the first of the columns' blocks (two: NVFP4 to bf16)
     const uint8_t* scales = p.scales + (row_tile * p.scale_tiles + block / 4) * kScaleTile + (block & 3);
-    uint4 code[kItems];
-    uint32_t bytes[kItems];
+#pragma unroll 1
+    for (int first = 0; first < kItems; first += kBatch) {
+        if (row0 + first * kStep >= p.rows) break;
+        uint2 code[kBatch][kHalves];
+        uint32_t bytes[kBatch];
 #pragma unroll
-    for (int it = 0; it < kItems; ++it) {
-        const int r = static_cast<int>(min(static_cast<int64_t>(r0 + it * kStep), p.rows - 1 - row0));
-        code[it] = ld_global_nc_v4(p.codes + (row0 + r) * p.ld_codes + col / 2);
-        if constexpr (N == 32) bytes[it] = __ldg(scales + scale_at(r, 0));
-        else bytes[it] = __ldg(reinterpret_cast<const unsigned short*>(scales + scale_at(r, 0)));
-    }
-#pragma unroll
-    for (int it = 0; it < kItems; ++it) {
-        const int64_t row = row0 + r0 + it * kStep;
-        if (row >= p.rows) break;
-        const float s[2] = {block_scale<FMT>(bytes[it] & 0xffu), block_scale<FMT>(N == 32 ? bytes[it] : bytes[it] >> 8)};
-        DST* out = reinterpret_cast<DST*>(p.out + row * p.ld_out) + col;
-        const uint32_t words[4] = {code[it].x, code[it].y, code[it].z, code[it].w};
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {                 // 16 columns at a time
-            float v[16];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) e2m1x2_to_f32((words[2 * h + i / 4] >> (8 * (i & 3))) & 0xffu, v[2 * i], v[2 * i + 1]);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                v[i] = __fmul_rn(v[i], s[h]);         // exact, but for MXFP4 scales at the ends of fp32's range
-                if constexpr (FMT == FP8MLP_NVFP4) v[i] = __fmul_rn(v[i], inv_g);
-            }
-            if (col + 16 * h + 16 <= p.cols) {
-#pragma unroll
-                for (int i = 0; i < 16; i += 32 / sizeof(DST)) {
-                    uint32_t w[8];
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        if constexpr (sizeof(DST) == 4) w[k] = __float_as_uint(v[(i + k) % 16]);
-                        else w[k] = cvt_bf16x2(v[(i + 2 * k) % 16], v[(i + 2 * k + 1) % 16]);
-                    }
-                    if constexpr (ALIGN >= 32) {
-                        st_global_v8(out + 16 * h + i, w);
-                    } else {
-                        st_global_v4(out + 16 * h + i, w[0], w[1], w[2], w[3]);
-                        st_global_v4(out + 16 * h + i + 16 / sizeof(DST), w[4], w[5], w[6], w[7]);
-                    }
-                }
+        for (int it = 0; it < kBatch; ++it) {
+            const int r = static_cast<int>(min(static_cast<int64_t>(r0 + (first + it) * kStep), p.rows - 1 - row0));
+            const uint8_t* at = p.codes + (row0 + r) * p.ld_codes + col / 2;
+            if constexpr (kHalves == 2) {
+                const uint4 w = ld_global_nc_v4(at);
+                code[it][0] = make_uint2(w.x, w.y);
+                code[it][1] = make_uint2(w.z, w.w);
             } else {
+                code[it][0] = __ldg(reinterpret_cast<const uint2*>(at));
+            }
+            if constexpr (N == 16 && kHalves == 2) bytes[it] = __ldg(reinterpret_cast<const unsigned short*>(scales + scale_at(r, 0)));
+            else bytes[it] = __ldg(scales + scale_at(r, 0));
+        }
 #pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (col + 16 * h + i < p.cols) {
-                        if constexpr (sizeof(DST) == 4) out[16 * h + i] = v[i];
-                        else out[16 * h + i] = static_cast<uint16_t>(cvt_bf16x2(v[i], 0.0f) & 0xffffu);
+        for (int it = 0; it < kBatch; ++it) {
+            const int64_t row = row0 + r0 + (first + it) * kStep;
+            if (row >= p.rows) break;
+            DST* out = reinterpret_cast<DST*>(p.out + row * p.ld_out) + col;
+#pragma unroll
+            for (int h = 0; h < kHalves; ++h) {       // 16 columns at a time
+                float v[16];
+                values_of<FMT>(code[it][h], block_scale<FMT>((N == 16 ? bytes[it] >> (8 * h) : bytes[it]) & 0xffu), inv_g, v);
+                if (col + 16 * h + 16 <= p.cols) {
+#pragma unroll
+                    for (int i = 0; i < 16; i += 32 / sizeof(DST)) {
+                        uint32_t w[8];
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) {
+                            if constexpr (sizeof(DST) == 4) w[k] = __float_as_uint(v[(i + k) % 16]);
+                            else w[k] = cvt_bf16x2(v[(i + 2 * k) % 16], v[(i + 2 * k + 1) % 16]);
+                        }
+                        if constexpr (ALIGN >= 32) {
+                            st_global_v8(out + 16 * h + i, w);
+                        } else {
+                            st_global_v4(out + 16 * h + i, w[0], w[1], w[2], w[3]);
+                            st_global_v4(out + 16 * h + i + 16 / sizeof(DST), w[4], w[5], w[6], w[7]);
+                        }
                     }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (col + 16 * h + i < p.cols) {
+                            if constexpr (sizeof(DST) == 4) out[16 * h + i] = v[i];
+                            else out[16 * h + i] = static_cast<uint16_t>(cvt_bf16x2(v[i], 0.0f) & 0xffffu);
+                        }
+                }
             }
         }
     }
 }
 
-// The same for output rows on any boundary: a warp takes 64 neighbouring columns of a row at a time, two a lane, so that what it
-// writes is in one piece.
-constexpr int kNarrowRows = 32;
-template <typename DST, int FMT>
-__global__ void __launch_bounds__(kThreads) dequantise_narrow_kernel(const DequantArgs p) {
-    constexpr int N = Fmt<FMT>::kBlock, kRowsPerWarp = kNarrowRows / 2;
-    const int64_t row_tile = blockIdx.x / p.col_tiles;
-    const int warp = threadIdx.x >> 5;
-    const int64_t row0 = row_tile * kNarrowRows + (warp >> 2) * kRowsPerWarp;
-    const int64_t col = (blockIdx.x - row_tile * p.col_tiles) * kColsBack + 64 * (warp & 3) + 2 * (threadIdx.x & 31);
+// The same for output rows on any boundary: 128 columns, 32 rows at a time, go through shared memory and leave in words of four
+// bytes, neighbouring lanes neighbouring words (8191 x 4099 NVFP4 to bf16: 118 us with two columns a lane and a scale for each, 24).
+// CHUNKS: times 32 rows to a block of threads.
+template <typename DST, int FMT, int CHUNKS>
+__global__ void __launch_bounds__(kThreads, 4) dequantise_narrow_kernel(const DequantArgs p) {
+    constexpr int N = Fmt<FMT>::kBlock, kBuffers = sizeof(DST) == 4 ? 1 : 2, kRowsPerWarp = kRowStep / (kThreads / 32);
+    __shared__ __align__(16) DST stage[kBuffers][kRowStep][kPitch<DST>];
+    const int64_t row_group = blockIdx.x / p.col_tiles;
+    const int64_t row0 = row_group * CHUNKS * kRowStep, col0 = (blockIdx.x - row_group * p.col_tiles) * kCols;
+    const int row_in_tile = static_cast<int>(row0 % kTileRows);
+    const int part = threadIdx.x % kParts, r0 = threadIdx.x / kParts, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     grid_dependency_wait();
     grid_launch_dependents();
-    if (col >= p.cols || row0 >= p.rows) return;
     const float inv_g = p.scale != nullptr ? __fdiv_rn(1.0f, *p.scale) : 1.0f;
-    const int64_t block = col / N;
-    uint32_t code[kRowsPerWarp], bytes[kRowsPerWarp];
+    // parts past the row's end take its last one, and rows past the matrix its last
+    const int64_t col = min(col0 + part * kPart, (p.cols - 1) & ~int64_t(kPart - 1)), block = col / N;
+    const uint8_t* scales = p.scales + (row0 / kTileRows * p.scale_tiles + block / 4) * kScaleTile;
+    uint2 code[CHUNKS];
+    uint32_t byte[CHUNKS];
 #pragma unroll
-    for (int i = 0; i < kRowsPerWarp; ++i) {
-        const int64_t row = min(row0 + i, p.rows - 1);
-        code[i] = __ldg(p.codes + row * p.ld_codes + col / 2);
-        bytes[i] = __ldg(p.scales + (row / kTileRows * p.scale_tiles + block / 4) * kScaleTile + scale_at(static_cast<int>(row % kTileRows), static_cast<int>(block & 3)));
+    for (int k = 0; k < CHUNKS; ++k) {
+        const int r = static_cast<int>(min(static_cast<int64_t>(r0 + k * kRowStep), p.rows - 1 - row0));
+        code[k] = __ldg(reinterpret_cast<const uint2*>(p.codes + (row0 + r) * p.ld_codes + col / 2));
+        byte[k] = __ldg(scales + scale_at(row_in_tile + r, static_cast<int>(block & 3)));
     }
+    const int cols = static_cast<int>(min(p.cols - col0, static_cast<int64_t>(kCols)));
 #pragma unroll
-    for (int i = 0; i < kRowsPerWarp; ++i) {
-        if (row0 + i >= p.rows) break;
-        const float s = block_scale<FMT>(bytes[i]);
-        float v[2];
-        e2m1x2_to_f32(code[i], v[0], v[1]);
-        DST* out = reinterpret_cast<DST*>(p.out + (row0 + i) * p.ld_out) + col;
+    for (int k = 0; k < CHUNKS; ++k) {
+        if (row0 + k * kRowStep >= p.rows) break;
+        float v[kPart];
+        values_of<FMT>(code[k], block_scale<FMT>(byte[k]), inv_g, v);
+        uint4* to = reinterpret_cast<uint4*>(&stage[k % kBuffers][r0][part * kPart]);
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            v[k] = __fmul_rn(v[k], s);
-            if constexpr (FMT == FP8MLP_NVFP4) v[k] = __fmul_rn(v[k], inv_g);
-            if (col + k < p.cols) {
-                if constexpr (sizeof(DST) == 4) out[k] = v[k];
-                else out[k] = static_cast<uint16_t>(cvt_bf16x2(v[k], 0.0f) & 0xffffu);
+        for (int i = 0; i < int(kPart * sizeof(DST) / 16); ++i) {
+            if constexpr (sizeof(DST) == 4) to[i] = make_uint4(__float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]), __float_as_uint(v[4 * i + 2]), __float_as_uint(v[4 * i + 3]));
+            else to[i] = make_uint4(cvt_bf16x2(v[(8 * i) % kPart], v[(8 * i + 1) % kPart]), cvt_bf16x2(v[(8 * i + 2) % kPart], v[(8 * i + 3) % kPart]),
+                                    cvt_bf16x2(v[(8 * i + 4) % kPart], v[(8 * i + 5) % kPart]), cvt_bf16x2(v[(8 * i + 6) % kPart], v[(8 * i + 7) % kPart]));
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kRowsPerWarp; ++i) {
+            const int r = warp * kRowsPerWarp + i;
+            if (row0 + k * kRowStep + r >= p.rows) break;
+            DST* out = reinterpret_cast<DST*>(p.out + (row0 + k * kRowStep + r) * p.ld_out) + col0;
+            const DST* from = stage[k % kBuffers][r];
+            if constexpr (sizeof(DST) == 4) {
+#pragma unroll
+                for (int q = 0; q < kCols; q += 32)
+                    if (q + lane < cols) out[q + lane] = from[q + lane];
+            } else {
+                const int odd = static_cast<int>(reinterpret_cast<uintptr_t>(out) >> 1) & 1;      // a row's first word may begin with its second column
+#pragma unroll
+                for (int q = 0; q < kCols; q += 64) {
+                    const int c = q + 2 * lane + odd;
+                    const uint32_t lo = from[min(c, kCols - 1)], hi = from[min(c + 1, kCols - 1)];
+                    if (c + 1 < cols) *reinterpret_cast<uint32_t*>(out + c) = lo | (hi << 16);
+                    else if (c < cols) out[c] = static_cast<DST>(lo);
+                }
+                if (odd && lane == 0) out[0] = from[0];
             }
         }
+        if (kBuffers == 1) __syncthreads();
     }
 }
 
@@ -806,8 +847,12 @@ extern "C" int fp8mlp_dequantize_fp4(const uint8_t* codes, int64_t ld_codes, con
     const int align = aligned(out, 32) && ld_out * (out_dtype == FP8MLP_F32 ? 4 : 2) % 32 == 0   ? 32
                       : aligned(out, 16) && ld_out * (out_dtype == FP8MLP_F32 ? 4 : 2) % 16 == 0 ? 16
                                                                                                  : 1;
-    const int tile_rows = align >= 16 ? kTileRows : kNarrowRows;
-    const int64_t tiles = (rows + tile_rows - 1) / tile_rows * ((cols + kColsBack - 1) / kColsBack);
+    const int width = align >= 16 ? kColsBack : kCols;
+    const int64_t col_tiles = (cols + width - 1) / width;
+    // rows on any boundary: few tiles are cut into four (1531 x 509, 48 tiles: 4.9 us, cut 2.5)
+    const bool cut = align == 1 && (rows + kTileRows - 1) / kTileRows * col_tiles <= 256;
+    const int tile_rows = cut ? kRowStep : kTileRows;
+    const int64_t tiles = (rows + tile_rows - 1) / tile_rows * col_tiles;
     if (tiles > INT32_MAX) return FP8MLP_ERR_SHAPE;
     if (rows > 0 && cols > 0 && (codes == nullptr || block_scales == nullptr || out == nullptr)) return FP8MLP_ERR_ARG;
     const int bytes = out_dtype == FP8MLP_F32 ? 4 : 2;
@@ -819,12 +864,13 @@ extern "C" int fp8mlp_dequantize_fp4(const uint8_t* codes, int64_t ld_codes, con
     a.ld_codes = ld_codes; a.ld_out = ld_out * bytes; a.rows = rows; a.cols = cols;
     const int per_tile = 4 * (fmt == FP8MLP_MXFP4 ? 32 : 16);
     a.scale_tiles = static_cast<int>((cols + per_tile - 1) / per_tile);
-    a.col_tiles = static_cast<int>((cols + kColsBack - 1) / kColsBack);
+    a.col_tiles = static_cast<int>(col_tiles);
     const dim3 grid(static_cast<unsigned>(tiles));
 #define FP8MLP_DEQUANT(D, F)                                                                                  \
     (align == 32 ? launch_chained(dequantise_kernel<D, F, 32>, grid, dim3(kThreads), 0, st, a)                \
      : align == 16 ? launch_chained(dequantise_kernel<D, F, 16>, grid, dim3(kThreads), 0, st, a)              \
-                   : launch_chained(dequantise_narrow_kernel<D, F>, grid, dim3(kThreads), 0, st, a))
+     : cut         ? launch_chained(dequantise_narrow_kernel<D, F, 1>, grid, dim3(kThreads), 0, st, a)        \
+                   : launch_chained(dequantise_narrow_kernel<D, F, kChunks>, grid, dim3(kThreads), 0, st, a))
     const bool f32 = out_dtype == FP8MLP_F32;
     const cudaError_t e = fmt == FP8MLP_MXFP4 ? (f32 ? FP8MLP_DEQUANT(float, FP8MLP_MXFP4) : FP8MLP_DEQUANT(uint16_t, FP8MLP_MXFP4))
                                               : (f32 ? FP8MLP_DEQUANT(float, FP8MLP_NVFP4) : FP8MLP_DEQUANT(uint16_t, FP8MLP_NVFP4));

@@ -77,6 +77,21 @@ def test_maximum_wherever_it_lies(rows, cols, pad, offset, dtype):
 
 
 @pytest.mark.parametrize("transpose", [False, True])
+@pytest.mark.parametrize("rows,cols", [(128, 2048), (128, 2056), (513, 512), (1, 65536), (65536, 1), (2048, 128), (400, 700), (300, 4096)])
+def test_scale_of_the_data_on_either_side_of_one_launch(rows, cols, transpose):
+    """Matrices around the size up to which one cluster does all; their largest element in the last row, column or both."""
+    for seed, at in enumerate(((rows - 1, cols - 1), (rows - 1, 0), (0, cols - 1))):
+        src = matrix(rows, cols, torch.bfloat16, seed=seed)
+        src[at] = -1000.0
+        op = B.new_fp4(B.NVFP4, cols if transpose else rows, rows if transpose else cols)
+        op.codes.fill_(0xAB)
+        op.scales.fill_(0xCD)
+        B.fp8mlp_quantize_fp4(src, op, transpose=transpose, scale_mode=B.SCALE_FROM_CURRENT_AMAX)
+        assert float(op.amax) == 1000.0 and float(op.scale) == R.tensor_scale(1000.0)
+        check_operand(op, src, float(op.scale), transpose)
+
+
+@pytest.mark.parametrize("transpose", [False, True])
 @pytest.mark.parametrize("fmt", FORMATS)
 def test_quantise_special_blocks(fmt, transpose):
     n = R.BLOCK[fmt]
@@ -147,6 +162,24 @@ def test_dequantise(fmt, dtype):
         want = (R.values(code, byte, fmt) * inv).float().to(dtype)          # one rounding to fp32, one to the type
         assert torch.equal(base[:, :cols].cpu(), want)
         assert (base[:, cols:] == 55.0).all()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("rows,cols,pad,offset", [(33, 129, 0, 0), (160, 300, 0, 1), (31, 127, 2, 1), (4100, 1153, 0, 0), (4097, 1153, 1, 3), (5000, 1032, 8, 8)])
+def test_dequantise_rows_on_any_boundary(fmt, dtype, rows, cols, pad, offset):
+    """Rows that begin on even and odd elements, few tiles and many, and what lies around them."""
+    gen = torch.Generator().manual_seed(cols)
+    code = torch.randint(0, 16, (rows, cols), generator=gen)
+    byte = torch.randint(100, 150, (rows, -(-cols // R.BLOCK[fmt])), generator=gen) if fmt == B.MXFP4 else \
+        torch.randint(0, 127, (rows, -(-cols // R.BLOCK[fmt])), generator=gen)
+    op = B.Fp4Operand(fmt, rows, cols, R.pack_codes(code).cuda(), R.tile_scales(byte).cuda())
+    base = torch.full((offset + rows * (cols + pad) + 64,), 55.0, dtype=dtype, device="cuda")
+    out = base[offset:offset + rows * (cols + pad)].view(rows, cols + pad)[:, :cols]
+    B.fp8mlp_dequantize_fp4(op, out)
+    assert torch.equal(out.cpu(), R.values(code, byte, fmt).float().to(dtype))
+    out.fill_(55.0)
+    assert (base == 55.0).all()
 
 
 # ---------------------------------------------------------------- products

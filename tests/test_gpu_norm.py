@@ -166,6 +166,13 @@ def test_backward(T, d, dtype):
         assert ((d_gain.double() - want_gain).abs() <= (min(T, 600) + 70) * U * gain_sizes).all()
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("T,d", [(16, 8192), (17, 4096), (32, 4096), (33, 4096), (16, 12304), (17, 12304), (40, 8208), (17, 16384), (513, 256)])
+def test_batches_on_either_side_of_one_cluster(T, d, dtype):
+    test_forward(T, d, dtype)
+    test_backward(T, d, dtype)
+
+
 def test_backward_in_place_without_gain_gradient_and_empty():
     dy, h, dh = (rows_of(64, 256, torch.bfloat16, seed=s)[0] for s in (1, 2, 3))
     rstd = torch.rand(64, device="cuda") + 0.5
