@@ -509,7 +509,7 @@ FP8MLP_API int fp8mlp_rmsnorm_backward(int64_t T, int64_t d, int dtype, const vo
  *   NVFP4: block scale Q_e4m3(a / 6), saturating; elements of a block whose scale rounds to 0 are 0
  *   element = v / block scale, rounded once to the nearest (ties to the even code), beyond 6 to 6
  * A block that holds a NaN or an infinity gets the scale NaN, so that all of it is NaN.
- * scale: g (NVFP4; null for MXFP4, whose scale_mode is FP8MLP_SCALE_GIVEN).  FP8MLP_SCALE_FROM_CURRENT_AMAX: g is written first:
+ * scale: g, not zero (NVFP4; null for MXFP4, whose scale_mode is FP8MLP_SCALE_GIVEN).  FP8MLP_SCALE_FROM_CURRENT_AMAX: g is written first:
  * the largest power of two with g * max |src| <= 448 * 6 (1 if that maximum is zero or not finite; within 2^-100 .. 2^100).
  * amax: receives max |src| (NaN left out); nullable with FP8MLP_SCALE_GIVEN.  Row r of the operand: codes + r * ld_codes, where
  * (columns + 1) / 2 bytes are used and those up to the next multiple of 16 cleared; codes and block_scales 16-byte aligned. */

@@ -102,7 +102,7 @@ __device__ __forceinline__ uint32_t quantise_block(const float (&v)[N], uint32_t
         }
         return finite ? byte : 0xffu;
     } else {
-        const float a = __fmul_rn(__uint_as_float(top), g);
+        const float a = __fmul_rn(__uint_as_float(top), fabsf(g));         // (a negative g is the elements' sign)
         const bool finite = __float_as_uint(a) < 0x7f800000u;
         // a / 6: a product with the reciprocal, corrected with its remainder.  E4M3's borders times 6 are fp32 numbers, and for any
         // other a the quotient is more than half a last place from them, so that what is left of its error turns no scale.

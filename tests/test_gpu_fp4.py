@@ -59,6 +59,19 @@ def test_quantise(fmt, dtype, transpose):
             check_operand(op, src, float(op.scale), transpose)
 
 
+def test_negative_scale_of_the_tensor():
+    """g < 0: the block scales stay positive (the tensor cores know no sign of theirs), the elements change theirs."""
+    src = matrix(40, 96, torch.float32, seed=3)
+    op, out = B.new_fp4(B.NVFP4, 40, 96, scale=torch.full((1,), -4.0, device="cuda")), torch.empty(40, 96, device="cuda")
+    ref, same = B.new_fp4(B.NVFP4, 40, 96, scale=torch.full((1,), 4.0, device="cuda")), torch.empty(40, 96, device="cuda")
+    B.fp8mlp_quantize_fp4(src, op)
+    B.fp8mlp_quantize_fp4(src, ref)
+    assert torch.equal(op.scales, ref.scales)
+    B.fp8mlp_dequantize_fp4(op, out)
+    B.fp8mlp_dequantize_fp4(ref, same)
+    assert torch.equal(out, same)
+
+
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("rows,cols,pad,offset", [(1, 1, 0, 0), (1, 7, 0, 3), (300, 517, 0, 0), (300, 517, 0, 1), (97, 515, 5, 3), (4, 100000, 0, 0),
                                                   (2000, 9, 1, 0), (700, 1024, 8, 8)])
