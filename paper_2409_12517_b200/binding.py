@@ -543,6 +543,15 @@ def _rows_like(t, shape, dtype, what, here):
     return ptr, ld
 
 
+def _floats(t, numel, what, here):
+    """Device pointer of a contiguous fp32 tensor of that size on the current GPU, or None."""
+    if t is None:
+        return None
+    if t.dtype is not _F32 or t.numel() != numel or t.get_device() != here or not t.is_contiguous():
+        _as(t, _F32, numel, what, here)
+    return t.data_ptr()
+
+
 def fp8mlp_rmsnorm(x, residual, gain, eps: float, y, h=None, out: int = RMS_SAME, scale=None, amax=None, rstd=None) -> None:
     """h = x + residual, y = h / rms(h) * gain.  x, residual, h: [T, d] bf16 or fp32, any row stride; residual, gain (fp32
     [d]), h, amax (1-element fp32) and rstd (fp32 [T]) may be None; h may be x or residual.  y by `out`: RMS_SAME: [T, d] of
@@ -553,20 +562,34 @@ def fp8mlp_rmsnorm(x, residual, gain, eps: float, y, h=None, out: int = RMS_SAME
     if len(shape) != 2 or dtype not in _DTYPES:
         raise ValueError(f"x: a 2-D bfloat16 or float32 tensor is needed, got {tuple(shape)} {dtype}")
     T, d = shape
-    x_ptr, ld_x = _rows_like(x, shape, dtype, "x", here)
-    r_ptr, ld_r = _rows_like(residual, shape, dtype, "residual", here)
-    h_ptr, ld_h = _rows_like(h, shape, dtype, "h", here)
+    # (the usual case is tested in place: eight tensors, and a call into a helper for each would be a tenth of a small norm's time)
+    if x.is_contiguous() and x.get_device() == here:
+        x_ptr, ld_x = x.data_ptr(), d
+    else:
+        x_ptr, ld_x = _rows_like(x, shape, dtype, "x", here)
+    if residual is None:
+        r_ptr, ld_r = None, 0
+    elif residual.dtype is dtype and residual.shape == shape and residual.is_contiguous() and residual.get_device() == here:
+        r_ptr, ld_r = residual.data_ptr(), d
+    else:
+        r_ptr, ld_r = _rows_like(residual, shape, dtype, "residual", here)
+    if h is None:
+        h_ptr, ld_h = None, 0
+    elif h.dtype is dtype and h.shape == shape and h.is_contiguous() and h.get_device() == here:
+        h_ptr, ld_h = h.data_ptr(), d
+    else:
+        h_ptr, ld_h = _rows_like(h, shape, dtype, "h", here)
     if out == RMS_SAME:
         y_ptr, ld_y = _rows_like(y, shape, dtype, "y", here)
     elif isinstance(y, int):
         y_ptr, ld_y = y, d
+    elif y.dtype is _U8 and y.shape == shape and y.is_contiguous() and y.get_device() == here:
+        y_ptr, ld_y = y.data_ptr(), d
     else:
         y_ptr, ld_y = _bytes(y, T, d, "y", here)
-    _check(lib().fp8mlp_rmsnorm(T, d, _DTYPES[dtype], x_ptr, ld_x, r_ptr, ld_r, h_ptr, ld_h,
-                                None if gain is None else _as(gain, _F32, d, "gain", here), eps, out, y_ptr, ld_y,
-                                None if scale is None else _as(scale, _F32, T if out == RMS_E4M3_ROWS else 1, "scale", here),
-                                None if amax is None else _as(amax, _F32, 1, "amax", here),
-                                None if rstd is None else _as(rstd, _F32, T, "rstd", here), _stream(here)), "fp8mlp_rmsnorm")
+    _check(lib().fp8mlp_rmsnorm(T, d, _DTYPES[dtype], x_ptr, ld_x, r_ptr, ld_r, h_ptr, ld_h, _floats(gain, d, "gain", here), eps, out,
+                                y_ptr, ld_y, _floats(scale, T if out == RMS_E4M3_ROWS else 1, "scale", here),
+                                _floats(amax, 1, "amax", here), _floats(rstd, T, "rstd", here), _stream(here)), "fp8mlp_rmsnorm")
 
 
 def fp8mlp_rmsnorm_backward(dy, h, gain, rstd, dh, dx, d_gain, workspace) -> None:
@@ -577,15 +600,27 @@ def fp8mlp_rmsnorm_backward(dy, h, gain, rstd, dh, dx, d_gain, workspace) -> Non
     if len(shape) != 2 or dtype not in _DTYPES:
         raise ValueError(f"h: a 2-D bfloat16 or float32 tensor is needed, got {tuple(shape)} {dtype}")
     T, d = shape
-    h_ptr, ld_h = _rows_like(h, shape, dtype, "h", here)
-    dy_ptr, ld_dy = _rows_like(dy, shape, dtype, "dy", here)
-    dh_ptr, ld_dh = _rows_like(dh, shape, dtype, "dh", here)
-    dx_ptr, ld_dx = _rows_like(dx, shape, dtype, "dx", here)
-    _check(lib().fp8mlp_rmsnorm_backward(T, d, _DTYPES[dtype], dy_ptr, ld_dy, h_ptr, ld_h,
-                                         None if gain is None else _as(gain, _F32, d, "gain", here),
+    if h.is_contiguous() and h.get_device() == here:
+        h_ptr, ld_h = h.data_ptr(), d
+    else:
+        h_ptr, ld_h = _rows_like(h, shape, dtype, "h", here)
+    if dy.dtype is dtype and dy.shape == shape and dy.is_contiguous() and dy.get_device() == here:
+        dy_ptr, ld_dy = dy.data_ptr(), d
+    else:
+        dy_ptr, ld_dy = _rows_like(dy, shape, dtype, "dy", here)
+    if dh is None:
+        dh_ptr, ld_dh = None, 0
+    elif dh.dtype is dtype and dh.shape == shape and dh.is_contiguous() and dh.get_device() == here:
+        dh_ptr, ld_dh = dh.data_ptr(), d
+    else:
+        dh_ptr, ld_dh = _rows_like(dh, shape, dtype, "dh", here)
+    if dx.dtype is dtype and dx.shape == shape and dx.is_contiguous() and dx.get_device() == here:
+        dx_ptr, ld_dx = dx.data_ptr(), d
+    else:
+        dx_ptr, ld_dx = _rows_like(dx, shape, dtype, "dx", here)
+    _check(lib().fp8mlp_rmsnorm_backward(T, d, _DTYPES[dtype], dy_ptr, ld_dy, h_ptr, ld_h, _floats(gain, d, "gain", here),
                                          _as(rstd, _F32, T, "rstd", here), dh_ptr, ld_dh, dx_ptr, ld_dx,
-                                         None if d_gain is None else _as(d_gain, _F32, d, "d_gain", here),
-                                         None if workspace is None else _as(workspace, _F32, RMS_PARTIALS * d, "workspace", here),
+                                         _floats(d_gain, d, "d_gain", here), _floats(workspace, RMS_PARTIALS * d, "workspace", here),
                                          _stream(here)), "fp8mlp_rmsnorm_backward")
 
 
