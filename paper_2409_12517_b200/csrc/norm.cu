@@ -6,12 +6,14 @@
 // loads are on their way while the present row is summed and written.
 #include "common.cuh"
 
+#include <type_traits>
+
 namespace fp8mlp {
 
 namespace {
 
 constexpr uint32_t kAll = 0xffffffffu;
-constexpr int kMaxWarps = 16;
+constexpr int kMaxWarps = 32;
 constexpr int kCluster = 16;                // blocks of the one cluster that takes a short batch as a whole
 
 struct NormArgs {
@@ -22,6 +24,7 @@ struct NormArgs {
     unsigned int* amax;
     int64_t T, ld_x, ld_res, ld_h, ld_y;      // row strides in bytes
     float eps, inv_d;
+    double inv_d64;
     int units, tpr;                           // 32-byte units of a row; threads that share it
     int cluster;                              // the grid is one cluster: it finds the maximum by itself
 };
@@ -103,35 +106,74 @@ __device__ __forceinline__ void load_gain(const float* gain, int first, float (&
     }
 }
 
-// Sum of one value, and with MAX the maximum of another (>= 0), over the tpr threads of a row; every one of them gets both.
-// `part`: two words per warp; the caller alternates between two such arrays, so that one barrier per call is enough.
-template <bool MAX>
-__device__ __forceinline__ void over_row(float& sum, float& top, int tpr, float* part) {
+// Sum of one value (fp32, or 64 bits for norms whose output is codes) over the tpr threads of a row, and with MAX the maximum of another,
+// held as an fp32 number >= 0 and what its rounding left off; every thread of the row gets them.  `part`: words for each warp; the
+// caller alternates between two such arrays, so that one barrier per call is enough.
+template <typename STAT> struct Part {
+    STAT sum[kMaxWarps];
+    float2 top[kMaxWarps];
+};
+// the maximum over a warp
+__device__ __forceinline__ void warp_top(float& top, float& rest) {
+    const float most = warp_max_nonneg(top);
+    uint32_t key = __float_as_uint(rest);                 // in the order of whole numbers
+    key = top == most ? (key ^ (static_cast<uint32_t>(static_cast<int32_t>(key) >> 31) | 0x80000000u)) : 0u;
+    key = __reduce_max_sync(kAll, key);
+    rest = __uint_as_float(key ^ (key & 0x80000000u ? 0x80000000u : 0xffffffffu));
+    top = most;
+}
+template <bool MAX, typename STAT>
+__device__ __forceinline__ void over_row(STAT& sum, float& top, float& rest, int tpr, Part<STAT>& part) {
     for (int o = min(tpr, 32) >> 1; o > 0; o >>= 1) {
-        sum = __fadd_rn(sum, __shfl_xor_sync(kAll, sum, o));
-        if (MAX) top = fmaxf(top, __shfl_xor_sync(kAll, top, o));
+        sum += __shfl_xor_sync(kAll, sum, o);
+        if (MAX && tpr < 32) {
+            const float other = __shfl_xor_sync(kAll, top, o), other_rest = __shfl_xor_sync(kAll, rest, o);
+            rest = other > top || (other == top && other_rest > rest) ? other_rest : rest;
+            top = fmaxf(top, other);
+        }
     }
+    if (MAX && tpr >= 32) warp_top(top, rest);
     if (tpr <= 32) return;
     const int warp = threadIdx.x >> 5, per_row = tpr >> 5, first = warp & ~(per_row - 1);
     if ((threadIdx.x & 31) == 0) {
-        part[warp] = sum;
-        if (MAX) part[kMaxWarps + warp] = top;
+        part.sum[warp] = sum;
+        if (MAX) part.top[warp] = make_float2(top, rest);
     }
     __syncthreads();
-    sum = part[first];
-    for (int i = 1; i < per_row; ++i) sum = __fadd_rn(sum, part[first + i]);
+    // every warp adds up those of its row, a lane for each
+    const int mine = first + (threadIdx.x & (per_row - 1));
+    sum = part.sum[mine];
+    for (int o = per_row >> 1; o > 0; o >>= 1) sum += __shfl_xor_sync(kAll, sum, o);
     if (MAX) {
-        top = part[kMaxWarps + first];
-        for (int i = 1; i < per_row; ++i) top = fmaxf(top, part[kMaxWarps + first + i]);
+        top = part.top[mine].x;
+        rest = part.top[mine].y;
+        warp_top(top, rest);
     }
 }
 
+// The E4M3 code of h * gain * factor (64 bits), rounded once: to fp32 with a last bit that says whether something was cut off, from
+// where the conversion rounds to the code.
+__device__ __forceinline__ float for_code(float h, float gain, double factor) {
+    const double v = static_cast<double>(h) * static_cast<double>(gain) * factor;
+    const float cut = __double2float_rz(v);
+    return static_cast<double>(cut) != v ? __uint_as_float(__float_as_uint(cut) | 1u) : cut;
+}
+
 // ---------------------------------------------------------------- forward
-// NU: units per thread.  With one (d <= 8192 bf16, 4096 fp32) the next row is fetched ahead and the gain stays in registers.
+// NU: units per thread.  With one (d <= 16384 bf16, 8192 fp32) the next row is fetched ahead and the gain stays in registers.
+// Codes (OUT != FP8MLP_RMS_SAME) are those next to the exact value: an fp32 product may land on the other side of a border between two
+// codes (one in 10^6 does, each a step of 6 percent).  A row's statistics are taken in 64 bits (bf16: from fp32 sums of four squares, which have 16 bits each); a unit's codes
+// are converted from its fp32 values a little increased and a little decreased, and where the two differ its products are taken again
+// in 64 bits (one unit in 5000).
+// Measured, 16384 x 4096 with residual: bf16 to codes 79 us (codes from fp32 products 77), 72 at the copy rate; to bf16 90 (82); codes
+// with a scale per row 89; fp32 to codes 135 (133).  2048 x 16384 bf16 to codes 44 (36).  DRAM and the row's chain of reductions.
 template <typename SRC, int BLOCK, int NU, bool WIDE, int OUT>
-__global__ void __launch_bounds__(BLOCK) norm_kernel(const NormArgs p) {
+__global__ void __launch_bounds__(BLOCK, 1024 / BLOCK) norm_kernel(const NormArgs p) {
     constexpr int E = Unit<SRC>::kElems;
-    __shared__ float part[2][2 * kMaxWarps];
+    constexpr bool kCodes = OUT != FP8MLP_RMS_SAME, kRows = OUT == FP8MLP_RMS_E4M3_ROWS;
+    using Stat = typename std::conditional<kCodes, double, float>::type;
+    __shared__ Part<Stat> part[2];
+    __shared__ float warp_max[kMaxWarps];
     __shared__ float block_max[kCluster];
     if (p.cluster) cluster_begin();
     const int sub = threadIdx.x / p.tpr, u0 = threadIdx.x % p.tpr, rows = BLOCK / p.tpr;
@@ -160,7 +202,8 @@ __global__ void __launch_bounds__(BLOCK) norm_kernel(const NormArgs p) {
     for (int64_t first = static_cast<int64_t>(blockIdx.x) * rows; first < p.T; first += step, row += step, parity ^= 1) {
         const bool here = row < p.T;
         uint32_t h[NU][8];
-        float sum = 0.0f, top = 0.0f;                       // of h^2, and max |h gain|
+        Stat sum = 0;                                       // of h^2
+        float top = 0.0f, top_rest = 0.0f;                  // max |h gain|, and what its rounding left off (a scale for the row)
 #pragma unroll
         for (int k = 0; k < NU; ++k) {
             const int u = u0 + k * p.tpr;
@@ -172,31 +215,51 @@ __global__ void __launch_bounds__(BLOCK) norm_kernel(const NormArgs p) {
                 if (p.h != nullptr) store_unit<WIDE>(p.h + row * p.ld_h + 32 * u, h[k]);
             }
             if (NU > 1) load_gain<E>(p.gain, u * E, gain);
-            float s[2] = {0.0f, 0.0f};
+            float s[E / 4];
 #pragma unroll
             for (int i = 0; i < E; ++i) {
-                const float v = elem<SRC>(h[k], i);
-                s[i & 1] = __fmaf_rn(v, v, s[i & 1]);
-                top = fmaxf(top, fabsf(__fmul_rn(v, gain[i])));
+                const float v = elem<SRC>(h[k], i), g = __fmul_rn(fabsf(v), fabsf(gain[i]));
+                if constexpr (kCodes && sizeof(SRC) == 4) sum += static_cast<Stat>(v) * static_cast<Stat>(v);
+                else s[i / 4] = i % 4 == 0 ? __fmul_rn(v, v) : __fmaf_rn(v, v, s[i / 4]);
+                if constexpr (kRows) {
+                    const float rest = __fmaf_rn(fabsf(v), fabsf(gain[i]), -g);
+                    top_rest = g > top ? rest : top_rest;
+                }
+                top = fmaxf(top, g);
             }
-            sum = __fadd_rn(sum, __fadd_rn(s[0], s[1]));
+            if constexpr (!kCodes || sizeof(SRC) == 2)
+#pragma unroll
+                for (int i = 0; i < E / 4; i += 2) sum += static_cast<Stat>(s[i]) + static_cast<Stat>(s[i + 1]);
         }
         if (NU == 1) fetch(row + step);
-        over_row<OUT == FP8MLP_RMS_E4M3_ROWS>(sum, top, p.tpr, part[parity]);
-        const float rstd = __fdiv_rn(1.0f, __fsqrt_rn(__fmaf_rn(sum, p.inv_d, p.eps)));
+        over_row<kRows>(sum, top, top_rest, p.tpr, part[parity]);
+        Stat exact = 0;                                     // 1 / rms
+        float rstd;
+        if constexpr (kCodes) {
+            const double mean = sum * p.inv_d64 + static_cast<double>(p.eps);
+            rstd = __fdiv_rn(1.0f, __fsqrt_rn(static_cast<float>(mean)));
+            exact = rstd;
+            if (rstd > 0.0f && !isinf(rstd)) exact = exact * (1.5 - 0.5 * mean * exact * exact);       // one step of Newton's method
+            rstd = static_cast<float>(exact);
+        } else {
+            rstd = __fdiv_rn(1.0f, __fsqrt_rn(__fmaf_rn(sum, p.inv_d, p.eps)));
+        }
         if (here && u0 == 0 && p.rstd != nullptr) p.rstd[row] = rstd;
         // y = (h gain) factor; codes with a scale of the row's own do not depend on rstd, as it cancels
-        float factor = rstd;
-        if (OUT == FP8MLP_RMS_E4M3) factor = __fmul_rn(rstd, scale);
-        if (OUT == FP8MLP_RMS_E4M3_ROWS) {
+        if (OUT == FP8MLP_RMS_E4M3) exact *= scale;
+        if constexpr (kRows) {
             const float most = __fmul_rn(top, rstd), row_scale = __fdiv_rn(448.0f, most);
             const float to_codes = __fdiv_rn(448.0f, top);
             const bool sound = most > 0.0f && !isinf(most) && !isinf(row_scale) && !isinf(to_codes);
-            if (sound) factor = to_codes;
+            if (sound) {
+                exact = to_codes;
+                exact += exact * (1.0 / 448.0) * (448.0 - exact * (static_cast<double>(top) + static_cast<double>(top_rest)));
+            }
             if (here && u0 == 0) p.scale[row] = sound ? row_scale : 1.0f;
         } else {
             run_max = fmaxf(run_max, __fmul_rn(top, rstd));
         }
+        const float factor = kCodes ? static_cast<float>(exact) : rstd;
 #pragma unroll
         for (int k = 0; k < NU; ++k) {
             const int u = u0 + k * p.tpr;
@@ -211,9 +274,26 @@ __global__ void __launch_bounds__(BLOCK) norm_kernel(const NormArgs p) {
                 store_unit<WIDE>(p.y + row * p.ld_y + 32 * u, w);
             } else {
                 uint8_t* dst = p.y + row * p.ld_y + E * u;
-                uint32_t c[E / 4];
+                // three roundings of 2^-24: the exact values lie between these
+                const f32x2 more = pack2(1.0f + 0x1p-21f, 1.0f + 0x1p-21f), less = pack2(1.0f - 0x1p-21f, 1.0f - 0x1p-21f);
+                uint32_t c[E / 4], differ = 0;
 #pragma unroll
-                for (int i = 0; i < E / 4; ++i) c[i] = cvt_fp8x4<FP8MLP_E4M3>(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+                for (int i = 0; i < E / 4; ++i) {
+                    const f32x2 a = pack2(v[4 * i], v[4 * i + 1]), b = pack2(v[4 * i + 2], v[4 * i + 3]);
+                    float hi[4], lo[4];
+                    unpack2(mul2(a, more), hi[0], hi[1]);
+                    unpack2(mul2(b, more), hi[2], hi[3]);
+                    unpack2(mul2(a, less), lo[0], lo[1]);
+                    unpack2(mul2(b, less), lo[2], lo[3]);
+                    c[i] = cvt_fp8x4<FP8MLP_E4M3>(hi[0], hi[1], hi[2], hi[3]);
+                    differ |= c[i] ^ cvt_fp8x4<FP8MLP_E4M3>(lo[0], lo[1], lo[2], lo[3]);
+                }
+                if (differ != 0) {
+#pragma unroll
+                    for (int i = 0; i < E / 4; ++i)
+                        c[i] = cvt_fp8x4<FP8MLP_E4M3>(for_code(elem<SRC>(h[k], 4 * i), gain[4 * i], exact), for_code(elem<SRC>(h[k], 4 * i + 1), gain[4 * i + 1], exact),
+                                                      for_code(elem<SRC>(h[k], 4 * i + 2), gain[4 * i + 2], exact), for_code(elem<SRC>(h[k], 4 * i + 3), gain[4 * i + 3], exact));
+                }
                 if constexpr (E == 16) st_global_v4(dst, c[0], c[1], c[2], c[3]); else st_global_v2(dst, c[0], c[1]);
             }
         }
@@ -222,10 +302,10 @@ __global__ void __launch_bounds__(BLOCK) norm_kernel(const NormArgs p) {
     if (OUT != FP8MLP_RMS_E4M3_ROWS && p.amax != nullptr) {
         __syncthreads();
         run_max = warp_max_nonneg(run_max);
-        if ((threadIdx.x & 31) == 0) part[0][threadIdx.x >> 5] = run_max;
+        if ((threadIdx.x & 31) == 0) warp_max[threadIdx.x >> 5] = run_max;
         __syncthreads();
         if (threadIdx.x < 32) {
-            run_max = warp_max_nonneg(threadIdx.x < BLOCK / 32 ? part[0][threadIdx.x] : 0.0f);
+            run_max = warp_max_nonneg(threadIdx.x < BLOCK / 32 ? warp_max[threadIdx.x] : 0.0f);
             // a single block or cluster has the whole maximum (nobody cleared the word for it then)
             if (threadIdx.x == 0 && gridDim.x == 1) *p.amax = __float_as_uint(run_max);
             else if (threadIdx.x == 0 && !p.cluster && run_max > 0.0f) atomicMax(p.amax, __float_as_uint(run_max));
@@ -249,7 +329,7 @@ __global__ void __launch_bounds__(BLOCK) norm_kernel(const NormArgs p) {
 template <typename SRC, int BLOCK, int NU, bool WIDE>
 __global__ void __launch_bounds__(BLOCK) norm_backward_kernel(const NormBackArgs p) {
     constexpr int E = Unit<SRC>::kElems;
-    __shared__ float part_sum[2][kMaxWarps];
+    __shared__ Part<float> part_sum[2];
     extern __shared__ float d_gain_row[];                        // [d]: NU > 1, or where several rows share a block
     const int sub = threadIdx.x / p.tpr, u0 = threadIdx.x % p.tpr, rows = BLOCK / p.tpr;
     const int64_t step = static_cast<int64_t>(gridDim.x) * rows;
@@ -304,7 +384,7 @@ __global__ void __launch_bounds__(BLOCK) norm_backward_kernel(const NormBackArgs
         }
         if (NU == 1) fetch(row + step);
         float unused = 0.0f;
-        over_row<false>(sum, unused, p.tpr, part_sum[parity]);
+        over_row<false>(sum, unused, unused, p.tpr, part_sum[parity]);
         const float mean = __fmul_rn(sum, p.inv_d);
 #pragma unroll
         for (int k = 0; k < NU; ++k) {
@@ -413,11 +493,11 @@ int sm_count_of_current(int* sms) {
 }
 
 struct RowShape { int units, tpr, block, nu; };
-// threads and units per row
-RowShape row_shape(int64_t d, int elems) {
+// threads and units per row, at most `most` threads (forward 1024, backward 512: its registers)
+RowShape row_shape(int64_t d, int elems, int most) {
     RowShape s;
     s.units = static_cast<int>(d / elems);
-    s.block = s.units <= 256 ? 256 : 512;
+    s.block = s.units <= 256 ? 256 : s.units <= 512 || most == 512 ? 512 : 1024;
     s.tpr = 1;
     while (s.tpr < s.units && s.tpr < s.block) s.tpr <<= 1;
     const int need = (s.units + s.tpr - 1) / s.tpr;
@@ -477,12 +557,15 @@ cudaError_t launch_norm_backward(const NormBackArgs& a, size_t smem, dim3 grid, 
 }
 
 // the instantiation for a shape: F<SRC, BLOCK, NU, WIDE>
-#define FP8MLP_NORM_PICK(F, SRC, WIDE, ...)                                                    \
-    (s.block == 256 ? F<SRC, 256, 1, WIDE>(__VA_ARGS__) : s.nu == 1 ? F<SRC, 512, 1, WIDE>(__VA_ARGS__) \
+#define FP8MLP_NORM_TYPES(PICK, F, ...)                                                                                   \
+    (dtype == FP8MLP_F32 ? (wide ? PICK(F, float, true, __VA_ARGS__) : PICK(F, float, false, __VA_ARGS__))                 \
+                         : (wide ? PICK(F, uint16_t, true, __VA_ARGS__) : PICK(F, uint16_t, false, __VA_ARGS__)))
+#define FP8MLP_NORM_FORWARD(F, SRC, WIDE, ...)                                                                            \
+    (s.block == 256 ? F<SRC, 256, 1, WIDE>(__VA_ARGS__) : s.block == 512 ? F<SRC, 512, 1, WIDE>(__VA_ARGS__)               \
+     : s.nu == 1 ? F<SRC, 1024, 1, WIDE>(__VA_ARGS__) : F<SRC, 1024, 2, WIDE>(__VA_ARGS__))
+#define FP8MLP_NORM_BACKWARD(F, SRC, WIDE, ...)                                                                           \
+    (s.block == 256 ? F<SRC, 256, 1, WIDE>(__VA_ARGS__) : s.nu == 1 ? F<SRC, 512, 1, WIDE>(__VA_ARGS__)                    \
      : s.nu == 2 ? F<SRC, 512, 2, WIDE>(__VA_ARGS__) : F<SRC, 512, 4, WIDE>(__VA_ARGS__))
-#define FP8MLP_NORM_LAUNCH(F, ...)                                                                                        \
-    (dtype == FP8MLP_F32 ? (wide ? FP8MLP_NORM_PICK(F, float, true, __VA_ARGS__) : FP8MLP_NORM_PICK(F, float, false, __VA_ARGS__)) \
-                         : (wide ? FP8MLP_NORM_PICK(F, uint16_t, true, __VA_ARGS__) : FP8MLP_NORM_PICK(F, uint16_t, false, __VA_ARGS__)))
 
 }  // namespace
 }  // namespace fp8mlp
@@ -512,13 +595,13 @@ extern "C" int fp8mlp_rmsnorm(int64_t T, int64_t d, int dtype, const void* x, in
     if (T == 0) return amax != nullptr ? clear_float(amax, st) : FP8MLP_OK;
     int sms = 0;
     if (int rc = sm_count_of_current(&sms)) return rc;
-    const RowShape s = row_shape(d, 32 / bytes);
+    const RowShape s = row_shape(d, 32 / bytes, 1024);
     NormArgs a{};
     a.x = static_cast<const uint8_t*>(x); a.residual = static_cast<const uint8_t*>(residual);
     a.h = static_cast<uint8_t*>(h_out); a.y = static_cast<uint8_t*>(y);
     a.gain = gain; a.scale = scale; a.rstd = rstd; a.amax = reinterpret_cast<unsigned int*>(amax);
     a.T = T; a.ld_x = ld_x * bytes; a.ld_res = ld_residual * bytes; a.ld_h = ld_h * bytes; a.ld_y = ld_y * out_bytes;
-    a.eps = eps; a.inv_d = 1.0f / static_cast<float>(d); a.units = s.units; a.tpr = s.tpr;
+    a.eps = eps; a.inv_d = 1.0f / static_cast<float>(d); a.inv_d64 = 1.0 / static_cast<double>(d); a.units = s.units; a.tpr = s.tpr;
     auto on32 = [&](const void* q, int64_t ld) { return aligned(q, 32) && (T <= 1 || ld % 32 == 0); };
     const bool wide = on32(x, a.ld_x) && (residual == nullptr || on32(residual, a.ld_res)) && (h_out == nullptr || on32(h_out, a.ld_h)) &&
                       (out_kind != FP8MLP_RMS_SAME || on32(y, a.ld_y));
@@ -527,7 +610,7 @@ extern "C" int fp8mlp_rmsnorm(int64_t T, int64_t d, int dtype, const void* x, in
     const dim3 grid(static_cast<unsigned>(a.cluster ? kCluster : blocks < most ? blocks : most));
     if (amax != nullptr && grid.x > 1 && !a.cluster)
         if (int rc = clear_float(amax, st)) return rc;
-    FP8MLP_CUDA_CHECK(FP8MLP_NORM_LAUNCH(launch_norm, a, out_kind, grid, st));
+    FP8MLP_CUDA_CHECK(FP8MLP_NORM_TYPES(FP8MLP_NORM_FORWARD, launch_norm, a, out_kind, grid, st));
     count_launch();
     return FP8MLP_OK;
 }
@@ -553,7 +636,7 @@ extern "C" int fp8mlp_rmsnorm_backward(int64_t T, int64_t d, int dtype, const vo
     }
     int sms = 0;
     if (int rc = sm_count_of_current(&sms)) return rc;
-    const RowShape s = row_shape(d, 32 / bytes);
+    const RowShape s = row_shape(d, 32 / bytes, 512);
     NormBackArgs a{};
     a.dy = static_cast<const uint8_t*>(dy); a.h = static_cast<const uint8_t*>(h); a.dh = static_cast<const uint8_t*>(dh);
     a.dx = static_cast<uint8_t*>(dx);
@@ -569,7 +652,7 @@ extern "C" int fp8mlp_rmsnorm_backward(int64_t T, int64_t d, int dtype, const vo
     if (one_cluster) { a.d_gain = d_gain; a.partial = nullptr; }
     const dim3 grid(static_cast<unsigned>(one_cluster ? kCluster : blocks < most ? blocks : most));
     const size_t smem = d_gain != nullptr && (s.nu > 1 || rows > 1 || one_cluster) ? sizeof(float) * d : 0;
-    FP8MLP_CUDA_CHECK(FP8MLP_NORM_LAUNCH(launch_norm_backward, a, smem, grid, st));
+    FP8MLP_CUDA_CHECK(FP8MLP_NORM_TYPES(FP8MLP_NORM_BACKWARD, launch_norm_backward, a, smem, grid, st));
     count_launch();
     if (d_gain != nullptr && !one_cluster) {
         FP8MLP_CUDA_CHECK(launch_chained(norm_gain_kernel, dim3(static_cast<unsigned>((d + 127) / 128)), dim3(32 * kGainWarps), 0, st,

@@ -117,6 +117,27 @@ def test_forward_rows_without_a_norm():
     assert torch.isnan(y[0]).all()                                       # 0 / 0
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("T,d,gained", [(2000, 512, True), (700, 4096, True), (700, 4096, False), (64, 16384, True), (3000, 48, True)])
+def test_codes_are_those_next_to_the_exact_values(T, d, gained, dtype):
+    """Not one code off, but for values within 2^-23 of a border: 1 / rms has 3 roundings of 2^-24 from sums of four squares, halved
+    by the root, and the root's and the division's remainders, which a step of Newton's method takes away.  Values on a border are
+    among them (bf16 rows without a gain: products with 448 / maximum that end in a five)."""
+    x = rows_of(T, d, dtype, scale=2.0, seed=d)[0]
+    gain = 1 + 0.2 * torch.randn(d, device="cuda") if gained else None
+    y = torch.empty(T, d, dtype=torch.uint8, device="cuda")
+    given, own = torch.full((1,), 96.5, device="cuda"), torch.empty(T, device="cuda")
+    want, _ = R.norm(x.cpu(), None if gain is None else gain.cpu(), EPS)
+    for out, scale in ((B.RMS_E4M3, given), (B.RMS_E4M3_ROWS, own)):
+        B.fp8mlp_rmsnorm(x, None, gain, EPS, y, out=out, scale=scale)
+        exact = (want * 96.5 if out == B.RMS_E4M3 else want * (448.0 / want.abs().amax(-1, keepdim=True))).abs()
+        slack = 2.0 ** -23 if out == B.RMS_E4M3 else 2.0 ** -40          # (1 / rms is not in the codes of a row of its own scale)
+        low, high = (R.nearest(R.E4M3_CODES[:127], exact * (1 + s * slack)) for s in (-1, 1))
+        got = (y & 0x7f).cpu().long()
+        assert ((got >= low) & (got <= high)).all()
+        assert torch.equal((y >= 0x80).cpu() | (got == 0), (want < 0) | (got == 0))
+
+
 def test_rows_too_small_for_a_scale_of_their_own():
     """448 / maximum beyond fp32, with the maximum of y, or of h gain alone: scale 1, codes of y as it is, no NaN."""
     x = torch.randn(5, 64, device="cuda")
