@@ -468,7 +468,7 @@ FP8MLP_API int fp8mlp_gemm_bf16(int64_t M, int64_t N, int64_t K, const void* A, 
  *   FP8MLP_RMS_E4M3       y: E4M3 codes Q(y * *scale), `scale` one device float that is read (delayed scaling)
  *   FP8MLP_RMS_E4M3_ROWS  y: E4M3 codes Q(y * scale[t]), scale fp32 [T] written: 448 / max_i |y[t, i]| (1 where that maximum is
  *                         zero or not finite, or where 448 / max_i |h[t, i] gain[i]| leaves fp32)
- * Codes are rounded once: they are those next to the exact value of the formula (its 1 / rms within 2^-23), not to an fp32 product.
+ * Codes are rounded once: they are those next to the exact value of the formula (its 1 / rms within six roundings of fp32).
  * scale is not used by FP8MLP_RMS_SAME.  amax (nullable, not with FP8MLP_RMS_E4M3_ROWS): receives max |y| of this call (before
  * any cast).  rstd (nullable): fp32 [T], for the backward pass.  With y = a context's FP8MLP_WS_XQ buffer (ld_y = d), scales.x
  * and amax.x the codes are the block's own operand: fp8mlp_forward with FP8MLP_SCALE_GIVEN_X_CAST does not read x again.

@@ -41,11 +41,6 @@ struct AmaxArgs {
 // place of a block's scale in its tile
 __device__ __forceinline__ int scale_at(int row, int block) { return (row & 31) * 16 + (row >> 5) * 4 + block; }
 
-__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
-    f32x2 r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-    return r;
-}
 // eight floats -> eight E2M1 codes, first in the low half of the low byte; nearest, ties to even, saturating
 __device__ __forceinline__ uint32_t cvt_e2m1x8(const float (&v)[8]) {
     uint32_t r;

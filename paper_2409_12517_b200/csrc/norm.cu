@@ -80,6 +80,13 @@ __device__ __forceinline__ float elem(const uint32_t (&w)[8], int i) {
     if constexpr (sizeof(SRC) == 4) return __uint_as_float(w[i]);
     else return (i & 1) ? bf16_hi(w[i >> 1]) : bf16_lo(w[i >> 1]);
 }
+template <typename SRC>                                       // elements i (even) and i + 1
+__device__ __forceinline__ f32x2 elems(const uint32_t (&w)[8], int i) { return pack2(elem<SRC>(w, i), elem<SRC>(w, i + 1)); }
+__device__ __forceinline__ float max3_abs(float a, float b, float c) {      // of the sizes; a NaN is not taken
+    float r;
+    asm("max.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
 template <typename SRC>
 __device__ __forceinline__ void pack_unit(const float (&v)[Unit<SRC>::kElems], uint32_t (&w)[8]) {
 #pragma unroll
@@ -94,7 +101,7 @@ __device__ __forceinline__ void add_unit(uint32_t (&w)[8], const uint32_t (&r)[8
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         if constexpr (sizeof(SRC) == 4) w[i] = __float_as_uint(__fadd_rn(__uint_as_float(w[i]), __uint_as_float(r[i])));
-        else w[i] = cvt_bf16x2(__fadd_rn(bf16_lo(w[i]), bf16_lo(r[i])), __fadd_rn(bf16_hi(w[i]), bf16_hi(r[i])));
+        else asm("add.rn.bf16x2 %0, %0, %1;" : "+r"(w[i]) : "r"(r[i]));
     }
 }
 template <int N>
@@ -122,9 +129,16 @@ __device__ __forceinline__ void warp_top(float& top, float& rest) {
     rest = __uint_as_float(key ^ (key & 0x80000000u ? 0x80000000u : 0xffffffffu));
     top = most;
 }
-template <bool MAX, typename STAT>
-__device__ __forceinline__ void over_row(STAT& sum, float& top, float& rest, int tpr, Part<STAT>& part) {
+// LEAN: where several warps have a row, their own sums are in fp32, and only those of the warps are added up in STAT.
+template <bool MAX, bool LEAN, typename STAT>
+__device__ __forceinline__ void over_row(STAT& sum, float lean_sum, float& top, float& rest, int tpr, Part<STAT>& part) {
+    if (LEAN && tpr > 32) {
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) lean_sum = __fadd_rn(lean_sum, __shfl_xor_sync(kAll, lean_sum, o));
+        sum = lean_sum;
+    }
     for (int o = min(tpr, 32) >> 1; o > 0; o >>= 1) {
+        if (LEAN && tpr > 32) break;
         sum += __shfl_xor_sync(kAll, sum, o);
         if (MAX && tpr < 32) {
             const float other = __shfl_xor_sync(kAll, top, o), other_rest = __shfl_xor_sync(kAll, rest, o);
@@ -154,6 +168,7 @@ __device__ __forceinline__ void over_row(STAT& sum, float& top, float& rest, int
 // The E4M3 code of h * gain * factor (64 bits), rounded once: to fp32 with a last bit that says whether something was cut off, from
 // where the conversion rounds to the code.
 __device__ __forceinline__ float for_code(float h, float gain, double factor) {
+    asm volatile("" : "+f"(gain));                // (the gain's 64-bit values are not to be made ahead of the loop and kept)
     const double v = static_cast<double>(h) * static_cast<double>(gain) * factor;
     const float cut = __double2float_rz(v);
     return static_cast<double>(cut) != v ? __uint_as_float(__float_as_uint(cut) | 1u) : cut;
@@ -162,15 +177,17 @@ __device__ __forceinline__ float for_code(float h, float gain, double factor) {
 // ---------------------------------------------------------------- forward
 // NU: units per thread.  With one (d <= 16384 bf16, 8192 fp32) the next row is fetched ahead and the gain stays in registers.
 // Codes (OUT != FP8MLP_RMS_SAME) are those next to the exact value: an fp32 product may land on the other side of a border between two
-// codes (one in 10^6 does, each a step of 6 percent).  A row's statistics are taken in 64 bits (bf16: from fp32 sums of four squares, which have 16 bits each); a unit's codes
+// codes (one in 10^6 does, each a step of 6 percent).  A row's statistics
+// are joined in 64 bits (of bf16 rows those of its warps, whose squares have 16 bits), the factor has a second fp32 number; a unit's codes
 // are converted from its fp32 values a little increased and a little decreased, and where the two differ its products are taken again
 // in 64 bits (one unit in 5000).
-// Measured, 16384 x 4096 with residual: bf16 to codes 79 us (codes from fp32 products 77), 72 at the copy rate; to bf16 90 (82); codes
-// with a scale per row 89; fp32 to codes 135 (133).  2048 x 16384 bf16 to codes 44 (36).  DRAM and the row's chain of reductions.
+// Measured, 16384 x 4096 with residual: bf16 to codes 80 us (from fp32 products alone 77; 72 at the copy rate), with a scale per row 81,
+// to bf16 89 (82); fp32 to codes 135 (133).  2048 x 16384 bf16 to codes 44 (36).  What bounds it: DRAM, and the row's chain of reductions.
 template <typename SRC, int BLOCK, int NU, bool WIDE, int OUT>
 __global__ void __launch_bounds__(BLOCK, 1024 / BLOCK) norm_kernel(const NormArgs p) {
     constexpr int E = Unit<SRC>::kElems;
     constexpr bool kCodes = OUT != FP8MLP_RMS_SAME, kRows = OUT == FP8MLP_RMS_E4M3_ROWS;
+    constexpr bool kLean = kCodes && sizeof(SRC) == 2;
     using Stat = typename std::conditional<kCodes, double, float>::type;
     __shared__ Part<Stat> part[2];
     __shared__ float warp_max[kMaxWarps];
@@ -203,6 +220,7 @@ __global__ void __launch_bounds__(BLOCK, 1024 / BLOCK) norm_kernel(const NormArg
         const bool here = row < p.T;
         uint32_t h[NU][8];
         Stat sum = 0;                                       // of h^2
+        float lean_sum = 0.0f;
         float top = 0.0f, top_rest = 0.0f;                  // max |h gain|, and what its rounding left off (a scale for the row)
 #pragma unroll
         for (int k = 0; k < NU; ++k) {
@@ -217,63 +235,90 @@ __global__ void __launch_bounds__(BLOCK, 1024 / BLOCK) norm_kernel(const NormArg
             if (NU > 1) load_gain<E>(p.gain, u * E, gain);
             float s[E / 4];
 #pragma unroll
-            for (int i = 0; i < E; ++i) {
-                const float v = elem<SRC>(h[k], i), g = __fmul_rn(fabsf(v), fabsf(gain[i]));
-                if constexpr (kCodes && sizeof(SRC) == 4) sum += static_cast<Stat>(v) * static_cast<Stat>(v);
-                else s[i / 4] = i % 4 == 0 ? __fmul_rn(v, v) : __fmaf_rn(v, v, s[i / 4]);
-                if constexpr (kRows) {
-                    const float rest = __fmaf_rn(fabsf(v), fabsf(gain[i]), -g);
-                    top_rest = g > top ? rest : top_rest;
+            for (int j = 0; j < E / 4; ++j) {               // four elements, two an instruction
+                const f32x2 a = elems<SRC>(h[k], 4 * j), b = elems<SRC>(h[k], 4 * j + 2);
+                if constexpr (!kCodes || sizeof(SRC) == 2) {
+                    float lo, hi;
+                    unpack2(fma2(b, b, mul2(a, a)), lo, hi);
+                    s[j] = __fadd_rn(lo, hi);
                 }
-                top = fmaxf(top, g);
+                if constexpr (!kRows) {
+                    float g[4];
+                    unpack2(mul2(a, pack2(gain[4 * j], gain[4 * j + 1])), g[0], g[1]);
+                    unpack2(mul2(b, pack2(gain[4 * j + 2], gain[4 * j + 3])), g[2], g[3]);
+                    top = max3_abs(max3_abs(top, g[0], g[1]), g[2], g[3]);
+                }
             }
-            if constexpr (!kCodes || sizeof(SRC) == 2)
 #pragma unroll
-                for (int i = 0; i < E / 4; i += 2) sum += static_cast<Stat>(s[i]) + static_cast<Stat>(s[i + 1]);
+            for (int i = 0; i < E; ++i) {
+                const float v = elem<SRC>(h[k], i);
+                if constexpr (kCodes && sizeof(SRC) == 4) sum += static_cast<Stat>(v) * static_cast<Stat>(v);
+                if constexpr (kRows) {
+                    const float g = __fmul_rn(fabsf(v), fabsf(gain[i])), rest = __fmaf_rn(fabsf(v), fabsf(gain[i]), -g);
+                    top_rest = g > top ? rest : top_rest;
+                    top = fmaxf(top, g);
+                }
+            }
+            if constexpr (kLean) {
+                if (p.tpr > 32) lean_sum = __fadd_rn(lean_sum, __fadd_rn(__fadd_rn(s[0], s[1]), __fadd_rn(s[2], s[3])));
+                else sum += (static_cast<Stat>(s[0]) + static_cast<Stat>(s[1])) + (static_cast<Stat>(s[2]) + static_cast<Stat>(s[3]));
+            } else if constexpr (!kCodes) {
+#pragma unroll
+                for (int i = 0; i < E / 4; i += 2) sum += s[i] + s[i + 1];
+            }
         }
         if (NU == 1) fetch(row + step);
-        over_row<kRows>(sum, top, top_rest, p.tpr, part[parity]);
-        Stat exact = 0;                                     // 1 / rms
-        float rstd;
+        over_row<kRows, kLean>(sum, lean_sum, top, top_rest, p.tpr, part[parity]);
+        float rstd, factor, factor_rest = 0.0f;             // the factor of codes, and what its rounding left off
         if constexpr (kCodes) {
             const double mean = sum * p.inv_d64 + static_cast<double>(p.eps);
-            rstd = __fdiv_rn(1.0f, __fsqrt_rn(static_cast<float>(mean)));
-            exact = rstd;
-            if (rstd > 0.0f && !isinf(rstd)) exact = exact * (1.5 - 0.5 * mean * exact * exact);       // one step of Newton's method
-            rstd = static_cast<float>(exact);
+            const float m = static_cast<float>(mean);
+            rstd = __fdiv_rn(1.0f, __fsqrt_rn(m));
+            // one step of Newton's method for 1 / sqrt(mean), its residual 1 - mean rstd^2 with what the roundings of both left off
+            float step = 0.0f;
+            if (rstd > 0.0f && !isinf(rstd)) {
+                const float square = __fmul_rn(rstd, rstd), square_rest = __fmaf_rn(rstd, rstd, -square), m_rest = static_cast<float>(mean - static_cast<double>(m));
+                step = __fmul_rn(__fmul_rn(0.5f, rstd), __fmaf_rn(-m_rest, square, __fmaf_rn(-m, square_rest, __fmaf_rn(-m, square, 1.0f))));
+            }
+            // y = (h gain) factor
+            factor = __fmul_rn(rstd, scale);
+            factor_rest = __fmaf_rn(step, scale, __fmaf_rn(rstd, scale, -factor));
+            rstd = __fadd_rn(rstd, step);
         } else {
             rstd = __fdiv_rn(1.0f, __fsqrt_rn(__fmaf_rn(sum, p.inv_d, p.eps)));
+            factor = rstd;
         }
         if (here && u0 == 0 && p.rstd != nullptr) p.rstd[row] = rstd;
-        // y = (h gain) factor; codes with a scale of the row's own do not depend on rstd, as it cancels
-        if (OUT == FP8MLP_RMS_E4M3) exact *= scale;
-        if constexpr (kRows) {
+        if constexpr (kRows) {                              // codes with a scale of the row's own do not depend on rstd, as it cancels
             const float most = __fmul_rn(top, rstd), row_scale = __fdiv_rn(448.0f, most);
             const float to_codes = __fdiv_rn(448.0f, top);
             const bool sound = most > 0.0f && !isinf(most) && !isinf(row_scale) && !isinf(to_codes);
             if (sound) {
-                exact = to_codes;
-                exact += exact * (1.0 / 448.0) * (448.0 - exact * (static_cast<double>(top) + static_cast<double>(top_rest)));
+                factor = to_codes;
+                factor_rest = __fmul_rn(__fmul_rn(to_codes, 1.0f / 448.0f), __fmaf_rn(-to_codes, top_rest, __fmaf_rn(-to_codes, top, 448.0f)));
             }
             if (here && u0 == 0) p.scale[row] = sound ? row_scale : 1.0f;
         } else {
             run_max = fmaxf(run_max, __fmul_rn(top, rstd));
         }
-        const float factor = kCodes ? static_cast<float>(exact) : rstd;
 #pragma unroll
         for (int k = 0; k < NU; ++k) {
             const int u = u0 + k * p.tpr;
             if (!here || u >= p.units) continue;
             if (NU > 1) load_gain<E>(p.gain, u * E, gain);
-            float v[E];
-#pragma unroll
-            for (int i = 0; i < E; ++i) v[i] = __fmul_rn(__fmul_rn(elem<SRC>(h[k], i), gain[i]), factor);
             if constexpr (OUT == FP8MLP_RMS_SAME) {
+                float v[E];
+#pragma unroll
+                for (int i = 0; i < E; i += 2)
+                    unpack2(mul2(mul2(elems<SRC>(h[k], i), pack2(gain[i], gain[i + 1])), pack2(factor, factor)), v[i], v[i + 1]);
                 uint32_t w[8];
                 pack_unit<SRC>(v, w);
                 store_unit<WIDE>(p.y + row * p.ld_y + 32 * u, w);
             } else {
                 uint8_t* dst = p.y + row * p.ld_y + E * u;
+                float v[E];
+#pragma unroll
+                for (int i = 0; i < E; ++i) v[i] = __fmul_rn(__fmul_rn(elem<SRC>(h[k], i), gain[i]), factor);
                 // three roundings of 2^-24: the exact values lie between these
                 const f32x2 more = pack2(1.0f + 0x1p-21f, 1.0f + 0x1p-21f), less = pack2(1.0f - 0x1p-21f, 1.0f - 0x1p-21f);
                 uint32_t c[E / 4], differ = 0;
@@ -289,6 +334,7 @@ __global__ void __launch_bounds__(BLOCK, 1024 / BLOCK) norm_kernel(const NormArg
                     differ |= c[i] ^ cvt_fp8x4<FP8MLP_E4M3>(lo[0], lo[1], lo[2], lo[3]);
                 }
                 if (differ != 0) {
+                    const double exact = static_cast<double>(factor) + static_cast<double>(isnan(factor_rest) ? 0.0f : factor_rest);
 #pragma unroll
                     for (int i = 0; i < E / 4; ++i)
                         c[i] = cvt_fp8x4<FP8MLP_E4M3>(for_code(elem<SRC>(h[k], 4 * i), gain[4 * i], exact), for_code(elem<SRC>(h[k], 4 * i + 1), gain[4 * i + 1], exact),
@@ -384,7 +430,7 @@ __global__ void __launch_bounds__(BLOCK) norm_backward_kernel(const NormBackArgs
         }
         if (NU == 1) fetch(row + step);
         float unused = 0.0f;
-        over_row<false>(sum, unused, unused, p.tpr, part_sum[parity]);
+        over_row<false, false>(sum, 0.0f, unused, unused, p.tpr, part_sum[parity]);
         const float mean = __fmul_rn(sum, p.inv_d);
 #pragma unroll
         for (int k = 0; k < NU; ++k) {
