@@ -6,15 +6,14 @@
 // P is A and Q is B, or the other way round where A has few rows: a product of one token with a large weight matrix is bound by
 // reading the weights, so their rows fill the 128 accumulator rows and the tokens are its 16 to 128 columns.
 //
-// A CTA is two TMA warps, which take turns, one warp that issues the MMAs and 4 or 8 epilogue warps.  At 384 cycles of MMAs a
-// stage, the loops of the first three are what bounds the kernel: a wait takes 100 cycles though nothing is to be waited for, a
-// stage's loads 290.  So the MMA warp has one barrier to look at, asks for the next stage's before it issues the present stage, and
-// all of it walks the loop while one elected lane issues, for addresses and descriptors then are the warp's, as the tensor
-// instructions need them (moving them over from a lane's registers: 115 cycles for each of 10 to 16 instructions a stage).
-// A stage holds 256 columns of the contraction: 128 bytes of codes a
-// row, and the scales' tiles of 512 bytes as they lie in memory (32 rows of 16 bytes), which tcgen05.cp copies to the four lane
-// quadrants of 4 tensor-memory columns.  Tensor memory holds the scales of two stages or more: those
-// of a stage are copied once the MMAs that read their place last are done.
+// A CTA is two TMA warps, which take turns, one warp that issues the MMAs and 4 or 8 epilogue warps.  A stage is 512 cycles of MMAs
+// at most, and the loops of the first three must be shorter: a wait takes 100 cycles though nothing is to be waited for, a stage's
+// loads 290 (one TMA warp of a pair could not keep up).  So the MMA warp has one barrier to look at, asks for the next stage's before
+// it issues the present stage, and all of it walks the loop while one elected lane issues, for addresses and descriptors then are
+// the warp's, as the tensor instructions need them (moving them over from a lane's registers: 115 cycles for each of 10 to 16
+// instructions a stage).  A stage holds 256 columns of the contraction: 128 bytes of codes a row, and the scales' tiles of 512 bytes
+// as they lie in memory (32 rows of 16 bytes), which tcgen05.cp copies to the four lane quadrants of 4 tensor-memory columns.
+// Tensor memory holds the scales of every stage of the ring beside the accumulator.
 //
 // Large products: CTA pairs on 256 x 256 tiles (cta_group::2; each CTA loads its 128 rows of P, half of the rows of Q, and the
 // scales of all of Q).  What bounds them is the way from L2 to the SMs, some 60 bytes a clock: 35 KB (MXFP4) a stage of 512 cycles
@@ -59,7 +58,7 @@ template <int FMT, int TN, bool PAIR> struct Shape {
     static constexpr int kSfBytes = kTiles * kScaleTile;                  // per 128 rows
     static constexpr int kStageBytes = kPBytes + kQBytes + (1 + kQGroups) * kSfBytes;
     // A single CTA shares its SM with another that works while it starts or ends.
-    static constexpr int kCtasPerSm = PAIR ? 1 : 2, kAccs = PAIR && TN <= 192 ? 2 : 1;
+    static constexpr int kCtasPerSm = PAIR ? 1 : 2;
     static constexpr int kStoreBytes = PAIR ? 8 * 4096 : 0;               // staging of the output, 4 KB for each epilogue warp
     static constexpr int kFit = (232448 - 1024 - 256 - kStoreBytes) / kStageBytes;
     static constexpr int kStages = PAIR ? (kFit < 6 ? kFit : 6) : TN >= 64 ? 3 : 4;
@@ -67,16 +66,13 @@ template <int FMT, int TN, bool PAIR> struct Shape {
     static constexpr int kThreads = 32 * (kOtherWarps + kEpiWarps);
     static constexpr int kWarpCols = TN / (kEpiWarps / 4);                // columns of a tile that an epilogue warp drains
     static constexpr int kSfCols = 4 * kTiles * (1 + kQGroups);           // tensor-memory columns of a stage's scales
-    // stages whose scales tensor memory holds at a time: as many as fit, at least two
-    static constexpr int kRoom = (512 / kCtasPerSm - kAccs * TN) / kSfCols;
-    static constexpr int kSfSlots = kRoom < kStages ? kRoom : kStages, kLag = kStages - kSfSlots;
-    static constexpr int kCols = kAccs * TN + kSfSlots * kSfCols;
+    static constexpr int kCols = TN + kStages * kSfCols;                  // the accumulator and the scales of all stages
     static constexpr int kTmem = kCols <= 128 ? 128 : kCols <= 256 ? 256 : 512;
-    static_assert(kSfSlots >= 2 && kCols <= 512 && kTmem * kCtasPerSm <= 512, "tensor memory");
+    static_assert(kCols <= 512 && kTmem * kCtasPerSm <= 512, "tensor memory");
 };
 
 struct __align__(8) Tail4 {
-    uint64_t full[6], empty[6], tmem_full[2], tmem_empty[2];
+    uint64_t full[6], empty[6], tmem_full, tmem_empty;
     uint32_t tmem_base;
     int abort;
 };
@@ -400,10 +396,8 @@ gemm4_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_constant__ CU
             mbar_init(smem_u32(&tail->full[s]), 1);
             mbar_init(smem_u32(&tail->empty[s]), 1);
         }
-        for (int b = 0; b < 2; ++b) {
-            mbar_init(smem_u32(&tail->tmem_full[b]), 1);
-            mbar_init(smem_u32(&tail->tmem_empty[b]), (PAIR ? 2 : 1) * S::kEpiWarps);
-        }
+        mbar_init(smem_u32(&tail->tmem_full), 1);
+        mbar_init(smem_u32(&tail->tmem_empty), (PAIR ? 2 : 1) * S::kEpiWarps);
         tail->abort = 0;
         mbar_init_fence();
     }
@@ -420,19 +414,15 @@ gemm4_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_constant__ CU
 
     if (warp < 2) {
         // ------------------------------------------------------------ TMA producers: every other stage each
-        // A stage's barrier is armed, so that it can complete, kLag stages after its loads were issued: then the stage whose
-        // scales it overwrites in tensor memory is known to be done, and the MMA warp has one barrier to wait for, not two.
         if (lane == 0) {
             const int per_tile = kb_end - kb_begin, my_tiles = !PAIR ? 1 : first_tile < num_tiles ? (num_tiles - 1 - first_tile) / tile_step + 1 : 0;
             const uint32_t total = static_cast<uint32_t>(per_tile) * my_tiles;
             int tile = first_tile, kb = kb_begin + warp, p_tile, q_tile;
             tile4_coords<PAIR>(p, tile, p_tile, q_tile);
-            for (uint32_t n = warp; n < total + S::kLag; n += 2, kb += 2) {
+            for (uint32_t n = warp; n < total; n += 2, kb += 2) {
                 const uint32_t stage = n % kStages, parity = (n / kStages) & 1u;
                 if (!mbar_wait(smem_u32(&tail->empty[stage]), parity ^ 1u, abort_flag, nullptr)) break;
-                if ((!PAIR || rank == 0) && n + 1 > S::kLag)         // a pair's bytes are counted by rank 0
-                    mbar_expect_tx(smem_u32(&tail->full[(n - S::kLag) % kStages]), (PAIR ? 2 : 1) * kStageBytes);
-                if (n >= total) continue;
+                if (!PAIR || rank == 0) mbar_expect_tx(smem_u32(&tail->full[stage]), (PAIR ? 2 : 1) * kStageBytes);      // a pair's bytes are counted by rank 0
                 while (kb >= kb_end) { kb -= per_tile; tile += tile_step; tile4_coords<PAIR>(p, tile, p_tile, q_tile); }
                 const int p_group = PAIR ? 2 * p_tile + static_cast<int>(rank) : p_tile, p0 = p_group * kRows;
                 const int q0 = q_tile * TN, q_first = q0 + (PAIR ? static_cast<int>(rank) * (TN / 2) : 0), q_group = q0 / kRows;
@@ -456,16 +446,13 @@ gemm4_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_constant__ CU
         if (!PAIR || rank == 0u) {
             const uint32_t leader = elect_one();
             Ring<kStages> ring;
-            uint32_t slot = 0;
             bool ok = true, ready = false;
             int it = 0;
             for (int tile = first_tile; ok && tile < num_tiles; tile += tile_step, ++it) {
                 int p_tile, q_tile;
                 tile4_coords<PAIR>(p, tile, p_tile, q_tile);
-                const uint32_t acc = it % S::kAccs, acc_phase = (it / S::kAccs) & 1;
-                if (!__all_sync(kAll, mbar_wait(smem_u32(&tail->tmem_empty[acc]), acc_phase ^ 1u, abort_flag, nullptr))) break;
+                if (!__all_sync(kAll, mbar_wait(smem_u32(&tail->tmem_empty), (it & 1) ^ 1u, abort_flag, nullptr))) break;
                 tc_fence_after();
-                const uint32_t d_tmem = tmem_base + acc * TN;
                 // first column of the tile's scales; the MMA takes them from even columns only, so that tiles narrower than 64 are
                 // for products with one such tile
                 const uint32_t q_offset = TN >= 64 ? static_cast<uint32_t>((q_tile * TN) % kRows) / 32u : 0u;
@@ -475,28 +462,27 @@ gemm4_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_constant__ CU
                         if (!ok) break;
                     }
                     tc_fence_after();
-                    const uint32_t sf_p = tmem_base + S::kAccs * TN + slot * S::kSfCols, sf_q = sf_p + 4 * S::kTiles;
+                    const uint32_t sf_p = tmem_base + TN + ring.stage * S::kSfCols, sf_q = sf_p + 4 * S::kTiles;
                     const uint32_t base = (tiles_addr + ring.stage * kStageBytes) >> 4;        // descriptors count in 16 bytes
                     const uint32_t sf_base = base + ((S::kPBytes + S::kQBytes) >> 4), done = smem_u32(&tail->empty[ring.stage]);
                     ring.next();
-                    if (++slot == S::kSfSlots) slot = 0;
                     const bool filled = mbar_peek(smem_u32(&tail->full[ring.stage]), ring.phase);
                     if (leader) {
                         const int left = p.K - kb * kStageK;
-                        if (left >= kStageK) issue_stage<FMT, TN, PAIR, true>(d_tmem, base, sf_base, sf_p, sf_q, q_offset, kb != kb_begin, left);
-                        else issue_stage<FMT, TN, PAIR, false>(d_tmem, base, sf_base, sf_p, sf_q, q_offset, kb != kb_begin, left);
+                        if (left >= kStageK) issue_stage<FMT, TN, PAIR, true>(tmem_base, base, sf_base, sf_p, sf_q, q_offset, kb != kb_begin, left);
+                        else issue_stage<FMT, TN, PAIR, false>(tmem_base, base, sf_base, sf_p, sf_q, q_offset, kb != kb_begin, left);
                         if constexpr (PAIR) umma_commit_pair(done); else umma_commit(done);
                     }
                     ready = __all_sync(kAll, filled);
                 }
                 if (ok && leader) {
-                    if constexpr (PAIR) umma_commit_pair(smem_u32(&tail->tmem_full[acc])); else umma_commit(smem_u32(&tail->tmem_full[acc]));
+                    if constexpr (PAIR) umma_commit_pair(smem_u32(&tail->tmem_full)); else umma_commit(smem_u32(&tail->tmem_full));
                 }
                 __syncwarp();
             }
             if constexpr (!PAIR) {
                 // the accumulator has been read: tensor memory is given back while the output is on its way (1 x 4096 x 1024: 4.0 -> 3.2 us)
-                if (ok && __all_sync(kAll, mbar_wait(smem_u32(&tail->tmem_empty[0]), 0u, abort_flag, nullptr))) {
+                if (ok && __all_sync(kAll, mbar_wait(smem_u32(&tail->tmem_empty), 0u, abort_flag, nullptr))) {
                     tc_fence_after();
                     tmem_dealloc(tmem_base, S::kTmem);
                     freed = true;
@@ -515,11 +501,10 @@ gemm4_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_constant__ CU
         for (int tile = first_tile; tile < num_tiles; tile += tile_step, ++it) {
             int p_tile, q_tile;
             tile4_coords<PAIR>(p, tile, p_tile, q_tile);
-            const uint32_t acc = it % S::kAccs, acc_phase = (it / S::kAccs) & 1;
-            const bool got = mbar_wait(smem_u32(&tail->tmem_full[acc]), acc_phase, abort_flag, nullptr);
+            const bool got = mbar_wait(smem_u32(&tail->tmem_full), it & 1, abort_flag, nullptr);
             if (!__all_sync(kAll, got)) break;
             tc_fence_after();
-            const uint32_t taddr = tmem_base + acc * TN + part * S::kWarpCols + (static_cast<uint32_t>(quad * 32) << 16);
+            const uint32_t taddr = tmem_base + part * S::kWarpCols + (static_cast<uint32_t>(quad * 32) << 16);
             const int row = (PAIR ? 2 * p_tile + static_cast<int>(rank) : p_tile) * kRows + quad * 32 + lane;
             const int col0 = q_tile * TN + part * S::kWarpCols;
             if constexpr (PAIR) {
@@ -530,7 +515,7 @@ gemm4_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_constant__ CU
                 tmem_ld_wait();
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive_cluster(mapa_shared(smem_u32(&tail->tmem_empty[acc]), 0));
+                if (lane == 0) mbar_arrive_cluster(mapa_shared(smem_u32(&tail->tmem_empty), 0));
                 static_assert(S::kWarpCols == 128, "write_wide");
                 if (!BULK && !p.f32 && col0 + 128 <= p.Q) {
                     uint32_t w[64];
@@ -558,7 +543,7 @@ gemm4_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_constant__ CU
                 tmem_ld_wait();
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&tail->tmem_empty[acc]));
+                if (lane == 0) mbar_arrive(smem_u32(&tail->tmem_empty));
 #pragma unroll
                 for (int c = 0; c < S::kWarpCols / kChunk; ++c) {
                     const int col = col0 + kChunk * c, have = min(kChunk, p.Q - col);      // columns of these that there are
