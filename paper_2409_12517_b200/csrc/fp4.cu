@@ -2,7 +2,7 @@
 //
 // Both directions stream their matrix once.  A block of threads owns 128 rows of the operand, so that it owns whole tiles of
 // block scales (512 bytes each, gathered in shared memory and written in one piece), and a stretch of columns.  The quotient
-// v / scale is taken exactly: a product with the reciprocal, corrected with its remainder (fused multiply-adds), so that the
+// v / scale is rounded once: a product with the reciprocal, corrected with its remainder (Markstein's correction), so that the
 // one rounding to E2M1 is right in ties and next to them; MXFP4 scales are powers of two and need none of that.
 #include "common.cuh"
 
@@ -99,7 +99,7 @@ __device__ __forceinline__ uint32_t quantise_block(const float (&v)[N], uint32_t
     } else {
         const float a = __fmul_rn(__uint_as_float(top), fabsf(g));         // (a negative g is the elements' sign)
         const bool finite = __float_as_uint(a) < 0x7f800000u;
-        // a / 6: a product with the reciprocal, corrected with its remainder.  E4M3's borders times 6 are fp32 numbers, and for any
+        // a / 6: a product with the reciprocal, corrected with its remainder (Markstein's correction).  E4M3's borders times 6 are fp32 numbers, and for any
         // other a the quotient is more than half a last place from them, so that what is left of its error turns no scale.
         constexpr float kSixth = 1.0f / 6.0f;
         const float near = __fmul_rn(a, kSixth), sixth = __fmaf_rn(__fmaf_rn(-6.0f, near, a), kSixth, near);

@@ -95,7 +95,7 @@ __device__ __forceinline__ void pack_unit(const float (&v)[Unit<SRC>::kElems], u
         else w[i] = cvt_bf16x2(v[2 * i], v[2 * i + 1]);
     }
 }
-// x + r, rounded to the type
+// x + r, rounded once to the type
 template <typename SRC>
 __device__ __forceinline__ void add_unit(uint32_t (&w)[8], const uint32_t (&r)[8]) {
 #pragma unroll
@@ -177,10 +177,9 @@ __device__ __forceinline__ float for_code(float h, float gain, double factor) {
 // ---------------------------------------------------------------- forward
 // NU: units per thread.  With one (d <= 16384 bf16, 8192 fp32) the next row is fetched ahead and the gain stays in registers.
 // Codes (OUT != FP8MLP_RMS_SAME) are those next to the exact value: an fp32 product may land on the other side of a border between two
-// codes (one in 10^6 does, each a step of 6 percent).  A row's statistics
-// are joined in 64 bits (of bf16 rows those of its warps, whose squares have 16 bits), the factor has a second fp32 number; a unit's codes
-// are converted from its fp32 values a little increased and a little decreased, and where the two differ its products are taken again
-// in 64 bits (one unit in 5000).
+// codes (one in 10^6 does, each a step of 6 percent).  A row's sums are joined in 64 bits (bf16: those of its warps, of squares that
+// have 16 bits), and the factor has a second fp32 number; a unit's codes are converted from its fp32 values a little increased and a
+// little decreased, and where the two differ its products are taken again in 64 bits (one unit in 5000).
 // Measured, 16384 x 4096 with residual: bf16 to codes 80 us (from fp32 products alone 77; 72 at the copy rate), with a scale per row 81,
 // to bf16 89 (82); fp32 to codes 135 (133).  2048 x 16384 bf16 to codes 44 (36).  What bounds it: DRAM, and the row's chain of reductions.
 template <typename SRC, int BLOCK, int NU, bool WIDE, int OUT>
