@@ -303,6 +303,38 @@ def test_codes_go_straight_into_the_block(merged):
         B.fp8mlp_destroy(ctx)
 
 
+@pytest.mark.parametrize("flags", [B.SAVE_FOR_BWD, B.SMOOTH | B.SAVE_FOR_BWD | B.GU_FP8, B.SAVE_FOR_BWD | B.H_BF16, B.SMOOTH])
+def test_codes_in_every_kind_of_context(flags):
+    """x as codes gives what the same x gives in bf16 (its codes are numbers of that type), forward and backward."""
+    T, d, f = 72, 256, 320
+    gen = torch.Generator(device="cuda").manual_seed(9)
+    randn = lambda *s: torch.randn(s, generator=gen, device="cuda")
+    x, dy, W1, W2, W3 = randn(T, d).bfloat16(), (1e-3 * randn(T, d)).bfloat16(), 0.05 * randn(d, f), 0.05 * randn(d, f), 0.05 * randn(f, d)
+    ctx = B.fp8mlp_create(T, d, f, flags)
+    try:
+        sc, am = B.new_scales(f), B.new_amax(f)
+        y = torch.empty(T, d, dtype=torch.bfloat16, device="cuda")
+        B.fp8mlp_forward(ctx, T, x, W1, W2, W3, B.SCALE_FROM_CURRENT_AMAX, sc, am, y)
+        sc["x"].fill_(64.0)
+        codes = torch.empty(T, d, dtype=torch.uint8, device="cuda")
+        ptr = B.fp8mlp_workspace(ctx, B.WS_XQ)[0]
+        for at in (codes, ptr):
+            B.fp8mlp_rmsnorm(x, None, None, EPS, at, out=B.RMS_E4M3, scale=sc["x"], amax=am["x"])
+        results = []
+        for mode, x_in in ((B.SCALE_GIVEN_X_CAST, None), (B.SCALE_GIVEN, (codes.view(torch.float8_e4m3fn).float() / 64).bfloat16())):
+            B.fp8mlp_forward(ctx, T, x_in, W1, W2, W3, mode, sc, am, y)
+            out = [y.clone()]
+            if flags & B.SAVE_FOR_BWD:
+                grads = [torch.empty_like(x)] + [torch.empty_like(w) for w in (W1, W2, W3)]
+                B.fp8mlp_backward(ctx, T, dy, B.SCALE_FROM_CURRENT_AMAX, sc, am, *grads)
+                out += grads
+            results.append(out)
+        assert all(torch.equal(a, b) for a, b in zip(*results)) and torch.isfinite(results[0][0].float()).all()
+        assert B.fp8mlp_status(ctx) == B.OK
+    finally:
+        B.fp8mlp_destroy(ctx)
+
+
 def test_another_device_or_shape_is_refused():
     x = torch.zeros(4, 64, dtype=torch.bfloat16, device="cuda")
     y = torch.zeros_like(x)
