@@ -490,12 +490,12 @@ __global__ void __launch_bounds__(BLOCK) norm_backward_kernel(const NormBackArgs
     for (int i = threadIdx.x; i < p.d; i += BLOCK) out[i] = d_gain_row[i];
 }
 
-// d_gain[i] = sum of the blocks' partial sums: 128 columns a block, every one of 32 warps takes every 32nd partial row and has
-// all their loads on their way together
-constexpr int kGainWarps = 32;
-__global__ void __launch_bounds__(32 * kGainWarps) norm_gain_kernel(const float* partial, int n_partial, int d, float* d_gain) {
-    __shared__ float4 part[kGainWarps][32];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, col = blockIdx.x * 128 + 4 * lane;
+// d_gain[i] = sum of the blocks' partial sums: 64 columns a block, 16 lanes to a row; every one of the 64 half-warps takes every 64th
+// partial row and has its loads on their way together
+constexpr int kGainThreads = 1024, kGainCols = 64, kGainRows = kGainThreads / 16;
+__global__ void __launch_bounds__(kGainThreads) norm_gain_kernel(const float* partial, int n_partial, int d, float* d_gain) {
+    __shared__ float4 part[kGainRows][16];
+    const int lane = threadIdx.x & 15, sub = threadIdx.x >> 4, col = blockIdx.x * kGainCols + 4 * lane;
     grid_dependency_wait();
     grid_launch_dependents();
     float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
@@ -504,26 +504,26 @@ __global__ void __launch_bounds__(32 * kGainWarps) norm_gain_kernel(const float*
     };
     if (col < d) {
         const float* at = partial + col;
-        for (int i = warp; i < n_partial; i += 8 * kGainWarps) {
-            float4 v[8];
+        for (int i = sub; i < n_partial; i += 5 * kGainRows) {
+            float4 v[5];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const int row = min(i + k * kGainWarps, n_partial - 1);
+            for (int k = 0; k < 5; ++k) {
+                const int row = min(i + k * kGainRows, n_partial - 1);
                 v[k] = __ldcg(reinterpret_cast<const float4*>(at + static_cast<int64_t>(row) * d));
             }
 #pragma unroll
-            for (int k = 0; k < 8; ++k)
-                if (i + k * kGainWarps < n_partial) add(sum, v[k]);
+            for (int k = 0; k < 5; ++k)
+                if (i + k * kGainRows < n_partial) add(sum, v[k]);
         }
     }
-    part[warp][lane] = sum;
+    part[sub][lane] = sum;
     __syncthreads();
-    if (threadIdx.x < 128 && blockIdx.x * 128 + threadIdx.x < d) {
+    if (threadIdx.x < kGainCols && blockIdx.x * kGainCols + threadIdx.x < d) {
         const float* mine = reinterpret_cast<const float*>(part) + threadIdx.x;
         float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int k = 0; k < kGainWarps; ++k) v[k & 3] = __fadd_rn(v[k & 3], mine[128 * k]);
-        d_gain[blockIdx.x * 128 + threadIdx.x] = __fadd_rn(__fadd_rn(v[0], v[1]), __fadd_rn(v[2], v[3]));
+        for (int k = 0; k < kGainRows; ++k) v[k & 3] = __fadd_rn(v[k & 3], mine[kGainCols * k]);
+        d_gain[blockIdx.x * kGainCols + threadIdx.x] = __fadd_rn(__fadd_rn(v[0], v[1]), __fadd_rn(v[2], v[3]));
     }
 }
 
@@ -700,7 +700,7 @@ extern "C" int fp8mlp_rmsnorm_backward(int64_t T, int64_t d, int dtype, const vo
     FP8MLP_CUDA_CHECK(FP8MLP_NORM_TYPES(FP8MLP_NORM_BACKWARD, launch_norm_backward, a, smem, grid, st));
     count_launch();
     if (d_gain != nullptr && !one_cluster) {
-        FP8MLP_CUDA_CHECK(launch_chained(norm_gain_kernel, dim3(static_cast<unsigned>((d + 127) / 128)), dim3(32 * kGainWarps), 0, st,
+        FP8MLP_CUDA_CHECK(launch_chained(norm_gain_kernel, dim3(static_cast<unsigned>((d + kGainCols - 1) / kGainCols)), dim3(kGainThreads), 0, st,
                                          static_cast<const float*>(workspace), static_cast<int>(grid.x), static_cast<int>(d), d_gain));
         count_launch();
     }
