@@ -593,7 +593,7 @@ cudaError_t launch_norm(const NormArgs& a, int out, dim3 grid, cudaStream_t st) 
 
 template <typename SRC, int BLOCK, int NU, bool WIDE>
 cudaError_t launch_norm_backward(const NormBackArgs& a, size_t smem, dim3 grid, cudaStream_t st) {
-    if (smem > 48 * 1024) {
+    if (smem + 2 * sizeof(Part<float>) > 48 * 1024) {        // with the kernel's own, more than a launch has without asking
         cudaError_t e = cudaFuncSetAttribute(norm_backward_kernel<SRC, BLOCK, NU, WIDE>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                              FP8MLP_MAX_NORM_WIDTH * 4);
         if (e != cudaSuccess) return e;
