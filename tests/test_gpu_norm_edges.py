@@ -4,8 +4,13 @@ import sys
 from pathlib import Path
 
 import pytest
+import torch
+
+import fp4_reference as R
+from paper_2409_12517_b200 import binding as B
 
 pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
 ROOT = Path(__file__).resolve().parent.parent
 
 
@@ -36,3 +41,33 @@ def test_gain_gradient_at_every_width():
     script = GAIN_GRADIENT.format(root=str(ROOT), tests=str(ROOT / "tests"))
     done = subprocess.run([sys.executable, "-c", script], capture_output=True, text=True, timeout=600)
     assert done.returncode == 0 and done.stdout.strip().endswith("fine"), done.stdout + done.stderr
+
+
+@pytest.mark.parametrize("out", [B.RMS_SAME, B.RMS_E4M3, B.RMS_E4M3_ROWS])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("d", [64, 4096])
+def test_rows_of_tiny_numbers_without_eps(d, dtype, out):
+    """eps = 0 and rows down to 2^-68: 1 / rms has no square in fp32, but is a number, and so are maximum and scale.
+    Squares are fp32 numbers, for fp32 rows to codes 64-bit ones: each of the d squares and of the sums is off by half of the
+    smallest number (2^-150) at most, beside the roundings counted in test_gpu_norm.py (32 for 1 / rms, 4 more for the scale)."""
+    gen = torch.Generator().manual_seed(d)
+    tops = torch.tensor([1.0, 2.0 ** -40, 2.0 ** -60, 2.0 ** -64, 2.0 ** -66, 2.0 ** -68])
+    x = (torch.randn(6, d, generator=gen) * tops[:, None]).to(dtype).cuda()
+    want, want_rstd = R.norm(x.cpu(), None, 0.0)
+    want, want_rstd = want.cuda(), want_rstd.cuda()
+    y = torch.empty_like(x) if out == B.RMS_SAME else torch.empty(6, d, dtype=torch.uint8, device="cuda")
+    scale = None if out == B.RMS_SAME else torch.full((6 if out == B.RMS_E4M3_ROWS else 1,), 50.0, device="cuda")
+    amax = None if out == B.RMS_E4M3_ROWS else torch.zeros(1, device="cuda")
+    rstd = torch.empty(6, device="cuda")
+    B.fp8mlp_rmsnorm(x, None, None, 0.0, y, out=out, scale=scale, amax=amax, rstd=rstd)
+    wide = out != B.RMS_SAME and dtype == torch.float32
+    low = torch.zeros_like(want_rstd) if wide else 2 * d * 2.0 ** -150 / x.double().square().sum(-1)
+    off = 32 * U + low + (2.0 ** -150 * want_rstd ** 2 if out == B.RMS_SAME else 0.0)          # (there the mean is an fp32 number too)
+    assert ((rstd.double() - want_rstd).abs() <= off * want_rstd).all()
+    if out == B.RMS_E4M3_ROWS:
+        want_scale = 448.0 / want.abs().amax(-1)
+        assert ((scale.double() - want_scale).abs() <= (off + 4 * U) * want_scale).all()
+        assert (y.view(torch.float8_e4m3fn).float().abs().amax(-1) == 448).all()
+    else:
+        top = want.abs().amax(-1)
+        assert float(amax) >= float((top * (1 - off - 4 * U)).max()) and float(amax) <= float((top * (1 + off + 4 * U)).max())
