@@ -322,7 +322,8 @@ __global__ void __launch_bounds__(BLOCK, 1024 / BLOCK) norm_kernel(const NormArg
                 float v[E];
 #pragma unroll
                 for (int i = 0; i < E; ++i) v[i] = __fmul_rn(__fmul_rn(elem<SRC>(h[k], i), gain[i]), factor);
-                // three roundings of 2^-24: the exact values lie between these
+                // The exact values lie between these: two products, the factor's product with the scale and 1 / rms (half a rounding of
+                // the mean, the root, the division) are 5.5 roundings of 2^-24 off, the products below one more; 2^-21 are eight.
                 const f32x2 more = pack2(1.0f + 0x1p-21f, 1.0f + 0x1p-21f), less = pack2(1.0f - 0x1p-21f, 1.0f - 0x1p-21f);
                 uint32_t c[E / 4], differ = 0;
 #pragma unroll
@@ -336,7 +337,8 @@ __global__ void __launch_bounds__(BLOCK, 1024 / BLOCK) norm_kernel(const NormArg
                     c[i] = cvt_fp8x4<FP8MLP_E4M3>(hi[0], hi[1], hi[2], hi[3]);
                     differ |= c[i] ^ cvt_fp8x4<FP8MLP_E4M3>(lo[0], lo[1], lo[2], lo[3]);
                 }
-                if (differ != 0) {
+                // (a factor beyond these may bring h gain back from where fp32 has few bits, or none)
+                if (differ != 0 || factor > 0x1p60f || factor < 0x1p-60f) {
                     const double exact = static_cast<double>(factor) + static_cast<double>(isnan(factor_rest) ? 0.0f : factor_rest);
 #pragma unroll
                     for (int i = 0; i < E / 4; ++i)

@@ -71,3 +71,28 @@ def test_rows_of_tiny_numbers_without_eps(d, dtype, out):
     else:
         top = want.abs().amax(-1)
         assert float(amax) >= float((top * (1 - off - 4 * U)).max()) and float(amax) <= float((top * (1 + off + 4 * U)).max())
+
+
+def between(y, exact, slack):
+    """E4M3 codes that a value within `slack` of the exact one has next to it."""
+    low, high = (R.nearest(R.E4M3_CODES[:127], exact.abs() * (1 + s * slack)) for s in (-1, 1))
+    got = (y & 0x7f).cpu().long()
+    return ((got >= low) & (got <= high)).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_codes_of_products_below_the_normal_numbers(dtype):
+    """h gain below 2^-126, where an fp32 product has few bits left, and a factor that brings it back among the codes."""
+    gen = torch.Generator().manual_seed(1)
+    T, d = 256, 1024
+    x = (torch.randn(T, d, generator=gen).sign() * torch.exp2(-116 - 12 * torch.rand(T, d, generator=gen))).to(dtype)
+    gain = 2.0 ** -8 * (1 + torch.rand(d, generator=gen))
+    x[:, 0] = 2.0 ** -110                                     # a row's largest: 448 / (h gain) stays in fp32
+    y, own = torch.empty(T, d, dtype=torch.uint8, device="cuda"), torch.empty(T, device="cuda")
+    want, _ = R.norm(x, gain, 1.0)
+    given = torch.full((1,), 2.0 ** 126, device="cuda")
+    B.fp8mlp_rmsnorm(x.cuda(), None, gain.cuda(), 1.0, y, out=B.RMS_E4M3, scale=given)
+    assert between(y, want * 2.0 ** 126, 6 * U)
+    B.fp8mlp_rmsnorm(x.cuda(), None, gain.cuda(), 1.0, y, out=B.RMS_E4M3_ROWS, scale=own)
+    # the largest h gain, about 2^-118, is known to the smallest number, half of 2^-149
+    assert between(y, want * (448.0 / want.abs().amax(-1, keepdim=True)), 2.0 ** -30)
