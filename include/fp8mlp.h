@@ -463,7 +463,7 @@ FP8MLP_API int fp8mlp_gemm_bf16(int64_t M, int64_t N, int64_t K, const void* A, 
  * x, residual, h: T rows of d elements of one type (FP8MLP_BF16 or FP8MLP_F32) with a row stride each; gain fp32 [d], null = 1.
  * h is rounded to that type once, and the norm is that of the rounded values: the gradient of what was computed follows from
  * the stored h.  Squares are summed in fp32.  h_out receives h (null: not wanted; needs a residual); it may be x or the
- * residual itself, no other outputs overlap inputs or one another.  out_kind:
+ * residual itself, with the same row stride; no other outputs overlap inputs or one another.  out_kind:
  *   FP8MLP_RMS_SAME       y in the type of x
  *   FP8MLP_RMS_E4M3       y: E4M3 codes Q(y * *scale), `scale` one device float that is read (delayed scaling)
  *   FP8MLP_RMS_E4M3_ROWS  y: E4M3 codes Q(y * scale[t]), scale fp32 [T] written: 448 / max_i |y[t, i]| (1 where that maximum is
@@ -484,7 +484,7 @@ FP8MLP_API int fp8mlp_rmsnorm(int64_t T, int64_t d, int dtype, const void* x, in
  *   g = dy * gain;   dx[t, i] = rstd[t] * (g[t, i] - h[t, i] rstd[t] * mean_j(g[t, j] h[t, j] rstd[t])) + dh[t, i]
  *   d_gain[i] = sum_t dy[t, i] h[t, i] rstd[t]           (fp32, overwritten)
  * dh (nullable): what reached h along the residual stream.  dx is the gradient of x and of the residual alike.  dy, h, dh, dx
- * of one type, a row stride each, as above; dx may be dy or dh itself.  d_gain is null if the gain has no gradient; it needs
+ * of one type, a row stride each, as above; dx may be dy or dh itself, with the same row stride.  d_gain is null if the gain has no gradient; it needs
  * `workspace`: FP8MLP_RMS_PARTIALS * d floats, 16-byte aligned, no state between calls; calls that may overlap need one each. */
 #define FP8MLP_RMS_PARTIALS 592
 FP8MLP_API int fp8mlp_rmsnorm_backward(int64_t T, int64_t d, int dtype, const void* dy, int64_t ld_dy, const void* h, int64_t ld_h,

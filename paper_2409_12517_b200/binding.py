@@ -554,7 +554,7 @@ def _floats(t, numel, what, here):
 
 def fp8mlp_rmsnorm(x, residual, gain, eps: float, y, h=None, out: int = RMS_SAME, scale=None, amax=None, rstd=None) -> None:
     """h = x + residual, y = h / rms(h) * gain.  x, residual, h: [T, d] bf16 or fp32, any row stride; residual, gain (fp32
-    [d]), h, amax (1-element fp32) and rstd (fp32 [T]) may be None; h may be x or residual.  y by `out`: RMS_SAME: [T, d] of
+    [d]), h, amax (1-element fp32) and rstd (fp32 [T]) may be None; h may be x or residual, in the same rows.  y by `out`: RMS_SAME: [T, d] of
     x's type; RMS_E4M3: codes (uint8 [T, d], or a device pointer as int, e.g. a context's WS_XQ, with rows of d bytes) of
     y * scale (1-element fp32, read); RMS_E4M3_ROWS: codes, scale (fp32 [T]) is written."""
     here = _here()
@@ -593,7 +593,7 @@ def fp8mlp_rmsnorm(x, residual, gain, eps: float, y, h=None, out: int = RMS_SAME
 
 
 def fp8mlp_rmsnorm_backward(dy, h, gain, rstd, dh, dx, d_gain, workspace) -> None:
-    """dx [T, d] (may be dy or dh) and d_gain (fp32 [d], or None) from dy, the stored h and rstd; dh: what reached h along the
+    """dx [T, d] (may be dy or dh, in the same rows) and d_gain (fp32 [d], or None) from dy, the stored h and rstd; dh: what reached h along the
     residual stream, or None; workspace: new_rmsnorm_workspace(d), or None without d_gain."""
     here = _here()
     shape, dtype = h.shape, h.dtype

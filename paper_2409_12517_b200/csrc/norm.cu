@@ -638,6 +638,8 @@ extern "C" int fp8mlp_rmsnorm(int64_t T, int64_t d, int dtype, const void* x, in
     if (h_out != nullptr && !stride_ok(T, ld_h, d, bytes)) return FP8MLP_ERR_SHAPE;
     if (T > 0 && (x == nullptr || y == nullptr)) return FP8MLP_ERR_ARG;
     if (y != nullptr && (y == x || y == residual || y == h_out)) return FP8MLP_ERR_ARG;
+    // in place, a row of the output has to lie over its own row of the input: over another, it is written before that is read, or after
+    if (h_out != nullptr && T > 1 && ((h_out == x && ld_h != ld_x) || (h_out == residual && ld_h != ld_residual))) return FP8MLP_ERR_ARG;
     if (out_kind == FP8MLP_RMS_E4M3 && scale == nullptr) return FP8MLP_ERR_ARG;
     if (out_kind == FP8MLP_RMS_E4M3_ROWS && T > 0 && scale == nullptr) return FP8MLP_ERR_ARG;
     if (!aligned(x, 16) || !aligned(residual, 16) || !aligned(h_out, 16) || !aligned(y, 16) || !aligned(gain, 16)) return FP8MLP_ERR_ALIGN;
@@ -677,6 +679,7 @@ extern "C" int fp8mlp_rmsnorm_backward(int64_t T, int64_t d, int dtype, const vo
     if (dh != nullptr && !stride_ok(T, ld_dh, d, bytes)) return FP8MLP_ERR_SHAPE;
     if (T > 0 && (dy == nullptr || h == nullptr || rstd == nullptr || dx == nullptr)) return FP8MLP_ERR_ARG;
     if (dx != nullptr && dx == h) return FP8MLP_ERR_ARG;
+    if (dx != nullptr && T > 1 && ((dx == dy && ld_dx != ld_dy) || (dx == dh && ld_dx != ld_dh))) return FP8MLP_ERR_ARG;      // (as above)
     if (!aligned(dy, 16) || !aligned(h, 16) || !aligned(dh, 16) || !aligned(dx, 16) || !aligned(gain, 16) || !aligned(workspace, 16))
         return FP8MLP_ERR_ALIGN;
     if (!aligned(rstd, 4) || !aligned(d_gain, 4)) return FP8MLP_ERR_ALIGN;

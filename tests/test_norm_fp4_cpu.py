@@ -44,6 +44,19 @@ def test_norm_refusals(lib):
         assert norm(**bad) == B.ERR_ARG, bad
 
 
+def test_norm_in_place_refuses_other_row_strides(lib):
+    """A row of the output would lie over another row of the input than its own.  (Refused before anything is launched.)"""
+    def norm(T=4, x=P, ldx=64, res=2 * P, ldr=64, h=3 * P, ldh=64):
+        return lib.fp8mlp_rmsnorm(T, 64, B.BF16, x, ldx, res, ldr, h, ldh, None, 1e-5, B.RMS_SAME, 8 * P, 64, None, None, None, None)
+
+    def back(T=4, dy=P, lddy=64, dh=2 * P, lddh=64, dx=3 * P, lddx=64):
+        return lib.fp8mlp_rmsnorm_backward(T, 64, B.BF16, dy, lddy, 4 * P, 64, None, P, dh, lddh, dx, lddx, None, None, None)
+    for bad in (dict(h=P, ldx=128), dict(h=P, ldh=128), dict(h=2 * P, ldr=72), dict(h=2 * P, ldh=80), dict(x=2 * P, h=2 * P, ldr=128)):
+        assert norm(**bad) == B.ERR_ARG, bad
+    for bad in (dict(dx=P, lddx=128), dict(dx=P, lddy=72), dict(dx=2 * P, lddx=80), dict(dx=2 * P, lddh=128), dict(dy=2 * P, dx=2 * P, lddy=128)):
+        assert back(**bad) == B.ERR_ARG, bad
+
+
 def test_norm_backward_refusals(lib):
     def back(T=4, d=64, dt=B.BF16, dy=P, lddy=64, h=2 * P, ldh=64, gain=P, rstd=P, dh=None, lddh=64, dx=P, lddx=64, dg=None, ws=None):
         return lib.fp8mlp_rmsnorm_backward(T, d, dt, dy, lddy, h, ldh, gain, rstd, dh, lddh, dx, lddx, dg, ws, None)
