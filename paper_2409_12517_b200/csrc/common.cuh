@@ -15,6 +15,9 @@ void set_cuda_error(const char* what, cudaError_t e);
 void set_cuda_error_str(const char* what, const char* msg);
 void count_launch();
 int clear_float(float* p, cudaStream_t st);      // *p = 0, in the stream's order
+// A cluster beyond the portable size of 8 blocks: small problems that one launch does.  Whether a GPU holds one is to be asked first.
+constexpr int kWideCluster = 16;
+int wide_cluster_fits(bool* fits);
 
 #define FP8MLP_CUDA_CHECK(expr)                                   \
     do {                                                          \

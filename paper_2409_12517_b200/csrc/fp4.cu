@@ -476,7 +476,7 @@ __global__ void __launch_bounds__(kThreads) amax_kernel(const AmaxArgs p) {
 
 // A small matrix with a scale of its own data (NVFP4) in one launch: the blocks of one cluster look for the maximum together,
 // exchange it over distributed shared memory and share the tiles.
-constexpr int kCluster = 16;
+constexpr int kCluster = kWideCluster;
 template <typename SRC, bool TRANSPOSED, bool VEC>
 __global__ void __launch_bounds__(kThreads) quantise_small_kernel(const QuantArgs p, const AmaxArgs m, int tiles) {
     __shared__ float warp_max[kThreads / 32], block_max[kCluster];
@@ -793,7 +793,9 @@ extern "C" int fp8mlp_quantize_fp4(const void* src, int src_dtype, int64_t rows,
     int dev = 0, sms = 0;
     FP8MLP_CUDA_CHECK(cudaGetDevice(&dev));
     FP8MLP_CUDA_CHECK(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
-    const bool one_launch = current && rows > 0 && cols > 0 && rows * cols * bytes <= kSmallBytes && tiles <= kSmallTiles;
+    bool one_launch = current && rows > 0 && cols > 0 && rows * cols * bytes <= kSmallBytes && tiles <= kSmallTiles;
+    if (one_launch)
+        if (int rc = wide_cluster_fits(&one_launch)) return rc;
     if (amax != nullptr && !one_launch)
         if (int rc = clear_float(amax, st)) return rc;
     unsigned int* amax_bits = reinterpret_cast<unsigned int*>(amax);

@@ -6,6 +6,7 @@
 // loads are on their way while the present row is summed and written.
 #include "common.cuh"
 
+#include <atomic>
 #include <type_traits>
 
 namespace fp8mlp {
@@ -14,7 +15,7 @@ namespace {
 
 constexpr uint32_t kAll = 0xffffffffu;
 constexpr int kMaxWarps = 32;
-constexpr int kCluster = 16;                // blocks of the one cluster that takes a short batch as a whole
+constexpr int kCluster = kWideCluster;      // blocks of the one cluster that takes a short batch as a whole
 
 struct NormArgs {
     const uint8_t *x, *residual;
@@ -619,6 +620,37 @@ cudaError_t launch_norm_backward(const NormBackArgs& a, size_t smem, dim3 grid, 
      : s.nu == 2 ? F<SRC, 512, 2, WIDE>(__VA_ARGS__) : F<SRC, 512, 4, WIDE>(__VA_ARGS__))
 
 }  // namespace
+
+// Asked once for each device: a part of a GPU may not have that many SMs side by side.  The kernel asked for has 64 registers for
+// each of 1024 threads, all of an SM; blocks that take less fit where these do.
+int wide_cluster_fits(bool* fits) {
+    static std::atomic<int> known[64];                       // 1 + the answer
+    int dev = 0;
+    FP8MLP_CUDA_CHECK(cudaGetDevice(&dev));
+    const int answer = dev < 64 ? known[dev].load(std::memory_order_relaxed) : 0;
+    *fits = answer == 2;
+    if (answer != 0) return FP8MLP_OK;
+    const auto kernel = norm_kernel<uint16_t, 1024, 1, true, FP8MLP_RMS_SAME>;
+    FP8MLP_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1));
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(kWideCluster);
+    cfg.blockDim = dim3(1024);
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = kWideCluster;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    int clusters = 0;
+    if (cudaOccupancyMaxActiveClusters(&clusters, kernel, &cfg) != cudaSuccess) {      // a size that the device does not know: it does not fit
+        cudaGetLastError();
+        clusters = 0;
+    }
+    *fits = clusters > 0;
+    if (dev < 64) known[dev].store(*fits ? 2 : 1, std::memory_order_relaxed);
+    return FP8MLP_OK;
+}
+
 }  // namespace fp8mlp
 
 using namespace fp8mlp;
@@ -659,7 +691,10 @@ extern "C" int fp8mlp_rmsnorm(int64_t T, int64_t d, int dtype, const void* x, in
     const bool wide = on32(x, a.ld_x) && (residual == nullptr || on32(residual, a.ld_res)) && (h_out == nullptr || on32(h_out, a.ld_h)) &&
                       (out_kind != FP8MLP_RMS_SAME || on32(y, a.ld_y));
     const int64_t rows = s.block / s.tpr, blocks = (T + rows - 1) / rows, most = static_cast<int64_t>(sms) * (1024 / s.block);
-    a.cluster = amax != nullptr && blocks > 1 && one_cluster_does(s, blocks) ? 1 : 0;
+    bool one_cluster = amax != nullptr && blocks > 1 && one_cluster_does(s, blocks);
+    if (one_cluster)
+        if (int rc = wide_cluster_fits(&one_cluster)) return rc;
+    a.cluster = one_cluster ? 1 : 0;
     const dim3 grid(static_cast<unsigned>(a.cluster ? kCluster : blocks < most ? blocks : most));
     if (amax != nullptr && grid.x > 1 && !a.cluster)
         if (int rc = clear_float(amax, st)) return rc;
@@ -702,7 +737,9 @@ extern "C" int fp8mlp_rmsnorm_backward(int64_t T, int64_t d, int dtype, const vo
     const int64_t rows = s.block / s.tpr, blocks = (T + rows - 1) / rows;
     int64_t most = static_cast<int64_t>(sms) * (512 / s.block);
     if (most > FP8MLP_RMS_PARTIALS) most = FP8MLP_RMS_PARTIALS;      // a row of the workspace per block
-    const bool one_cluster = d_gain != nullptr && one_cluster_does(s, blocks);
+    bool one_cluster = d_gain != nullptr && one_cluster_does(s, blocks);
+    if (one_cluster)
+        if (int rc = wide_cluster_fits(&one_cluster)) return rc;
     if (one_cluster) { a.d_gain = d_gain; a.partial = nullptr; }
     const dim3 grid(static_cast<unsigned>(one_cluster ? kCluster : blocks < most ? blocks : most));
     const size_t smem = d_gain != nullptr && (s.nu > 1 || rows > 1 || one_cluster) ? sizeof(float) * d : 0;
