@@ -217,12 +217,12 @@ def fp8mlp_destroy(ctx: int) -> None:
     _check(lib().fp8mlp_destroy(C.c_void_p(ctx)), "fp8mlp_destroy")
 
 
-def fp8mlp_status(ctx: int) -> int:
-    """Synchronises the current stream and returns OK or ERR_TIMEOUT (does not raise)."""
+def fp8mlp_status(ctx: int | None) -> int:
+    """Synchronises the current stream and returns OK or ERR_TIMEOUT (does not raise); ctx None: of the products without one."""
     return int(lib().fp8mlp_status(C.c_void_p(ctx), _stream()))
 
 
-def fp8mlp_selftest_wait_timeout(ctx: int, timeout_us: int) -> None:
+def fp8mlp_selftest_wait_timeout(ctx: int | None, timeout_us: int) -> None:
     """Runs a kernel whose bounded wait must time out; afterwards fp8mlp_status reports ERR_TIMEOUT once."""
     _check(lib().fp8mlp_selftest_wait_timeout(C.c_void_p(ctx), timeout_us, _stream()), "fp8mlp_selftest_wait_timeout")
 

@@ -246,6 +246,20 @@ int check_forward_args(const fp8mlp_ctx* c, int64_t T, const void* x, const floa
     return FP8MLP_OK;
 }
 
+// Waits for the stream; a status word that a wait has raised is reported and cleared.
+int take_status(int* at, cudaStream_t st) {
+    int word = 0;
+    FP8MLP_CUDA_CHECK(cudaMemcpyAsync(&word, at, sizeof(int), cudaMemcpyDeviceToHost, st));
+    FP8MLP_CUDA_CHECK(cudaStreamSynchronize(st));
+    if (word != STATUS_OK) {
+        FP8MLP_CUDA_CHECK(cudaMemsetAsync(at, 0, sizeof(int), st));
+        return FP8MLP_ERR_TIMEOUT;
+    }
+    return FP8MLP_OK;
+}
+
+__device__ int selftest_gave_up;
+
 }  // namespace
 
 extern "C" {
@@ -338,25 +352,30 @@ int fp8mlp_destroy(fp8mlp_ctx* c) {
 }
 
 int fp8mlp_status(fp8mlp_ctx* c, void* stream) {
-    if (c == nullptr) return FP8MLP_ERR_ARG;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    int word = 0;
-    FP8MLP_CUDA_CHECK(cudaMemcpyAsync(&word, c->status, sizeof(int), cudaMemcpyDeviceToHost, st));
-    FP8MLP_CUDA_CHECK(cudaStreamSynchronize(st));
-    if (word != STATUS_OK) {
-        FP8MLP_CUDA_CHECK(cudaMemsetAsync(c->status, 0, sizeof(int), st));
-        return FP8MLP_ERR_TIMEOUT;
+    if (c != nullptr) return take_status(c->status, st);
+    int* words[2];
+    FP8MLP_TRY(gemm_status_word(&words[0]));
+    FP8MLP_TRY(gemm4_status_word(&words[1]));
+    int rc = FP8MLP_OK;
+    for (int* word : words) {
+        const int one = take_status(word, st);
+        if (one != FP8MLP_OK && one != FP8MLP_ERR_TIMEOUT) return one;
+        if (one != FP8MLP_OK) rc = one;
     }
-    return FP8MLP_OK;
+    return rc;
 }
 
 int fp8mlp_selftest_wait_timeout(fp8mlp_ctx* c, int64_t timeout_us, void* stream) {
-    if (c == nullptr) return FP8MLP_ERR_ARG;
     if (timeout_us < 1 || timeout_us > 1000000) return FP8MLP_ERR_ARG;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    int* gave_up = reinterpret_cast<int*>(c->dummy + 6);      // a spare word of the context
+    int* status;
+    if (c != nullptr) status = c->status;
+    else FP8MLP_TRY(gemm4_status_word(&status));
+    int* gave_up;
+    FP8MLP_CUDA_CHECK(cudaGetSymbolAddress(reinterpret_cast<void**>(&gave_up), selftest_gave_up));
     FP8MLP_CUDA_CHECK(cudaMemsetAsync(gave_up, 0, sizeof(int), st));
-    wait_selftest_kernel<<<1, 32, 0, st>>>(c->status, static_cast<uint64_t>(timeout_us) * 1000ull, gave_up);
+    wait_selftest_kernel<<<1, 32, 0, st>>>(status, static_cast<uint64_t>(timeout_us) * 1000ull, gave_up);
     FP8MLP_LAUNCH_CHECK();
     int flag = 0;
     FP8MLP_CUDA_CHECK(cudaMemcpyAsync(&flag, gave_up, sizeof(int), cudaMemcpyDeviceToHost, st));
@@ -839,6 +858,7 @@ int fp8mlp_gemm_bf16(int64_t M, int64_t N, int64_t K, const void* A, int a_kmajo
     if (a_kmajor) FP8MLP_TRY(make_tmap(&tmA, A, 2, false, K, M, 2 * K)); else FP8MLP_TRY(make_tmap(&tmA, A, 2, true, M, K, 2 * M));
     if (b_kmajor) FP8MLP_TRY(make_tmap(&tmB, B, 2, false, K, N, 2 * K)); else FP8MLP_TRY(make_tmap(&tmB, B, 2, true, N, K, 2 * N));
     GemmArgs a = base_args(nullptr, static_cast<int>(M), static_cast<int>(N), static_cast<int>(K));
+    FP8MLP_TRY(gemm_status_word(&a.status));
     a.elem_bytes = 2;
     a.out_f32_0 = out; a.out_f32_1 = out;
     return launch_gemm(EPI_F32, !a_kmajor, !b_kmajor, 1, 1, tmA, tmB, tmB, a, sms, static_cast<cudaStream_t>(stream));
@@ -857,6 +877,7 @@ int fp8mlp_gemm_fp8(int64_t M, int64_t N, int64_t K, const uint8_t* A, int a_kma
     if (a_kmajor) FP8MLP_TRY(make_tmap_u8(&tmA, A, K, M, K)); else FP8MLP_TRY(make_tmap_u8(&tmA, A, M, K, M));
     if (b_kmajor) FP8MLP_TRY(make_tmap_u8(&tmB, B, K, N, K)); else FP8MLP_TRY(make_tmap_u8(&tmB, B, N, K, N));
     GemmArgs a = base_args(nullptr, static_cast<int>(M), static_cast<int>(N), static_cast<int>(K));
+    FP8MLP_TRY(gemm_status_word(&a.status));
     a.s0 = scale_a; a.s1 = scale_b;
     a.out_f32_0 = out; a.out_f32_1 = out;
     return launch_gemm(EPI_F32, !a_kmajor, !b_kmajor, a_fmt, b_fmt, tmA, tmB, tmB, a, sms, static_cast<cudaStream_t>(stream));

@@ -1089,6 +1089,15 @@ int make_tmap_out_f32(CUtensorMap* map, const void* base, uint64_t cols, uint64_
 }
 
 namespace {
+__device__ int wait_status;
+}  // namespace
+
+int gemm_status_word(int** word) {
+    FP8MLP_CUDA_CHECK(cudaGetSymbolAddress(reinterpret_cast<void**>(word), wait_status));
+    return FP8MLP_OK;
+}
+
+namespace {
 int make_tmap_bytes(CUtensorMap* map, const void* base, uint32_t rank, const cuuint64_t* dims, const cuuint64_t* strides,
                     const cuuint32_t* box, CUtensorMapSwizzle swizzle) {
     EncodeTiledFn fn = encode_fn();

@@ -103,6 +103,9 @@ int make_tmap_u8(CUtensorMap* map, const void* base, uint64_t inner, uint64_t ou
 // the GEMM will read the matrix (an MN-major 16-bit operand is fetched in boxes of 64 K-rows).
 int make_tmap(CUtensorMap* map, const void* base, int elem_bytes, bool mn_major, uint64_t inner, uint64_t outer,
               uint64_t row_stride_bytes);
+// Status words, on the current GPU, of products that have no context: those of gemm.cu, and the 4-bit ones.
+int gemm_status_word(int** word);
+int gemm4_status_word(int** word);
 // Codes of a 4-bit operand: boxes of 128 bytes x box_rows rows, 128-byte swizzle; zero fill out of bounds.
 int make_tmap_fp4(CUtensorMap* map, const void* base, uint64_t row_bytes, uint64_t rows, uint64_t row_stride, uint32_t box_rows);
 // Its block scales, tiles of 512 bytes as 4 rows of 128: [groups of 128 operand rows][4 x tiles of a group][128], no swizzle.

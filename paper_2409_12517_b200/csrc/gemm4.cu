@@ -22,7 +22,7 @@
 // meanwhile.  The output leaves through shared memory in bulk stores (8192 x 8192 x 256: 49 us with stores of 32 bytes a lane, 26).
 // Others: single CTAs, two to an SM, on one 128 x 16 .. 128 tile each; with few tiles the contraction is cut among the 2, 4 or 8
 // CTAs of a cluster, which add their shares over distributed shared memory in the order of their ranks.
-// Every wait is bounded.
+// Every wait is bounded; one that gives up raises the status word of products without a context.
 #include "gemm.cuh"
 
 #include <mutex>
@@ -37,6 +37,7 @@ constexpr int kStepK = 64;                   // and per MMA
 constexpr int kScaleTile = 512;              // 128 rows x 4 blocks
 constexpr uint32_t kAll = 0xffffffffu;
 constexpr int kOtherWarps = 3;               // two TMA producers, the MMA issuer
+__device__ int wait_status;                  // status word of these products, which have no context: a wait gave up
 
 struct Gemm4Args {
     int P, Q, K;
@@ -421,7 +422,7 @@ gemm4_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_constant__ CU
             tile4_coords<PAIR>(p, tile, p_tile, q_tile);
             for (uint32_t n = warp; n < total; n += 2, kb += 2) {
                 const uint32_t stage = n % kStages, parity = (n / kStages) & 1u;
-                if (!mbar_wait(smem_u32(&tail->empty[stage]), parity ^ 1u, abort_flag, nullptr)) break;
+                if (!mbar_wait(smem_u32(&tail->empty[stage]), parity ^ 1u, abort_flag, &wait_status)) break;
                 if (!PAIR || rank == 0) mbar_expect_tx(smem_u32(&tail->full[stage]), (PAIR ? 2 : 1) * kStageBytes);      // a pair's bytes are counted by rank 0
                 while (kb >= kb_end) { kb -= per_tile; tile += tile_step; tile4_coords<PAIR>(p, tile, p_tile, q_tile); }
                 const int p_group = PAIR ? 2 * p_tile + static_cast<int>(rank) : p_tile, p0 = p_group * kRows;
@@ -451,14 +452,14 @@ gemm4_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_constant__ CU
             for (int tile = first_tile; ok && tile < num_tiles; tile += tile_step, ++it) {
                 int p_tile, q_tile;
                 tile4_coords<PAIR>(p, tile, p_tile, q_tile);
-                if (!__all_sync(kAll, mbar_wait(smem_u32(&tail->tmem_empty), (it & 1) ^ 1u, abort_flag, nullptr))) break;
+                if (!__all_sync(kAll, mbar_wait(smem_u32(&tail->tmem_empty), (it & 1) ^ 1u, abort_flag, &wait_status))) break;
                 tc_fence_after();
                 // first column of the tile's scales; the MMA takes them from even columns only, so that tiles narrower than 64 are
                 // for products with one such tile
                 const uint32_t q_offset = TN >= 64 ? static_cast<uint32_t>((q_tile * TN) % kRows) / 32u : 0u;
                 for (int kb = kb_begin; kb < kb_end; ++kb) {
                     if (!ready) {
-                        ok = __all_sync(kAll, mbar_wait(smem_u32(&tail->full[ring.stage]), ring.phase, abort_flag, nullptr));
+                        ok = __all_sync(kAll, mbar_wait(smem_u32(&tail->full[ring.stage]), ring.phase, abort_flag, &wait_status));
                         if (!ok) break;
                     }
                     tc_fence_after();
@@ -482,7 +483,7 @@ gemm4_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_constant__ CU
             }
             if constexpr (!PAIR) {
                 // the accumulator has been read: tensor memory is given back while the output is on its way (1 x 4096 x 1024: 4.0 -> 3.2 us)
-                if (ok && __all_sync(kAll, mbar_wait(smem_u32(&tail->tmem_empty), 0u, abort_flag, nullptr))) {
+                if (ok && __all_sync(kAll, mbar_wait(smem_u32(&tail->tmem_empty), 0u, abort_flag, &wait_status))) {
                     tc_fence_after();
                     tmem_dealloc(tmem_base, S::kTmem);
                     freed = true;
@@ -501,7 +502,7 @@ gemm4_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_constant__ CU
         for (int tile = first_tile; tile < num_tiles; tile += tile_step, ++it) {
             int p_tile, q_tile;
             tile4_coords<PAIR>(p, tile, p_tile, q_tile);
-            const bool got = mbar_wait(smem_u32(&tail->tmem_full), it & 1, abort_flag, nullptr);
+            const bool got = mbar_wait(smem_u32(&tail->tmem_full), it & 1, abort_flag, &wait_status);
             if (!__all_sync(kAll, got)) break;
             tc_fence_after();
             const uint32_t taddr = tmem_base + part * S::kWarpCols + (static_cast<uint32_t>(quad * 32) << 16);
@@ -600,6 +601,9 @@ gemm4_kernel(const __grid_constant__ CUtensorMap tmP, const __grid_constant__ CU
     if (*abort_flag) {
         for (int i = 0; i < 200; ++i) __nanosleep(1000);      // copies in flight land before shared memory is released
         __syncthreads();
+        if (!PAIR && p.split > 1)                             // a share that is not there is NaN, and so is the tile
+            for (int i = threadIdx.x; i < max(TN * (kRows + 4), kRows * (TN + 4)); i += S::kThreads)
+                reinterpret_cast<float*>(smem_raw + (tiles_addr - raw_addr))[i] = __uint_as_float(0x7fffffffu);
     }
     if (!PAIR && p.split > 1) {
         cluster_sync_all();                                   // all shares of the tile lie in their CTAs' shared memory
@@ -741,6 +745,12 @@ int dispatch4(const Plan4& pl, const CUtensorMap (&tm)[5], const Gemm4Args& a, i
 }
 
 }  // namespace
+
+int gemm4_status_word(int** word) {
+    FP8MLP_CUDA_CHECK(cudaGetSymbolAddress(reinterpret_cast<void**>(word), wait_status));
+    return FP8MLP_OK;
+}
+
 }  // namespace fp8mlp
 
 using namespace fp8mlp;

@@ -34,3 +34,25 @@ def test_bounded_wait_gives_up_reports_timeout_and_leaves_the_context_usable():
             B.fp8mlp_selftest_wait_timeout(ctx, 0)                 # limit out of range: refused before any launch
     finally:
         B.fp8mlp_destroy(ctx)
+
+
+def test_products_without_a_context_report_a_wait_that_gave_up():
+    """Their word is the library's: reported and cleared once, apart from any context's, and products go on."""
+    ctx = B.fp8mlp_create(16, 64, 64, 0)
+    try:
+        assert B.fp8mlp_status(None) == B.OK
+        B.fp8mlp_selftest_wait_timeout(None, 20000)
+        assert B.fp8mlp_status(ctx) == B.OK
+        assert B.fp8mlp_status(None) == B.ERR_TIMEOUT
+        assert B.fp8mlp_status(None) == B.OK
+        B.fp8mlp_selftest_wait_timeout(ctx, 20000)
+        assert B.fp8mlp_status(None) == B.OK and B.fp8mlp_status(ctx) == B.ERR_TIMEOUT
+        a, out = B.new_fp4(B.MXFP4, 300, 4096), torch.empty(300, 300, device="cuda")
+        B.fp8mlp_quantize_fp4(torch.ones(300, 4096, device="cuda"), a)
+        B.fp8mlp_gemm_fp4(a, a, out)
+        assert (out == 4096).all()
+        codes = torch.full((64, 128), 0x38, dtype=torch.uint8, device="cuda")             # 1 in E4M3
+        B.fp8mlp_gemm_fp8(64, 64, 128, codes, True, B.E4M3, codes, True, B.E4M3, None, None, out[:64, :64].contiguous())
+        assert B.fp8mlp_status(None) == B.OK
+    finally:
+        B.fp8mlp_destroy(ctx)
