@@ -472,8 +472,8 @@ FP8MLP_API int fp8mlp_gemm_bf16(int64_t M, int64_t N, int64_t K, const void* A, 
  *                         zero or not finite, or where 448 / max_i |h[t, i] gain[i]| leaves fp32)
  * Codes are rounded once: they are those next to the exact value of the formula (its 1 / rms within six roundings of fp32).
  * scale is not used by FP8MLP_RMS_SAME.  amax (nullable, not with FP8MLP_RMS_E4M3_ROWS): receives max |y| of this call (before
- * any cast).  rstd (nullable): fp32 [T], for the backward pass.  With y = a context's FP8MLP_WS_XQ buffer (ld_y = d), scales.x
- * and amax.x the codes are the block's own operand: fp8mlp_forward with FP8MLP_SCALE_GIVEN_X_CAST does not read x again.
+ * any cast).  rstd (nullable): fp32 [T], for the backward pass.  With y = a context's FP8MLP_WS_XQ buffer (ld_y = d, T at most
+ * the context's T_max), scales.x and amax.x the codes are the block's own operand: fp8mlp_forward with FP8MLP_SCALE_GIVEN_X_CAST does not read x again.
  * d a multiple of 16, at most FP8MLP_MAX_NORM_WIDTH; row strides in elements, at least d, of 16 bytes' multiples; all rows and
  * gain start on 16-byte boundaries.  A row that holds a NaN or an infinity, or whose sum of squares leaves fp32 (elements around
  * 2^64), has no norm: rstd is NaN or 0, and y what the formulas make of that; a row of zeros is zeros if eps > 0. */

@@ -227,11 +227,25 @@ def fp8mlp_selftest_wait_timeout(ctx: int | None, timeout_us: int) -> None:
     _check(lib().fp8mlp_selftest_wait_timeout(C.c_void_p(ctx), timeout_us, _stream()), "fp8mlp_selftest_wait_timeout")
 
 
+class WorkspacePointer(int):
+    """Address of a context's buffer that knows how many bytes there are from it on."""
+    nbytes: int
+
+    def __new__(cls, address: int, nbytes: int):
+        p = super().__new__(cls, address)
+        p.nbytes = nbytes
+        return p
+
+    def __add__(self, offset: int):
+        """The address so many bytes on, as one that knows its size; outside the buffer, a plain number."""
+        return WorkspacePointer(int(self) + offset, self.nbytes - offset) if 0 <= offset <= self.nbytes else int(self) + offset
+
+
 def fp8mlp_workspace(ctx: int, which: int):
-    """(device pointer, bytes) of one of the WS_* buffers."""
+    """(device pointer, bytes) of one of the WS_* buffers; the pointer is a WorkspacePointer."""
     p, n = C.c_void_p(), C.c_int64()
     _check(lib().fp8mlp_workspace(C.c_void_p(ctx), which, C.byref(p), C.byref(n)), "fp8mlp_workspace")
-    return p.value, n.value
+    return WorkspacePointer(p.value or 0, n.value), n.value
 
 
 def fp8mlp_profile_enable(ctx: int, on: bool) -> None:
@@ -555,7 +569,7 @@ def _floats(t, numel, what, here):
 def fp8mlp_rmsnorm(x, residual, gain, eps: float, y, h=None, out: int = RMS_SAME, scale=None, amax=None, rstd=None) -> None:
     """h = x + residual, y = h / rms(h) * gain.  x, residual, h: [T, d] bf16 or fp32, any row stride; residual, gain (fp32
     [d]), h, amax (1-element fp32) and rstd (fp32 [T]) may be None; h may be x or residual, in the same rows.  y by `out`: RMS_SAME: [T, d] of
-    x's type; RMS_E4M3: codes (uint8 [T, d], or a device pointer as int, e.g. a context's WS_XQ, with rows of d bytes) of
+    x's type; RMS_E4M3: codes (uint8 [T, d], or a context's buffer by its WorkspacePointer, WS_XQ with rows of d bytes) of
     y * scale (1-element fp32, read); RMS_E4M3_ROWS: codes, scale (fp32 [T]) is written."""
     here = _here()
     shape, dtype = x.shape, x.dtype
@@ -579,10 +593,13 @@ def fp8mlp_rmsnorm(x, residual, gain, eps: float, y, h=None, out: int = RMS_SAME
         h_ptr, ld_h = h.data_ptr(), d
     else:
         h_ptr, ld_h = _rows_like(h, shape, dtype, "h", here)
-    if out == RMS_SAME:
-        y_ptr, ld_y = _rows_like(y, shape, dtype, "y", here)
-    elif isinstance(y, int):
+    if isinstance(y, int):
+        if out == RMS_SAME or not isinstance(y, WorkspacePointer) or T * d > y.nbytes:
+            raise ValueError(f"y: {T * d} bytes of codes go to a uint8 tensor or to a context's buffer of that size (the pointer from "
+                             f"fp8mlp_workspace), got {f'{y.nbytes} bytes' if isinstance(y, WorkspacePointer) else 'a bare address'}")
         y_ptr, ld_y = y, d
+    elif out == RMS_SAME:
+        y_ptr, ld_y = _rows_like(y, shape, dtype, "y", here)
     elif y.dtype is _U8 and y.shape == shape and y.is_contiguous() and y.get_device() == here:
         y_ptr, ld_y = y.data_ptr(), d
     else:

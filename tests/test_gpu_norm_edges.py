@@ -96,3 +96,25 @@ def test_codes_of_products_below_the_normal_numbers(dtype):
     B.fp8mlp_rmsnorm(x.cuda(), None, gain.cuda(), 1.0, y, out=B.RMS_E4M3_ROWS, scale=own)
     # the largest h gain, about 2^-118, is known to the smallest number, half of 2^-149
     assert between(y, want * (448.0 / want.abs().amax(-1, keepdim=True)), 2.0 ** -30)
+
+
+def test_codes_stay_inside_a_context_s_buffer():
+    """More rows than the context has room for, rows from an offset on, and addresses whose size nobody knows are refused by the call."""
+    T, d = 24, 64
+    ctx = B.fp8mlp_create(T, d, 64, 0)
+    try:
+        ptr, nbytes = B.fp8mlp_workspace(ctx, B.WS_XQ)
+        assert ptr.nbytes == nbytes == T * d and (ptr + 3 * d).nbytes == (T - 3) * d
+        x, scale = torch.randn(T + 1, d, device="cuda"), torch.full((1,), 50.0, device="cuda")
+        whole = torch.empty(T, d, dtype=torch.uint8, device="cuda")
+        B.fp8mlp_rmsnorm(x[:T], None, None, 1e-5, whole, out=B.RMS_E4M3, scale=scale)
+        B.fp8mlp_rmsnorm(x[:5], None, None, 1e-5, ptr, out=B.RMS_E4M3, scale=scale)
+        B.fp8mlp_rmsnorm(x[5:T], None, None, 1e-5, ptr + 5 * d, out=B.RMS_E4M3, scale=scale)
+        assert torch.equal(B.workspace_tensor(ctx, B.WS_XQ, (T, d), torch.uint8), whole)
+        for rows, y, out in ((T + 1, ptr, B.RMS_E4M3), (T, ptr + d, B.RMS_E4M3), (T, int(ptr), B.RMS_E4M3), (T, ptr + (T * d + 16), B.RMS_E4M3),
+                             (1, ptr - d, B.RMS_E4M3), (1, ptr, B.RMS_SAME)):
+            with pytest.raises(ValueError, match="codes go to"):
+                B.fp8mlp_rmsnorm(x[:rows], None, None, 1e-5, y, out=out, scale=scale)
+        assert torch.equal(B.workspace_tensor(ctx, B.WS_XQ, (T, d), torch.uint8), whole)
+    finally:
+        B.fp8mlp_destroy(ctx)
