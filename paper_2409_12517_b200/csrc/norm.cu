@@ -608,16 +608,17 @@ cudaError_t launch_norm_backward(const NormBackArgs& a, size_t smem, dim3 grid, 
     return launch_rows(norm_backward_kernel<SRC, BLOCK, NU, WIDE>, a.d_gain != nullptr, grid, BLOCK, smem, st, a);
 }
 
-// the instantiation for a shape: F<SRC, BLOCK, NU, WIDE>
+// the instantiation for a shape: F<SRC, BLOCK, NU, WIDE>; a row of bf16 has half as many units as one of fp32
+template <typename SRC> constexpr int kMostUnits = FP8MLP_MAX_NORM_WIDTH / Unit<SRC>::kElems;
 #define FP8MLP_NORM_TYPES(PICK, F, ...)                                                                                   \
     (dtype == FP8MLP_F32 ? (wide ? PICK(F, float, true, __VA_ARGS__) : PICK(F, float, false, __VA_ARGS__))                 \
                          : (wide ? PICK(F, uint16_t, true, __VA_ARGS__) : PICK(F, uint16_t, false, __VA_ARGS__)))
 #define FP8MLP_NORM_FORWARD(F, SRC, WIDE, ...)                                                                            \
     (s.block == 256 ? F<SRC, 256, 1, WIDE>(__VA_ARGS__) : s.block == 512 ? F<SRC, 512, 1, WIDE>(__VA_ARGS__)               \
-     : s.nu == 1 ? F<SRC, 1024, 1, WIDE>(__VA_ARGS__) : F<SRC, 1024, 2, WIDE>(__VA_ARGS__))
+     : s.nu == 1 ? F<SRC, 1024, 1, WIDE>(__VA_ARGS__) : F<SRC, 1024, kMostUnits<SRC> / 1024, WIDE>(__VA_ARGS__))
 #define FP8MLP_NORM_BACKWARD(F, SRC, WIDE, ...)                                                                           \
     (s.block == 256 ? F<SRC, 256, 1, WIDE>(__VA_ARGS__) : s.nu == 1 ? F<SRC, 512, 1, WIDE>(__VA_ARGS__)                    \
-     : s.nu == 2 ? F<SRC, 512, 2, WIDE>(__VA_ARGS__) : F<SRC, 512, 4, WIDE>(__VA_ARGS__))
+     : s.nu == 2 ? F<SRC, 512, 2, WIDE>(__VA_ARGS__) : F<SRC, 512, kMostUnits<SRC> / 512, WIDE>(__VA_ARGS__))
 
 }  // namespace
 
