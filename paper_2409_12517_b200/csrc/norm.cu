@@ -271,19 +271,24 @@ __global__ void __launch_bounds__(BLOCK, 1024 / BLOCK) norm_kernel(const NormArg
         over_row<kRows, kLean>(sum, lean_sum, top, top_rest, p.tpr, part[parity]);
         float rstd, factor, factor_rest = 0.0f;             // the factor of codes, and what its rounding left off
         if constexpr (kCodes) {
-            // (1 / rms of a mean below 2^-100 may have no square in fp32: that of 2^200 times the mean is taken, and 2^100 times it)
-            const double plain = sum * p.inv_d64 + static_cast<double>(p.eps);
-            const bool tiny = plain < 0x1p-100;
-            const double mean = tiny ? plain * 0x1p200 : plain;
-            const float m = static_cast<float>(mean);
-            rstd = __fdiv_rn(1.0f, __fsqrt_rn(m));
             // one step of Newton's method for 1 / sqrt(mean), its residual 1 - mean rstd^2 with what the roundings of both left off
-            float step = 0.0f;
-            if (rstd > 0.0f && !isinf(rstd)) {
-                const float square = __fmul_rn(rstd, rstd), square_rest = __fmaf_rn(rstd, rstd, -square), m_rest = static_cast<float>(mean - static_cast<double>(m));
-                step = __fmul_rn(__fmul_rn(0.5f, rstd), __fmaf_rn(-m_rest, square, __fmaf_rn(-m, square_rest, __fmaf_rn(-m, square, 1.0f))));
+            float step;
+            auto inverse_root = [&](double mean) {
+                const float m = static_cast<float>(mean);
+                rstd = __fdiv_rn(1.0f, __fsqrt_rn(m));
+                step = 0.0f;
+                if (rstd > 0.0f && !isinf(rstd)) {
+                    const float square = __fmul_rn(rstd, rstd), square_rest = __fmaf_rn(rstd, rstd, -square), m_rest = static_cast<float>(mean - static_cast<double>(m));
+                    step = __fmul_rn(__fmul_rn(0.5f, rstd), __fmaf_rn(-m_rest, square, __fmaf_rn(-m, square_rest, __fmaf_rn(-m, square, 1.0f))));
+                }
+            };
+            const double mean = sum * p.inv_d64 + static_cast<double>(p.eps);
+            inverse_root(mean);
+            if (rstd > 0x1p50f) {                           // its square may leave fp32, or the mean: of 2^200 times the mean
+                inverse_root(mean * 0x1p200);
+                rstd = __fmul_rn(rstd, 0x1p100f);
+                step = __fmul_rn(step, 0x1p100f);
             }
-            if (tiny) { rstd = __fmul_rn(rstd, 0x1p100f); step = __fmul_rn(step, 0x1p100f); }
             // y = (h gain) factor
             factor = __fmul_rn(rstd, scale);
             factor_rest = __fmaf_rn(step, scale, __fmaf_rn(rstd, scale, -factor));
