@@ -344,7 +344,7 @@ __global__ void __launch_bounds__(BLOCK, 1024 / BLOCK) norm_kernel(const NormArg
                     differ |= c[i] ^ cvt_fp8x4<FP8MLP_E4M3>(lo[0], lo[1], lo[2], lo[3]);
                 }
                 // (a factor beyond these may bring h gain back from where fp32 has few bits, or none)
-                if (differ != 0 || factor > 0x1p60f || factor < 0x1p-60f) {
+                if (differ != 0 || fabsf(factor) > 0x1p60f || fabsf(factor) < 0x1p-60f) {
                     const double exact = static_cast<double>(factor) + static_cast<double>(isnan(factor_rest) ? 0.0f : factor_rest);
 #pragma unroll
                     for (int i = 0; i < E / 4; ++i)
