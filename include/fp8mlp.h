@@ -464,19 +464,24 @@ FP8MLP_API int fp8mlp_gemm_bf16(int64_t M, int64_t N, int64_t K, const void* A, 
  *   y[t, i] = h[t, i] * rstd[t] * gain[i],               rstd[t] = 1 / sqrt(mean_i h[t, i]^2 + eps)
  * x, residual, h: T rows of d elements of one type (FP8MLP_BF16 or FP8MLP_F32) with a row stride each; gain fp32 [d], null = 1.
  * h is rounded to that type once, and the norm is that of the rounded values: the gradient of what was computed follows from
- * the stored h.  Squares are summed in fp32.  h_out receives h (null: not wanted; needs a residual); it may be x or the
+ * the stored h.  Squares are summed in fp32, for codes in fp32 within a warp (bf16 rows above 512 elements) or in 64 bits throughout
+ * (fp32 rows, bf16 ones up to 512 whose squares are added by fours).  h_out receives h (null: not wanted; needs a residual); it may be x or the
  * residual itself, with the same row stride; no other outputs overlap inputs or one another.  out_kind:
  *   FP8MLP_RMS_SAME       y in the type of x
  *   FP8MLP_RMS_E4M3       y: E4M3 codes Q(y * *scale), `scale` one device float that is read (delayed scaling)
  *   FP8MLP_RMS_E4M3_ROWS  y: E4M3 codes Q(y * scale[t]), scale fp32 [T] written: 448 / max_i |y[t, i]| (1 where that maximum is
- *                         zero or not finite, or where 448 / max_i |h[t, i] gain[i]| leaves fp32)
- * Codes are rounded once: they are those next to the exact value of the formula (its 1 / rms within six roundings of fp32).
+ *                         zero or not finite, or where 448 / max_i |h[t, i] gain[i]| leaves fp32).  For a product of the caller's with
+ *                         a scale per row: this library's block and products take one scale for the tensor
+ * Codes are rounded once: they are those next to the exact value of the formula (its 1 / rms within six roundings of fp32, as long as
+ * the squares are normal numbers; a row's own scale within 2^-30; 1 / rms times *scale has to lie in fp32's range).
  * scale is not used by FP8MLP_RMS_SAME.  amax (nullable, not with FP8MLP_RMS_E4M3_ROWS): receives max |y| of this call (before
- * any cast).  rstd (nullable): fp32 [T], for the backward pass.  With y = a context's FP8MLP_WS_XQ buffer (ld_y = d, T at most
+ * any cast), rows without a norm (NaN) left out.  rstd (nullable): fp32 [T], for the backward pass.  With y = a context's FP8MLP_WS_XQ buffer (ld_y = d, T at most
  * the context's T_max), scales.x and amax.x the codes are the block's own operand: fp8mlp_forward with FP8MLP_SCALE_GIVEN_X_CAST does not read x again.
  * d a multiple of 16, at most FP8MLP_MAX_NORM_WIDTH; row strides in elements, at least d, of 16 bytes' multiples; all rows and
  * gain start on 16-byte boundaries.  A row that holds a NaN or an infinity, or whose sum of squares leaves fp32 (elements around
- * 2^64), has no norm: rstd is NaN or 0, and y what the formulas make of that; a row of zeros is zeros if eps > 0. */
+ * 2^64), has no norm: rstd is NaN or 0, and y what the formulas make of that; a row of zeros is zeros if eps > 0.  Without eps, a row
+ * whose sum of squares is zero in the precision of the sum (elements below 2^-75 in fp32), or whose 1 / rms leaves fp32, has rstd
+ * infinite. */
 enum { FP8MLP_RMS_SAME = 0, FP8MLP_RMS_E4M3 = 1, FP8MLP_RMS_E4M3_ROWS = 2 };
 #define FP8MLP_MAX_NORM_WIDTH 16384
 FP8MLP_API int fp8mlp_rmsnorm(int64_t T, int64_t d, int dtype, const void* x, int64_t ld_x, const void* residual,
@@ -530,6 +535,7 @@ FP8MLP_API int fp8mlp_dequantize_fp4(const uint8_t* codes, int64_t ld_codes, con
  *   out[m, n] = (sum_k A(m, k) B(n, k)) * ((1 / *scale_a) * (1 / *scale_b)),   fp32 accumulation, out bf16 or fp32
  * A [M, K], B [N, K]: codes and block scales as above; scale_a, scale_b null = 1 (always null for MXFP4).  out: row stride
  * ld_out >= N elements, aligned to its type, overlaps no operand.  M = 0 or N = 0: nothing to do.  K >= 1, any; M, N, K <= 2^24.
+ * The product of both reciprocals is taken first, in fp32: scales of which it leaves the range give zeros, or infinities and NaN.
  * A layer y = x W^T is trained with it as y = Q(x) Q(W)^T, dx = Q(dy) Q(W^T)^T, dW = Q(dy^T) Q(x^T)^T. */
 FP8MLP_API int fp8mlp_gemm_fp4(int64_t M, int64_t N, int64_t K, int fp4_fmt, const uint8_t* A, int64_t ld_a, const uint8_t* a_scales,
                                const float* scale_a, const uint8_t* B, int64_t ld_b, const uint8_t* b_scales, const float* scale_b,

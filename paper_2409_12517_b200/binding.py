@@ -658,7 +658,7 @@ def _bytes(t, rows, cols, what, here):
 
 class Fp4Operand:
     """A [rows, cols] matrix in 4 bits, its columns the contraction of a product: codes (uint8 [rows, at least cols / 2 rounded
-    up to 16], any row stride), block scales (uint8, fp8mlp_fp4_scale_bytes) and, for NVFP4, the tensor's scale (1-element fp32,
+    up to 16], a row stride that is a multiple of 16), block scales (uint8, fp8mlp_fp4_scale_bytes) and, for NVFP4, the tensor's scale (1-element fp32,
     None = 1).  Marshalled once: it holds the tensors and their addresses; what is in them is read anew by every call."""
 
     def __init__(self, fmt: int, rows: int, cols: int, codes, scales, scale=None, amax=None):

@@ -692,8 +692,8 @@ __global__ void __launch_bounds__(kThreads, 4) dequantise_narrow_kernel(const De
 // ---------------------------------------------------------------- host side
 bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 constexpr int64_t kMost = int64_t(1) << 24;      // rows and columns
-// One launch instead of three (its call 5.8 us, theirs 9.6) up to where 16 SMs take longer for the data: 256 x 1024 bf16 4.9 and 5.0 us
-// on the device, 512 x 1024 7.4 and 4.9.
+// One launch instead of three (its call 5.5 us, theirs 9.4) up to where 16 SMs take longer for the data: 256 x 1024 bf16 4.8 us on the
+// device either way, 512 x 1024 7.4 and 4.9.
 constexpr int64_t kSmallBytes = int64_t(512) << 10, kSmallTiles = 2 * kCluster;
 
 constexpr unsigned int kLittleShared = 8;        // percent
@@ -711,7 +711,7 @@ cudaError_t launch_quantise(const QuantArgs& a, bool transpose, dim3 grid, cudaS
                                  : launch_chained(quantise_kernel<SRC, FMT, true, false>, grid, dim3(kThreads), 0, st, a);
     if (!vec_rows<SRC>(a.src, a.ld, a.cols)) return launch_chained(quantise_kernel<SRC, FMT, false, false>, grid, dim3(kThreads), 0, st, a);
     // behind the search for the maximum the SMs are divided nearly as needed, and asking again costs 4 us of blocks not set up early:
-    // worth it for large matrices only (1531 x 512 fp32 6.0 us, asking again 10; 11008 x 4096 fp32 64 and 57; 4096 x 4096 26.2 and 24.7)
+    // worth it for large matrices only (1531 x 512 fp32 6.0 us, asking again 9.7; 4096 x 4096 29.5 and 27.2; 11008 x 4096 70 and 62.6)
     const bool divided = a.amax_in != nullptr && a.rows * a.cols * static_cast<int64_t>(sizeof(SRC)) < (int64_t(64) << 20);
     return divided ? launch_chained(quantise_kernel<SRC, FMT, false, true>, grid, dim3(kThreads), 0, st, a)
                    : launch_chained_shared(kLittleShared, quantise_kernel<SRC, FMT, false, true>, grid, dim3(kThreads), 0, st, a);

@@ -270,7 +270,8 @@ __device__ __forceinline__ uint32_t shared_word(uint32_t at) {
 }
 
 // Rows on any boundary, `rows` x `cols` of the block inside the matrix: each row is written by neighbouring lanes, in words of four
-// bytes (16384 x 1411 bf16 with a row per lane, element by element: 234 us; this way 74, with write_wide 39).
+// bytes (16384 x 1411 bf16 with a row per lane, element by element: 234 us; this way 74, with write_wide 39; behind large products,
+// when power holds the clock down, 48 to 52).
 __device__ __forceinline__ void write_rows(const Gemm4Args& p, uint32_t stage, int lane, int row, int col, int rows, int cols,
                                            const float (&v)[32]) {
     if (lane == 0) tma_store_wait_read<0>();
@@ -706,13 +707,13 @@ int launch4(const CUtensorMap (&tm)[5], const Gemm4Args& a, int sm_count, cudaSt
 struct Plan4 { bool pair, swap; int tn, split; };
 
 // How a product runs, by what was measured on 148 SMs (NVFP4, bf16 out; us in a chain of launches).
-// CTA pairs on 256 x 256 tiles, where at least half of the SMs get one (1536 x 2048 x 4096, 48 pairs: 11.4, single CTAs 14.0;
-// 1500 x 1500 x 4096, 36 pairs: 15.1 and 12.0).  Otherwise single CTAs: their 128 rows are of the longer side where the other one has
+// CTA pairs on 256 x 256 tiles, where at least half of the SMs get one (1536 x 2048 x 4096, 48 pairs: 11.2, single CTAs 14.2;
+// 1500 x 1500 x 4096, 36 pairs: 14.8 and 11.3).  Otherwise single CTAs: their 128 rows are of the longer side where the other one has
 // at most 128, by as many columns as that one needs; with more than 64 of them, tiles 64 wide as long as all are on the SMs at once
-// (1024 x 1024 x 1024: 4.7, 128 wide 6.1; 512 x 8192 x 1024, 512 tiles: 11.0 and 8.5).  The contraction is split where it has 8 stages
-// or more (1 x 4096 x 4096, 16 stages: 6.5 -> 5.8 with 4 shares; 1 x 4096 x 1024, 4 stages: 4.0 -> 4.8 with 2), into shares of at least
-// 2 stages, for as many CTAs as there are SMs (256 x 4096 x 4096, 128 tiles: 9.3 whole, 10.6 with 2 shares), or twice as many
-// where a share still has 16 stages (1 x 11008 x 11008, 86 tiles: 18.1 -> 15.9).
+// (1024 x 1024 x 1024: 4.3, 128 wide 6.1; 512 x 8192 x 1024, 512 tiles: 10.1 and 8.9).  The contraction is split where it has 8 stages
+// or more (1 x 4096 x 4096, 16 stages: 5.7 -> 5.1 with 4 shares; 1 x 4096 x 1024, 4 stages: 3.3 -> 4.2 with 2), into shares of at least
+// 2 stages, for as many CTAs as there are SMs (256 x 4096 x 4096, 128 tiles: 8.2 whole, 9.9 with 2 shares), or twice as many
+// where a share still has 16 stages (1 x 11008 x 11008, 86 tiles: 17.5 -> 15.6).
 Plan4 plan4(int64_t M, int64_t N, int64_t K, int sms) {
     Plan4 pl{};
     const int64_t shorter = M < N ? M : N;

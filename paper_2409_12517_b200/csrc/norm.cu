@@ -182,7 +182,9 @@ __device__ __forceinline__ float for_code(float h, float gain, double factor) {
 // have 16 bits), and the factor has a second fp32 number; a unit's codes are converted from its fp32 values a little increased and a
 // little decreased, and where the two differ its products are taken again in 64 bits (one unit in 5000).
 // Measured, 16384 x 4096 with residual: bf16 to codes 80 us (from fp32 products alone 77; 72 at the copy rate), with a scale per row 81,
-// to bf16 89 (82); fp32 to codes 135 (133).  2048 x 16384 bf16 to codes 44 (36).  What bounds it: DRAM, and the row's chain of reductions.
+// to bf16 88 (82); fp32 to codes 136 (133).  2048 x 16384 bf16 to codes 43 (36), fp32 94 (67: two units a thread, no row ahead).  16384
+// rows of 5120, 6144, 7168 bf16 to codes: 111, 121, 133 (90, 108, 125): a row's threads are a power of two.  One token: 2.9 us, 2.5 from
+// fp32 products.  What bounds it: DRAM, and the row's chain of reductions.  bf16 to codes spills 20 to 32 bytes a thread.
 template <typename SRC, int BLOCK, int NU, bool WIDE, int OUT>
 __global__ void __launch_bounds__(BLOCK, 1024 / BLOCK) norm_kernel(const NormArgs p) {
     constexpr int E = Unit<SRC>::kElems;
@@ -383,6 +385,9 @@ __global__ void __launch_bounds__(BLOCK, 1024 / BLOCK) norm_kernel(const NormArg
 // A thread keeps the columns of its units through all rows of its block and sums their part of d_gain in registers (NU = 1)
 // or in its own words of shared memory; blocks leave one row of partial sums each, which a second kernel
 // adds in their order; a cluster that has the whole batch adds them over distributed shared memory.
+// Measured with the residual stream's gradient, 16384 x 4096: bf16 88.7 us (82 at the copy rate), fp32 209 (164).  NU > 1: 2048 x 16384
+// bf16 89 (41), fp32 160 (82), 4096 x 8192 fp32 119 (82): by count, lanes' words of shared memory share banks (8 or 16 to one);
+// no row is fetched ahead, and four units of fp32 spill 332 bytes.  16384 rows of 5120, 6144, 7168 bf16: 143, 152, 165 (102, 123, 143), one block to an SM.
 template <typename SRC, int BLOCK, int NU, bool WIDE>
 __global__ void __launch_bounds__(BLOCK) norm_backward_kernel(const NormBackArgs p) {
     constexpr int E = Unit<SRC>::kElems;
@@ -563,9 +568,10 @@ RowShape row_shape(int64_t d, int elems, int most) {
 }
 
 // Whether one cluster takes the batch, without a launch before (which clears the maximum) or after it (which adds up the gradient of
-// the gain): two rounds of its blocks take as long on the device as the launch, and a call 2 us less (32 x 4096 bf16, two rounds:
-// forward 4.1 and 3.3 us on the device, 8.2 and 10.1 called, backward 6.0 and 5.6, 7.8 and 9.8; 64 x 4096, four rounds: 5.6 and 3.3 forward,
-// 7.6 and 5.6 backward).  Wide rows take longer than a launch already in their second round.
+// the gain): a call takes 1.8 us less, which is the host's time (32 x 4096 bf16: forward 6.2 and 8.0 us, backward 7.2 and 9.0).  On the
+// device alone, as a captured graph runs, one round of its blocks takes 3.7 us and two launches 4.1 forward, 5.4 and 4.6 backward; two
+// rounds (32 x 4096) 4.8 and 4.2, 6.2 and 4.9; four (64 x 4096) 6.8 and 4.4, 7.8 and 5.4.  Wide rows take longer than a launch already
+// in their second round.
 bool one_cluster_does(const RowShape& s, int64_t blocks) { return blocks <= (s.nu == 1 ? 2 : 1) * kCluster; }
 
 // a row stride in elements -> bytes; false where it is no multiple of 16 bytes or shorter than the row
